@@ -75,17 +75,17 @@ def draw(rng):
         kv = rng.choice((1, 2, 4, 8))
         heads = kv * rng.choice((1, 2, 4)) if kv < 8 else kv * rng.choice((1, 2))
         if kind == "step":
-            return _attn("step", 1, _log(rng, 1, 8000 // heads), heads, kv, dk, dv, dtype, rng.choice((0.0, 0.02)))
+            return _attn("step", 1, _log(rng, 1, 4000 // heads), heads, kv, dk, dv, dtype, rng.choice((0.0, 0.02)))
         T = _log(rng, 1, 8192 if kind == "fwd" and dtype == "bf16" else 2048)
-        # the rows of all heads, and the T x T products of the plain form, stay below those of the largest listed case
-        most = min((65536 if dtype == "bf16" else 16384) // (T * heads), (1 << 27) // (T * T * heads))
+        # rows and states of all heads, and the T x T products of the plain form, stay below those of the largest listed cases
+        most = min((131072 if dtype == "bf16" else 32768) // T, (1 << 30) // (T * T), 1500) // heads
         return _attn(kind, T, _log(rng, 1, max(1, most)), heads, kv, dk, dv, dtype, rng.choice((0.0, 0.002, 0.02)), rng.random() < 0.7)
     dtype = rng.choice(("bf16", "bf16", "f16", "f32"))
     if kind in ("norm", "norm_bwd"):
         groups = rng.choice((1, 2, 3, 4, 8, 16, 32))
         HW = 1 if rng.random() < 0.25 else _log(rng, 2, 19200)
         C = groups * rng.choice((8, 16, 24, 32, 64) if HW < 4 else (2, 4, 6, 8, 16, 24, 32, 64))
-        return _norm(kind, max(1, _log(rng, 1, max(1, 32000000 // (HW * C)))), HW, C, groups, rng.choice(_ACTS), dtype)
+        return _norm(kind, max(1, _log(rng, 1, max(1, 64000000 // (HW * C)))), HW, C, groups, rng.choice(_ACTS), dtype)
     vocab = _log(rng, 2, 160000)
     rows = _log(rng, 1, max(1, min(16384, 60000000 // vocab)))
     if kind == "logp":
