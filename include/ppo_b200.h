@@ -381,6 +381,118 @@ int ppo_policy_step(ppo_model *m, const ppo_minibatch *obs, int rows, const uint
  * Errors: t outside [0,T) -> INVALID_ARG; buffer and model shapes (H, W, P, A) differ -> SHAPE. */
 int ppo_policy_act(ppo_model *m, ppo_buffer *buf, int t, const float *dev_eps, void *stream);
 
+/* ----------------------------------------- operators for policies in tokens -- */
+
+/* What a policy that answers in tokens (or other discrete actions), with a memory of constant size, needs beside the network
+ * above; no counterpart in the paper.  They work on bare arrays, keep nothing between calls and take any workspace from the
+ * caller (its size from the query next to each, 0: none needed; the calls write what they read of it; two calls that may
+ * overlap on the GPU need two).  Arrays of 16- and 32-bit elements need only the alignment of their elements, states and
+ * workspaces 16 bytes.  Element types: */
+enum { PPO_F32 = 0, PPO_BF16 = 1, PPO_F16 = 2 };
+
+/* Linear attention with a decay for each head, over a sequence minibatch as ppo_shuffle_gather_sequences leaves it: T time
+ * steps of Be envs, rows time-major, row = t * Be + e.  Query head h of env e reads key and value head h / (heads /
+ * kv_heads) and keeps a state S [dk][dv]; with lambda = decay[h] and S_{-1} the state that came in,
+ *   S_t = lambda S'_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t,   S'_t = S_t, or zeros where done[t] is set (S'_{-1} = S_{-1})
+ * and S'_{T-1} is the state the step after the sequence starts from.
+ *   q [T*Be][heads][dk], k [T*Be][kv_heads][dk], v [T*Be][kv_heads][dv], o [T*Be][heads][dv] of type dtype (PPO_F32 or
+ *   PPO_BF16); ldq, ldk, ldv, ldo: elements from one row to the next, so that a row may be part of a wider one (at least
+ *   the row's own length); decay fp32 [heads], in [0, 1], a constant of the call as gamma and lambda are of ppo_compute_gae;
+ *   done uint8 [T][Be] (NULL: no flag is set); states fp32 [Be][heads][dk][dv] (in NULL: zeros; out NULL: not wanted).
+ * Sums and states are held in fp32.  1 <= dk, dv <= 128. */
+typedef struct {
+    int32_t T, Be, heads, kv_heads, dk, dv, dtype;
+    int64_t ldq, ldk, ldv, ldo;
+    float scale;
+} ppo_decay_attention_desc;
+
+size_t ppo_decay_attention_workspace_bytes(const ppo_decay_attention_desc *desc, int backward);
+
+/* o and the state that is left.  dev_state_out may be dev_state_in. */
+int ppo_decay_attention_fwd(const ppo_decay_attention_desc *desc, const void *dev_q, const void *dev_k, const void *dev_v,
+                            const float *dev_decay, const uint8_t *dev_done, const float *dev_state_in, void *dev_o,
+                            float *dev_state_out, void *dev_workspace, size_t ws_bytes, void *stream);
+
+/* Writes the gradients of q, k, v (laid out and strided as these are; key and value heads that are shared receive the sum
+ * over their query heads) and of the state that came in (dev_dstate_in, may be NULL) from the gradients of o (dev_do, strided
+ * as o) and of the state that is left (dev_dstate_out, NULL: zeros).  dev_dstate_in may be dev_dstate_out.  Sums are added in
+ * a fixed order: same bits run to run. */
+int ppo_decay_attention_bwd(const ppo_decay_attention_desc *desc, const void *dev_q, const void *dev_k, const void *dev_v,
+                            const float *dev_decay, const uint8_t *dev_done, const float *dev_state_in, const void *dev_do,
+                            const float *dev_dstate_out, void *dev_dq, void *dev_dk, void *dev_dv, float *dev_dstate_in,
+                            void *dev_workspace, size_t ws_bytes, void *stream);
+
+/* One decision: a sequence of one step (desc->T == 1, else SHAPE) with the state updated in place.  dev_start uint8 [Be]
+ * (NULL: none): envs whose flag is set start from a zero state, whatever their rows of dev_state hold; the flags the env
+ * step before returned as done. */
+int ppo_decay_attention_step(const ppo_decay_attention_desc *desc, const void *dev_q, const void *dev_k, const void *dev_v,
+                             const float *dev_decay, const uint8_t *dev_start, float *dev_state, void *dev_o, void *stream);
+
+/* Group normalisation with an activation, channels last (as the convolutions keep their pixels; with HW == 1 the rows of a
+ * matrix, a group being for instance a head).  x, y of type dtype: B images of HW pixels of C channels, ldx and ldy elements
+ * from one pixel to the next (>= C), HW * ldx from one image to the next.  Over the HW * C / groups values of each image
+ * and group, with the biased variance,
+ *   xhat = (x - mean) / sqrt(var + eps),   y = act(gamma xhat + beta)
+ * gamma, beta fp32 [C] (both NULL: 1 and 0); mean and rstd fp32 [B][groups] receive mean and 1 / sqrt(var + eps).
+ * Statistics and arithmetic in fp32.  y may be x where ldy == ldx. */
+enum { PPO_ACT_NONE = 0, PPO_ACT_RELU = 1, PPO_ACT_SILU = 2 };
+typedef struct {
+    int32_t B, HW, C, groups, act, dtype;
+    int64_t ldx, ldy;
+} ppo_group_norm_desc;
+
+size_t ppo_group_norm_workspace_bytes(const ppo_group_norm_desc *desc, int backward);
+
+int ppo_group_norm_fwd(const ppo_group_norm_desc *desc, float eps, const void *dev_x, const float *dev_gamma, const float *dev_beta,
+                       void *dev_y, float *dev_mean, float *dev_rstd, void *dev_workspace, size_t ws_bytes, void *stream);
+
+/* Gradients from dL/dy (dev_dy, strided as y), x and what the forward pass left in mean and rstd: dev_dx (strided as x; may be
+ * dev_dy where ldx == ldy) is written; dL/dgamma and dL/dbeta fp32 [C] (both NULL: not wanted) are added to (accumulate != 0) or
+ * written.  Sums in a fixed order: same bits run to run.  The derivative of the ReLU at 0 is 0. */
+int ppo_group_norm_bwd(const ppo_group_norm_desc *desc, const void *dev_x, const float *dev_gamma, const float *dev_beta,
+                       const float *dev_mean, const float *dev_rstd, const void *dev_dy, void *dev_dx, float *dev_dgamma,
+                       float *dev_dbeta, int accumulate, void *dev_workspace, size_t ws_bytes, void *stream);
+
+/* Log-probability of each row's token and entropy of each row's distribution, with x = scale * logits:
+ *   logp = x_a - log sum_j exp(x_j),   H = -sum_j p_j log p_j.
+ * logits [rows][vocab] of type dtype, ld elements from one row to the next (>= vocab); dev_tokens int32 [rows]; dev_logp,
+ * dev_entropy fp32 [rows] (the latter may be NULL).  A logit of minus infinity is a token that cannot occur: p = 0, nothing to the
+ * entropy.  A row whose token is outside [0, vocab) is left out (not read; logp = entropy = 0); a row all of whose logits are
+ * minus infinity has logp = minus infinity and entropy 0. */
+typedef struct {
+    int32_t rows, vocab, dtype;
+    int64_t ld;
+    float scale;
+} ppo_token_desc;
+
+int ppo_token_logp(const ppo_token_desc *desc, const void *dev_logits, const int32_t *dev_tokens, float *dev_logp,
+                   float *dev_entropy, void *stream);
+
+/* The clipped policy loss of ppo_loss_fwd_bwd for tokens, with a penalty on the distance from a reference policy, fused with its
+ * gradient.  Per row, logp and H as above, old and ref the log-probabilities of the token under the rollout policy and the
+ * reference (dev_logp_ref NULL: no penalty), w = dev_weight[row] (NULL: 1):
+ *   r = exp(logp - old);  s = min(r Adv, clamp(r, 1 - clip_low, 1 + clip_high) Adv);  d = ref - logp;  kl = exp(d) - d - 1
+ *   L = sum_rows w / B_total (-s + kl_coef kl - ent_coef H)
+ * (at a tie of the min the unclipped branch is taken).  Writes grad_scale * dL/dlogits to dev_dlogits (type dtype, ld_grad elements
+ * from row to row; may be dev_logits where ld_grad == ld; columns behind vocab are left as they are), the log-probabilities to
+ * dev_logp_out [rows] (may be NULL), and writes (accumulate == 0) or adds this call's share of {L_pi = mean(-s), mean(kl),
+ * mean(H), mean(old - logp), mean(r outside the clip range)}, each weighted by w, to dev_loss_out fp32 [5].
+ * Rows of weight 0, rows whose token is outside [0, vocab) and rows without a finite logit are left out: they
+ * contribute nothing, their gradient is 0 and their dev_logp_out 0; of the first two nothing else is read.  grad_scale: 1, or a
+ * loss scale where 16-bit gradients (PPO_F16) would underflow.  dev_workspace: ppo_token_loss_workspace_bytes(desc) bytes.
+ * Sums in a fixed order: same bits run to run. */
+typedef struct {
+    float clip_low, clip_high, kl_coef, ent_coef, grad_scale;
+    int32_t B_total;
+} ppo_token_loss_coef;
+
+size_t ppo_token_loss_workspace_bytes(const ppo_token_desc *desc);
+
+int ppo_token_loss_fwd_bwd(const ppo_token_desc *desc, const ppo_token_loss_coef *coef, const void *dev_logits,
+                           const int32_t *dev_tokens, const float *dev_logp_old, const float *dev_logp_ref, const float *dev_adv,
+                           const float *dev_weight, void *dev_dlogits, int64_t ld_grad, float *dev_logp_out, float *dev_loss_out,
+                           int accumulate, void *dev_workspace, size_t ws_bytes, void *stream);
+
 /* Number of kernels and memsets the library has enqueued in this process so far (all handles, all
  * devices).  Instrumentation for benchmarks that report launches per step; no counterpart in the paper. */
 uint64_t ppo_launch_count(void);

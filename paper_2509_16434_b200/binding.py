@@ -31,6 +31,9 @@ EXPORTS = [
     "ppo_model_sync_masks", "ppo_buffer_write_obs", "ppo_buffer_write_outcome", "ppo_policy_act", "ppo_launch_count",
     "ppo_selftest_wait_timeout", "ppo_buffer_render_depth", "ppo_model_set_sequence", "ppo_shuffle_gather_sequences",
     "ppo_model_read_state", "ppo_state_reset", "ppo_policy_step", "ppo_selftest_first_gradient",
+    "ppo_decay_attention_workspace_bytes", "ppo_decay_attention_fwd", "ppo_decay_attention_bwd", "ppo_decay_attention_step",
+    "ppo_group_norm_workspace_bytes", "ppo_group_norm_fwd", "ppo_group_norm_bwd", "ppo_token_logp",
+    "ppo_token_loss_workspace_bytes", "ppo_token_loss_fwd_bwd",
 ]
 
 
@@ -55,6 +58,23 @@ class Minibatch(C.Structure):
     _fields_ = [("depth_f16", C.c_void_p), ("proprio", C.c_void_p), ("action", C.c_void_p),
                 ("logp_old", C.c_void_p), ("value_old", C.c_void_p), ("adv", C.c_void_p), ("ret", C.c_void_p),
                 ("index", C.c_void_p), ("B", C.c_int32)]
+
+
+class DecayAttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "Be", "heads", "kv_heads", "dk", "dv", "dtype")] + \
+               [(n, C.c_int64) for n in ("ldq", "ldk", "ldv", "ldo")] + [("scale", C.c_float)]
+
+
+class GroupNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "HW", "C", "groups", "act", "dtype")] + [("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
+class TokenDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("ld", C.c_int64), ("scale", C.c_float)]
+
+
+class TokenLossCoef(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("clip_low", "clip_high", "kl_coef", "ent_coef", "grad_scale")] + [("B_total", C.c_int32)]
 
 
 _lib = None
@@ -122,6 +142,20 @@ def lib():
         L.ppo_gae_static.argtypes = [C.c_void_p] * 4 + [C.c_int, C.c_int, C.c_float, C.c_float, C.c_int] + [C.c_void_p] * 4
         L.ppo_model_activation_ptr.argtypes = [C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_void_p),
                                                C.POINTER(C.c_size_t)]
+        L.ppo_decay_attention_workspace_bytes.restype = C.c_size_t
+        L.ppo_decay_attention_workspace_bytes.argtypes = [C.POINTER(DecayAttentionDesc), C.c_int]
+        L.ppo_decay_attention_fwd.argtypes = [C.POINTER(DecayAttentionDesc)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
+        L.ppo_decay_attention_bwd.argtypes = [C.POINTER(DecayAttentionDesc)] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p]
+        L.ppo_decay_attention_step.argtypes = [C.POINTER(DecayAttentionDesc)] + [C.c_void_p] * 8
+        L.ppo_group_norm_workspace_bytes.restype = C.c_size_t
+        L.ppo_group_norm_workspace_bytes.argtypes = [C.POINTER(GroupNormDesc), C.c_int]
+        L.ppo_group_norm_fwd.argtypes = [C.POINTER(GroupNormDesc), C.c_float] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]
+        L.ppo_group_norm_bwd.argtypes = [C.POINTER(GroupNormDesc)] + [C.c_void_p] * 9 + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ppo_token_logp.argtypes = [C.POINTER(TokenDesc)] + [C.c_void_p] * 5
+        L.ppo_token_loss_workspace_bytes.restype = C.c_size_t
+        L.ppo_token_loss_workspace_bytes.argtypes = [C.POINTER(TokenDesc)]
+        L.ppo_token_loss_fwd_bwd.argtypes = [C.POINTER(TokenDesc), C.POINTER(TokenLossCoef)] + [C.c_void_p] * 7 + \
+                                            [C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -445,3 +479,184 @@ def ppo_policy_act(m: Model, buf: Buffer, t: int, eps, stream=None):
 def ppo_policy_sample(m: Model, rows: int, mean, eps, action, logp, stream=None):
     _check(lib().ppo_policy_sample(m.handle, rows, _ptr(mean), _ptr(eps), _ptr(action), _ptr(logp),
                                    _stream(stream)), "ppo_policy_sample")
+
+
+# ------------------------------------------------------------------- operators for policies in tokens --
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ACTS = {"none": 0, "relu": 1, "silu": 2}
+
+
+def _refuse(status: int, where: str, ok: bool):
+    if not ok:
+        raise PpoError(status, where)
+
+
+def _want(where: str, device, *tensors):
+    """(tensor, type, shape) each: what the pointer is taken to be.  None is passed on; other tensors are dense, on the device
+    the call runs on."""
+    for t, dtype, shape in tensors:
+        if t is not None:
+            _refuse(1, where, t.dtype == dtype and t.device == device)
+            _refuse(2, where, t.shape == shape and t.is_contiguous())
+
+
+def _here(where: str, t):
+    _refuse(1, where, t.dtype in _DTYPES and (not t.is_cuda or t.device.index == torch.cuda.current_device()))
+    return t.device
+
+
+def _ld(where: str, t, lead: int) -> int:
+    """Elements from one row to the next of a tensor whose last dimensions make up a row, dense, and whose first `lead` dimensions
+    number the rows in order."""
+    inner = 1
+    for n, st in zip(reversed(t.shape[lead:]), reversed(t.stride()[lead:])):
+        _refuse(2, where, n == 1 or st == inner)
+        inner *= n
+    ld, count = None, 1
+    for n, st in zip(reversed(t.shape[:lead]), reversed(t.stride()[:lead])):
+        if n != 1:
+            ld = st // count if ld is None else ld
+            _refuse(2, where, st == ld * count)
+        count *= n
+    return inner if ld is None else ld
+
+
+def _attention_desc(where: str, q, k, v, o, scale: float, lead: int) -> DecayAttentionDesc:
+    device = _here(where, q)
+    rows = tuple(q.shape[:lead])
+    _refuse(2, where, q.dim() == k.dim() == v.dim() == o.dim() == lead + 2)
+    heads, dk, kv, dv = q.shape[-2], q.shape[-1], k.shape[-2], v.shape[-1]
+    for t, shape in ((k, rows + (kv, dk)), (v, rows + (kv, dv)), (o, rows + (heads, dv))):
+        _refuse(1, where, t.dtype == q.dtype and t.device == device)
+        _refuse(2, where, t.shape == shape)
+    T, Be = rows if lead == 2 else (1,) + rows
+    return DecayAttentionDesc(T, Be, heads, kv, dk, dv, _DTYPES[q.dtype], *(_ld(where, t, lead) for t in (q, k, v, o)), scale)
+
+
+def ppo_decay_attention_workspace_bytes(q, k, v, backward: bool) -> int:
+    """Bytes the calls with these q [T,Be,heads,dk], k [T,Be,kv_heads,dk], v [T,Be,kv_heads,dv] need (0: none)."""
+    T, Be, heads, dk = q.shape
+    d = DecayAttentionDesc(T, Be, heads, k.shape[2], dk, v.shape[3], _DTYPES[q.dtype], heads * dk, k.shape[2] * dk, k.shape[2] * v.shape[3],
+                           heads * v.shape[3], 1.0)
+    return lib().ppo_decay_attention_workspace_bytes(C.byref(d), int(backward))
+
+
+def _bytes_of(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def ppo_decay_attention_fwd(q, k, v, decay, o, done=None, state_in=None, state_out=None, scale: float = 1.0, workspace=None, stream=None):
+    """q [T,Be,heads,dk], k [T,Be,kv_heads,dk], v [T,Be,kv_heads,dv] -> o [T,Be,heads,dv] (fp32 or bf16; rows may be parts of wider
+    ones); decay fp32 [heads]; done uint8 [T,Be]; states fp32 [Be,heads,dk,dv]."""
+    f = "ppo_decay_attention_fwd"
+    d = _attention_desc(f, q, k, v, o, scale, 2)
+    state = (d.Be, d.heads, d.dk, d.dv)
+    _want(f, q.device, (decay, torch.float32, (d.heads,)), (done, torch.uint8, (d.T, d.Be)), (state_in, torch.float32, state),
+          (state_out, torch.float32, state))
+    _check(lib().ppo_decay_attention_fwd(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(decay), _ptr(done), _ptr(state_in), _ptr(o), _ptr(state_out),
+                                         _ptr(workspace), _bytes_of(workspace), _stream(stream)), f)
+
+
+def ppo_decay_attention_bwd(q, k, v, decay, do, dq, dk, dv, done=None, state_in=None, dstate_out=None, dstate_in=None, scale: float = 1.0,
+                            workspace=None, stream=None):
+    """Gradients dq, dk, dv (shaped and strided as q, k, v) and dstate_in from do [T,Be,heads,dv] and dstate_out."""
+    f = "ppo_decay_attention_bwd"
+    d = _attention_desc(f, q, k, v, do, scale, 2)
+    for t, like, ld in ((dq, q, d.ldq), (dk, k, d.ldk), (dv, v, d.ldv)):
+        _refuse(1, f, t.dtype == q.dtype and t.device == q.device)
+        _refuse(2, f, t.shape == like.shape and _ld(f, t, 2) == ld)
+    state = (d.Be, d.heads, d.dk, d.dv)
+    _want(f, q.device, (decay, torch.float32, (d.heads,)), (done, torch.uint8, (d.T, d.Be)), (state_in, torch.float32, state),
+          (dstate_out, torch.float32, state), (dstate_in, torch.float32, state))
+    _check(lib().ppo_decay_attention_bwd(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(decay), _ptr(done), _ptr(state_in), _ptr(do), _ptr(dstate_out),
+                                         _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dstate_in), _ptr(workspace), _bytes_of(workspace), _stream(stream)), f)
+
+
+def ppo_decay_attention_step(q, k, v, decay, state, o, start=None, scale: float = 1.0, stream=None):
+    """One decision: q [Be,heads,dk], k [Be,kv_heads,dk], v [Be,kv_heads,dv] -> o [Be,heads,dv], state fp32 [Be,heads,dk,dv] in place;
+    start uint8 [Be]: envs that start from a zero state."""
+    f = "ppo_decay_attention_step"
+    d = _attention_desc(f, q, k, v, o, scale, 1)
+    _want(f, q.device, (decay, torch.float32, (d.heads,)), (start, torch.uint8, (d.Be,)), (state, torch.float32, (d.Be, d.heads, d.dk, d.dv)))
+    _check(lib().ppo_decay_attention_step(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(decay), _ptr(start), _ptr(state), _ptr(o), _stream(stream)), f)
+
+
+def ppo_group_norm_workspace_bytes(x, groups: int, backward: bool) -> int:
+    """Bytes the calls with this x [B,HW,C] need (0: none)."""
+    B, HW, n = x.shape
+    d = GroupNormDesc(B, HW, n, groups, 0, _DTYPES[x.dtype], n, n)
+    return lib().ppo_group_norm_workspace_bytes(C.byref(d), int(backward))
+
+
+def _norm_desc(where: str, x, groups: int, y, act: str) -> GroupNormDesc:
+    device = _here(where, x)
+    _refuse(1, where, act in _ACTS and y.dtype == x.dtype and y.device == device)
+    _refuse(2, where, x.dim() == 3 and x.shape == y.shape)
+    B, HW, n = x.shape
+    return GroupNormDesc(B, HW, n, groups, _ACTS[act], _DTYPES[x.dtype], _ld(where, x, 2), _ld(where, y, 2))
+
+
+def ppo_group_norm_fwd(x, groups: int, gamma, beta, y, mean, rstd, act: str = "none", eps: float = 1e-5, workspace=None, stream=None):
+    """x, y [B,HW,C] (fp32, bf16 or fp16; pixels may be parts of wider rows); gamma, beta fp32 [C] or None; mean, rstd fp32
+    [B,groups] are written; act: none, relu or silu."""
+    f = "ppo_group_norm_fwd"
+    d = _norm_desc(f, x, groups, y, act)
+    _want(f, x.device, (gamma, torch.float32, (d.C,)), (beta, torch.float32, (d.C,)), (mean, torch.float32, (d.B, groups)),
+          (rstd, torch.float32, (d.B, groups)))
+    _check(lib().ppo_group_norm_fwd(C.byref(d), eps, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd), _ptr(workspace),
+                                    _bytes_of(workspace), _stream(stream)), f)
+
+
+def ppo_group_norm_bwd(x, groups: int, gamma, beta, mean, rstd, dy, dx, dgamma=None, dbeta=None, act: str = "none", accumulate: bool = False,
+                       workspace=None, stream=None):
+    """dx (strided as x) and, unless they are None, dgamma and dbeta fp32 [C] (added to where accumulate) from dy."""
+    f = "ppo_group_norm_bwd"
+    d = _norm_desc(f, x, groups, dy, act)
+    _refuse(1, f, dx.dtype == x.dtype and dx.device == x.device)
+    _refuse(2, f, dx.shape == x.shape and _ld(f, dx, 2) == d.ldx)
+    _want(f, x.device, (gamma, torch.float32, (d.C,)), (beta, torch.float32, (d.C,)), (mean, torch.float32, (d.B, groups)),
+          (rstd, torch.float32, (d.B, groups)), (dgamma, torch.float32, (d.C,)), (dbeta, torch.float32, (d.C,)))
+    _check(lib().ppo_group_norm_bwd(C.byref(d), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(dx), _ptr(dgamma),
+                                    _ptr(dbeta), int(accumulate), _ptr(workspace), _bytes_of(workspace), _stream(stream)), f)
+
+
+def _token_desc(where: str, logits, tokens, scale: float) -> TokenDesc:
+    device = _here(where, logits)
+    _refuse(2, where, logits.dim() == 2)
+    rows, vocab = logits.shape
+    _want(where, device, (tokens, torch.int32, (rows,)))
+    return TokenDesc(rows, vocab, _DTYPES[logits.dtype], _ld(where, logits, 1), scale)
+
+
+def ppo_token_logp(logits, tokens, logp, entropy=None, scale: float = 1.0, stream=None):
+    """logits [rows,vocab] (fp32, bf16 or fp16; rows may be parts of wider ones), tokens int32 [rows] -> logp, entropy fp32 [rows] of
+    the distributions of scale * logits."""
+    f = "ppo_token_logp"
+    d = _token_desc(f, logits, tokens, scale)
+    _want(f, logits.device, (logp, torch.float32, (d.rows,)), (entropy, torch.float32, (d.rows,)))
+    _check(lib().ppo_token_logp(C.byref(d), _ptr(logits), _ptr(tokens), _ptr(logp), _ptr(entropy), _stream(stream)), f)
+
+
+def ppo_token_loss_workspace_bytes(logits) -> int:
+    rows, vocab = logits.shape
+    d = TokenDesc(rows, vocab, _DTYPES[logits.dtype], vocab, 1.0)
+    return lib().ppo_token_loss_workspace_bytes(C.byref(d))
+
+
+def ppo_token_loss_fwd_bwd(logits, tokens, logp_old, adv, B_total: int, dlogits, loss_out, logp_ref=None, weight=None, clip_low: float = 0.2,
+                           clip_high: float = 0.2, kl_coef: float = 0.0, ent_coef: float = 0.0, scale: float = 1.0, grad_scale: float = 1.0,
+                           logp_out=None, accumulate: bool = False, workspace=None, stream=None):
+    """Clipped policy loss over logits [rows,vocab] with its gradient in dlogits (may be logits); logp_old, adv, logp_ref, weight,
+    logp_out fp32 [rows]; loss_out fp32 [5] = L_pi, KL, H, mean(old - logp), clip fraction (added to where accumulate)."""
+    f = "ppo_token_loss_fwd_bwd"
+    d = _token_desc(f, logits, tokens, scale)
+    row = (d.rows,)
+    _refuse(1, f, dlogits.dtype == logits.dtype and dlogits.device == logits.device)
+    _refuse(2, f, dlogits.shape == logits.shape)
+    _want(f, logits.device, (logp_old, torch.float32, row), (adv, torch.float32, row), (logp_ref, torch.float32, row), (weight, torch.float32, row),
+          (logp_out, torch.float32, row), (loss_out, torch.float32, (5,)))
+    c = TokenLossCoef(clip_low, clip_high, kl_coef, ent_coef, grad_scale, B_total)
+    _check(lib().ppo_token_loss_fwd_bwd(C.byref(d), C.byref(c), _ptr(logits), _ptr(tokens), _ptr(logp_old), _ptr(logp_ref), _ptr(adv), _ptr(weight),
+                                        _ptr(dlogits), _ld(f, dlogits, 1), _ptr(logp_out), _ptr(loss_out), int(accumulate), _ptr(workspace),
+                                        _bytes_of(workspace), _stream(stream)), f)
