@@ -43,6 +43,25 @@ int ppo_enqueue(const void *fn, dim3 grid, dim3 block, size_t smem, bool togethe
     return PPO_OK;
 }
 
+int ppo_enqueue_cluster(const void *fn, int cluster, dim3 grid, dim3 block, size_t smem, cudaStream_t st, void **argv) {
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid;
+    c.blockDim = block;
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    c.attrs = at;
+    c.numAttrs = 2;
+    ppo_count_launches(1);
+    PPO_CUDA_CHECK(cudaLaunchKernelExC(&c, fn, argv));
+    return PPO_OK;
+}
+
 int ppo_replay(const Launches &launches, cudaStream_t st, const void *last, size_t last_bytes) {
     for (const LaunchRecord &r : launches) {
         void *argv[32];

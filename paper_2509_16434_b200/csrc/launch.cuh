@@ -77,6 +77,18 @@ int ppo_launch_together(void (*fn)(P...), dim3 grid, dim3 block, size_t smem, cu
     return ppo_launch_as(true, fn, grid, block, smem, st, args...);
 }
 
+// In clusters of `cluster` blocks along x; such launches are not recorded.
+int ppo_enqueue_cluster(const void *fn, int cluster, dim3 grid, dim3 block, size_t smem, cudaStream_t st, void **argv);
+template <typename... P, typename... A>
+int ppo_launch_cluster(void (*fn)(P...), int cluster, dim3 grid, dim3 block, size_t smem, cudaStream_t st, A... args) {
+    static_assert(sizeof...(P) == sizeof...(A), "argument count");
+    void *argv[sizeof...(A)];
+    int n = 0;
+    std::tuple<std::remove_const_t<P>...> vals(static_cast<std::remove_const_t<P>>(args)...);
+    std::apply([&](auto &...v) { ((argv[n++] = (void *)&v), ...); }, vals);
+    return ppo_enqueue_cluster(reinterpret_cast<const void *>(fn), cluster, grid, block, smem, st, argv);
+}
+
 // Enqueues a recorded operation.  last (null: none): what takes the place of the last argument of every launch, last_bytes long; for
 // arguments that are no part of the preparation, such as the addresses of results, and of the key neither.
 int ppo_replay(const Launches &launches, cudaStream_t st, const void *last = nullptr, size_t last_bytes = 0);

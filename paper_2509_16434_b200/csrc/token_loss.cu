@@ -1,5 +1,12 @@
 // Log-probabilities of tokens, and the clipped policy loss over a vocabulary with its gradient.
+//
+// One pass: a row of logits is read once into registers, its maximum, sum of exponentials and sum of exponentials times logits are
+// taken there, and the gradient is written from there.  A row belongs to a warp, to a block, or to a cluster of up to eight blocks
+// that exchange their sums through distributed shared memory, by the bytes of a row alone: who sums what, and so every bit of a row's
+// results, depends neither on the other rows of a call nor on where the row lies, and the call that scores a token while acting gives
+// what the loss gives (a ratio of exactly 1 in a first epoch).
 #include "elem.cuh"
+#include "tcgen05.cuh"
 
 namespace {
 
@@ -17,104 +24,300 @@ struct TokenArgs {
     float *terms;  // [5][rows]
 };
 
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Of logits x: the largest, the sum of e = 2^d with d = (x - top) scale log2(e), and the sum of e d.
 struct RowStat {
-    float top, sum, xe;  // max, sum of e = exp(x - top), sum of e (x - top)
+    float top, sum, xe;
 };
-__device__ __forceinline__ RowStat merge(RowStat a, RowStat b) {
+// Every rounding is written out, so that all kernels round alike.
+__device__ __forceinline__ RowStat merge(RowStat a, RowStat b, float c) {
     if (b.top > a.top) {
         const RowStat t = a;
         a = b;
         b = t;
     }
     if (b.top == -INFINITY) return a;  // nothing in it
-    const float d = b.top - a.top, f = expf(d);
-    if (f > 0.f) {
-        a.xe += f * (b.xe + d * b.sum);
-        a.sum += f * b.sum;
+    const float d = __fmul_rn(b.top - a.top, c), f = exp2f(d);
+    if (!(f == 0.f)) {
+        a.xe = fmaf(f, fmaf(d, b.sum, b.xe), a.xe);
+        a.sum = fmaf(f, b.sum, a.sum);
     }
     return a;
 }
+// Lanes o apart, the lower one first in both.
+__device__ __forceinline__ RowStat merge_lanes(RowStat s, int o, float c) {
+    RowStat t;
+    t.top = __shfl_xor_sync(0xffffffffu, s.top, o);
+    t.sum = __shfl_xor_sync(0xffffffffu, s.sum, o);
+    t.xe = __shfl_xor_sync(0xffffffffu, s.xe, o);
+    return threadIdx.x & o ? merge(t, s, c) : merge(s, t, c);
+}
 
-constexpr int kRowThreads = 256;
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
-template <typename T, bool LOSS>
-__global__ void __launch_bounds__(kRowThreads) token_row_kernel(TokenArgs a) {
+// Bytes s .. s + 15 of 32.
+__device__ __forceinline__ uint4 window(uint4 lo, uint4 hi, int s) {
+    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (s & 8) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (s & 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    const int bits = (s & 3) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                      __funnelshift_r(w[3], w[4], bits));
+}
+
+// Single elements, at the ends of a row.
+template <typename T>
+__device__ __forceinline__ uint4 load_some(const T *x, int n) {
+    uint32_t w[4] = {};
+#pragma unroll 1
+    for (int i = 0; i < Vec<T>::N; ++i) {
+        const T e = i < n ? x[i] : from_f32<T>(-INFINITY);
+        if constexpr (sizeof(T) == 4) {
+            const uint32_t u = __float_as_uint(e);
+            w[0] = i == 0 ? u : w[0], w[1] = i == 1 ? u : w[1], w[2] = i == 2 ? u : w[2], w[3] = i == 3 ? u : w[3];
+        } else {
+            const uint32_t u = (uint32_t)*reinterpret_cast<const uint16_t *>(&e) << (16 * (i & 1));
+            w[0] |= i / 2 == 0 ? u : 0, w[1] |= i / 2 == 1 ? u : 0, w[2] |= i / 2 == 2 ? u : 0, w[3] |= i / 2 == 3 ? u : 0;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ void store_some(T *g, uint4 v, int from, int to) {
+#pragma unroll 1
+    for (int i = from; i < to; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            g[i] = __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+        } else {
+            const uint32_t w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
+            *reinterpret_cast<uint16_t *>(g + i) = (uint16_t)(w >> (16 * (i & 1)));
+        }
+    }
+}
+
+// Elements 16 / sizeof(T) j .. of a row that starts anywhere; minus infinity behind its end.
+template <typename T>
+__device__ __forceinline__ Vec<T> load_row(const T *x, int vocab, int j) {
+    constexpr int N = Vec<T>::N;
+    const int s = (int)(reinterpret_cast<uintptr_t>(x) & 15), first = j * N;
+    Vec<T> v;
+    if (first + N <= vocab && s == 0) {
+        v.raw = *reinterpret_cast<const uint4 *>(x + first);
+    } else if (j > 0 && first + 2 * N <= vocab) {  // both aligned windows lie inside the row
+        const uint4 *p = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(x) - s) + j;
+        v.raw = window(p[0], p[1], s);
+    } else {
+        v.raw = load_some(x + first, vocab - first);
+    }
+    return v;
+}
+
+// Stores elements N j .. of a row that starts anywhere; the lanes of the warp hold consecutive j.  Where the row is not aligned,
+// a lane writes the aligned 16 bytes that its first elements share with the last ones of the lane in front.
+template <typename T>
+__device__ __forceinline__ void store_row(T *g, int vocab, int j, const Vec<T> &v) {
+    constexpr int N = Vec<T>::N;
+    const int s = (int)(reinterpret_cast<uintptr_t>(g) & 15), lane = threadIdx.x & 31, first = j * N;
+    const bool full = first + N <= vocab;
+    if (s == 0) {
+        if (full) *reinterpret_cast<uint4 *>(g + first) = v.raw;
+        else if (first < vocab) store_some(g + first, v.raw, 0, vocab - first);
+        return;
+    }
+    uint4 prev;
+    prev.x = __shfl_up_sync(0xffffffffu, v.raw.x, 1);
+    prev.y = __shfl_up_sync(0xffffffffu, v.raw.y, 1);
+    prev.z = __shfl_up_sync(0xffffffffu, v.raw.z, 1);
+    prev.w = __shfl_up_sync(0xffffffffu, v.raw.w, 1);
+    const int split = (16 - s) / (int)sizeof(T);  // elements in front of the next aligned address
+    if (first >= vocab) return;
+    if (lane > 0 && full) *(reinterpret_cast<uint4 *>(reinterpret_cast<uintptr_t>(g) - s) + j) = window(prev, v.raw, 16 - s);
+    else store_some(g + first, v.raw, 0, min(split, vocab - first));
+    if (lane == 31 || first + 2 * N > vocab) store_some(g + first, v.raw, split, min(N, vocab - first));
+}
+
+// The larger ones of two vectors' elements, and the largest of one's; a NaN gives way to a number.
+template <typename T>
+__device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
+    if constexpr (sizeof(T) == 4) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    } else if constexpr (std::is_same_v<T, bf16>) {
+        const __nv_bfloat162 m = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    } else {
+        const __half2 m = __hmax2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint4 max_of(uint4 a, uint4 b) {
+    return make_uint4(max_word<T>(a.x, b.x), max_word<T>(a.y, b.y), max_word<T>(a.z, b.z), max_word<T>(a.w, b.w));
+}
+template <typename T>
+__device__ __forceinline__ float largest(uint4 a) {
+    Vec<T> v;
+    float f[Vec<T>::N], m = -INFINITY;
+    v.raw = a;
+    v.get(f);
+#pragma unroll
+    for (int k = 0; k < Vec<T>::N; ++k) m = fmaxf(m, f[k]);
+    return m;
+}
+
+// Keeps the compiler from holding the elements of a vector, unpacked, from one use to the next: there are registers for them packed only.
+__device__ __forceinline__ void stay_packed(uint4 &v) { asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)); }
+
+// THREADS per row and block of a cluster, NV 16-byte vectors of each in registers; rows that are longer than the cluster's
+// registers are read in pieces, and again for the gradient.
+template <typename T, int THREADS, int NV, bool LOSS>
+__global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 ? 2 : 6) token_row_kernel(TokenArgs a, int cluster) {
     grid_wait();
-    __shared__ RowStat part[kRowThreads / 32];
-    const int row = blockIdx.x, tid = threadIdx.x;
+    constexpr int N = Vec<T>::N, WARPS = THREADS / 32;
+    __shared__ RowStat part[WARPS], whole[8];
+    if (cluster > 1) tc::cluster_arrive();
+    const int t = threadIdx.x % THREADS;
+    const int rank = cluster > 1 ? blockIdx.x % cluster : 0;
+    const int row = THREADS < 128 ? blockIdx.x * (128 / THREADS) + threadIdx.x / THREADS : blockIdx.x / cluster;
+    if (row >= a.rows) return;  // a whole warp
     const T *x = static_cast<const T *>(a.logits) + (long long)row * a.ld;
-    T *g = LOSS ? static_cast<T *>(a.grad) + (long long)row * a.ld_grad : nullptr;
     const int token = a.tokens[row];
     const float w = LOSS && a.weight ? a.weight[row] : 1.f;
     const bool out = token < 0 || token >= a.vocab || w == 0.f;
+    const float c = a.scale * kLog2e;
+    const int step = THREADS * cluster, j0 = rank * THREADS + t, pieces = (a.vocab + N * NV * step - 1) / (N * NV * step);
+    Vec<T> v[NV];
     RowStat s = {-INFINITY, 0.f, 0.f};
+    const float xa = out ? 0.f : to_f32(x[token]);
     if (!out) {
-        float top = -INFINITY;
-        for (int j = tid; j < a.vocab; j += kRowThreads) top = fmaxf(top, to_f32(x[j]) * a.scale);
-        s.top = top;
-        for (int j = tid; j < a.vocab; j += kRowThreads) {
-            const float d = to_f32(x[j]) * a.scale - top, e = top == -INFINITY ? 0.f : expf(d);
-            s.sum += e;
-            if (e > 0.f) s.xe += e * d;
+        for (int p = 0; p < pieces; ++p) {
+            RowStat r = {-INFINITY, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0);
+            uint4 most = v[0].raw;
+#pragma unroll
+            for (int i = 1; i < NV; ++i) {
+                most = max_of<T>(most, v[i].raw);
+            }
+            r.top = largest<T>(most);
+            const float top = r.top == -INFINITY ? 0.f : r.top;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float f[N];
+                stay_packed(v[i].raw);
+                v[i].get(f);
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float d = __fmul_rn(f[k] - top, c), e = exp2_fast(d);
+                    r.sum += e;
+                    r.xe = fmaf(e, fmaxf(d, -150.f), r.xe);  // e is 0 from there on
+                }
+            }
+            if (r.sum != r.sum) r.top = INFINITY;  // a NaN among numbers, or alone: the row's results are NaN
+            s = p == 0 ? r : merge(s, r, c);
         }
     }
-    for (int o = 16; o > 0; o >>= 1) {
-        RowStat t;
-        t.top = __shfl_xor_sync(0xffffffffu, s.top, o);
-        t.sum = __shfl_xor_sync(0xffffffffu, s.sum, o);
-        t.xe = __shfl_xor_sync(0xffffffffu, s.xe, o);
-        s = merge(s, t);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) s = merge_lanes(s, o, c);
+    if constexpr (WARPS > 1) {
+        if (t % 32 == 0) part[t / 32] = s;
+        __syncthreads();
+        s = part[0];
+        for (int i = 1; i < WARPS; ++i) s = merge(s, part[i], c);
+        if (cluster > 1) {
+            tc::cluster_wait();  // all blocks of the cluster run
+            if (t < cluster) {  // to each block of the cluster
+                const uint32_t at = tc::in_cta(tc::smem_u32(&whole[rank]), t);
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(s.top) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(s.sum) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(s.xe) : "memory");
+            }
+            tc::cluster_sync();
+            s = whole[0];
+            for (int i = 1; i < cluster; ++i) s = merge(s, whole[i], c);
+        }
     }
-    if (tid % 32 == 0) part[tid / 32] = s;
-    __syncthreads();
-    s = part[0];
-    for (int i = 1; i < kRowThreads / 32; ++i) s = merge(s, part[i]);
-    const bool empty = s.top == -INFINITY;
+    const bool empty = s.top == -INFINITY, first = t == 0 && rank == 0;
     const float log_sum = logf(s.sum);
-    float logp = out ? 0.f : empty ? -INFINITY : to_f32(x[token]) * a.scale - s.top - log_sum;
-    const float H = out || empty ? 0.f : log_sum - s.xe / s.sum;
+    float logp = out ? 0.f : empty ? -INFINITY : fmaf(xa - s.top, a.scale, -log_sum);
+    const float H = out || empty ? 0.f : fmaf(-kLn2, s.xe / s.sum, log_sum);
     if constexpr (!LOSS) {
-        if (tid == 0) {
+        if (first) {
             a.logp[row] = logp;
             if (a.entropy) a.entropy[row] = H;
         }
-        return;
-    }
-    const bool skip = out || empty;
-    float dl = 0.f, share = 0.f;
-    if (!skip) {
-        const float ratio = expf(logp - a.old[row]), adv = a.adv[row];
-        const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
-        const float free_ = ratio * adv, held = fminf(fmaxf(ratio, lo), hi) * adv;
-        float kl = 0.f;
-        dl = free_ <= held ? -free_ : 0.f;
-        if (a.ref) {
-            const float d = a.ref[row] - logp, m = expm1f(d);
-            kl = m - d;
-            dl -= a.kl_coef * m;
+    } else {
+        T *g = static_cast<T *>(a.grad) + (long long)row * a.ld_grad;
+        const bool skip = out || empty;
+        float dl = 0.f, share = 0.f, terms[5] = {};
+        if (skip) {
+            logp = 0.f;
+        } else {
+            const float old = a.old[row], adv = a.adv[row], ratio = expf(logp - old);
+            const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
+            // NaN is kept: it shows in gradient and sums
+            const float free_ = ratio * adv, held = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
+            dl = free_ > held ? 0.f : -free_;
+            share = w * a.inv_total;
+            terms[0] = -share * (free_ > held ? held : free_);
+            if (a.ref) {
+                const float d = a.ref[row] - logp, m = expm1f(d);
+                terms[1] = share * (m - d);
+                dl -= a.kl_coef * m;
+            }
+            terms[2] = share * H;
+            terms[3] = share * (old - logp);
+            terms[4] = ratio < lo || ratio > hi ? share : 0.f;
         }
-        share = w * a.inv_total;
-        if (tid == 0) {
-            const float t[5] = {-fminf(free_, held), kl, H, a.old[row] - logp, ratio < lo || ratio > hi ? 1.f : 0.f};
-            for (int i = 0; i < 5; ++i) a.terms[(size_t)i * a.rows + row] = share * t[i];
+        if (first) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) a.terms[(size_t)i * a.rows + row] = terms[i];
+            if (a.logp) a.logp[row] = logp;
         }
-    } else if (tid == 0) {
-        for (int i = 0; i < 5; ++i) a.terms[(size_t)i * a.rows + row] = 0.f;
-        logp = 0.f;
-    }
-    if (tid == 0 && a.logp) a.logp[row] = logp;
-    __syncthreads();  // the gradient may take the place of the logits: all have read x[token]
-    const float inv = 1.f / s.sum, f = share * a.grad_scale * a.scale;
-    for (int j = tid; j < a.vocab; j += kRowThreads) {
-        float v = 0.f;
-        if (!skip) {
-            const float d = to_f32(x[j]) * a.scale - s.top, p = expf(d) * inv;
-            v = -dl * p;
-            if (p > 0.f) v += a.ent_coef * p * (d - log_sum + H);
-            if (j == token) v += dl;
-            v *= f;
+        // e (alpha + beta d), and dl at the token
+        const float f = share * a.grad_scale * a.scale, inv = f / s.sum;
+        const float alpha = inv * fmaf(a.ent_coef, H - log_sum, -dl), beta = inv * a.ent_coef * kLn2, hot = f * dl;
+        for (int p = 0; p < pieces; ++p) {
+            if (pieces > 1 && !skip) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int j = (p * NV + i) * step + j0;
+                float o[N];
+                if (skip) {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) o[k] = 0.f;
+                } else {
+                    stay_packed(v[i].raw);
+                    v[i].get(o);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const float d = __fmul_rn(o[k] - s.top, c);
+                        o[k] = exp2_fast(d) * fmaf(beta, fmaxf(d, -150.f), alpha);
+                    }
+                    if (token / N == j) {
+#pragma unroll
+                        for (int k = 0; k < N; ++k)
+                            if (token % N == k) o[k] += hot;
+                    }
+                }
+                Vec<T> r;
+                r.set(o);
+                if ((j & ~31) * N < a.vocab) store_row(g, a.vocab, j, r);  // the same in all lanes
+            }
         }
-        g[j] = from_f32<T>(v);
     }
 }
 
@@ -133,10 +336,23 @@ __global__ void __launch_bounds__(256) token_sum_kernel(const float *terms, int 
     if (threadIdx.x == 0) out[blockIdx.x] = (float)(part[0] + (accumulate ? (double)out[blockIdx.x] : 0.));
 }
 
+// A warp for rows of up to 4 KB, a block of 128 threads to 16 KB, of 512 to 64 KB, then clusters of 2, 4, 8 blocks (to 512 KB in
+// registers).
+template <typename T, bool LOSS>
+int launch_rows(const TokenArgs &a, cudaStream_t st) {
+    const size_t bytes = (size_t)a.vocab * sizeof(T);
+    if (bytes <= 4096) return ppo_launch(token_row_kernel<T, 32, 8, LOSS>, dim3(ppo_cdiv(a.rows, 4)), dim3(128), 0, st, a, 1);
+    if (bytes <= 16384) return ppo_launch(token_row_kernel<T, 128, 8, LOSS>, dim3(a.rows), dim3(128), 0, st, a, 1);
+    int n = 1;
+    while (n < 8 && bytes > (size_t)n * 65536) n *= 2;
+    return ppo_launch_cluster(token_row_kernel<T, 512, 8, LOSS>, n, dim3(a.rows * n), dim3(512), 0, st, a, n);
+}
+
 int check(const ppo_token_desc *d) {
     if (!d || d->rows <= 0 || d->vocab <= 0 || !(d->scale > 0.f) || d->scale > 3.0e38f) return PPO_ERR_INVALID_ARG;
     if (d->dtype < PPO_F32 || d->dtype > PPO_F16) return PPO_ERR_INVALID_ARG;
     if (d->ld < d->vocab) return PPO_ERR_SHAPE;
+    if (d->rows > 0x7fffffff / 8 || d->vocab > 0x7fffffff / 2) return PPO_ERR_UNSUPPORTED;
     return PPO_OK;
 }
 
@@ -160,7 +376,7 @@ extern "C" int ppo_token_logp(const ppo_token_desc *d, const void *logits, const
     a.logp = logp;
     a.entropy = entropy;
     return with_elem(d->dtype, [&](auto t) {
-        return ppo_launch(token_row_kernel<decltype(t), false>, dim3(d->rows), dim3(kRowThreads), 0, static_cast<cudaStream_t>(stream), a);
+        return launch_rows<decltype(t), false>(a, static_cast<cudaStream_t>(stream));
     });
 }
 
@@ -201,7 +417,7 @@ extern "C" int ppo_token_loss_fwd_bwd(const ppo_token_desc *d, const ppo_token_l
     a.terms = static_cast<float *>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     PPO_TRY(with_elem(d->dtype, [&](auto t) {
-        return ppo_launch(token_row_kernel<decltype(t), true>, dim3(d->rows), dim3(kRowThreads), 0, st, a);
+        return launch_rows<decltype(t), true>(a, st);
     }));
     return ppo_launch(token_sum_kernel, dim3(5), dim3(256), 0, st, (const float *)a.terms, (int)d->rows, loss_out, accumulate);
 }

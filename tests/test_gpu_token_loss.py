@@ -186,6 +186,17 @@ def test_rows_that_are_left_out_and_distributions_at_the_edge(vocab, dtype):
     assert bool((none[0] == 0).all()) and bool((none[2] == 0).all()) and bool((none[1] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [1, 40, 3000, 20000, 150001])
+def test_a_nan_in_a_row_that_counts_shows(vocab, dtype):
+    x, tokens, old, ref, adv, _ = _inputs(4, vocab, dtype, 6)
+    x[1, vocab // 2], x[2] = float("nan"), float("nan")
+    logp, H = _logp(x, tokens)
+    assert torch.isnan(logp).tolist() == [False, True, True, False] and torch.isnan(H).tolist() == [False, True, True, False]
+    grad, lp, loss = _loss(x, tokens, torch.zeros_like(old), adv, ent_coef=0.1)
+    assert torch.isnan(grad).any(1).tolist() == [False, True, True, False] and bool(torch.isnan(loss[:4:2]).all())
+
+
 def test_first_epoch_and_micro_batches():
     """Where the policy is still the one that acted every ratio is 1 and no row is clipped; micro-batches add up."""
     x, tokens, _, _, adv, _ = _inputs(300, 777, torch.bfloat16, 8)
