@@ -1,5 +1,6 @@
 // Group normalisation with an activation, channels last, and its gradients.
 #include "elem.cuh"
+#include "tcgen05.cuh"
 
 namespace {
 
@@ -8,13 +9,13 @@ struct NormArgs {
     void *y, *dx;
     const float *gamma, *beta;
     float *mean, *rstd;
-    float *part;  // gradients of gamma and beta of each image, [2][B][C]
+    float *part;  // shares of the gradients of gamma and beta, [parts][2][C]
     long long ldx, ldy;
     int B, HW, C, groups, per, act;
     float eps;
 };
 
-constexpr int kNormThreads = 256;
+constexpr int kThreads = 256;
 
 // Sum over the block, the same in every thread; tmp holds one value per warp.
 __device__ __forceinline__ float block_sum(float v, float *tmp) {
@@ -23,128 +24,639 @@ __device__ __forceinline__ float block_sum(float v, float *tmp) {
     if (threadIdx.x % 32 == 0) tmp[threadIdx.x / 32] = v;
     __syncthreads();
     v = 0.f;
-    for (int i = 0; i < kNormThreads / 32; ++i) v += tmp[i];
+    for (int i = 0; i < kThreads / 32; ++i) v += tmp[i];
+    return v;
+}
+// Sum over `lanes` (a power of two) neighbouring lanes, the same in each.
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-__device__ __forceinline__ float activate(float z, int act) {
-    return act == PPO_ACT_RELU ? fmaxf(z, 0.f) : act == PPO_ACT_SILU ? z / (1.f + expf(-z)) : z;
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+    return ACT == PPO_ACT_RELU ? (z < 0.f ? 0.f : z) : ACT == PPO_ACT_SILU ? z * sigmoid(z) : z;
 }
 
-// Which side of 0 gamma xhat + beta is on: rounding to 32 bits decides it wrongly only within a few units of the last place of its
-// terms, and there 64 bits do.
-__device__ __forceinline__ bool relu_open(float x, float mean, float rstd, float gamma, float beta, float z) {
-    if (fabsf(z) > 1e-6f * (fabsf(gamma) * rstd * (fabsf(x) + fabsf(mean)) + fabsf(beta))) return z > 0.f;
-    return ((double)x - (double)mean) * (double)rstd * (double)gamma + (double)beta > 0.;
+// z = gamma xhat + beta as one product: (x - mean) scale + shift with scale = rstd gamma, shift = beta.
+struct Affine {
+    float scale, shift;
+};
+
+// dL/dz.  Which side of 0 z is on decides the ReLU's gradient; 32 bits decide it wrongly only where the two terms of z cancel to
+// within their own rounding (three units of the last place of the product), and there 64 bits do.
+template <int ACT>
+__device__ __forceinline__ float grad_z(float dy, float xc, Affine f, float x, float mean, float rstd, float gamma) {
+    if (ACT == PPO_ACT_NONE) return dy;
+    const float z = fmaf(xc, f.scale, f.shift);
+    if (ACT == PPO_ACT_SILU) {
+        const float p = sigmoid(z);
+        return dy * (p * fmaf(z, 1.f - p, 1.f));
+    }
+    bool open = z > 0.f;
+    if (fabsf(z) <= 5e-7f * fabsf(f.shift)) open = ((double)x - (double)mean) * (double)rstd * (double)gamma + (double)f.shift > 0.;
+    return open ? dy : 0.f;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(NormArgs a) {
+// ---- any channel count, stride and alignment: a block per image and group, element by element ----
+
+// Threads (p, c): c channels of the group side by side, p pixels.
+struct Tile {
+    int lanes, rows, c, p;
+    __device__ Tile(int per) {
+        lanes = min(per, kThreads);
+        rows = kThreads / lanes;
+        c = threadIdx.x % lanes;
+        p = threadIdx.x / lanes;
+    }
+};
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kThreads) norm_fwd_any_kernel(NormArgs a) {
     grid_wait();
-    __shared__ float tmp[kNormThreads / 32];
+    __shared__ float tmp[kThreads / 32];
     const int b = blockIdx.x / a.groups, g = blockIdx.x % a.groups, c0 = g * a.per;
     const T *x = static_cast<const T *>(a.x) + (long long)b * a.HW * a.ldx + c0;
     T *y = static_cast<T *>(a.y) + (long long)b * a.HW * a.ldy + c0;
-    const long long n = (long long)a.HW * a.per;
+    const float n = (float)a.HW * (float)a.per;
+    const Tile t(a.per);
     float s = 0.f;
-    for (long long i = threadIdx.x; i < n; i += kNormThreads) s += to_f32(x[i / a.per * a.ldx + i % a.per]);
-    const float mean = block_sum(s, tmp) / (float)n;
+    if (t.p < t.rows)
+        for (int c = t.c; c < a.per; c += t.lanes)
+            for (int i = t.p; i < a.HW; i += t.rows) s += to_f32(x[i * a.ldx + c]);
+    const float mean = block_sum(s, tmp) / n;
     s = 0.f;
-    for (long long i = threadIdx.x; i < n; i += kNormThreads) {
-        const float d = to_f32(x[i / a.per * a.ldx + i % a.per]) - mean;
-        s += d * d;
-    }
-    const float rstd = 1.f / sqrtf(block_sum(s, tmp) / (float)n + a.eps);
+    if (t.p < t.rows)
+        for (int c = t.c; c < a.per; c += t.lanes)
+            for (int i = t.p; i < a.HW; i += t.rows) {
+                const float d = to_f32(x[i * a.ldx + c]) - mean;
+                s = fmaf(d, d, s);
+            }
+    const float rstd = 1.f / sqrtf(block_sum(s, tmp) / n + a.eps);
     if (threadIdx.x == 0) {
         a.mean[blockIdx.x] = mean;
         a.rstd[blockIdx.x] = rstd;
     }
-    for (long long i = threadIdx.x; i < n; i += kNormThreads) {
-        const int c = (int)(i % a.per);
-        const float xhat = (to_f32(x[i / a.per * a.ldx + c]) - mean) * rstd;
-        const float z = a.gamma ? xhat * a.gamma[c0 + c] + a.beta[c0 + c] : xhat;
-        y[i / a.per * a.ldy + c] = from_f32<T>(activate(z, a.act));
+    if (t.p < t.rows)
+        for (int c = t.c; c < a.per; c += t.lanes) {
+            const float scale = rstd * (a.gamma ? a.gamma[c0 + c] : 1.f), shift = a.gamma ? a.beta[c0 + c] : 0.f;
+            for (int i = t.p; i < a.HW; i += t.rows) y[i * a.ldy + c] = from_f32<T>(activate<ACT>(fmaf(to_f32(x[i * a.ldx + c]) - mean, scale, shift)));
+        }
+}
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kThreads) norm_bwd_any_kernel(NormArgs a) {
+    grid_wait();
+    __shared__ float tmp[kThreads / 32], part[2][kThreads];
+    const int b = blockIdx.x / a.groups, g = blockIdx.x % a.groups, c0 = g * a.per;
+    const T *x = static_cast<const T *>(a.x) + (long long)b * a.HW * a.ldx + c0, *dy = static_cast<const T *>(a.dy) + (long long)b * a.HW * a.ldy + c0;
+    T *dx = static_cast<T *>(a.dx) + (long long)b * a.HW * a.ldx + c0;
+    const float mean = a.mean[blockIdx.x], rstd = a.rstd[blockIdx.x], n = (float)a.HW * (float)a.per;
+    const Tile t(a.per);
+    float m1 = 0.f, m2 = 0.f;
+    for (int c = t.c; c - t.c < a.per; c += t.lanes) {
+        const bool on = c < a.per && t.p < t.rows;
+        const float gamma = on && a.gamma ? a.gamma[c0 + c] : 1.f;
+        const Affine f = {rstd * gamma, on && a.gamma ? a.beta[c0 + c] : 0.f};
+        float s1 = 0.f, s2 = 0.f;
+        if (on)
+            for (int i = t.p; i < a.HW; i += t.rows) {
+                const float v = to_f32(x[i * a.ldx + c]), xc = v - mean, dz = grad_z<ACT>(to_f32(dy[i * a.ldy + c]), xc, f, v, mean, rstd, gamma);
+                s1 += dz;
+                s2 = fmaf(dz, xc, s2);
+            }
+        __syncthreads();
+        part[0][threadIdx.x] = s1;
+        part[1][threadIdx.x] = s2;
+        __syncthreads();
+        if (t.p == 0 && on) {
+            for (int p = 1; p < t.rows; ++p) {
+                s1 += part[0][p * t.lanes + t.c];
+                s2 += part[1][p * t.lanes + t.c];
+            }
+            s2 *= rstd;
+            if (a.part) {
+                a.part[(size_t)b * 2 * a.C + c0 + c] = s2;
+                a.part[((size_t)b * 2 + 1) * a.C + c0 + c] = s1;
+            }
+            m1 = fmaf(gamma, s1, m1);
+            m2 = fmaf(gamma, s2, m2);
+        }
+    }
+    m1 = block_sum(m1, tmp) / n;
+    m2 = block_sum(m2, tmp) / n * rstd;
+    if (t.p < t.rows)
+        for (int c = t.c; c < a.per; c += t.lanes) {
+            const float gamma = a.gamma ? a.gamma[c0 + c] : 1.f;
+            const Affine f = {rstd * gamma, a.gamma ? a.beta[c0 + c] : 0.f};
+            for (int i = t.p; i < a.HW; i += t.rows) {
+                const float v = to_f32(x[i * a.ldx + c]), xc = v - mean, dz = grad_z<ACT>(to_f32(dy[i * a.ldy + c]), xc, f, v, mean, rstd, gamma);
+                dx[i * a.ldx + c] = from_f32<T>(rstd * (fmaf(gamma, dz, -m1) - xc * m2));
+            }
+        }
+}
+
+// ---- few values per image and group (up to 4 KB): `lanes` lanes of a warp per group, its values in registers ----
+//
+// A lane's vectors hold the same channels at every pixel (lanes is a multiple of a pixel's vectors of the group), so it keeps
+// their scales, and the sums over images of their gradients, for all images its block goes through.
+
+template <typename T, int ACT, int NV>
+__global__ void __launch_bounds__(kThreads) norm_fwd_small_kernel(NormArgs a, int lanes, long long items) {
+    grid_wait();
+    constexpr int N = Vec<T>::N;
+    const int vecs = a.per / N, all = a.HW * vecs, l = threadIdx.x % lanes;
+    const long long item = (long long)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
+    const bool on = item < items;
+    const int b = on ? (int)(item / a.groups) : 0, g = on ? (int)(item % a.groups) : 0, c0 = g * a.per + l % vecs * N;
+    const T *x = static_cast<const T *>(a.x) + (long long)b * a.HW * a.ldx + c0;
+    Vec<T> v[NV];
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = i * lanes + l;
+        v[i].raw = on && at < all ? *reinterpret_cast<const uint4 *>(x + at / vecs * a.ldx) : make_uint4(0, 0, 0, 0);
+    }
+    const float n = (float)a.HW * (float)a.per;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float f[N];
+        v[i].get(f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) s += f[k];
+    }
+    const float mean = lanes_sum(s, lanes) / n;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float f[N];
+        v[i].get(f);
+        if (i * lanes + l < all) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) s = fmaf(f[k] - mean, f[k] - mean, s);
+        }
+    }
+    const float rstd = 1.f / sqrtf(lanes_sum(s, lanes) / n + a.eps);
+    if (!on) return;
+    if (l == 0) {
+        a.mean[item] = mean;
+        a.rstd[item] = rstd;
+    }
+    float scale[N], shift[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        scale[k] = a.gamma ? rstd * a.gamma[c0 + k] : rstd;
+        shift[k] = a.gamma ? a.beta[c0 + k] : 0.f;
+    }
+    T *y = static_cast<T *>(a.y) + (long long)b * a.HW * a.ldy + c0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = i * lanes + l;
+        float f[N];
+        v[i].get(f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] = activate<ACT>(fmaf(f[k] - mean, scale[k], shift[k]));
+        v[i].set(f);
+        if (at < all) *reinterpret_cast<uint4 *>(y + at / vecs * a.ldy) = v[i].raw;
     }
 }
 
-template <typename T>
-struct Grad {
-    const T *x, *dy;
-    float mean, rstd;
-    int act;
-    // xhat and dL/dz of one element
-    __device__ __forceinline__ void at(long long ix, long long iy, float gamma, float beta, float &xhat, float &dz) const {
-        const float v = to_f32(x[ix]);
-        xhat = (v - mean) * rstd;
-        const float z = gamma * xhat + beta;
-        dz = to_f32(dy[iy]);
-        if (act == PPO_ACT_RELU) {
-            if (!relu_open(v, mean, rstd, gamma, beta, z)) dz = 0.f;
-        } else if (act == PPO_ACT_SILU) {
-            const float p = 1.f / (1.f + expf(-z));
-            dz *= p * (1.f + z * (1.f - p));
+// Block (x, y): groups y * kThreads / lanes .. of the images x, x + gridDim.x, ...
+template <typename T, int ACT, int NV>
+__global__ void __launch_bounds__(kThreads) norm_bwd_small_kernel(NormArgs a, int lanes) {
+    grid_wait();
+    constexpr int N = Vec<T>::N;
+    const int vecs = a.per / N, all = a.HW * vecs, l = threadIdx.x % lanes;
+    const int g = blockIdx.y * (kThreads / lanes) + threadIdx.x / lanes;
+    const bool on = g < a.groups;
+    const int c0 = (on ? g * a.per : 0) + l % vecs * N;
+    const float n = (float)a.HW * (float)a.per;
+    float gamma[N], beta[N], s1[N], s2[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        gamma[k] = a.gamma ? a.gamma[c0 + k] : 1.f;
+        beta[k] = a.gamma ? a.beta[c0 + k] : 0.f;
+        s1[k] = s2[k] = 0.f;
+    }
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+        const T *x = static_cast<const T *>(a.x) + (long long)b * a.HW * a.ldx + c0, *dy = static_cast<const T *>(a.dy) + (long long)b * a.HW * a.ldy + c0;
+        T *dx = static_cast<T *>(a.dx) + (long long)b * a.HW * a.ldx + c0;
+        const float mean = on ? a.mean[(long long)b * a.groups + g] : 0.f, rstd = on ? a.rstd[(long long)b * a.groups + g] : 0.f;
+        Vec<T> v[NV], d[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = i * lanes + l, p = at / vecs;
+            const bool ok = on && at < all;
+            v[i].raw = ok ? *reinterpret_cast<const uint4 *>(x + p * a.ldx) : make_uint4(0, 0, 0, 0);
+            d[i].raw = ok ? *reinterpret_cast<const uint4 *>(dy + p * a.ldy) : make_uint4(0, 0, 0, 0);
+        }
+        float m1 = 0.f, m2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float f[N], e[N];
+            v[i].get(f);
+            d[i].get(e);
+            if (i * lanes + l < all) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float xc = f[k] - mean, dz = grad_z<ACT>(e[k], xc, {rstd * gamma[k], beta[k]}, f[k], mean, rstd, gamma[k]);
+                    s1[k] += dz;
+                    s2[k] = fmaf(dz, xc * rstd, s2[k]);
+                    m1 = fmaf(gamma[k], dz, m1);
+                    m2 = fmaf(gamma[k] * dz, xc, m2);
+                }
+            }
+        }
+        m1 = lanes_sum(m1, lanes) / n;
+        m2 = lanes_sum(m2, lanes) / n * rstd * rstd;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = i * lanes + l;
+            float f[N], e[N];
+            v[i].get(f);
+            d[i].get(e);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float xc = f[k] - mean, dz = grad_z<ACT>(e[k], xc, {rstd * gamma[k], beta[k]}, f[k], mean, rstd, gamma[k]);
+                f[k] = rstd * (fmaf(gamma[k], dz, -m1) - xc * m2);
+            }
+            v[i].set(f);
+            if (on && at < all) *reinterpret_cast<uint4 *>(dx + at / vecs * a.ldx) = v[i].raw;
         }
     }
+    if (!a.part) return;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        for (int o = vecs; o < lanes; o <<= 1) {  // lanes of other pixels of the same channels
+            s1[k] += __shfl_xor_sync(0xffffffffu, s1[k], o);
+            s2[k] += __shfl_xor_sync(0xffffffffu, s2[k], o);
+        }
+    if (on && l < vecs) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            a.part[(size_t)blockIdx.x * 2 * a.C + c0 + k] = s2[k];
+            a.part[((size_t)blockIdx.x * 2 + 1) * a.C + c0 + k] = s1[k];
+        }
+    }
+}
+
+// ---- larger images: a cluster of blocks per image, each with a run of its pixels, which it keeps in shared memory ----
+//
+// Thread (pl, vc) has the same vector of channels of the pixels pl, pl + lanes, ...: memory is read and written in whole rows,
+// once, and what a thread copies in is what it uses, so that only the sums meet at barriers.  K: parts of a vector that belong
+// to different groups (1: a group has whole vectors).  `keep` 0: images that do not fit are read again for each use, from L2 where
+// that holds what the running clusters work on.
+
+struct Cluster {
+    int n, pixels, keep;  // blocks per image, pixels per block
+    size_t smem;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(NormArgs a) {
+// Entries of group g among the threads' K parts: thread pl * VC + first + i has part k; pl < lanes, i < span.
+struct Members {
+    int first, span, k;
+};
+template <int N, int K>
+__device__ __forceinline__ Members members(int g, int per) {
+    return K == 1 ? Members{g * (per / N), per / N, 0} : Members{g / K, 1, g % K};
+}
+
+template <typename T, int ACT, int K>
+__global__ void __launch_bounds__(kThreads) norm_fwd_cluster_kernel(NormArgs a, Cluster cl) {
     grid_wait();
-    __shared__ float tmp[kNormThreads / 32];
-    const int b = blockIdx.x / a.groups, g = blockIdx.x % a.groups, c0 = g * a.per;
-    const Grad<T> f = {static_cast<const T *>(a.x) + (long long)b * a.HW * a.ldx + c0, static_cast<const T *>(a.dy) + (long long)b * a.HW * a.ldy + c0,
-                       a.mean[blockIdx.x], a.rstd[blockIdx.x], a.act};
-    T *dx = static_cast<T *>(a.dx) + (long long)b * a.HW * a.ldx + c0;
-    float m1 = 0.f, m2 = 0.f;
-    for (int c = 0; c < a.per; ++c) {
-        const float gamma = a.gamma ? a.gamma[c0 + c] : 1.f, beta = a.gamma ? a.beta[c0 + c] : 0.f;
-        float s1 = 0.f, s2 = 0.f;
-        for (int i = threadIdx.x; i < a.HW; i += kNormThreads) {
-            float xhat, dz;
-            f.at(i * a.ldx + c, i * a.ldy + c, gamma, beta, xhat, dz);
-            s1 += dz;
-            s2 += dz * xhat;
-        }
-        s1 = block_sum(s1, tmp);
-        s2 = block_sum(s2, tmp);
-        if (a.part && threadIdx.x == 0) {
-            a.part[(size_t)b * a.C + c0 + c] = s2;
-            a.part[((size_t)a.B + b) * a.C + c0 + c] = s1;
-        }
-        m1 += gamma * s1;
-        m2 += gamma * s2;
+    tc::cluster_arrive();
+    constexpr int N = Vec<T>::N, M = N / K;
+    extern __shared__ __align__(16) float mem[];
+    float *tm = mem, *tq = tm + kThreads * K, *sent = tq + kThreads * K, *stat = sent + (cl.n * a.groups * 2 + 3) / 4 * 4;
+    uint4 *kept = reinterpret_cast<uint4 *>(stat + (a.groups * 2 + 3) / 4 * 4);
+    const int rank = blockIdx.x % cl.n, b = blockIdx.x / cl.n;
+    const int VC = a.C / N, lanes = kThreads / VC, tid = threadIdx.x, pl = tid / VC, vc = tid % VC;
+    const int p0 = rank * cl.pixels, P = max(0, min(cl.pixels, a.HW - p0));
+    const int cnt = pl < lanes && pl < P ? (P - 1 - pl) / lanes + 1 : 0;
+    const T *x = static_cast<const T *>(a.x) + ((long long)b * a.HW + p0 + pl) * a.ldx + vc * N;
+    T *y = static_cast<T *>(a.y) + ((long long)b * a.HW + p0 + pl) * a.ldy + vc * N;
+    const long long sx = lanes * a.ldx, sy = lanes * a.ldy;
+    if (cl.keep) {
+        for (int i = 0; i < cnt; ++i) tc::cp_async16(tc::smem_u32(kept + i * kThreads + tid), x + i * sx, true);
+        tc::cp_async_commit();
+        tc::cp_async_wait<0>();
     }
-    const long long n = (long long)a.HW * a.per;
-    m1 /= (float)n;
-    m2 /= (float)n;
-    __syncthreads();  // dx may be dy
-    for (long long i = threadIdx.x; i < n; i += kNormThreads) {
-        const int c = (int)(i % a.per);
-        const float gamma = a.gamma ? a.gamma[c0 + c] : 1.f, beta = a.gamma ? a.beta[c0 + c] : 0.f;
-        float xhat, dz;
-        f.at(i / a.per * a.ldx + c, i / a.per * a.ldy + c, gamma, beta, xhat, dz);
-        dx[i / a.per * a.ldx + c] = from_f32<T>(f.rstd * (gamma * dz - m1 - xhat * m2));
+    auto get = [&](int i, float *f) {
+        Vec<T> v;
+        v.raw = cl.keep ? kept[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(x + i * sx);
+        v.get(f);
+    };
+    // mean and squares about it of this thread's values, then of the block's, then of the image's
+    float m[K], q[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) m[k] = q[k] = 0.f;
+    for (int i = 0; i < cnt; ++i) {
+        float f[N];
+        get(i, f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) m[k / M] += f[k];
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) m[k] = cnt ? m[k] / (float)(cnt * M) : 0.f;
+    for (int i = 0; i < cnt; ++i) {
+        float f[N];
+        get(i, f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) q[k / M] = fmaf(f[k] - m[k / M], f[k] - m[k / M], q[k / M]);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        tm[tid * K + k] = m[k];
+        tq[tid * K + k] = q[k];
+    }
+    __syncthreads();
+    tc::cluster_wait();  // all blocks of the cluster run
+    for (int g = tid / 32; g < a.groups; g += kThreads / 32) {
+        const Members e = members<N, K>(g, a.per);
+        const float total = (float)P * (float)a.per;
+        float sum = 0.f, sq = 0.f;
+        for (int i = tid % 32; i < lanes * e.span; i += 32) {
+            const int p = i / e.span, t = p * VC + e.first + i % e.span;
+            const float w = p < P ? (float)(((P - 1 - p) / lanes + 1) * M) : 0.f;
+            sum = fmaf(w, tm[t * K + e.k], sum);
+        }
+        const float mean = P ? warp_sum(sum) / total : 0.f;
+        for (int i = tid % 32; i < lanes * e.span; i += 32) {
+            const int p = i / e.span, t = p * VC + e.first + i % e.span;
+            const float w = p < P ? (float)(((P - 1 - p) / lanes + 1) * M) : 0.f, d = tm[t * K + e.k] - mean;
+            if (w > 0.f) sq += fmaf(w * d, d, tq[t * K + e.k]);
+        }
+        sq = warp_sum(sq);
+        if (tid % 32 < cl.n) {
+            const uint32_t at = tc::in_cta(tc::smem_u32(sent + (rank * a.groups + g) * 2), tid % 32);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(mean) : "memory");
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(sq) : "memory");
+        }
+    }
+    tc::cluster_sync();
+    for (int g = tid; g < a.groups; g += kThreads) {
+        float mean = 0.f, sq = 0.f;
+        const float per = (float)a.per, n = (float)a.HW * per;
+        for (int r = 0; r < cl.n; ++r) mean = fmaf((float)max(0, min(cl.pixels, a.HW - r * cl.pixels)) * per, sent[(r * a.groups + g) * 2], mean);
+        mean /= n;
+        for (int r = 0; r < cl.n; ++r) {
+            const float w = (float)max(0, min(cl.pixels, a.HW - r * cl.pixels)) * per, d = sent[(r * a.groups + g) * 2] - mean;
+            if (w > 0.f) sq += fmaf(w * d, d, sent[(r * a.groups + g) * 2 + 1]);
+        }
+        const float rstd = 1.f / sqrtf(sq / n + a.eps);
+        stat[g * 2] = mean;
+        stat[g * 2 + 1] = rstd;
+        if (rank == 0) {
+            a.mean[(long long)b * a.groups + g] = mean;
+            a.rstd[(long long)b * a.groups + g] = rstd;
+        }
+    }
+    __syncthreads();
+    if (cnt == 0) return;
+    float mean[K], scale[N], shift[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int c = vc * N + k, g = K == 1 ? c / a.per : vc * K + k / M;
+        const float rstd = stat[g * 2 + 1];
+        mean[k / M] = stat[g * 2];
+        scale[k] = a.gamma ? rstd * a.gamma[c] : rstd;
+        shift[k] = a.gamma ? a.beta[c] : 0.f;
+    }
+#pragma unroll 4
+    for (int i = 0; i < cnt; ++i) {
+        float f[N];
+        get(i, f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] = activate<ACT>(fmaf(f[k] - mean[k / M], scale[k], shift[k]));
+        Vec<T> v;
+        v.set(f);
+        *reinterpret_cast<uint4 *>(y + i * sy) = v.raw;
     }
 }
 
-// Sums over the images, a thread per channel.
-__global__ void __launch_bounds__(128) norm_sum_kernel(const float *part, int B, int C, float *dgamma, float *dbeta, int accumulate) {
+template <typename T, int ACT, int K>
+__global__ void __launch_bounds__(kThreads) norm_bwd_cluster_kernel(NormArgs a, Cluster cl) {
     grid_wait();
-    const int c = blockIdx.x * 128 + threadIdx.x;
-    if (c >= C) return;
-    for (int k = 0; k < 2; ++k) {
-        double s = 0;
-        for (int b = 0; b < B; ++b) s += part[((size_t)k * B + b) * C + c];
+    tc::cluster_arrive();
+    constexpr int N = Vec<T>::N, M = N / K;
+    extern __shared__ __align__(16) float mem[];
+    float *ts = mem, *chan = ts + kThreads * 2 * N, *sent = chan + 2 * a.C, *stat = sent + (cl.n * a.groups * 2 + 3) / 4 * 4;
+    uint4 *keptx = reinterpret_cast<uint4 *>(stat + (a.groups * 2 + 3) / 4 * 4);
+    const int rank = blockIdx.x % cl.n, b = blockIdx.x / cl.n;
+    const int VC = a.C / N, lanes = kThreads / VC, tid = threadIdx.x, pl = tid / VC, vc = tid % VC;
+    const int p0 = rank * cl.pixels, P = max(0, min(cl.pixels, a.HW - p0)), rounds = (cl.pixels + lanes - 1) / lanes;
+    uint4 *keptd = keptx + rounds * kThreads;
+    const int cnt = pl < lanes && pl < P ? (P - 1 - pl) / lanes + 1 : 0;
+    const long long px = ((long long)b * a.HW + p0 + pl) * a.ldx + vc * N, py = ((long long)b * a.HW + p0 + pl) * a.ldy + vc * N;
+    const T *x = static_cast<const T *>(a.x) + px, *dy = static_cast<const T *>(a.dy) + py;
+    T *dx = static_cast<T *>(a.dx) + px;
+    const long long sx = lanes * a.ldx, sy = lanes * a.ldy;
+    if (cl.keep) {
+        for (int i = 0; i < cnt; ++i) {
+            tc::cp_async16(tc::smem_u32(keptx + i * kThreads + tid), x + i * sx, true);
+            tc::cp_async16(tc::smem_u32(keptd + i * kThreads + tid), dy + i * sy, true);
+        }
+        tc::cp_async_commit();
+    }
+    float mean[K], rstd[K], gamma[N], beta[N], s1[N], s2[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int c = min(vc * N + k, a.C - 1), g = K == 1 ? c / a.per : vc * K + k / M;
+        mean[k / M] = a.mean[(long long)b * a.groups + g];
+        rstd[k / M] = a.rstd[(long long)b * a.groups + g];
+        gamma[k] = a.gamma ? a.gamma[c] : 1.f;
+        beta[k] = a.gamma ? a.beta[c] : 0.f;
+        s1[k] = s2[k] = 0.f;
+    }
+    if (cl.keep) tc::cp_async_wait<0>();
+    auto get = [&](int i, float *f, float *e) {
+        Vec<T> v, d;
+        v.raw = cl.keep ? keptx[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(x + i * sx);
+        d.raw = cl.keep ? keptd[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(dy + i * sy);
+        v.get(f);
+        d.get(e);
+    };
+    for (int i = 0; i < cnt; ++i) {
+        float f[N], e[N];
+        get(i, f, e);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float xc = f[k] - mean[k / M];
+            const float dz = grad_z<ACT>(e[k], xc, {rstd[k / M] * gamma[k], beta[k]}, f[k], mean[k / M], rstd[k / M], gamma[k]);
+            s1[k] += dz;
+            s2[k] = fmaf(dz, xc, s2[k]);
+        }
+    }
+    // [2][N][threads]
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        ts[k * kThreads + tid] = s1[k];
+        ts[(N + k) * kThreads + tid] = s2[k] * rstd[k / M];
+    }
+    __syncthreads();
+    tc::cluster_wait();  // all blocks of the cluster run
+    int sub = 1;  // lanes per channel and sum
+    while (sub < 32 && sub * 2 * 2 * a.C <= kThreads) sub *= 2;
+    for (int i0 = 0; i0 < 2 * a.C; i0 += kThreads / sub) {
+        const int i = i0 + tid / sub, k2 = i / a.C, c = i % a.C;
+        float s = 0.f;
+        if (i < 2 * a.C)
+            for (int p = tid % sub; p < lanes; p += sub) s += ts[(k2 * N + c % N) * kThreads + p * VC + c / N];
+        s = lanes_sum(s, sub);
+        if (i < 2 * a.C && tid % sub == 0) {
+            chan[i] = s;
+            if (a.part) a.part[((size_t)blockIdx.x * 2 + 1 - k2) * a.C + c] = s;  // gamma's first
+        }
+    }
+    __syncthreads();
+    for (int g = tid / 32; g < a.groups; g += kThreads / 32) {
+        float m1 = 0.f, m2 = 0.f;
+        for (int c = g * a.per + tid % 32; c < (g + 1) * a.per; c += 32) {
+            const float w = a.gamma ? a.gamma[c] : 1.f;
+            m1 = fmaf(w, chan[c], m1);
+            m2 = fmaf(w, chan[a.C + c], m2);
+        }
+        m1 = warp_sum(m1);
+        m2 = warp_sum(m2);
+        if (tid % 32 < cl.n) {
+            const uint32_t at = tc::in_cta(tc::smem_u32(sent + (rank * a.groups + g) * 2), tid % 32);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(m1) : "memory");
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(m2) : "memory");
+        }
+    }
+    tc::cluster_sync();
+    for (int g = tid; g < a.groups; g += kThreads) {
+        float m1 = 0.f, m2 = 0.f;
+        for (int r = 0; r < cl.n; ++r) {
+            m1 += sent[(r * a.groups + g) * 2];
+            m2 += sent[(r * a.groups + g) * 2 + 1];
+        }
+        const float n = (float)a.HW * (float)a.per;
+        stat[g * 2] = m1 / n;
+        stat[g * 2 + 1] = m2 / n;
+    }
+    __syncthreads();
+    if (cnt == 0) return;
+    // dx = A dz + (D xc + E)
+    float D[K], E[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int g = K == 1 ? vc * N / a.per : vc * K + k;
+        D[k] = -rstd[k] * rstd[k] * stat[g * 2 + 1];
+        E[k] = -rstd[k] * stat[g * 2];
+    }
+#pragma unroll 2
+    for (int i = 0; i < cnt; ++i) {
+        float f[N], e[N];
+        get(i, f, e);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float xc = f[k] - mean[k / M], scale = rstd[k / M] * gamma[k];
+            const float dz = grad_z<ACT>(e[k], xc, {scale, beta[k]}, f[k], mean[k / M], rstd[k / M], gamma[k]);
+            f[k] = fmaf(scale, dz, fmaf(D[k / M], xc, E[k / M]));
+        }
+        Vec<T> v;
+        v.set(f);
+        *reinterpret_cast<uint4 *>(dx + i * sx) = v.raw;
+    }
+}
+
+// Sums of the shares, in a fixed order: 32 channels per block, 16 warps with every 16th share each.
+__global__ void __launch_bounds__(512) norm_sum_kernel(const float *part, int parts, int C, float *dgamma, float *dbeta, int accumulate) {
+    grid_wait();
+    __shared__ double sum[16][33];
+    const int c = blockIdx.x * 32 + threadIdx.x % 32, w = threadIdx.x / 32, k = blockIdx.y;
+    double s = 0;
+    if (c < C)
+        for (int i = w; i < parts; i += 16) s += part[((size_t)i * 2 + k) * C + c];
+    sum[w][threadIdx.x % 32] = s;
+    __syncthreads();
+    if (w == 0 && c < C) {
+        for (int i = 1; i < 16; ++i) s += sum[i][threadIdx.x];
         float *out = k == 0 ? dgamma : dbeta;
         out[c] = (float)(s + (accumulate ? (double)out[c] : 0.));
     }
+}
+
+// ---- which kernel ----
+
+struct Plan {
+    enum { ANY, SMALL, CLUSTER } kind;
+    int lanes, nv, blocks;  // SMALL: lanes per group, vectors per lane, blocks along the images (backward)
+    int K;                  // CLUSTER
+    Cluster cl;
+    int parts;              // shares of the gradients of gamma and beta
+};
+
+// By sizes alone (so that the workspace is known before the addresses are); rows that turn out not to be aligned take the kernels
+// for any alignment, whose shares (one per image) fit in the same workspace.
+Plan plan_of(const ppo_group_norm_desc *d, bool bwd) {
+    Plan p = {};
+    const int size = (int)elem_bytes(d->dtype), N = 16 / size, per = d->C / d->groups;
+    p.kind = Plan::ANY;
+    p.parts = d->B;
+    if (d->C % N != 0 || d->ldx % N != 0 || d->ldy % N != 0) return p;
+    const long long all = (long long)d->HW * per / N;  // vectors of an image and group
+    const int vecs = per / N;
+    if (per % N == 0 && vecs <= 32 && (vecs & (vecs - 1)) == 0 && all <= 32 * 4) {
+        int lanes = vecs;
+        while (lanes < 32 && lanes < all) lanes *= 2;
+        p.kind = Plan::SMALL;
+        p.lanes = lanes;
+        p.nv = all <= lanes ? 1 : all <= 2 * lanes ? 2 : 4;
+        const int columns = ppo_cdiv(d->groups, kThreads / lanes);
+        p.blocks = ppo_cdiv(4 * 148, columns);
+        if (p.blocks > d->B) p.blocks = d->B;
+        p.parts = p.blocks;
+        return p;
+    }
+    p.K = per % N == 0 ? 1 : N % per == 0 ? N / per : 0;
+    const int VC = d->C / N;
+    if (p.K == 0 || VC > kThreads || d->groups > 2048) return p;
+    p.kind = Plan::CLUSTER;
+    const int lanes = kThreads / VC;
+    auto smem = [&](int n, int keep) {
+        const int pixels = ppo_cdiv(d->HW, n), rounds = ppo_cdiv(pixels, lanes);
+        const size_t floats = (bwd ? kThreads * 2 * N + 2 * d->C : kThreads * p.K * 2) + ((size_t)n * d->groups * 2 + 3) / 4 * 4 + (d->groups * 2 + 3) / 4 * 4;
+        return floats * 4 + 16 + (keep ? (size_t)rounds * kThreads * 16 * (bwd ? 2 : 1) : 0);
+    };
+    // as few blocks per image as leave room for two on an SM, else for one
+    int n = 1;
+    while (n < 8 && smem(n, 1) > 110 * 1024) n *= 2;
+    const int keep = smem(n, 1) <= 220 * 1024;
+    p.cl = {n, ppo_cdiv(d->HW, n), keep, smem(n, keep)};
+    p.parts = d->B * n;
+    return p;
+}
+
+template <typename T, typename F>
+int with_act(int act, F &&fn) {
+    if (act == PPO_ACT_RELU) return fn(T{}, std::integral_constant<int, PPO_ACT_RELU>{});
+    if (act == PPO_ACT_SILU) return fn(T{}, std::integral_constant<int, PPO_ACT_SILU>{});
+    return fn(T{}, std::integral_constant<int, PPO_ACT_NONE>{});
+}
+template <typename F>
+int with_elem_act(int dtype, int act, F &&fn) {
+    if (dtype == PPO_F32) return with_act<float>(act, fn);
+    if (dtype == PPO_BF16) return with_act<bf16>(act, fn);
+    return with_act<__half>(act, fn);
+}
+
+// In clusters, with more shared memory than a kernel has by itself.
+template <auto FN>
+int launch_cluster(const NormArgs &a, const Cluster &cl, cudaStream_t st) {
+    static PerDevice<bool> allowed;
+    PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(FN, 227 * 1024); }));
+    return ppo_launch_cluster(FN, cl.n, dim3((unsigned)(a.B * cl.n)), dim3(kThreads), cl.smem, st, a, cl);
 }
 
 int check(const ppo_group_norm_desc *d) {
     if (!d || d->B <= 0 || d->HW <= 0 || d->C <= 0 || d->groups <= 0) return PPO_ERR_INVALID_ARG;
     if (d->act < PPO_ACT_NONE || d->act > PPO_ACT_SILU || d->dtype < PPO_F32 || d->dtype > PPO_F16) return PPO_ERR_INVALID_ARG;
     if (d->C % d->groups != 0 || d->ldx < d->C || d->ldy < d->C) return PPO_ERR_SHAPE;
-    if ((long long)d->B * d->groups > 0x7fffffffll) return PPO_ERR_UNSUPPORTED;
+    if ((long long)d->B * d->groups > 0x7fffffffll || d->B > 0x0fffffff) return PPO_ERR_UNSUPPORTED;
     return PPO_OK;
 }
 
@@ -165,7 +677,8 @@ NormArgs args(const ppo_group_norm_desc *d) {
 
 extern "C" size_t ppo_group_norm_workspace_bytes(const ppo_group_norm_desc *d, int backward) {
     if (check(d) != PPO_OK || !backward) return 0;
-    return (size_t)2 * d->B * d->C * sizeof(float);
+    const int parts = plan_of(d, true).parts;
+    return (size_t)2 * (parts > d->B ? parts : d->B) * d->C * sizeof(float);
 }
 
 extern "C" int ppo_group_norm_fwd(const ppo_group_norm_desc *d, float eps, const void *x, const float *gamma, const float *beta, void *y, float *mean,
@@ -187,8 +700,25 @@ extern "C" int ppo_group_norm_fwd(const ppo_group_norm_desc *d, float eps, const
     a.mean = mean;
     a.rstd = rstd;
     a.eps = eps;
-    return with_elem(d->dtype, [&](auto t) {
-        return ppo_launch(norm_fwd_kernel<decltype(t)>, dim3(d->B * d->groups), dim3(kNormThreads), 0, static_cast<cudaStream_t>(stream), a);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Plan p = plan_of(d, false);
+    if (!ppo_aligned(x, 16) || !ppo_aligned(y, 16)) p.kind = Plan::ANY;
+    return with_elem_act(d->dtype, d->act, [&](auto t, auto act) -> int {
+        using T = decltype(t);
+        constexpr int ACT = decltype(act)::value, N = Vec<T>::N;
+        const dim3 block(kThreads);
+        const long long items = (long long)a.B * a.groups;
+        if (p.kind == Plan::ANY) return ppo_launch(norm_fwd_any_kernel<T, ACT>, dim3((unsigned)items), block, 0, st, a);
+        if (p.kind == Plan::SMALL) {
+            const dim3 grid(ppo_cdiv(items, kThreads / p.lanes));
+            if (p.nv == 1) return ppo_launch(norm_fwd_small_kernel<T, ACT, 1>, grid, block, 0, st, a, p.lanes, items);
+            if (p.nv == 2) return ppo_launch(norm_fwd_small_kernel<T, ACT, 2>, grid, block, 0, st, a, p.lanes, items);
+            return ppo_launch(norm_fwd_small_kernel<T, ACT, 4>, grid, block, 0, st, a, p.lanes, items);
+        }
+        if (p.K == 1) return launch_cluster<norm_fwd_cluster_kernel<T, ACT, 1>>(a, p.cl, st);
+        if (p.K == 2) return launch_cluster<norm_fwd_cluster_kernel<T, ACT, 2>>(a, p.cl, st);
+        if (p.K == 4) return launch_cluster<norm_fwd_cluster_kernel<T, ACT, 4>>(a, p.cl, st);
+        return launch_cluster<norm_fwd_cluster_kernel<T, ACT, N>>(a, p.cl, st);
     });
 }
 
@@ -214,10 +744,28 @@ extern "C" int ppo_group_norm_bwd(const ppo_group_norm_desc *d, const void *x, c
     a.rstd = const_cast<float *>(rstd);
     a.part = dgamma ? static_cast<float *>(workspace) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    PPO_TRY(with_elem(d->dtype, [&](auto t) {
-        return ppo_launch(norm_bwd_kernel<decltype(t)>, dim3(d->B * d->groups), dim3(kNormThreads), 0, st, a);
+    Plan p = plan_of(d, true);
+    if (!ppo_aligned(x, 16) || !ppo_aligned(dy, 16) || !ppo_aligned(dx, 16)) {
+        p.kind = Plan::ANY;
+        p.parts = d->B;
+    }
+    PPO_TRY(with_elem_act(d->dtype, d->act, [&](auto t, auto act) -> int {
+        using T = decltype(t);
+        constexpr int ACT = decltype(act)::value, N = Vec<T>::N;
+        const dim3 block(kThreads);
+        if (p.kind == Plan::ANY) return ppo_launch(norm_bwd_any_kernel<T, ACT>, dim3(a.B * a.groups), block, 0, st, a);
+        if (p.kind == Plan::SMALL) {
+            const dim3 grid(p.blocks, ppo_cdiv(a.groups, kThreads / p.lanes));
+            if (p.nv == 1) return ppo_launch(norm_bwd_small_kernel<T, ACT, 1>, grid, block, 0, st, a, p.lanes);
+            if (p.nv == 2) return ppo_launch(norm_bwd_small_kernel<T, ACT, 2>, grid, block, 0, st, a, p.lanes);
+            return ppo_launch(norm_bwd_small_kernel<T, ACT, 4>, grid, block, 0, st, a, p.lanes);
+        }
+        if (p.K == 1) return launch_cluster<norm_bwd_cluster_kernel<T, ACT, 1>>(a, p.cl, st);
+        if (p.K == 2) return launch_cluster<norm_bwd_cluster_kernel<T, ACT, 2>>(a, p.cl, st);
+        if (p.K == 4) return launch_cluster<norm_bwd_cluster_kernel<T, ACT, 4>>(a, p.cl, st);
+        return launch_cluster<norm_bwd_cluster_kernel<T, ACT, N>>(a, p.cl, st);
     }));
     if (!dgamma) return PPO_OK;
-    return ppo_launch(norm_sum_kernel, dim3(ppo_cdiv(d->C, 128)), dim3(128), 0, st, (const float *)a.part, (int)d->B, (int)d->C, dgamma, dbeta,
+    return ppo_launch(norm_sum_kernel, dim3(ppo_cdiv(d->C, 32), 2), dim3(512), 0, st, (const float *)a.part, p.parts, (int)d->C, dgamma, dbeta,
                       accumulate);
 }
