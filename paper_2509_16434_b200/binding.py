@@ -487,99 +487,129 @@ _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _ACTS = {"none": 0, "relu": 1, "silu": 2}
 
 
-def _refuse(status: int, where: str, ok: bool):
-    if not ok:
-        raise PpoError(status, where)
+# Checks of tensors, in few steps each: a decision of a few envs takes the GPU less than 5 us.
 
 
-def _want(where: str, device, *tensors):
-    """(tensor, type, shape) each: what the pointer is taken to be.  None is passed on; other tensors are dense, on the device
-    the call runs on."""
-    for t, dtype, shape in tensors:
-        if t is not None:
-            _refuse(1, where, t.dtype == dtype and t.device == device)
-            _refuse(2, where, t.shape == shape and t.is_contiguous())
+def _dense(where: str, dev: int, t, dtype, shape):
+    """The address of a dense tensor of that type and shape on device `dev` (-1: host), None of None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise PpoError(1, where)
+    if t.shape != shape or not t.is_contiguous():
+        raise PpoError(2, where)
+    return t.data_ptr()
 
 
-def _here(where: str, t):
-    _refuse(1, where, t.dtype in _DTYPES and (not t.is_cuda or t.device.index == torch.cuda.current_device()))
-    return t.device
-
-
-def _ld(where: str, t, lead: int) -> int:
-    """Elements from one row to the next of a tensor whose last dimensions make up a row, dense, and whose first `lead` dimensions
-    number the rows in order."""
-    inner = 1
-    for n, st in zip(reversed(t.shape[lead:]), reversed(t.stride()[lead:])):
-        _refuse(2, where, n == 1 or st == inner)
-        inner *= n
+def _operand(where: str, dev: int, t, dtype, shape, lead: int):
+    """The address of a tensor, and the elements from one row to the next: its last dimensions make up a row, dense, and its first
+    `lead` ones number the rows in order."""
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise PpoError(1, where)
+    if t.shape != shape:
+        raise PpoError(2, where)
+    row = 1
+    for n in shape[lead:]:
+        row *= n
+    if t.is_contiguous():
+        return t.data_ptr(), row
+    stride, inner = t.stride(), 1
+    for i in range(len(shape) - 1, lead - 1, -1):
+        if shape[i] != 1 and stride[i] != inner:
+            raise PpoError(2, where)
+        inner *= shape[i]
     ld, count = None, 1
-    for n, st in zip(reversed(t.shape[:lead]), reversed(t.stride()[:lead])):
-        if n != 1:
-            ld = st // count if ld is None else ld
-            _refuse(2, where, st == ld * count)
-        count *= n
-    return inner if ld is None else ld
+    for i in range(lead - 1, -1, -1):
+        if shape[i] != 1:
+            ld = stride[i] // count if ld is None else ld
+            if stride[i] != ld * count:
+                raise PpoError(2, where)
+        count *= shape[i]
+    return t.data_ptr(), row if ld is None else ld
 
 
-def _attention_desc(where: str, q, k, v, o, scale: float, lead: int) -> DecayAttentionDesc:
-    device = _here(where, q)
-    rows = tuple(q.shape[:lead])
-    _refuse(2, where, q.dim() == k.dim() == v.dim() == o.dim() == lead + 2)
-    heads, dk, kv, dv = q.shape[-2], q.shape[-1], k.shape[-2], v.shape[-1]
-    for t, shape in ((k, rows + (kv, dk)), (v, rows + (kv, dv)), (o, rows + (heads, dv))):
-        _refuse(1, where, t.dtype == q.dtype and t.device == device)
-        _refuse(2, where, t.shape == shape)
-    T, Be = rows if lead == 2 else (1,) + rows
-    return DecayAttentionDesc(T, Be, heads, kv, dk, dv, _DTYPES[q.dtype], *(_ld(where, t, lead) for t in (q, k, v, o)), scale)
+def _device_of(where: str, t, types) -> int:
+    """The device of the operands, which has to be the one the call runs on."""
+    dev = t.get_device()
+    if t.dtype not in types or (dev >= 0 and dev != torch._C._cuda_getDevice()):
+        raise PpoError(1, where)
+    return dev
+
+
+def _space(where: str, dev: int, t):
+    """Address and bytes of a workspace."""
+    if t is None:
+        return None, 0
+    if t.get_device() != dev or not t.is_contiguous():
+        raise PpoError(1, where)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+_F32, _U8, _I32 = torch.float32, torch.uint8, torch.int32
 
 
 def ppo_decay_attention_workspace_bytes(q, k, v, backward: bool) -> int:
     """Bytes the calls with these q [T,Be,heads,dk], k [T,Be,kv_heads,dk], v [T,Be,kv_heads,dv] need (0: none)."""
     T, Be, heads, dk = q.shape
-    d = DecayAttentionDesc(T, Be, heads, k.shape[2], dk, v.shape[3], _DTYPES[q.dtype], heads * dk, k.shape[2] * dk, k.shape[2] * v.shape[3],
-                           heads * v.shape[3], 1.0)
+    kv, dv = v.shape[2:]
+    d = DecayAttentionDesc(T, Be, heads, kv, dk, dv, _DTYPES[q.dtype], heads * dk, kv * dk, kv * dv, heads * dv, 1.0)
     return lib().ppo_decay_attention_workspace_bytes(C.byref(d), int(backward))
 
 
-def _bytes_of(t) -> int:
-    return 0 if t is None else t.numel() * t.element_size()
+def _attention(where: str, q, k, v, o, scale: float, lead: int):
+    """Descriptor, device, and the addresses of q, k, v, o."""
+    dev, dtype = _device_of(where, q, _DTYPES), q.dtype
+    shape = tuple(q.shape)
+    if len(shape) != lead + 2 or k.dim() != lead + 2 or v.dim() != lead + 2:
+        raise PpoError(2, where)
+    rows, (heads, dk), kv, dv = shape[:lead], shape[lead:], k.shape[lead], v.shape[lead + 1]
+    pq, ldq = _operand(where, dev, q, dtype, shape, lead)
+    pk, ldk = _operand(where, dev, k, dtype, rows + (kv, dk), lead)
+    pv, ldv = _operand(where, dev, v, dtype, rows + (kv, dv), lead)
+    po, ldo = _operand(where, dev, o, dtype, rows + (heads, dv), lead)
+    T, Be = rows if lead == 2 else (1, rows[0])
+    return DecayAttentionDesc(T, Be, heads, kv, dk, dv, _DTYPES[dtype], ldq, ldk, ldv, ldo, scale), dev, pq, pk, pv, po
 
 
 def ppo_decay_attention_fwd(q, k, v, decay, o, done=None, state_in=None, state_out=None, scale: float = 1.0, workspace=None, stream=None):
     """q [T,Be,heads,dk], k [T,Be,kv_heads,dk], v [T,Be,kv_heads,dv] -> o [T,Be,heads,dv] (fp32 or bf16; rows may be parts of wider
     ones); decay fp32 [heads]; done uint8 [T,Be]; states fp32 [Be,heads,dk,dv]."""
     f = "ppo_decay_attention_fwd"
-    d = _attention_desc(f, q, k, v, o, scale, 2)
-    state = (d.Be, d.heads, d.dk, d.dv)
-    _want(f, q.device, (decay, torch.float32, (d.heads,)), (done, torch.uint8, (d.T, d.Be)), (state_in, torch.float32, state),
-          (state_out, torch.float32, state))
-    _check(lib().ppo_decay_attention_fwd(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(decay), _ptr(done), _ptr(state_in), _ptr(o), _ptr(state_out),
-                                         _ptr(workspace), _bytes_of(workspace), _stream(stream)), f)
+    d, dev, pq, pk, pv, po = _attention(f, q, k, v, o, scale, 2)
+    T, Be, heads, dk = q.shape
+    state = (Be, heads, dk, v.shape[3])
+    ws, n = _space(f, dev, workspace)
+    _check(lib().ppo_decay_attention_fwd(C.byref(d), pq, pk, pv, _dense(f, dev, decay, _F32, (heads,)), _dense(f, dev, done, _U8, (T, Be)),
+                                         _dense(f, dev, state_in, _F32, state), po, _dense(f, dev, state_out, _F32, state), ws, n, _stream(stream)), f)
 
 
 def ppo_decay_attention_bwd(q, k, v, decay, do, dq, dk, dv, done=None, state_in=None, dstate_out=None, dstate_in=None, scale: float = 1.0,
                             workspace=None, stream=None):
     """Gradients dq, dk, dv (shaped and strided as q, k, v) and dstate_in from do [T,Be,heads,dv] and dstate_out."""
     f = "ppo_decay_attention_bwd"
-    d = _attention_desc(f, q, k, v, do, scale, 2)
+    d, dev, pq, pk, pv, po = _attention(f, q, k, v, do, scale, 2)
+    out = []
     for t, like, ld in ((dq, q, d.ldq), (dk, k, d.ldk), (dv, v, d.ldv)):
-        _refuse(1, f, t.dtype == q.dtype and t.device == q.device)
-        _refuse(2, f, t.shape == like.shape and _ld(f, t, 2) == ld)
-    state = (d.Be, d.heads, d.dk, d.dv)
-    _want(f, q.device, (decay, torch.float32, (d.heads,)), (done, torch.uint8, (d.T, d.Be)), (state_in, torch.float32, state),
-          (dstate_out, torch.float32, state), (dstate_in, torch.float32, state))
-    _check(lib().ppo_decay_attention_bwd(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(decay), _ptr(done), _ptr(state_in), _ptr(do), _ptr(dstate_out),
-                                         _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dstate_in), _ptr(workspace), _bytes_of(workspace), _stream(stream)), f)
+        p, ldt = _operand(f, dev, t, q.dtype, tuple(like.shape), 2)
+        if ldt != ld:
+            raise PpoError(2, f)
+        out.append(p)
+    T, Be, heads, n = q.shape
+    state = (Be, heads, n, v.shape[3])
+    ws, n = _space(f, dev, workspace)
+    _check(lib().ppo_decay_attention_bwd(C.byref(d), pq, pk, pv, _dense(f, dev, decay, _F32, (heads,)), _dense(f, dev, done, _U8, (T, Be)),
+                                         _dense(f, dev, state_in, _F32, state), po, _dense(f, dev, dstate_out, _F32, state), *out,
+                                         _dense(f, dev, dstate_in, _F32, state), ws, n, _stream(stream)), f)
 
 
 def ppo_decay_attention_step(q, k, v, decay, state, o, start=None, scale: float = 1.0, stream=None):
     """One decision: q [Be,heads,dk], k [Be,kv_heads,dk], v [Be,kv_heads,dv] -> o [Be,heads,dv], state fp32 [Be,heads,dk,dv] in place;
     start uint8 [Be]: envs that start from a zero state."""
     f = "ppo_decay_attention_step"
-    d = _attention_desc(f, q, k, v, o, scale, 1)
-    _want(f, q.device, (decay, torch.float32, (d.heads,)), (start, torch.uint8, (d.Be,)), (state, torch.float32, (d.Be, d.heads, d.dk, d.dv)))
-    _check(lib().ppo_decay_attention_step(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(decay), _ptr(start), _ptr(state), _ptr(o), _stream(stream)), f)
+    d, dev, pq, pk, pv, po = _attention(f, q, k, v, o, scale, 1)
+    Be, heads, dk = q.shape
+    _check(lib().ppo_decay_attention_step(C.byref(d), pq, pk, pv, _dense(f, dev, decay, _F32, (heads,)), _dense(f, dev, start, _U8, (Be,)),
+                                          _dense(f, dev, state, _F32, (Be, heads, dk, v.shape[2])), po, _stream(stream)), f)
 
 
 def ppo_group_norm_workspace_bytes(x, groups: int, backward: bool) -> int:
@@ -589,53 +619,60 @@ def ppo_group_norm_workspace_bytes(x, groups: int, backward: bool) -> int:
     return lib().ppo_group_norm_workspace_bytes(C.byref(d), int(backward))
 
 
-def _norm_desc(where: str, x, groups: int, y, act: str) -> GroupNormDesc:
-    device = _here(where, x)
-    _refuse(1, where, act in _ACTS and y.dtype == x.dtype and y.device == device)
-    _refuse(2, where, x.dim() == 3 and x.shape == y.shape)
-    B, HW, n = x.shape
-    return GroupNormDesc(B, HW, n, groups, _ACTS[act], _DTYPES[x.dtype], _ld(where, x, 2), _ld(where, y, 2))
+def _norm(where: str, x, groups: int, y, act: str):
+    """Descriptor, device, and the addresses of x and y."""
+    dev = _device_of(where, x, _DTYPES)
+    if act not in _ACTS:
+        raise PpoError(1, where)
+    shape = tuple(x.shape)
+    if len(shape) != 3:
+        raise PpoError(2, where)
+    px, ldx = _operand(where, dev, x, x.dtype, shape, 2)
+    py, ldy = _operand(where, dev, y, x.dtype, shape, 2)
+    return GroupNormDesc(*shape, groups, _ACTS[act], _DTYPES[x.dtype], ldx, ldy), dev, shape, px, py
 
 
 def ppo_group_norm_fwd(x, groups: int, gamma, beta, y, mean, rstd, act: str = "none", eps: float = 1e-5, workspace=None, stream=None):
     """x, y [B,HW,C] (fp32, bf16 or fp16; pixels may be parts of wider rows); gamma, beta fp32 [C] or None; mean, rstd fp32
     [B,groups] are written; act: none, relu or silu."""
     f = "ppo_group_norm_fwd"
-    d = _norm_desc(f, x, groups, y, act)
-    _want(f, x.device, (gamma, torch.float32, (d.C,)), (beta, torch.float32, (d.C,)), (mean, torch.float32, (d.B, groups)),
-          (rstd, torch.float32, (d.B, groups)))
-    _check(lib().ppo_group_norm_fwd(C.byref(d), eps, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd), _ptr(workspace),
-                                    _bytes_of(workspace), _stream(stream)), f)
+    d, dev, (B, _, n), px, py = _norm(f, x, groups, y, act)
+    ws, size = _space(f, dev, workspace)
+    _check(lib().ppo_group_norm_fwd(C.byref(d), eps, px, _dense(f, dev, gamma, _F32, (n,)), _dense(f, dev, beta, _F32, (n,)), py,
+                                    _dense(f, dev, mean, _F32, (B, groups)), _dense(f, dev, rstd, _F32, (B, groups)), ws, size, _stream(stream)), f)
 
 
 def ppo_group_norm_bwd(x, groups: int, gamma, beta, mean, rstd, dy, dx, dgamma=None, dbeta=None, act: str = "none", accumulate: bool = False,
                        workspace=None, stream=None):
     """dx (strided as x) and, unless they are None, dgamma and dbeta fp32 [C] (added to where accumulate) from dy."""
     f = "ppo_group_norm_bwd"
-    d = _norm_desc(f, x, groups, dy, act)
-    _refuse(1, f, dx.dtype == x.dtype and dx.device == x.device)
-    _refuse(2, f, dx.shape == x.shape and _ld(f, dx, 2) == d.ldx)
-    _want(f, x.device, (gamma, torch.float32, (d.C,)), (beta, torch.float32, (d.C,)), (mean, torch.float32, (d.B, groups)),
-          (rstd, torch.float32, (d.B, groups)), (dgamma, torch.float32, (d.C,)), (dbeta, torch.float32, (d.C,)))
-    _check(lib().ppo_group_norm_bwd(C.byref(d), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(dx), _ptr(dgamma),
-                                    _ptr(dbeta), int(accumulate), _ptr(workspace), _bytes_of(workspace), _stream(stream)), f)
+    d, dev, shape, px, py = _norm(f, x, groups, dy, act)
+    B, _, n = shape
+    pd, ldd = _operand(f, dev, dx, x.dtype, shape, 2)
+    if ldd != d.ldx:
+        raise PpoError(2, f)
+    ws, size = _space(f, dev, workspace)
+    _check(lib().ppo_group_norm_bwd(C.byref(d), px, _dense(f, dev, gamma, _F32, (n,)), _dense(f, dev, beta, _F32, (n,)),
+                                    _dense(f, dev, mean, _F32, (B, groups)), _dense(f, dev, rstd, _F32, (B, groups)), py, pd,
+                                    _dense(f, dev, dgamma, _F32, (n,)), _dense(f, dev, dbeta, _F32, (n,)), int(accumulate), ws, size, _stream(stream)), f)
 
 
-def _token_desc(where: str, logits, tokens, scale: float) -> TokenDesc:
-    device = _here(where, logits)
-    _refuse(2, where, logits.dim() == 2)
-    rows, vocab = logits.shape
-    _want(where, device, (tokens, torch.int32, (rows,)))
-    return TokenDesc(rows, vocab, _DTYPES[logits.dtype], _ld(where, logits, 1), scale)
+def _token(where: str, logits, scale: float):
+    """Descriptor, device, the shape of a row's scalar, and the address of the logits."""
+    dev, shape = _device_of(where, logits, _DTYPES), tuple(logits.shape)
+    if len(shape) != 2:
+        raise PpoError(2, where)
+    p, ld = _operand(where, dev, logits, logits.dtype, shape, 1)
+    return TokenDesc(*shape, _DTYPES[logits.dtype], ld, scale), dev, shape[:1], p
 
 
 def ppo_token_logp(logits, tokens, logp, entropy=None, scale: float = 1.0, stream=None):
     """logits [rows,vocab] (fp32, bf16 or fp16; rows may be parts of wider ones), tokens int32 [rows] -> logp, entropy fp32 [rows] of
     the distributions of scale * logits."""
     f = "ppo_token_logp"
-    d = _token_desc(f, logits, tokens, scale)
-    _want(f, logits.device, (logp, torch.float32, (d.rows,)), (entropy, torch.float32, (d.rows,)))
-    _check(lib().ppo_token_logp(C.byref(d), _ptr(logits), _ptr(tokens), _ptr(logp), _ptr(entropy), _stream(stream)), f)
+    d, dev, row, p = _token(f, logits, scale)
+    _check(lib().ppo_token_logp(C.byref(d), p, _dense(f, dev, tokens, _I32, row), _dense(f, dev, logp, _F32, row), _dense(f, dev, entropy, _F32, row),
+                                _stream(stream)), f)
 
 
 def ppo_token_loss_workspace_bytes(logits) -> int:
@@ -650,13 +687,11 @@ def ppo_token_loss_fwd_bwd(logits, tokens, logp_old, adv, B_total: int, dlogits,
     """Clipped policy loss over logits [rows,vocab] with its gradient in dlogits (may be logits); logp_old, adv, logp_ref, weight,
     logp_out fp32 [rows]; loss_out fp32 [5] = L_pi, KL, H, mean(old - logp), clip fraction (added to where accumulate)."""
     f = "ppo_token_loss_fwd_bwd"
-    d = _token_desc(f, logits, tokens, scale)
-    row = (d.rows,)
-    _refuse(1, f, dlogits.dtype == logits.dtype and dlogits.device == logits.device)
-    _refuse(2, f, dlogits.shape == logits.shape)
-    _want(f, logits.device, (logp_old, torch.float32, row), (adv, torch.float32, row), (logp_ref, torch.float32, row), (weight, torch.float32, row),
-          (logp_out, torch.float32, row), (loss_out, torch.float32, (5,)))
+    d, dev, row, p = _token(f, logits, scale)
+    pg, ldg = _operand(f, dev, dlogits, logits.dtype, tuple(logits.shape), 1)
     c = TokenLossCoef(clip_low, clip_high, kl_coef, ent_coef, grad_scale, B_total)
-    _check(lib().ppo_token_loss_fwd_bwd(C.byref(d), C.byref(c), _ptr(logits), _ptr(tokens), _ptr(logp_old), _ptr(logp_ref), _ptr(adv), _ptr(weight),
-                                        _ptr(dlogits), _ld(f, dlogits, 1), _ptr(logp_out), _ptr(loss_out), int(accumulate), _ptr(workspace),
-                                        _bytes_of(workspace), _stream(stream)), f)
+    ws, size = _space(f, dev, workspace)
+    _check(lib().ppo_token_loss_fwd_bwd(C.byref(d), C.byref(c), p, _dense(f, dev, tokens, _I32, row), _dense(f, dev, logp_old, _F32, row),
+                                        _dense(f, dev, logp_ref, _F32, row), _dense(f, dev, adv, _F32, row), _dense(f, dev, weight, _F32, row), pg, ldg,
+                                        _dense(f, dev, logp_out, _F32, row), _dense(f, dev, loss_out, _F32, (5,)), int(accumulate), ws, size,
+                                        _stream(stream)), f)

@@ -9,6 +9,7 @@
 // in front of it: the gradient of the state that is left enters the last step undecayed, that of the state that came in
 // leaves the first one decayed.
 #include "elem.cuh"
+#include "tcgen05.cuh"
 
 namespace {
 
@@ -137,6 +138,331 @@ __global__ void __launch_bounds__(128) sweep_kernel(Sweep s) {
 
 // decay ** n
 __device__ __forceinline__ float power(float log2_decay, int n) { return n == 0 ? 1.f : exp2f((float)n * log2_decay); }
+
+// ---- chunks of 64 steps on the tensor cores (bf16) ----
+//
+// Within a chunk of n steps, with i and j counted from its first one, w_ij = lambda^(i-j) and M the state in front of it,
+//   out_i = sum_{j <= i} w_ij (x_i . a_j) b_j + lambda^(i+1) x_i^T M,    M <- lambda^n M + sum_j lambda^(n-1-j) a_j b_j^T
+// (backwards one power less in the second and one more in the last term); terms with a reset between j and i, or between M and
+// i, fall away.  Four products of 64-row tiles; the state stays in registers in 32 bits, 64 of its columns per block.
+// Rounded to bf16: the weights w_ij (x_i . a_j), and the state where x reads it, whose errors of half a step, 2^-9 relative on
+// average less, stay next to that of the output itself.  lambda^.. a_j is not: as one bf16 number it would leave 2^-9 in a state
+// that is handed out in 32 bits; three terms that sum up to 24 bits are exact to 2^-25, and two (2^-17) do where only outputs of
+// bf16 come of it.
+// A product has no masked places: 0 times a NaN of a later step would reach an earlier one, or stay behind a reset.  So chunks that
+// hold an infinity or a NaN are taken step by step, each as a chunk of its own.
+
+constexpr int kChunk = 64, kBlockCols = 64;
+
+__device__ __forceinline__ void mma_bf16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldsm(uint32_t *r, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t *r, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ float low(uint32_t p) { return __uint_as_float(p << 16); }
+__device__ __forceinline__ float high(uint32_t p) { return __uint_as_float(p & 0xFFFF0000u); }
+__device__ __forceinline__ bool not_finite(uint4 v) {  // one of eight bf16 numbers
+    bool bad = false;
+    for (uint32_t w : {v.x, v.y, v.z, v.w}) bad |= (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
+    return bad;
+}
+
+// Shared memory: per stage the tiles of X and A [64][RB + 8] and B [64][72] (rows padded by 16 bytes: ldmatrix without bank
+// conflicts), then M [RB][72], all bf16, then the powers of the decay.
+template <int RB>
+struct ChunkSmem {
+    static constexpr int kRow = RB + 8, kCol = kBlockCols + 8;
+    static constexpr int kWide = kChunk * kRow * 2, kNarrow = kChunk * kCol * 2, kStage = 2 * kWide + kNarrow, kState = RB * kCol * 2;
+    static constexpr int bytes(int stages) { return stages * kStage + kState + 80 * 4; }
+};
+
+// RB: rows of the state, padded (64 or 128).  STATE: only what the segment leaves, from an empty state.  TERMS: of the weighted a.
+template <int RB, bool STATE, int TERMS>
+__global__ void __launch_bounds__(128, RB == 64 ? 4 : 2) chunk_kernel(Sweep s, int stages) {
+    grid_wait();
+    using L = ChunkSmem<RB>;
+    constexpr int MT = RB / 64, KR = RB / 16;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const uint32_t base = tc::smem_u32(smem);
+    uint8_t *ms = smem + stages * L::kStage;
+    const uint32_t ms_at = base + stages * L::kStage;
+    float *pow = reinterpret_cast<float *>(ms + L::kState);
+    const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index(), g = lane / 4, t4 = lane % 4;
+    const int ncol = (s.C + kBlockCols - 1) / kBlockCols, c0 = blockIdx.x % ncol * kBlockCols, cols = min(kBlockCols, s.C - c0);
+    const int eh = blockIdx.x / ncol, e = eh / s.heads, h = eh % s.heads, seg = blockIdx.y;
+    const bf16 *A = static_cast<const bf16 *>(s.a) + (long long)(h / s.share_a) * s.R;
+    const bf16 *B = static_cast<const bf16 *>(s.b) + (long long)(h / s.share_b) * s.C + c0;
+    const bf16 *X = static_cast<const bf16 *>(s.x) + (long long)(h / s.share_x) * s.R;
+    const int rev = s.reverse;
+    if (tid < 66) pow[tid] = power(log2f(s.decay[h]), tid);
+
+    // the state: rows 64 m + 16 w + g (+ 8), columns 8 n + 2 t4 (+ 1)
+    const long long sr = s.nseg > 1 ? s.C : s.stride_r, sc = s.nseg > 1 ? 1 : s.stride_c;
+    const float *in = STATE ? nullptr : s.nseg > 1 ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.m_in ? s.m_in + eh * s.state : nullptr;
+    float *out_state = STATE ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.nseg > 1 || !s.m_out ? nullptr : s.m_out + eh * s.state;
+    float M[MT][8][4];
+    auto at_state = [&](auto &&fn) {  // every place of the state that this thread holds, columns in pairs
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = 64 * m + 16 * w + g + 8 * i, c = 8 * n + 2 * t4;
+                    fn(M[m][n][2 * i], M[m][n][2 * i + 1], r < s.R && c < cols, r < s.R && c + 1 < cols, r * sr + (c0 + c) * sc);
+                }
+    };
+    const bool pairs = sc == 1 && (sr & 1) == 0 && (s.C & 1) == 0;  // pairs of columns are 8 aligned bytes
+    at_state([&](float &m0, float &m1, bool ok0, bool ok1, long long at) {
+        if (pairs) {
+            const float2 f = in && ok0 ? *reinterpret_cast<const float2 *>(in + at) : make_float2(0.f, 0.f);
+            m0 = f.x, m1 = f.y;
+        } else {
+            m0 = in && ok0 ? in[at] : 0.f;
+            m1 = in && ok1 ? in[at + sc] : 0.f;
+        }
+    });
+    bool filled = in != nullptr;  // M holds something
+
+    const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
+    // Rows first .. first + count of the sweep into rows 0 .. of a stage, zeros behind them and behind R and C.
+    auto copy = [&](int stage, int first, int count) {
+        const uint32_t to = base + stage * L::kStage;
+        constexpr int WV = RB / 8, NV = kBlockCols / 8;
+#pragma unroll
+        for (int k = 0; k < kChunk * WV / 128; ++k) {
+            const int i = k * 128 + tid, j = i / WV, v = i % WV, t = rev ? s.T - 1 - (first + j) : first + j;
+            const bool ok = j < count && v * 8 < s.R;
+            const long long row = ok ? (long long)t * s.Be + e : 0;
+            if (!STATE) tc::cp_async16(to + (j * L::kRow + v * 8) * 2, ok ? X + row * s.ldx + v * 8 : X, ok);
+            tc::cp_async16(to + L::kWide + (j * L::kRow + v * 8) * 2, ok ? A + row * s.lda + v * 8 : A, ok);
+        }
+#pragma unroll
+        for (int k = 0; k < kChunk * NV / 128; ++k) {
+            const int i = k * 128 + tid, j = i / NV, v = i % NV, t = rev ? s.T - 1 - (first + j) : first + j;
+            const bool ok = j < count && v * 8 < cols;
+            const long long row = ok ? (long long)t * s.Be + e : 0;
+            tc::cp_async16(to + 2 * L::kWide + (j * L::kCol + v * 8) * 2, ok ? B + row * s.ldb + v * 8 : B, ok);
+        }
+        tc::cp_async_commit();
+    };
+    // What this thread has copied.
+    auto odd = [&](int stage) {
+        const uint8_t *from = smem + stage * L::kStage;
+        constexpr int WV = RB / 8, NV = kBlockCols / 8;
+        bool bad = false;
+#pragma unroll
+        for (int k = 0; k < kChunk * WV / 128; ++k) {
+            const int i = k * 128 + tid, at = (i / WV * L::kRow + i % WV * 8) * 2;
+            if (!STATE) bad |= not_finite(*reinterpret_cast<const uint4 *>(from + at));
+            bad |= not_finite(*reinterpret_cast<const uint4 *>(from + L::kWide + at));
+        }
+#pragma unroll
+        for (int k = 0; k < kChunk * NV / 128; ++k) {
+            const int i = k * 128 + tid;
+            bad |= not_finite(*reinterpret_cast<const uint4 *>(from + 2 * L::kWide + (i / NV * L::kCol + i % NV * 8) * 2));
+        }
+        return bad;
+    };
+    auto reset_at = [&](int step) { return s.done && step < n1 && s.done[(long long)(rev ? s.T - 1 - step : step) * s.Be + e] != 0; };
+    auto store_ms = [&] {  // M as the operand of the next chunk
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    *reinterpret_cast<uint32_t *>(ms + ((64 * m + 16 * w + g + 8 * i) * L::kCol + 8 * n + 2 * t4) * 2) =
+                        pack_bf16x2(M[m][n][2 * i], M[m][n][2 * i + 1]);
+    };
+
+    // The n steps from `first` on, in rows 0 .. of a stage; resets: bit i set where done is at step first + i.
+    auto process = [&](int stage, int first, int n, unsigned long long resets, bool last) {
+        const uint32_t xs = base + stage * L::kStage, as = xs + L::kWide, bs = xs + 2 * L::kWide;
+        const auto before = [&](int i) { return __popcll(resets & (((1ull << i) << rev) - 1)); };  // resets in front of i
+        if (!STATE && 16 * w < n) {
+            float o[8][4] = {};
+            uint32_t xf[KR][4];
+#pragma unroll
+            for (int k = 0; k < KR; ++k) ldsm(xf[k], xs + ((16 * w + lane % 16) * L::kRow + k * 16 + lane / 16 * 8) * 2);
+            const int i0 = 16 * w + g, i1 = i0 + 8;
+            if (filled) {
+#pragma unroll
+                for (int k = 0; k < KR; ++k)
+#pragma unroll
+                    for (int nn = 0; nn < 4; ++nn) {
+                        uint32_t b[4];
+                        ldsm_t(b, ms_at + ((k * 16 + lane % 16) * L::kCol + nn * 16 + lane / 16 * 8) * 2);
+                        mma_bf16(o[2 * nn], xf[k], b[0], b[1]);
+                        mma_bf16(o[2 * nn + 1], xf[k], b[2], b[3]);
+                    }
+                const bool on0 = resets == 0 || before(i0) == 0, on1 = resets == 0 || before(i1) == 0;
+                const float f0 = pow[i0 + 1 - rev], f1 = pow[i1 + 1 - rev];
+#pragma unroll
+                for (int nn = 0; nn < 8; ++nn) {
+                    o[nn][0] = on0 ? o[nn][0] * f0 : 0.f;
+                    o[nn][1] = on0 ? o[nn][1] * f0 : 0.f;
+                    o[nn][2] = on1 ? o[nn][2] * f1 : 0.f;
+                    o[nn][3] = on1 ? o[nn][3] * f1 : 0.f;
+                }
+            }
+            // 16 steps j at a time, up to the diagonal
+#pragma unroll
+            for (int js = 0; js < 4; ++js) {
+                if (js > w) break;
+                float p[2][4] = {};
+#pragma unroll
+                for (int k = 0; k < KR; ++k) {
+                    uint32_t b[4];
+                    ldsm(b, as + ((js * 16 + lane / 16 * 8 + lane % 8) * L::kRow + k * 16 + lane / 8 % 2 * 8) * 2);
+                    mma_bf16(p[0], xf[k], b[0], b[1]);
+                    mma_bf16(p[1], xf[k], b[2], b[3]);
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const int i = v < 2 ? i0 : i1, j = js * 16 + q * 8 + 2 * t4 + v % 2;
+                        const bool on = i >= j && (resets == 0 || before(i) == before(j));
+                        p[q][v] = on ? p[q][v] * (pow[max(i - j, 0)] * s.a_scale) : 0.f;
+                    }
+                const uint32_t pf[4] = {pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]),
+                                        pack_bf16x2(p[1][2], p[1][3])};
+#pragma unroll
+                for (int nn = 0; nn < 4; ++nn) {
+                    uint32_t b[4];
+                    ldsm_t(b, bs + ((js * 16 + lane % 16) * L::kCol + nn * 16 + lane / 16 * 8) * 2);
+                    mma_bf16(o[2 * nn], pf, b[0], b[1]);
+                    mma_bf16(o[2 * nn + 1], pf, b[2], b[3]);
+                }
+            }
+            if (s.shared) {
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const int i = v ? i1 : i0, t = rev ? s.T - 1 - (first + i) : first + i;
+                    float *to = s.shared + (((long long)t * s.Be + e) * s.heads + h) * s.C + c0;
+                    if (i < n) {
+#pragma unroll
+                        for (int nn = 0; nn < 8; ++nn)
+                            if (8 * nn + 2 * t4 < cols) *reinterpret_cast<float2 *>(to + 8 * nn + 2 * t4) = make_float2(o[nn][2 * v] * s.out_scale, o[nn][2 * v + 1] * s.out_scale);
+                    }
+                }
+            } else {
+                // through this warp's rows of X, which no other warp reads, to whole rows of 16-byte stores
+                uint8_t *mine = smem + stage * L::kStage + 16 * w * L::kRow * 2;
+                __syncwarp();
+#pragma unroll
+                for (int nn = 0; nn < 8; ++nn) {
+                    *reinterpret_cast<uint32_t *>(mine + (g * L::kRow + 8 * nn + 2 * t4) * 2) = pack_bf16x2(o[nn][0] * s.out_scale, o[nn][1] * s.out_scale);
+                    *reinterpret_cast<uint32_t *>(mine + ((g + 8) * L::kRow + 8 * nn + 2 * t4) * 2) = pack_bf16x2(o[nn][2] * s.out_scale, o[nn][3] * s.out_scale);
+                }
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = k * 4 + lane / 8, v = lane % 8, i = 16 * w + r, t = rev ? s.T - 1 - (first + i) : first + i;
+                    if (i < n && v * 8 < cols)
+                        *reinterpret_cast<uint4 *>(static_cast<bf16 *>(s.out) + ((long long)t * s.Be + e) * s.ldo + (long long)h * s.C + c0 + v * 8) =
+                            *reinterpret_cast<const uint4 *>(mine + (r * L::kRow + v * 8) * 2);
+                }
+            }
+        }
+        if (last && !out_state) return;
+        const float keep = pow[n];
+        const int end = __popcll(resets);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int nn = 0; nn < 8; ++nn)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) M[m][nn][v] = resets == 0 ? M[m][nn][v] * keep : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (16 * k >= n) break;
+            float wj[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int j = 16 * k + 2 * t4 + v % 2 + v / 2 * 8;
+                wj[v] = j < n && (resets == 0 || before(j) == end) ? pow[max(n - 1 - j + rev, 0)] * s.a_scale : 0.f;
+            }
+            uint32_t b[4][4];
+#pragma unroll
+            for (int nn = 0; nn < 4; ++nn) ldsm_t(b[nn], bs + ((k * 16 + lane % 16) * L::kCol + nn * 16 + lane / 16 * 8) * 2);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                uint32_t a[4], part[TERMS][4];
+                ldsm_t(a, as + ((k * 16 + lane / 16 * 8 + lane % 8) * L::kRow + 64 * m + 16 * w + lane / 8 % 2 * 8) * 2);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {  // a[v] holds steps 2 t4, 2 t4 + 1 (+ 8 in the upper two)
+                    float f0 = low(a[v]) * wj[v / 2 * 2], f1 = high(a[v]) * wj[v / 2 * 2 + 1];
+                    if (wj[v / 2 * 2] == 0.f) f0 = 0.f;
+                    if (wj[v / 2 * 2 + 1] == 0.f) f1 = 0.f;
+#pragma unroll
+                    for (int q = 0; q < TERMS; ++q) {
+                        part[q][v] = pack_bf16x2(f0, f1);
+                        f0 -= low(part[q][v]);
+                        f1 -= high(part[q][v]);
+                    }
+                }
+#pragma unroll
+                for (int q = TERMS - 1; q >= 0; --q)
+#pragma unroll
+                    for (int nn = 0; nn < 4; ++nn) {
+                        mma_bf16(M[m][2 * nn], part[q], b[nn][0], b[nn][1]);
+                        mma_bf16(M[m][2 * nn + 1], part[q], b[nn][2], b[nn][3]);
+                    }
+            }
+        }
+    };
+
+    copy(0, n0, min(kChunk, n1 - n0));
+    bool flag0 = reset_at(n0 + lane), flag1 = reset_at(n0 + 32 + lane);
+    int stage = 0;
+    for (int n = n0; n < n1; n += kChunk) {
+        const int count = min(kChunk, n1 - n);
+        const bool more = n + kChunk < n1;
+        const unsigned long long resets =
+            (unsigned long long)__ballot_sync(0xffffffffu, flag0) | (unsigned long long)__ballot_sync(0xffffffffu, flag1) << 32;
+        tc::cp_async_wait<0>();
+        if (!STATE && filled) store_ms();
+        const bool bad = __syncthreads_or(odd(stage));
+        if (more) {
+            copy(stage ^ 1, n + kChunk, min(kChunk, n1 - n - kChunk));
+            flag0 = reset_at(n + kChunk + lane);
+            flag1 = reset_at(n + kChunk + 32 + lane);
+        }
+        for (int i = 0; i < (bad ? count : 1); ++i) {
+            if (bad) {
+                __syncthreads();
+                copy(stage, n + i, 1);
+                tc::cp_async_wait<0>();  // the next chunk's with it
+                if (!STATE && filled) store_ms();
+                __syncthreads();
+            }
+            process(stage, n + i, bad ? 1 : count, bad ? resets >> i & 1 : resets, !more && (!bad || i == count - 1));
+            filled = true;
+        }
+        __syncthreads();
+        stage ^= 1;
+    }
+    if (!out_state) return;
+    at_state([&](float &m0, float &m1, bool ok0, bool ok1, long long at) {
+        if (pairs) {
+            if (ok0) *reinterpret_cast<float2 *>(out_state + at) = make_float2(m0, m1);
+        } else {
+            if (ok0) out_state[at] = m0;
+            if (ok1) out_state[at + sc] = m1;
+        }
+    });
+}
 
 // What each segment starts from, in place of what it adds, and the state that is left.
 __global__ void __launch_bounds__(256) segments_kernel(Sweep s) {
@@ -289,13 +615,33 @@ int sweep_launch(const Sweep &s, cudaStream_t st) {
     if (s.R <= 64) return ppo_launch(sweep_kernel<T, 16, STATE>, grid, dim3(128), 0, st, s);
     return ppo_launch(sweep_kernel<T, 32, STATE>, grid, dim3(128), 0, st, s);
 }
+template <int RB, bool STATE, int TERMS>
+int chunk_launch_as(const Sweep &s, cudaStream_t st) {
+    static PerDevice<bool> allowed;
+    PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(chunk_kernel<RB, STATE, TERMS>, ChunkSmem<RB>::bytes(2)); }));
+    const int stages = s.seg_len > kChunk ? 2 : 1;
+    return ppo_launch(chunk_kernel<RB, STATE, TERMS>, dim3(ppo_cdiv(s.C, kBlockCols) * s.Be * s.heads, s.nseg), dim3(128), ChunkSmem<RB>::bytes(stages), st, s,
+                      stages);
+}
+template <bool STATE>
+int chunk_launch(const Sweep &s, bool exact, cudaStream_t st) {
+    if (s.R <= 64) return exact ? chunk_launch_as<64, STATE, 3>(s, st) : chunk_launch_as<64, STATE, 2>(s, st);
+    return exact ? chunk_launch_as<128, STATE, 3>(s, st) : chunk_launch_as<128, STATE, 2>(s, st);
+}
+// Rows of 16-byte vectors.
+bool chunks_fit(const Sweep &s) {
+    const auto rows = [](const void *p, long long ld) { return ppo_aligned(p, 16) && ld % 8 == 0; };
+    return s.R % 8 == 0 && s.C % 8 == 0 && rows(s.a, s.lda) && rows(s.b, s.ldb) && rows(s.x, s.ldx) && (s.shared || rows(s.out, s.ldo));
+}
 template <typename T>
 int sweep(const Sweep &s, cudaStream_t st) {
+    const bool chunks = std::is_same_v<T, bf16> && chunks_fit(s);
     if (s.nseg > 1) {
-        PPO_TRY(sweep_launch<T, true>(s, st));
+        if (chunks) PPO_TRY(chunk_launch<true>(s, s.m_out != nullptr, st));
+        else PPO_TRY(sweep_launch<T, true>(s, st));
         PPO_TRY(ppo_launch(segments_kernel, dim3(s.Be * s.heads, ppo_cdiv((long long)s.R * s.C, 256)), dim3(256), 0, st, s));
     }
-    return sweep_launch<T, false>(s, st);
+    return chunks ? chunk_launch<false>(s, s.nseg == 1 && s.m_out, st) : sweep_launch<T, false>(s, st);
 }
 
 Sweep sweep_of(const ppo_decay_attention_desc *d, const float *decay, const uint8_t *done, float *seg) {

@@ -192,6 +192,36 @@ def test_what_no_step_reaches_changes_nothing():
             assert torch.equal(a[:, [0, 2]], b[:, [0, 2]])
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 40), (24, 104), (5, 7)])
+def test_later_steps_and_those_before_a_reset_reach_nothing(dk, dv, dtype, bad):
+    """Infinities and NaN at some steps: outputs in front of them and behind the next reset are those of finite numbers there."""
+    T = 200
+    c = Case(T, 2, 4, 2, dk, dv, dtype, 0.0)
+    c.done = torch.zeros(T, 2, dtype=torch.uint8, device=DEV)
+    c.done[[20, 70, 71, 150]] = 1
+    for x in (c.q, c.k, c.v, c.do):
+        x[60:66] = 1.0
+        x[110:112] = -1.0
+    (ow, sw), (oa, sa) = plain.attention(*c.args()), plain.attention_abs(*c.args())
+    want, size = (f(*c.args(), c.do, c.ds) for f in (plain.attention, plain.attention_abs))
+    for x in (c.q, c.k, c.v, c.do):
+        x[60:66], x[110:112] = bad, bad
+    o, s = c.fwd()
+    back = c.bwd()
+    # what sees the bad steps: outputs and dq from them on to the next reset, dk and dv from them back to the last one
+    after = [t for t in range(T) if not (60 <= t <= 70 or 110 <= t <= 150)]
+    front = [t for t in range(T) if not (21 <= t < 66 or 72 <= t < 112)]
+    _near(o[after], ow[after], oa[after], T, dk, dtype)
+    _near(s, sw, sa, T, dk, F32)
+    _near(back[0][after], want[0][after], size[0][after], T, dv, dtype)
+    for i in (1, 2):
+        _near(back[i][front], want[i][front], size[i][front], T, 2 * max(dk, dv), dtype)
+    _near(back[3], want[3], size[3], T, dk, F32)
+    assert not bool(torch.isfinite(o[62].float()).any()) and not bool(torch.isfinite(back[1][62].float()).any())
+
+
 def test_many_heads_of_many_envs():
     """More states than a grid has rows, and offsets of the states that pass 32 bits."""
     Be, heads, dk, dv = 5000, 16, 16, 16
