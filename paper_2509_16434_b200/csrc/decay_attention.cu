@@ -186,17 +186,23 @@ struct ChunkSmem {
 };
 
 // RB: rows of the state, padded (64 or 128).  STATE: only what the segment leaves, from an empty state.  TERMS: of the weighted a.
+//
+// Eight warps.  Outputs: warp (wr, wc) has 16 rows of the chunk and 32 columns; the two warps of the same rows both make their
+// weights (a sixth more products than one alone, against an exchange).  State: warp w has 16 rows and all columns where there are
+// 128 rows, else 16 rows and half of the columns.  Two blocks of 256 threads and 128 registers on an SM; with four warps and the
+// whole state in theirs (240 registers) it is two of 128 threads, and an SM issues 1.3 to 1.7 instructions per cycle.
 template <int RB, bool STATE, int TERMS>
-__global__ void __launch_bounds__(128, RB == 64 ? 4 : 2) chunk_kernel(Sweep s, int stages) {
+__global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
     grid_wait();
     using L = ChunkSmem<RB>;
-    constexpr int MT = RB / 64, KR = RB / 16;
+    constexpr int KR = RB / 16, MN = RB == 128 ? 8 : 4;  // 16-row steps of a product over R; column tiles of a warp's state
     extern __shared__ __align__(16) uint8_t smem[];
     const uint32_t base = tc::smem_u32(smem);
     uint8_t *ms = smem + stages * L::kStage;
     const uint32_t ms_at = base + stages * L::kStage;
     float *pow = reinterpret_cast<float *>(ms + L::kState);
     const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index(), g = lane / 4, t4 = lane % 4;
+    const int wr = w % 4, wc = w / 4, mr = RB == 128 ? 16 * w : 16 * wr, mc = RB == 128 ? 0 : 32 * wc;
     const int ncol = (s.C + kBlockCols - 1) / kBlockCols, c0 = blockIdx.x % ncol * kBlockCols, cols = min(kBlockCols, s.C - c0);
     const int eh = blockIdx.x / ncol, e = eh / s.heads, h = eh % s.heads, seg = blockIdx.y;
     const bf16 *A = static_cast<const bf16 *>(s.a) + (long long)(h / s.share_a) * s.R;
@@ -205,23 +211,45 @@ __global__ void __launch_bounds__(128, RB == 64 ? 4 : 2) chunk_kernel(Sweep s, i
     const int rev = s.reverse;
     if (tid < 66) pow[tid] = power(log2f(s.decay[h]), tid);
 
-    // the state: rows 64 m + 16 w + g (+ 8), columns 8 n + 2 t4 (+ 1)
+    const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
+    // Rows first .. first + count of the sweep into rows 0 .. of a stage, zeros behind them and behind R and C.
+    auto copy = [&](int stage, int first, int count) {
+        const uint32_t to = base + stage * L::kStage;
+        constexpr int WV = RB / 8, NV = kBlockCols / 8;
+#pragma unroll
+        for (int k = 0; k < kChunk * WV / 256; ++k) {
+            const int i = k * 256 + tid, j = i / WV, v = i % WV, t = rev ? s.T - 1 - (first + j) : first + j;
+            const bool ok = j < count && v * 8 < s.R;
+            const long long row = ok ? (long long)t * s.Be + e : 0;
+            if (!STATE) tc::cp_async16(to + (j * L::kRow + v * 8) * 2, ok ? X + row * s.ldx + v * 8 : X, ok);
+            tc::cp_async16(to + L::kWide + (j * L::kRow + v * 8) * 2, ok ? A + row * s.lda + v * 8 : A, ok);
+        }
+#pragma unroll
+        for (int k = 0; k < kChunk * NV / 256; ++k) {
+            const int i = k * 256 + tid, j = i / NV, v = i % NV, t = rev ? s.T - 1 - (first + j) : first + j;
+            const bool ok = j < count && v * 8 < cols;
+            const long long row = ok ? (long long)t * s.Be + e : 0;
+            tc::cp_async16(to + 2 * L::kWide + (j * L::kCol + v * 8) * 2, ok ? B + row * s.ldb + v * 8 : B, ok);
+        }
+        tc::cp_async_commit();
+    };
+    copy(0, n0, min(kChunk, n1 - n0));
+
+    // the state: rows mr + g (+ 8), columns mc + 8 n + 2 t4 (+ 1)
     const long long sr = s.nseg > 1 ? s.C : s.stride_r, sc = s.nseg > 1 ? 1 : s.stride_c;
     const float *in = STATE ? nullptr : s.nseg > 1 ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.m_in ? s.m_in + eh * s.state : nullptr;
     float *out_state = STATE ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.nseg > 1 || !s.m_out ? nullptr : s.m_out + eh * s.state;
-    float M[MT][8][4];
+    float M[MN][4];
     auto at_state = [&](auto &&fn) {  // every place of the state that this thread holds, columns in pairs
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 0; n < MN; ++n)
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = 64 * m + 16 * w + g + 8 * i, c = 8 * n + 2 * t4;
-                    fn(M[m][n][2 * i], M[m][n][2 * i + 1], r < s.R && c < cols, r < s.R && c + 1 < cols, r * sr + (c0 + c) * sc);
-                }
+            for (int i = 0; i < 2; ++i) {
+                const int r = mr + g + 8 * i, c = mc + 8 * n + 2 * t4;
+                fn(M[n][2 * i], M[n][2 * i + 1], r < s.R && c < cols, r < s.R && c + 1 < cols, r * sr + (c0 + c) * sc);
+            }
     };
-    const bool pairs = sc == 1 && (sr & 1) == 0 && (s.C & 1) == 0;  // pairs of columns are 8 aligned bytes
+    const bool pairs = sc == 1;  // pairs of columns are 8 aligned bytes: C is a multiple of 8
     at_state([&](float &m0, float &m1, bool ok0, bool ok1, long long at) {
         if (pairs) {
             const float2 f = in && ok0 ? *reinterpret_cast<const float2 *>(in + at) : make_float2(0.f, 0.f);
@@ -233,82 +261,51 @@ __global__ void __launch_bounds__(128, RB == 64 ? 4 : 2) chunk_kernel(Sweep s, i
     });
     bool filled = in != nullptr;  // M holds something
 
-    const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
-    // Rows first .. first + count of the sweep into rows 0 .. of a stage, zeros behind them and behind R and C.
-    auto copy = [&](int stage, int first, int count) {
-        const uint32_t to = base + stage * L::kStage;
-        constexpr int WV = RB / 8, NV = kBlockCols / 8;
-#pragma unroll
-        for (int k = 0; k < kChunk * WV / 128; ++k) {
-            const int i = k * 128 + tid, j = i / WV, v = i % WV, t = rev ? s.T - 1 - (first + j) : first + j;
-            const bool ok = j < count && v * 8 < s.R;
-            const long long row = ok ? (long long)t * s.Be + e : 0;
-            if (!STATE) tc::cp_async16(to + (j * L::kRow + v * 8) * 2, ok ? X + row * s.ldx + v * 8 : X, ok);
-            tc::cp_async16(to + L::kWide + (j * L::kRow + v * 8) * 2, ok ? A + row * s.lda + v * 8 : A, ok);
-        }
-#pragma unroll
-        for (int k = 0; k < kChunk * NV / 128; ++k) {
-            const int i = k * 128 + tid, j = i / NV, v = i % NV, t = rev ? s.T - 1 - (first + j) : first + j;
-            const bool ok = j < count && v * 8 < cols;
-            const long long row = ok ? (long long)t * s.Be + e : 0;
-            tc::cp_async16(to + 2 * L::kWide + (j * L::kCol + v * 8) * 2, ok ? B + row * s.ldb + v * 8 : B, ok);
-        }
-        tc::cp_async_commit();
-    };
-    // What this thread has copied.
+    // Whether what this thread has copied of B holds an infinity or a NaN.  (In X one reaches its own step's output, in A those it is
+    // meant to; the weights that are masked, or zero, are set to zero whatever they come from.)
     auto odd = [&](int stage) {
-        const uint8_t *from = smem + stage * L::kStage;
-        constexpr int WV = RB / 8, NV = kBlockCols / 8;
+        constexpr int NV = kBlockCols / 8;
         bool bad = false;
 #pragma unroll
-        for (int k = 0; k < kChunk * WV / 128; ++k) {
-            const int i = k * 128 + tid, at = (i / WV * L::kRow + i % WV * 8) * 2;
-            if (!STATE) bad |= not_finite(*reinterpret_cast<const uint4 *>(from + at));
-            bad |= not_finite(*reinterpret_cast<const uint4 *>(from + L::kWide + at));
-        }
-#pragma unroll
-        for (int k = 0; k < kChunk * NV / 128; ++k) {
-            const int i = k * 128 + tid;
-            bad |= not_finite(*reinterpret_cast<const uint4 *>(from + 2 * L::kWide + (i / NV * L::kCol + i % NV * 8) * 2));
+        for (int k = 0; k < kChunk * NV / 256; ++k) {
+            const int i = k * 256 + tid;
+            bad |= not_finite(*reinterpret_cast<const uint4 *>(smem + stage * L::kStage + 2 * L::kWide + (i / NV * L::kCol + i % NV * 8) * 2));
         }
         return bad;
     };
     auto reset_at = [&](int step) { return s.done && step < n1 && s.done[(long long)(rev ? s.T - 1 - step : step) * s.Be + e] != 0; };
     auto store_ms = [&] {  // M as the operand of the next chunk
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 0; n < MN; ++n)
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    *reinterpret_cast<uint32_t *>(ms + ((64 * m + 16 * w + g + 8 * i) * L::kCol + 8 * n + 2 * t4) * 2) =
-                        pack_bf16x2(M[m][n][2 * i], M[m][n][2 * i + 1]);
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<uint32_t *>(ms + ((mr + g + 8 * i) * L::kCol + mc + 8 * n + 2 * t4) * 2) = pack_bf16x2(M[n][2 * i], M[n][2 * i + 1]);
     };
 
     // The n steps from `first` on, in rows 0 .. of a stage; resets: bit i set where done is at step first + i.
     auto process = [&](int stage, int first, int n, unsigned long long resets, bool last) {
         const uint32_t xs = base + stage * L::kStage, as = xs + L::kWide, bs = xs + 2 * L::kWide;
         const auto before = [&](int i) { return __popcll(resets & (((1ull << i) << rev) - 1)); };  // resets in front of i
-        if (!STATE && 16 * w < n) {
-            float o[8][4] = {};
+        if (!STATE && 16 * wr < n) {
+            float o[4][4] = {};
             uint32_t xf[KR][4];
 #pragma unroll
-            for (int k = 0; k < KR; ++k) ldsm(xf[k], xs + ((16 * w + lane % 16) * L::kRow + k * 16 + lane / 16 * 8) * 2);
-            const int i0 = 16 * w + g, i1 = i0 + 8;
+            for (int k = 0; k < KR; ++k) ldsm(xf[k], xs + ((16 * wr + lane % 16) * L::kRow + k * 16 + lane / 16 * 8) * 2);
+            const int i0 = 16 * wr + g, i1 = i0 + 8;
             if (filled) {
 #pragma unroll
                 for (int k = 0; k < KR; ++k)
 #pragma unroll
-                    for (int nn = 0; nn < 4; ++nn) {
+                    for (int nn = 0; nn < 2; ++nn) {
                         uint32_t b[4];
-                        ldsm_t(b, ms_at + ((k * 16 + lane % 16) * L::kCol + nn * 16 + lane / 16 * 8) * 2);
+                        ldsm_t(b, ms_at + ((k * 16 + lane % 16) * L::kCol + wc * 32 + nn * 16 + lane / 16 * 8) * 2);
                         mma_bf16(o[2 * nn], xf[k], b[0], b[1]);
                         mma_bf16(o[2 * nn + 1], xf[k], b[2], b[3]);
                     }
                 const bool on0 = resets == 0 || before(i0) == 0, on1 = resets == 0 || before(i1) == 0;
                 const float f0 = pow[i0 + 1 - rev], f1 = pow[i1 + 1 - rev];
 #pragma unroll
-                for (int nn = 0; nn < 8; ++nn) {
+                for (int nn = 0; nn < 4; ++nn) {
                     o[nn][0] = on0 ? o[nn][0] * f0 : 0.f;
                     o[nn][1] = on0 ? o[nn][1] * f0 : 0.f;
                     o[nn][2] = on1 ? o[nn][2] * f1 : 0.f;
@@ -318,7 +315,7 @@ __global__ void __launch_bounds__(128, RB == 64 ? 4 : 2) chunk_kernel(Sweep s, i
             // 16 steps j at a time, up to the diagonal
 #pragma unroll
             for (int js = 0; js < 4; ++js) {
-                if (js > w) break;
+                if (js > wr) break;
                 float p[2][4] = {};
 #pragma unroll
                 for (int k = 0; k < KR; ++k) {
@@ -332,15 +329,22 @@ __global__ void __launch_bounds__(128, RB == 64 ? 4 : 2) chunk_kernel(Sweep s, i
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         const int i = v < 2 ? i0 : i1, j = js * 16 + q * 8 + 2 * t4 + v % 2;
-                        const bool on = i >= j && (resets == 0 || before(i) == before(j));
-                        p[q][v] = on ? p[q][v] * (pow[max(i - j, 0)] * s.a_scale) : 0.f;
+                        p[q][v] = i >= j ? p[q][v] * pow[max(i - j, 0)] : 0.f;
                     }
-                const uint32_t pf[4] = {pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]),
-                                        pack_bf16x2(p[1][2], p[1][3])};
+                if (resets != 0) {
 #pragma unroll
-                for (int nn = 0; nn < 4; ++nn) {
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            if (before(v < 2 ? i0 : i1) != before(js * 16 + q * 8 + 2 * t4 + v % 2)) p[q][v] = 0.f;
+                }
+                const float f = s.a_scale;
+                const uint32_t pf[4] = {pack_bf16x2(p[0][0] * f, p[0][1] * f), pack_bf16x2(p[0][2] * f, p[0][3] * f), pack_bf16x2(p[1][0] * f, p[1][1] * f),
+                                        pack_bf16x2(p[1][2] * f, p[1][3] * f)};
+#pragma unroll
+                for (int nn = 0; nn < 2; ++nn) {
                     uint32_t b[4];
-                    ldsm_t(b, bs + ((js * 16 + lane % 16) * L::kCol + nn * 16 + lane / 16 * 8) * 2);
+                    ldsm_t(b, bs + ((js * 16 + lane % 16) * L::kCol + wc * 32 + nn * 16 + lane / 16 * 8) * 2);
                     mma_bf16(o[2 * nn], pf, b[0], b[1]);
                     mma_bf16(o[2 * nn + 1], pf, b[2], b[3]);
                 }
@@ -349,28 +353,29 @@ __global__ void __launch_bounds__(128, RB == 64 ? 4 : 2) chunk_kernel(Sweep s, i
 #pragma unroll
                 for (int v = 0; v < 2; ++v) {
                     const int i = v ? i1 : i0, t = rev ? s.T - 1 - (first + i) : first + i;
-                    float *to = s.shared + (((long long)t * s.Be + e) * s.heads + h) * s.C + c0;
+                    float *to = s.shared + (((long long)t * s.Be + e) * s.heads + h) * s.C + c0 + wc * 32;
                     if (i < n) {
 #pragma unroll
-                        for (int nn = 0; nn < 8; ++nn)
-                            if (8 * nn + 2 * t4 < cols) *reinterpret_cast<float2 *>(to + 8 * nn + 2 * t4) = make_float2(o[nn][2 * v] * s.out_scale, o[nn][2 * v + 1] * s.out_scale);
+                        for (int nn = 0; nn < 4; ++nn)
+                            if (wc * 32 + 8 * nn + 2 * t4 < cols)
+                                *reinterpret_cast<float2 *>(to + 8 * nn + 2 * t4) = make_float2(o[nn][2 * v] * s.out_scale, o[nn][2 * v + 1] * s.out_scale);
                     }
                 }
             } else {
-                // through this warp's rows of X, which no other warp reads, to whole rows of 16-byte stores
-                uint8_t *mine = smem + stage * L::kStage + 16 * w * L::kRow * 2;
-                __syncwarp();
+                // through the rows of X that only this warp and its neighbour read, to 64-byte rows of 16-byte stores
+                uint8_t *mine = smem + stage * L::kStage + (16 * wr * L::kRow + wc * 32) * 2;
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + wr) : "memory");  // both have read them
 #pragma unroll
-                for (int nn = 0; nn < 8; ++nn) {
+                for (int nn = 0; nn < 4; ++nn) {
                     *reinterpret_cast<uint32_t *>(mine + (g * L::kRow + 8 * nn + 2 * t4) * 2) = pack_bf16x2(o[nn][0] * s.out_scale, o[nn][1] * s.out_scale);
                     *reinterpret_cast<uint32_t *>(mine + ((g + 8) * L::kRow + 8 * nn + 2 * t4) * 2) = pack_bf16x2(o[nn][2] * s.out_scale, o[nn][3] * s.out_scale);
                 }
                 __syncwarp();
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int r = k * 4 + lane / 8, v = lane % 8, i = 16 * w + r, t = rev ? s.T - 1 - (first + i) : first + i;
-                    if (i < n && v * 8 < cols)
-                        *reinterpret_cast<uint4 *>(static_cast<bf16 *>(s.out) + ((long long)t * s.Be + e) * s.ldo + (long long)h * s.C + c0 + v * 8) =
+                for (int k = 0; k < 2; ++k) {
+                    const int r = k * 8 + lane / 4, v = lane % 4, i = 16 * wr + r, t = rev ? s.T - 1 - (first + i) : first + i;
+                    if (i < n && wc * 32 + v * 8 < cols)
+                        *reinterpret_cast<uint4 *>(static_cast<bf16 *>(s.out) + ((long long)t * s.Be + e) * s.ldo + (long long)h * s.C + c0 + wc * 32 + v * 8) =
                             *reinterpret_cast<const uint4 *>(mine + (r * L::kRow + v * 8) * 2);
                 }
             }
@@ -379,51 +384,53 @@ __global__ void __launch_bounds__(128, RB == 64 ? 4 : 2) chunk_kernel(Sweep s, i
         const float keep = pow[n];
         const int end = __popcll(resets);
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int nn = 0; nn < MN; ++nn)
 #pragma unroll
-            for (int nn = 0; nn < 8; ++nn)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) M[m][nn][v] = resets == 0 ? M[m][nn][v] * keep : 0.f;
+            for (int v = 0; v < 4; ++v) M[nn][v] = resets == 0 ? M[nn][v] * keep : 0.f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (16 * k >= n) break;
+            uint32_t a[4], part[TERMS][4];
+            ldsm_t(a, as + ((k * 16 + lane / 16 * 8 + lane % 8) * L::kRow + mr + lane / 8 % 2 * 8) * 2);
             float wj[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int j = 16 * k + 2 * t4 + v % 2 + v / 2 * 8;
                 wj[v] = j < n && (resets == 0 || before(j) == end) ? pow[max(n - 1 - j + rev, 0)] * s.a_scale : 0.f;
             }
-            uint32_t b[4][4];
 #pragma unroll
-            for (int nn = 0; nn < 4; ++nn) ldsm_t(b[nn], bs + ((k * 16 + lane % 16) * L::kCol + nn * 16 + lane / 16 * 8) * 2);
+            for (int v = 0; v < 4; ++v) {  // a[v] holds steps 2 t4, 2 t4 + 1 (+ 8 in the upper two)
+                float f0 = low(a[v]) * wj[v / 2 * 2], f1 = high(a[v]) * wj[v / 2 * 2 + 1];
+                if (wj[v / 2 * 2] == 0.f) f0 = 0.f;
+                if (wj[v / 2 * 2 + 1] == 0.f) f1 = 0.f;
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                uint32_t a[4], part[TERMS][4];
-                ldsm_t(a, as + ((k * 16 + lane / 16 * 8 + lane % 8) * L::kRow + 64 * m + 16 * w + lane / 8 % 2 * 8) * 2);
+                for (int q = 0; q < TERMS; ++q) {
+                    part[q][v] = pack_bf16x2(f0, f1);
+                    f0 -= low(part[q][v]);
+                    f1 -= high(part[q][v]);
+                }
+            }
+            // 16 steps are summed up by themselves and added to the state with a rounding to nearest: the tensor core cuts what it
+            // adds to a larger number off, always downwards, which over thousands of steps shows
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {  // a[v] holds steps 2 t4, 2 t4 + 1 (+ 8 in the upper two)
-                    float f0 = low(a[v]) * wj[v / 2 * 2], f1 = high(a[v]) * wj[v / 2 * 2 + 1];
-                    if (wj[v / 2 * 2] == 0.f) f0 = 0.f;
-                    if (wj[v / 2 * 2 + 1] == 0.f) f1 = 0.f;
+            for (int nn = 0; nn < MN / 2; ++nn) {
+                uint32_t b[4];
+                ldsm_t(b, bs + ((k * 16 + lane % 16) * L::kCol + mc + nn * 16 + lane / 16 * 8) * 2);
+                float s0[4] = {}, s1[4] = {};
 #pragma unroll
-                    for (int q = 0; q < TERMS; ++q) {
-                        part[q][v] = pack_bf16x2(f0, f1);
-                        f0 -= low(part[q][v]);
-                        f1 -= high(part[q][v]);
-                    }
+                for (int q = TERMS - 1; q >= 0; --q) {
+                    mma_bf16(s0, part[q], b[0], b[1]);
+                    mma_bf16(s1, part[q], b[2], b[3]);
                 }
 #pragma unroll
-                for (int q = TERMS - 1; q >= 0; --q)
-#pragma unroll
-                    for (int nn = 0; nn < 4; ++nn) {
-                        mma_bf16(M[m][2 * nn], part[q], b[nn][0], b[nn][1]);
-                        mma_bf16(M[m][2 * nn + 1], part[q], b[nn][2], b[nn][3]);
-                    }
+                for (int v = 0; v < 4; ++v) {
+                    M[2 * nn][v] += s0[v];
+                    M[2 * nn + 1][v] += s1[v];
+                }
             }
         }
     };
 
-    copy(0, n0, min(kChunk, n1 - n0));
     bool flag0 = reset_at(n0 + lane), flag1 = reset_at(n0 + 32 + lane);
     int stage = 0;
     for (int n = n0; n < n1; n += kChunk) {
@@ -573,12 +580,12 @@ __global__ void __launch_bounds__(256) step_kernel(const T *q, const T *k, const
     }
 }
 
+// Segments a sequence is cut into: as many as give the GPU one round of two blocks per SM (64 columns of a head each; the GPU's 148
+// SMs as a constant, so that the size of the workspace does not depend on where it is asked for), none shorter than 256 steps.
 constexpr int kSegment = 256;
-
-// Segments a sequence is cut into: as many as give the GPU two blocks per SM, none shorter than 256 steps.
 int segments(const ppo_decay_attention_desc *d, int *len) {
-    const long long blocks = (long long)d->Be * d->heads;
-    int n = (int)((2 * 148 + blocks - 1) / blocks);
+    const long long blocks = (long long)d->Be * d->heads * ppo_cdiv(d->dk > d->dv ? d->dk : d->dv, 64);
+    int n = blocks < 2 * 148 ? (int)(2 * 148 / blocks) : 1;
     const int most = ppo_cdiv(d->T, kSegment);
     if (n > most) n = most;
     const int per = ppo_cdiv(ppo_cdiv(d->T, n), 64) * 64;
@@ -620,7 +627,7 @@ int chunk_launch_as(const Sweep &s, cudaStream_t st) {
     static PerDevice<bool> allowed;
     PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(chunk_kernel<RB, STATE, TERMS>, ChunkSmem<RB>::bytes(2)); }));
     const int stages = s.seg_len > kChunk ? 2 : 1;
-    return ppo_launch(chunk_kernel<RB, STATE, TERMS>, dim3(ppo_cdiv(s.C, kBlockCols) * s.Be * s.heads, s.nseg), dim3(128), ChunkSmem<RB>::bytes(stages), st, s,
+    return ppo_launch(chunk_kernel<RB, STATE, TERMS>, dim3(ppo_cdiv(s.C, kBlockCols) * s.Be * s.heads, s.nseg), dim3(256), ChunkSmem<RB>::bytes(stages), st, s,
                       stages);
 }
 template <bool STATE>
