@@ -29,6 +29,7 @@ struct Sweep {
     int reverse;
     int seg_len, nseg;   // steps per segment of the sequence (nseg == 1: all)
     float *seg;          // [nseg][Be * heads][R * C]: what each segment adds to a state, then what each starts from
+    int *seg_reset;      // [nseg][Be * heads]: whether a done flag is set in it
 };
 
 constexpr int kTokens = 16, kCols = 32, kSlices = 4;
@@ -59,6 +60,7 @@ __global__ void __launch_bounds__(128) sweep_kernel(Sweep s) {
         M[i] = !STATE && in && r < s.R && c < s.C ? in[r * sr + sc] : 0.f;
     }
     const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
+    int any = 0;
     for (int n = n0; n < n1; n += kTokens) {
         const int cnt = min(kTokens, n1 - n);
         __syncthreads();
@@ -83,6 +85,7 @@ __global__ void __launch_bounds__(128) sweep_kernel(Sweep s) {
         for (int j = 0; j < cnt; ++j) {
             const float b = tb[j][lane];
             const bool empty = gate[j];
+            any |= empty;
             float acc = 0.f;
             if (s.reverse && empty) {
 #pragma unroll
@@ -134,6 +137,7 @@ __global__ void __launch_bounds__(128) sweep_kernel(Sweep s) {
             if (r < s.R) out[r * sr + sc] = M[i];
         }
     }
+    if (STATE && c0 == 0 && threadIdx.x == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any;
 }
 
 // decay ** n
@@ -432,12 +436,14 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
     };
 
     bool flag0 = reset_at(n0 + lane), flag1 = reset_at(n0 + 32 + lane);
+    unsigned long long any = 0;
     int stage = 0;
     for (int n = n0; n < n1; n += kChunk) {
         const int count = min(kChunk, n1 - n);
         const bool more = n + kChunk < n1;
         const unsigned long long resets =
             (unsigned long long)__ballot_sync(0xffffffffu, flag0) | (unsigned long long)__ballot_sync(0xffffffffu, flag1) << 32;
+        any |= resets;
         tc::cp_async_wait<0>();
         if (!STATE && filled) store_ms();
         const bool bad = __syncthreads_or(odd(stage));
@@ -460,6 +466,7 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
         __syncthreads();
         stage ^= 1;
     }
+    if (STATE && c0 == 0 && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any != 0;
     if (!out_state) return;
     at_state([&](float &m0, float &m1, bool ok0, bool ok1, long long at) {
         if (pairs) {
@@ -471,35 +478,222 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
     });
 }
 
+// Sequences of up to 16 steps: one chunk, four warps, and little else than the state to move, so as many blocks on an SM as keep its
+// loads in flight.  Every warp makes the 16 x 16 weights and has 16 columns of the outputs; of the state it has RB / 4 rows.
+template <int RB, int TERMS>
+__global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(Sweep s) {
+    grid_wait();
+    constexpr int kRow = RB + 8, kCol = kBlockCols + 8, KR = RB / 16, MT = RB / 64;
+    __shared__ __align__(16) bf16 xs[16 * kRow], as[16 * kRow], bs[16 * kCol], ms[RB * kCol];
+    __shared__ float pow[20];
+    const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index(), g = lane / 4, t4 = lane % 4;
+    const int ncol = (s.C + kBlockCols - 1) / kBlockCols, c0 = blockIdx.x % ncol * kBlockCols, cols = min(kBlockCols, s.C - c0);
+    const int eh = blockIdx.x / ncol, e = eh / s.heads, h = eh % s.heads, rev = s.reverse, n = s.T;
+    const bf16 *A = static_cast<const bf16 *>(s.a) + (long long)(h / s.share_a) * s.R;
+    const bf16 *B = static_cast<const bf16 *>(s.b) + (long long)(h / s.share_b) * s.C + c0;
+    const bf16 *X = static_cast<const bf16 *>(s.x) + (long long)(h / s.share_x) * s.R;
+
+    // rows 64 m + 16 w + g (+ 8), columns 8 n + 2 t4 (+ 1)
+    const bool pairs = s.stride_c == 1;
+    float M[MT][8][4];
+    auto at_state = [&](auto &&fn) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = 64 * m + 16 * w + g + 8 * i, c = 8 * k + 2 * t4;
+                    fn(M[m][k][2 * i], M[m][k][2 * i + 1], r < s.R && c < cols, r * s.stride_r + (c0 + c) * s.stride_c);
+                }
+    };
+    const float *in = s.m_in ? s.m_in + eh * s.state : nullptr;
+    if (in)
+        at_state([&](float &m0, float &m1, bool ok, long long at) {
+            if (pairs) {
+                const float2 f = ok ? __ldcs(reinterpret_cast<const float2 *>(in + at)) : make_float2(0.f, 0.f);
+                m0 = f.x, m1 = f.y;
+            } else {
+                m0 = ok ? __ldcs(in + at) : 0.f;
+                m1 = ok ? __ldcs(in + at + s.stride_c) : 0.f;
+            }
+        });
+    else at_state([&](float &m0, float &m1, bool, long long) { m0 = m1 = 0.f; });
+
+    auto copy = [&](int first, int count) {  // as in chunk_kernel
+        constexpr int WV = RB / 8, NV = kBlockCols / 8;
+        for (int i = tid; i < 16 * WV; i += 128) {
+            const int j = i / WV, v = i % WV, t = rev ? s.T - 1 - (first + j) : first + j;
+            const bool ok = j < count && v * 8 < s.R;
+            const long long row = ok ? (long long)t * s.Be + e : 0;
+            tc::cp_async16(tc::smem_u32(xs + j * kRow + v * 8), ok ? X + row * s.ldx + v * 8 : X, ok);
+            tc::cp_async16(tc::smem_u32(as + j * kRow + v * 8), ok ? A + row * s.lda + v * 8 : A, ok);
+        }
+        {
+            const int j = tid / NV, v = tid % NV, t = rev ? s.T - 1 - (first + j) : first + j;
+            const bool ok = j < count && v * 8 < cols;
+            const long long row = ok ? (long long)t * s.Be + e : 0;
+            tc::cp_async16(tc::smem_u32(bs + j * kCol + v * 8), ok ? B + row * s.ldb + v * 8 : B, ok);
+        }
+        tc::cp_async_commit();
+        tc::cp_async_wait<0>();
+    };
+    copy(0, n);
+    const bool flag = s.done && lane < n && s.done[(long long)(rev ? s.T - 1 - lane : lane) * s.Be + e] != 0;
+    const uint32_t resets_all = __ballot_sync(0xffffffffu, flag);
+    if (tid < 18) pow[tid] = power(log2f(s.decay[h]), tid);
+    const bool bad = __syncthreads_or(not_finite(*reinterpret_cast<const uint4 *>(bs + tid / 8 * kCol + tid % 8 * 8)));
+    bool filled = in != nullptr;
+    for (int piece = 0; piece < (bad ? n : 1); ++piece) {
+        const int count = bad ? 1 : n, first = bad ? piece : 0;
+        const uint32_t resets = bad ? resets_all >> piece & 1 : resets_all;
+        if (bad) {
+            __syncthreads();
+            copy(piece, 1);
+        }
+        if (filled) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        *reinterpret_cast<uint32_t *>(ms + (64 * m + 16 * w + g + 8 * i) * kCol + 8 * k + 2 * t4) = pack_bf16x2(M[m][k][2 * i], M[m][k][2 * i + 1]);
+        }
+        __syncthreads();
+        const auto before = [&](int i) { return __popc(resets & (((1u << i) << rev) - 1)); };
+        {
+            float o[2][4] = {}, p[2][4] = {};
+#pragma unroll
+            for (int k = 0; k < KR; ++k) {
+                uint32_t xf[4], b[4];
+                ldsm(xf, tc::smem_u32(xs + (lane % 16) * kRow + k * 16 + lane / 16 * 8));
+                ldsm(b, tc::smem_u32(as + (lane / 16 * 8 + lane % 8) * kRow + k * 16 + lane / 8 % 2 * 8));
+                mma_bf16(p[0], xf, b[0], b[1]);
+                mma_bf16(p[1], xf, b[2], b[3]);
+                if (filled) {
+                    ldsm_t(b, tc::smem_u32(ms + (k * 16 + lane % 16) * kCol + 16 * w + lane / 16 * 8));
+                    mma_bf16(o[0], xf, b[0], b[1]);
+                    mma_bf16(o[1], xf, b[2], b[3]);
+                }
+            }
+            const bool on0 = before(g) == 0, on1 = before(g + 8) == 0;
+            const float f0 = pow[g + 1 - rev], f1 = pow[g + 9 - rev];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                o[q][0] = on0 ? o[q][0] * f0 : 0.f;
+                o[q][1] = on0 ? o[q][1] * f0 : 0.f;
+                o[q][2] = on1 ? o[q][2] * f1 : 0.f;
+                o[q][3] = on1 ? o[q][3] * f1 : 0.f;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const int i = v < 2 ? g : g + 8, j = q * 8 + 2 * t4 + v % 2;
+                    p[q][v] = i >= j && before(i) == before(j) ? p[q][v] * (pow[max(i - j, 0)] * s.a_scale) : 0.f;
+                }
+            }
+            const uint32_t pf[4] = {pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])};
+            uint32_t b[4];
+            ldsm_t(b, tc::smem_u32(bs + (lane % 16) * kCol + 16 * w + lane / 16 * 8));
+            mma_bf16(o[0], pf, b[0], b[1]);
+            mma_bf16(o[1], pf, b[2], b[3]);
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int i = g + 8 * v, t = rev ? s.T - 1 - (first + i) : first + i;
+                const long long row = (long long)t * s.Be + e;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int c = 16 * w + 8 * q + 2 * t4;
+                    if (i >= count || c >= cols) continue;
+                    const float o0 = o[q][2 * v] * s.out_scale, o1 = o[q][2 * v + 1] * s.out_scale;
+                    if (s.shared) *reinterpret_cast<float2 *>(s.shared + (row * s.heads + h) * s.C + c0 + c) = make_float2(o0, o1);
+                    else *reinterpret_cast<uint32_t *>(static_cast<bf16 *>(s.out) + row * s.ldo + (long long)h * s.C + c0 + c) = pack_bf16x2(o0, o1);
+                }
+            }
+        }
+        filled = true;
+        if (!s.m_out && (!bad || piece == n - 1)) continue;
+        const int end = __popc(resets);
+        const float keep = pow[count];
+        float wj[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int j = 2 * t4 + v % 2 + v / 2 * 8;
+            wj[v] = j < count && before(j) == end ? pow[max(count - 1 - j + rev, 0)] * s.a_scale : 0.f;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            uint32_t a[4], part[TERMS][4];
+            ldsm_t(a, tc::smem_u32(as + (lane / 16 * 8 + lane % 8) * kRow + 64 * m + 16 * w + lane / 8 % 2 * 8));
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                float f0 = low(a[v]) * wj[v / 2 * 2], f1 = high(a[v]) * wj[v / 2 * 2 + 1];
+                if (wj[v / 2 * 2] == 0.f) f0 = 0.f;
+                if (wj[v / 2 * 2 + 1] == 0.f) f1 = 0.f;
+#pragma unroll
+                for (int q = 0; q < TERMS; ++q) {
+                    part[q][v] = pack_bf16x2(f0, f1);
+                    f0 -= low(part[q][v]);
+                    f1 -= high(part[q][v]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t b[4];
+                ldsm_t(b, tc::smem_u32(bs + (lane % 16) * kCol + k * 16 + lane / 16 * 8));
+                float s0[4] = {}, s1[4] = {};
+#pragma unroll
+                for (int q = TERMS - 1; q >= 0; --q) {
+                    mma_bf16(s0, part[q], b[0], b[1]);
+                    mma_bf16(s1, part[q], b[2], b[3]);
+                }
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    M[m][2 * k][v] = resets == 0 ? fmaf(M[m][2 * k][v], keep, s0[v]) : s0[v];
+                    M[m][2 * k + 1][v] = resets == 0 ? fmaf(M[m][2 * k + 1][v], keep, s1[v]) : s1[v];
+                }
+            }
+        }
+    }
+    if (!s.m_out) return;
+    float *out = s.m_out + eh * s.state;
+    at_state([&](float &m0, float &m1, bool ok, long long at) {
+        if (!ok) return;
+        if (pairs) {
+            __stcs(reinterpret_cast<float2 *>(out + at), make_float2(m0, m1));
+        } else {
+            __stcs(out + at, m0);
+            __stcs(out + at + s.stride_c, m1);
+        }
+    });
+}
+
 // What each segment starts from, in place of what it adds, and the state that is left.
 __global__ void __launch_bounds__(256) segments_kernel(Sweep s) {
     grid_wait();
-    __shared__ int reset;
-    const int eh = blockIdx.x, e = eh / s.heads, h = eh % s.heads;
-    const int i = blockIdx.y * 256 + threadIdx.x;  // element r * C + c
-    const bool on = i < s.R * s.C;
-    const long long at = on ? (i / s.C) * s.stride_r + (i % s.C) * s.stride_c : 0;
-    const float l2 = log2f(s.decay[h]);
-    float m = on && s.m_in ? s.m_in[eh * s.state + at] : 0.f;
-    for (int seg = 0; seg < s.nseg; ++seg) {
-        const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
-        __syncthreads();
-        if (threadIdx.x == 0) reset = 0;
-        __syncthreads();
-        if (s.done) {
-            bool any = false;
-            for (int n = n0 + threadIdx.x; n < n1; n += 256) any |= s.done[(long long)(s.reverse ? s.T - 1 - n : n) * s.Be + e] != 0;
-            if (any) reset = 1;
+    const int eh = blockIdx.x, h = eh % s.heads, i = blockIdx.y * 256 + threadIdx.x;  // element r * C + c
+    if (i >= s.R * s.C) return;
+    const long long at = (i / s.C) * s.stride_r + (i % s.C) * s.stride_c, all = (long long)s.Be * s.heads;
+    const float l2 = log2f(s.decay[h]), whole = power(l2, s.seg_len), rest = power(l2, s.T - (s.nseg - 1) * s.seg_len);
+    float m = s.m_in ? s.m_in[eh * s.state + at] : 0.f;
+    float *p = s.seg + eh * (long long)s.R * s.C + i;
+    const long long step = all * s.R * s.C;
+    for (int seg = 0; seg < s.nseg; seg += 8) {
+        float add[8];
+        int reset[8];
+        const int n = min(8, s.nseg - seg);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            add[k] = k < n ? p[(seg + k) * step] : 0.f;
+            reset[k] = k < n ? s.seg_reset[(seg + k) * all + eh] : 0;
         }
-        __syncthreads();
-        if (on) {
-            float *p = s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C + i;
-            const float add = *p;
-            *p = m;
-            m = reset ? add : fmaf(power(l2, n1 - n0), m, add);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k >= n) break;
+            p[(seg + k) * step] = m;
+            m = reset[k] ? add[k] : fmaf(seg + k == s.nseg - 1 ? rest : whole, m, add[k]);
         }
     }
-    if (on && s.m_out) s.m_out[eh * s.state + at] = m;
+    if (s.m_out) s.m_out[eh * s.state + at] = m;
 }
 
 // Gradient of a shared head: the sum of those of its query heads.
@@ -609,7 +803,7 @@ int check(const ppo_decay_attention_desc *d) {
 size_t seg_floats(const ppo_decay_attention_desc *d) {
     int len;
     const int n = segments(d, &len);
-    return n > 1 ? (size_t)n * d->Be * d->heads * d->dk * d->dv : 0;
+    return n > 1 ? (size_t)n * d->Be * d->heads * (d->dk * d->dv + 1) + 3 & ~(size_t)3 : 0;  // with a flag each
 }
 size_t shared_floats(const ppo_decay_attention_desc *d) {
     return d->heads != d->kv_heads ? (size_t)d->T * d->Be * d->heads * (d->dk > d->dv ? d->dk : d->dv) : 0;
@@ -635,6 +829,11 @@ int chunk_launch(const Sweep &s, bool exact, cudaStream_t st) {
     if (s.R <= 64) return exact ? chunk_launch_as<64, STATE, 3>(s, st) : chunk_launch_as<64, STATE, 2>(s, st);
     return exact ? chunk_launch_as<128, STATE, 3>(s, st) : chunk_launch_as<128, STATE, 2>(s, st);
 }
+int short_launch(const Sweep &s, cudaStream_t st) {
+    const dim3 grid(ppo_cdiv(s.C, kBlockCols) * s.Be * s.heads);
+    if (s.R <= 64) return s.m_out ? ppo_launch(short_kernel<64, 3>, grid, dim3(128), 0, st, s) : ppo_launch(short_kernel<64, 2>, grid, dim3(128), 0, st, s);
+    return s.m_out ? ppo_launch(short_kernel<128, 3>, grid, dim3(128), 0, st, s) : ppo_launch(short_kernel<128, 2>, grid, dim3(128), 0, st, s);
+}
 // Rows of 16-byte vectors.
 bool chunks_fit(const Sweep &s) {
     const auto rows = [](const void *p, long long ld) { return ppo_aligned(p, 16) && ld % 8 == 0; };
@@ -648,6 +847,7 @@ int sweep(const Sweep &s, cudaStream_t st) {
         else PPO_TRY(sweep_launch<T, true>(s, st));
         PPO_TRY(ppo_launch(segments_kernel, dim3(s.Be * s.heads, ppo_cdiv((long long)s.R * s.C, 256)), dim3(256), 0, st, s));
     }
+    if (chunks && s.T <= 16) return short_launch(s, st);
     return chunks ? chunk_launch<false>(s, s.nseg == 1 && s.m_out, st) : sweep_launch<T, false>(s, st);
 }
 
@@ -663,6 +863,7 @@ Sweep sweep_of(const ppo_decay_attention_desc *d, const float *decay, const uint
     s.share_a = s.share_b = s.share_x = 1;
     s.nseg = segments(d, &s.seg_len);
     s.seg = seg;
+    s.seg_reset = reinterpret_cast<int *>(seg + (size_t)s.nseg * d->Be * d->heads * d->dk * d->dv);
     return s;
 }
 // M [dk][dv], the state as it is stored, or M [dv][dk]
