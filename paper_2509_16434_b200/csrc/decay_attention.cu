@@ -667,6 +667,390 @@ __global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(Sweep s) {
     });
 }
 
+// ---- chunks of 128 steps on tcgen05 (bf16, longer sequences) ----
+//
+// The same four products as tcgen05.mma with accumulators in tensor memory, whole heads per block: S = X A^T and O1 = X M as soon as the
+// rows have landed; K = (w A)^T B while S is weighted into P; O2 = P B.  A thread owns a row of each accumulator (a step, or a row of the
+// state) and half of its columns.  Operands lie in panels of 64 columns, 128 bytes a row, swizzled: A is read along its rows for S and
+// down its columns (MN-major) for K.  The state stays in registers in 32 bits; M is its bf16 image.
+//   64 rows: the weighted keys' first two terms are the two halves of a 128-row operand, and what comes of them stays apart, as rows r
+// and 64 + r of the state, which X reads one after the other: their sum is made once, at the end.
+// mma.sync at these sizes is bound by what goes with it, 13 instructions for each product (8192 steps of 16 x 128: 219 us).
+
+// RB, CB: rows and columns of the state, padded to 64 or 128.
+template <int RB, int CB, bool STATE, int TERMS>
+struct TileSmem {
+    static constexpr int kPanel = 128 * 128;  // bytes: 128 rows of 64 bf16 numbers
+    static constexpr int kX = 0, kA = kX + (STATE ? 0 : RB / 64 * kPanel), kB = kA + RB / 64 * kPanel, kM = kB + CB / 64 * kPanel,
+                         kSplit = kM + (STATE ? 0 : CB / 64 * kPanel), kSplitBytes = RB == 128 ? TERMS * 2 * kPanel : (TERMS + 1) / 2 * 2 * kPanel,
+                         kEnd = kSplit + kSplitBytes;
+    static constexpr int kP0 = kX, kP1 = kX + kPanel;  // P takes the place of X, and where that is one panel of A behind it
+    static constexpr int kBytes = kEnd + 1152 + 1024;  // tables and barriers; alignment
+    static constexpr uint32_t kCols = STATE ? (CB < 32 ? 32 : CB) : 128 + 2 * CB > 256 ? 512 : 256;  // of tensor memory
+};
+struct TileTables {
+    float pow[132], scaled[132];  // decay^n, and times a_scale
+    uint64_t bar[3];
+    int abort_flag;
+    uint32_t slot;
+};
+static_assert(sizeof(TileTables) <= 1152, "place of the tables");
+
+template <int RB, int CB, bool STATE, int TERMS>
+__global__ void __launch_bounds__(256, RB == 64 && CB == 64 ? 2 : 1) tile_kernel(Sweep s, int32_t *status) {
+    using L = TileSmem<RB, CB, STATE, TERMS>;
+    static_assert(L::kBytes <= 227 * 1024, "shared memory of a block");
+    constexpr int H = CB / 2;  // columns of a thread
+    constexpr int kO1 = 128, kK = STATE ? 0 : 128 + CB;  // columns of tensor memory: S and O2 from 0
+    extern __shared__ uint8_t raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    TileTables *tab = reinterpret_cast<TileTables *>(smem + L::kEnd);
+    const uint32_t base = tc::smem_u32(smem);
+    const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index(), lq = w % 4, wc = w / 4, row = 32 * lq + lane;
+    volatile int *abort_flag = &tab->abort_flag;
+    if (tid == 0) {
+        for (int i = 0; i < 3; ++i) tc::mbar_init(&tab->bar[i], 1);
+        tab->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (RB == 64 && TERMS == 3) {  // the half beside the third term
+        for (int i = tid; i < L::kPanel / 16; i += 256) reinterpret_cast<uint4 *>(smem + L::kSplit + 3 * L::kPanel)[i] = make_uint4(0, 0, 0, 0);
+    }
+    if (w == 0) tc::tmem_alloc(&tab->slot, L::kCols);
+    grid_wait();
+    const int eh = blockIdx.x, e = eh / s.heads, h = eh % s.heads, seg = blockIdx.y, rev = s.reverse;
+    if (tid < 130) {
+        const float p = power(log2f(s.decay[h]), tid);
+        tab->pow[tid] = p;
+        tab->scaled[tid] = p * s.a_scale;
+    }
+    const bf16 *A = static_cast<const bf16 *>(s.a) + (long long)(h / s.share_a) * s.R;
+    const bf16 *B = static_cast<const bf16 *>(s.b) + (long long)(h / s.share_b) * s.C;
+    const bf16 *X = static_cast<const bf16 *>(s.x) + (long long)(h / s.share_x) * s.R;
+    const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
+    // Rows first .. first + count of the sweep into rows 0 .., zeros behind them and behind R and C.
+    auto rows = [&](int to, const bf16 *from, long long ld, int width, int padded, int first, int count) {
+        const int V = padded / 8;
+        for (int i = tid; i < 128 * V; i += 256) {
+            const int j = i / V, v = i % V, t = rev ? s.T - 1 - (first + j) : first + j;
+            const bool ok = j < count && v * 8 < width;
+            const bf16 *p = ok ? from + ((long long)t * s.Be + e) * ld + v * 8 : from;
+            tc::cp_async16(base + to + v / 8 * L::kPanel + j * 128 + ((v % 8) ^ (j % 8)) * 16, p, ok);
+        }
+    };
+    auto copy = [&](int first, int count) {
+        if (!STATE) rows(L::kX, X, s.ldx, s.R, RB, first, count);
+        rows(L::kA, A, s.lda, s.R, RB, first, count);
+        rows(L::kB, B, s.ldb, s.C, CB, first, count);
+        tc::cp_async_commit();
+    };
+    copy(n0, min(128, n1 - n0));
+
+    // row `row` of the state (with 64: rows 64 .. are the second terms' share), columns wc H ..
+    const long long sr = s.nseg > 1 ? s.C : s.stride_r, sc = s.nseg > 1 ? 1 : s.stride_c;
+    const long long place = s.nseg > 1 ? ((long long)seg * s.Be * s.heads + eh) * s.R * s.C : eh * s.state;
+    const float *in = STATE ? nullptr : s.nseg > 1 ? s.seg + place : s.m_in ? s.m_in + place : nullptr;
+    float *out_state = STATE ? s.seg + place : s.nseg > 1 || !s.m_out ? nullptr : s.m_out + place;
+    float M[H];
+    {
+        const bool on = in && row < s.R && (RB == 128 || row < 64);
+        const float *p = in + row * sr + wc * H * sc;
+        if (sc == 1) {
+#pragma unroll
+            for (int c = 0; c < H; c += 4) {
+                const float4 f = on && wc * H + c < s.C ? *reinterpret_cast<const float4 *>(p + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                M[c] = f.x, M[c + 1] = f.y, M[c + 2] = f.z, M[c + 3] = f.w;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < H; ++c) M[c] = on && wc * H + c < s.C ? p[c * sc] : 0.f;
+        }
+    }
+    bool filled = in != nullptr;
+    auto store_m = [&] {  // its image: row `row`, pieces of 8 columns
+#pragma unroll
+        for (int c = 0; c < H; c += 8) {
+            const int v = (wc * H + c) / 8;
+            *reinterpret_cast<uint4 *>(smem + L::kM + v / 8 * L::kPanel + row * 128 + ((v % 8) ^ (row % 8)) * 16) =
+                make_uint4(pack_bf16x2(M[c], M[c + 1]), pack_bf16x2(M[c + 2], M[c + 3]), pack_bf16x2(M[c + 4], M[c + 5]), pack_bf16x2(M[c + 6], M[c + 7]));
+        }
+    };
+    if (!STATE && filled) store_m();
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = tab->slot, mine = tmem + ((uint32_t)(32 * lq) << 16);
+
+    // Descriptors: along the rows (K-major), and down the columns with the panels `apart` bytes from one another (MN-major).
+    const uint64_t dk = tc::smem_desc_sw(base, 16, 1024, 128), dm = tc::smem_desc_sw(base, L::kPanel, 1024, 128);
+    const uint32_t k_hi = (uint32_t)(dk >> 32), m_hi = (uint32_t)(dm >> 32), k_lo = (uint32_t)dk, m_lo = (uint32_t)dm;
+    auto along = [&](int panel, int k) { return k_lo + (uint32_t)(panel >> 4) + 2u * k; };       // step k of 16 columns of one panel
+    auto down = [&](int panels, int k) { return m_lo + (uint32_t)(panels >> 4) + 128u * k; };    // step k of 16 rows
+    bool ok = true;
+    uint32_t phase[3] = {0, 0, 0};
+    auto wait = [&](int i) {
+        ok = tc::mbar_wait(&tab->bar[i], phase[i], abort_flag, status) && ok;
+        phase[i] ^= 1;
+        tc::tc_fence_after();
+    };
+
+    // The n steps from `first` on, in rows 0 ..; resets: bit i of the four words set where done is at step first + i.
+    auto process = [&](int first, int n, const uint32_t (&resets)[4], bool last) {
+        int last_reset = -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (resets[i]) last_reset = 32 * i + 31 - __clz(resets[i]);
+        const bool update = !last || out_state;
+        if (!STATE && w == 0) {
+            if (tc::elect_one()) {
+#pragma unroll
+                for (int k = 0; k < RB / 16; ++k)
+                    tc::umma_bf16_lh(tmem, along(L::kX + k / 4 * L::kPanel, k % 4), k_hi, along(L::kA + k / 4 * L::kPanel, k % 4), k_hi,
+                                     tc::instr_desc(128, 128, 0, 0), k > 0);
+                if (filled) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int xk = k % (RB / 16);
+                        tc::umma_bf16_lh(tmem + kO1, along(L::kX + xk / 4 * L::kPanel, xk % 4), k_hi, down(L::kM, k), m_hi, tc::instr_desc(128, CB, 0, 1), k > 0);
+                    }
+                }
+                tc::umma_commit(&tab->bar[0]);
+            }
+            __syncwarp();
+        }
+        if (update) {
+            // w_j a_j in TERMS terms
+            constexpr int V = RB / 8;
+#pragma unroll 2
+            for (int i = tid; i < 128 * V; i += 256) {
+                const int j = i / V, v = i % V, at = j * 128 + ((v % 8) ^ (j % 8)) * 16;
+                const float wj = j < n && (rev ? j >= last_reset : j > last_reset) ? tab->scaled[max(n - 1 - j + rev, 0)] : 0.f;
+                const uint4 a = *reinterpret_cast<const uint4 *>(smem + L::kA + v / 8 * L::kPanel + at);
+                const uint32_t in4[4] = {a.x, a.y, a.z, a.w};
+                uint32_t part[TERMS][4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float f0 = wj == 0.f ? 0.f : low(in4[q]) * wj, f1 = wj == 0.f ? 0.f : high(in4[q]) * wj;
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t) {
+                        part[t][q] = pack_bf16x2(f0, f1);
+                        f0 -= low(part[t][q]);
+                        f1 -= high(part[t][q]);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t)
+                    *reinterpret_cast<uint4 *>(smem + L::kSplit + (RB == 128 ? 2 * t + v / 8 : t) * L::kPanel + at) =
+                        make_uint4(part[t][0], part[t][1], part[t][2], part[t][3]);
+            }
+            tc::fence_async_smem();
+            tc::tc_fence_before();
+        }
+        __syncthreads();
+        if (update && w == 0) {
+            tc::tc_fence_after();
+            if (tc::elect_one()) {
+                constexpr int SETS = RB == 128 ? TERMS : (TERMS + 1) / 2;
+#pragma unroll
+                for (int t = SETS - 1; t >= 0; --t)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        tc::umma_bf16_lh(tmem + kK, down(L::kSplit + 2 * t * L::kPanel, k), m_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 1, 1),
+                                         t < SETS - 1 || k > 0);
+                tc::umma_commit(&tab->bar[1]);
+            }
+            __syncwarp();
+        }
+        int visible = 0;      // the first step that this row sees
+        bool reached = true;  // and whether it sees the state
+        if constexpr (!STATE) {
+            const int upto = rev ? row : row - 1;  // the last flag in front of this row
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = upto - 32 * i;
+                const uint32_t f = k < 0 ? 0 : resets[i] & (k >= 31 ? 0xffffffffu : (2u << k) - 1);
+                if (f) {
+                    visible = 32 * i + 31 - __clz(f) + 1 - rev;
+                    reached = false;
+                }
+            }
+            wait(0);
+            // P: row `row`, columns 64 wc ..
+            uint8_t *p = smem + (wc ? L::kP1 : L::kP0) + row * 128;
+            if (wc == 1 && lq < 2) {
+#pragma unroll
+                for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4 *>(p + v * 16) = make_uint4(0, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float f[32];
+                    tc::tmem_ld32(mine + 64 * wc + 32 * half, f);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        const int j = 64 * wc + 32 * half + c;
+                        f[c] = j <= row && j >= visible ? f[c] * tab->scaled[max(row - j, 0)] : 0.f;
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; c += 8)
+                        *reinterpret_cast<uint4 *>(p + ((4 * half + c / 8) ^ (row % 8)) * 16) =
+                            make_uint4(pack_bf16x2(f[c], f[c + 1]), pack_bf16x2(f[c + 2], f[c + 3]), pack_bf16x2(f[c + 4], f[c + 5]), pack_bf16x2(f[c + 6], f[c + 7]));
+                }
+            }
+            tc::fence_async_smem();
+            tc::tc_fence_before();
+            __syncthreads();
+            if (w == 0) {
+                tc::tc_fence_after();
+                if (tc::elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        tc::umma_bf16_lh(tmem, along(k < 4 ? L::kP0 : L::kP1, k % 4), k_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 0, 1), k > 0);
+                    tc::umma_commit(&tab->bar[2]);
+                }
+                __syncwarp();
+            }
+        }
+        if (update) {
+            wait(1);
+            const float keep = tab->pow[n];
+#pragma unroll
+            for (int c0 = 0; c0 < H; c0 += 32) {
+                float f[32];
+                tc::tmem_ld32(mine + kK + wc * H + c0, f);
+#pragma unroll
+                for (int c = 0; c < 32; ++c) M[c0 + c] = last_reset < 0 ? fmaf(M[c0 + c], keep, f[c]) : f[c];
+            }
+            if (!STATE && !last) store_m();
+        }
+        if constexpr (!STATE) {
+            wait(2);
+            const float f1 = tab->pow[row + 1 - rev];
+            const int t = rev ? s.T - 1 - (first + row) : first + row;
+            const long long at = (long long)t * s.Be + e;
+#pragma unroll
+            for (int c0 = 0; c0 < H; c0 += 32) {
+                float o[32];
+                tc::tmem_ld32(mine + wc * H + c0, o);
+                if (filled) {
+                    float m[32];
+                    tc::tmem_ld32(mine + kO1 + wc * H + c0, m);
+                    if (reached) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) o[c] = fmaf(m[c], f1, o[c]);
+                    }
+                }
+                if (s.shared) {
+                    float *to = s.shared + (at * s.heads + h) * s.C + wc * H + c0;
+                    if (row < n) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4)
+                            if (wc * H + c0 + c < s.C)
+                                *reinterpret_cast<float4 *>(to + c) = make_float4(o[c] * s.out_scale, o[c + 1] * s.out_scale, o[c + 2] * s.out_scale, o[c + 3] * s.out_scale);
+                    }
+                } else {  // through the place of P to whole rows
+#pragma unroll
+                    for (int c = 0; c < 32; c += 8) {
+                        const int v = (wc * H + c0 + c) / 8;
+                        *reinterpret_cast<uint4 *>(smem + (v / 8 ? L::kP1 : L::kP0) + row * 128 + ((v % 8) ^ (row % 8)) * 16) =
+                            make_uint4(pack_bf16x2(o[c] * s.out_scale, o[c + 1] * s.out_scale), pack_bf16x2(o[c + 2] * s.out_scale, o[c + 3] * s.out_scale),
+                                       pack_bf16x2(o[c + 4] * s.out_scale, o[c + 5] * s.out_scale), pack_bf16x2(o[c + 6] * s.out_scale, o[c + 7] * s.out_scale));
+                    }
+                }
+            }
+            if (!s.shared) {
+                __syncthreads();
+                constexpr int V = CB / 8;
+#pragma unroll 4
+                for (int i = tid; i < 128 * V; i += 256) {
+                    const int j = i / V, v = i % V, tj = rev ? s.T - 1 - (first + j) : first + j;
+                    if (j < n && v * 8 < s.C)
+                        *reinterpret_cast<uint4 *>(static_cast<bf16 *>(s.out) + ((long long)tj * s.Be + e) * s.ldo + (long long)h * s.C + v * 8) =
+                            *reinterpret_cast<const uint4 *>(smem + (v / 8 ? L::kP1 : L::kP0) + j * 128 + ((v % 8) ^ (j % 8)) * 16);
+                }
+            }
+        }
+        tc::tc_fence_before();
+        filled = true;
+    };
+
+    uint32_t any = 0;
+    for (int n = n0; n < n1; n += 128) {
+        const int count = min(128, n1 - n);
+        const bool more = n + 128 < n1;
+        uint32_t resets[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int step = n + 32 * i + lane;
+            resets[i] = __ballot_sync(0xffffffffu, s.done && step < n1 && s.done[(long long)(rev ? s.T - 1 - step : step) * s.Be + e] != 0);
+            any |= resets[i];
+        }
+        if (n > n0) {
+            __syncthreads();  // every operand of the last chunk is read
+            copy(n, count);
+        }
+        tc::cp_async_wait<0>();
+        bool bad = false;
+        for (int i = tid; i < 128 * CB / 8; i += 256) {  // what this thread has copied of B
+            const int j = i / (CB / 8), v = i % (CB / 8);
+            bad |= not_finite(*reinterpret_cast<const uint4 *>(smem + L::kB + v / 8 * L::kPanel + j * 128 + ((v % 8) ^ (j % 8)) * 16));
+        }
+        tc::fence_async_smem();  // the copies, and M
+        bad = __syncthreads_or(bad);
+        tc::tc_fence_after();
+        for (int i = 0; i < (bad ? count : 1); ++i) {
+            if (bad) {
+                __syncthreads();
+                copy(n + i, 1);
+                tc::cp_async_wait<0>();
+                tc::fence_async_smem();
+                __syncthreads();
+                tc::tc_fence_after();
+                uint32_t one[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i / 32 == k) one[0] = resets[k] >> (i % 32) & 1;
+                process(n + i, 1, one, !more && i == count - 1);
+            } else {
+                process(n, count, resets, !more);
+            }
+        }
+        if (__syncthreads_or(!ok)) break;
+    }
+    if (STATE && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any != 0;
+    if (out_state) {
+        if (RB == 64) {  // the two shares of a row
+            float *x = reinterpret_cast<float *>(smem + L::kSplit);
+            if (row >= 64) {
+#pragma unroll
+                for (int c = 0; c < H; ++c) x[(wc * H + c) * 64 + row - 64] = M[c];
+            }
+            __syncthreads();
+            if (row < 64) {
+#pragma unroll
+                for (int c = 0; c < H; ++c) M[c] += x[(wc * H + c) * 64 + row];
+            }
+        }
+        if (row < s.R && (RB == 128 || row < 64)) {
+            float *p = out_state + row * sr + wc * H * sc;
+            if (sc == 1) {
+#pragma unroll
+                for (int c = 0; c < H; c += 4)
+                    if (wc * H + c < s.C) *reinterpret_cast<float4 *>(p + c) = make_float4(M[c], M[c + 1], M[c + 2], M[c + 3]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < H; ++c)
+                    if (wc * H + c < s.C) p[c * sc] = M[c];
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (w == 0) {
+        tc::tc_fence_after();
+        tc::tmem_dealloc(tmem, L::kCols);
+    }
+}
+
 // What each segment starts from, in place of what it adds, and the state that is left.
 __global__ void __launch_bounds__(256) segments_kernel(Sweep s) {
     grid_wait();
@@ -782,7 +1166,7 @@ int segments(const ppo_decay_attention_desc *d, int *len) {
     int n = blocks < 2 * 148 ? (int)(2 * 148 / blocks) : 1;
     const int most = ppo_cdiv(d->T, kSegment);
     if (n > most) n = most;
-    const int per = ppo_cdiv(ppo_cdiv(d->T, n), 64) * 64;
+    const int per = ppo_cdiv(ppo_cdiv(d->T, n), 128) * 128;
     *len = per;
     return ppo_cdiv(d->T, per);
 }
@@ -834,21 +1218,41 @@ int short_launch(const Sweep &s, cudaStream_t st) {
     if (s.R <= 64) return s.m_out ? ppo_launch(short_kernel<64, 3>, grid, dim3(128), 0, st, s) : ppo_launch(short_kernel<64, 2>, grid, dim3(128), 0, st, s);
     return s.m_out ? ppo_launch(short_kernel<128, 3>, grid, dim3(128), 0, st, s) : ppo_launch(short_kernel<128, 2>, grid, dim3(128), 0, st, s);
 }
+template <int RB, int CB, bool STATE, int TERMS>
+int tile_launch_as(const Sweep &s, cudaStream_t st) {
+    using L = TileSmem<RB, CB, STATE, TERMS>;
+    static PerDevice<bool> allowed;
+    int32_t *status = ppo_device_status_ptr();
+    if (!status) return PPO_ERR_CUDA;
+    PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(tile_kernel<RB, CB, STATE, TERMS>, L::kBytes); }));
+    return ppo_launch(tile_kernel<RB, CB, STATE, TERMS>, dim3(s.Be * s.heads, s.nseg), dim3(256), L::kBytes, st, s, status);
+}
+template <bool STATE, int TERMS>
+int tile_launch_of(const Sweep &s, cudaStream_t st) {
+    if (s.R <= 64) return s.C <= 64 ? tile_launch_as<64, 64, STATE, TERMS>(s, st) : tile_launch_as<64, 128, STATE, TERMS>(s, st);
+    return s.C <= 64 ? tile_launch_as<128, 64, STATE, TERMS>(s, st) : tile_launch_as<128, 128, STATE, TERMS>(s, st);
+}
+template <bool STATE>
+int tile_launch(const Sweep &s, bool exact, cudaStream_t st) {
+    return exact ? tile_launch_of<STATE, 3>(s, st) : tile_launch_of<STATE, 2>(s, st);
+}
 // Rows of 16-byte vectors.
 bool chunks_fit(const Sweep &s) {
     const auto rows = [](const void *p, long long ld) { return ppo_aligned(p, 16) && ld % 8 == 0; };
     return s.R % 8 == 0 && s.C % 8 == 0 && rows(s.a, s.lda) && rows(s.b, s.ldb) && rows(s.x, s.ldx) && (s.shared || rows(s.out, s.ldo));
 }
+// bf16 rows that vectors fit: up to 16 steps, up to 64, more.
 template <typename T>
 int sweep(const Sweep &s, cudaStream_t st) {
-    const bool chunks = std::is_same_v<T, bf16> && chunks_fit(s);
+    const bool chunks = std::is_same_v<T, bf16> && chunks_fit(s), exact = s.m_out != nullptr;
     if (s.nseg > 1) {
-        if (chunks) PPO_TRY(chunk_launch<true>(s, s.m_out != nullptr, st));
-        else PPO_TRY(sweep_launch<T, true>(s, st));
+        PPO_TRY(chunks ? tile_launch<true>(s, exact, st) : sweep_launch<T, true>(s, st));
         PPO_TRY(ppo_launch(segments_kernel, dim3(s.Be * s.heads, ppo_cdiv((long long)s.R * s.C, 256)), dim3(256), 0, st, s));
     }
-    if (chunks && s.T <= 16) return short_launch(s, st);
-    return chunks ? chunk_launch<false>(s, s.nseg == 1 && s.m_out, st) : sweep_launch<T, false>(s, st);
+    if (!chunks) return sweep_launch<T, false>(s, st);
+    if (s.T <= 16) return short_launch(s, st);
+    if (s.T <= kChunk) return chunk_launch<false>(s, exact, st);
+    return tile_launch<false>(s, exact && s.nseg == 1, st);
 }
 
 Sweep sweep_of(const ppo_decay_attention_desc *d, const float *decay, const uint8_t *done, float *seg) {
