@@ -10,6 +10,7 @@
 // leaves the first one decayed.
 #include "elem.cuh"
 #include "tcgen05.cuh"
+#include "tma_host.cuh"
 
 namespace {
 
@@ -27,7 +28,9 @@ struct Sweep {
     int T, Be, heads, R, C;
     float a_scale, out_scale;
     int reverse;
-    int seg_len, nseg;   // steps per segment of the sequence (nseg == 1: all)
+    int seg_len, nseg;   // steps per segment of the sequence (nseg == 1: all); segments are numbered in time's order
+    int seg_made;        // 1: an earlier sweep over the same states has left what each segment starts from
+    long long seg_r, seg_c;  // strides of a state in it
     float *seg;          // [nseg][Be * heads][R * C]: what each segment adds to a state, then what each starts from
     int *seg_reset;      // [nseg][Be * heads]: whether a done flag is set in it
 };
@@ -52,14 +55,15 @@ __global__ void __launch_bounds__(128) sweep_kernel(Sweep s) {
     const T *X = static_cast<const T *>(s.x) + (long long)(h / s.share_x) * s.R;
     float M[KS];
     // this thread's element of row r of the state lies at r * sr + sc
-    const long long sr = s.nseg > 1 ? s.C : s.stride_r, sc = s.nseg > 1 ? c : c * s.stride_c;
+    const long long sr = s.nseg > 1 ? s.seg_r : s.stride_r, sc = c * (s.nseg > 1 ? s.seg_c : s.stride_c);
     const float *in = s.nseg > 1 ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.m_in ? s.m_in + eh * s.state : nullptr;
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
         const int r = w * KS + i;
         M[i] = !STATE && in && r < s.R && c < s.C ? in[r * sr + sc] : 0.f;
     }
-    const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
+    const int t_lo = seg * s.seg_len, t_hi = min(t_lo + s.seg_len, s.T);
+    const int n0 = s.reverse ? s.T - t_hi : t_lo, n1 = s.reverse ? s.T - t_lo : t_hi;  // in the sweep's order
     int any = 0;
     for (int n = n0; n < n1; n += kTokens) {
         const int cnt = min(kTokens, n1 - n);
@@ -240,7 +244,7 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
     copy(0, n0, min(kChunk, n1 - n0));
 
     // the state: rows mr + g (+ 8), columns mc + 8 n + 2 t4 (+ 1)
-    const long long sr = s.nseg > 1 ? s.C : s.stride_r, sc = s.nseg > 1 ? 1 : s.stride_c;
+    const long long sr = s.nseg > 1 ? s.seg_r : s.stride_r, sc = s.nseg > 1 ? s.seg_c : s.stride_c;
     const float *in = STATE ? nullptr : s.nseg > 1 ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.m_in ? s.m_in + eh * s.state : nullptr;
     float *out_state = STATE ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.nseg > 1 || !s.m_out ? nullptr : s.m_out + eh * s.state;
     float M[MN][4];
@@ -667,388 +671,501 @@ __global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(Sweep s) {
     });
 }
 
-// ---- chunks of 128 steps on tcgen05 (bf16, longer sequences) ----
+// ---- chunks of 128 steps on tcgen05 (bf16, more than 64 steps) ----
 //
 // The same four products as tcgen05.mma with accumulators in tensor memory, whole heads per block: S = X A^T and O1 = X M as soon as the
-// rows have landed; K = (w A)^T B while S is weighted into P; O2 = P B.  A thread owns a row of each accumulator (a step, or a row of the
-// state) and half of its columns.  Operands lie in panels of 64 columns, 128 bytes a row, swizzled: A is read along its rows for S and
-// down its columns (MN-major) for K.  The state stays in registers in 32 bits; M is its bf16 image.
+// rows have landed; K = (w A)^T B while S is weighted into P; O2 = P B.  Warp 8 moves tiles (TMA) and issues the products; the other
+// eight are between them: a thread owns a row of each accumulator (a step, or a row of the state) and half of its columns.  Operands lie
+// in panels of 64 columns, 128 bytes a row, swizzled: A is read along its rows for S and down its columns (MN-major) for K.  The state
+// stays in registers in 32 bits; M is its bf16 image.  Rows of a tile are steps in time's order; backwards, the chunks and the masks turn
+// round.
 //   64 rows: the weighted keys' first two terms are the two halves of a 128-row operand, and what comes of them stays apart, as rows r
 // and 64 + r of the state, which X reads one after the other: their sum is made once, at the end.
 // mma.sync at these sizes is bound by what goes with it, 13 instructions for each product (8192 steps of 16 x 128: 219 us).
 
-// RB, CB: rows and columns of the state, padded to 64 or 128.
+// RB, CB: rows and columns of the state, padded to 64 or 128.  STATE: only what the segment leaves, from an empty state.  TERMS: of the
+// weighted a.
 template <int RB, int CB, bool STATE, int TERMS>
 struct TileSmem {
     static constexpr int kPanel = 128 * 128;  // bytes: 128 rows of 64 bf16 numbers
-    static constexpr int kX = 0, kA = kX + (STATE ? 0 : RB / 64 * kPanel), kB = kA + RB / 64 * kPanel, kM = kB + CB / 64 * kPanel,
+    // P takes the place of X, and where that is one panel, of A behind it.  With 128 rows there is room for X of the next chunk
+    // (with three terms there is not), and A's place is free once it is split.
+    static constexpr bool kAhead = RB == 128 && TERMS == 2 && !STATE;
+    static constexpr int kWide = RB / 64 * kPanel, kX = 0, kA = kX + (STATE ? 0 : (kAhead ? 2 : 1) * kWide), kB = kA + kWide, kM = kB + CB / 64 * kPanel,
                          kSplit = kM + (STATE ? 0 : CB / 64 * kPanel), kSplitBytes = RB == 128 ? TERMS * 2 * kPanel : (TERMS + 1) / 2 * 2 * kPanel,
                          kEnd = kSplit + kSplitBytes;
-    static constexpr int kP0 = kX, kP1 = kX + kPanel;  // P takes the place of X, and where that is one panel of A behind it
-    static constexpr int kBytes = kEnd + 1152 + 1024;  // tables and barriers; alignment
-    static constexpr uint32_t kCols = STATE ? (CB < 32 ? 32 : CB) : 128 + 2 * CB > 256 ? 512 : 256;  // of tensor memory
+    static constexpr int kTables = 1664, kBytes = kEnd + kTables + 1024;  // with the alignment
+    static constexpr uint32_t kCols = STATE ? CB : 128 + 2 * CB > 256 ? 512 : 256;  // of tensor memory
+    static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 struct TileTables {
-    float pow[132], scaled[132];  // decay^n, and times a_scale
-    uint64_t bar[3];
-    int abort_flag;
+    float weight[256];  // a_scale lambda^|p - c| of step c for step p at 127 - p + c, 0 where p does not see c
+    float pow[132];     // lambda^n
+    uint64_t got_a, got_b, bar[3];    // X and A, B have landed; S and O1, K, O2 are made
+    uint64_t split, weighted, emptied;  // of the eight warps: A is split; P is there; accumulators are read, M and outputs in place
+    int abort_flag, bad;
     uint32_t slot;
 };
-static_assert(sizeof(TileTables) <= 1152, "place of the tables");
+static_assert(sizeof(TileTables) <= 1664, "place of the tables");
+
+struct TileMaps {
+    CUtensorMap x, a, b, out;
+};
+
+// The segment step by step, a thread per column: what infinities and NaN in B are left to, which a product of masked weights would let
+// reach steps that do not see them.
+template <bool STATE>
+__device__ __noinline__ void segment_slowly(const Sweep &s, float *m, const float *in, float *out_state, long long sr, long long sc, int eh, int t_lo,
+                                            int t_hi) {
+    const int e = eh / s.heads, h = eh % s.heads, c = threadIdx.x, rev = s.reverse;
+    const float lam = s.decay[h];
+    if (c >= s.C) return;
+    for (int r = 0; r < s.R; ++r) m[r * s.C + c] = in ? in[r * sr + c * sc] : 0.f;
+    for (int n = 0; n < t_hi - t_lo; ++n) {
+        const int t = rev ? t_hi - 1 - n : t_lo + n;
+        const long long row = (long long)t * s.Be + e;
+        const bool gate = s.done && s.done[row] != 0;
+        const bf16 *a = static_cast<const bf16 *>(s.a) + row * s.lda + (long long)(h / s.share_a) * s.R;
+        const bf16 *x = static_cast<const bf16 *>(s.x) + row * s.ldx + (long long)(h / s.share_x) * s.R;
+        const float b = bf2f(static_cast<const bf16 *>(s.b)[row * s.ldb + (long long)(h / s.share_b) * s.C + c]);
+        float o = 0.f;
+        for (int r = 0; r < s.R; ++r) {
+            float v = m[r * s.C + c];
+            v = rev ? (gate ? 0.f : v) : v * lam;
+            v = fmaf(bf2f(a[r]) * s.a_scale, b, v);
+            if (!STATE) o = fmaf(bf2f(x[r]), v, o);
+            m[r * s.C + c] = rev ? v * lam : gate ? 0.f : v;
+        }
+        if (STATE) continue;
+        o *= s.out_scale;
+        if (s.shared) s.shared[(row * s.heads + h) * s.C + c] = o;
+        else static_cast<bf16 *>(s.out)[row * s.ldo + (long long)h * s.C + c] = __float2bfloat16_rn(o);
+    }
+    if (out_state)
+        for (int r = 0; r < s.R; ++r) out_state[r * sr + c * sc] = m[r * s.C + c];
+}
 
 template <int RB, int CB, bool STATE, int TERMS>
-__global__ void __launch_bounds__(256, RB == 64 && CB == 64 ? 2 : 1) tile_kernel(Sweep s, int32_t *status) {
+__global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel(const __grid_constant__ Sweep s, const __grid_constant__ TileMaps maps,
+                                                                                int32_t *status) {
     using L = TileSmem<RB, CB, STATE, TERMS>;
-    static_assert(L::kBytes <= 227 * 1024, "shared memory of a block");
-    constexpr int H = CB / 2;  // columns of a thread
+    constexpr int H = CB / 2;                            // columns of a thread
     constexpr int kO1 = 128, kK = STATE ? 0 : 128 + CB;  // columns of tensor memory: S and O2 from 0
+    constexpr int SETS = RB == 128 ? TERMS : (TERMS + 1) / 2;
     extern __shared__ uint8_t raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     TileTables *tab = reinterpret_cast<TileTables *>(smem + L::kEnd);
     const uint32_t base = tc::smem_u32(smem);
-    const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index(), lq = w % 4, wc = w / 4, row = 32 * lq + lane;
+    const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index();
     volatile int *abort_flag = &tab->abort_flag;
-    if (tid == 0) {
-        for (int i = 0; i < 3; ++i) tc::mbar_init(&tab->bar[i], 1);
-        tab->abort_flag = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (w == 8) {  // the warp that uses them first
+        if (lane == 0) {
+            tc::mbar_init(&tab->got_a, 1);
+            tc::mbar_init(&tab->got_b, 1);
+            for (int i = 0; i < 3; ++i) tc::mbar_init(&tab->bar[i], 1);
+            tc::mbar_init(&tab->split, 8);
+            tc::mbar_init(&tab->weighted, 8);
+            tc::mbar_init(&tab->emptied, 8);
+            tab->abort_flag = tab->bad = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
     }
     if (RB == 64 && TERMS == 3) {  // the half beside the third term
-        for (int i = tid; i < L::kPanel / 16; i += 256) reinterpret_cast<uint4 *>(smem + L::kSplit + 3 * L::kPanel)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = tid; i < L::kPanel / 16; i += 288) reinterpret_cast<uint4 *>(smem + L::kSplit + 3 * L::kPanel)[i] = make_uint4(0, 0, 0, 0);
     }
-    if (w == 0) tc::tmem_alloc(&tab->slot, L::kCols);
+    if (w == 8) tc::tmem_alloc(&tab->slot, L::kCols);
     grid_wait();
     const int eh = blockIdx.x, e = eh / s.heads, h = eh % s.heads, seg = blockIdx.y, rev = s.reverse;
-    if (tid < 130) {
-        const float p = power(log2f(s.decay[h]), tid);
-        tab->pow[tid] = p;
-        tab->scaled[tid] = p * s.a_scale;
+    const int t_lo = seg * s.seg_len, t_hi = min(t_lo + s.seg_len, s.T), chunks = (t_hi - t_lo + 127) / 128;
+    if (tid < 256) {
+        const float l2 = log2f(s.decay[h]);
+        const int d = rev ? tid - 127 : 127 - tid;  // steps between
+        tab->weight[tid] = d < 0 ? 0.f : power(l2, d) * s.a_scale;
+        if (tid < 130) tab->pow[tid] = power(l2, tid);
     }
-    const bf16 *A = static_cast<const bf16 *>(s.a) + (long long)(h / s.share_a) * s.R;
-    const bf16 *B = static_cast<const bf16 *>(s.b) + (long long)(h / s.share_b) * s.C;
-    const bf16 *X = static_cast<const bf16 *>(s.x) + (long long)(h / s.share_x) * s.R;
-    const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
-    // Rows first .. first + count of the sweep into rows 0 .., zeros behind them and behind R and C.
-    auto rows = [&](int to, const bf16 *from, long long ld, int width, int padded, int first, int count) {
-        const int V = padded / 8;
-        for (int i = tid; i < 128 * V; i += 256) {
-            const int j = i / V, v = i % V, t = rev ? s.T - 1 - (first + j) : first + j;
-            const bool ok = j < count && v * 8 < width;
-            const bf16 *p = ok ? from + ((long long)t * s.Be + e) * ld + v * 8 : from;
-            tc::cp_async16(base + to + v / 8 * L::kPanel + j * 128 + ((v % 8) ^ (j % 8)) * 16, p, ok);
-        }
-    };
-    auto copy = [&](int first, int count) {
-        if (!STATE) rows(L::kX, X, s.ldx, s.R, RB, first, count);
-        rows(L::kA, A, s.lda, s.R, RB, first, count);
-        rows(L::kB, B, s.ldb, s.C, CB, first, count);
-        tc::cp_async_commit();
-    };
-    copy(n0, min(128, n1 - n0));
-
-    // row `row` of the state (with 64: rows 64 .. are the second terms' share), columns wc H ..
-    const long long sr = s.nseg > 1 ? s.C : s.stride_r, sc = s.nseg > 1 ? 1 : s.stride_c;
+    const long long sr = s.nseg > 1 ? s.seg_r : s.stride_r, sc = s.nseg > 1 ? s.seg_c : s.stride_c;
     const long long place = s.nseg > 1 ? ((long long)seg * s.Be * s.heads + eh) * s.R * s.C : eh * s.state;
     const float *in = STATE ? nullptr : s.nseg > 1 ? s.seg + place : s.m_in ? s.m_in + place : nullptr;
     float *out_state = STATE ? s.seg + place : s.nseg > 1 || !s.m_out ? nullptr : s.m_out + place;
-    float M[H];
-    {
-        const bool on = in && row < s.R && (RB == 128 || row < 64);
-        const float *p = in + row * sr + wc * H * sc;
-        if (sc == 1) {
-#pragma unroll
-            for (int c = 0; c < H; c += 4) {
-                const float4 f = on && wc * H + c < s.C ? *reinterpret_cast<const float4 *>(p + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-                M[c] = f.x, M[c + 1] = f.y, M[c + 2] = f.z, M[c + 3] = f.w;
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < H; ++c) M[c] = on && wc * H + c < s.C ? p[c * sc] : 0.f;
-        }
-    }
-    bool filled = in != nullptr;
-    auto store_m = [&] {  // its image: row `row`, pieces of 8 columns
-#pragma unroll
-        for (int c = 0; c < H; c += 8) {
-            const int v = (wc * H + c) / 8;
-            *reinterpret_cast<uint4 *>(smem + L::kM + v / 8 * L::kPanel + row * 128 + ((v % 8) ^ (row % 8)) * 16) =
-                make_uint4(pack_bf16x2(M[c], M[c + 1]), pack_bf16x2(M[c + 2], M[c + 3]), pack_bf16x2(M[c + 4], M[c + 5]), pack_bf16x2(M[c + 6], M[c + 7]));
-        }
-    };
-    if (!STATE && filled) store_m();
-    tc::tc_fence_before();
-    __syncthreads();
-    tc::tc_fence_after();
-    const uint32_t tmem = tab->slot, mine = tmem + ((uint32_t)(32 * lq) << 16);
-
-    // Descriptors: along the rows (K-major), and down the columns with the panels `apart` bytes from one another (MN-major).
-    const uint64_t dk = tc::smem_desc_sw(base, 16, 1024, 128), dm = tc::smem_desc_sw(base, L::kPanel, 1024, 128);
-    const uint32_t k_hi = (uint32_t)(dk >> 32), m_hi = (uint32_t)(dm >> 32), k_lo = (uint32_t)dk, m_lo = (uint32_t)dm;
-    auto along = [&](int panel, int k) { return k_lo + (uint32_t)(panel >> 4) + 2u * k; };       // step k of 16 columns of one panel
-    auto down = [&](int panels, int k) { return m_lo + (uint32_t)(panels >> 4) + 128u * k; };    // step k of 16 rows
+    const auto start_of = [&](int i) { return t_lo + 128 * (rev ? chunks - 1 - i : i); };  // of the i-th chunk
     bool ok = true;
-    uint32_t phase[3] = {0, 0, 0};
-    auto wait = [&](int i) {
-        ok = tc::mbar_wait(&tab->bar[i], phase[i], abort_flag, status) && ok;
-        phase[i] ^= 1;
-        tc::tc_fence_after();
-    };
 
-    // The n steps from `first` on, in rows 0 ..; resets: bit i of the four words set where done is at step first + i.
-    auto process = [&](int first, int n, const uint32_t (&resets)[4], bool last) {
-        int last_reset = -1;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (resets[i]) last_reset = 32 * i + 31 - __clz(resets[i]);
-        const bool update = !last || out_state;
-        if (!STATE && w == 0) {
-            if (tc::elect_one()) {
-#pragma unroll
-                for (int k = 0; k < RB / 16; ++k)
-                    tc::umma_bf16_lh(tmem, along(L::kX + k / 4 * L::kPanel, k % 4), k_hi, along(L::kA + k / 4 * L::kPanel, k % 4), k_hi,
-                                     tc::instr_desc(128, 128, 0, 0), k > 0);
-                if (filled) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int xk = k % (RB / 16);
-                        tc::umma_bf16_lh(tmem + kO1, along(L::kX + xk / 4 * L::kPanel, xk % 4), k_hi, down(L::kM, k), m_hi, tc::instr_desc(128, CB, 0, 1), k > 0);
-                    }
-                }
-                tc::umma_commit(&tab->bar[0]);
-            }
-            __syncwarp();
+    if (w == 8) {
+        // ---------------- tiles and products
+        const auto load = [&](int to, const CUtensorMap *map, int width, int head, int t, uint64_t *bar) {
+            for (int p = 0; p < width / 64; ++p) tc::tma_load_4d(base + to + p * L::kPanel, map, bar, 64 * p, head, e, t);
+        };
+        const auto load_x = [&](int i) { load(L::kX + (L::kAhead ? i % 2 * L::kWide : 0), &maps.x, RB, h / s.share_x, start_of(i), &tab->got_a); };
+        const auto load_a = [&](int i) { load(L::kA, &maps.a, RB, h / s.share_a, start_of(i), &tab->got_a); };
+        const auto load_b = [&](int i) { load(L::kB, &maps.b, CB, h / s.share_b, start_of(i), &tab->got_b); };
+        const auto expect_a = [&] { tc::mbar_arrive_expect_tx(&tab->got_a, (STATE ? 1 : 2) * L::kWide); };
+        const auto expect_b = [&] { tc::mbar_arrive_expect_tx(&tab->got_b, CB / 64 * L::kPanel); };
+        if (tc::elect_one()) {
+            expect_a();
+            if (!STATE) load_x(0);
+            load_a(0);
+            expect_b();
+            load_b(0);
         }
-        if (update) {
-            // w_j a_j in TERMS terms
-            constexpr int V = RB / 8;
-#pragma unroll 2
-            for (int i = tid; i < 128 * V; i += 256) {
-                const int j = i / V, v = i % V, at = j * 128 + ((v % 8) ^ (j % 8)) * 16;
-                const float wj = j < n && (rev ? j >= last_reset : j > last_reset) ? tab->scaled[max(n - 1 - j + rev, 0)] : 0.f;
-                const uint4 a = *reinterpret_cast<const uint4 *>(smem + L::kA + v / 8 * L::kPanel + at);
-                const uint32_t in4[4] = {a.x, a.y, a.z, a.w};
-                uint32_t part[TERMS][4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float f0 = wj == 0.f ? 0.f : low(in4[q]) * wj, f1 = wj == 0.f ? 0.f : high(in4[q]) * wj;
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t) {
-                        part[t][q] = pack_bf16x2(f0, f1);
-                        f0 -= low(part[t][q]);
-                        f1 -= high(part[t][q]);
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < TERMS; ++t)
-                    *reinterpret_cast<uint4 *>(smem + L::kSplit + (RB == 128 ? 2 * t + v / 8 : t) * L::kPanel + at) =
-                        make_uint4(part[t][0], part[t][1], part[t][2], part[t][3]);
-            }
-            tc::fence_async_smem();
-            tc::tc_fence_before();
-        }
+        __syncwarp();
+        tc::tc_fence_before();
         __syncthreads();
-        if (update && w == 0) {
-            tc::tc_fence_after();
-            if (tc::elect_one()) {
-                constexpr int SETS = RB == 128 ? TERMS : (TERMS + 1) / 2;
-#pragma unroll
-                for (int t = SETS - 1; t >= 0; --t)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        tc::umma_bf16_lh(tmem + kK, down(L::kSplit + 2 * t * L::kPanel, k), m_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 1, 1),
-                                         t < SETS - 1 || k > 0);
-                tc::umma_commit(&tab->bar[1]);
-            }
-            __syncwarp();
-        }
-        int visible = 0;      // the first step that this row sees
-        bool reached = true;  // and whether it sees the state
-        if constexpr (!STATE) {
-            const int upto = rev ? row : row - 1;  // the last flag in front of this row
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = upto - 32 * i;
-                const uint32_t f = k < 0 ? 0 : resets[i] & (k >= 31 ? 0xffffffffu : (2u << k) - 1);
-                if (f) {
-                    visible = 32 * i + 31 - __clz(f) + 1 - rev;
-                    reached = false;
-                }
-            }
-            wait(0);
-            // P: row `row`, columns 64 wc ..
-            uint8_t *p = smem + (wc ? L::kP1 : L::kP0) + row * 128;
-            if (wc == 1 && lq < 2) {
-#pragma unroll
-                for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4 *>(p + v * 16) = make_uint4(0, 0, 0, 0);
-            } else {
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float f[32];
-                    tc::tmem_ld32(mine + 64 * wc + 32 * half, f);
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        const int j = 64 * wc + 32 * half + c;
-                        f[c] = j <= row && j >= visible ? f[c] * tab->scaled[max(row - j, 0)] : 0.f;
-                    }
-#pragma unroll
-                    for (int c = 0; c < 32; c += 8)
-                        *reinterpret_cast<uint4 *>(p + ((4 * half + c / 8) ^ (row % 8)) * 16) =
-                            make_uint4(pack_bf16x2(f[c], f[c + 1]), pack_bf16x2(f[c + 2], f[c + 3]), pack_bf16x2(f[c + 4], f[c + 5]), pack_bf16x2(f[c + 6], f[c + 7]));
-                }
-            }
-            tc::fence_async_smem();
-            tc::tc_fence_before();
-            __syncthreads();
-            if (w == 0) {
+        tc::tc_fence_after();
+        const uint32_t tmem = tab->slot;
+        // Descriptors: along the rows (K-major), and down the columns (MN-major, panels side by side).
+        const uint64_t dk = tc::smem_desc_sw(base, 16, 1024, 128), dm = tc::smem_desc_sw(base, L::kPanel, 1024, 128);
+        const uint32_t k_hi = (uint32_t)(dk >> 32), m_hi = (uint32_t)(dm >> 32), k_lo = (uint32_t)dk, m_lo = (uint32_t)dm;
+        const auto along = [&](int panel, int k) { return k_lo + (uint32_t)(panel >> 4) + 2u * k; };     // step k of 16 columns of one panel
+        const auto down = [&](int panels, int k) { return m_lo + (uint32_t)(panels >> 4) + 128u * k; };  // step k of 16 rows
+        const auto wait = [&](uint64_t *bar, int i) { ok = tc::mbar_wait_warp(bar, i & 1, abort_flag, status) && ok; };
+        bool filled = in != nullptr;
+        for (int i = 0; i < chunks; ++i) {
+            const bool more = i + 1 < chunks, update = more || out_state;
+            const int x = L::kX + (L::kAhead ? i % 2 * L::kWide : 0);
+            if (!STATE) {
+                wait(&tab->got_a, i);
                 tc::tc_fence_after();
                 if (tc::elect_one()) {
 #pragma unroll
+                    for (int k = 0; k < RB / 16; ++k)
+                        tc::umma_bf16_lh(tmem, along(x + k / 4 * L::kPanel, k % 4), k_hi, along(L::kA + k / 4 * L::kPanel, k % 4), k_hi,
+                                         tc::instr_desc(128, 128, 0, 0), k > 0);
+                    if (filled) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int xk = k % (RB / 16);
+                            tc::umma_bf16_lh(tmem + kO1, along(x + xk / 4 * L::kPanel, xk % 4), k_hi, down(L::kM, k), m_hi, tc::instr_desc(128, CB, 0, 1), k > 0);
+                        }
+                    }
+                    tc::umma_commit(&tab->bar[0]);
+                    if (L::kAhead && more) {
+                        tc::bulk_wait_read<0>();  // the chunk before has left that place
+                        expect_a();
+                        load_x(i + 1);
+                    }
+                }
+                __syncwarp();
+            }
+            wait(&tab->split, i);
+            if (update) {
+                wait(&tab->got_b, i);
+                tc::tc_fence_after();
+                if (tc::elect_one()) {
+#pragma unroll
+                    for (int t = SETS - 1; t >= 0; --t)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            tc::umma_bf16_lh(tmem + kK, down(L::kSplit + 2 * t * L::kPanel, k), m_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 1, 1),
+                                             t < SETS - 1 || k > 0);
+                    tc::umma_commit(&tab->bar[1]);
+                }
+                __syncwarp();
+            }
+            if (STATE && more && tc::elect_one()) {
+                expect_a();
+                load_a(i + 1);
+            }
+            __syncwarp();
+            if (!STATE) {
+                if (L::kAhead && more) {
+                    wait(&tab->bar[0], i);  // S is made
+                    if (tc::elect_one()) load_a(i + 1);
+                    __syncwarp();
+                }
+                wait(&tab->weighted, i);
+                if (!update) wait(&tab->got_b, i);
+                tc::tc_fence_after();
+                if (tc::elect_one()) {
+                    const int p1 = RB == 128 ? x + L::kPanel : L::kA;
+#pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        tc::umma_bf16_lh(tmem, along(k < 4 ? L::kP0 : L::kP1, k % 4), k_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 0, 1), k > 0);
+                        tc::umma_bf16_lh(tmem, along(k < 4 ? x : p1, k % 4), k_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 0, 1), k > 0);
                     tc::umma_commit(&tab->bar[2]);
                 }
                 __syncwarp();
             }
-        }
-        if (update) {
-            wait(1);
-            const float keep = tab->pow[n];
-#pragma unroll
-            for (int c0 = 0; c0 < H; c0 += 32) {
-                float f[32];
-                tc::tmem_ld32(mine + kK + wc * H + c0, f);
-#pragma unroll
-                for (int c = 0; c < 32; ++c) M[c0 + c] = last_reset < 0 ? fmaf(M[c0 + c], keep, f[c]) : f[c];
-            }
-            if (!STATE && !last) store_m();
-        }
-        if constexpr (!STATE) {
-            wait(2);
-            const float f1 = tab->pow[row + 1 - rev];
-            const int t = rev ? s.T - 1 - (first + row) : first + row;
-            const long long at = (long long)t * s.Be + e;
-#pragma unroll
-            for (int c0 = 0; c0 < H; c0 += 32) {
-                float o[32];
-                tc::tmem_ld32(mine + wc * H + c0, o);
-                if (filled) {
-                    float m[32];
-                    tc::tmem_ld32(mine + kO1 + wc * H + c0, m);
-                    if (reached) {
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) o[c] = fmaf(m[c], f1, o[c]);
-                    }
+            if (more) {  // all that reads B is made
+                wait(&tab->bar[STATE ? 1 : 2], i);
+                if (tc::elect_one()) {
+                    expect_b();
+                    load_b(i + 1);
                 }
-                if (s.shared) {
-                    float *to = s.shared + (at * s.heads + h) * s.C + wc * H + c0;
-                    if (row < n) {
-#pragma unroll
-                        for (int c = 0; c < 32; c += 4)
-                            if (wc * H + c0 + c < s.C)
-                                *reinterpret_cast<float4 *>(to + c) = make_float4(o[c] * s.out_scale, o[c + 1] * s.out_scale, o[c + 2] * s.out_scale, o[c + 3] * s.out_scale);
-                    }
-                } else {  // through the place of P to whole rows
-#pragma unroll
-                    for (int c = 0; c < 32; c += 8) {
-                        const int v = (wc * H + c0 + c) / 8;
-                        *reinterpret_cast<uint4 *>(smem + (v / 8 ? L::kP1 : L::kP0) + row * 128 + ((v % 8) ^ (row % 8)) * 16) =
-                            make_uint4(pack_bf16x2(o[c] * s.out_scale, o[c + 1] * s.out_scale), pack_bf16x2(o[c + 2] * s.out_scale, o[c + 3] * s.out_scale),
-                                       pack_bf16x2(o[c + 4] * s.out_scale, o[c + 5] * s.out_scale), pack_bf16x2(o[c + 6] * s.out_scale, o[c + 7] * s.out_scale));
-                    }
+                __syncwarp();
+            }
+            wait(&tab->emptied, i);
+            tc::tc_fence_after();
+            if (!STATE && tc::elect_one()) {
+                if (!s.shared) {
+                    for (int p = 0; p < CB / 64; ++p)
+                        if (64 * p < s.C) tc::tma_store_4d(&maps.out, base + (p == 0 ? x : RB == 128 ? x + L::kPanel : L::kA), 64 * p, h, e, start_of(i));
+                    tc::bulk_commit();
+                }
+                if (!L::kAhead && more) {
+                    tc::bulk_wait_read<0>();
+                    expect_a();
+                    load_x(i + 1);
+                    load_a(i + 1);
                 }
             }
-            if (!s.shared) {
-                __syncthreads();
-                constexpr int V = CB / 8;
-#pragma unroll 4
-                for (int i = tid; i < 128 * V; i += 256) {
-                    const int j = i / V, v = i % V, tj = rev ? s.T - 1 - (first + j) : first + j;
-                    if (j < n && v * 8 < s.C)
-                        *reinterpret_cast<uint4 *>(static_cast<bf16 *>(s.out) + ((long long)tj * s.Be + e) * s.ldo + (long long)h * s.C + v * 8) =
-                            *reinterpret_cast<const uint4 *>(smem + (v / 8 ? L::kP1 : L::kP0) + j * 128 + ((v % 8) ^ (j % 8)) * 16);
-                }
+            __syncwarp();
+            filled = true;
+        }
+        if (!STATE && tc::elect_one()) tc::bulk_wait_all();
+        __syncwarp();
+        if (!ok) {  // copies in flight land meanwhile
+            const long long t0 = clock64();
+            while (clock64() - t0 < 200000) {
             }
         }
-        tc::tc_fence_before();
-        filled = true;
-    };
-
-    uint32_t any = 0;
-    for (int n = n0; n < n1; n += 128) {
-        const int count = min(128, n1 - n);
-        const bool more = n + 128 < n1;
-        uint32_t resets[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int step = n + 32 * i + lane;
-            resets[i] = __ballot_sync(0xffffffffu, s.done && step < n1 && s.done[(long long)(rev ? s.T - 1 - step : step) * s.Be + e] != 0);
-            any |= resets[i];
-        }
-        if (n > n0) {
-            __syncthreads();  // every operand of the last chunk is read
-            copy(n, count);
-        }
-        tc::cp_async_wait<0>();
-        bool bad = false;
-        for (int i = tid; i < 128 * CB / 8; i += 256) {  // what this thread has copied of B
-            const int j = i / (CB / 8), v = i % (CB / 8);
-            bad |= not_finite(*reinterpret_cast<const uint4 *>(smem + L::kB + v / 8 * L::kPanel + j * 128 + ((v % 8) ^ (j % 8)) * 16));
-        }
-        tc::fence_async_smem();  // the copies, and M
-        bad = __syncthreads_or(bad);
-        tc::tc_fence_after();
-        for (int i = 0; i < (bad ? count : 1); ++i) {
-            if (bad) {
-                __syncthreads();
-                copy(n + i, 1);
-                tc::cp_async_wait<0>();
-                tc::fence_async_smem();
-                __syncthreads();
-                tc::tc_fence_after();
-                uint32_t one[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (i / 32 == k) one[0] = resets[k] >> (i % 32) & 1;
-                process(n + i, 1, one, !more && i == count - 1);
-            } else {
-                process(n, count, resets, !more);
-            }
-        }
-        if (__syncthreads_or(!ok)) break;
-    }
-    if (STATE && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any != 0;
-    if (out_state) {
-        if (RB == 64) {  // the two shares of a row
-            float *x = reinterpret_cast<float *>(smem + L::kSplit);
-            if (row >= 64) {
-#pragma unroll
-                for (int c = 0; c < H; ++c) x[(wc * H + c) * 64 + row - 64] = M[c];
-            }
-            __syncthreads();
-            if (row < 64) {
-#pragma unroll
-                for (int c = 0; c < H; ++c) M[c] += x[(wc * H + c) * 64 + row];
-            }
-        }
-        if (row < s.R && (RB == 128 || row < 64)) {
-            float *p = out_state + row * sr + wc * H * sc;
+    } else {
+        // ---------------- what is between the products
+        const int lq = w % 4, wc = w / 4, row = 32 * lq + lane;
+        // row `row` of the state (with 64: rows 64 .. are the second terms' share), columns wc H ..
+        float M[H];
+        const bool mine_on = row < s.R && (RB == 128 || row < 64);
+        {
+            const bool on = in && mine_on;
+            const float *p = in + row * sr + wc * H * sc;
             if (sc == 1) {
 #pragma unroll
-                for (int c = 0; c < H; c += 4)
-                    if (wc * H + c < s.C) *reinterpret_cast<float4 *>(p + c) = make_float4(M[c], M[c + 1], M[c + 2], M[c + 3]);
+                for (int c = 0; c < H; c += 4) {
+                    const float4 f = on && wc * H + c < s.C ? *reinterpret_cast<const float4 *>(p + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    M[c] = f.x, M[c + 1] = f.y, M[c + 2] = f.z, M[c + 3] = f.w;
+                }
             } else {
 #pragma unroll
-                for (int c = 0; c < H; ++c)
-                    if (wc * H + c < s.C) p[c * sc] = M[c];
+                for (int c = 0; c < H; ++c) M[c] = on && wc * H + c < s.C ? p[c * sc] : 0.f;
+            }
+        }
+        const auto piece = [&](int panel, int r, int v) { return smem + panel + r * 128 + ((v ^ r) & 7) * 16; };
+        const auto store_m = [&] {
+#pragma unroll
+            for (int c = 0; c < H; c += 8) {
+                const int v = (wc * H + c) / 8;
+                *reinterpret_cast<uint4 *>(piece(L::kM + v / 8 * L::kPanel, row, v)) =
+                    make_uint4(pack_bf16x2(M[c], M[c + 1]), pack_bf16x2(M[c + 2], M[c + 3]), pack_bf16x2(M[c + 4], M[c + 5]), pack_bf16x2(M[c + 6], M[c + 7]));
+            }
+        };
+        bool filled = in != nullptr, bad = false;
+        if (!STATE && filled) store_m();
+        tc::fence_async_smem();
+        tc::tc_fence_before();
+        __syncthreads();
+        tc::tc_fence_after();
+        const uint32_t mine = tab->slot + ((uint32_t)(32 * lq) << 16);
+        const auto wait = [&](uint64_t *bar, int i) { ok = tc::mbar_wait(bar, i & 1, abort_flag, status) && ok; };
+        const auto tell = [&](uint64_t *bar) {
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(bar);
+        };
+        uint32_t any = 0, flags[4];
+        const auto flags_of = [&](int i, uint32_t (&f)[4]) {  // done at the steps of the i-th chunk
+            const int t0 = start_of(i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int t = t0 + 32 * k + lane;
+                f[k] = s.done && t < t_hi ? s.done[(long long)t * s.Be + e] : 0;
+            }
+        };
+        flags_of(0, flags);
+        for (int i = 0; i < chunks; ++i) {
+            const int n = min(128, t_hi - start_of(i));
+            const bool more = i + 1 < chunks, update = more || out_state;
+            const int x = L::kX + (L::kAhead ? i % 2 * L::kWide : 0);
+            uint32_t resets[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) any |= resets[k] = __ballot_sync(0xffffffffu, flags[k] != 0);
+            if (more) flags_of(i + 1, flags);
+            const bool some = (resets[0] | resets[1] | resets[2] | resets[3]) != 0;
+            // the flag that the state behind the chunk sees first, looking back
+            int edge = rev ? 128 : -1;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (!rev && resets[k]) edge = 32 * k + 31 - __clz(resets[k]);
+                if (rev && resets[3 - k]) edge = 32 * (3 - k) + __ffs(resets[3 - k]) - 1;
+            }
+            wait(&tab->got_a, i);
+            if (update) {
+                // w_c a_c in TERMS terms
+                constexpr int V = RB / 8;
+#pragma unroll 4
+                for (int k = 0; k < 128 * V / 256; ++k) {
+                    const int c = (k * 256 + tid) / V, v = (k * 256 + tid) % V;
+                    const bool sees = c < n && (rev ? c <= edge : c > edge);
+                    const float wj = sees ? tab->pow[max(rev ? c + 1 : n - 1 - c, 0)] * s.a_scale : 0.f;
+                    const uint4 a = *reinterpret_cast<const uint4 *>(piece(L::kA + v / 8 * L::kPanel, c, v));
+                    const uint32_t in4[4] = {a.x, a.y, a.z, a.w};
+                    uint32_t part[TERMS][4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float f0 = low(in4[q]) * wj, f1 = high(in4[q]) * wj;
+                        f0 = sees ? f0 : 0.f;
+                        f1 = sees ? f1 : 0.f;
+#pragma unroll
+                        for (int t = 0; t < TERMS; ++t) {
+                            part[t][q] = pack_bf16x2(f0, f1);
+                            f0 -= low(part[t][q]);
+                            f1 -= high(part[t][q]);
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t)
+                        *reinterpret_cast<uint4 *>(piece(L::kSplit + (RB == 128 ? 2 * t + v / 8 : t) * L::kPanel, c, v)) =
+                            make_uint4(part[t][0], part[t][1], part[t][2], part[t][3]);
+                }
+                tc::fence_async_smem();
+            }
+            tell(&tab->split);
+            wait(&tab->got_b, i);
+#pragma unroll
+            for (int k = 0; k < CB / 16; ++k) {
+                const int r = (k * 256 + tid) / (CB / 8), v = (k * 256 + tid) % (CB / 8);
+                bad |= not_finite(*reinterpret_cast<const uint4 *>(piece(L::kB + v / 8 * L::kPanel, r, v)));
+            }
+            bool reached = true;  // whether this row sees the state in front of the chunk
+            if constexpr (!STATE) {
+                int bound = rev ? 127 : 0;  // the last step that it sees (backwards: the farthest)
+                if (some) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        // flags at steps in front of this one; backwards, at it and behind it
+                        const int at = row - 32 * (rev ? 3 - k : k), from = max(at, 0);
+                        const uint32_t r = resets[rev ? 3 - k : k];
+                        const uint32_t f = rev ? (at > 31 ? 0u : r >> from << from) : (at <= 0 ? 0u : at > 31 ? r : r & ((1u << at) - 1));
+                        if (f) {
+                            bound = rev ? 32 * (3 - k) + __ffs(f) - 1 : 32 * k + 32 - __clz(f);
+                            reached = false;
+                        }
+                    }
+                }
+                wait(&tab->bar[0], i);
+                if (RB == 64 && wc == 1) wait(&tab->split, i);  // the other warps have read A, whose place the second half takes
+                tc::tc_fence_after();
+                // P: row `row`, columns 64 wc ..
+                const int panel = wc == 0 ? x : RB == 128 ? x + L::kPanel : L::kA;
+                if (rev ? wc == 0 && lq >= 2 : wc == 1 && lq < 2) {
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4 *>(piece(panel, row, v)) = make_uint4(0, 0, 0, 0);
+                } else {
+                    const float *weight = tab->weight + 127 - row + 64 * wc;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float f[32];
+                        tc::tmem_ld32(mine + 64 * wc + 32 * half, f);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            const float wt = weight[32 * half + c], p = f[c] * wt;
+                            f[c] = wt != 0.f ? p : 0.f;  // whatever it is that is not seen
+                        }
+                        if (some) {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                const int j = 64 * wc + 32 * half + c;
+                                if (rev ? j > bound : j < bound) f[c] = 0.f;
+                            }
+                        }
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8)
+                            *reinterpret_cast<uint4 *>(piece(panel, row, 4 * half + c / 8)) =
+                                make_uint4(pack_bf16x2(f[c], f[c + 1]), pack_bf16x2(f[c + 2], f[c + 3]), pack_bf16x2(f[c + 4], f[c + 5]), pack_bf16x2(f[c + 6], f[c + 7]));
+                    }
+                }
+                tc::fence_async_smem();
+                tc::tc_fence_before();
+                tell(&tab->weighted);
+            }
+            if (update) {
+                wait(&tab->bar[1], i);
+                tc::tc_fence_after();
+                const float keep = tab->pow[n];
+#pragma unroll
+                for (int c0 = 0; c0 < H; c0 += 32) {
+                    float f[32];
+                    tc::tmem_ld32(mine + kK + wc * H + c0, f);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) M[c0 + c] = some ? f[c] : fmaf(M[c0 + c], keep, f[c]);
+                }
+                if (!STATE && more) store_m();
+            }
+            if constexpr (!STATE) {
+                wait(&tab->bar[2], i);
+                tc::tc_fence_after();
+                const float f1 = tab->pow[max(rev ? n - 1 - row : row + 1, 0)];
+                const long long at = (long long)(start_of(i) + row) * s.Be + e;
+#pragma unroll
+                for (int c0 = 0; c0 < H; c0 += 32) {
+                    float o[32];
+                    tc::tmem_ld32(mine + wc * H + c0, o);
+                    if (filled) {
+                        float m[32];
+                        tc::tmem_ld32(mine + kO1 + wc * H + c0, m);
+                        if (reached) {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) o[c] = fmaf(m[c], f1, o[c]);
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) o[c] *= s.out_scale;
+                    if (s.shared) {
+                        float *to = s.shared + (at * s.heads + h) * s.C + wc * H + c0;
+                        if (row < n) {
+#pragma unroll
+                            for (int c = 0; c < 32; c += 4)
+                                if (wc * H + c0 + c < s.C) *reinterpret_cast<float4 *>(to + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                        }
+                    } else {  // through the place of P
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8) {
+                            const int v = (wc * H + c0 + c) / 8;
+                            *reinterpret_cast<uint4 *>(piece(v < 8 ? x : RB == 128 ? x + L::kPanel : L::kA, row, v)) =
+                                make_uint4(pack_bf16x2(o[c], o[c + 1]), pack_bf16x2(o[c + 2], o[c + 3]), pack_bf16x2(o[c + 4], o[c + 5]), pack_bf16x2(o[c + 6], o[c + 7]));
+                        }
+                    }
+                }
+            }
+            tc::fence_async_smem();
+            tc::tc_fence_before();
+            tell(&tab->emptied);
+            filled = true;
+        }
+        if (bad) tab->bad = 1;
+        if (STATE && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any != 0;
+        asm volatile("bar.sync 4, 256;" ::: "memory");
+        if (out_state && !tab->bad) {
+            if (RB == 64) {  // the two shares of a row
+                float *y = reinterpret_cast<float *>(smem + L::kSplit);
+                if (row >= 64) {
+#pragma unroll
+                    for (int c = 0; c < H; ++c) y[(wc * H + c) * 64 + row - 64] = M[c];
+                }
+                asm volatile("bar.sync 4, 256;" ::: "memory");
+                if (row < 64) {
+#pragma unroll
+                    for (int c = 0; c < H; ++c) M[c] += y[(wc * H + c) * 64 + row];
+                }
+            }
+            if (mine_on) {
+                float *p = out_state + row * sr + wc * H * sc;
+                if (sc == 1) {
+#pragma unroll
+                    for (int c = 0; c < H; c += 4)
+                        if (wc * H + c < s.C) *reinterpret_cast<float4 *>(p + c) = make_float4(M[c], M[c + 1], M[c + 2], M[c + 3]);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < H; ++c)
+                        if (wc * H + c < s.C) p[c * sc] = M[c];
+                }
             }
         }
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (w == 0) {
+    if (w == 8) {
         tc::tc_fence_after();
-        tc::tmem_dealloc(tmem, L::kCols);
+        tc::tmem_dealloc(tab->slot, L::kCols);
     }
+    if (tab->bad) segment_slowly<STATE>(s, reinterpret_cast<float *>(smem), in, out_state, sr, sc, eh, t_lo, t_hi);
 }
 
 // What each segment starts from, in place of what it adds, and the state that is left.
@@ -1057,24 +1174,25 @@ __global__ void __launch_bounds__(256) segments_kernel(Sweep s) {
     const int eh = blockIdx.x, h = eh % s.heads, i = blockIdx.y * 256 + threadIdx.x;  // element r * C + c
     if (i >= s.R * s.C) return;
     const long long at = (i / s.C) * s.stride_r + (i % s.C) * s.stride_c, all = (long long)s.Be * s.heads;
-    const float l2 = log2f(s.decay[h]), whole = power(l2, s.seg_len), rest = power(l2, s.T - (s.nseg - 1) * s.seg_len);
+    const float l2 = log2f(s.decay[h]), whole = power(l2, s.seg_len), tail = power(l2, s.T - (s.nseg - 1) * s.seg_len);
     float m = s.m_in ? s.m_in[eh * s.state + at] : 0.f;
     float *p = s.seg + eh * (long long)s.R * s.C + i;
     const long long step = all * s.R * s.C;
-    for (int seg = 0; seg < s.nseg; seg += 8) {
+    for (int n = 0; n < s.nseg; n += 8) {  // in the sweep's order
         float add[8];
         int reset[8];
-        const int n = min(8, s.nseg - seg);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            add[k] = k < n ? p[(seg + k) * step] : 0.f;
-            reset[k] = k < n ? s.seg_reset[(seg + k) * all + eh] : 0;
+            const int seg = s.reverse ? s.nseg - 1 - n - k : n + k;
+            add[k] = n + k < s.nseg ? p[seg * step] : 0.f;
+            reset[k] = n + k < s.nseg ? s.seg_reset[seg * all + eh] : 0;
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            if (k >= n) break;
-            p[(seg + k) * step] = m;
-            m = reset[k] ? add[k] : fmaf(seg + k == s.nseg - 1 ? rest : whole, m, add[k]);
+            if (n + k >= s.nseg) break;
+            const int seg = s.reverse ? s.nseg - 1 - n - k : n + k;
+            p[seg * step] = m;
+            m = reset[k] ? add[k] : fmaf(seg == s.nseg - 1 ? tail : whole, m, add[k]);
         }
     }
     if (s.m_out) s.m_out[eh * s.state + at] = m;
@@ -1219,22 +1337,34 @@ int short_launch(const Sweep &s, cudaStream_t st) {
     return s.m_out ? ppo_launch(short_kernel<128, 3>, grid, dim3(128), 0, st, s) : ppo_launch(short_kernel<128, 2>, grid, dim3(128), 0, st, s);
 }
 template <int RB, int CB, bool STATE, int TERMS>
-int tile_launch_as(const Sweep &s, cudaStream_t st) {
+int tile_launch_as(const Sweep &s, const TileMaps &maps, cudaStream_t st) {
     using L = TileSmem<RB, CB, STATE, TERMS>;
     static PerDevice<bool> allowed;
     int32_t *status = ppo_device_status_ptr();
     if (!status) return PPO_ERR_CUDA;
     PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(tile_kernel<RB, CB, STATE, TERMS>, L::kBytes); }));
-    return ppo_launch(tile_kernel<RB, CB, STATE, TERMS>, dim3(s.Be * s.heads, s.nseg), dim3(256), L::kBytes, st, s, status);
+    return ppo_launch(tile_kernel<RB, CB, STATE, TERMS>, dim3(s.Be * s.heads, s.nseg), dim3(288), L::kBytes, st, s, maps, status);
 }
 template <bool STATE, int TERMS>
-int tile_launch_of(const Sweep &s, cudaStream_t st) {
-    if (s.R <= 64) return s.C <= 64 ? tile_launch_as<64, 64, STATE, TERMS>(s, st) : tile_launch_as<64, 128, STATE, TERMS>(s, st);
-    return s.C <= 64 ? tile_launch_as<128, 64, STATE, TERMS>(s, st) : tile_launch_as<128, 128, STATE, TERMS>(s, st);
+int tile_launch_of(const Sweep &s, const TileMaps &maps, cudaStream_t st) {
+    if (s.R <= 64) return s.C <= 64 ? tile_launch_as<64, 64, STATE, TERMS>(s, maps, st) : tile_launch_as<64, 128, STATE, TERMS>(s, maps, st);
+    return s.C <= 64 ? tile_launch_as<128, 64, STATE, TERMS>(s, maps, st) : tile_launch_as<128, 128, STATE, TERMS>(s, maps, st);
 }
 template <bool STATE>
-int tile_launch(const Sweep &s, bool exact, cudaStream_t st) {
-    return exact ? tile_launch_of<STATE, 3>(s, st) : tile_launch_of<STATE, 2>(s, st);
+int tile_launch(const Sweep &s, const TileMaps &maps, bool exact, cudaStream_t st) {
+    return exact ? tile_launch_of<STATE, 3>(s, maps, st) : tile_launch_of<STATE, 2>(s, maps, st);
+}
+// Rows of heads as [T][Be][heads][width], boxes of 128 steps and 64 columns of one head.
+int tile_maps(const Sweep &s, TileMaps *m) {
+    const int box[4] = {64, 1, 1, 128};
+    const auto map = [&](CUtensorMap *to, const void *p, int width, int heads, long long ld) {
+        const long long dims[4] = {width, heads, s.Be, s.T}, strides[3] = {2ll * width, 2 * ld, 2 * ld * s.Be};
+        return make_map_strided(to, p, 4, dims, strides, box);
+    };
+    PPO_TRY(map(&m->x, s.x, s.R, s.heads / s.share_x, s.ldx));
+    PPO_TRY(map(&m->a, s.a, s.R, s.heads / s.share_a, s.lda));
+    PPO_TRY(map(&m->b, s.b, s.C, s.heads / s.share_b, s.ldb));
+    return s.shared ? PPO_OK : map(&m->out, s.out, s.C, s.heads, s.ldo);
 }
 // Rows of 16-byte vectors.
 bool chunks_fit(const Sweep &s) {
@@ -1244,15 +1374,18 @@ bool chunks_fit(const Sweep &s) {
 // bf16 rows that vectors fit: up to 16 steps, up to 64, more.
 template <typename T>
 int sweep(const Sweep &s, cudaStream_t st) {
-    const bool chunks = std::is_same_v<T, bf16> && chunks_fit(s), exact = s.m_out != nullptr;
-    if (s.nseg > 1) {
-        PPO_TRY(chunks ? tile_launch<true>(s, exact, st) : sweep_launch<T, true>(s, st));
+    bool chunks = std::is_same_v<T, bf16> && chunks_fit(s);
+    const bool exact = s.m_out != nullptr;
+    TileMaps maps = {};
+    if (chunks && s.T > kChunk) chunks = tile_maps(s, &maps) == PPO_OK;  // strides of 2^40 bytes have none
+    if (s.nseg > 1 && !s.seg_made) {
+        PPO_TRY(chunks ? tile_launch<true>(s, maps, exact, st) : sweep_launch<T, true>(s, st));
         PPO_TRY(ppo_launch(segments_kernel, dim3(s.Be * s.heads, ppo_cdiv((long long)s.R * s.C, 256)), dim3(256), 0, st, s));
     }
     if (!chunks) return sweep_launch<T, false>(s, st);
     if (s.T <= 16) return short_launch(s, st);
     if (s.T <= kChunk) return chunk_launch<false>(s, exact, st);
-    return tile_launch<false>(s, exact && s.nseg == 1, st);
+    return tile_launch<false>(s, maps, exact && s.nseg == 1, st);
 }
 
 Sweep sweep_of(const ppo_decay_attention_desc *d, const float *decay, const uint8_t *done, float *seg) {
@@ -1274,14 +1407,16 @@ Sweep sweep_of(const ppo_decay_attention_desc *d, const float *decay, const uint
 void plain_state(Sweep *s, const ppo_decay_attention_desc *d) {
     s->R = d->dk;
     s->C = d->dv;
-    s->stride_r = d->dv;
-    s->stride_c = 1;
+    s->stride_r = s->seg_r = d->dv;
+    s->stride_c = s->seg_c = 1;
 }
 void turned_state(Sweep *s, const ppo_decay_attention_desc *d) {
     s->R = d->dv;
     s->C = d->dk;
     s->stride_r = 1;
     s->stride_c = d->dv;
+    s->seg_r = d->dk;
+    s->seg_c = 1;
 }
 
 bool misaligned(std::initializer_list<const void *> ps, size_t a) {
@@ -1339,7 +1474,10 @@ extern "C" int ppo_decay_attention_bwd(const ppo_decay_attention_desc *d, const 
         s.out_scale = d->scale;
         s.m_in = state_in;
         PPO_TRY(sweep<T>(s, st));
-        for (int key = 1; key >= 0; --key) {  // dk, then dv, which leaves the gradient of the state that came in
+        // dk reads the states of dv's sweep, so it comes first where the sequence is not cut, for dstate_in may be dstate_out; with
+        // segments dv's leaves in the workspace what they start from
+        const int first = s.nseg > 1 ? 0 : 1;
+        for (int key : {first, 1 - first}) {
             s = sweep_of(d, decay, done, seg);
             s.reverse = 1;
             s.share_x = share;
@@ -1348,6 +1486,9 @@ extern "C" int ppo_decay_attention_bwd(const ppo_decay_attention_desc *d, const 
             T *out = static_cast<T *>(key ? dk : dv);
             if (key) {
                 turned_state(&s, d);
+                s.seg_made = s.nseg > 1;
+                s.seg_r = 1;
+                s.seg_c = d->dv;
                 s.a = d_o, s.lda = d->ldo, s.b = q, s.ldb = d->ldq, s.x = v, s.ldx = d->ldv, s.ldo = d->ldk;
             } else {
                 plain_state(&s, d);

@@ -115,6 +115,26 @@ def test_gradients(shape, dtype, state):
     assert ppo.ppo_poll_status() == 0
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(1500, 5, 16, 4, 64, 64, 0.002), (900, 9, 8, 8, 128, 128, 0.002), (700, 6, 16, 4, 64, 128, 0.0), (650, 7, 8, 8, 104, 48, 0.01)],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_many_blocks_of_many_chunks(shape, dtype):
+    """Blocks that share an SM and run at different speeds, several chunks each."""
+    c = Case(*shape[:6], dtype, shape[6])
+    (o, s), (ow, sw), (oa, sa) = c.fwd(), plain.attention(*c.args()), plain.attention_abs(*c.args())
+    _near(o, ow, oa, c.T, c.dk, dtype)
+    _near(s, sw, sa, c.T, c.dk, F32)
+    want, size = (f(*c.args(), c.do, c.ds) for f in (plain.attention, plain.attention_abs))
+    first = c.bwd()
+    for i in range(3):
+        _near(first[i], want[i], size[i], c.T, max(c.dk, c.dv) * (c.heads // c.kv), dtype)
+    _near(first[3], want[3], size[3], c.T, c.dk, F32)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(first, c.bwd()))
+        assert all(torch.equal(a, b) for a, b in zip((o, s), c.fwd()))
+    assert ppo.ppo_poll_status() == 0
+
+
 @pytest.mark.parametrize("offset", [0, 8, 3])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_that_are_parts_of_wider_ones(dtype, offset):
