@@ -674,8 +674,8 @@ __global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(Sweep s) {
 // ---- chunks of 128 steps on tcgen05 (bf16, more than 64 steps) ----
 //
 // The same four products as tcgen05.mma with accumulators in tensor memory, whole heads per block: S = X A^T and O1 = X M as soon as the
-// rows have landed; K = (w A)^T B while S is weighted into P; O2 = P B.  Warp 8 moves tiles (TMA) and issues the products; the other
-// eight are between them: a thread owns a row of each accumulator (a step, or a row of the state) and half of its columns.  Operands lie
+// rows have landed; K = (w A)^T B while S is weighted into P; O2 = P B.  One warp moves tiles (TMA) and issues the products; the
+// others are between them: a thread owns a row of each accumulator (a step, or a row of the state) and a part of its columns.  Operands lie
 // in panels of 64 columns, 128 bytes a row, swizzled: A is read along its rows for S and down its columns (MN-major) for K.  The state
 // stays in registers in 32 bits; M is its bf16 image.  Rows of a tile are steps in time's order; backwards, the chunks and the masks turn
 // round.
@@ -692,21 +692,69 @@ struct TileSmem {
     // (with three terms there is not), and A's place is free once it is split.
     static constexpr bool kAhead = RB == 128 && TERMS == 2 && !STATE;
     static constexpr int kWide = RB / 64 * kPanel, kX = 0, kA = kX + (STATE ? 0 : (kAhead ? 2 : 1) * kWide), kB = kA + kWide, kM = kB + CB / 64 * kPanel,
-                         kSplit = kM + (STATE ? 0 : CB / 64 * kPanel), kSplitBytes = RB == 128 ? TERMS * 2 * kPanel : (TERMS + 1) / 2 * 2 * kPanel,
+                         kSplit = kM + (STATE ? 0 : CB / 64 * kPanel), kSplitBytes = RB == 128 ? TERMS * 2 * kPanel : TERMS * kPanel,
                          kEnd = kSplit + kSplitBytes;
     static constexpr int kTables = 1664, kBytes = kEnd + kTables + 1024;  // with the alignment
     static constexpr uint32_t kCols = STATE ? CB : 128 + 2 * CB > 256 ? 512 : 256;  // of tensor memory
     static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 struct TileTables {
-    float weight[256];  // a_scale lambda^|p - c| of step c for step p at 127 - p + c, 0 where p does not see c
+    float weight[256];  // a_scale lambda^|p - c| of step c for step p at 127 - p + c
     float pow[132];     // lambda^n
     uint64_t got_a, got_b, bar[3];    // X and A, B have landed; S and O1, K, O2 are made
-    uint64_t split, weighted, emptied;  // of the eight warps: A is split; P is there; accumulators are read, M and outputs in place
+    uint64_t split, weighted, emptied;  // of the workers' warps: A is split; P is there; accumulators are read, M and outputs in place
+    uint32_t flags[2][4];  // done at the steps of a chunk, a bit each
     int abort_flag, bad;
     uint32_t slot;
 };
 static_assert(sizeof(TileTables) <= 1664, "place of the tables");
+
+// w a for eight bf16 numbers a, as sums of bf16 numbers.  With w = w0 + w1 + w2, 8 bits each, hi = a w0 to the nearest and a w0 - hi are
+// bf16 numbers that hold a w0 entirely (16 bits), in two packed operations a pair; four terms are exact to 2^-26, two to 2^-17.
+// Three come from 32 bits, 17 operations a pair: with 128 rows, where the fourth would cost more products and shared memory than
+// it saves (8192 steps of 16 x 128: 97 and 90 us).
+template <int TERMS>
+__device__ __forceinline__ void split_products(const uint32_t (&a)[4], float w, uint32_t (&part)[TERMS][4]) {
+    if constexpr (TERMS == 3) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float f0 = low(a[q]) * w, f1 = high(a[q]) * w;
+#pragma unroll
+            for (int t = 0; t < 3; ++t) {
+                part[t][q] = pack_bf16x2(f0, f1);
+                f0 -= low(part[t][q]);
+                f1 -= high(part[t][q]);
+            }
+        }
+    } else {
+        __nv_bfloat162 ws[3];
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+            ws[t] = __float2bfloat162_rn(w);
+            w -= __low2float(ws[t]);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&a[q]);
+            __nv_bfloat162 p[4];
+            p[0] = __hmul2_rn(x, ws[0]);
+            p[1] = __hfma2(x, ws[0], __hneg2(p[0]));
+            if constexpr (TERMS == 2) {
+                p[1] = __hfma2(x, ws[1], p[1]);
+            } else {
+                p[2] = __hmul2_rn(x, ws[1]);
+                p[3] = __hfma2(x, ws[2], __hfma2(x, ws[1], __hneg2(p[2])));
+            }
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) part[t][q] = *reinterpret_cast<const uint32_t *>(&p[t]);
+        }
+    }
+}
+__device__ __forceinline__ void store_32_bytes(float *p, const float *v) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]),
+                 "f"(v[6]), "f"(v[7])
+                 : "memory");
+}
 
 struct TileMaps {
     CUtensorMap x, a, b, out;
@@ -745,36 +793,45 @@ __device__ __noinline__ void segment_slowly(const Sweep &s, float *m, const floa
         for (int r = 0; r < s.R; ++r) out_state[r * sr + c * sc] = m[r * s.C + c];
 }
 
+// A warp for tiles and products, and workers: eight warps of two blocks on an SM, or sixteen of one (eight where there are no outputs:
+// 128 x 128, eight and sixteen: 36 and 40 us of states, 54 and 48 of outputs).
+__host__ __device__ constexpr int tile_threads(int RB, int CB, bool STATE) { return STATE || (RB == 64 && CB == 64) ? 288 : 544; }
+template <int N>
+__device__ __forceinline__ void tmem_get(uint32_t at, float *v) {
+    if constexpr (N == 16) tc::tmem_ld16(at, v);
+    else tc::tmem_ld32(at, v);
+}
+
 template <int RB, int CB, bool STATE, int TERMS>
-__global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel(const __grid_constant__ Sweep s, const __grid_constant__ TileMaps maps,
+__global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB == 64 ? 2 : 1) tile_kernel(const __grid_constant__ Sweep s, const __grid_constant__ TileMaps maps,
                                                                                 int32_t *status) {
     using L = TileSmem<RB, CB, STATE, TERMS>;
-    constexpr int H = CB / 2;                            // columns of a thread
+    constexpr int WG = (tile_threads(RB, CB, STATE) - 32) / 128, WORKERS = 128 * WG;  // warps 0 ..; column groups
+    constexpr int H = CB / WG, PC = 128 / WG;            // columns of a thread: of the state and the outputs, of S and P
+    constexpr int G = H < 32 ? 16 : WG == 4 ? 16 : 32;   // at a time
     constexpr int kO1 = 128, kK = STATE ? 0 : 128 + CB;  // columns of tensor memory: S and O2 from 0
-    constexpr int SETS = RB == 128 ? TERMS : (TERMS + 1) / 2;
+    constexpr int SETS = RB == 128 ? TERMS : TERMS / 2;
+    static_assert(RB == 128 || TERMS != 3, "two terms side by side");
     extern __shared__ uint8_t raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     TileTables *tab = reinterpret_cast<TileTables *>(smem + L::kEnd);
     const uint32_t base = tc::smem_u32(smem);
     const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index();
     volatile int *abort_flag = &tab->abort_flag;
-    if (w == 8) {  // the warp that uses them first
+    if (w == 4 * WG) {  // the warp that uses them first
         if (lane == 0) {
             tc::mbar_init(&tab->got_a, 1);
             tc::mbar_init(&tab->got_b, 1);
             for (int i = 0; i < 3; ++i) tc::mbar_init(&tab->bar[i], 1);
-            tc::mbar_init(&tab->split, 8);
-            tc::mbar_init(&tab->weighted, 8);
-            tc::mbar_init(&tab->emptied, 8);
+            tc::mbar_init(&tab->split, 4 * WG);
+            tc::mbar_init(&tab->weighted, 4 * WG);
+            tc::mbar_init(&tab->emptied, 4 * WG);
             tab->abort_flag = tab->bad = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
     }
-    if (RB == 64 && TERMS == 3) {  // the half beside the third term
-        for (int i = tid; i < L::kPanel / 16; i += 288) reinterpret_cast<uint4 *>(smem + L::kSplit + 3 * L::kPanel)[i] = make_uint4(0, 0, 0, 0);
-    }
-    if (w == 8) tc::tmem_alloc(&tab->slot, L::kCols);
+    if (w == 4 * WG) tc::tmem_alloc(&tab->slot, L::kCols);
     grid_wait();
     const int eh = blockIdx.x, e = eh / s.heads, h = eh % s.heads, seg = blockIdx.y, rev = s.reverse;
     const int t_lo = seg * s.seg_len, t_hi = min(t_lo + s.seg_len, s.T), chunks = (t_hi - t_lo + 127) / 128;
@@ -791,7 +848,7 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
     const auto start_of = [&](int i) { return t_lo + 128 * (rev ? chunks - 1 - i : i); };  // of the i-th chunk
     bool ok = true;
 
-    if (w == 8) {
+    if (w == 4 * WG) {
         // ---------------- tiles and products
         const auto load = [&](int to, const CUtensorMap *map, int width, int head, int t, uint64_t *bar) {
             for (int p = 0; p < width / 64; ++p) tc::tma_load_4d(base + to + p * L::kPanel, map, bar, 64 * p, head, e, t);
@@ -799,8 +856,25 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
         const auto load_x = [&](int i) { load(L::kX + (L::kAhead ? i % 2 * L::kWide : 0), &maps.x, RB, h / s.share_x, start_of(i), &tab->got_a); };
         const auto load_a = [&](int i) { load(L::kA, &maps.a, RB, h / s.share_a, start_of(i), &tab->got_a); };
         const auto load_b = [&](int i) { load(L::kB, &maps.b, CB, h / s.share_b, start_of(i), &tab->got_b); };
+        // done at the steps of the i-th chunk, for the workers; in front of the arrival that they wait for
+        const auto flags_of = [&](int i) {
+            const int t0 = start_of(i);
+            uint8_t f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int t = t0 + 32 * k + lane;
+                f[k] = s.done && t < t_hi ? s.done[(long long)t * s.Be + e] : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t word = __ballot_sync(0xffffffffu, f[k] != 0);
+                if (lane == 0) tab->flags[i % 2][k] = word;
+            }
+            __syncwarp();
+        };
         const auto expect_a = [&] { tc::mbar_arrive_expect_tx(&tab->got_a, (STATE ? 1 : 2) * L::kWide); };
         const auto expect_b = [&] { tc::mbar_arrive_expect_tx(&tab->got_b, CB / 64 * L::kPanel); };
+        flags_of(0);
         if (tc::elect_one()) {
             expect_a();
             if (!STATE) load_x(0);
@@ -839,14 +913,16 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
                         }
                     }
                     tc::umma_commit(&tab->bar[0]);
-                    if (L::kAhead && more) {
-                        tc::bulk_wait_read<0>();  // the chunk before has left that place
-                        expect_a();
-                        load_x(i + 1);
-                    }
                 }
                 __syncwarp();
             }
+            if (more) flags_of(i + 1);
+            if (L::kAhead && more && tc::elect_one()) {
+                tc::bulk_wait_read<0>();  // the chunk before has left that place
+                expect_a();
+                load_x(i + 1);
+            }
+            __syncwarp();
             wait(&tab->split, i);
             if (update) {
                 wait(&tab->got_b, i);
@@ -947,7 +1023,8 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
                     make_uint4(pack_bf16x2(M[c], M[c + 1]), pack_bf16x2(M[c + 2], M[c + 3]), pack_bf16x2(M[c + 4], M[c + 5]), pack_bf16x2(M[c + 6], M[c + 7]));
             }
         };
-        bool filled = in != nullptr, bad = false;
+        bool filled = in != nullptr;
+        __nv_bfloat162 zeros = __float2bfloat162_rn(0.f);  // of all of B that this thread looks at
         if (!STATE && filled) store_m();
         tc::fence_async_smem();
         tc::tc_fence_before();
@@ -959,24 +1036,15 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar);
         };
-        uint32_t any = 0, flags[4];
-        const auto flags_of = [&](int i, uint32_t (&f)[4]) {  // done at the steps of the i-th chunk
-            const int t0 = start_of(i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int t = t0 + 32 * k + lane;
-                f[k] = s.done && t < t_hi ? s.done[(long long)t * s.Be + e] : 0;
-            }
-        };
-        flags_of(0, flags);
+        uint32_t any = 0;
         for (int i = 0; i < chunks; ++i) {
             const int n = min(128, t_hi - start_of(i));
             const bool more = i + 1 < chunks, update = more || out_state;
             const int x = L::kX + (L::kAhead ? i % 2 * L::kWide : 0);
+            wait(&tab->got_a, i);
             uint32_t resets[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) any |= resets[k] = __ballot_sync(0xffffffffu, flags[k] != 0);
-            if (more) flags_of(i + 1, flags);
+            for (int k = 0; k < 4; ++k) any |= resets[k] = tab->flags[i % 2][k];
             const bool some = (resets[0] | resets[1] | resets[2] | resets[3]) != 0;
             // the flag that the state behind the chunk sees first, looking back
             int edge = rev ? 128 : -1;
@@ -985,30 +1053,18 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
                 if (!rev && resets[k]) edge = 32 * k + 31 - __clz(resets[k]);
                 if (rev && resets[3 - k]) edge = 32 * (3 - k) + __ffs(resets[3 - k]) - 1;
             }
-            wait(&tab->got_a, i);
             if (update) {
                 // w_c a_c in TERMS terms
                 constexpr int V = RB / 8;
 #pragma unroll 4
-                for (int k = 0; k < 128 * V / 256; ++k) {
-                    const int c = (k * 256 + tid) / V, v = (k * 256 + tid) % V;
+                for (int k = 0; k < 128 * V / WORKERS; ++k) {
+                    const int c = (k * WORKERS + tid) / V, v = (k * WORKERS + tid) % V;
                     const bool sees = c < n && (rev ? c <= edge : c > edge);
                     const float wj = sees ? tab->pow[max(rev ? c + 1 : n - 1 - c, 0)] * s.a_scale : 0.f;
                     const uint4 a = *reinterpret_cast<const uint4 *>(piece(L::kA + v / 8 * L::kPanel, c, v));
-                    const uint32_t in4[4] = {a.x, a.y, a.z, a.w};
+                    const uint32_t in4[4] = {sees ? a.x : 0u, sees ? a.y : 0u, sees ? a.z : 0u, sees ? a.w : 0u};
                     uint32_t part[TERMS][4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float f0 = low(in4[q]) * wj, f1 = high(in4[q]) * wj;
-                        f0 = sees ? f0 : 0.f;
-                        f1 = sees ? f1 : 0.f;
-#pragma unroll
-                        for (int t = 0; t < TERMS; ++t) {
-                            part[t][q] = pack_bf16x2(f0, f1);
-                            f0 -= low(part[t][q]);
-                            f1 -= high(part[t][q]);
-                        }
-                    }
+                    split_products<TERMS>(in4, wj, part);
 #pragma unroll
                     for (int t = 0; t < TERMS; ++t)
                         *reinterpret_cast<uint4 *>(piece(L::kSplit + (RB == 128 ? 2 * t + v / 8 : t) * L::kPanel, c, v)) =
@@ -1019,9 +1075,13 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
             tell(&tab->split);
             wait(&tab->got_b, i);
 #pragma unroll
-            for (int k = 0; k < CB / 16; ++k) {
-                const int r = (k * 256 + tid) / (CB / 8), v = (k * 256 + tid) % (CB / 8);
-                bad |= not_finite(*reinterpret_cast<const uint4 *>(piece(L::kB + v / 8 * L::kPanel, r, v)));
+            for (int k = 0; k < 128 * (CB / 8) / WORKERS; ++k) {
+                const int r = (k * WORKERS + tid) / (CB / 8), v = (k * WORKERS + tid) % (CB / 8);
+                const uint4 b = *reinterpret_cast<const uint4 *>(piece(L::kB + v / 8 * L::kPanel, r, v));
+                for (uint32_t word : {b.x, b.y, b.z, b.w}) {  // 0 times an infinity or a NaN is a NaN
+                    const __nv_bfloat162 two = *reinterpret_cast<const __nv_bfloat162 *>(&word);
+                    zeros = __hfma2(two, __float2bfloat162_rn(0.f), zeros);
+                }
             }
             bool reached = true;  // whether this row sees the state in front of the chunk
             if constexpr (!STATE) {
@@ -1040,36 +1100,37 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
                     }
                 }
                 wait(&tab->bar[0], i);
-                if (RB == 64 && wc == 1) wait(&tab->split, i);  // the other warps have read A, whose place the second half takes
+                if (RB == 64 && PC * wc >= 64) wait(&tab->split, i);  // the other warps have read A, whose place the second half takes
                 tc::tc_fence_after();
-                // P: row `row`, columns 64 wc ..
-                const int panel = wc == 0 ? x : RB == 128 ? x + L::kPanel : L::kA;
-                if (rev ? wc == 0 && lq >= 2 : wc == 1 && lq < 2) {
+                // P: row `row`, 32 columns at a time, from PC wc on
 #pragma unroll
-                    for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4 *>(piece(panel, row, v)) = make_uint4(0, 0, 0, 0);
-                } else {
-                    const float *weight = tab->weight + 127 - row + 64 * wc;
+                for (int b0 = 0; b0 < PC; b0 += 32) {
+                    const int col = PC * wc + b0;
+                    const int panel = col < 64 ? x : RB == 128 ? x + L::kPanel : L::kA, v0 = col % 64 / 8;
+                    if (rev ? col < 32 * lq : col > 32 * lq) {  // nothing of it is seen, whatever it holds
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        float f[32];
-                        tc::tmem_ld32(mine + 64 * wc + 32 * half, f);
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            const float wt = weight[32 * half + c], p = f[c] * wt;
-                            f[c] = wt != 0.f ? p : 0.f;  // whatever it is that is not seen
-                        }
-                        if (some) {
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) {
-                                const int j = 64 * wc + 32 * half + c;
-                                if (rev ? j > bound : j < bound) f[c] = 0.f;
-                            }
-                        }
-#pragma unroll
-                        for (int c = 0; c < 32; c += 8)
-                            *reinterpret_cast<uint4 *>(piece(panel, row, 4 * half + c / 8)) =
-                                make_uint4(pack_bf16x2(f[c], f[c + 1]), pack_bf16x2(f[c + 2], f[c + 3]), pack_bf16x2(f[c + 4], f[c + 5]), pack_bf16x2(f[c + 6], f[c + 7]));
+                        for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4 *>(piece(panel, row, v0 + v)) = make_uint4(0, 0, 0, 0);
+                        continue;
                     }
+                    const float *weight = tab->weight + 127 - row + col;
+                    float f[32];
+                    tc::tmem_ld32(mine + col, f);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) f[c] *= weight[c];
+                    if (col == 32 * lq) {  // on the diagonal
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (rev ? c < lane : c > lane) f[c] = 0.f;
+                    }
+                    if (some) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (rev ? col + c > bound : col + c < bound) f[c] = 0.f;
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; c += 8)
+                        *reinterpret_cast<uint4 *>(piece(panel, row, v0 + c / 8)) =
+                            make_uint4(pack_bf16x2(f[c], f[c + 1]), pack_bf16x2(f[c + 2], f[c + 3]), pack_bf16x2(f[c + 4], f[c + 5]), pack_bf16x2(f[c + 6], f[c + 7]));
                 }
                 tc::fence_async_smem();
                 tc::tc_fence_before();
@@ -1080,11 +1141,11 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
                 tc::tc_fence_after();
                 const float keep = tab->pow[n];
 #pragma unroll
-                for (int c0 = 0; c0 < H; c0 += 32) {
-                    float f[32];
-                    tc::tmem_ld32(mine + kK + wc * H + c0, f);
+                for (int c0 = 0; c0 < H; c0 += G) {
+                    float f[G];
+                    tmem_get<G>(mine + kK + wc * H + c0, f);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) M[c0 + c] = some ? f[c] : fmaf(M[c0 + c], keep, f[c]);
+                    for (int c = 0; c < G; ++c) M[c0 + c] = some ? f[c] : fmaf(M[c0 + c], keep, f[c]);
                 }
                 if (!STATE && more) store_m();
             }
@@ -1094,29 +1155,29 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
                 const float f1 = tab->pow[max(rev ? n - 1 - row : row + 1, 0)];
                 const long long at = (long long)(start_of(i) + row) * s.Be + e;
 #pragma unroll
-                for (int c0 = 0; c0 < H; c0 += 32) {
-                    float o[32];
-                    tc::tmem_ld32(mine + wc * H + c0, o);
+                for (int c0 = 0; c0 < H; c0 += G) {
+                    float o[G];
+                    tmem_get<G>(mine + wc * H + c0, o);
                     if (filled) {
-                        float m[32];
-                        tc::tmem_ld32(mine + kO1 + wc * H + c0, m);
+                        float m[G];
+                        tmem_get<G>(mine + kO1 + wc * H + c0, m);
                         if (reached) {
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) o[c] = fmaf(m[c], f1, o[c]);
+                            for (int c = 0; c < G; ++c) o[c] = fmaf(m[c], f1, o[c]);
                         }
                     }
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) o[c] *= s.out_scale;
+                    for (int c = 0; c < G; ++c) o[c] *= s.out_scale;
                     if (s.shared) {
                         float *to = s.shared + (at * s.heads + h) * s.C + wc * H + c0;
                         if (row < n) {
 #pragma unroll
-                            for (int c = 0; c < 32; c += 4)
-                                if (wc * H + c0 + c < s.C) *reinterpret_cast<float4 *>(to + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                            for (int c = 0; c < G; c += 8)
+                                if (wc * H + c0 + c < s.C) store_32_bytes(to + c, o + c);  // whole sectors: a lane's neighbours write other rows
                         }
                     } else {  // through the place of P
 #pragma unroll
-                        for (int c = 0; c < 32; c += 8) {
+                        for (int c = 0; c < G; c += 8) {
                             const int v = (wc * H + c0 + c) / 8;
                             *reinterpret_cast<uint4 *>(piece(v < 8 ? x : RB == 128 ? x + L::kPanel : L::kA, row, v)) =
                                 make_uint4(pack_bf16x2(o[c], o[c + 1]), pack_bf16x2(o[c + 2], o[c + 3]), pack_bf16x2(o[c + 4], o[c + 5]), pack_bf16x2(o[c + 6], o[c + 7]));
@@ -1129,9 +1190,9 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
             tell(&tab->emptied);
             filled = true;
         }
-        if (bad) tab->bad = 1;
+        if (!__hbeq2(zeros, __float2bfloat162_rn(0.f))) tab->bad = 1;
         if (STATE && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any != 0;
-        asm volatile("bar.sync 4, 256;" ::: "memory");
+        asm volatile("bar.sync 4, %0;" ::"n"(WORKERS) : "memory");
         if (out_state && !tab->bad) {
             if (RB == 64) {  // the two shares of a row
                 float *y = reinterpret_cast<float *>(smem + L::kSplit);
@@ -1139,7 +1200,7 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
 #pragma unroll
                     for (int c = 0; c < H; ++c) y[(wc * H + c) * 64 + row - 64] = M[c];
                 }
-                asm volatile("bar.sync 4, 256;" ::: "memory");
+                asm volatile("bar.sync 4, %0;" ::"n"(WORKERS) : "memory");
                 if (row < 64) {
 #pragma unroll
                     for (int c = 0; c < H; ++c) M[c] += y[(wc * H + c) * 64 + row];
@@ -1161,7 +1222,7 @@ __global__ void __launch_bounds__(288, RB == 64 && CB == 64 ? 2 : 1) tile_kernel
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (w == 8) {
+    if (w == 4 * WG) {
         tc::tc_fence_after();
         tc::tmem_dealloc(tab->slot, L::kCols);
     }
@@ -1198,17 +1259,30 @@ __global__ void __launch_bounds__(256) segments_kernel(Sweep s) {
     if (s.m_out) s.m_out[eh * s.state + at] = m;
 }
 
-// Gradient of a shared head: the sum of those of its query heads.
+// Gradient of a shared head: the sum of those of its query heads.  Four columns a thread where C has them.
 template <typename T>
 __global__ void __launch_bounds__(256) shared_sum_kernel(const float *part, T *out, long long ldo, long long rows, int kv_heads, int share, int C) {
     grid_wait();
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / (kv_heads * C);
+    const bool four = C % 4 == 0;
+    const int n = four ? 4 : 1, width = kv_heads * C / n;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / width;
     if (row >= rows) return;
-    const int at = (int)(i % (kv_heads * C)), g = at / C, c = at % C;
+    const int at = (int)(i % width) * n, g = at / C, c = at % C;
     const float *p = part + (row * kv_heads + g) * share * C + c;
-    float v = 0.f;
-    for (int k = 0; k < share; ++k) v += p[k * C];
-    out[row * ldo + at] = from_f32<T>(v);
+    T *to = out + row * ldo + at;
+    if (four) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < share; ++k) {
+            const float4 f = *reinterpret_cast<const float4 *>(p + k * C);
+            v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+        }
+        to[0] = from_f32<T>(v.x), to[1] = from_f32<T>(v.y), to[2] = from_f32<T>(v.z), to[3] = from_f32<T>(v.w);
+    } else {
+        float v = 0.f;
+        for (int k = 0; k < share; ++k) v += p[k * C];
+        to[0] = from_f32<T>(v);
+    }
 }
 
 // One step of one head of one env per block: thread (g, l) holds columns VEC l.. of the rows g, g + groups, ...; the state
@@ -1305,7 +1379,7 @@ int check(const ppo_decay_attention_desc *d) {
 size_t seg_floats(const ppo_decay_attention_desc *d) {
     int len;
     const int n = segments(d, &len);
-    return n > 1 ? (size_t)n * d->Be * d->heads * (d->dk * d->dv + 1) + 3 & ~(size_t)3 : 0;  // with a flag each
+    return n > 1 ? (size_t)n * d->Be * d->heads * (d->dk * d->dv + 1) + 7 & ~(size_t)7 : 0;  // with a flag each; in 32 bytes
 }
 size_t shared_floats(const ppo_decay_attention_desc *d) {
     return d->heads != d->kv_heads ? (size_t)d->T * d->Be * d->heads * (d->dk > d->dv ? d->dk : d->dv) : 0;
@@ -1343,16 +1417,16 @@ int tile_launch_as(const Sweep &s, const TileMaps &maps, cudaStream_t st) {
     int32_t *status = ppo_device_status_ptr();
     if (!status) return PPO_ERR_CUDA;
     PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(tile_kernel<RB, CB, STATE, TERMS>, L::kBytes); }));
-    return ppo_launch(tile_kernel<RB, CB, STATE, TERMS>, dim3(s.Be * s.heads, s.nseg), dim3(288), L::kBytes, st, s, maps, status);
+    return ppo_launch(tile_kernel<RB, CB, STATE, TERMS>, dim3(s.Be * s.heads, s.nseg), dim3(tile_threads(RB, CB, STATE)), L::kBytes, st, s, maps, status);
 }
-template <bool STATE, int TERMS>
+template <bool STATE, int TERMS, int WIDE_TERMS>
 int tile_launch_of(const Sweep &s, const TileMaps &maps, cudaStream_t st) {
     if (s.R <= 64) return s.C <= 64 ? tile_launch_as<64, 64, STATE, TERMS>(s, maps, st) : tile_launch_as<64, 128, STATE, TERMS>(s, maps, st);
-    return s.C <= 64 ? tile_launch_as<128, 64, STATE, TERMS>(s, maps, st) : tile_launch_as<128, 128, STATE, TERMS>(s, maps, st);
+    return s.C <= 64 ? tile_launch_as<128, 64, STATE, WIDE_TERMS>(s, maps, st) : tile_launch_as<128, 128, STATE, WIDE_TERMS>(s, maps, st);
 }
 template <bool STATE>
 int tile_launch(const Sweep &s, const TileMaps &maps, bool exact, cudaStream_t st) {
-    return exact ? tile_launch_of<STATE, 3>(s, maps, st) : tile_launch_of<STATE, 2>(s, maps, st);
+    return exact ? tile_launch_of<STATE, 4, 3>(s, maps, st) : tile_launch_of<STATE, 2, 2>(s, maps, st);
 }
 // Rows of heads as [T][Be][heads][width], boxes of 128 steps and 64 columns of one head.
 int tile_maps(const Sweep &s, TileMaps *m) {
@@ -1439,7 +1513,7 @@ extern "C" int ppo_decay_attention_fwd(const ppo_decay_attention_desc *d, const 
     const size_t need = ppo_decay_attention_workspace_bytes(d, 0);
     if (!q || !k || !v || !decay || !o || (need > 0 && !workspace)) return PPO_ERR_INVALID_ARG;
     if (ws_bytes < need) return PPO_ERR_SHAPE;
-    if (misaligned({q, k, v, o}, elem_bytes(d->dtype)) || misaligned({decay}, 4) || misaligned({state_in, state_out, workspace}, 16)) return PPO_ERR_ALIGN;
+    if (misaligned({q, k, v, o}, elem_bytes(d->dtype)) || misaligned({decay}, 4) || misaligned({state_in, state_out}, 16) || misaligned({workspace}, 32)) return PPO_ERR_ALIGN;
     Sweep s = sweep_of(d, decay, done, static_cast<float *>(workspace));
     plain_state(&s, d);
     s.a = k, s.lda = d->ldk, s.b = v, s.ldb = d->ldv, s.x = q, s.ldx = d->ldq, s.out = o, s.ldo = d->ldo;
@@ -1459,7 +1533,7 @@ extern "C" int ppo_decay_attention_bwd(const ppo_decay_attention_desc *d, const 
     if (!q || !k || !v || !decay || !d_o || !dq || !dk || !dv || (need > 0 && !workspace)) return PPO_ERR_INVALID_ARG;
     if (ws_bytes < need) return PPO_ERR_SHAPE;
     if (misaligned({q, k, v, d_o, dq, dk, dv}, elem_bytes(d->dtype)) || misaligned({decay}, 4) ||
-        misaligned({state_in, dstate_out, dstate_in, workspace}, 16))
+        misaligned({state_in, dstate_out, dstate_in}, 16) || misaligned({workspace}, 32))
         return PPO_ERR_ALIGN;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int share = d->heads / d->kv_heads;
@@ -1499,7 +1573,7 @@ extern "C" int ppo_decay_attention_bwd(const ppo_decay_attention_desc *d, const 
             s.out = out;
             PPO_TRY(sweep<T>(s, st));
             if (part)
-                PPO_TRY(ppo_launch(shared_sum_kernel<T>, dim3(ppo_cdiv(rows * d->kv_heads * s.C, 256)), dim3(256), 0, st, (const float *)part, out, s.ldo,
+                PPO_TRY(ppo_launch(shared_sum_kernel<T>, dim3(ppo_cdiv(rows * d->kv_heads * s.C / (s.C % 4 == 0 ? 4 : 1), 256)), dim3(256), 0, st, (const float *)part, out, s.ldo,
                                    rows, d->kv_heads, share, s.C));
         }
         return PPO_OK;

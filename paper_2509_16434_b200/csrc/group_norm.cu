@@ -691,7 +691,7 @@ extern "C" int ppo_group_norm_fwd(const ppo_group_norm_desc *d, float eps, const
     if (ws_bytes < need) return PPO_ERR_SHAPE;
     for (const void *p : {(const void *)gamma, (const void *)beta, (const void *)mean, (const void *)rstd})
         if (!ppo_aligned(p, 4)) return PPO_ERR_ALIGN;
-    if (!ppo_aligned(x, e) || !ppo_aligned(y, e) || !ppo_aligned(workspace, 16)) return PPO_ERR_ALIGN;
+    if (!ppo_aligned(x, e) || !ppo_aligned(y, e) || !ppo_aligned(workspace, 32)) return PPO_ERR_ALIGN;
     NormArgs a = args(d);
     a.x = x;
     a.y = y;
@@ -733,7 +733,7 @@ extern "C" int ppo_group_norm_bwd(const ppo_group_norm_desc *d, const void *x, c
     if (ws_bytes < need) return PPO_ERR_SHAPE;
     for (const void *p : {(const void *)gamma, (const void *)beta, (const void *)mean, (const void *)rstd, (const void *)dgamma, (const void *)dbeta})
         if (!ppo_aligned(p, 4)) return PPO_ERR_ALIGN;
-    if (!ppo_aligned(x, e) || !ppo_aligned(dy, e) || !ppo_aligned(dx, e) || !ppo_aligned(workspace, 16)) return PPO_ERR_ALIGN;
+    if (!ppo_aligned(x, e) || !ppo_aligned(dy, e) || !ppo_aligned(dx, e) || !ppo_aligned(workspace, 32)) return PPO_ERR_ALIGN;
     NormArgs a = args(d);
     a.x = x;
     a.dy = dy;

@@ -390,7 +390,7 @@ extern "C" int ppo_token_loss_fwd_bwd(const ppo_token_desc *d, const ppo_token_l
     if (ld_grad < d->vocab || (dlogits == logits && ld_grad != d->ld)) return PPO_ERR_SHAPE;
     if (ws_bytes < ppo_token_loss_workspace_bytes(d)) return PPO_ERR_SHAPE;
     const size_t e = elem_bytes(d->dtype);
-    if (!ppo_aligned(logits, e) || !ppo_aligned(dlogits, e) || !ppo_aligned(workspace, 16)) return PPO_ERR_ALIGN;
+    if (!ppo_aligned(logits, e) || !ppo_aligned(dlogits, e) || !ppo_aligned(workspace, 32)) return PPO_ERR_ALIGN;
     for (const void *p : {(const void *)tokens, (const void *)logp_old, (const void *)logp_ref, (const void *)adv, (const void *)weight,
                           (const void *)logp_out, (const void *)loss_out})
         if (!ppo_aligned(p, 4)) return PPO_ERR_ALIGN;
