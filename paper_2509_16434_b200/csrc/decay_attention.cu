@@ -35,117 +35,172 @@ struct Sweep {
     int *seg_reset;      // [nseg][Be * heads]: whether a done flag is set in it
 };
 
-constexpr int kTokens = 16, kCols = 32, kSlices = 4;
+// decay ** n
+__device__ __forceinline__ float power(float log2_decay, int n) { return n == 0 ? 1.f : exp2f((float)n * log2_decay); }
 
-// One block: 32 columns of one head's state (a column per lane, R / 4 rows per warp) over one segment.
+// ---- step by step (32 bits, and rows that no vector fits) ----
+//
+// One block: 64 columns of one head's state over one segment, in registers: two columns a lane, R / 8 rows a warp.  Steps come in tiles of
+// 8; a thread fetches its share of the next tile while it works on this one.  Bound by issue: two multiply-adds for each element and
+// step, and a broadcast load of shared memory for eight of them.  For that the decay is not applied step by step: within a tile the
+// state is kept as N = M lambda^-e behind e steps, so that N += a b lambda^-e, and out = lambda^e x^T N; with lambda >= 1/2 that is a
+// factor of at most 2^8.  Smaller decays are applied step by step, in three operations.
+constexpr int kTokens = 8, kCols = 64, kSlices = 8;
+
 // STATE: only what the segment leaves behind, from an empty state.
 template <typename T, int KS, bool STATE>
-__global__ void __launch_bounds__(128) sweep_kernel(Sweep s) {
+__global__ void __launch_bounds__(256) sweep_kernel(Sweep s) {
     grid_wait();
     constexpr int RP = KS * kSlices;
-    __shared__ __align__(16) float ta[kTokens][RP], tx[kTokens][RP], tb[kTokens][kCols], part[kSlices][kTokens][kCols];
-    __shared__ uint8_t gate[kTokens];
-    const int lane = threadIdx.x % 32, w = threadIdx.x / 32;
-    const int ncol = (s.C + kCols - 1) / kCols, c0 = blockIdx.x % ncol * kCols, c = c0 + lane;
+    __shared__ __align__(16) float ta[kTokens][RP], tx[STATE ? 1 : kTokens][RP], tb[kTokens][kCols], part[STATE ? 1 : kSlices][kTokens][kCols];
+    __shared__ float up[kTokens], down[kTokens + 1];
+    __shared__ int gate[kTokens];
+    const int tid = threadIdx.x, lane = tid % 32, w = tid / 32;
+    const int ncol = (s.C + kCols - 1) / kCols, c0 = blockIdx.x % ncol * kCols;
     const int eh = blockIdx.x / ncol, e = eh / s.heads, h = eh % s.heads;
-    const int seg = blockIdx.y;
+    const int seg = blockIdx.y, rev = s.reverse;
     const float lam = s.decay[h];
+    const bool scaled = lam >= 0.5f;
     const T *A = static_cast<const T *>(s.a) + (long long)(h / s.share_a) * s.R;
-    const T *B = static_cast<const T *>(s.b) + (long long)(h / s.share_b) * s.C;
+    const T *B = static_cast<const T *>(s.b) + (long long)(h / s.share_b) * s.C + c0;
     const T *X = static_cast<const T *>(s.x) + (long long)(h / s.share_x) * s.R;
-    float M[KS];
-    // this thread's element of row r of the state lies at r * sr + sc
-    const long long sr = s.nseg > 1 ? s.seg_r : s.stride_r, sc = c * (s.nseg > 1 ? s.seg_c : s.stride_c);
-    const float *in = s.nseg > 1 ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.m_in ? s.m_in + eh * s.state : nullptr;
-#pragma unroll
-    for (int i = 0; i < KS; ++i) {
-        const int r = w * KS + i;
-        M[i] = !STATE && in && r < s.R && c < s.C ? in[r * sr + sc] : 0.f;
+    if (tid <= kTokens) {
+        const float l2 = log2f(lam);
+        const int n = tid + 1 - rev;  // decays up to step tid
+        if (tid < kTokens) up[tid] = scaled ? exp2f(-n * l2) : 1.f;
+        // what outputs are multiplied with; the last: what the state is behind a whole tile
+        down[tid] = !scaled ? 1.f : power(l2, tid < kTokens ? n : kTokens);
     }
+    float M[2][KS];
+    // this thread's element of row r of the state lies at r * sr + c * sc
+    const long long sr = s.nseg > 1 ? s.seg_r : s.stride_r, sc = s.nseg > 1 ? s.seg_c : s.stride_c;
+    const float *in = s.nseg > 1 ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.m_in ? s.m_in + eh * s.state : nullptr;
+    float *out = STATE ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.nseg > 1 || !s.m_out ? nullptr : s.m_out + eh * s.state;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            const int r = w * KS + i, c = c0 + 32 * k + lane;
+            M[k][i] = !STATE && in && r < s.R && c < s.C ? in[r * sr + c * sc] : 0.f;
+        }
     const int t_lo = seg * s.seg_len, t_hi = min(t_lo + s.seg_len, s.T);
-    const int n0 = s.reverse ? s.T - t_hi : t_lo, n1 = s.reverse ? s.T - t_lo : t_hi;  // in the sweep's order
+    const int n0 = rev ? s.T - t_hi : t_lo, n1 = rev ? s.T - t_lo : t_hi;  // in the sweep's order
     int any = 0;
+    // thread (j, l) fetches elements l, l + 32, ... of step j
+    constexpr int RL = RP / 32, CL = kCols / 32;
+    static_assert(kTokens == 8 && RP % 32 == 0, "a warp per step");
+    const int j = w, l = lane;
+    T fa[RL], fx[RL], fb[CL];
+    int fg = 0;
+    const auto fetch = [&](int n) {
+        const bool on = n + j < n1;
+        const long long row = on ? (long long)(rev ? s.T - 1 - (n + j) : n + j) * s.Be + e : 0;
+#pragma unroll
+        for (int i = 0; i < RL; ++i) {
+            const int r = l + 32 * i;
+            const bool ok = on && r < s.R;
+            fa[i] = ok ? A[row * s.lda + r] : from_f32<T>(0.f);
+            if (!STATE) fx[i] = ok ? X[row * s.ldx + r] : from_f32<T>(0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < CL; ++i) fb[i] = on && c0 + l + 32 * i < s.C ? B[row * s.ldb + l + 32 * i] : from_f32<T>(0.f);
+        if (l == 0) fg = on && s.done && s.done[row] != 0;
+    };
+    fetch(n0);
     for (int n = n0; n < n1; n += kTokens) {
         const int cnt = min(kTokens, n1 - n);
-        __syncthreads();
-        for (int i = threadIdx.x; i < kTokens * RP; i += 128) {
-            const int j = i / RP, r = i % RP;
-            const int t = s.reverse ? s.T - 1 - (n + j) : n + j;
-            const bool ok = j < cnt && r < s.R;
-            const long long row = (long long)t * s.Be + e;
-            ta[j][r] = ok ? to_f32(A[row * s.lda + r]) * s.a_scale : 0.f;
-            if (!STATE) tx[j][r] = ok ? to_f32(X[row * s.ldx + r]) : 0.f;
-        }
-        for (int i = threadIdx.x; i < kTokens * kCols; i += 128) {
-            const int j = i / kCols, k = i % kCols;
-            const int t = s.reverse ? s.T - 1 - (n + j) : n + j;
-            tb[j][k] = j < cnt && c0 + k < s.C ? to_f32(B[((long long)t * s.Be + e) * s.ldb + c0 + k]) : 0.f;
-        }
-        if (threadIdx.x < cnt) {
-            const int t = s.reverse ? s.T - 1 - (n + threadIdx.x) : n + threadIdx.x;
-            gate[threadIdx.x] = s.done && s.done[(long long)t * s.Be + e];
-        }
-        __syncthreads();
-        for (int j = 0; j < cnt; ++j) {
-            const float b = tb[j][lane];
-            const bool empty = gate[j];
-            any |= empty;
-            float acc = 0.f;
-            if (s.reverse && empty) {
+        __syncthreads();  // the tile before is worked off
 #pragma unroll
-                for (int i = 0; i < KS; ++i) M[i] = 0.f;
-            }
-            const float before = s.reverse ? 1.f : lam, after = s.reverse ? lam : 1.f;
+        for (int i = 0; i < RL; ++i)
+        {
+            ta[j][l + 32 * i] = to_f32(fa[i]) * s.a_scale;
+            if (!STATE) tx[j][l + 32 * i] = to_f32(fx[i]);
+        }
 #pragma unroll
-            for (int i = 0; i < KS; i += 4) {
-                const float4 a = *reinterpret_cast<const float4 *>(&ta[j][w * KS + i]);
-                M[i] = fmaf(before, M[i], a.x * b);
-                M[i + 1] = fmaf(before, M[i + 1], a.y * b);
-                M[i + 2] = fmaf(before, M[i + 2], a.z * b);
-                M[i + 3] = fmaf(before, M[i + 3], a.w * b);
+        for (int i = 0; i < CL; ++i) tb[j][l + 32 * i] = to_f32(fb[i]) * up[j];
+        if (l == 0) gate[j] = fg;
+        __syncthreads();
+        if (n + kTokens < n1) fetch(n + kTokens);
+        const auto steps = [&](auto plain) {
+            constexpr bool PLAIN = decltype(plain)::value;
+            for (int t = 0; t < cnt; ++t) {
+                const float b0 = tb[t][lane], b1 = tb[t][32 + lane];
+                const int empty = gate[t];
+                any |= empty;
+                if (rev && empty) {
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) M[0][i] = M[1][i] = 0.f;
+                }
+                float o0[2] = {}, o1[2] = {};
+                const float before = rev ? 1.f : lam;
+#pragma unroll
+                for (int i = 0; i < KS; i += 4) {
+                    const float4 a4 = *reinterpret_cast<const float4 *>(&ta[t][w * KS + i]);
+                    const float a[4] = {a4.x, a4.y, a4.z, a4.w};
+                    float x[4] = {};
+                    if constexpr (!STATE) {
+                        const float4 x4 = *reinterpret_cast<const float4 *>(&tx[t][w * KS + i]);
+                        x[0] = x4.x, x[1] = x4.y, x[2] = x4.z, x[3] = x4.w;
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float &m0 = M[0][i + q], &m1 = M[1][i + q];
+                        m0 = PLAIN ? fmaf(before, m0, a[q] * b0) : fmaf(a[q], b0, m0);
+                        m1 = PLAIN ? fmaf(before, m1, a[q] * b1) : fmaf(a[q], b1, m1);
+                        if constexpr (!STATE) {
+                            o0[q % 2] = fmaf(x[q], m0, o0[q % 2]);
+                            o1[q % 2] = fmaf(x[q], m1, o1[q % 2]);
+                        }
+                    }
+                }
+                if (rev ? PLAIN : empty) {
+                    const float after = rev ? lam : 0.f;
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        M[0][i] = rev ? M[0][i] * after : 0.f;
+                        M[1][i] = rev ? M[1][i] * after : 0.f;
+                    }
+                }
                 if constexpr (!STATE) {
-                    const float4 x = *reinterpret_cast<const float4 *>(&tx[j][w * KS + i]);
-                    acc = fmaf(x.x, M[i], acc);
-                    acc = fmaf(x.y, M[i + 1], acc);
-                    acc = fmaf(x.z, M[i + 2], acc);
-                    acc = fmaf(x.w, M[i + 3], acc);
+                    part[w][t][lane] = o0[0] + o0[1];
+                    part[w][t][32 + lane] = o1[0] + o1[1];
                 }
             }
-            if (s.reverse) {
+        };
+        if (scaled) {
+            steps(std::false_type{});
+            const float f = cnt == kTokens ? down[kTokens] : power(log2f(lam), cnt);
 #pragma unroll
-                for (int i = 0; i < KS; ++i) M[i] *= after;
-            } else if (empty) {
-#pragma unroll
-                for (int i = 0; i < KS; ++i) M[i] = 0.f;
-            }
-            if constexpr (!STATE) part[w][j][lane] = acc;
+            for (int i = 0; i < KS; ++i) M[0][i] *= f, M[1][i] *= f;
+        } else {
+            steps(std::true_type{});
         }
         if constexpr (!STATE) {
             __syncthreads();
-            for (int i = threadIdx.x; i < cnt * kCols; i += 128) {
-                const int j = i / kCols, k = i % kCols;
-                if (c0 + k >= s.C) continue;
-                const int t = s.reverse ? s.T - 1 - (n + j) : n + j;
-                const long long row = (long long)t * s.Be + e;
-                const float v = s.out_scale * ((part[0][j][k] + part[1][j][k]) + (part[2][j][k] + part[3][j][k]));
-                if (s.shared) s.shared[(row * s.heads + h) * s.C + c0 + k] = v;
-                else static_cast<T *>(s.out)[row * s.ldo + (long long)h * s.C + c0 + k] = from_f32<T>(v);
+            for (int i = tid; i < cnt * kCols; i += 256) {
+                const int t = i / kCols, c = i % kCols;
+                if (c0 + c >= s.C) continue;
+                float v = 0.f;
+#pragma unroll
+                for (int k = 0; k < kSlices; ++k) v += part[k][t][c];
+                v *= s.out_scale * down[t];
+                const long long row = (long long)(rev ? s.T - 1 - (n + t) : n + t) * s.Be + e;
+                if (s.shared) s.shared[(row * s.heads + h) * s.C + c0 + c] = v;
+                else static_cast<T *>(s.out)[row * s.ldo + (long long)h * s.C + c0 + c] = from_f32<T>(v);
             }
         }
     }
-    float *out = STATE ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.nseg > 1 || !s.m_out ? nullptr : s.m_out + eh * s.state;
-    if (out && c < s.C) {
+    if (out) {
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            const int r = w * KS + i;
-            if (r < s.R) out[r * sr + sc] = M[i];
-        }
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const int r = w * KS + i, c = c0 + 32 * k + lane;
+                if (r < s.R && c < s.C) out[r * sr + c * sc] = M[k][i];
+            }
     }
-    if (STATE && c0 == 0 && threadIdx.x == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any;
+    if (STATE && c0 == 0 && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any;
 }
-
-// decay ** n
-__device__ __forceinline__ float power(float log2_decay, int n) { return n == 0 ? 1.f : exp2f((float)n * log2_decay); }
 
 // ---- chunks of 64 steps on the tensor cores (bf16) ----
 //
@@ -1385,12 +1440,12 @@ size_t shared_floats(const ppo_decay_attention_desc *d) {
     return d->heads != d->kv_heads ? (size_t)d->T * d->Be * d->heads * (d->dk > d->dv ? d->dk : d->dv) : 0;
 }
 
-template <typename T, bool STATE>
+template <typename T, bool STATE, int KS = 4>
 int sweep_launch(const Sweep &s, cudaStream_t st) {
-    const dim3 grid(ppo_cdiv(s.C, kCols) * s.Be * s.heads, s.nseg);
-    if (s.R <= 32) return ppo_launch(sweep_kernel<T, 8, STATE>, grid, dim3(128), 0, st, s);
-    if (s.R <= 64) return ppo_launch(sweep_kernel<T, 16, STATE>, grid, dim3(128), 0, st, s);
-    return ppo_launch(sweep_kernel<T, 32, STATE>, grid, dim3(128), 0, st, s);
+    if constexpr (KS < 16) {
+        if (s.R > KS * kSlices) return sweep_launch<T, STATE, KS + 4>(s, st);
+    }
+    return ppo_launch(sweep_kernel<T, KS, STATE>, dim3(ppo_cdiv(s.C, kCols) * s.Be * s.heads, s.nseg), dim3(256), 0, st, s);
 }
 template <int RB, bool STATE, int TERMS>
 int chunk_launch_as(const Sweep &s, cudaStream_t st) {
