@@ -45,16 +45,27 @@ __device__ __forceinline__ float power(float log2_decay, int n) { return n == 0 
 // step, and a broadcast load of shared memory for eight of them.  For that the decay is not applied step by step: within a tile the
 // state is kept as N = M lambda^-e behind e steps, so that N += a b lambda^-e, and out = lambda^e x^T N; with lambda >= 1/2 that is a
 // factor of at most 2^8.  Smaller decays are applied step by step, in three operations.
+// Sweeps of one call that do not wait for one another, along z of one launch.
+struct Sweeps {
+    Sweep s[3];
+};
+
 constexpr int kTokens = 8, kCols = 64, kSlices = 8;
 
 // STATE: only what the segment leaves behind, from an empty state.
+struct StepTiles {
+    float a[kTokens * 128], x[kTokens * 128], b[kTokens][kCols], part[kSlices][kTokens][kCols], up[kTokens], down[kTokens + 1];
+    int gate[kTokens];
+};
 template <typename T, int KS, bool STATE>
-__global__ void __launch_bounds__(256) sweep_kernel(Sweep s) {
-    grid_wait();
+__device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
     constexpr int RP = KS * kSlices;
-    __shared__ __align__(16) float ta[kTokens][RP], tx[STATE ? 1 : kTokens][RP], tb[kTokens][kCols], part[STATE ? 1 : kSlices][kTokens][kCols];
-    __shared__ float up[kTokens], down[kTokens + 1];
-    __shared__ int gate[kTokens];
+    auto *const ta = reinterpret_cast<float (*)[RP]>(tile.a), *const tx = reinterpret_cast<float (*)[RP]>(tile.x);
+    auto &tb = tile.b;
+    auto &part = tile.part;
+    auto &up = tile.up;
+    auto &down = tile.down;
+    auto &gate = tile.gate;
     const int tid = threadIdx.x, lane = tid % 32, w = tid / 32;
     const int ncol = (s.C + kCols - 1) / kCols, c0 = blockIdx.x % ncol * kCols;
     const int eh = blockIdx.x / ncol, e = eh / s.heads, h = eh % s.heads;
@@ -201,6 +212,17 @@ __global__ void __launch_bounds__(256) sweep_kernel(Sweep s) {
     }
     if (STATE && c0 == 0 && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any;
 }
+template <typename T, bool STATE>
+__global__ void __launch_bounds__(256) sweep_kernel(const __grid_constant__ Sweeps all) {
+    grid_wait();
+    __shared__ __align__(16) StepTiles tile;
+    const Sweep &s = all.s[blockIdx.z];
+    if (blockIdx.x >= (s.C + kCols - 1) / kCols * s.Be * s.heads) return;
+    if (s.R <= 32) sweep_rows<T, 4, STATE>(s, tile);
+    else if (s.R <= 64) sweep_rows<T, 8, STATE>(s, tile);
+    else if (s.R <= 96) sweep_rows<T, 12, STATE>(s, tile);
+    else sweep_rows<T, 16, STATE>(s, tile);
+}
 
 // ---- chunks of 64 steps on the tensor cores (bf16) ----
 //
@@ -239,69 +261,70 @@ __device__ __forceinline__ bool not_finite(uint4 v) {  // one of eight bf16 numb
     return bad;
 }
 
-// Shared memory: per stage the tiles of X and A [64][RB + 8] and B [64][72] (rows padded by 16 bytes: ldmatrix without bank
-// conflicts), then M [RB][72], all bf16, then the powers of the decay.
+// Shared memory: the tiles of X and A [64][RB + 8] and B [64][72] (rows padded by 16 bytes: ldmatrix without bank conflicts), M [RB][72],
+// all bf16, then the powers of the decay.
 template <int RB>
 struct ChunkSmem {
     static constexpr int kRow = RB + 8, kCol = kBlockCols + 8;
-    static constexpr int kWide = kChunk * kRow * 2, kNarrow = kChunk * kCol * 2, kStage = 2 * kWide + kNarrow, kState = RB * kCol * 2;
-    static constexpr int bytes(int stages) { return stages * kStage + kState + 80 * 4; }
+    static constexpr int kWide = kChunk * kRow * 2, kNarrow = kChunk * kCol * 2, kState = RB * kCol * 2;
+    static constexpr int kBytes = 2 * kWide + kNarrow + kState + 80 * 4;
 };
 
-// RB: rows of the state, padded (64 or 128).  STATE: only what the segment leaves, from an empty state.  TERMS: of the weighted a.
+// Sequences of 17 to 64 steps: one chunk.  RB: rows of the state, padded (64 or 128).
 //
 // Eight warps.  Outputs: warp (wr, wc) has 16 rows of the chunk and 32 columns; the two warps of the same rows both make their
 // weights (a sixth more products than one alone, against an exchange).  State: warp w has 16 rows and all columns where there are
 // 128 rows, else 16 rows and half of the columns.  Two blocks of 256 threads and 128 registers on an SM; with four warps and the
 // whole state in theirs (240 registers) it is two of 128 threads, and an SM issues 1.3 to 1.7 instructions per cycle.
-template <int RB, bool STATE, int TERMS>
-__global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
+template <int RB>
+__global__ void __launch_bounds__(256, 2) chunk_kernel(const __grid_constant__ Sweeps all) {
     grid_wait();
+    const Sweep &s = all.s[blockIdx.z];
     using L = ChunkSmem<RB>;
+    constexpr int TERMS = 3;
     constexpr int KR = RB / 16, MN = RB == 128 ? 8 : 4;  // 16-row steps of a product over R; column tiles of a warp's state
     extern __shared__ __align__(16) uint8_t smem[];
     const uint32_t base = tc::smem_u32(smem);
-    uint8_t *ms = smem + stages * L::kStage;
-    const uint32_t ms_at = base + stages * L::kStage;
+    const uint32_t xs = base, as = xs + L::kWide, bs = as + L::kWide, ms_at = bs + L::kNarrow;
+    uint8_t *ms = smem + 2 * L::kWide + L::kNarrow;
     float *pow = reinterpret_cast<float *>(ms + L::kState);
     const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index(), g = lane / 4, t4 = lane % 4;
     const int wr = w % 4, wc = w / 4, mr = RB == 128 ? 16 * w : 16 * wr, mc = RB == 128 ? 0 : 32 * wc;
     const int ncol = (s.C + kBlockCols - 1) / kBlockCols, c0 = blockIdx.x % ncol * kBlockCols, cols = min(kBlockCols, s.C - c0);
-    const int eh = blockIdx.x / ncol, e = eh / s.heads, h = eh % s.heads, seg = blockIdx.y;
+    const int eh = blockIdx.x / ncol, e = eh / s.heads, h = eh % s.heads, steps = s.T;
+    if (e >= s.Be) return;  // another sweep of the launch has more columns
     const bf16 *A = static_cast<const bf16 *>(s.a) + (long long)(h / s.share_a) * s.R;
     const bf16 *B = static_cast<const bf16 *>(s.b) + (long long)(h / s.share_b) * s.C + c0;
     const bf16 *X = static_cast<const bf16 *>(s.x) + (long long)(h / s.share_x) * s.R;
     const int rev = s.reverse;
     if (tid < 66) pow[tid] = power(log2f(s.decay[h]), tid);
 
-    const int n0 = seg * s.seg_len, n1 = min(n0 + s.seg_len, s.T);
-    // Rows first .. first + count of the sweep into rows 0 .. of a stage, zeros behind them and behind R and C.
-    auto copy = [&](int stage, int first, int count) {
-        const uint32_t to = base + stage * L::kStage;
+    // Rows first .. first + count of the sweep into rows 0 .., zeros behind them and behind R and C.
+    auto copy = [&](int first, int count) {
         constexpr int WV = RB / 8, NV = kBlockCols / 8;
 #pragma unroll
         for (int k = 0; k < kChunk * WV / 256; ++k) {
             const int i = k * 256 + tid, j = i / WV, v = i % WV, t = rev ? s.T - 1 - (first + j) : first + j;
             const bool ok = j < count && v * 8 < s.R;
             const long long row = ok ? (long long)t * s.Be + e : 0;
-            if (!STATE) tc::cp_async16(to + (j * L::kRow + v * 8) * 2, ok ? X + row * s.ldx + v * 8 : X, ok);
-            tc::cp_async16(to + L::kWide + (j * L::kRow + v * 8) * 2, ok ? A + row * s.lda + v * 8 : A, ok);
+            tc::cp_async16(xs + (j * L::kRow + v * 8) * 2, ok ? X + row * s.ldx + v * 8 : X, ok);
+            tc::cp_async16(as + (j * L::kRow + v * 8) * 2, ok ? A + row * s.lda + v * 8 : A, ok);
         }
 #pragma unroll
         for (int k = 0; k < kChunk * NV / 256; ++k) {
             const int i = k * 256 + tid, j = i / NV, v = i % NV, t = rev ? s.T - 1 - (first + j) : first + j;
             const bool ok = j < count && v * 8 < cols;
             const long long row = ok ? (long long)t * s.Be + e : 0;
-            tc::cp_async16(to + 2 * L::kWide + (j * L::kCol + v * 8) * 2, ok ? B + row * s.ldb + v * 8 : B, ok);
+            tc::cp_async16(bs + (j * L::kCol + v * 8) * 2, ok ? B + row * s.ldb + v * 8 : B, ok);
         }
         tc::cp_async_commit();
     };
-    copy(0, n0, min(kChunk, n1 - n0));
+    copy(0, steps);
 
     // the state: rows mr + g (+ 8), columns mc + 8 n + 2 t4 (+ 1)
-    const long long sr = s.nseg > 1 ? s.seg_r : s.stride_r, sc = s.nseg > 1 ? s.seg_c : s.stride_c;
-    const float *in = STATE ? nullptr : s.nseg > 1 ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.m_in ? s.m_in + eh * s.state : nullptr;
-    float *out_state = STATE ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.nseg > 1 || !s.m_out ? nullptr : s.m_out + eh * s.state;
+    const long long sr = s.stride_r, sc = s.stride_c;
+    const float *in = s.m_in ? s.m_in + eh * s.state : nullptr;
+    float *out_state = s.m_out ? s.m_out + eh * s.state : nullptr;
     float M[MN][4];
     auto at_state = [&](auto &&fn) {  // every place of the state that this thread holds, columns in pairs
 #pragma unroll
@@ -326,18 +349,18 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
 
     // Whether what this thread has copied of B holds an infinity or a NaN.  (In X one reaches its own step's output, in A those it is
     // meant to; the weights that are masked, or zero, are set to zero whatever they come from.)
-    auto odd = [&](int stage) {
+    auto odd = [&] {
         constexpr int NV = kBlockCols / 8;
         bool bad = false;
 #pragma unroll
         for (int k = 0; k < kChunk * NV / 256; ++k) {
             const int i = k * 256 + tid;
-            bad |= not_finite(*reinterpret_cast<const uint4 *>(smem + stage * L::kStage + 2 * L::kWide + (i / NV * L::kCol + i % NV * 8) * 2));
+            bad |= not_finite(*reinterpret_cast<const uint4 *>(smem + 2 * L::kWide + (i / NV * L::kCol + i % NV * 8) * 2));
         }
         return bad;
     };
-    auto reset_at = [&](int step) { return s.done && step < n1 && s.done[(long long)(rev ? s.T - 1 - step : step) * s.Be + e] != 0; };
-    auto store_ms = [&] {  // M as the operand of the next chunk
+    auto reset_at = [&](int step) { return s.done && step < steps && s.done[(long long)(rev ? s.T - 1 - step : step) * s.Be + e] != 0; };
+    auto store_ms = [&] {  // M as an operand
 #pragma unroll
         for (int n = 0; n < MN; ++n)
 #pragma unroll
@@ -345,11 +368,10 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
                 *reinterpret_cast<uint32_t *>(ms + ((mr + g + 8 * i) * L::kCol + mc + 8 * n + 2 * t4) * 2) = pack_bf16x2(M[n][2 * i], M[n][2 * i + 1]);
     };
 
-    // The n steps from `first` on, in rows 0 .. of a stage; resets: bit i set where done is at step first + i.
-    auto process = [&](int stage, int first, int n, unsigned long long resets, bool last) {
-        const uint32_t xs = base + stage * L::kStage, as = xs + L::kWide, bs = xs + 2 * L::kWide;
+    // The n steps from `first` on, in rows 0 ..; resets: bit i set where done is at step first + i.
+    auto process = [&](int first, int n, unsigned long long resets, bool last) {
         const auto before = [&](int i) { return __popcll(resets & (((1ull << i) << rev) - 1)); };  // resets in front of i
-        if (!STATE && 16 * wr < n) {
+        if (16 * wr < n) {
             float o[4][4] = {};
             uint32_t xf[KR][4];
 #pragma unroll
@@ -426,7 +448,7 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
                 }
             } else {
                 // through the rows of X that only this warp and its neighbour read, to 64-byte rows of 16-byte stores
-                uint8_t *mine = smem + stage * L::kStage + (16 * wr * L::kRow + wc * 32) * 2;
+                uint8_t *mine = smem + (16 * wr * L::kRow + wc * 32) * 2;
                 asm volatile("bar.sync %0, 64;" ::"r"(1 + wr) : "memory");  // both have read them
 #pragma unroll
                 for (int nn = 0; nn < 4; ++nn) {
@@ -494,38 +516,22 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
         }
     };
 
-    bool flag0 = reset_at(n0 + lane), flag1 = reset_at(n0 + 32 + lane);
-    unsigned long long any = 0;
-    int stage = 0;
-    for (int n = n0; n < n1; n += kChunk) {
-        const int count = min(kChunk, n1 - n);
-        const bool more = n + kChunk < n1;
-        const unsigned long long resets =
-            (unsigned long long)__ballot_sync(0xffffffffu, flag0) | (unsigned long long)__ballot_sync(0xffffffffu, flag1) << 32;
-        any |= resets;
-        tc::cp_async_wait<0>();
-        if (!STATE && filled) store_ms();
-        const bool bad = __syncthreads_or(odd(stage));
-        if (more) {
-            copy(stage ^ 1, n + kChunk, min(kChunk, n1 - n - kChunk));
-            flag0 = reset_at(n + kChunk + lane);
-            flag1 = reset_at(n + kChunk + 32 + lane);
+    const unsigned long long resets = (unsigned long long)__ballot_sync(0xffffffffu, reset_at(lane)) |
+                                      (unsigned long long)__ballot_sync(0xffffffffu, reset_at(32 + lane)) << 32;
+    if (filled) store_ms();
+    tc::cp_async_wait<0>();
+    const bool bad = __syncthreads_or(odd());
+    for (int i = 0; i < (bad ? steps : 1); ++i) {
+        if (bad) {
+            __syncthreads();
+            copy(i, 1);
+            tc::cp_async_wait<0>();
+            if (filled) store_ms();
+            __syncthreads();
         }
-        for (int i = 0; i < (bad ? count : 1); ++i) {
-            if (bad) {
-                __syncthreads();
-                copy(stage, n + i, 1);
-                tc::cp_async_wait<0>();  // the next chunk's with it
-                if (!STATE && filled) store_ms();
-                __syncthreads();
-            }
-            process(stage, n + i, bad ? 1 : count, bad ? resets >> i & 1 : resets, !more && (!bad || i == count - 1));
-            filled = true;
-        }
-        __syncthreads();
-        stage ^= 1;
+        process(i, bad ? 1 : steps, bad ? resets >> i & 1 : resets, !bad || i == steps - 1);
+        filled = true;
     }
-    if (STATE && c0 == 0 && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any != 0;
     if (!out_state) return;
     at_state([&](float &m0, float &m1, bool ok0, bool ok1, long long at) {
         if (pairs) {
@@ -539,15 +545,18 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(Sweep s, int stages) {
 
 // Sequences of up to 16 steps: one chunk, four warps, and little else than the state to move, so as many blocks on an SM as keep its
 // loads in flight.  Every warp makes the 16 x 16 weights and has 16 columns of the outputs; of the state it has RB / 4 rows.
-template <int RB, int TERMS>
-__global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(Sweep s) {
+template <int RB>
+__global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(const __grid_constant__ Sweeps all) {
     grid_wait();
+    const Sweep &s = all.s[blockIdx.z];
+    constexpr int TERMS = 3;
     constexpr int kRow = RB + 8, kCol = kBlockCols + 8, KR = RB / 16, MT = RB / 64;
     __shared__ __align__(16) bf16 xs[16 * kRow], as[16 * kRow], bs[16 * kCol], ms[RB * kCol];
     __shared__ float pow[20];
     const int tid = threadIdx.x, lane = tid % 32, w = tc::warp_index(), g = lane / 4, t4 = lane % 4;
     const int ncol = (s.C + kBlockCols - 1) / kBlockCols, c0 = blockIdx.x % ncol * kBlockCols, cols = min(kBlockCols, s.C - c0);
     const int eh = blockIdx.x / ncol, e = eh / s.heads, h = eh % s.heads, rev = s.reverse, n = s.T;
+    if (e >= s.Be) return;  // another sweep of the launch has more columns
     const bf16 *A = static_cast<const bf16 *>(s.a) + (long long)(h / s.share_a) * s.R;
     const bf16 *B = static_cast<const bf16 *>(s.b) + (long long)(h / s.share_b) * s.C + c0;
     const bf16 *X = static_cast<const bf16 *>(s.x) + (long long)(h / s.share_x) * s.R;
@@ -811,8 +820,11 @@ __device__ __forceinline__ void store_32_bytes(float *p, const float *v) {
                  : "memory");
 }
 
-struct TileMaps {
+struct TileMap {
     CUtensorMap x, a, b, out;
+};
+struct TileMaps {
+    TileMap m[3];
 };
 
 // The segment step by step, a thread per column: what infinities and NaN in B are left to, which a product of masked weights would let
@@ -858,8 +870,10 @@ __device__ __forceinline__ void tmem_get(uint32_t at, float *v) {
 }
 
 template <int RB, int CB, bool STATE, int TERMS>
-__global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB == 64 ? 2 : 1) tile_kernel(const __grid_constant__ Sweep s, const __grid_constant__ TileMaps maps,
+__global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB == 64 ? 2 : 1) tile_kernel(const __grid_constant__ Sweeps all, const __grid_constant__ TileMaps all_maps,
                                                                                 int32_t *status) {
+    const Sweep &s = all.s[blockIdx.z];
+    const TileMap &maps = all_maps.m[blockIdx.z];
     using L = TileSmem<RB, CB, STATE, TERMS>;
     constexpr int WG = (tile_threads(RB, CB, STATE) - 32) / 128, WORKERS = 128 * WG;  // warps 0 ..; column groups
     constexpr int H = CB / WG, PC = 128 / WG;            // columns of a thread: of the state and the outputs, of S and P
@@ -1285,15 +1299,16 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
 }
 
 // What each segment starts from, in place of what it adds, and the state that is left.
-__global__ void __launch_bounds__(256) segments_kernel(Sweep s) {
+__global__ void __launch_bounds__(256) segments_kernel(const __grid_constant__ Sweeps all) {
     grid_wait();
+    const Sweep &s = all.s[blockIdx.z];
     const int eh = blockIdx.x, h = eh % s.heads, i = blockIdx.y * 256 + threadIdx.x;  // element r * C + c
     if (i >= s.R * s.C) return;
-    const long long at = (i / s.C) * s.stride_r + (i % s.C) * s.stride_c, all = (long long)s.Be * s.heads;
+    const long long at = (i / s.C) * s.stride_r + (i % s.C) * s.stride_c, states = (long long)s.Be * s.heads;
     const float l2 = log2f(s.decay[h]), whole = power(l2, s.seg_len), tail = power(l2, s.T - (s.nseg - 1) * s.seg_len);
     float m = s.m_in ? s.m_in[eh * s.state + at] : 0.f;
     float *p = s.seg + eh * (long long)s.R * s.C + i;
-    const long long step = all * s.R * s.C;
+    const long long step = states * s.R * s.C;
     for (int n = 0; n < s.nseg; n += 8) {  // in the sweep's order
         float add[8];
         int reset[8];
@@ -1301,7 +1316,7 @@ __global__ void __launch_bounds__(256) segments_kernel(Sweep s) {
         for (int k = 0; k < 8; ++k) {
             const int seg = s.reverse ? s.nseg - 1 - n - k : n + k;
             add[k] = n + k < s.nseg ? p[seg * step] : 0.f;
-            reset[k] = n + k < s.nseg ? s.seg_reset[seg * all + eh] : 0;
+            reset[k] = n + k < s.nseg ? s.seg_reset[seg * states + eh] : 0;
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -1316,16 +1331,16 @@ __global__ void __launch_bounds__(256) segments_kernel(Sweep s) {
 
 // Gradient of a shared head: the sum of those of its query heads.  Four columns a thread where C has them.
 template <typename T>
-__global__ void __launch_bounds__(256) shared_sum_kernel(const float *part, T *out, long long ldo, long long rows, int kv_heads, int share, int C) {
+__global__ void __launch_bounds__(256) shared_sum_kernel(const __grid_constant__ Sweeps all, int share) {
     grid_wait();
-    const bool four = C % 4 == 0;
-    const int n = four ? 4 : 1, width = kv_heads * C / n;
+    const Sweep &s = all.s[blockIdx.z];
+    const int C = s.C, kv_heads = s.heads / share, n = C % 4 == 0 ? 4 : 1, width = kv_heads * C / n;
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / width;
-    if (row >= rows) return;
+    if (row >= (long long)s.T * s.Be) return;
     const int at = (int)(i % width) * n, g = at / C, c = at % C;
-    const float *p = part + (row * kv_heads + g) * share * C + c;
-    T *to = out + row * ldo + at;
-    if (four) {
+    const float *p = s.shared + (row * kv_heads + g) * share * C + c;
+    T *to = static_cast<T *>(s.out) + row * s.ldo + at;
+    if (n == 4) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int k = 0; k < share; ++k) {
@@ -1436,55 +1451,52 @@ size_t seg_floats(const ppo_decay_attention_desc *d) {
     const int n = segments(d, &len);
     return n > 1 ? (size_t)n * d->Be * d->heads * (d->dk * d->dv + 1) + 7 & ~(size_t)7 : 0;  // with a flag each; in 32 bytes
 }
-size_t shared_floats(const ppo_decay_attention_desc *d) {
-    return d->heads != d->kv_heads ? (size_t)d->T * d->Be * d->heads * (d->dk > d->dv ? d->dk : d->dv) : 0;
+// In 32 bits: gradients of shared heads, of each of their query heads; in whole 32 bytes.
+size_t shared_floats(const ppo_decay_attention_desc *d, int width) {
+    return d->heads != d->kv_heads ? ((size_t)d->T * d->Be * d->heads * width + 7) & ~(size_t)7 : 0;
 }
 
-template <typename T, bool STATE, int KS = 4>
-int sweep_launch(const Sweep &s, cudaStream_t st) {
-    if constexpr (KS < 16) {
-        if (s.R > KS * kSlices) return sweep_launch<T, STATE, KS + 4>(s, st);
-    }
-    return ppo_launch(sweep_kernel<T, KS, STATE>, dim3(ppo_cdiv(s.C, kCols) * s.Be * s.heads, s.nseg), dim3(256), 0, st, s);
+// The sweeps of a call; those from `later` on wait for the others.
+struct Work {
+    Sweep s[3];
+    int n, later;
+};
+
+// fn(sweeps, how many) for the sweeps lo .. hi for which `which` holds.
+template <typename W, typename F>
+int launch_group(const Work &w, int lo, int hi, W &&which, F &&fn) {
+    Sweeps all = {};
+    int n = 0;
+    for (int i = lo; i < hi; ++i)
+        if (which(w.s[i])) all.s[n++] = w.s[i];
+    return n ? fn(all, n) : PPO_OK;
 }
-template <int RB, bool STATE, int TERMS>
-int chunk_launch_as(const Sweep &s, cudaStream_t st) {
+const auto every = [](const Sweep &) { return true; };
+
+// Blocks along x: as many as the sweep with the most columns has, `cols` of them a block.
+unsigned blocks_of(const Sweeps &all, int n, int cols) {
+    int most = 0;
+    for (int i = 0; i < n; ++i) most = most > all.s[i].C ? most : all.s[i].C;
+    return (unsigned)(ppo_cdiv(most, cols) * all.s[0].Be * all.s[0].heads);
+}
+
+template <typename T, bool STATE>
+int sweep_launch(const Sweeps &all, int n, cudaStream_t st) {
+    return ppo_launch(sweep_kernel<T, STATE>, dim3(blocks_of(all, n, kCols), all.s[0].nseg, n), dim3(256), 0, st, all);
+}
+template <int RB>
+int chunk_launch(const Sweeps &all, int n, cudaStream_t st) {
     static PerDevice<bool> allowed;
-    PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(chunk_kernel<RB, STATE, TERMS>, ChunkSmem<RB>::bytes(2)); }));
-    const int stages = s.seg_len > kChunk ? 2 : 1;
-    return ppo_launch(chunk_kernel<RB, STATE, TERMS>, dim3(ppo_cdiv(s.C, kBlockCols) * s.Be * s.heads, s.nseg), dim3(256), ChunkSmem<RB>::bytes(stages), st, s,
-                      stages);
+    PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(chunk_kernel<RB>, ChunkSmem<RB>::kBytes); }));
+    return ppo_launch(chunk_kernel<RB>, dim3(blocks_of(all, n, kBlockCols), 1, n), dim3(256), ChunkSmem<RB>::kBytes, st, all);
 }
-template <bool STATE>
-int chunk_launch(const Sweep &s, bool exact, cudaStream_t st) {
-    if (s.R <= 64) return exact ? chunk_launch_as<64, STATE, 3>(s, st) : chunk_launch_as<64, STATE, 2>(s, st);
-    return exact ? chunk_launch_as<128, STATE, 3>(s, st) : chunk_launch_as<128, STATE, 2>(s, st);
+template <int RB>
+int short_launch(const Sweeps &all, int n, cudaStream_t st) {
+    return ppo_launch(short_kernel<RB>, dim3(blocks_of(all, n, kBlockCols), 1, n), dim3(128), 0, st, all);
 }
-int short_launch(const Sweep &s, cudaStream_t st) {
-    const dim3 grid(ppo_cdiv(s.C, kBlockCols) * s.Be * s.heads);
-    if (s.R <= 64) return s.m_out ? ppo_launch(short_kernel<64, 3>, grid, dim3(128), 0, st, s) : ppo_launch(short_kernel<64, 2>, grid, dim3(128), 0, st, s);
-    return s.m_out ? ppo_launch(short_kernel<128, 3>, grid, dim3(128), 0, st, s) : ppo_launch(short_kernel<128, 2>, grid, dim3(128), 0, st, s);
-}
-template <int RB, int CB, bool STATE, int TERMS>
-int tile_launch_as(const Sweep &s, const TileMaps &maps, cudaStream_t st) {
-    using L = TileSmem<RB, CB, STATE, TERMS>;
-    static PerDevice<bool> allowed;
-    int32_t *status = ppo_device_status_ptr();
-    if (!status) return PPO_ERR_CUDA;
-    PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(tile_kernel<RB, CB, STATE, TERMS>, L::kBytes); }));
-    return ppo_launch(tile_kernel<RB, CB, STATE, TERMS>, dim3(s.Be * s.heads, s.nseg), dim3(tile_threads(RB, CB, STATE)), L::kBytes, st, s, maps, status);
-}
-template <bool STATE, int TERMS, int WIDE_TERMS>
-int tile_launch_of(const Sweep &s, const TileMaps &maps, cudaStream_t st) {
-    if (s.R <= 64) return s.C <= 64 ? tile_launch_as<64, 64, STATE, TERMS>(s, maps, st) : tile_launch_as<64, 128, STATE, TERMS>(s, maps, st);
-    return s.C <= 64 ? tile_launch_as<128, 64, STATE, WIDE_TERMS>(s, maps, st) : tile_launch_as<128, 128, STATE, WIDE_TERMS>(s, maps, st);
-}
-template <bool STATE>
-int tile_launch(const Sweep &s, const TileMaps &maps, bool exact, cudaStream_t st) {
-    return exact ? tile_launch_of<STATE, 4, 3>(s, maps, st) : tile_launch_of<STATE, 2, 2>(s, maps, st);
-}
+
 // Rows of heads as [T][Be][heads][width], boxes of 128 steps and 64 columns of one head.
-int tile_maps(const Sweep &s, TileMaps *m) {
+int tile_map(const Sweep &s, TileMap *m) {
     const int box[4] = {64, 1, 1, 128};
     const auto map = [&](CUtensorMap *to, const void *p, int width, int heads, long long ld) {
         const long long dims[4] = {width, heads, s.Be, s.T}, strides[3] = {2ll * width, 2 * ld, 2 * ld * s.Be};
@@ -1495,26 +1507,80 @@ int tile_maps(const Sweep &s, TileMaps *m) {
     PPO_TRY(map(&m->b, s.b, s.C, s.heads / s.share_b, s.ldb));
     return s.shared ? PPO_OK : map(&m->out, s.out, s.C, s.heads, s.ldo);
 }
-// Rows of 16-byte vectors.
+template <int RB, int CB, bool STATE, int TERMS>
+int tile_launch_as(const Sweeps &all, int n, cudaStream_t st) {
+    using L = TileSmem<RB, CB, STATE, TERMS>;
+    static PerDevice<bool> allowed;
+    int32_t *status = ppo_device_status_ptr();
+    if (!status) return PPO_ERR_CUDA;
+    PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(tile_kernel<RB, CB, STATE, TERMS>, L::kBytes); }));
+    TileMaps maps = {};
+    for (int i = 0; i < n; ++i) PPO_TRY(tile_map(all.s[i], &maps.m[i]));
+    return ppo_launch(tile_kernel<RB, CB, STATE, TERMS>, dim3(all.s[0].Be * all.s[0].heads, all.s[0].nseg, n), dim3(tile_threads(RB, CB, STATE)), L::kBytes,
+                      st, all, maps, status);
+}
+// The sweeps lo .. hi of `which`, those of one shape together; exact: whether a sweep hands out a state that it makes here.
+template <bool STATE, typename W>
+int tile_launch(const Work &w, int lo, int hi, W &&which, cudaStream_t st) {
+    const auto exact = [](const Sweep &s) { return s.m_out && (STATE || s.nseg == 1); };
+    for (int rows = 64; rows <= 128; rows += 64)
+        for (int cols = 64; cols <= 128; cols += 64) {
+            bool e = false;
+            const auto shape = [&](const Sweep &s) { return which(s) && (s.R <= 64) == (rows == 64) && (s.C <= 64) == (cols == 64); };
+            PPO_TRY(launch_group(w, lo, hi, shape, [&](const Sweeps &all, int n) {
+                for (int i = 0; i < n; ++i) e = e || exact(all.s[i]);
+                if (rows == 64 && cols == 64) return e ? tile_launch_as<64, 64, STATE, 4>(all, n, st) : tile_launch_as<64, 64, STATE, 2>(all, n, st);
+                if (rows == 64) return e ? tile_launch_as<64, 128, STATE, 4>(all, n, st) : tile_launch_as<64, 128, STATE, 2>(all, n, st);
+                if (cols == 64) return e ? tile_launch_as<128, 64, STATE, 3>(all, n, st) : tile_launch_as<128, 64, STATE, 2>(all, n, st);
+                return e ? tile_launch_as<128, 128, STATE, 3>(all, n, st) : tile_launch_as<128, 128, STATE, 2>(all, n, st);
+            }));
+        }
+    return PPO_OK;
+}
+// Rows of 16-byte vectors, which the tiles' maps reach.
 bool chunks_fit(const Sweep &s) {
-    const auto rows = [](const void *p, long long ld) { return ppo_aligned(p, 16) && ld % 8 == 0; };
+    const auto rows = [&](const void *p, long long ld) { return ppo_aligned(p, 16) && ld % 8 == 0 && ld * s.Be < 1ll << 38; };
     return s.R % 8 == 0 && s.C % 8 == 0 && rows(s.a, s.lda) && rows(s.b, s.ldb) && rows(s.x, s.ldx) && (s.shared || rows(s.out, s.ldo));
 }
+
 // bf16 rows that vectors fit: up to 16 steps, up to 64, more.
 template <typename T>
-int sweep(const Sweep &s, cudaStream_t st) {
-    bool chunks = std::is_same_v<T, bf16> && chunks_fit(s);
-    const bool exact = s.m_out != nullptr;
-    TileMaps maps = {};
-    if (chunks && s.T > kChunk) chunks = tile_maps(s, &maps) == PPO_OK;  // strides of 2^40 bytes have none
-    if (s.nseg > 1 && !s.seg_made) {
-        PPO_TRY(chunks ? tile_launch<true>(s, maps, exact, st) : sweep_launch<T, true>(s, st));
-        PPO_TRY(ppo_launch(segments_kernel, dim3(s.Be * s.heads, ppo_cdiv((long long)s.R * s.C, 256)), dim3(256), 0, st, s));
+int run(const Work &w, cudaStream_t st) {
+    bool chunks = std::is_same_v<T, bf16>;
+    for (int i = 0; i < w.n; ++i) chunks = chunks && chunks_fit(w.s[i]);
+    const Sweep &f = w.s[0];
+    if (f.nseg > 1) {
+        const auto to_make = [](const Sweep &s) { return !s.seg_made; };
+        if (chunks) PPO_TRY(tile_launch<true>(w, 0, w.n, to_make, st));
+        else PPO_TRY(launch_group(w, 0, w.n, to_make, [&](const Sweeps &all, int n) { return sweep_launch<T, true>(all, n, st); }));
+        PPO_TRY(launch_group(w, 0, w.n, to_make, [&](const Sweeps &all, int n) {
+            return ppo_launch(segments_kernel, dim3(f.Be * f.heads, ppo_cdiv(f.R * f.C, 256), n), dim3(256), 0, st, all);
+        }));
     }
-    if (!chunks) return sweep_launch<T, false>(s, st);
-    if (s.T <= 16) return short_launch(s, st);
-    if (s.T <= kChunk) return chunk_launch<false>(s, exact, st);
-    return tile_launch<false>(s, maps, exact && s.nseg == 1, st);
+    for (int lo = 0; lo < w.n; lo = lo < w.later ? w.later : w.n) {
+        const int hi = lo < w.later ? w.later : w.n;
+        if (!chunks) {
+            PPO_TRY(launch_group(w, lo, hi, every, [&](const Sweeps &all, int n) { return sweep_launch<T, false>(all, n, st); }));
+        } else if (f.T > kChunk) {
+            PPO_TRY(tile_launch<false>(w, lo, hi, every, st));
+        } else {
+            PPO_TRY(launch_group(w, lo, hi, [](const Sweep &s) { return s.R <= 64; }, [&](const Sweeps &all, int n) {
+                return f.T <= 16 ? short_launch<64>(all, n, st) : chunk_launch<64>(all, n, st);
+            }));
+            PPO_TRY(launch_group(w, lo, hi, [](const Sweep &s) { return s.R > 64; }, [&](const Sweeps &all, int n) {
+                return f.T <= 16 ? short_launch<128>(all, n, st) : chunk_launch<128>(all, n, st);
+            }));
+        }
+    }
+    return launch_group(w, 0, w.n, [](const Sweep &s) { return s.shared != nullptr; }, [&](const Sweeps &all, int n) {
+        const int share = all.s[0].share_x;
+        long long most = 0;
+        for (int i = 0; i < n; ++i) {
+            const long long items = (long long)f.T * f.Be * f.heads / share * all.s[i].C / (all.s[i].C % 4 == 0 ? 4 : 1);
+            most = most > items ? most : items;
+        }
+        return ppo_launch(shared_sum_kernel<T>, dim3((unsigned)((most + 255) / 256), 1, n), dim3(256), 0, st, all, share);
+    });
 }
 
 Sweep sweep_of(const ppo_decay_attention_desc *d, const float *decay, const uint8_t *done, float *seg) {
@@ -1558,7 +1624,8 @@ bool misaligned(std::initializer_list<const void *> ps, size_t a) {
 
 extern "C" size_t ppo_decay_attention_workspace_bytes(const ppo_decay_attention_desc *d, int backward) {
     if (check(d) != PPO_OK) return 0;
-    return (seg_floats(d) + (backward ? shared_floats(d) : 0)) * sizeof(float);
+    if (!backward) return seg_floats(d) * sizeof(float);
+    return (2 * seg_floats(d) + shared_floats(d, d->dk) + shared_floats(d, d->dv)) * sizeof(float);
 }
 
 extern "C" int ppo_decay_attention_fwd(const ppo_decay_attention_desc *d, const void *q, const void *k, const void *v, const float *decay,
@@ -1569,7 +1636,10 @@ extern "C" int ppo_decay_attention_fwd(const ppo_decay_attention_desc *d, const 
     if (!q || !k || !v || !decay || !o || (need > 0 && !workspace)) return PPO_ERR_INVALID_ARG;
     if (ws_bytes < need) return PPO_ERR_SHAPE;
     if (misaligned({q, k, v, o}, elem_bytes(d->dtype)) || misaligned({decay}, 4) || misaligned({state_in, state_out}, 16) || misaligned({workspace}, 32)) return PPO_ERR_ALIGN;
-    Sweep s = sweep_of(d, decay, done, static_cast<float *>(workspace));
+    Work w = {};
+    w.n = w.later = 1;
+    Sweep &s = w.s[0];
+    s = sweep_of(d, decay, done, static_cast<float *>(workspace));
     plain_state(&s, d);
     s.a = k, s.lda = d->ldk, s.b = v, s.ldb = d->ldv, s.x = q, s.ldx = d->ldq, s.out = o, s.ldo = d->ldo;
     s.share_a = s.share_b = d->heads / d->kv_heads;
@@ -1577,7 +1647,7 @@ extern "C" int ppo_decay_attention_fwd(const ppo_decay_attention_desc *d, const 
     s.m_in = state_in;
     s.m_out = state_out;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return d->dtype == PPO_F32 ? sweep<float>(s, st) : sweep<bf16>(s, st);
+    return d->dtype == PPO_F32 ? run<float>(w, st) : run<bf16>(w, st);
 }
 
 extern "C" int ppo_decay_attention_bwd(const ppo_decay_attention_desc *d, const void *q, const void *k, const void *v, const float *decay,
@@ -1590,49 +1660,39 @@ extern "C" int ppo_decay_attention_bwd(const ppo_decay_attention_desc *d, const 
     if (misaligned({q, k, v, d_o, dq, dk, dv}, elem_bytes(d->dtype)) || misaligned({decay}, 4) ||
         misaligned({state_in, dstate_out, dstate_in}, 16) || misaligned({workspace}, 32))
         return PPO_ERR_ALIGN;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int share = d->heads / d->kv_heads;
-    float *seg = static_cast<float *>(workspace), *part = share > 1 ? seg + seg_floats(d) : nullptr;
-    const long long rows = (long long)d->T * d->Be;
-    return [&](auto run) { return d->dtype == PPO_F32 ? run(float{}) : run(bf16{}); }([&](auto t) -> int {
-        using T = decltype(t);
-        Sweep s = sweep_of(d, decay, done, seg);
-        turned_state(&s, d);
-        s.a = v, s.lda = d->ldv, s.b = k, s.ldb = d->ldk, s.x = d_o, s.ldx = d->ldo, s.out = dq, s.ldo = d->ldq;
-        s.share_a = s.share_b = share;
-        s.out_scale = d->scale;
-        s.m_in = state_in;
-        PPO_TRY(sweep<T>(s, st));
-        // dk reads the states of dv's sweep, so it comes first where the sequence is not cut, for dstate_in may be dstate_out; with
-        // segments dv's leaves in the workspace what they start from
-        const int first = s.nseg > 1 ? 0 : 1;
-        for (int key : {first, 1 - first}) {
-            s = sweep_of(d, decay, done, seg);
-            s.reverse = 1;
-            s.share_x = share;
-            s.m_in = dstate_out;
-            s.shared = part;
-            T *out = static_cast<T *>(key ? dk : dv);
-            if (key) {
-                turned_state(&s, d);
-                s.seg_made = s.nseg > 1;
-                s.seg_r = 1;
-                s.seg_c = d->dv;
-                s.a = d_o, s.lda = d->ldo, s.b = q, s.ldb = d->ldq, s.x = v, s.ldx = d->ldv, s.ldo = d->ldk;
-            } else {
-                plain_state(&s, d);
-                s.a = q, s.lda = d->ldq, s.b = d_o, s.ldb = d->ldo, s.x = k, s.ldx = d->ldk, s.ldo = d->ldv;
-                s.m_out = dstate_in;
-            }
-            s.a_scale = d->scale;
-            s.out = out;
-            PPO_TRY(sweep<T>(s, st));
-            if (part)
-                PPO_TRY(ppo_launch(shared_sum_kernel<T>, dim3(ppo_cdiv(rows * d->kv_heads * s.C / (s.C % 4 == 0 ? 4 : 1), 256)), dim3(256), 0, st, (const float *)part, out, s.ldo,
-                                   rows, d->kv_heads, share, s.C));
-        }
-        return PPO_OK;
-    });
+    float *seg = static_cast<float *>(workspace), *back = seg + seg_floats(d), *part = share > 1 ? back + seg_floats(d) : nullptr;
+    Work w = {};
+    Sweep &sq = w.s[0], &sk = w.s[1], &sv = w.s[2];
+    sq = sweep_of(d, decay, done, seg);
+    turned_state(&sq, d);
+    sq.a = v, sq.lda = d->ldv, sq.b = k, sq.ldb = d->ldk, sq.x = d_o, sq.ldx = d->ldo, sq.out = dq, sq.ldo = d->ldq;
+    sq.share_a = sq.share_b = share;
+    sq.out_scale = d->scale;
+    sq.m_in = state_in;
+    sk = sweep_of(d, decay, done, back);
+    turned_state(&sk, d);
+    sk.a = d_o, sk.lda = d->ldo, sk.b = q, sk.ldb = d->ldq, sk.x = v, sk.ldx = d->ldv, sk.out = dk, sk.ldo = d->ldk;
+    sk.shared = part;
+    sv = sweep_of(d, decay, done, back);
+    plain_state(&sv, d);
+    sv.a = q, sv.lda = d->ldq, sv.b = d_o, sv.ldb = d->ldo, sv.x = k, sv.ldx = d->ldk, sv.out = dv, sv.ldo = d->ldv;
+    sv.m_out = dstate_in;
+    sv.shared = part ? part + shared_floats(d, d->dk) : nullptr;
+    for (Sweep *s : {&sk, &sv}) {
+        s->reverse = 1;
+        s->share_x = share;
+        s->m_in = dstate_out;
+        s->a_scale = d->scale;
+    }
+    // with segments dv's states are dk's, turned; without, dv's sweep may overwrite those that dk's starts from
+    sk.seg_made = sk.nseg > 1;
+    sk.seg_r = 1;
+    sk.seg_c = d->dv;
+    w.n = 3;
+    w.later = sk.nseg == 1 && dstate_in && dstate_in == dstate_out ? 2 : 3;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return d->dtype == PPO_F32 ? run<float>(w, st) : run<bf16>(w, st);
 }
 
 extern "C" int ppo_decay_attention_step(const ppo_decay_attention_desc *d, const void *q, const void *k, const void *v, const float *decay,
