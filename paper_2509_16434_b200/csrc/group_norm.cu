@@ -15,7 +15,7 @@ struct NormArgs {
     float eps;
 };
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kBlocks = 3;  // blocks on an SM that a split of an image leaves room for
 
 // Sum over the block, the same in every thread; tmp holds one value per warp.
 __device__ __forceinline__ float block_sum(float v, float *tmp) {
@@ -58,6 +58,34 @@ __device__ __forceinline__ float grad_z(float dy, float xc, Affine f, float x, f
     bool open = z > 0.f;
     if (fabsf(z) <= 5e-7f * fabsf(f.shift)) open = ((double)x - (double)mean) * (double)rstd * (double)gamma + (double)f.shift > 0.;
     return open ? dy : 0.f;
+}
+
+// dL/dz of a vector: gated for the ReLU.  xc = x - mean, per element; the check for values next to 0 is one for all of them.
+template <int ACT, int N, int M>
+__device__ __forceinline__ void grad_vector(float (&e)[N], const float (&xc)[N], const float (&x)[N], const float (&mean)[N / M], const float (&rstd)[N / M],
+                                            const float (&gamma)[N], const float (&scale)[N], const float (&beta)[N]) {
+    if constexpr (ACT == PPO_ACT_SILU) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float z = fmaf(xc[k], scale[k], beta[k]), p = sigmoid(z);
+            e[k] *= p * fmaf(z, 1.f - p, 1.f);
+        }
+    } else if constexpr (ACT == PPO_ACT_RELU) {
+        bool near = false;
+        float z[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            z[k] = fmaf(xc[k], scale[k], beta[k]);
+            near |= fabsf(z[k]) <= 5e-7f * fabsf(beta[k]);
+        }
+        if (near) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) e[k] = grad_z<ACT>(e[k], xc[k], {scale[k], beta[k]}, x[k], mean[k / M], rstd[k / M], gamma[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) e[k] = z[k] > 0.f ? e[k] : 0.f;
+        }
+    }
 }
 
 // ---- any channel count, stride and alignment: a block per image and group, element by element ----
@@ -158,25 +186,29 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_any_kernel(NormArgs a) {
         }
 }
 
-// ---- few values per image and group (up to 4 KB): `lanes` lanes of a warp per group, its values in registers ----
+// ---- few values per image and group (up to 256 vectors): `width` lanes of a warp per group, its values in registers ----
 //
-// A lane's vectors hold the same channels at every pixel (lanes is a multiple of a pixel's vectors of the group), so it keeps
+// `active` of them, a multiple of a pixel's vectors of the group: a lane's vectors hold the same channels at every pixel, so it keeps
 // their scales, and the sums over images of their gradients, for all images its block goes through.
 
+struct Lanes {
+    int width, active;
+};
+
 template <typename T, int ACT, int NV>
-__global__ void __launch_bounds__(kThreads) norm_fwd_small_kernel(NormArgs a, int lanes, long long items) {
+__global__ void __launch_bounds__(kThreads) norm_fwd_small_kernel(NormArgs a, Lanes ln, long long items) {
     grid_wait();
     constexpr int N = Vec<T>::N;
-    const int vecs = a.per / N, all = a.HW * vecs, l = threadIdx.x % lanes;
-    const long long item = (long long)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
-    const bool on = item < items;
+    const int vecs = a.per / N, all = a.HW * vecs, l = threadIdx.x % ln.width;
+    const long long item = (long long)blockIdx.x * (kThreads / ln.width) + threadIdx.x / ln.width;
+    const bool on = item < items && l < ln.active;
     const int b = on ? (int)(item / a.groups) : 0, g = on ? (int)(item % a.groups) : 0, c0 = g * a.per + l % vecs * N;
     const T *x = static_cast<const T *>(a.x) + (long long)b * a.HW * a.ldx + c0;
     Vec<T> v[NV];
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int at = i * lanes + l;
+        const int at = i * ln.active + l;
         v[i].raw = on && at < all ? *reinterpret_cast<const uint4 *>(x + at / vecs * a.ldx) : make_uint4(0, 0, 0, 0);
     }
     const float n = (float)a.HW * (float)a.per;
@@ -187,18 +219,18 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_small_kernel(NormArgs a, in
 #pragma unroll
         for (int k = 0; k < N; ++k) s += f[k];
     }
-    const float mean = lanes_sum(s, lanes) / n;
+    const float mean = lanes_sum(s, ln.width) / n;
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         float f[N];
         v[i].get(f);
-        if (i * lanes + l < all) {
+        if (on && i * ln.active + l < all) {
 #pragma unroll
             for (int k = 0; k < N; ++k) s = fmaf(f[k] - mean, f[k] - mean, s);
         }
     }
-    const float rstd = 1.f / sqrtf(lanes_sum(s, lanes) / n + a.eps);
+    const float rstd = 1.f / sqrtf(lanes_sum(s, ln.width) / n + a.eps);
     if (!on) return;
     if (l == 0) {
         a.mean[item] = mean;
@@ -213,7 +245,7 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_small_kernel(NormArgs a, in
     T *y = static_cast<T *>(a.y) + (long long)b * a.HW * a.ldy + c0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int at = i * lanes + l;
+        const int at = i * ln.active + l;
         float f[N];
         v[i].get(f);
 #pragma unroll
@@ -223,14 +255,15 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_small_kernel(NormArgs a, in
     }
 }
 
-// Block (x, y): groups y * kThreads / lanes .. of the images x, x + gridDim.x, ...
+// Block (x, y): groups y * kThreads / width .. of the images x, x + gridDim.x, ...  From NV = 4 on the values are read again (from L1)
+// instead of kept.
 template <typename T, int ACT, int NV>
-__global__ void __launch_bounds__(kThreads) norm_bwd_small_kernel(NormArgs a, int lanes) {
+__global__ void __launch_bounds__(kThreads, 2) norm_bwd_small_kernel(NormArgs a, Lanes ln) {
     grid_wait();
-    constexpr int N = Vec<T>::N;
-    const int vecs = a.per / N, all = a.HW * vecs, l = threadIdx.x % lanes;
-    const int g = blockIdx.y * (kThreads / lanes) + threadIdx.x / lanes;
-    const bool on = g < a.groups;
+    constexpr int N = Vec<T>::N, KEEP = NV < 4 ? NV : 1;
+    const int vecs = a.per / N, all = a.HW * vecs, l = threadIdx.x % ln.width;
+    const int g = blockIdx.y * (kThreads / ln.width) + threadIdx.x / ln.width;
+    const bool on = g < a.groups && l < ln.active;
     const int c0 = (on ? g * a.per : 0) + l % vecs * N;
     const float n = (float)a.HW * (float)a.per;
     float gamma[N], beta[N], s1[N], s2[N];
@@ -243,56 +276,82 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_small_kernel(NormArgs a, in
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
         const T *x = static_cast<const T *>(a.x) + (long long)b * a.HW * a.ldx + c0, *dy = static_cast<const T *>(a.dy) + (long long)b * a.HW * a.ldy + c0;
         T *dx = static_cast<T *>(a.dx) + (long long)b * a.HW * a.ldx + c0;
-        const float mean = on ? a.mean[(long long)b * a.groups + g] : 0.f, rstd = on ? a.rstd[(long long)b * a.groups + g] : 0.f;
-        Vec<T> v[NV], d[NV];
+        const float mean[1] = {on ? a.mean[(long long)b * a.groups + g] : 0.f}, rstd[1] = {on ? a.rstd[(long long)b * a.groups + g] : 0.f};
+        float scale[N];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = i * lanes + l, p = at / vecs;
+        for (int k = 0; k < N; ++k) scale[k] = rstd[0] * gamma[k];
+        Vec<T> v[KEEP], d[KEEP];
+        const auto load = [&](int i, Vec<T> &vx, Vec<T> &vd) {
+            const int at = i * ln.active + l, p = at / vecs;
             const bool ok = on && at < all;
-            v[i].raw = ok ? *reinterpret_cast<const uint4 *>(x + p * a.ldx) : make_uint4(0, 0, 0, 0);
-            d[i].raw = ok ? *reinterpret_cast<const uint4 *>(dy + p * a.ldy) : make_uint4(0, 0, 0, 0);
+            vx.raw = ok ? *reinterpret_cast<const uint4 *>(x + p * a.ldx) : make_uint4(0, 0, 0, 0);
+            vd.raw = ok ? *reinterpret_cast<const uint4 *>(dy + p * a.ldy) : make_uint4(0, 0, 0, 0);
+        };
+        const auto both = [&](const Vec<T> &vx, const Vec<T> &vd, float (&xc)[N], float (&dz)[N]) {
+            float f[N];
+            vx.get(f);
+            vd.get(dz);
+#pragma unroll
+            for (int k = 0; k < N; ++k) xc[k] = f[k] - mean[0];
+            grad_vector<ACT, N, N>(dz, xc, f, mean, rstd, gamma, scale, beta);
+        };
+        if constexpr (KEEP == NV) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) load(i, v[i], d[i]);
         }
         float m1 = 0.f, m2 = 0.f;
-#pragma unroll
+#pragma unroll(KEEP == NV ? NV : 2)
         for (int i = 0; i < NV; ++i) {
-            float f[N], e[N];
-            v[i].get(f);
-            d[i].get(e);
-            if (i * lanes + l < all) {
+            if constexpr (KEEP != NV) load(i, v[0], d[0]);
+            float xc[N], dz[N];
+            both(v[i % KEEP], d[i % KEEP], xc, dz);
+            if (on && i * ln.active + l < all) {
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
-                    const float xc = f[k] - mean, dz = grad_z<ACT>(e[k], xc, {rstd * gamma[k], beta[k]}, f[k], mean, rstd, gamma[k]);
-                    s1[k] += dz;
-                    s2[k] = fmaf(dz, xc * rstd, s2[k]);
-                    m1 = fmaf(gamma[k], dz, m1);
-                    m2 = fmaf(gamma[k] * dz, xc, m2);
+                    s1[k] += dz[k];
+                    s2[k] = fmaf(dz[k], xc[k] * rstd[0], s2[k]);
+                    m1 = fmaf(gamma[k], dz[k], m1);
+                    m2 = fmaf(gamma[k] * dz[k], xc[k], m2);
                 }
             }
         }
-        m1 = lanes_sum(m1, lanes) / n;
-        m2 = lanes_sum(m2, lanes) / n * rstd * rstd;
-#pragma unroll
+        m1 = lanes_sum(m1, ln.width) / n;
+        m2 = lanes_sum(m2, ln.width) / n * rstd[0] * rstd[0];
+#pragma unroll(KEEP == NV ? NV : 2)
         for (int i = 0; i < NV; ++i) {
-            const int at = i * lanes + l;
-            float f[N], e[N];
-            v[i].get(f);
-            d[i].get(e);
+            if constexpr (KEEP != NV) load(i, v[0], d[0]);
+            const int at = i * ln.active + l;
+            float xc[N], dz[N];
+            both(v[i % KEEP], d[i % KEEP], xc, dz);
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const float xc = f[k] - mean, dz = grad_z<ACT>(e[k], xc, {rstd * gamma[k], beta[k]}, f[k], mean, rstd, gamma[k]);
-                f[k] = rstd * (fmaf(gamma[k], dz, -m1) - xc * m2);
-            }
-            v[i].set(f);
-            if (on && at < all) *reinterpret_cast<uint4 *>(dx + at / vecs * a.ldx) = v[i].raw;
+            for (int k = 0; k < N; ++k) dz[k] = rstd[0] * (fmaf(gamma[k], dz[k], -m1) - xc[k] * m2);
+            Vec<T> r;
+            r.set(dz);
+            if (on && at < all) *reinterpret_cast<uint4 *>(dx + at / vecs * a.ldx) = r.raw;
         }
     }
     if (!a.part) return;
+    // lanes of other pixels of the same channels
+    const int pixels = ln.active / vecs;
+    if ((pixels & (pixels - 1)) == 0 && ln.active == ln.width) {
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-        for (int o = vecs; o < lanes; o <<= 1) {  // lanes of other pixels of the same channels
-            s1[k] += __shfl_xor_sync(0xffffffffu, s1[k], o);
-            s2[k] += __shfl_xor_sync(0xffffffffu, s2[k], o);
+        for (int k = 0; k < N; ++k)
+            for (int o = vecs; o < ln.width; o <<= 1) {
+                s1[k] += __shfl_xor_sync(0xffffffffu, s1[k], o);
+                s2[k] += __shfl_xor_sync(0xffffffffu, s2[k], o);
+            }
+    } else {  // a whole warp; lane l < vecs adds those of l + vecs, l + 2 vecs, ...
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float t1 = s1[k], t2 = s2[k];
+            for (int p = 1; p < pixels; ++p) {
+                t1 += __shfl_sync(0xffffffffu, s1[k], (l + p * vecs) & 31);
+                t2 += __shfl_sync(0xffffffffu, s2[k], (l + p * vecs) & 31);
+            }
+            s1[k] = t1;
+            s2[k] = t2;
         }
+    }
     if (on && l < vecs) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -302,16 +361,19 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_small_kernel(NormArgs a, in
     }
 }
 
-// ---- larger images: a cluster of blocks per image, each with a run of its pixels, which it keeps in shared memory ----
+// ---- larger images: several blocks per image, each with a run of its pixels ----
 //
-// Thread (pl, vc) has the same vector of channels of the pixels pl, pl + lanes, ...: memory is read and written in whole rows,
-// once, and what a thread copies in is what it uses, so that only the sums meet at barriers.  K: parts of a vector that belong
-// to different groups (1: a group has whole vectors).  `keep` 0: images that do not fit are read again for each use, from L2 where
-// that holds what the running clusters work on.
+// Thread (pl, vc) has the same vector of channels of the pixels pl, pl + lanes, ...: memory is read and written in whole rows.
+// K: parts of a vector that belong to different groups (1: a group has whole vectors).
+//   WHOLE: a cluster per image, whose blocks keep their pixels in shared memory between the sums, which they exchange there, and
+// the result: read once, written once.  What a thread copies in is what it uses, so that only the sums meet at barriers.
+//   SUMS, then APPLY: images that do not fit eight blocks; the sums go through the workspace, and the second launch reads the image again.
+enum { WHOLE, SUMS, APPLY };
 
-struct Cluster {
-    int n, pixels, keep;  // blocks per image, pixels per block
+struct Split {
+    int n, pixels;  // blocks per image, pixels per block
     size_t smem;
+    float *sums;    // SUMS, APPLY: [B][n][groups][2]
 };
 
 // Entries of group g among the threads' K parts: thread pl * VC + first + i has part k; pl < lanes, i < span.
@@ -322,95 +384,110 @@ template <int N, int K>
 __device__ __forceinline__ Members members(int g, int per) {
     return K == 1 ? Members{g * (per / N), per / N, 0} : Members{g / K, 1, g % K};
 }
+// A pair of numbers of this block (rank) and group, to every block of the cluster.
+__device__ __forceinline__ void send(float *sent, int rank, int groups, int g, int n, float a, float b) {
+    const int to = threadIdx.x % 32;
+    if (to < n) {
+        const uint32_t at = tc::in_cta(tc::smem_u32(sent + (rank * groups + g) * 2), to);
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(a) : "memory");
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(b) : "memory");
+    }
+}
 
-template <typename T, int ACT, int K>
-__global__ void __launch_bounds__(kThreads) norm_fwd_cluster_kernel(NormArgs a, Cluster cl) {
+template <typename T, int ACT, int K, int MODE>
+__global__ void __launch_bounds__(kThreads) norm_fwd_image_kernel(NormArgs a, Split sp) {
     grid_wait();
-    tc::cluster_arrive();
+    if (MODE == WHOLE) tc::cluster_arrive();
     constexpr int N = Vec<T>::N, M = N / K;
     extern __shared__ __align__(16) float mem[];
-    float *tm = mem, *tq = tm + kThreads * K, *sent = tq + kThreads * K, *stat = sent + (cl.n * a.groups * 2 + 3) / 4 * 4;
+    float *tm = mem, *tq = tm + kThreads * K, *sent = tq + kThreads * K, *stat = sent + (MODE == WHOLE ? (sp.n * a.groups * 2 + 3) / 4 * 4 : 0);
     uint4 *kept = reinterpret_cast<uint4 *>(stat + (a.groups * 2 + 3) / 4 * 4);
-    const int rank = blockIdx.x % cl.n, b = blockIdx.x / cl.n;
+    const int rank = blockIdx.x % sp.n, b = blockIdx.x / sp.n;
     const int VC = a.C / N, lanes = kThreads / VC, tid = threadIdx.x, pl = tid / VC, vc = tid % VC;
-    const int p0 = rank * cl.pixels, P = max(0, min(cl.pixels, a.HW - p0));
+    const int p0 = rank * sp.pixels, P = max(0, min(sp.pixels, a.HW - p0));
     const int cnt = pl < lanes && pl < P ? (P - 1 - pl) / lanes + 1 : 0;
     const T *x = static_cast<const T *>(a.x) + ((long long)b * a.HW + p0 + pl) * a.ldx + vc * N;
     T *y = static_cast<T *>(a.y) + ((long long)b * a.HW + p0 + pl) * a.ldy + vc * N;
     const long long sx = lanes * a.ldx, sy = lanes * a.ldy;
-    if (cl.keep) {
+    if (MODE == WHOLE) {
         for (int i = 0; i < cnt; ++i) tc::cp_async16(tc::smem_u32(kept + i * kThreads + tid), x + i * sx, true);
         tc::cp_async_commit();
         tc::cp_async_wait<0>();
     }
-    auto get = [&](int i, float *f) {
+    const auto get = [&](int i, float (&f)[N]) {
         Vec<T> v;
-        v.raw = cl.keep ? kept[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(x + i * sx);
+        v.raw = MODE == WHOLE ? kept[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(x + i * sx);
         v.get(f);
     };
-    // mean and squares about it of this thread's values, then of the block's, then of the image's
-    float m[K], q[K];
+    if constexpr (MODE != APPLY) {
+        // mean and squares about it of this thread's values, then of the block's
+        float m[K], q[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) m[k] = q[k] = 0.f;
-    for (int i = 0; i < cnt; ++i) {
-        float f[N];
-        get(i, f);
+        for (int k = 0; k < K; ++k) m[k] = q[k] = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < cnt; ++i) {
+            float f[N];
+            get(i, f);
 #pragma unroll
-        for (int k = 0; k < N; ++k) m[k / M] += f[k];
+            for (int k = 0; k < N; ++k) m[k / M] += f[k];
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) m[k] = cnt ? m[k] / (float)(cnt * M) : 0.f;
+#pragma unroll 4
+        for (int i = 0; i < cnt; ++i) {
+            float f[N];
+            get(i, f);
+#pragma unroll
+            for (int k = 0; k < N; ++k) q[k / M] = fmaf(f[k] - m[k / M], f[k] - m[k / M], q[k / M]);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            tm[tid * K + k] = m[k];
+            tq[tid * K + k] = q[k];
+        }
+        __syncthreads();
+        if (MODE == WHOLE) tc::cluster_wait();  // all blocks of the cluster run
+        for (int g = tid / 32; g < a.groups; g += kThreads / 32) {
+            const Members e = members<N, K>(g, a.per);
+            const float total = (float)P * (float)a.per;
+            float sum = 0.f, sq = 0.f;
+            for (int i = tid % 32; i < lanes * e.span; i += 32) {
+                const int p = i / e.span, t = p * VC + e.first + i % e.span;
+                const float w = p < P ? (float)(((P - 1 - p) / lanes + 1) * M) : 0.f;
+                sum = fmaf(w, tm[t * K + e.k], sum);
+            }
+            const float mean = P ? warp_sum(sum) / total : 0.f;
+            for (int i = tid % 32; i < lanes * e.span; i += 32) {
+                const int p = i / e.span, t = p * VC + e.first + i % e.span;
+                const float w = p < P ? (float)(((P - 1 - p) / lanes + 1) * M) : 0.f, d = tm[t * K + e.k] - mean;
+                if (w > 0.f) sq += fmaf(w * d, d, tq[t * K + e.k]);
+            }
+            sq = warp_sum(sq);
+            if (MODE == WHOLE) send(sent, rank, a.groups, g, sp.n, mean, sq);
+            else if (tid % 32 == 0) *reinterpret_cast<float2 *>(sp.sums + ((size_t)blockIdx.x * a.groups + g) * 2) = make_float2(mean, sq);
+        }
+        if (MODE == SUMS) return;
+        tc::cluster_sync();
     }
-#pragma unroll
-    for (int k = 0; k < K; ++k) m[k] = cnt ? m[k] / (float)(cnt * M) : 0.f;
-    for (int i = 0; i < cnt; ++i) {
-        float f[N];
-        get(i, f);
-#pragma unroll
-        for (int k = 0; k < N; ++k) q[k / M] = fmaf(f[k] - m[k / M], f[k] - m[k / M], q[k / M]);
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        tm[tid * K + k] = m[k];
-        tq[tid * K + k] = q[k];
-    }
-    __syncthreads();
-    tc::cluster_wait();  // all blocks of the cluster run
+    // of the image
+    const float *from = MODE == WHOLE ? sent : sp.sums + (size_t)b * sp.n * a.groups * 2;
     for (int g = tid / 32; g < a.groups; g += kThreads / 32) {
-        const Members e = members<N, K>(g, a.per);
-        const float total = (float)P * (float)a.per;
-        float sum = 0.f, sq = 0.f;
-        for (int i = tid % 32; i < lanes * e.span; i += 32) {
-            const int p = i / e.span, t = p * VC + e.first + i % e.span;
-            const float w = p < P ? (float)(((P - 1 - p) / lanes + 1) * M) : 0.f;
-            sum = fmaf(w, tm[t * K + e.k], sum);
-        }
-        const float mean = P ? warp_sum(sum) / total : 0.f;
-        for (int i = tid % 32; i < lanes * e.span; i += 32) {
-            const int p = i / e.span, t = p * VC + e.first + i % e.span;
-            const float w = p < P ? (float)(((P - 1 - p) / lanes + 1) * M) : 0.f, d = tm[t * K + e.k] - mean;
-            if (w > 0.f) sq += fmaf(w * d, d, tq[t * K + e.k]);
-        }
-        sq = warp_sum(sq);
-        if (tid % 32 < cl.n) {
-            const uint32_t at = tc::in_cta(tc::smem_u32(sent + (rank * a.groups + g) * 2), tid % 32);
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(mean) : "memory");
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(sq) : "memory");
-        }
-    }
-    tc::cluster_sync();
-    for (int g = tid; g < a.groups; g += kThreads) {
-        float mean = 0.f, sq = 0.f;
         const float per = (float)a.per, n = (float)a.HW * per;
-        for (int r = 0; r < cl.n; ++r) mean = fmaf((float)max(0, min(cl.pixels, a.HW - r * cl.pixels)) * per, sent[(r * a.groups + g) * 2], mean);
-        mean /= n;
-        for (int r = 0; r < cl.n; ++r) {
-            const float w = (float)max(0, min(cl.pixels, a.HW - r * cl.pixels)) * per, d = sent[(r * a.groups + g) * 2] - mean;
-            if (w > 0.f) sq += fmaf(w * d, d, sent[(r * a.groups + g) * 2 + 1]);
+        float sum = 0.f, sq = 0.f;
+        for (int r = tid % 32; r < sp.n; r += 32) sum = fmaf((float)max(0, min(sp.pixels, a.HW - r * sp.pixels)) * per, from[(r * a.groups + g) * 2], sum);
+        const float mean = warp_sum(sum) / n;
+        for (int r = tid % 32; r < sp.n; r += 32) {
+            const float w = (float)max(0, min(sp.pixels, a.HW - r * sp.pixels)) * per, d = from[(r * a.groups + g) * 2] - mean;
+            if (w > 0.f) sq += fmaf(w * d, d, from[(r * a.groups + g) * 2 + 1]);
         }
-        const float rstd = 1.f / sqrtf(sq / n + a.eps);
-        stat[g * 2] = mean;
-        stat[g * 2 + 1] = rstd;
-        if (rank == 0) {
-            a.mean[(long long)b * a.groups + g] = mean;
-            a.rstd[(long long)b * a.groups + g] = rstd;
+        const float rstd = 1.f / sqrtf(warp_sum(sq) / n + a.eps);
+        if (tid % 32 == 0) {
+            stat[g * 2] = mean;
+            stat[g * 2 + 1] = rstd;
+            if (rank == 0) {
+                a.mean[(long long)b * a.groups + g] = mean;
+                a.rstd[(long long)b * a.groups + g] = rstd;
+            }
         }
     }
     __syncthreads();
@@ -436,31 +513,31 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_cluster_kernel(NormArgs a, 
     }
 }
 
-template <typename T, int ACT, int K>
-__global__ void __launch_bounds__(kThreads) norm_bwd_cluster_kernel(NormArgs a, Cluster cl) {
+template <typename T, int ACT, int K, int MODE>
+__global__ void __launch_bounds__(kThreads, 2) norm_bwd_image_kernel(NormArgs a, Split sp) {
     grid_wait();
-    tc::cluster_arrive();
+    if (MODE == WHOLE) tc::cluster_arrive();
     constexpr int N = Vec<T>::N, M = N / K;
     extern __shared__ __align__(16) float mem[];
-    float *ts = mem, *chan = ts + kThreads * 2 * N, *sent = chan + 2 * a.C, *stat = sent + (cl.n * a.groups * 2 + 3) / 4 * 4;
+    float *ts = mem, *chan = ts + kThreads * 2 * N, *sent = chan + 2 * a.C, *stat = sent + (MODE == WHOLE ? (sp.n * a.groups * 2 + 3) / 4 * 4 : 0);
     uint4 *keptx = reinterpret_cast<uint4 *>(stat + (a.groups * 2 + 3) / 4 * 4);
-    const int rank = blockIdx.x % cl.n, b = blockIdx.x / cl.n;
+    const int rank = blockIdx.x % sp.n, b = blockIdx.x / sp.n;
     const int VC = a.C / N, lanes = kThreads / VC, tid = threadIdx.x, pl = tid / VC, vc = tid % VC;
-    const int p0 = rank * cl.pixels, P = max(0, min(cl.pixels, a.HW - p0)), rounds = (cl.pixels + lanes - 1) / lanes;
+    const int p0 = rank * sp.pixels, P = max(0, min(sp.pixels, a.HW - p0)), rounds = (sp.pixels + lanes - 1) / lanes;
     uint4 *keptd = keptx + rounds * kThreads;
     const int cnt = pl < lanes && pl < P ? (P - 1 - pl) / lanes + 1 : 0;
     const long long px = ((long long)b * a.HW + p0 + pl) * a.ldx + vc * N, py = ((long long)b * a.HW + p0 + pl) * a.ldy + vc * N;
     const T *x = static_cast<const T *>(a.x) + px, *dy = static_cast<const T *>(a.dy) + py;
     T *dx = static_cast<T *>(a.dx) + px;
     const long long sx = lanes * a.ldx, sy = lanes * a.ldy;
-    if (cl.keep) {
+    if (MODE == WHOLE) {
         for (int i = 0; i < cnt; ++i) {
             tc::cp_async16(tc::smem_u32(keptx + i * kThreads + tid), x + i * sx, true);
             tc::cp_async16(tc::smem_u32(keptd + i * kThreads + tid), dy + i * sy, true);
         }
         tc::cp_async_commit();
     }
-    float mean[K], rstd[K], gamma[N], beta[N], s1[N], s2[N];
+    float mean[K], rstd[K], scale[N], gamma[N], beta[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int c = min(vc * N + k, a.C - 1), g = K == 1 ? c / a.per : vc * K + k / M;
@@ -468,78 +545,95 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_cluster_kernel(NormArgs a, 
         rstd[k / M] = a.rstd[(long long)b * a.groups + g];
         gamma[k] = a.gamma ? a.gamma[c] : 1.f;
         beta[k] = a.gamma ? a.beta[c] : 0.f;
-        s1[k] = s2[k] = 0.f;
+        scale[k] = rstd[k / M] * gamma[k];
     }
-    if (cl.keep) tc::cp_async_wait<0>();
-    auto get = [&](int i, float *f, float *e) {
+    if (MODE == WHOLE) tc::cp_async_wait<0>();
+    // x - mean and dL/dz; a gated dL/dy of the ReLU is kept, in the place of dL/dy, for the second time
+    const auto get = [&](int i, float (&xc)[N], float (&dz)[N], bool again) {
         Vec<T> v, d;
-        v.raw = cl.keep ? keptx[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(x + i * sx);
-        d.raw = cl.keep ? keptd[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(dy + i * sy);
+        v.raw = MODE == WHOLE ? keptx[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(x + i * sx);
+        d.raw = MODE == WHOLE ? keptd[i * kThreads + tid] : *reinterpret_cast<const uint4 *>(dy + i * sy);
+        float f[N];
         v.get(f);
-        d.get(e);
+        d.get(dz);
+#pragma unroll
+        for (int k = 0; k < N; ++k) xc[k] = f[k] - mean[k / M];
+        if (MODE == WHOLE && ACT == PPO_ACT_RELU && again) return;
+        grad_vector<ACT, N, M>(dz, xc, f, mean, rstd, gamma, scale, beta);
+        if (MODE == WHOLE && ACT == PPO_ACT_RELU) {
+            d.set(dz);
+            keptd[i * kThreads + tid] = d.raw;
+        }
     };
-    for (int i = 0; i < cnt; ++i) {
-        float f[N], e[N];
-        get(i, f, e);
+    if constexpr (MODE != APPLY) {
+        float s1[N], s2[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) s1[k] = s2[k] = 0.f;
+#pragma unroll 2
+        for (int i = 0; i < cnt; ++i) {
+            float xc[N], dz[N];
+            get(i, xc, dz, false);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                s1[k] += dz[k];
+                s2[k] = fmaf(dz[k], xc[k], s2[k]);
+            }
+        }
+        // [2][N][threads]
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const float xc = f[k] - mean[k / M];
-            const float dz = grad_z<ACT>(e[k], xc, {rstd[k / M] * gamma[k], beta[k]}, f[k], mean[k / M], rstd[k / M], gamma[k]);
-            s1[k] += dz;
-            s2[k] = fmaf(dz, xc, s2[k]);
+            ts[k * kThreads + tid] = s1[k];
+            ts[(N + k) * kThreads + tid] = s2[k] * rstd[k / M];
         }
-    }
-    // [2][N][threads]
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        ts[k * kThreads + tid] = s1[k];
-        ts[(N + k) * kThreads + tid] = s2[k] * rstd[k / M];
-    }
-    __syncthreads();
-    tc::cluster_wait();  // all blocks of the cluster run
-    int sub = 1;  // lanes per channel and sum
-    while (sub < 32 && sub * 2 * 2 * a.C <= kThreads) sub *= 2;
-    for (int i0 = 0; i0 < 2 * a.C; i0 += kThreads / sub) {
-        const int i = i0 + tid / sub, k2 = i / a.C, c = i % a.C;
-        float s = 0.f;
-        if (i < 2 * a.C)
-            for (int p = tid % sub; p < lanes; p += sub) s += ts[(k2 * N + c % N) * kThreads + p * VC + c / N];
-        s = lanes_sum(s, sub);
-        if (i < 2 * a.C && tid % sub == 0) {
-            chan[i] = s;
-            if (a.part) a.part[((size_t)blockIdx.x * 2 + 1 - k2) * a.C + c] = s;  // gamma's first
+        __syncthreads();
+        if (MODE == WHOLE) tc::cluster_wait();  // all blocks of the cluster run
+        int sub = 1;  // lanes per channel and sum
+        while (sub < 32 && sub * 2 * 2 * a.C <= kThreads) sub *= 2;
+        for (int i0 = 0; i0 < 2 * a.C; i0 += kThreads / sub) {
+            const int i = i0 + tid / sub, k2 = i / a.C, c = i % a.C;
+            float s = 0.f;
+            if (i < 2 * a.C)
+                for (int p = tid % sub; p < lanes; p += sub) s += ts[(k2 * N + c % N) * kThreads + p * VC + c / N];
+            s = lanes_sum(s, sub);
+            if (i < 2 * a.C && tid % sub == 0) {
+                chan[i] = s;
+                if (a.part) a.part[((size_t)blockIdx.x * 2 + 1 - k2) * a.C + c] = s;  // gamma's first
+            }
         }
+        __syncthreads();
+        for (int g = tid / 32; g < a.groups; g += kThreads / 32) {
+            float m1 = 0.f, m2 = 0.f;
+            for (int c = g * a.per + tid % 32; c < (g + 1) * a.per; c += 32) {
+                const float w = a.gamma ? a.gamma[c] : 1.f;
+                m1 = fmaf(w, chan[c], m1);
+                m2 = fmaf(w, chan[a.C + c], m2);
+            }
+            m1 = warp_sum(m1);
+            m2 = warp_sum(m2);
+            if (MODE == WHOLE) send(sent, rank, a.groups, g, sp.n, m1, m2);
+            else if (tid % 32 == 0) *reinterpret_cast<float2 *>(sp.sums + ((size_t)blockIdx.x * a.groups + g) * 2) = make_float2(m1, m2);
+        }
+        if (MODE == SUMS) return;
+        tc::cluster_sync();
     }
-    __syncthreads();
+    const float *from = MODE == WHOLE ? sent : sp.sums + (size_t)b * sp.n * a.groups * 2;
     for (int g = tid / 32; g < a.groups; g += kThreads / 32) {
         float m1 = 0.f, m2 = 0.f;
-        for (int c = g * a.per + tid % 32; c < (g + 1) * a.per; c += 32) {
-            const float w = a.gamma ? a.gamma[c] : 1.f;
-            m1 = fmaf(w, chan[c], m1);
-            m2 = fmaf(w, chan[a.C + c], m2);
-        }
-        m1 = warp_sum(m1);
-        m2 = warp_sum(m2);
-        if (tid % 32 < cl.n) {
-            const uint32_t at = tc::in_cta(tc::smem_u32(sent + (rank * a.groups + g) * 2), tid % 32);
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(m1) : "memory");
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(m2) : "memory");
-        }
-    }
-    tc::cluster_sync();
-    for (int g = tid; g < a.groups; g += kThreads) {
-        float m1 = 0.f, m2 = 0.f;
-        for (int r = 0; r < cl.n; ++r) {
-            m1 += sent[(r * a.groups + g) * 2];
-            m2 += sent[(r * a.groups + g) * 2 + 1];
+        for (int r = tid % 32; r < sp.n; r += 32) {
+            m1 += from[(r * a.groups + g) * 2];
+            m2 += from[(r * a.groups + g) * 2 + 1];
         }
         const float n = (float)a.HW * (float)a.per;
-        stat[g * 2] = m1 / n;
-        stat[g * 2 + 1] = m2 / n;
+        m1 = warp_sum(m1);
+        m2 = warp_sum(m2);
+        if (tid % 32 == 0) {
+            stat[g * 2] = m1 / n;
+            stat[g * 2 + 1] = m2 / n;
+        }
     }
     __syncthreads();
     if (cnt == 0) return;
-    // dx = A dz + (D xc + E)
+    // dx = scale dz + (D xc + E)
     float D[K], E[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -549,16 +643,12 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_cluster_kernel(NormArgs a, 
     }
 #pragma unroll 2
     for (int i = 0; i < cnt; ++i) {
-        float f[N], e[N];
-        get(i, f, e);
+        float xc[N], dz[N];
+        get(i, xc, dz, true);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const float xc = f[k] - mean[k / M], scale = rstd[k / M] * gamma[k];
-            const float dz = grad_z<ACT>(e[k], xc, {scale, beta[k]}, f[k], mean[k / M], rstd[k / M], gamma[k]);
-            f[k] = fmaf(scale, dz, fmaf(D[k / M], xc, E[k / M]));
-        }
+        for (int k = 0; k < N; ++k) dz[k] = fmaf(scale[k], dz[k], fmaf(D[k / M], xc[k], E[k / M]));
         Vec<T> v;
-        v.set(f);
+        v.set(dz);
         *reinterpret_cast<uint4 *>(dx + i * sx) = v.raw;
     }
 }
@@ -583,11 +673,13 @@ __global__ void __launch_bounds__(512) norm_sum_kernel(const float *part, int pa
 // ---- which kernel ----
 
 struct Plan {
-    enum { ANY, SMALL, CLUSTER } kind;
-    int lanes, nv, blocks;  // SMALL: lanes per group, vectors per lane, blocks along the images (backward)
-    int K;                  // CLUSTER
-    Cluster cl;
-    int parts;              // shares of the gradients of gamma and beta
+    enum { ANY, SMALL, IMAGE } kind;
+    Lanes lanes;     // SMALL: per group; vectors per lane, blocks along the images (backward)
+    int nv, blocks;
+    int K, whole;    // IMAGE
+    Split sp;
+    int parts;       // shares of the gradients of gamma and beta
+    size_t floats;   // of the workspace
 };
 
 // By sizes alone (so that the workspace is known before the addresses are); rows that turn out not to be aligned take the kernels
@@ -597,37 +689,48 @@ Plan plan_of(const ppo_group_norm_desc *d, bool bwd) {
     const int size = (int)elem_bytes(d->dtype), N = 16 / size, per = d->C / d->groups;
     p.kind = Plan::ANY;
     p.parts = d->B;
+    p.floats = bwd ? (size_t)2 * d->B * d->C : 0;
     if (d->C % N != 0 || d->ldx % N != 0 || d->ldy % N != 0) return p;
     const long long all = (long long)d->HW * per / N;  // vectors of an image and group
     const int vecs = per / N;
-    if (per % N == 0 && vecs <= 32 && (vecs & (vecs - 1)) == 0 && all <= 32 * 4) {
-        int lanes = vecs;
-        while (lanes < 32 && lanes < all) lanes *= 2;
+    if (per % N == 0 && vecs <= 32 && all <= 32 / vecs * vecs * 8) {
+        int width = 32, active = 32 / vecs * vecs;
+        if ((vecs & (vecs - 1)) == 0)
+            for (width = vecs, active = 0; width < 32 && width < all;) width *= 2;
+        if (active == 0) active = width;
         p.kind = Plan::SMALL;
-        p.lanes = lanes;
-        p.nv = all <= lanes ? 1 : all <= 2 * lanes ? 2 : 4;
-        const int columns = ppo_cdiv(d->groups, kThreads / lanes);
+        p.lanes = {width, active};
+        p.nv = all <= active ? 1 : all <= 2 * active ? 2 : all <= 4 * active ? 4 : 8;
+        const int columns = ppo_cdiv(d->groups, kThreads / width);
         p.blocks = ppo_cdiv(4 * 148, columns);
         if (p.blocks > d->B) p.blocks = d->B;
         p.parts = p.blocks;
-        return p;
+    } else {
+        p.K = per % N == 0 ? 1 : N % per == 0 ? N / per : 0;
+        const int VC = d->C / N;
+        if (p.K == 0 || VC > kThreads || d->groups > 1024) return p;
+        p.kind = Plan::IMAGE;
+        const int lanes = kThreads / VC;
+        const auto smem = [&](int n, bool whole) {
+            const int rounds = ppo_cdiv(ppo_cdiv(d->HW, n), lanes);
+            const size_t floats = (bwd ? kThreads * 2 * N + 2 * d->C : kThreads * p.K * 2) + (whole ? ((size_t)n * d->groups * 2 + 3) / 4 * 4 : 0) +
+                                  (d->groups * 2 + 3) / 4 * 4;
+            return floats * 4 + (whole ? (size_t)rounds * kThreads * 16 * (bwd ? 2 : 1) : 0);
+        };
+        // as few blocks per image as leave room for kBlocks on an SM, else for two or one
+        int n = 1;
+        while (n < 8 && smem(n, true) > 227 * 1024 / kBlocks - 1024) n *= 2;
+        p.whole = smem(n, true) <= 227 * 1024;
+        if (!p.whole) {  // as many as give every SM four, none with less than four rows of its lanes
+            n = ppo_cdiv(4 * 148, d->B);
+            const int most = ppo_cdiv(d->HW, 4 * lanes);
+            if (n > most) n = most;
+        }
+        p.sp = {n, ppo_cdiv(d->HW, n), smem(n, p.whole), nullptr};
+        p.parts = d->B * n;
     }
-    p.K = per % N == 0 ? 1 : N % per == 0 ? N / per : 0;
-    const int VC = d->C / N;
-    if (p.K == 0 || VC > kThreads || d->groups > 2048) return p;
-    p.kind = Plan::CLUSTER;
-    const int lanes = kThreads / VC;
-    auto smem = [&](int n, int keep) {
-        const int pixels = ppo_cdiv(d->HW, n), rounds = ppo_cdiv(pixels, lanes);
-        const size_t floats = (bwd ? kThreads * 2 * N + 2 * d->C : kThreads * p.K * 2) + ((size_t)n * d->groups * 2 + 3) / 4 * 4 + (d->groups * 2 + 3) / 4 * 4;
-        return floats * 4 + 16 + (keep ? (size_t)rounds * kThreads * 16 * (bwd ? 2 : 1) : 0);
-    };
-    // as few blocks per image as leave room for two on an SM, else for one
-    int n = 1;
-    while (n < 8 && smem(n, 1) > 110 * 1024) n *= 2;
-    const int keep = smem(n, 1) <= 220 * 1024;
-    p.cl = {n, ppo_cdiv(d->HW, n), keep, smem(n, keep)};
-    p.parts = d->B * n;
+    p.floats = bwd ? (size_t)2 * (p.parts > d->B ? p.parts : d->B) * d->C : 0;
+    if (p.kind == Plan::IMAGE && !p.whole) p.floats += (p.floats & 1) + (size_t)p.parts * d->groups * 2;
     return p;
 }
 
@@ -644,12 +747,24 @@ int with_elem_act(int dtype, int act, F &&fn) {
     return with_act<__half>(act, fn);
 }
 
-// In clusters, with more shared memory than a kernel has by itself.
 template <auto FN>
-int launch_cluster(const NormArgs &a, const Cluster &cl, cudaStream_t st) {
+int launch_image(bool cluster, const NormArgs &a, const Split &sp, cudaStream_t st) {
     static PerDevice<bool> allowed;
     PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(FN, 227 * 1024); }));
-    return ppo_launch_cluster(FN, cl.n, dim3((unsigned)(a.B * cl.n)), dim3(kThreads), cl.smem, st, a, cl);
+    const dim3 grid((unsigned)(a.B * sp.n)), block(kThreads);
+    return cluster ? ppo_launch_cluster(FN, sp.n, grid, block, sp.smem, st, a, sp) : ppo_launch(FN, grid, block, sp.smem, st, a, sp);
+}
+template <typename T, int ACT, int K>
+int fwd_image(const Plan &p, const NormArgs &a, cudaStream_t st) {
+    if (p.whole) return launch_image<norm_fwd_image_kernel<T, ACT, K, WHOLE>>(true, a, p.sp, st);
+    PPO_TRY((launch_image<norm_fwd_image_kernel<T, PPO_ACT_NONE, K, SUMS>>(false, a, p.sp, st)));
+    return launch_image<norm_fwd_image_kernel<T, ACT, K, APPLY>>(false, a, p.sp, st);
+}
+template <typename T, int ACT, int K>
+int bwd_image(const Plan &p, const NormArgs &a, cudaStream_t st) {
+    if (p.whole) return launch_image<norm_bwd_image_kernel<T, ACT, K, WHOLE>>(true, a, p.sp, st);
+    PPO_TRY((launch_image<norm_bwd_image_kernel<T, ACT, K, SUMS>>(false, a, p.sp, st)));
+    return launch_image<norm_bwd_image_kernel<T, ACT, K, APPLY>>(false, a, p.sp, st);
 }
 
 int check(const ppo_group_norm_desc *d) {
@@ -676,9 +791,7 @@ NormArgs args(const ppo_group_norm_desc *d) {
 }  // namespace
 
 extern "C" size_t ppo_group_norm_workspace_bytes(const ppo_group_norm_desc *d, int backward) {
-    if (check(d) != PPO_OK || !backward) return 0;
-    const int parts = plan_of(d, true).parts;
-    return (size_t)2 * (parts > d->B ? parts : d->B) * d->C * sizeof(float);
+    return check(d) == PPO_OK ? plan_of(d, backward != 0).floats * sizeof(float) : 0;
 }
 
 extern "C" int ppo_group_norm_fwd(const ppo_group_norm_desc *d, float eps, const void *x, const float *gamma, const float *beta, void *y, float *mean,
@@ -702,6 +815,7 @@ extern "C" int ppo_group_norm_fwd(const ppo_group_norm_desc *d, float eps, const
     a.eps = eps;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     Plan p = plan_of(d, false);
+    p.sp.sums = static_cast<float *>(workspace);
     if (!ppo_aligned(x, 16) || !ppo_aligned(y, 16)) p.kind = Plan::ANY;
     return with_elem_act(d->dtype, d->act, [&](auto t, auto act) -> int {
         using T = decltype(t);
@@ -710,15 +824,16 @@ extern "C" int ppo_group_norm_fwd(const ppo_group_norm_desc *d, float eps, const
         const long long items = (long long)a.B * a.groups;
         if (p.kind == Plan::ANY) return ppo_launch(norm_fwd_any_kernel<T, ACT>, dim3((unsigned)items), block, 0, st, a);
         if (p.kind == Plan::SMALL) {
-            const dim3 grid(ppo_cdiv(items, kThreads / p.lanes));
+            const dim3 grid(ppo_cdiv(items, kThreads / p.lanes.width));
             if (p.nv == 1) return ppo_launch(norm_fwd_small_kernel<T, ACT, 1>, grid, block, 0, st, a, p.lanes, items);
             if (p.nv == 2) return ppo_launch(norm_fwd_small_kernel<T, ACT, 2>, grid, block, 0, st, a, p.lanes, items);
-            return ppo_launch(norm_fwd_small_kernel<T, ACT, 4>, grid, block, 0, st, a, p.lanes, items);
+            if (p.nv == 4) return ppo_launch(norm_fwd_small_kernel<T, ACT, 4>, grid, block, 0, st, a, p.lanes, items);
+            return ppo_launch(norm_fwd_small_kernel<T, ACT, 8>, grid, block, 0, st, a, p.lanes, items);
         }
-        if (p.K == 1) return launch_cluster<norm_fwd_cluster_kernel<T, ACT, 1>>(a, p.cl, st);
-        if (p.K == 2) return launch_cluster<norm_fwd_cluster_kernel<T, ACT, 2>>(a, p.cl, st);
-        if (p.K == 4) return launch_cluster<norm_fwd_cluster_kernel<T, ACT, 4>>(a, p.cl, st);
-        return launch_cluster<norm_fwd_cluster_kernel<T, ACT, N>>(a, p.cl, st);
+        if (p.K == 1) return fwd_image<T, ACT, 1>(p, a, st);
+        if (p.K == 2) return fwd_image<T, ACT, 2>(p, a, st);
+        if (p.K == 4) return fwd_image<T, ACT, 4>(p, a, st);
+        return fwd_image<T, ACT, N>(p, a, st);
     });
 }
 
@@ -745,6 +860,7 @@ extern "C" int ppo_group_norm_bwd(const ppo_group_norm_desc *d, const void *x, c
     a.part = dgamma ? static_cast<float *>(workspace) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     Plan p = plan_of(d, true);
+    if (p.kind == Plan::IMAGE && !p.whole) p.sp.sums = static_cast<float *>(workspace) + (p.floats - (size_t)p.parts * d->groups * 2);
     if (!ppo_aligned(x, 16) || !ppo_aligned(dy, 16) || !ppo_aligned(dx, 16)) {
         p.kind = Plan::ANY;
         p.parts = d->B;
@@ -755,15 +871,16 @@ extern "C" int ppo_group_norm_bwd(const ppo_group_norm_desc *d, const void *x, c
         const dim3 block(kThreads);
         if (p.kind == Plan::ANY) return ppo_launch(norm_bwd_any_kernel<T, ACT>, dim3(a.B * a.groups), block, 0, st, a);
         if (p.kind == Plan::SMALL) {
-            const dim3 grid(p.blocks, ppo_cdiv(a.groups, kThreads / p.lanes));
+            const dim3 grid(p.blocks, ppo_cdiv(a.groups, kThreads / p.lanes.width));
             if (p.nv == 1) return ppo_launch(norm_bwd_small_kernel<T, ACT, 1>, grid, block, 0, st, a, p.lanes);
             if (p.nv == 2) return ppo_launch(norm_bwd_small_kernel<T, ACT, 2>, grid, block, 0, st, a, p.lanes);
-            return ppo_launch(norm_bwd_small_kernel<T, ACT, 4>, grid, block, 0, st, a, p.lanes);
+            if (p.nv == 4) return ppo_launch(norm_bwd_small_kernel<T, ACT, 4>, grid, block, 0, st, a, p.lanes);
+            return ppo_launch(norm_bwd_small_kernel<T, ACT, 8>, grid, block, 0, st, a, p.lanes);
         }
-        if (p.K == 1) return launch_cluster<norm_bwd_cluster_kernel<T, ACT, 1>>(a, p.cl, st);
-        if (p.K == 2) return launch_cluster<norm_bwd_cluster_kernel<T, ACT, 2>>(a, p.cl, st);
-        if (p.K == 4) return launch_cluster<norm_bwd_cluster_kernel<T, ACT, 4>>(a, p.cl, st);
-        return launch_cluster<norm_bwd_cluster_kernel<T, ACT, N>>(a, p.cl, st);
+        if (p.K == 1) return bwd_image<T, ACT, 1>(p, a, st);
+        if (p.K == 2) return bwd_image<T, ACT, 2>(p, a, st);
+        if (p.K == 4) return bwd_image<T, ACT, 4>(p, a, st);
+        return bwd_image<T, ACT, N>(p, a, st);
     }));
     if (!dgamma) return PPO_OK;
     return ppo_launch(norm_sum_kernel, dim3(ppo_cdiv(d->C, 32), 2), dim3(512), 0, st, (const float *)a.part, p.parts, (int)d->C, dgamma, dbeta,

@@ -92,7 +92,8 @@ def _check_bwd(x, groups, gamma, beta, mean, rstd, dy, act, got):
 
 
 SHAPES = [(1, 1, 1, 1), (1, 1, 8, 2), (3, 1, 64, 4), (5, 1, 1024, 16), (2, 1, 96, 1), (2, 7, 6, 3), (3, 33, 24, 8), (2, 100, 64, 8), (3, 713, 96, 3),
-          (2, 1200, 64, 8), (1, 4800, 32, 4), (2, 5000, 10, 5), (1, 19200, 16, 2), (2, 3000, 256, 32), (1, 1001, 513, 27), (300, 4, 32, 32), (4097, 1, 16, 2)]
+          (2, 1200, 64, 8), (1, 4800, 32, 4), (2, 5000, 10, 5), (1, 19200, 16, 2), (2, 3000, 256, 32), (1, 1001, 513, 27), (300, 4, 32, 32), (4097, 1, 16, 2),
+          (700, 56, 24, 1), (50, 20, 240, 2), (3, 9, 512, 2), (2, 18309, 96, 4), (1, 40000, 128, 32), (40, 3000, 64, 16)]
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "silu"])
@@ -171,15 +172,17 @@ def test_nan_stays_in_its_group():
         assert bool(torch.isnan(yb[hit.expand_as(yb)]).all()) and torch.equal(yb[~hit.expand_as(yb)], y[~hit.expand_as(y)])
 
 
-def test_other_streams_and_captured_calls():
-    x, gamma, beta, dy = _inputs(4, 1200, 64, torch.bfloat16)
-    y, mean, rstd = _fwd(x, 8, gamma, beta, "relu")
-    want = _bwd(x, 8, gamma, beta, mean, rstd, dy, "relu")
+@pytest.mark.parametrize("shape", [(4, 1200, 64, 8), (2, 20000, 64, 8), (9, 1, 64, 4), (3, 50, 30, 5)])
+def test_other_streams_and_captured_calls(shape):
+    B, HW, C, groups = shape
+    x, gamma, beta, dy = _inputs(B, HW, C, torch.bfloat16)
+    y, mean, rstd = _fwd(x, groups, gamma, beta, "relu")
+    want = _bwd(x, groups, gamma, beta, mean, rstd, dy, "relu")
     out = [torch.empty_like(t) for t in (y, mean, rstd, *want)]
-    n = [ppo.ppo_group_norm_workspace_bytes(x, 8, b) for b in (False, True)]
+    n = [ppo.ppo_group_norm_workspace_bytes(x, groups, b) for b in (False, True)]
     ws = torch.empty(max(n), dtype=torch.uint8, device=DEV)
-    call = lambda: (ppo.ppo_group_norm_fwd(x, 8, gamma, beta, *out[:3], act="relu", workspace=ws),  # noqa: E731
-                    ppo.ppo_group_norm_bwd(x, 8, gamma, beta, mean, rstd, dy, *out[3:], act="relu", workspace=ws))
+    call = lambda: (ppo.ppo_group_norm_fwd(x, groups, gamma, beta, *out[:3], act="relu", workspace=ws),  # noqa: E731
+                    ppo.ppo_group_norm_bwd(x, groups, gamma, beta, mean, rstd, dy, *out[3:], act="relu", workspace=ws))
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
