@@ -45,6 +45,11 @@ struct Affine {
     float scale, shift;
 };
 
+// Out of line: its 64-bit registers are no part of the kernels' own.
+__device__ __noinline__ bool open_exactly(float x, float mean, float rstd, float gamma, float shift) {
+    return ((double)x - (double)mean) * (double)rstd * (double)gamma + (double)shift > 0.;
+}
+
 // dL/dz.  Which side of 0 z is on decides the ReLU's gradient; 32 bits decide it wrongly only where the two terms of z cancel to
 // within their own rounding (three units of the last place of the product), and there 64 bits do.
 template <int ACT>
@@ -56,14 +61,14 @@ __device__ __forceinline__ float grad_z(float dy, float xc, Affine f, float x, f
         return dy * (p * fmaf(z, 1.f - p, 1.f));
     }
     bool open = z > 0.f;
-    if (fabsf(z) <= 5e-7f * fabsf(f.shift)) open = ((double)x - (double)mean) * (double)rstd * (double)gamma + (double)f.shift > 0.;
+    if (fabsf(z) <= 5e-7f * fabsf(f.shift)) open = open_exactly(x, mean, rstd, gamma, f.shift);
     return open ? dy : 0.f;
 }
 
 // dL/dz of a vector: gated for the ReLU.  xc = x - mean, per element; the check for values next to 0 is one for all of them.
 template <int ACT, int N, int M>
 __device__ __forceinline__ void grad_vector(float (&e)[N], const float (&xc)[N], const float (&x)[N], const float (&mean)[N / M], const float (&rstd)[N / M],
-                                            const float (&gamma)[N], const float (&scale)[N], const float (&beta)[N]) {
+                                            const float *gamma, const float (&scale)[N], const float (&beta)[N]) {
     if constexpr (ACT == PPO_ACT_SILU) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -80,7 +85,7 @@ __device__ __forceinline__ void grad_vector(float (&e)[N], const float (&xc)[N],
         }
         if (near) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) e[k] = grad_z<ACT>(e[k], xc[k], {scale[k], beta[k]}, x[k], mean[k / M], rstd[k / M], gamma[k]);
+            for (int k = 0; k < N; ++k) e[k] = grad_z<ACT>(e[k], xc[k], {scale[k], beta[k]}, x[k], mean[k / M], rstd[k / M], gamma ? gamma[k] : 1.f);
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k) e[k] = z[k] > 0.f ? e[k] : 0.f;
@@ -293,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_small_kernel(NormArgs a,
             vd.get(dz);
 #pragma unroll
             for (int k = 0; k < N; ++k) xc[k] = f[k] - mean[0];
-            grad_vector<ACT, N, N>(dz, xc, f, mean, rstd, gamma, scale, beta);
+            grad_vector<ACT, N, N>(dz, xc, f, mean, rstd, a.gamma ? a.gamma + c0 : nullptr, scale, beta);
         };
         if constexpr (KEEP == NV) {
 #pragma unroll
@@ -514,7 +519,7 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_image_kernel(NormArgs a, Sp
 }
 
 template <typename T, int ACT, int K, int MODE>
-__global__ void __launch_bounds__(kThreads, 2) norm_bwd_image_kernel(NormArgs a, Split sp) {
+__global__ void __launch_bounds__(kThreads, 3) norm_bwd_image_kernel(NormArgs a, Split sp) {
     grid_wait();
     if (MODE == WHOLE) tc::cluster_arrive();
     constexpr int N = Vec<T>::N, M = N / K;
@@ -537,15 +542,14 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_image_kernel(NormArgs a,
         }
         tc::cp_async_commit();
     }
-    float mean[K], rstd[K], scale[N], gamma[N], beta[N];
+    float mean[K], rstd[K], scale[N], beta[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int c = min(vc * N + k, a.C - 1), g = K == 1 ? c / a.per : vc * K + k / M;
         mean[k / M] = a.mean[(long long)b * a.groups + g];
         rstd[k / M] = a.rstd[(long long)b * a.groups + g];
-        gamma[k] = a.gamma ? a.gamma[c] : 1.f;
         beta[k] = a.gamma ? a.beta[c] : 0.f;
-        scale[k] = rstd[k / M] * gamma[k];
+        scale[k] = a.gamma ? rstd[k / M] * a.gamma[c] : rstd[k / M];
     }
     if (MODE == WHOLE) tc::cp_async_wait<0>();
     // x - mean and dL/dz; a gated dL/dy of the ReLU is kept, in the place of dL/dy, for the second time
@@ -559,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_image_kernel(NormArgs a,
 #pragma unroll
         for (int k = 0; k < N; ++k) xc[k] = f[k] - mean[k / M];
         if (MODE == WHOLE && ACT == PPO_ACT_RELU && again) return;
-        grad_vector<ACT, N, M>(dz, xc, f, mean, rstd, gamma, scale, beta);
+        grad_vector<ACT, N, M>(dz, xc, f, mean, rstd, a.gamma ? a.gamma + vc * N : nullptr, scale, beta);
         if (MODE == WHOLE && ACT == PPO_ACT_RELU) {
             d.set(dz);
             keptd[i * kThreads + tid] = d.raw;
@@ -653,18 +657,32 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_image_kernel(NormArgs a,
     }
 }
 
-// Sums of the shares, in a fixed order: 32 channels per block, 16 warps with every 16th share each.
-__global__ void __launch_bounds__(512) norm_sum_kernel(const float *part, int parts, int C, float *dgamma, float *dbeta, int accumulate) {
+// Sums of the shares, in a fixed order: 32 channels per cluster of n blocks, 16 warps each with every 16 n-th share.
+__global__ void __launch_bounds__(512) norm_sum_kernel(const float *part, int parts, int C, float *dgamma, float *dbeta, int accumulate, int n) {
     grid_wait();
-    __shared__ double sum[16][33];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, w = threadIdx.x / 32, k = blockIdx.y;
+    if (n > 1) tc::cluster_arrive();
+    __shared__ double sum[16][33], whole[8][32];
+    const int rank = blockIdx.x % n, l = threadIdx.x % 32, c = blockIdx.x / n * 32 + l, w = threadIdx.x / 32, k = blockIdx.y;
     double s = 0;
-    if (c < C)
-        for (int i = w; i < parts; i += 16) s += part[((size_t)i * 2 + k) * C + c];
-    sum[w][threadIdx.x % 32] = s;
+    if (c < C) {
+#pragma unroll 8
+        for (int i = rank * 16 + w; i < parts; i += 16 * n) s += part[((size_t)i * 2 + k) * C + c];
+    }
+    sum[w][l] = s;
     __syncthreads();
-    if (w == 0 && c < C) {
-        for (int i = 1; i < 16; ++i) s += sum[i][threadIdx.x];
+    if (n > 1) tc::cluster_wait();
+    if (w == 0) {
+        for (int i = 1; i < 16; ++i) s += sum[i][l];
+        if (n > 1) asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(tc::in_cta(tc::smem_u32(&whole[rank][l]), 0)), "d"(s) : "memory");
+    }
+    if (n > 1) {
+        tc::cluster_sync();
+        if (rank == 0 && w == 0) {
+            s = whole[0][l];
+            for (int i = 1; i < n; ++i) s += whole[i][l];
+        }
+    }
+    if (rank == 0 && w == 0 && c < C) {
         float *out = k == 0 ? dgamma : dbeta;
         out[c] = (float)(s + (accumulate ? (double)out[c] : 0.));
     }
@@ -883,6 +901,8 @@ extern "C" int ppo_group_norm_bwd(const ppo_group_norm_desc *d, const void *x, c
         return bwd_image<T, ACT, N>(p, a, st);
     }));
     if (!dgamma) return PPO_OK;
-    return ppo_launch(norm_sum_kernel, dim3(ppo_cdiv(d->C, 32), 2), dim3(512), 0, st, (const float *)a.part, p.parts, (int)d->C, dgamma, dbeta,
-                      accumulate);
+    const int n = p.parts > 64 ? 8 : 1, cols = ppo_cdiv(d->C, 32);  // 4096 shares of 32 channels: 80 us by one block, 5 by eight
+    const auto sum = [&](auto &&launch) { return launch(dim3(cols * n, 2), dim3(512), 0, st, (const float *)a.part, p.parts, (int)d->C, dgamma, dbeta, accumulate, n); };
+    if (n == 1) return sum([&](auto... args) { return ppo_launch(norm_sum_kernel, args...); });
+    return sum([&](auto... args) { return ppo_launch_cluster(norm_sum_kernel, n, args...); });
 }

@@ -45,14 +45,6 @@ __device__ __forceinline__ RowStat merge(RowStat a, RowStat b, float c) {
     }
     return a;
 }
-// Lanes o apart, the lower one first in both.
-__device__ __forceinline__ RowStat merge_lanes(RowStat s, int o, float c) {
-    RowStat t;
-    t.top = __shfl_xor_sync(0xffffffffu, s.top, o);
-    t.sum = __shfl_xor_sync(0xffffffffu, s.sum, o);
-    t.xe = __shfl_xor_sync(0xffffffffu, s.xe, o);
-    return threadIdx.x & o ? merge(t, s, c) : merge(s, t, c);
-}
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -106,13 +98,16 @@ __device__ __forceinline__ void store_some(T *g, uint4 v, int from, int to) {
     }
 }
 
-// Elements 16 / sizeof(T) j .. of a row that starts anywhere; minus infinity behind its end.
+// Elements 16 / sizeof(T) j .. of a row that starts anywhere; minus infinity behind its end.  plain: it is aligned and has whole vectors.
 template <typename T>
-__device__ __forceinline__ Vec<T> load_row(const T *x, int vocab, int j) {
+__device__ __forceinline__ Vec<T> load_row(const T *x, int vocab, int j, bool plain) {
     constexpr int N = Vec<T>::N;
     const int s = (int)(reinterpret_cast<uintptr_t>(x) & 15), first = j * N;
     Vec<T> v;
-    if (first + N <= vocab && s == 0) {
+    if (plain) {
+        constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : std::is_same_v<T, bf16> ? 0xFF80FF80u : 0xFC00FC00u;
+        v.raw = first < vocab ? *reinterpret_cast<const uint4 *>(x + first) : make_uint4(none, none, none, none);
+    } else if (first + N <= vocab && s == 0) {
         v.raw = *reinterpret_cast<const uint4 *>(x + first);
     } else if (j > 0 && first + 2 * N <= vocab) {  // both aligned windows lie inside the row
         const uint4 *p = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(x) - s) + j;
@@ -126,8 +121,12 @@ __device__ __forceinline__ Vec<T> load_row(const T *x, int vocab, int j) {
 // Stores elements N j .. of a row that starts anywhere; the lanes of the warp hold consecutive j.  Where the row is not aligned,
 // a lane writes the aligned 16 bytes that its first elements share with the last ones of the lane in front.
 template <typename T>
-__device__ __forceinline__ void store_row(T *g, int vocab, int j, const Vec<T> &v) {
+__device__ __forceinline__ void store_row(T *g, int vocab, int j, const Vec<T> &v, bool plain) {
     constexpr int N = Vec<T>::N;
+    if (plain) {
+        if (j * N < vocab) *reinterpret_cast<uint4 *>(g + j * N) = v.raw;
+        return;
+    }
     const int s = (int)(reinterpret_cast<uintptr_t>(g) & 15), lane = threadIdx.x & 31, first = j * N;
     const bool full = first + N <= vocab;
     if (s == 0) {
@@ -184,13 +183,15 @@ template <typename T, int THREADS, int NV, bool LOSS>
 __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 ? 2 : 6) token_row_kernel(TokenArgs a, int cluster) {
     grid_wait();
     constexpr int N = Vec<T>::N, WARPS = THREADS / 32;
-    __shared__ RowStat part[WARPS], whole[8];
+    __shared__ float part[3][WARPS];
+    __shared__ RowStat whole[8];
     if (cluster > 1) tc::cluster_arrive();
     const int t = threadIdx.x % THREADS;
     const int rank = cluster > 1 ? blockIdx.x % cluster : 0;
     const int row = THREADS < 128 ? blockIdx.x * (128 / THREADS) + threadIdx.x / THREADS : blockIdx.x / cluster;
     if (row >= a.rows) return;  // a whole warp
     const T *x = static_cast<const T *>(a.logits) + (long long)row * a.ld;
+    const bool plain = a.vocab % N == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
     const int token = a.tokens[row];
     const float w = LOSS && a.weight ? a.weight[row] : 1.f;
     const bool out = token < 0 || token >= a.vocab || w == 0.f;
@@ -199,18 +200,29 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 
     Vec<T> v[NV];
     RowStat s = {-INFINITY, 0.f, 0.f};
     const float xa = out ? 0.f : to_f32(x[token]);
-    if (!out) {
-        for (int p = 0; p < pieces; ++p) {
-            RowStat r = {-INFINITY, 0.f, 0.f};
+    // The block's largest first: sums about one common value need no factors when they are joined.
+    for (int p = 0; p < pieces; ++p) {
+        RowStat r = {-INFINITY, 0.f, 0.f};
+        if (!out) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0);
+            for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0, plain);
             uint4 most = v[0].raw;
 #pragma unroll
-            for (int i = 1; i < NV; ++i) {
-                most = max_of<T>(most, v[i].raw);
-            }
+            for (int i = 1; i < NV; ++i) most = max_of<T>(most, v[i].raw);
             r.top = largest<T>(most);
-            const float top = r.top == -INFINITY ? 0.f : r.top;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
+        if constexpr (WARPS > 1) {
+            if (p > 0) __syncthreads();  // the sums of the piece before are read
+            if (t % 32 == 0) part[0][t / 32] = r.top;
+            __syncthreads();
+            r.top = part[0][0];
+#pragma unroll
+            for (int i = 1; i < WARPS; ++i) r.top = fmaxf(r.top, part[0][i]);
+        }
+        const float top = r.top == -INFINITY ? 0.f : r.top;
+        if (!out) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 float f[N];
@@ -223,20 +235,30 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 
                     r.xe = fmaf(e, fmaxf(d, -150.f), r.xe);  // e is 0 from there on
                 }
             }
-            if (r.sum != r.sum) r.top = INFINITY;  // a NaN among numbers, or alone: the row's results are NaN
-            s = p == 0 ? r : merge(s, r, c);
         }
-    }
+        r.sum = warp_sum(r.sum);
+        r.xe = warp_sum(r.xe);
+        if constexpr (WARPS > 1) {
+            if (t % 32 == 0) {
+                part[1][t / 32] = r.sum;
+                part[2][t / 32] = r.xe;
+            }
+            __syncthreads();
+            r.sum = part[1][0];
+            r.xe = part[2][0];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) s = merge_lanes(s, o, c);
+            for (int i = 1; i < WARPS; ++i) {
+                r.sum += part[1][i];
+                r.xe += part[2][i];
+            }
+        }
+        if (r.sum != r.sum) r.top = INFINITY;  // a NaN among numbers, or alone: the row's results are NaN
+        s = p == 0 ? r : merge(s, r, c);
+    }
     if constexpr (WARPS > 1) {
-        if (t % 32 == 0) part[t / 32] = s;
-        __syncthreads();
-        s = part[0];
-        for (int i = 1; i < WARPS; ++i) s = merge(s, part[i], c);
         if (cluster > 1) {
             tc::cluster_wait();  // all blocks of the cluster run
-            if (t < cluster) {  // to each block of the cluster
+            if (t < cluster) {   // to each block of the cluster
                 const uint32_t at = tc::in_cta(tc::smem_u32(&whole[rank]), t);
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(s.top) : "memory");
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(s.sum) : "memory");
@@ -258,7 +280,7 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 
         }
     } else {
         T *g = static_cast<T *>(a.grad) + (long long)row * a.ld_grad;
-        const bool skip = out || empty;
+        const bool skip = out || empty, plain_g = a.vocab % N == 0 && (reinterpret_cast<uintptr_t>(g) & 15) == 0;
         float dl = 0.f, share = 0.f, terms[5] = {};
         if (skip) {
             logp = 0.f;
@@ -290,7 +312,7 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 
         for (int p = 0; p < pieces; ++p) {
             if (pieces > 1 && !skip) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0);
+                for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0, plain);
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -315,7 +337,7 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 
                 }
                 Vec<T> r;
                 r.set(o);
-                if ((j & ~31) * N < a.vocab) store_row(g, a.vocab, j, r);  // the same in all lanes
+                if (plain_g || (j & ~31) * N < a.vocab) store_row(g, a.vocab, j, r, plain_g);  // the same in all lanes
             }
         }
     }
