@@ -212,15 +212,16 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
     }
     if (STATE && c0 == 0 && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any;
 }
-template <typename T, bool STATE>
-__global__ void __launch_bounds__(256) sweep_kernel(const __grid_constant__ Sweeps all) {
+// KMOST: rows a warp of the sweep with the most, of 8 warps; fewer leave registers for more blocks on an SM.
+template <typename T, bool STATE, int KMOST>
+__global__ void __launch_bounds__(256, KMOST == 16 ? 2 : KMOST == 12 ? 3 : 4) sweep_kernel(const __grid_constant__ Sweeps all) {
     grid_wait();
     __shared__ __align__(16) StepTiles tile;
     const Sweep &s = all.s[blockIdx.z];
     if (blockIdx.x >= (s.C + kCols - 1) / kCols * s.Be * s.heads) return;
     if (s.R <= 32) sweep_rows<T, 4, STATE>(s, tile);
-    else if (s.R <= 64) sweep_rows<T, 8, STATE>(s, tile);
-    else if (s.R <= 96) sweep_rows<T, 12, STATE>(s, tile);
+    else if (KMOST == 8 || s.R <= 64) sweep_rows<T, 8, STATE>(s, tile);
+    else if (KMOST == 12 || s.R <= 96) sweep_rows<T, 12, STATE>(s, tile);
     else sweep_rows<T, 16, STATE>(s, tile);
 }
 
@@ -1482,7 +1483,12 @@ unsigned blocks_of(const Sweeps &all, int n, int cols) {
 
 template <typename T, bool STATE>
 int sweep_launch(const Sweeps &all, int n, cudaStream_t st) {
-    return ppo_launch(sweep_kernel<T, STATE>, dim3(blocks_of(all, n, kCols), all.s[0].nseg, n), dim3(256), 0, st, all);
+    int rows = 0;
+    for (int i = 0; i < n; ++i) rows = rows > all.s[i].R ? rows : all.s[i].R;
+    const dim3 grid(blocks_of(all, n, kCols), all.s[0].nseg, n);
+    if (rows <= 64) return ppo_launch(sweep_kernel<T, STATE, 8>, grid, dim3(256), 0, st, all);
+    if (rows <= 96) return ppo_launch(sweep_kernel<T, STATE, 12>, grid, dim3(256), 0, st, all);
+    return ppo_launch(sweep_kernel<T, STATE, 16>, grid, dim3(256), 0, st, all);
 }
 template <int RB>
 int chunk_launch(const Sweeps &all, int n, cudaStream_t st) {

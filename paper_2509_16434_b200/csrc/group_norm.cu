@@ -524,7 +524,8 @@ __global__ void __launch_bounds__(kThreads, 3) norm_bwd_image_kernel(NormArgs a,
     if (MODE == WHOLE) tc::cluster_arrive();
     constexpr int N = Vec<T>::N, M = N / K;
     extern __shared__ __align__(16) float mem[];
-    float *ts = mem, *chan = ts + kThreads * 2 * N, *sent = chan + 2 * a.C, *stat = sent + (MODE == WHOLE ? (sp.n * a.groups * 2 + 3) / 4 * 4 : 0);
+    constexpr int kPitch = kThreads + 1;  // of a sum's shares: no eight of one bank
+    float *ts = mem, *chan = ts + (kPitch * 2 * N + 3) / 4 * 4, *sent = chan + 2 * a.C, *stat = sent + (MODE == WHOLE ? (sp.n * a.groups * 2 + 3) / 4 * 4 : 0);
     uint4 *keptx = reinterpret_cast<uint4 *>(stat + (a.groups * 2 + 3) / 4 * 4);
     const int rank = blockIdx.x % sp.n, b = blockIdx.x / sp.n;
     const int VC = a.C / N, lanes = kThreads / VC, tid = threadIdx.x, pl = tid / VC, vc = tid % VC;
@@ -586,8 +587,8 @@ __global__ void __launch_bounds__(kThreads, 3) norm_bwd_image_kernel(NormArgs a,
         // [2][N][threads]
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            ts[k * kThreads + tid] = s1[k];
-            ts[(N + k) * kThreads + tid] = s2[k] * rstd[k / M];
+            ts[k * kPitch + tid] = s1[k];
+            ts[(N + k) * kPitch + tid] = s2[k] * rstd[k / M];
         }
         __syncthreads();
         if (MODE == WHOLE) tc::cluster_wait();  // all blocks of the cluster run
@@ -597,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_bwd_image_kernel(NormArgs a,
             const int i = i0 + tid / sub, k2 = i / a.C, c = i % a.C;
             float s = 0.f;
             if (i < 2 * a.C)
-                for (int p = tid % sub; p < lanes; p += sub) s += ts[(k2 * N + c % N) * kThreads + p * VC + c / N];
+                for (int p = tid % sub; p < lanes; p += sub) s += ts[(k2 * N + c % N) * kPitch + p * VC + c / N];
             s = lanes_sum(s, sub);
             if (i < 2 * a.C && tid % sub == 0) {
                 chan[i] = s;
@@ -731,7 +732,7 @@ Plan plan_of(const ppo_group_norm_desc *d, bool bwd) {
         const int lanes = kThreads / VC;
         const auto smem = [&](int n, bool whole) {
             const int rounds = ppo_cdiv(ppo_cdiv(d->HW, n), lanes);
-            const size_t floats = (bwd ? kThreads * 2 * N + 2 * d->C : kThreads * p.K * 2) + (whole ? ((size_t)n * d->groups * 2 + 3) / 4 * 4 : 0) +
+            const size_t floats = (bwd ? ((kThreads + 1) * 2 * N + 3) / 4 * 4 + 2 * d->C : kThreads * p.K * 2) + (whole ? ((size_t)n * d->groups * 2 + 3) / 4 * 4 : 0) +
                                   (d->groups * 2 + 3) / 4 * 4;
             return floats * 4 + (whole ? (size_t)rounds * kThreads * 16 * (bwd ? 2 : 1) : 0);
         };
