@@ -38,11 +38,34 @@ struct Sweep {
 // decay ** n
 __device__ __forceinline__ float power(float log2_decay, int n) { return n == 0 ? 1.f : exp2f((float)n * log2_decay); }
 
+// Two 32-bit numbers in a register pair, one instruction for both.
+typedef unsigned long long pair32;
+__device__ __forceinline__ pair32 pair_of(float a, float b) {
+    pair32 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 parts(pair32 p) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+    return f;
+}
+__device__ __forceinline__ pair32 fma2(pair32 a, pair32 b, pair32 c) {
+    pair32 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ pair32 mul2(pair32 a, pair32 b) {
+    pair32 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // ---- step by step (32 bits, and rows that no vector fits) ----
 //
 // One block: 64 columns of one head's state over one segment, in registers: two columns a lane, R / 8 rows a warp.  Steps come in tiles of
 // 8; a thread fetches its share of the next tile while it works on this one.  Bound by issue: two multiply-adds for each element and
-// step, and a broadcast load of shared memory for eight of them.  For that the decay is not applied step by step: within a tile the
+// step, for two rows in one instruction, and a broadcast load of shared memory for sixteen of them.  For that the decay is not applied step by step: within a tile the
 // state is kept as N = M lambda^-e behind e steps, so that N += a b lambda^-e, and out = lambda^e x^T N; with lambda >= 1/2 that is a
 // factor of at most 2^8.  Smaller decays are applied step by step, in three operations.
 // Sweeps of one call that do not wait for one another, along z of one launch.
@@ -82,7 +105,7 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
         // what outputs are multiplied with; the last: what the state is behind a whole tile
         down[tid] = !scaled ? 1.f : power(l2, tid < kTokens ? n : kTokens);
     }
-    float M[2][KS];
+    pair32 M[2][KS / 2];  // of two columns, rows in pairs
     // this thread's element of row r of the state lies at r * sr + c * sc
     const long long sr = s.nseg > 1 ? s.seg_r : s.stride_r, sc = s.nseg > 1 ? s.seg_c : s.stride_c;
     const float *in = s.nseg > 1 ? s.seg + ((size_t)seg * s.Be * s.heads + eh) * s.R * s.C : s.m_in ? s.m_in + eh * s.state : nullptr;
@@ -90,9 +113,10 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
+        for (int i = 0; i < KS; i += 2) {
             const int r = w * KS + i, c = c0 + 32 * k + lane;
-            M[k][i] = !STATE && in && r < s.R && c < s.C ? in[r * sr + c * sc] : 0.f;
+            const bool on = !STATE && in && c < s.C;
+            M[k][i / 2] = pair_of(on && r < s.R ? in[r * sr + c * sc] : 0.f, on && r + 1 < s.R ? in[(r + 1) * sr + c * sc] : 0.f);
         }
     const int t_lo = seg * s.seg_len, t_hi = min(t_lo + s.seg_len, s.T);
     const int n0 = rev ? s.T - t_hi : t_lo, n1 = rev ? s.T - t_lo : t_hi;  // in the sweep's order
@@ -136,45 +160,39 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
             constexpr bool PLAIN = decltype(plain)::value;
             for (int t = 0; t < cnt; ++t) {
                 const float b0 = tb[t][lane], b1 = tb[t][32 + lane];
+                const pair32 b[2] = {pair_of(b0, b0), pair_of(b1, b1)};
                 const int empty = gate[t];
                 any |= empty;
                 if (rev && empty) {
 #pragma unroll
-                    for (int i = 0; i < KS; ++i) M[0][i] = M[1][i] = 0.f;
+                    for (int i = 0; i < KS / 2; ++i) M[0][i] = M[1][i] = 0;
                 }
-                float o0[2] = {}, o1[2] = {};
-                const float before = rev ? 1.f : lam;
+                pair32 o[2] = {0, 0};
+                const pair32 before = rev ? pair_of(1.f, 1.f) : pair_of(lam, lam);
 #pragma unroll
                 for (int i = 0; i < KS; i += 4) {
-                    const float4 a4 = *reinterpret_cast<const float4 *>(&ta[t][w * KS + i]);
-                    const float a[4] = {a4.x, a4.y, a4.z, a4.w};
-                    float x[4] = {};
-                    if constexpr (!STATE) {
-                        const float4 x4 = *reinterpret_cast<const float4 *>(&tx[t][w * KS + i]);
-                        x[0] = x4.x, x[1] = x4.y, x[2] = x4.z, x[3] = x4.w;
-                    }
+                    const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(&ta[t][w * KS + i]);
+                    const ulonglong2 x = STATE ? make_ulonglong2(0, 0) : *reinterpret_cast<const ulonglong2 *>(&tx[t][w * KS + i]);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        float &m0 = M[0][i + q], &m1 = M[1][i + q];
-                        m0 = PLAIN ? fmaf(before, m0, a[q] * b0) : fmaf(a[q], b0, m0);
-                        m1 = PLAIN ? fmaf(before, m1, a[q] * b1) : fmaf(a[q], b1, m1);
-                        if constexpr (!STATE) {
-                            o0[q % 2] = fmaf(x[q], m0, o0[q % 2]);
-                            o1[q % 2] = fmaf(x[q], m1, o1[q % 2]);
-                        }
+                        pair32 &m = M[q % 2][i / 2 + q / 2];
+                        const pair32 aa = q < 2 ? a.x : a.y;
+                        m = PLAIN ? fma2(before, m, mul2(aa, b[q % 2])) : fma2(aa, b[q % 2], m);
+                        if constexpr (!STATE) o[q % 2] = fma2(q < 2 ? x.x : x.y, m, o[q % 2]);
                     }
                 }
                 if (rev ? PLAIN : empty) {
-                    const float after = rev ? lam : 0.f;
+                    const pair32 after = pair_of(lam, lam);
 #pragma unroll
-                    for (int i = 0; i < KS; ++i) {
-                        M[0][i] = rev ? M[0][i] * after : 0.f;
-                        M[1][i] = rev ? M[1][i] * after : 0.f;
+                    for (int i = 0; i < KS / 2; ++i) {
+                        M[0][i] = rev ? mul2(M[0][i], after) : 0;
+                        M[1][i] = rev ? mul2(M[1][i], after) : 0;
                     }
                 }
                 if constexpr (!STATE) {
-                    part[w][t][lane] = o0[0] + o0[1];
-                    part[w][t][32 + lane] = o1[0] + o1[1];
+                    const float2 f0 = parts(o[0]), f1 = parts(o[1]);
+                    part[w][t][lane] = f0.x + f0.y;
+                    part[w][t][32 + lane] = f1.x + f1.y;
                 }
             }
         };
@@ -182,7 +200,10 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
             steps(std::false_type{});
             const float f = cnt == kTokens ? down[kTokens] : power(log2f(lam), cnt);
 #pragma unroll
-            for (int i = 0; i < KS; ++i) M[0][i] *= f, M[1][i] *= f;
+            for (int i = 0; i < KS / 2; ++i) {
+                M[0][i] = mul2(M[0][i], pair_of(f, f));
+                M[1][i] = mul2(M[1][i], pair_of(f, f));
+            }
         } else {
             steps(std::true_type{});
         }
@@ -205,9 +226,11 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
+            for (int i = 0; i < KS; i += 2) {
                 const int r = w * KS + i, c = c0 + 32 * k + lane;
-                if (r < s.R && c < s.C) out[r * sr + c * sc] = M[k][i];
+                const float2 f = parts(M[k][i / 2]);
+                if (r < s.R && c < s.C) out[r * sr + c * sc] = f.x;
+                if (r + 1 < s.R && c < s.C) out[(r + 1) * sr + c * sc] = f.y;
             }
     }
     if (STATE && c0 == 0 && tid == 0) s.seg_reset[(size_t)seg * s.Be * s.heads + eh] = any;
