@@ -478,7 +478,7 @@ int ppo_token_logp(const ppo_token_desc *desc, const void *dev_logits, const int
  * dev_logp_out [rows] (may be NULL), and writes (accumulate == 0) or adds this call's share of {L_pi = mean(-s), mean(kl),
  * mean(H), mean(old - logp), mean(r outside the clip range)}, each weighted by w, to dev_loss_out fp32 [5].
  * Rows of weight 0, rows whose token is outside [0, vocab) and rows without a finite logit are left out: they
- * contribute nothing, their gradient is 0 and their dev_logp_out 0; of the first two nothing else is read.  grad_scale: 1, or a
+ * contribute nothing, their gradient is 0 and their dev_logp_out 0; the logits of the first two are not read.  grad_scale: 1, or a
  * loss scale where 16-bit gradients (PPO_F16) would underflow.  dev_workspace: ppo_token_loss_workspace_bytes(desc) bytes.
  * Sums in a fixed order: same bits run to run. */
 typedef struct {

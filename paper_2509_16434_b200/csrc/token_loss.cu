@@ -177,6 +177,156 @@ __device__ __forceinline__ float largest(uint4 a) {
 // Keeps the compiler from holding the elements of a vector, unpacked, from one use to the next: there are registers for them packed only.
 __device__ __forceinline__ void stay_packed(uint4 &v) { asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)); }
 
+// What is said of a row besides its logits.
+struct RowSaid {
+    int token;
+    float w, old, adv, ref;
+    bool out;  // left out: nothing else of it counts
+};
+template <bool LOSS>
+__device__ __forceinline__ RowSaid said_of(const TokenArgs &a, int row) {
+    RowSaid r = {a.tokens[row], 1.f, 0.f, 0.f, 0.f, false};
+    if (LOSS) {
+        if (a.weight) r.w = a.weight[row];
+        r.old = a.old[row];
+        r.adv = a.adv[row];
+        if (a.ref) r.ref = a.ref[row];
+    }
+    r.out = r.token < 0 || r.token >= a.vocab || r.w == 0.f;
+    return r;
+}
+
+// The sums of the vectors that the WARPS warps of a row hold (thread t of them).  Their largest first: sums about one common value
+// need no factors when they are joined.
+template <typename T, int NV, int WARPS>
+__device__ __forceinline__ RowStat stat_of(Vec<T> (&v)[NV], bool out, float c, int t, float (&part)[3][WARPS]) {
+    constexpr int N = Vec<T>::N;
+    RowStat r = {-INFINITY, 0.f, 0.f};
+    if (!out) {
+        uint4 most = v[0].raw;
+#pragma unroll
+        for (int i = 1; i < NV; ++i) most = max_of<T>(most, v[i].raw);
+        r.top = largest<T>(most);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
+    if constexpr (WARPS > 1) {
+        if (t % 32 == 0) part[0][t / 32] = r.top;
+        __syncthreads();
+        r.top = part[0][0];
+#pragma unroll
+        for (int i = 1; i < WARPS; ++i) r.top = fmaxf(r.top, part[0][i]);
+    }
+    const float top = r.top == -INFINITY ? 0.f : r.top;
+    if (!out) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float f[N];
+            stay_packed(v[i].raw);
+            v[i].get(f);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float d = __fmul_rn(f[k] - top, c), e = exp2_fast(d);
+                r.sum += e;
+                r.xe = fmaf(e, fmaxf(d, -150.f), r.xe);  // e is 0 from there on
+            }
+        }
+    }
+    r.sum = warp_sum(r.sum);
+    r.xe = warp_sum(r.xe);
+    if constexpr (WARPS > 1) {
+        if (t % 32 == 0) {
+            part[1][t / 32] = r.sum;
+            part[2][t / 32] = r.xe;
+        }
+        __syncthreads();
+        r.sum = part[1][0];
+        r.xe = part[2][0];
+#pragma unroll
+        for (int i = 1; i < WARPS; ++i) {
+            r.sum += part[1][i];
+            r.xe += part[2][i];
+        }
+    }
+    if (r.sum != r.sum) r.top = INFINITY;  // a NaN among numbers, or alone: the row's results are NaN
+    return r;
+}
+
+// The gradient as e (alpha + beta d), and `hot` more at the token; skip: zeros.
+struct RowGrad {
+    float alpha, beta, hot;
+    bool skip;
+};
+// A row's results from its sums; the first thread writes the scalars.
+template <bool LOSS>
+__device__ __forceinline__ RowGrad results(const TokenArgs &a, int row, const RowSaid &r, float xa, const RowStat &s, bool first) {
+    const bool empty = s.top == -INFINITY;
+    const float log_sum = logf(s.sum);
+    float logp = r.out ? 0.f : empty ? -INFINITY : fmaf(xa - s.top, a.scale, -log_sum);
+    const float H = r.out || empty ? 0.f : fmaf(-kLn2, s.xe / s.sum, log_sum);
+    if constexpr (!LOSS) {
+        if (first) {
+            a.logp[row] = logp;
+            if (a.entropy) a.entropy[row] = H;
+        }
+        return {};
+    } else {
+        const bool skip = r.out || empty;
+        float dl = 0.f, share = 0.f, terms[5] = {};
+        if (skip) {
+            logp = 0.f;
+        } else {
+            const float ratio = expf(logp - r.old), lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
+            // NaN is kept: it shows in gradient and sums
+            const float free_ = ratio * r.adv, held = (ratio < lo ? lo : ratio > hi ? hi : ratio) * r.adv;
+            dl = free_ > held ? 0.f : -free_;
+            share = r.w * a.inv_total;
+            terms[0] = -share * (free_ > held ? held : free_);
+            if (a.ref) {
+                const float d = r.ref - logp, m = expm1f(d);
+                terms[1] = share * (m - d);
+                dl -= a.kl_coef * m;
+            }
+            terms[2] = share * H;
+            terms[3] = share * (r.old - logp);
+            terms[4] = ratio < lo || ratio > hi ? share : 0.f;
+        }
+        if (first) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) a.terms[(size_t)i * a.rows + row] = terms[i];
+            if (a.logp) a.logp[row] = logp;
+        }
+        const float f = share * a.grad_scale * a.scale, inv = f / s.sum;
+        return {inv * fmaf(a.ent_coef, H - log_sum, -dl), inv * a.ent_coef * kLn2, f * dl, skip};
+    }
+}
+// Of vector j.
+template <typename T>
+__device__ __forceinline__ Vec<T> grad_of(Vec<T> &v, int j, int token, float top, float c, const RowGrad &g) {
+    constexpr int N = Vec<T>::N;
+    float o[N];
+    if (g.skip) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[k] = 0.f;
+    } else {
+        stay_packed(v.raw);
+        v.get(o);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float d = __fmul_rn(o[k] - top, c);
+            o[k] = exp2_fast(d) * fmaf(g.beta, fmaxf(d, -150.f), g.alpha);
+        }
+        if (token / N == j) {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (token % N == k) o[k] += g.hot;
+        }
+    }
+    Vec<T> r;
+    r.set(o);
+    return r;
+}
+
 // THREADS per row and block of a cluster, NV 16-byte vectors of each in registers; rows that are longer than the cluster's
 // registers are read in pieces, and again for the gradient.
 template <typename T, int THREADS, int NV, bool LOSS>
@@ -192,67 +342,21 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 
     if (row >= a.rows) return;  // a whole warp
     const T *x = static_cast<const T *>(a.logits) + (long long)row * a.ld;
     const bool plain = a.vocab % N == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
-    const int token = a.tokens[row];
-    const float w = LOSS && a.weight ? a.weight[row] : 1.f;
-    const bool out = token < 0 || token >= a.vocab || w == 0.f;
+    const RowSaid said = said_of<LOSS>(a, row);
     const float c = a.scale * kLog2e;
     const int step = THREADS * cluster, j0 = rank * THREADS + t, pieces = (a.vocab + N * NV * step - 1) / (N * NV * step);
     Vec<T> v[NV];
     RowStat s = {-INFINITY, 0.f, 0.f};
-    const float xa = out ? 0.f : to_f32(x[token]);
-    // The block's largest first: sums about one common value need no factors when they are joined.
+    const float xa = said.out ? 0.f : to_f32(x[said.token]);
+    const auto load = [&](int p) {
+        if (said.out) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0, plain);
+    };
     for (int p = 0; p < pieces; ++p) {
-        RowStat r = {-INFINITY, 0.f, 0.f};
-        if (!out) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0, plain);
-            uint4 most = v[0].raw;
-#pragma unroll
-            for (int i = 1; i < NV; ++i) most = max_of<T>(most, v[i].raw);
-            r.top = largest<T>(most);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
-        if constexpr (WARPS > 1) {
-            if (p > 0) __syncthreads();  // the sums of the piece before are read
-            if (t % 32 == 0) part[0][t / 32] = r.top;
-            __syncthreads();
-            r.top = part[0][0];
-#pragma unroll
-            for (int i = 1; i < WARPS; ++i) r.top = fmaxf(r.top, part[0][i]);
-        }
-        const float top = r.top == -INFINITY ? 0.f : r.top;
-        if (!out) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                float f[N];
-                stay_packed(v[i].raw);
-                v[i].get(f);
-#pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    const float d = __fmul_rn(f[k] - top, c), e = exp2_fast(d);
-                    r.sum += e;
-                    r.xe = fmaf(e, fmaxf(d, -150.f), r.xe);  // e is 0 from there on
-                }
-            }
-        }
-        r.sum = warp_sum(r.sum);
-        r.xe = warp_sum(r.xe);
-        if constexpr (WARPS > 1) {
-            if (t % 32 == 0) {
-                part[1][t / 32] = r.sum;
-                part[2][t / 32] = r.xe;
-            }
-            __syncthreads();
-            r.sum = part[1][0];
-            r.xe = part[2][0];
-#pragma unroll
-            for (int i = 1; i < WARPS; ++i) {
-                r.sum += part[1][i];
-                r.xe += part[2][i];
-            }
-        }
-        if (r.sum != r.sum) r.top = INFINITY;  // a NaN among numbers, or alone: the row's results are NaN
+        load(p);
+        if (WARPS > 1 && p > 0) __syncthreads();  // the sums of the piece before are read
+        const RowStat r = stat_of<T, NV, WARPS>(v, said.out, c, t, part);
         s = p == 0 ? r : merge(s, r, c);
     }
     if constexpr (WARPS > 1) {
@@ -269,74 +373,16 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 
             for (int i = 1; i < cluster; ++i) s = merge(s, whole[i], c);
         }
     }
-    const bool empty = s.top == -INFINITY, first = t == 0 && rank == 0;
-    const float log_sum = logf(s.sum);
-    float logp = out ? 0.f : empty ? -INFINITY : fmaf(xa - s.top, a.scale, -log_sum);
-    const float H = out || empty ? 0.f : fmaf(-kLn2, s.xe / s.sum, log_sum);
-    if constexpr (!LOSS) {
-        if (first) {
-            a.logp[row] = logp;
-            if (a.entropy) a.entropy[row] = H;
-        }
-    } else {
+    const RowGrad grad = results<LOSS>(a, row, said, xa, s, t == 0 && rank == 0);
+    if constexpr (LOSS) {
         T *g = static_cast<T *>(a.grad) + (long long)row * a.ld_grad;
-        const bool skip = out || empty, plain_g = a.vocab % N == 0 && (reinterpret_cast<uintptr_t>(g) & 15) == 0;
-        float dl = 0.f, share = 0.f, terms[5] = {};
-        if (skip) {
-            logp = 0.f;
-        } else {
-            const float old = a.old[row], adv = a.adv[row], ratio = expf(logp - old);
-            const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
-            // NaN is kept: it shows in gradient and sums
-            const float free_ = ratio * adv, held = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
-            dl = free_ > held ? 0.f : -free_;
-            share = w * a.inv_total;
-            terms[0] = -share * (free_ > held ? held : free_);
-            if (a.ref) {
-                const float d = a.ref[row] - logp, m = expm1f(d);
-                terms[1] = share * (m - d);
-                dl -= a.kl_coef * m;
-            }
-            terms[2] = share * H;
-            terms[3] = share * (old - logp);
-            terms[4] = ratio < lo || ratio > hi ? share : 0.f;
-        }
-        if (first) {
-#pragma unroll
-            for (int i = 0; i < 5; ++i) a.terms[(size_t)i * a.rows + row] = terms[i];
-            if (a.logp) a.logp[row] = logp;
-        }
-        // e (alpha + beta d), and dl at the token
-        const float f = share * a.grad_scale * a.scale, inv = f / s.sum;
-        const float alpha = inv * fmaf(a.ent_coef, H - log_sum, -dl), beta = inv * a.ent_coef * kLn2, hot = f * dl;
+        const bool plain_g = a.vocab % N == 0 && (reinterpret_cast<uintptr_t>(g) & 15) == 0;
         for (int p = 0; p < pieces; ++p) {
-            if (pieces > 1 && !skip) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) v[i] = load_row(x, a.vocab, (p * NV + i) * step + j0, plain);
-            }
+            if (pieces > 1 && !grad.skip) load(p);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int j = (p * NV + i) * step + j0;
-                float o[N];
-                if (skip) {
-#pragma unroll
-                    for (int k = 0; k < N; ++k) o[k] = 0.f;
-                } else {
-                    stay_packed(v[i].raw);
-                    v[i].get(o);
-#pragma unroll
-                    for (int k = 0; k < N; ++k) {
-                        const float d = __fmul_rn(o[k] - s.top, c);
-                        o[k] = exp2_fast(d) * fmaf(beta, fmaxf(d, -150.f), alpha);
-                    }
-                    if (token / N == j) {
-#pragma unroll
-                        for (int k = 0; k < N; ++k)
-                            if (token % N == k) o[k] += hot;
-                    }
-                }
-                Vec<T> r;
-                r.set(o);
+                const Vec<T> r = grad_of(v[i], j, said.token, s.top, c, grad);
                 if (plain_g || (j & ~31) * N < a.vocab) store_row(g, a.vocab, j, r, plain_g);  // the same in all lanes
             }
         }

@@ -197,6 +197,31 @@ def test_a_nan_in_a_row_that_counts_shows(vocab, dtype):
     assert torch.isnan(grad).any(1).tolist() == [False, True, True, False] and bool(torch.isnan(loss[:4:2]).all())
 
 
+@pytest.mark.parametrize("rows,vocab,dtype", [(700, 9000, torch.bfloat16), (1500, 4104, torch.float32), (650, 32768, torch.float16), (900, 16384, torch.float32)])
+def test_many_rows_are_each_what_a_few_give(rows, vocab, dtype):
+    """Rows that go through the GPU in numbers, left-out ones among them, bit for bit as two at a time, and against 64 bits."""
+    x, tokens, old, ref, adv, weight = _inputs(rows, vocab, dtype, 11)
+    tokens[5], tokens[rows - 1] = -1, vocab
+    gs = 64.0 * rows if dtype == torch.float16 else 1.0
+    kw = dict(kl_coef=0.1, ent_coef=0.02)
+    got = _loss(x, tokens, old, adv, ref, weight, grad_scale=gs, **kw)
+    for at in (0, 4, 147, 148, 296, rows - 2):
+        few = _loss(x[at:at + 2], tokens[at:at + 2], old[at:at + 2], adv[at:at + 2], ref[at:at + 2], weight[at:at + 2], total=rows, grad_scale=gs, **kw)
+        assert torch.equal(few[0], got[0][at:at + 2]) and torch.equal(few[1], got[1][at:at + 2])
+    part = slice(0, 60)
+    _check_loss(x[part], tokens[part], old[part], adv[part], ref[part], weight[part],
+                _loss(x[part], tokens[part], old[part], adv[part], ref[part], weight[part], grad_scale=gs, **kw), grad_scale=gs, **kw)
+    logp, H = _logp(x, tokens)
+    few_logp, few_H = _logp(x[:300], tokens[:300])
+    assert torch.equal(logp[:300], few_logp) and torch.equal(H[:300], few_H)
+    counted = (weight != 0) & (tokens >= 0) & (tokens < vocab)
+    assert torch.equal(torch.where(counted, logp, torch.zeros_like(logp)), got[1])
+    same = x.clone()
+    again = _loss(same, tokens, old, adv, ref, weight, grad=same, grad_scale=gs, **kw)
+    assert all(torch.equal(a, b) for a, b in zip(again, got))
+    assert ppo.ppo_poll_status() == 0
+
+
 def test_first_epoch_and_micro_batches():
     """Where the policy is still the one that acted every ratio is 1 and no row is clipped; micro-batches add up."""
     x, tokens, _, _, adv, _ = _inputs(300, 777, torch.bfloat16, 8)
