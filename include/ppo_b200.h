@@ -386,7 +386,7 @@ int ppo_policy_act(ppo_model *m, ppo_buffer *buf, int t, const float *dev_eps, v
 /* What a policy that answers in tokens (or other discrete actions), with a memory of constant size, needs beside the network
  * above; no counterpart in the paper.  They work on bare arrays, keep nothing between calls and take any workspace from the
  * caller (its size from the query next to each, 0: none needed; the calls write what they read of it; two calls that may
- * overlap on the GPU need two).  Arrays of 16- and 32-bit elements need only the alignment of their elements, states 16
+ * overlap on the GPU need two).  Outputs overlap neither inputs nor one another, but where it says that one may be the other.  Arrays of 16- and 32-bit elements need only the alignment of their elements, states 16
  * bytes, workspaces 32.  Element types: */
 enum { PPO_F32 = 0, PPO_BF16 = 1, PPO_F16 = 2 };
 

@@ -536,6 +536,13 @@ def _device_of(where: str, t, types) -> int:
     return dev
 
 
+def _stream_on(where: str, dev: int, stream):
+    """The stream; looked up last, when everything else is known to fit: tensors of the host go no further."""
+    if dev < 0:
+        raise PpoError(1, where)
+    return _stream(stream)
+
+
 def _space(where: str, dev: int, t):
     """Address and bytes of a workspace."""
     if t is None:
@@ -580,7 +587,7 @@ def ppo_decay_attention_fwd(q, k, v, decay, o, done=None, state_in=None, state_o
     state = (Be, heads, dk, v.shape[3])
     ws, n = _space(f, dev, workspace)
     _check(lib().ppo_decay_attention_fwd(C.byref(d), pq, pk, pv, _dense(f, dev, decay, _F32, (heads,)), _dense(f, dev, done, _U8, (T, Be)),
-                                         _dense(f, dev, state_in, _F32, state), po, _dense(f, dev, state_out, _F32, state), ws, n, _stream(stream)), f)
+                                         _dense(f, dev, state_in, _F32, state), po, _dense(f, dev, state_out, _F32, state), ws, n, _stream_on(f, dev, stream)), f)
 
 
 def ppo_decay_attention_bwd(q, k, v, decay, do, dq, dk, dv, done=None, state_in=None, dstate_out=None, dstate_in=None, scale: float = 1.0,
@@ -599,7 +606,7 @@ def ppo_decay_attention_bwd(q, k, v, decay, do, dq, dk, dv, done=None, state_in=
     ws, n = _space(f, dev, workspace)
     _check(lib().ppo_decay_attention_bwd(C.byref(d), pq, pk, pv, _dense(f, dev, decay, _F32, (heads,)), _dense(f, dev, done, _U8, (T, Be)),
                                          _dense(f, dev, state_in, _F32, state), po, _dense(f, dev, dstate_out, _F32, state), *out,
-                                         _dense(f, dev, dstate_in, _F32, state), ws, n, _stream(stream)), f)
+                                         _dense(f, dev, dstate_in, _F32, state), ws, n, _stream_on(f, dev, stream)), f)
 
 
 def ppo_decay_attention_step(q, k, v, decay, state, o, start=None, scale: float = 1.0, stream=None):
@@ -609,7 +616,7 @@ def ppo_decay_attention_step(q, k, v, decay, state, o, start=None, scale: float 
     d, dev, pq, pk, pv, po = _attention(f, q, k, v, o, scale, 1)
     Be, heads, dk = q.shape
     _check(lib().ppo_decay_attention_step(C.byref(d), pq, pk, pv, _dense(f, dev, decay, _F32, (heads,)), _dense(f, dev, start, _U8, (Be,)),
-                                          _dense(f, dev, state, _F32, (Be, heads, dk, v.shape[2])), po, _stream(stream)), f)
+                                          _dense(f, dev, state, _F32, (Be, heads, dk, v.shape[2])), po, _stream_on(f, dev, stream)), f)
 
 
 def ppo_group_norm_workspace_bytes(x, groups: int, backward: bool) -> int:
@@ -639,7 +646,7 @@ def ppo_group_norm_fwd(x, groups: int, gamma, beta, y, mean, rstd, act: str = "n
     d, dev, (B, _, n), px, py = _norm(f, x, groups, y, act)
     ws, size = _space(f, dev, workspace)
     _check(lib().ppo_group_norm_fwd(C.byref(d), eps, px, _dense(f, dev, gamma, _F32, (n,)), _dense(f, dev, beta, _F32, (n,)), py,
-                                    _dense(f, dev, mean, _F32, (B, groups)), _dense(f, dev, rstd, _F32, (B, groups)), ws, size, _stream(stream)), f)
+                                    _dense(f, dev, mean, _F32, (B, groups)), _dense(f, dev, rstd, _F32, (B, groups)), ws, size, _stream_on(f, dev, stream)), f)
 
 
 def ppo_group_norm_bwd(x, groups: int, gamma, beta, mean, rstd, dy, dx, dgamma=None, dbeta=None, act: str = "none", accumulate: bool = False,
@@ -654,7 +661,7 @@ def ppo_group_norm_bwd(x, groups: int, gamma, beta, mean, rstd, dy, dx, dgamma=N
     ws, size = _space(f, dev, workspace)
     _check(lib().ppo_group_norm_bwd(C.byref(d), px, _dense(f, dev, gamma, _F32, (n,)), _dense(f, dev, beta, _F32, (n,)),
                                     _dense(f, dev, mean, _F32, (B, groups)), _dense(f, dev, rstd, _F32, (B, groups)), py, pd,
-                                    _dense(f, dev, dgamma, _F32, (n,)), _dense(f, dev, dbeta, _F32, (n,)), int(accumulate), ws, size, _stream(stream)), f)
+                                    _dense(f, dev, dgamma, _F32, (n,)), _dense(f, dev, dbeta, _F32, (n,)), int(accumulate), ws, size, _stream_on(f, dev, stream)), f)
 
 
 def _token(where: str, logits, scale: float):
@@ -672,7 +679,7 @@ def ppo_token_logp(logits, tokens, logp, entropy=None, scale: float = 1.0, strea
     f = "ppo_token_logp"
     d, dev, row, p = _token(f, logits, scale)
     _check(lib().ppo_token_logp(C.byref(d), p, _dense(f, dev, tokens, _I32, row), _dense(f, dev, logp, _F32, row), _dense(f, dev, entropy, _F32, row),
-                                _stream(stream)), f)
+                                _stream_on(f, dev, stream)), f)
 
 
 def ppo_token_loss_workspace_bytes(logits) -> int:
@@ -694,4 +701,4 @@ def ppo_token_loss_fwd_bwd(logits, tokens, logp_old, adv, B_total: int, dlogits,
     _check(lib().ppo_token_loss_fwd_bwd(C.byref(d), C.byref(c), p, _dense(f, dev, tokens, _I32, row), _dense(f, dev, logp_old, _F32, row),
                                         _dense(f, dev, logp_ref, _F32, row), _dense(f, dev, adv, _F32, row), _dense(f, dev, weight, _F32, row), pg, ldg,
                                         _dense(f, dev, logp_out, _F32, row), _dense(f, dev, loss_out, _F32, (5,)), int(accumulate), ws, size,
-                                        _stream(stream)), f)
+                                        _stream_on(f, dev, stream)), f)

@@ -223,3 +223,13 @@ def test_the_binding_refuses_tensors_that_no_descriptor_says():
     assert status(ppo.ppo_token_logp, logits, torch.zeros(4, dtype=torch.int64), torch.zeros(4)) == 1
     assert status(ppo.ppo_token_logp, logits.t(), torch.zeros(10, dtype=torch.int32), torch.zeros(10)) == 2
     assert status(ppo.ppo_token_logp, logits, torch.zeros(4, dtype=torch.int32), torch.zeros(3)) == 2
+    # all of it fits, but it is not on a GPU
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    assert status(f, q, k, v, decay, o) == 1
+    assert status(ppo.ppo_decay_attention_bwd, q, k, v, decay, o, q.clone(), k.clone(), v.clone(), workspace=ws) == 1
+    assert status(ppo.ppo_decay_attention_step, q[0], k[0], v[0], decay, torch.zeros(2, 4, 16, 24), o[0]) == 1
+    assert status(ppo.ppo_group_norm_fwd, x, 3, None, None, x.clone(), torch.zeros(2, 3), torch.zeros(2, 3)) == 1
+    assert status(ppo.ppo_group_norm_bwd, x, 3, None, None, torch.zeros(2, 3), torch.zeros(2, 3), x.clone(), x.clone()) == 1
+    four = torch.zeros(4)
+    assert status(ppo.ppo_token_logp, logits, torch.zeros(4, dtype=torch.int32), four) == 1
+    assert status(ppo.ppo_token_loss_fwd_bwd, logits, torch.zeros(4, dtype=torch.int32), four, four, 4, logits.clone(), torch.zeros(5), workspace=ws) == 1
