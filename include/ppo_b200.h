@@ -386,8 +386,10 @@ int ppo_policy_act(ppo_model *m, ppo_buffer *buf, int t, const float *dev_eps, v
 /* What a policy that answers in tokens (or other discrete actions), with a memory of constant size, needs beside the network
  * above; no counterpart in the paper.  They work on bare arrays, keep nothing between calls and take any workspace from the
  * caller (its size from the query next to each, 0: none needed; the calls write what they read of it; two calls that may
- * overlap on the GPU need two).  Outputs overlap neither inputs nor one another, but where it says that one may be the other.  Arrays of 16- and 32-bit elements need only the alignment of their elements, states 16
- * bytes, workspaces 32.  Element types: */
+ * overlap on the GPU need two).  Outputs overlap neither inputs nor one another, but where it says that one may be the other.
+ * Arrays of 16- and 32-bit elements need only the alignment of their elements, states 16 bytes, workspaces 32.  An infinity or a
+ * NaN among the inputs shows in what the formulas make of it, where an infinity may come out as a NaN, and nowhere else.
+ * Element types: */
 enum { PPO_F32 = 0, PPO_BF16 = 1, PPO_F16 = 2 };
 
 /* Linear attention with a decay for each head, over a sequence minibatch as ppo_shuffle_gather_sequences leaves it: T time
@@ -399,7 +401,7 @@ enum { PPO_F32 = 0, PPO_BF16 = 1, PPO_F16 = 2 };
  *   PPO_BF16); ldq, ldk, ldv, ldo: elements from one row to the next, so that a row may be part of a wider one (at least
  *   the row's own length); decay fp32 [heads], in [0, 1], a constant of the call as gamma and lambda are of ppo_compute_gae;
  *   done uint8 [T][Be] (NULL: no flag is set); states fp32 [Be][heads][dk][dv] (in NULL: zeros; out NULL: not wanted).
- * Sums and states are held in fp32.  1 <= dk, dv <= 128. */
+ * Sums and states are held in fp32.  1 <= dk, dv <= 128; T * Be up to 0x7f000000 (else UNSUPPORTED). */
 typedef struct {
     int32_t T, Be, heads, kv_heads, dk, dv, dtype;
     int64_t ldq, ldk, ldv, ldo;
@@ -455,7 +457,7 @@ int ppo_group_norm_bwd(const ppo_group_norm_desc *desc, const void *dev_x, const
 
 /* Log-probability of each row's token and entropy of each row's distribution, with x = scale * logits:
  *   logp = x_a - log sum_j exp(x_j),   H = -sum_j p_j log p_j.
- * logits [rows][vocab] of type dtype, ld elements from one row to the next (>= vocab); dev_tokens int32 [rows]; dev_logp,
+ * 0 < scale <= 1e38; logits [rows][vocab] of type dtype, ld elements from one row to the next (>= vocab); dev_tokens int32 [rows]; dev_logp,
  * dev_entropy fp32 [rows] (the latter may be NULL).  A logit of minus infinity is a token that cannot occur: p = 0, nothing to the
  * entropy.  A row whose token is outside [0, vocab) is left out (not read; logp = entropy = 0); a row all of whose logits are
  * minus infinity has logp = minus infinity and entropy 0. */

@@ -1463,7 +1463,7 @@ int check(const ppo_decay_attention_desc *d) {
     if (!(d->scale > -3.0e38f && d->scale < 3.0e38f)) return PPO_ERR_INVALID_ARG;
     if (d->heads % d->kv_heads != 0) return PPO_ERR_SHAPE;
     if (d->dk > 128 || d->dv > 128) return PPO_ERR_UNSUPPORTED;
-    if ((long long)d->T * d->Be > 0x7fffffffll || (long long)d->Be * d->heads > 0x1fffffffll) return PPO_ERR_UNSUPPORTED;
+    if ((long long)d->T * d->Be > 0x7f000000ll || (long long)d->Be * d->heads > 0x1fffffffll) return PPO_ERR_UNSUPPORTED;
     if (d->ldq < (int64_t)d->heads * d->dk || d->ldk < (int64_t)d->kv_heads * d->dk || d->ldv < (int64_t)d->kv_heads * d->dv ||
         d->ldo < (int64_t)d->heads * d->dv)
         return PPO_ERR_SHAPE;

@@ -721,6 +721,10 @@ Plan plan_of(const ppo_group_norm_desc *d, bool bwd) {
         p.lanes = {width, active};
         p.nv = all <= active ? 1 : all <= 2 * active ? 2 : all <= 4 * active ? 4 : 8;
         const int columns = ppo_cdiv(d->groups, kThreads / width);
+        if (bwd && columns > 65535) {  // more than a grid has along y
+            p.kind = Plan::ANY;
+            return p;
+        }
         p.blocks = ppo_cdiv(4 * 148, columns);
         if (p.blocks > d->B) p.blocks = d->B;
         p.parts = p.blocks;

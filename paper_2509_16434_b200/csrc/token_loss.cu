@@ -377,6 +377,7 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 512 
     if constexpr (LOSS) {
         T *g = static_cast<T *>(a.grad) + (long long)row * a.ld_grad;
         const bool plain_g = a.vocab % N == 0 && (reinterpret_cast<uintptr_t>(g) & 15) == 0;
+        __syncwarp();  // in place: all lanes have read their logits, and the token's
         for (int p = 0; p < pieces; ++p) {
             if (pieces > 1 && !grad.skip) load(p);
 #pragma unroll
@@ -417,7 +418,7 @@ int launch_rows(const TokenArgs &a, cudaStream_t st) {
 }
 
 int check(const ppo_token_desc *d) {
-    if (!d || d->rows <= 0 || d->vocab <= 0 || !(d->scale > 0.f) || d->scale > 3.0e38f) return PPO_ERR_INVALID_ARG;
+    if (!d || d->rows <= 0 || d->vocab <= 0 || !(d->scale > 0.f) || d->scale > 1.0e38f) return PPO_ERR_INVALID_ARG;
     if (d->dtype < PPO_F32 || d->dtype > PPO_F16) return PPO_ERR_INVALID_ARG;
     if (d->ld < d->vocab) return PPO_ERR_SHAPE;
     if (d->rows > 0x7fffffff / 8 || d->vocab > 0x7fffffff / 2) return PPO_ERR_UNSUPPORTED;

@@ -199,3 +199,12 @@ def test_other_streams_and_captured_calls(shape):
         g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(out, (y, mean, rstd, *want)))
+
+
+def test_more_groups_than_a_grid_has_rows():
+    # 17 pixels of one vector: a warp each, eight a block, more than 65535 blocks
+    B, HW, C, groups = 1, 17, 8 * 524289, 524289
+    x, gamma, beta, dy = _inputs(B, HW, C, torch.bfloat16, seed=8)
+    y, mean, rstd = _fwd(x, groups, gamma, beta, "relu")
+    _check_fwd(x, groups, gamma, beta, "relu", (y, mean, rstd))
+    _check_bwd(x, groups, gamma, beta, mean, rstd, dy, "relu", _bwd(x, groups, gamma, beta, mean, rstd, dy, "relu"))

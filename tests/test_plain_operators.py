@@ -199,6 +199,11 @@ def test_token_arguments_are_refused():
     assert need > 0 and _token_loss(d, c, ws=None, n=need) == 1 and _token_loss(d, c, n=need - 1) == 2
 
 
+def test_sizes_and_scales_beyond_the_arithmetic_are_refused():
+    assert _logp(_token(scale=2.0e38)) == 1  # times log2(e) it is no 32-bit number
+    assert _step(_attention(T=0x7F000001, Be=1)) == 7  # steps are counted in 32 bits, in whole tiles
+
+
 def test_the_binding_refuses_tensors_that_no_descriptor_says():
     def status(fn, *a, **k):
         with pytest.raises(ppo.PpoError) as e:
