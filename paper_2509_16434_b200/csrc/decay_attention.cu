@@ -777,12 +777,17 @@ template <int RB, int CB, bool STATE, int TERMS>
 struct TileSmem {
     static constexpr int kPanel = 128 * 128;  // bytes: 128 rows of 64 bf16 numbers
     // P takes the place of X, and where that is one panel, of A behind it.  With 128 rows there is room for X of the next chunk
-    // (with three terms there is not), and A's place is free once it is split.
-    static constexpr bool kAhead = RB == 128 && TERMS == 2 && !STATE;
+    // (with three terms there is not), and A's place is free once it is split.  With 64 X and A change places with the first two terms
+    // from chunk to chunk: these are free once K is made, long before the outputs have left P's place (gradients 2048 x 4 x 16 x 64: 154 -> 137 us, with
+    // 16 columns of the accumulators at a time).
+    static constexpr bool kAhead = RB == 128 && TERMS == 2 && !STATE, kTurns = RB == 64 && !STATE;
+    __device__ static int x_at(int i) { return kAhead ? kX + i % 2 * kWide : kTurns && i % 2 ? kSplit : kX; }
+    __device__ static int a_at(int i) { return kTurns ? x_at(i) + kPanel : kA; }
+    __device__ static int split_at(int i, int panel) { return kTurns && i % 2 && panel < 2 ? kX + panel * kPanel : kSplit + panel * kPanel; }
     static constexpr int kWide = RB / 64 * kPanel, kX = 0, kA = kX + (STATE ? 0 : (kAhead ? 2 : 1) * kWide), kB = kA + kWide, kM = kB + CB / 64 * kPanel,
                          kSplit = kM + (STATE ? 0 : CB / 64 * kPanel), kSplitBytes = RB == 128 ? TERMS * 2 * kPanel : TERMS * kPanel,
                          kEnd = kSplit + kSplitBytes;
-    static constexpr int kTables = 1664, kBytes = kEnd + kTables + 1024;  // with the alignment
+    static constexpr int kTables = 1680, kBytes = kEnd + kTables + 1024;  // with the alignment
     static constexpr uint32_t kCols = STATE ? CB : 128 + 2 * CB > 256 ? 512 : 256;  // of tensor memory
     static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
@@ -791,11 +796,12 @@ struct TileTables {
     float pow[132];     // lambda^n
     uint64_t got_a, got_b, bar[3];    // X and A, B have landed; S and O1, K, O2 are made
     uint64_t split, weighted, emptied;  // of the workers' warps: A is split; P is there; accumulators are read, M and outputs in place
+    uint64_t left;                      // outputs have left shared memory (kTurns)
     uint32_t flags[2][4];  // done at the steps of a chunk, a bit each
     int abort_flag, bad;
     uint32_t slot;
 };
-static_assert(sizeof(TileTables) <= 1664, "place of the tables");
+static_assert(sizeof(TileTables) <= 1680, "place of the tables");
 
 // w a for eight bf16 numbers a, as sums of bf16 numbers.  With w = w0 + w1 + w2, 8 bits each, hi = a w0 to the nearest and a w0 - hi are
 // bf16 numbers that hold a w0 entirely (16 bits), in two packed operations a pair; four terms are exact to 2^-26, two to 2^-17.
@@ -901,7 +907,7 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
     using L = TileSmem<RB, CB, STATE, TERMS>;
     constexpr int WG = (tile_threads(RB, CB, STATE) - 32) / 128, WORKERS = 128 * WG;  // warps 0 ..; column groups
     constexpr int H = CB / WG, PC = 128 / WG;            // columns of a thread: of the state and the outputs, of S and P
-    constexpr int G = H < 32 ? 16 : WG == 4 ? 16 : 32;   // at a time
+    constexpr int G = STATE && H >= 32 ? 32 : 16;        // at a time: with outputs there are registers for 16 of two accumulators
     constexpr int kO1 = 128, kK = STATE ? 0 : 128 + CB;  // columns of tensor memory: S and O2 from 0
     constexpr int SETS = RB == 128 ? TERMS : TERMS / 2;
     static_assert(RB == 128 || TERMS != 3, "two terms side by side");
@@ -919,6 +925,7 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
             tc::mbar_init(&tab->split, 4 * WG);
             tc::mbar_init(&tab->weighted, 4 * WG);
             tc::mbar_init(&tab->emptied, 4 * WG);
+            tc::mbar_init(&tab->left, 1);
             tab->abort_flag = tab->bad = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -946,8 +953,8 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
         const auto load = [&](int to, const CUtensorMap *map, int width, int head, int t, uint64_t *bar) {
             for (int p = 0; p < width / 64; ++p) tc::tma_load_4d(base + to + p * L::kPanel, map, bar, 64 * p, head, e, t);
         };
-        const auto load_x = [&](int i) { load(L::kX + (L::kAhead ? i % 2 * L::kWide : 0), &maps.x, RB, h / s.share_x, start_of(i), &tab->got_a); };
-        const auto load_a = [&](int i) { load(L::kA, &maps.a, RB, h / s.share_a, start_of(i), &tab->got_a); };
+        const auto load_x = [&](int i) { load(L::x_at(i), &maps.x, RB, h / s.share_x, start_of(i), &tab->got_a); };
+        const auto load_a = [&](int i) { load(L::a_at(i), &maps.a, RB, h / s.share_a, start_of(i), &tab->got_a); };
         const auto load_b = [&](int i) { load(L::kB, &maps.b, CB, h / s.share_b, start_of(i), &tab->got_b); };
         // done at the steps of the i-th chunk, for the workers; in front of the arrival that they wait for
         const auto flags_of = [&](int i) {
@@ -989,14 +996,14 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
         bool filled = in != nullptr;
         for (int i = 0; i < chunks; ++i) {
             const bool more = i + 1 < chunks, update = more || out_state;
-            const int x = L::kX + (L::kAhead ? i % 2 * L::kWide : 0);
+            const int x = L::x_at(i), at_a = L::a_at(i);
             if (!STATE) {
                 wait(&tab->got_a, i);
                 tc::tc_fence_after();
                 if (tc::elect_one()) {
 #pragma unroll
                     for (int k = 0; k < RB / 16; ++k)
-                        tc::umma_bf16_lh(tmem, along(x + k / 4 * L::kPanel, k % 4), k_hi, along(L::kA + k / 4 * L::kPanel, k % 4), k_hi,
+                        tc::umma_bf16_lh(tmem, along(x + k / 4 * L::kPanel, k % 4), k_hi, along(at_a + k / 4 * L::kPanel, k % 4), k_hi,
                                          tc::instr_desc(128, 128, 0, 0), k > 0);
                     if (filled) {
 #pragma unroll
@@ -1025,11 +1032,20 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                     for (int t = SETS - 1; t >= 0; --t)
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
-                            tc::umma_bf16_lh(tmem + kK, down(L::kSplit + 2 * t * L::kPanel, k), m_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 1, 1),
+                            tc::umma_bf16_lh(tmem + kK, down(L::split_at(i, 2 * t), k), m_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 1, 1),
                                              t < SETS - 1 || k > 0);
                     tc::umma_commit(&tab->bar[1]);
                 }
                 __syncwarp();
+                if (L::kTurns && more) {
+                    wait(&tab->bar[1], i);  // K is made
+                    if (tc::elect_one()) {
+                        expect_a();
+                        load_x(i + 1);
+                        load_a(i + 1);
+                    }
+                    __syncwarp();
+                }
             }
             if (STATE && more && tc::elect_one()) {
                 expect_a();
@@ -1046,10 +1062,9 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                 if (!update) wait(&tab->got_b, i);
                 tc::tc_fence_after();
                 if (tc::elect_one()) {
-                    const int p1 = RB == 128 ? x + L::kPanel : L::kA;
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        tc::umma_bf16_lh(tmem, along(k < 4 ? x : p1, k % 4), k_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 0, 1), k > 0);
+                        tc::umma_bf16_lh(tmem, along(x + k / 4 * L::kPanel, k % 4), k_hi, down(L::kB, k), m_hi, tc::instr_desc(128, CB, 0, 1), k > 0);
                     tc::umma_commit(&tab->bar[2]);
                 }
                 __syncwarp();
@@ -1067,10 +1082,13 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
             if (!STATE && tc::elect_one()) {
                 if (!s.shared) {
                     for (int p = 0; p < CB / 64; ++p)
-                        if (64 * p < s.C) tc::tma_store_4d(&maps.out, base + (p == 0 ? x : RB == 128 ? x + L::kPanel : L::kA), 64 * p, h, e, start_of(i));
+                        if (64 * p < s.C) tc::tma_store_4d(&maps.out, base + x + p * L::kPanel, 64 * p, h, e, start_of(i));
                     tc::bulk_commit();
                 }
-                if (!L::kAhead && more) {
+                if (L::kTurns) {
+                    tc::bulk_wait_read<0>();
+                    tc::mbar_arrive(&tab->left);
+                } else if (!L::kAhead && more) {
                     tc::bulk_wait_read<0>();
                     expect_a();
                     load_x(i + 1);
@@ -1133,7 +1151,7 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
         for (int i = 0; i < chunks; ++i) {
             const int n = min(128, t_hi - start_of(i));
             const bool more = i + 1 < chunks, update = more || out_state;
-            const int x = L::kX + (L::kAhead ? i % 2 * L::kWide : 0);
+            const int x = L::x_at(i), at_a = L::a_at(i);
             wait(&tab->got_a, i);
             uint32_t resets[4];
 #pragma unroll
@@ -1146,6 +1164,7 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                 if (!rev && resets[k]) edge = 32 * k + 31 - __clz(resets[k]);
                 if (rev && resets[3 - k]) edge = 32 * (3 - k) + __ffs(resets[3 - k]) - 1;
             }
+            if (L::kTurns && i > 0) wait(&tab->left, i - 1);  // the split terms' place
             if (update) {
                 // w_c a_c in TERMS terms
                 constexpr int V = RB / 8;
@@ -1154,13 +1173,13 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                     const int c = (k * WORKERS + tid) / V, v = (k * WORKERS + tid) % V;
                     const bool sees = c < n && (rev ? c <= edge : c > edge);
                     const float wj = sees ? tab->pow[max(rev ? c + 1 : n - 1 - c, 0)] * s.a_scale : 0.f;
-                    const uint4 a = *reinterpret_cast<const uint4 *>(piece(L::kA + v / 8 * L::kPanel, c, v));
+                    const uint4 a = *reinterpret_cast<const uint4 *>(piece(at_a + v / 8 * L::kPanel, c, v));
                     const uint32_t in4[4] = {sees ? a.x : 0u, sees ? a.y : 0u, sees ? a.z : 0u, sees ? a.w : 0u};
                     uint32_t part[TERMS][4];
                     split_products<TERMS>(in4, wj, part);
 #pragma unroll
                     for (int t = 0; t < TERMS; ++t)
-                        *reinterpret_cast<uint4 *>(piece(L::kSplit + (RB == 128 ? 2 * t + v / 8 : t) * L::kPanel, c, v)) =
+                        *reinterpret_cast<uint4 *>(piece(L::split_at(i, RB == 128 ? 2 * t + v / 8 : t), c, v)) =
                             make_uint4(part[t][0], part[t][1], part[t][2], part[t][3]);
                 }
                 tc::fence_async_smem();
@@ -1195,11 +1214,11 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                 wait(&tab->bar[0], i);
                 if (RB == 64 && PC * wc >= 64) wait(&tab->split, i);  // the other warps have read A, whose place the second half takes
                 tc::tc_fence_after();
-                // P: row `row`, 32 columns at a time, from PC wc on
-#pragma unroll
+                // P: row `row`, 32 columns at a time, from PC wc on, one after the other (two side by side do not fit the registers)
+#pragma unroll 1
                 for (int b0 = 0; b0 < PC; b0 += 32) {
                     const int col = PC * wc + b0;
-                    const int panel = col < 64 ? x : RB == 128 ? x + L::kPanel : L::kA, v0 = col % 64 / 8;
+                    const int panel = x + col / 64 * L::kPanel, v0 = col % 64 / 8;
                     if (rev ? col < 32 * lq : col > 32 * lq) {  // nothing of it is seen, whatever it holds
 #pragma unroll
                         for (int v = 0; v < 4; ++v) *reinterpret_cast<uint4 *>(piece(panel, row, v0 + v)) = make_uint4(0, 0, 0, 0);
@@ -1238,7 +1257,10 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                     float f[G];
                     tmem_get<G>(mine + kK + wc * H + c0, f);
 #pragma unroll
-                    for (int c = 0; c < G; ++c) M[c0 + c] = some ? f[c] : fmaf(M[c0 + c], keep, f[c]);
+                    for (int c = 0; c < G; c += 2) {
+                        const float2 p = some ? make_float2(f[c], f[c + 1]) : parts(fma2(pair_of(M[c0 + c], M[c0 + c + 1]), pair_of(keep, keep), pair_of(f[c], f[c + 1])));
+                        M[c0 + c] = p.x, M[c0 + c + 1] = p.y;
+                    }
                 }
                 if (!STATE && more) store_m();
             }
@@ -1256,11 +1278,17 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                         tmem_get<G>(mine + kO1 + wc * H + c0, m);
                         if (reached) {
 #pragma unroll
-                            for (int c = 0; c < G; ++c) o[c] = fmaf(m[c], f1, o[c]);
+                            for (int c = 0; c < G; c += 2) {
+                                const float2 p = parts(fma2(pair_of(m[c], m[c + 1]), pair_of(f1, f1), pair_of(o[c], o[c + 1])));
+                                o[c] = p.x, o[c + 1] = p.y;
+                            }
                         }
                     }
 #pragma unroll
-                    for (int c = 0; c < G; ++c) o[c] *= s.out_scale;
+                    for (int c = 0; c < G; c += 2) {
+                        const float2 p = parts(mul2(pair_of(o[c], o[c + 1]), pair_of(s.out_scale, s.out_scale)));
+                        o[c] = p.x, o[c + 1] = p.y;
+                    }
                     if (s.shared) {
                         float *to = s.shared + (at * s.heads + h) * s.C + wc * H + c0;
                         if (row < n) {
@@ -1272,7 +1300,7 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
 #pragma unroll
                         for (int c = 0; c < G; c += 8) {
                             const int v = (wc * H + c0 + c) / 8;
-                            *reinterpret_cast<uint4 *>(piece(v < 8 ? x : RB == 128 ? x + L::kPanel : L::kA, row, v)) =
+                            *reinterpret_cast<uint4 *>(piece(x + v / 8 * L::kPanel, row, v)) =
                                 make_uint4(pack_bf16x2(o[c], o[c + 1]), pack_bf16x2(o[c + 2], o[c + 3]), pack_bf16x2(o[c + 4], o[c + 5]), pack_bf16x2(o[c + 6], o[c + 7]));
                         }
                     }
@@ -1288,7 +1316,7 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
         asm volatile("bar.sync 4, %0;" ::"n"(WORKERS) : "memory");
         if (out_state && !tab->bad) {
             if (RB == 64) {  // the two shares of a row
-                float *y = reinterpret_cast<float *>(smem + L::kSplit);
+                float *y = reinterpret_cast<float *>(smem + L::split_at(chunks - 1, 0));
                 if (row >= 64) {
 #pragma unroll
                     for (int c = 0; c < H; ++c) y[(wc * H + c) * 64 + row - 64] = M[c];

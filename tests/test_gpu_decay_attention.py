@@ -135,6 +135,23 @@ def test_many_blocks_of_many_chunks(shape, dtype):
     assert ppo.ppo_poll_status() == 0
 
 
+@pytest.mark.parametrize("shape", [(500, 40, 8, 8, 64, 64, 0.004), (400, 38, 8, 4, 48, 128, 0.004), (330, 20, 16, 16, 128, 64, 0.0)], ids=lambda s: "-".join(map(str, s)))
+def test_states_of_many_heads_over_several_chunks(shape):
+    """Heads enough that no sequence is cut: the state that is left is built in the pass that writes the outputs."""
+    c = Case(*shape[:6], BF16, shape[6])
+    assert ppo.ppo_decay_attention_workspace_bytes(c.q, c.k, c.v, False) == 0
+    (o, s), (ow, sw), (oa, sa) = c.fwd(), plain.attention(*c.args()), plain.attention_abs(*c.args())
+    _near(o, ow, oa, c.T, c.dk, BF16)
+    _near(s, sw, sa, c.T, c.dk, F32)
+    got, again = c.bwd(), c.bwd()
+    want, size = (f(*c.args(), c.do, c.ds) for f in (plain.attention, plain.attention_abs))
+    for i in range(3):
+        _near(got[i], want[i], size[i], c.T, max(c.dk, c.dv) * (c.heads // c.kv), BF16)
+    _near(got[3], want[3], size[3], c.T, c.dk, F32)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+    assert ppo.ppo_poll_status() == 0
+
+
 @pytest.mark.parametrize("offset", [0, 8, 3])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_that_are_parts_of_wider_ones(dtype, offset):
