@@ -64,10 +64,12 @@ __device__ __forceinline__ pair32 mul2(pair32 a, pair32 b) {
 // ---- step by step (32 bits, and rows that no vector fits) ----
 //
 // One block: 64 columns of one head's state over one segment, in registers: two columns a lane, R / 8 rows a warp.  Steps come in tiles of
-// 8; a thread fetches its share of the next tile while it works on this one.  Bound by issue: two multiply-adds for each element and
-// step, for two rows in one instruction, and a broadcast load of shared memory for sixteen of them.  For that the decay is not applied step by step: within a tile the
-// state is kept as N = M lambda^-e behind e steps, so that N += a b lambda^-e, and out = lambda^e x^T N; with lambda >= 1/2 that is a
-// factor of at most 2^8.  Smaller decays are applied step by step, in three operations.
+// 8; a thread fetches its share of the next tile while it works on this one.  Two multiply-adds for each element and step, for two
+// rows in one instruction, and a broadcast load of shared memory for sixteen of them: bound by issue and by the chain from step to
+// step (gradients of 119 steps of 37 x 6 heads of 48 x 80, fp32: 123 us; one row an instruction 138, one column a lane 183 of two
+// launches).  For that the decay is not applied step by step: within a tile the state is kept as N = M lambda^-e behind e steps, so that
+// N += a b lambda^-e, and out = lambda^e x^T N; with lambda >= 1/2 that is a factor of at most 2^8.  Smaller decays are applied step
+// by step, in three operations.  Products of 32-bit numbers have no tensor core instruction without a rounding to 11 bits.
 // Sweeps of one call that do not wait for one another, along z of one launch.
 struct Sweeps {
     Sweep s[3];
@@ -248,18 +250,17 @@ __global__ void __launch_bounds__(256, KMOST == 16 ? 2 : KMOST == 12 ? 3 : 4) sw
     else sweep_rows<T, 16, STATE>(s, tile);
 }
 
-// ---- chunks of 64 steps on the tensor cores (bf16) ----
+// ---- one chunk of up to 64 steps on the tensor cores (bf16) ----
 //
 // Within a chunk of n steps, with i and j counted from its first one, w_ij = lambda^(i-j) and M the state in front of it,
 //   out_i = sum_{j <= i} w_ij (x_i . a_j) b_j + lambda^(i+1) x_i^T M,    M <- lambda^n M + sum_j lambda^(n-1-j) a_j b_j^T
 // (backwards one power less in the second and one more in the last term); terms with a reset between j and i, or between M and
 // i, fall away.  Four products of 64-row tiles; the state stays in registers in 32 bits, 64 of its columns per block.
-// Rounded to bf16: the weights w_ij (x_i . a_j), and the state where x reads it, whose errors of half a step, 2^-9 relative on
-// average less, stay next to that of the output itself.  lambda^.. a_j is not: as one bf16 number it would leave 2^-9 in a state
-// that is handed out in 32 bits; three terms that sum up to 24 bits are exact to 2^-25, and two (2^-17) do where only outputs of
-// bf16 come of it.
-// A product has no masked places: 0 times a NaN of a later step would reach an earlier one, or stay behind a reset.  So chunks that
-// hold an infinity or a NaN are taken step by step, each as a chunk of its own.
+// Rounded to bf16: the weights w_ij (x_i . a_j), and the state where x reads it; half a step each, next to that of the output
+// itself.  lambda^.. a_j is not: as one bf16 number it would leave 2^-8 in a state that is handed out in 32 bits; three terms that
+// sum up to 24 bits are exact to 2^-25 (in the kernel for many chunks two, 2^-17, where only outputs of bf16 come of it).
+// A product has no masked places: 0 times a NaN of a later step would reach an earlier one, or stay behind a reset.  So a chunk that
+// holds an infinity or a NaN is taken step by step, each as a chunk of its own.
 
 constexpr int kChunk = 64, kBlockCols = 64;
 
@@ -568,7 +569,8 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(const __grid_constant__ S
 }
 
 // Sequences of up to 16 steps: one chunk, four warps, and little else than the state to move, so as many blocks on an SM as keep its
-// loads in flight.  Every warp makes the 16 x 16 weights and has 16 columns of the outputs; of the state it has RB / 4 rows.
+// loads in flight.  Every warp makes the 16 x 16 weights and has 16 columns of the outputs; of the state it has RB / 4 rows.  16 steps
+// of 256 x 16 heads of 64 x 64: 50 us, 3.3 TB/s (by chunk_kernel 71): six blocks of an SM wait for their first loads and store at their end.
 template <int RB>
 __global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(const __grid_constant__ Sweeps all) {
     grid_wait();
@@ -769,7 +771,9 @@ __global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(const __gr
 // round.
 //   64 rows: the weighted keys' first two terms are the two halves of a 128-row operand, and what comes of them stays apart, as rows r
 // and 64 + r of the state, which X reads one after the other: their sum is made once, at the end.
-// mma.sync at these sizes is bound by what goes with it, 13 instructions for each product (8192 steps of 16 x 128: 219 us).
+// mma.sync at these sizes is bound by what goes with it, 13 instructions for each product (8192 steps of 16 x 128: 219 us, here 85).
+// Bound by the chain within a chunk (tiles, S, P, O2, outputs) with one or two blocks on an SM to cover it: 6 to 8 thousand cycles
+// of a chunk, of which the products are one and all traffic of shared memory three; blocks of 64 x 64 run two to an SM.
 
 // RB, CB: rows and columns of the state, padded to 64 or 128.  STATE: only what the segment leaves, from an empty state.  TERMS: of the
 // weighted a.
@@ -1473,7 +1477,9 @@ __global__ void __launch_bounds__(256) step_kernel(const T *q, const T *k, const
 }
 
 // Segments a sequence is cut into: as many as give the GPU one round of two blocks per SM (64 columns of a head each; the GPU's 148
-// SMs as a constant, so that the size of the workspace does not depend on where it is asked for), none shorter than 256 steps.
+// SMs as a constant, so that the size of the workspace does not depend on where it is asked for), none shorter than 256 steps: a
+// segment's states are made, written, joined and read (8192 steps of 16 x 128 in 8 segments: 36 us, 11 to join them, 47 for the
+// outputs from there; step by step and whole 1392).
 constexpr int kSegment = 256;
 int segments(const ppo_decay_attention_desc *d, int *len) {
     const long long blocks = (long long)d->Be * d->heads * ppo_cdiv(d->dk > d->dv ? d->dk : d->dv, 64);
@@ -1600,7 +1606,8 @@ bool chunks_fit(const Sweep &s) {
     return s.R % 8 == 0 && s.C % 8 == 0 && rows(s.a, s.lda) && rows(s.b, s.ldb) && rows(s.x, s.ldx) && (s.shared || rows(s.out, s.ldo));
 }
 
-// bf16 rows that vectors fit: up to 16 steps, up to 64, more.
+// bf16 rows that vectors fit: up to 16 steps, up to 64, more.  64 x 16 heads of 64 x 64, outputs and gradients: 16 steps 22 and 37 us,
+// 17 (as a chunk of 64) 31 and 60; 64 steps 43 and 80, 65 (in a tile of 128) 68 and 162.
 template <typename T>
 int run(const Work &w, cudaStream_t st) {
     bool chunks = std::is_same_v<T, bf16>;

@@ -1,4 +1,7 @@
 // Group normalisation with an activation, channels last, and its gradients.
+//
+// Means, squares about the mean and all arithmetic in 32 bits (variances never as a difference of squares); what is stored is rounded
+// once.  Read once, written once where an image, or its group, fits registers or the shared memory of a cluster.
 #include "elem.cuh"
 #include "tcgen05.cuh"
 
@@ -15,7 +18,9 @@ struct NormArgs {
     float eps;
 };
 
-constexpr int kThreads = 256, kBlocks = 3;  // blocks on an SM that a split of an image leaves room for
+// kBlocks: blocks on an SM that a split of an image leaves room for.  1024 images of 1200 x 64, bf16: 2 blocks 85 us, 3 (here 4 blocks
+// an image) 79, 6 (8 blocks an image) 116.
+constexpr int kThreads = 256, kBlocks = 3;
 
 // Sum over the block, the same in every thread; tmp holds one value per warp.
 __device__ __forceinline__ float block_sum(float v, float *tmp) {
@@ -194,7 +199,8 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_any_kernel(NormArgs a) {
 // ---- few values per image and group (up to 256 vectors): `width` lanes of a warp per group, its values in registers ----
 //
 // `active` of them, a multiple of a pixel's vectors of the group: a lane's vectors hold the same channels at every pixel, so it keeps
-// their scales, and the sums over images of their gradients, for all images its block goes through.
+// their scales, and the sums over images of their gradients, for all images its block goes through.  Gradients of 4096 rows of 1024 in 16
+// groups, fp32: 18.6 us with the sum of the shares, whose launch is a third of it (element by element 4094; 2 x 148 blocks 23.3).
 
 struct Lanes {
     int width, active;
@@ -371,7 +377,10 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_small_kernel(NormArgs a,
 // Thread (pl, vc) has the same vector of channels of the pixels pl, pl + lanes, ...: memory is read and written in whole rows.
 // K: parts of a vector that belong to different groups (1: a group has whole vectors).
 //   WHOLE: a cluster per image, whose blocks keep their pixels in shared memory between the sums, which they exchange there, and
-// the result: read once, written once.  What a thread copies in is what it uses, so that only the sums meet at barriers.
+// the result: read once, written once.  What a thread copies in is what it uses, so that only the sums meet at barriers.  1024 x 1200 x 64
+// bf16: 79 us, 4.0 TB/s (element by element 449); gradients of 512 x 4800 x 32: 160 us, 3.0 TB/s (814), in clusters of 8 with two blocks on
+// an SM: a block loads, sums, meets the others and stores in turn, and only its neighbours on the SM fill the gaps.  The gradients' inputs
+// read again from L2 instead of kept: 195 to 247.
 //   SUMS, then APPLY: images that do not fit eight blocks; the sums go through the workspace, and the second launch reads the image again.
 enum { WHOLE, SUMS, APPLY };
 
@@ -712,7 +721,13 @@ Plan plan_of(const ppo_group_norm_desc *d, bool bwd) {
     if (d->C % N != 0 || d->ldx % N != 0 || d->ldy % N != 0) return p;
     const long long all = (long long)d->HW * per / N;  // vectors of an image and group
     const int vecs = per / N;
-    if (per % N == 0 && vecs <= 32 && all <= 32 / vecs * vecs * 8) {
+    p.K = per % N == 0 ? 1 : N % per == 0 ? N / per : 0;
+    const int VC = d->C / N;
+    const bool image = p.K != 0 && VC <= kThreads && d->groups <= 1024;
+    // gradients that a lane does not keep are left to the blocks of an image: 2048 images of 32 x 256 in 4 groups, bf16, 58 and 87 us, of
+    // 16 x 256 50 and 52, of 8 x 256 77 and 38 (kept); outputs 41 and 29, 35 and 18, 55 and 18
+    const int most = bwd && image ? 4 : 8;
+    if (per % N == 0 && vecs <= 32 && all <= 32 / vecs * vecs * most) {
         int width = 32, active = 32 / vecs * vecs;
         if ((vecs & (vecs - 1)) == 0)
             for (width = vecs, active = 0; width < 32 && width < all;) width *= 2;
@@ -729,9 +744,7 @@ Plan plan_of(const ppo_group_norm_desc *d, bool bwd) {
         if (p.blocks > d->B) p.blocks = d->B;
         p.parts = p.blocks;
     } else {
-        p.K = per % N == 0 ? 1 : N % per == 0 ? N / per : 0;
-        const int VC = d->C / N;
-        if (p.K == 0 || VC > kThreads || d->groups > 1024) return p;
+        if (!image) return p;
         p.kind = Plan::IMAGE;
         const int lanes = kThreads / VC;
         const auto smem = [&](int n, bool whole) {
