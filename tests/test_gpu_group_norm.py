@@ -201,6 +201,16 @@ def test_other_streams_and_captured_calls(shape):
     assert all(torch.equal(a, b) for a, b in zip(out, (y, mean, rstd, *want)))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(70, 1, 768, 32), (9, 2, 48, 2), (33, 5, 72, 3), (5, 3, 320, 8), (700, 1, 60, 5), (12, 7, 168, 7)])
+def test_groups_whose_vectors_are_no_power_of_two(shape, dtype):
+    B, HW, C, groups = shape
+    x, gamma, beta, dy = _inputs(B, HW, C, dtype, seed=9)
+    y, mean, rstd = _fwd(x, groups, gamma, beta, "silu")
+    _check_fwd(x, groups, gamma, beta, "silu", (y, mean, rstd))
+    _check_bwd(x, groups, gamma, beta, mean, rstd, dy, "silu", _bwd(x, groups, gamma, beta, mean, rstd, dy, "silu"))
+
+
 def test_more_groups_than_a_grid_has_rows():
     # 17 pixels of one vector: a warp each, eight a block, more than 65535 blocks
     B, HW, C, groups = 1, 17, 8 * 524289, 524289
