@@ -1478,7 +1478,7 @@ __global__ void __launch_bounds__(256) step_kernel(const T *q, const T *k, const
 
 // Segments a sequence is cut into: as many as give the GPU one round of two blocks per SM (64 columns of a head each; the GPU's 148
 // SMs as a constant, so that the size of the workspace does not depend on where it is asked for), none shorter than 256 steps: a
-// segment's states are made, written, joined and read (8192 steps of 16 x 128 in 8 segments: 36 us, 11 to join them, 47 for the
+// segment's states are made, written, joined and read (8192 steps of 16 x 128 in 8 segments: 37 us, 10 to join them, 44 for the
 // outputs from there; step by step and whole 1392).
 constexpr int kSegment = 256;
 int segments(const ppo_decay_attention_desc *d, int *len) {
