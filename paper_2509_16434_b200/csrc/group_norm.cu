@@ -284,62 +284,79 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_small_kernel(NormArgs a,
         beta[k] = a.gamma ? a.beta[c0 + k] : 0.f;
         s1[k] = s2[k] = 0.f;
     }
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    struct Image {
+        float mean[1], rstd[1];
+        Vec<T> v[KEEP], d[KEEP];
+    };
+    const auto load = [&](int b, int i, Vec<T> &vx, Vec<T> &vd) {
+        const int at = i * ln.active + l, p = at / vecs;
+        const bool ok = on && at < all && b < a.B;
         const T *x = static_cast<const T *>(a.x) + (long long)b * a.HW * a.ldx + c0, *dy = static_cast<const T *>(a.dy) + (long long)b * a.HW * a.ldy + c0;
+        vx.raw = ok ? *reinterpret_cast<const uint4 *>(x + p * a.ldx) : make_uint4(0, 0, 0, 0);
+        vd.raw = ok ? *reinterpret_cast<const uint4 *>(dy + p * a.ldy) : make_uint4(0, 0, 0, 0);
+    };
+    const auto fetch = [&](int b, Image &m) {
+        const bool ok = on && b < a.B;
+        m.mean[0] = ok ? a.mean[(long long)b * a.groups + g] : 0.f;
+        m.rstd[0] = ok ? a.rstd[(long long)b * a.groups + g] : 0.f;
+        if constexpr (KEEP == NV) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) load(b, i, m.v[i], m.d[i]);
+        }
+    };
+    const auto work = [&](int b, Image &m) {
         T *dx = static_cast<T *>(a.dx) + (long long)b * a.HW * a.ldx + c0;
-        const float mean[1] = {on ? a.mean[(long long)b * a.groups + g] : 0.f}, rstd[1] = {on ? a.rstd[(long long)b * a.groups + g] : 0.f};
+        const float rstd = m.rstd[0];
         float scale[N];
 #pragma unroll
-        for (int k = 0; k < N; ++k) scale[k] = rstd[0] * gamma[k];
-        Vec<T> v[KEEP], d[KEEP];
-        const auto load = [&](int i, Vec<T> &vx, Vec<T> &vd) {
-            const int at = i * ln.active + l, p = at / vecs;
-            const bool ok = on && at < all;
-            vx.raw = ok ? *reinterpret_cast<const uint4 *>(x + p * a.ldx) : make_uint4(0, 0, 0, 0);
-            vd.raw = ok ? *reinterpret_cast<const uint4 *>(dy + p * a.ldy) : make_uint4(0, 0, 0, 0);
-        };
+        for (int k = 0; k < N; ++k) scale[k] = rstd * gamma[k];
         const auto both = [&](const Vec<T> &vx, const Vec<T> &vd, float (&xc)[N], float (&dz)[N]) {
             float f[N];
             vx.get(f);
             vd.get(dz);
 #pragma unroll
-            for (int k = 0; k < N; ++k) xc[k] = f[k] - mean[0];
-            grad_vector<ACT, N, N>(dz, xc, f, mean, rstd, a.gamma ? a.gamma + c0 : nullptr, scale, beta);
+            for (int k = 0; k < N; ++k) xc[k] = f[k] - m.mean[0];
+            grad_vector<ACT, N, N>(dz, xc, f, m.mean, m.rstd, a.gamma ? a.gamma + c0 : nullptr, scale, beta);
         };
-        if constexpr (KEEP == NV) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) load(i, v[i], d[i]);
-        }
         float m1 = 0.f, m2 = 0.f;
 #pragma unroll(KEEP == NV ? NV : 2)
         for (int i = 0; i < NV; ++i) {
-            if constexpr (KEEP != NV) load(i, v[0], d[0]);
+            if constexpr (KEEP != NV) load(b, i, m.v[0], m.d[0]);
             float xc[N], dz[N];
-            both(v[i % KEEP], d[i % KEEP], xc, dz);
+            both(m.v[i % KEEP], m.d[i % KEEP], xc, dz);
             if (on && i * ln.active + l < all) {
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
                     s1[k] += dz[k];
-                    s2[k] = fmaf(dz[k], xc[k] * rstd[0], s2[k]);
+                    s2[k] = fmaf(dz[k], xc[k] * rstd, s2[k]);
                     m1 = fmaf(gamma[k], dz[k], m1);
                     m2 = fmaf(gamma[k] * dz[k], xc[k], m2);
                 }
             }
         }
         m1 = lanes_sum(m1, ln.width) / n;
-        m2 = lanes_sum(m2, ln.width) / n * rstd[0] * rstd[0];
+        m2 = lanes_sum(m2, ln.width) / n * rstd * rstd;
 #pragma unroll(KEEP == NV ? NV : 2)
         for (int i = 0; i < NV; ++i) {
-            if constexpr (KEEP != NV) load(i, v[0], d[0]);
+            if constexpr (KEEP != NV) load(b, i, m.v[0], m.d[0]);
             const int at = i * ln.active + l;
             float xc[N], dz[N];
-            both(v[i % KEEP], d[i % KEEP], xc, dz);
+            both(m.v[i % KEEP], m.d[i % KEEP], xc, dz);
 #pragma unroll
-            for (int k = 0; k < N; ++k) dz[k] = rstd[0] * (fmaf(gamma[k], dz[k], -m1) - xc[k] * m2);
+            for (int k = 0; k < N; ++k) dz[k] = rstd * (fmaf(gamma[k], dz[k], -m1) - xc[k] * m2);
             Vec<T> r;
             r.set(dz);
             if (on && at < all) *reinterpret_cast<uint4 *>(dx + at / vecs * a.ldx) = r.raw;
         }
+    };
+    constexpr int AT_ONCE = KEEP == NV ? 2 : 1;  // images whose loads are on their way (38907 rows of 32 x 24 bf16: 169 us by one, 142)
+    for (int b = blockIdx.x; b < a.B; b += AT_ONCE * gridDim.x) {
+        Image image[AT_ONCE];
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) fetch(b + q * (int)gridDim.x, image[q]);
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q)
+            if (b + q * (int)gridDim.x < a.B) work(b + q * (int)gridDim.x, image[q]);
     }
     if (!a.part) return;
     // lanes of other pixels of the same channels
@@ -728,7 +745,7 @@ Plan plan_of(const ppo_group_norm_desc *d, bool bwd) {
     // 16 x 256 50 and 52, of 8 x 256 77 and 38 (kept); outputs 41 and 29, 35 and 18, 55 and 18
     const int most = bwd && image ? 4 : 8;
     if (per % N == 0 && vecs <= 32 && all <= 32 / vecs * vecs * most) {
-        int width = 1;  // as few lanes as hold the group in a vector each (38907 rows of 32 x 24 bf16: 672 us by whole warps, now 169)
+        int width = 1;  // as few lanes as hold the group in a vector each (38907 rows of 32 x 24 bf16: 672 us by whole warps, now 142)
         while (width < vecs || (width < 32 && width / vecs * vecs < all)) width *= 2;
         const int active = width / vecs * vecs;
         p.kind = Plan::SMALL;
