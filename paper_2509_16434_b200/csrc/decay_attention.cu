@@ -799,7 +799,8 @@ struct TileTables {
     float weight[256];  // a_scale lambda^|p - c| of step c for step p at 127 - p + c
     float pow[132];     // lambda^n
     uint64_t got_a, got_b, bar[3];    // X and A, B have landed; S and O1, K, O2 are made
-    uint64_t split, weighted, emptied;  // of the workers' warps: A is split; P is there; accumulators are read, M and outputs in place
+    // of the workers' warps: A is split; B is looked at, and with outputs P is there; accumulators are read, M and outputs in place
+    uint64_t split, weighted, emptied;
     uint64_t left;                      // outputs have left shared memory (kTurns)
     uint32_t flags[2][4];  // done at the steps of a chunk, a bit each
     int abort_flag, bad;
@@ -1073,8 +1074,9 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                 }
                 __syncwarp();
             }
-            if (more) {  // all that reads B is made
+            if (more) {  // all that reads B is made, and the workers have looked at it
                 wait(&tab->bar[STATE ? 1 : 2], i);
+                if (STATE) wait(&tab->weighted, i);
                 if (tc::elect_one()) {
                     expect_b();
                     load_b(i + 1);
@@ -1199,6 +1201,7 @@ __global__ void __launch_bounds__(tile_threads(RB, CB, STATE), RB == 64 && CB ==
                     zeros = __hfma2(two, __float2bfloat162_rn(0.f), zeros);
                 }
             }
+            if (STATE) tell(&tab->weighted);
             bool reached = true;  // whether this row sees the state in front of the chunk
             if constexpr (!STATE) {
                 int bound = rev ? 127 : 0;  // the last step that it sees (backwards: the farthest)
