@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(256, KMOST == 16 ? 2 : KMOST == 12 ? 3 : 4) sw
 // itself.  lambda^.. a_j is not: as one bf16 number it would leave 2^-8 in a state that is handed out in 32 bits; three terms that
 // sum up to 24 bits are exact to 2^-25 (in the kernel for many chunks two, 2^-17, where only outputs of bf16 come of it).
 // A product has no masked places: 0 times a NaN of a later step would reach an earlier one, or stay behind a reset.  So a chunk that
-// holds an infinity or a NaN is taken step by step, each as a chunk of its own.
+// holds an infinity or a NaN is taken step by step, each as a chunk of its own, of which nothing is added where its flag is set.
 
 constexpr int kChunk = 64, kBlockCols = 64;
 
@@ -497,6 +497,7 @@ __global__ void __launch_bounds__(256, 2) chunk_kernel(const __grid_constant__ S
         for (int nn = 0; nn < MN; ++nn)
 #pragma unroll
             for (int v = 0; v < 4; ++v) M[nn][v] = resets == 0 ? M[nn][v] * keep : 0.f;
+        if (n == 1 && resets != 0 && !rev) return;  // one step with its flag set: a product with weight 0 would let its NaN pass
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (16 * k >= n) break;
@@ -708,6 +709,11 @@ __global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(const __gr
         if (!s.m_out && (!bad || piece == n - 1)) continue;
         const int end = __popc(resets);
         const float keep = pow[count];
+        if (count == 1 && resets != 0 && !rev) {  // nothing of the step is left; a product with weight 0 would let its NaN pass
+            __syncthreads();
+            if (tid < kBlockCols) bs[tid] = from_f32<bf16>(0.f);
+            __syncthreads();
+        }
         float wj[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {

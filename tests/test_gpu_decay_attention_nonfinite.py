@@ -78,7 +78,7 @@ def _check(shape, dtype, done, bad, values, cut=None):
 
 def _steps(T, Be, *places):
     m = torch.zeros(T, Be, dtype=torch.bool)
-    for e, at in enumerate(places):
+    for e, at in enumerate(places[:Be]):
         m[[t for t in at if t < T], e] = True
     return m
 
@@ -95,3 +95,15 @@ def test_sequences_that_are_cut(shape):
         bad[e::97, e] = True
         done[3 * e::89, e] = True
     _check(shape, BF16, done, bad, (NAN, INF), cut=True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(1, 4, 4, 2, 64, 64), (2, 4, 2, 2, 16, 128), (9, 5, 4, 2, 64, 64), (16, 5, 4, 4, 128, 48), (17, 5, 4, 2, 64, 128), (50, 6, 4, 2, 104, 64),
+                                   (64, 6, 2, 1, 64, 64), (65, 6, 4, 2, 64, 64), (200, 6, 4, 2, 128, 128), (50, 6, 4, 2, 7, 33)], ids=lambda s: "-".join(map(str, s)))
+def test_sequences_of_one_piece(shape, dtype):
+    """Envs whose bad steps carry a flag, lie in front of one or behind one, the first and the last step among them."""
+    T, Be = shape[:2]
+    last = T - 1
+    bad = _steps(T, Be, (0, 7, 40), (1, 6, 15, 63), (), (last,), (8, 16, 33, 64, 127), (0, 3, last))
+    done = _steps(T, Be, (0, 7, 40), (2, 6, 16, 63), (3, 11, 48), (last, 5), (9, 15, 16, 34, 64, 128), (2, last))
+    _check(shape, dtype, done, bad, (NAN, INF, -INF), cut=False)
