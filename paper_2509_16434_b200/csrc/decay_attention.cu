@@ -67,9 +67,9 @@ __device__ __forceinline__ pair32 mul2(pair32 a, pair32 b) {
 // 8; a thread fetches its share of the next tile while it works on this one.  Two multiply-adds for each element and step, for two
 // rows in one instruction, and a broadcast load of shared memory for sixteen of them: bound by issue and by the chain from step to
 // step (gradients of 119 steps of 37 x 6 heads of 48 x 80, fp32: 123 us; one row an instruction 138, one column a lane 183 of two
-// launches).  For that the decay is not applied step by step: within a tile the state is kept as N = M lambda^-e behind e steps, so that
-// N += a b lambda^-e, and out = lambda^e x^T N; with lambda >= 1/2 that is a factor of at most 2^8.  Smaller decays are applied step
-// by step, in three operations.  Products of 32-bit numbers have no tensor core instruction without a rounding to 11 bits.
+// launches).  For that the decay is not applied step by step: within a tile the state is kept as N = M lambda^(8-e) behind e steps, so that
+// N += a b lambda^(8-e), and out = lambda^(e-8) x^T N.  With lambda >= 1/2 N is at most 2^8 smaller than M, never larger: nothing becomes
+// infinite that the formula leaves finite.  Smaller decays are applied step by step, in three operations.  Products of 32-bit numbers have no tensor core instruction without a rounding to 11 bits.
 // Sweeps of one call that do not wait for one another, along z of one launch.
 struct Sweeps {
     Sweep s[3];
@@ -102,10 +102,10 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
     const T *X = static_cast<const T *>(s.x) + (long long)(h / s.share_x) * s.R;
     if (tid <= kTokens) {
         const float l2 = log2f(lam);
-        const int n = tid + 1 - rev;  // decays up to step tid
-        if (tid < kTokens) up[tid] = scaled ? exp2f(-n * l2) : 1.f;
-        // what outputs are multiplied with; the last: what the state is behind a whole tile
-        down[tid] = !scaled ? 1.f : power(l2, tid < kTokens ? n : kTokens);
+        const int n = kTokens - (tid + 1 - rev);  // decays of a whole tile that come behind step tid
+        if (tid < kTokens) up[tid] = scaled ? power(l2, n) : 1.f;
+        // what outputs are multiplied with; the last: what the state is in front of a tile
+        down[tid] = !scaled ? 1.f : tid < kTokens ? exp2f(-n * l2) : power(l2, kTokens);
     }
     pair32 M[2][KS / 2];  // of two columns, rows in pairs
     // this thread's element of row r of the state lies at r * sr + c * sc
@@ -199,13 +199,16 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
             }
         };
         if (scaled) {
-            steps(std::false_type{});
-            const float f = cnt == kTokens ? down[kTokens] : power(log2f(lam), cnt);
+            const auto times = [&](float f) {
 #pragma unroll
-            for (int i = 0; i < KS / 2; ++i) {
-                M[0][i] = mul2(M[0][i], pair_of(f, f));
-                M[1][i] = mul2(M[1][i], pair_of(f, f));
-            }
+                for (int i = 0; i < KS / 2; ++i) {
+                    M[0][i] = mul2(M[0][i], pair_of(f, f));
+                    M[1][i] = mul2(M[1][i], pair_of(f, f));
+                }
+            };
+            times(down[kTokens]);
+            steps(std::false_type{});
+            if (cnt < kTokens) times(exp2f((cnt - kTokens) * log2f(lam)));
         } else {
             steps(std::true_type{});
         }
@@ -217,7 +220,7 @@ __device__ __forceinline__ void sweep_rows(const Sweep &s, StepTiles &tile) {
                 float v = 0.f;
 #pragma unroll
                 for (int k = 0; k < kSlices; ++k) v += part[k][t][c];
-                v *= s.out_scale * down[t];
+                v = v * down[t] * s.out_scale;
                 const long long row = (long long)(rev ? s.T - 1 - (n + t) : n + t) * s.Be + e;
                 if (s.shared) s.shared[(row * s.heads + h) * s.C + c0 + c] = v;
                 else static_cast<T *>(s.out)[row * s.ldo + (long long)h * s.C + c0 + c] = from_f32<T>(v);
