@@ -260,8 +260,8 @@ __global__ void __launch_bounds__(256, KMOST == 16 ? 2 : KMOST == 12 ? 3 : 4) sw
 // (backwards one power less in the second and one more in the last term); terms with a reset between j and i, or between M and
 // i, fall away.  Four products of 64-row tiles; the state stays in registers in 32 bits, 64 of its columns per block.
 // Rounded to bf16: the weights w_ij (x_i . a_j), and the state where x reads it; half a step each, next to that of the output
-// itself.  lambda^.. a_j is not: as one bf16 number it would leave 2^-8 in a state that is handed out in 32 bits; three terms that
-// sum up to 24 bits are exact to 2^-25 (in the kernel for many chunks two, 2^-17, where only outputs of bf16 come of it).
+// itself.  lambda^.. a_j is not: as one bf16 number it would leave 2^-8 in a state that is handed out in 32 bits; three terms hold
+// the product in 32 bits, 2^-24 (in the kernel for many chunks two, 3 2^-16, where only outputs of bf16 come of it).
 // A product has no masked places: 0 times a NaN of a later step would reach an earlier one, or stay behind a reset.  So a chunk that
 // holds an infinity or a NaN is taken step by step, each as a chunk of its own, of which nothing is added where its flag is set.
 
@@ -818,9 +818,9 @@ struct TileTables {
 static_assert(sizeof(TileTables) <= 1680, "place of the tables");
 
 // w a for eight bf16 numbers a, as sums of bf16 numbers.  With w = w0 + w1 + w2, 8 bits each, hi = a w0 to the nearest and a w0 - hi are
-// bf16 numbers that hold a w0 entirely (16 bits), in two packed operations a pair; four terms are exact to 2^-26, two to 2^-17.
-// Three come from 32 bits, 17 operations a pair: with 128 rows, where the fourth would cost more products and shared memory than
-// it saves (8192 steps of 16 x 128: 97 and 90 us).
+// bf16 numbers that hold a w0 entirely (16 bits), in two packed operations a pair; four terms are off by less than 2^-23 (at most
+// 0.72 2^-24 of 2 million), two by less than 3 2^-16 (1.64).  Three come from 32 bits, 17 operations a pair, and are off by 2^-24: with 128
+// rows, where the fourth would cost more products and shared memory than it saves (8192 steps of 16 x 128: 97 and 90 us).
 template <int TERMS>
 __device__ __forceinline__ void split_products(const uint32_t (&a)[4], float w, uint32_t (&part)[TERMS][4]) {
     if constexpr (TERMS == 3) {
