@@ -401,7 +401,12 @@ enum { PPO_F32 = 0, PPO_BF16 = 1, PPO_F16 = 2 };
  *   PPO_BF16); ldq, ldk, ldv, ldo: elements from one row to the next, so that a row may be part of a wider one (at least
  *   the row's own length); decay fp32 [heads], in [0, 1], a constant of the call as gamma and lambda are of ppo_compute_gae;
  *   done uint8 [T][Be] (NULL: no flag is set); states fp32 [Be][heads][dk][dv] (in NULL: zeros; out NULL: not wanted).
- * Sums and states are held in fp32.  1 <= dk, dv <= 128; T * Be up to 0x7f000000 (else UNSUPPORTED). */
+ * Sums and states are held in fp32.  Sequences of PPO_BF16 rows that are whole, aligned 16-byte vectors are taken in chunks: there the
+ * weights lambda^(i-j) q_i . k_j of pairs of steps and the state as q reads it are rounded to bf16 on their way into o (in the
+ * gradients, their counterparts on the way into dq, dk and dv), which makes up to 1.02 * 2^-8 of the sum of the terms' absolute values,
+ * beside the rounding of the result itself; a state that is handed out is not rounded.  ppo_decay_attention_step reads the state
+ * in fp32: its o may differ by as much from that of the same step in a sequence.  Within a chunk the inner products q_i . k_j and do_i . v_j
+ * have to be finite in fp32.  1 <= dk, dv <= 128; T * Be up to 0x7f000000 (else UNSUPPORTED). */
 typedef struct {
     int32_t T, Be, heads, kv_heads, dk, dv, dtype;
     int64_t ldq, ldk, ldv, ldo;
@@ -479,8 +484,8 @@ int ppo_token_logp(const ppo_token_desc *desc, const void *dev_logits, const int
  * from row to row; may be dev_logits where ld_grad == ld; columns behind vocab are left as they are), the log-probabilities to
  * dev_logp_out [rows] (may be NULL), and writes (accumulate == 0) or adds this call's share of {L_pi = mean(-s), mean(kl),
  * mean(H), mean(old - logp), mean(r outside the clip range)}, each weighted by w, to dev_loss_out fp32 [5].
- * Rows of weight 0, rows whose token is outside [0, vocab) and rows without a finite logit are left out: they
- * contribute nothing, their gradient is 0 and their dev_logp_out 0; the logits of the first two are not read.  grad_scale: 1, or a
+ * Rows of weight 0, rows whose token is outside [0, vocab) and rows all of whose logits are minus infinity are left
+ * out: they contribute nothing, their gradient is 0 and their dev_logp_out 0; the logits of the first two are not read.  grad_scale: 1, or a
  * loss scale where 16-bit gradients (PPO_F16) would underflow.  dev_workspace: ppo_token_loss_workspace_bytes(desc) bytes.
  * Sums in a fixed order: same bits run to run. */
 typedef struct {

@@ -69,7 +69,8 @@ __device__ __forceinline__ pair32 mul2(pair32 a, pair32 b) {
 // step (gradients of 119 steps of 37 x 6 heads of 48 x 80, fp32: 123 us; one row an instruction 138, one column a lane 183 of two
 // launches).  For that the decay is not applied step by step: within a tile the state is kept as N = M lambda^(8-e) behind e steps, so that
 // N += a b lambda^(8-e), and out = lambda^(e-8) x^T N.  With lambda >= 1/2 N is at most 2^8 smaller than M, never larger: nothing becomes
-// infinite that the formula leaves finite.  Smaller decays are applied step by step, in three operations.  Products of 32-bit numbers have no tensor core instruction without a rounding to 11 bits.
+// infinite that the formula leaves finite.  Smaller decays are applied step by step, in three operations.  Products of 32-bit numbers have no tensor core instruction without a rounding to 11
+// bits; operands as sums of bf16 terms, as the chunks below have them for their states, have not been tried here.
 // Sweeps of one call that do not wait for one another, along z of one launch.
 struct Sweeps {
     Sweep s[3];
@@ -781,8 +782,9 @@ __global__ void __launch_bounds__(128, RB == 64 ? 6 : 3) short_kernel(const __gr
 //   64 rows: the weighted keys' first two terms are the two halves of a 128-row operand, and what comes of them stays apart, as rows r
 // and 64 + r of the state, which X reads one after the other: their sum is made once, at the end.
 // mma.sync at these sizes is bound by what goes with it, 13 instructions for each product (8192 steps of 16 x 128: 219 us, here 85).
-// Bound by the chain within a chunk (tiles, S, P, O2, outputs) with one or two blocks on an SM to cover it: 6 to 8 thousand cycles
-// of a chunk, of which the products are one and all traffic of shared memory three; blocks of 64 x 64 run two to an SM.
+// Bound by the steps of a chunk one after another (tiles, S, P, O2, outputs) with one or two blocks on an SM to cover them: 6 to 8 thousand
+// cycles of a chunk, of which the products are one and all traffic of shared memory three; blocks of 64 x 64 run two to an SM.  Only O1
+// needs the state in front of the chunk: S, the split and K could be made a chunk ahead, and are not.
 
 // RB, CB: rows and columns of the state, padded to 64 or 128.  STATE: only what the segment leaves, from an empty state.  TERMS: of the
 // weighted a.
@@ -1489,9 +1491,10 @@ __global__ void __launch_bounds__(256) step_kernel(const T *q, const T *k, const
 }
 
 // Segments a sequence is cut into: as many as give the GPU one round of two blocks per SM (64 columns of a head each; the GPU's 148
-// SMs as a constant, so that the size of the workspace does not depend on where it is asked for), none shorter than 256 steps: a
-// segment's states are made, written, joined and read (8192 steps of 16 x 128 in 8 segments: 37 us, 10 to join them, 44 for the
-// outputs from there; step by step and whole 1392).
+// SMs as a constant, so that the size of the workspace does not depend on where it is asked for), none but the last
+// shorter than 256 steps: a segment's states are made, written, joined and read (8192 steps of 16 x 128 in 8 segments: 37 us, 10 to join
+// them, 44 for the outputs from there; step by step and whole 1392).  The blocks of one sweep are counted, also where a call for gradients
+// launches three together (2048 steps of 4 x 16 heads of 64: 768 blocks, 2.6 rounds).
 constexpr int kSegment = 256;
 int segments(const ppo_decay_attention_desc *d, int *len) {
     const long long blocks = (long long)d->Be * d->heads * ppo_cdiv(d->dk > d->dv ? d->dk : d->dv, 64);

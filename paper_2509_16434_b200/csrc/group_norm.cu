@@ -14,12 +14,12 @@ struct NormArgs {
     float *mean, *rstd;
     float *part;  // shares of the gradients of gamma and beta, [parts][2][C]
     long long ldx, ldy;
-    int B, HW, C, groups, per, act;
+    int B, HW, C, groups, per;
     float eps;
 };
 
-// kBlocks: blocks on an SM that a split of an image leaves room for.  1024 images of 1200 x 64, bf16: 2 blocks 85 us, 3 (here 4 blocks
-// an image) 79, 6 (8 blocks an image) 116.
+// kBlocks: an image is split over 1, 2, 4 or 8 blocks until an SM has shared memory for at least so many.  1024 images of 1200 x 64, bf16: 2
+// (2 blocks an image) 85 us; 3, 4 or 5 (4 blocks an image, of which an SM holds five) 79; 6 (8 blocks an image) 116.
 constexpr int kThreads = 256, kBlocks = 3;
 
 // Sum over the block, the same in every thread; tmp holds one value per warp.
@@ -836,7 +836,6 @@ NormArgs args(const ppo_group_norm_desc *d) {
     a.C = d->C;
     a.groups = d->groups;
     a.per = d->C / d->groups;
-    a.act = d->act;
     return a;
 }
 

@@ -6,8 +6,8 @@
 // results, depends neither on the other rows of a call nor on where the row lies, and the call that scores a token while acting gives
 // what the loss gives (a ratio of exactly 1 in a first epoch).
 //
-// Sums, maxima and arithmetic in 32 bits; only the gradient is rounded, once.  4096 rows of 32000 bf16 logits with their gradient, a twentieth of
-// the rows left out: 160 us, 3.1 TB/s of the 498 MB that have to move.  26 instructions for each logit, two exponentials among them, at two blocks of 16 warps an SM,
+// Sums, maxima and arithmetic in 32 bits; only the gradient is rounded, once.  4096 rows of 32000 bf16 logits with their gradient, a tenth of the
+// rows left out: 160 to 165 us, 3.0 to 3.1 TB/s of the 498 MB that have to move.  26 instructions for each logit, two exponentials among them, at two blocks of 16 warps an SM,
 // which is what 64 registers a thread leave: loads of one block run under the arithmetic of the other.  Rows in shared memory, three
 // blocks: 157, and log-probabilities of 40 rows of 100003 in 12.1 us, not 11.2; blocks that stay and copy rows ahead: 175.
 #include "elem.cuh"
