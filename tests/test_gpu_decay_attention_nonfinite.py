@@ -107,3 +107,30 @@ def test_sequences_of_one_piece(shape, dtype):
     bad = _steps(T, Be, (0, 7, 40), (1, 6, 15, 63), (), (last,), (8, 16, 33, 64, 127), (0, 3, last))
     done = _steps(T, Be, (0, 7, 40), (2, 6, 16, 63), (3, 11, 48), (last, 5), (9, 15, 16, 34, 64, 128), (2, last))
     _check(shape, dtype, done, bad, (NAN, INF, -INF), cut=False)
+
+
+@pytest.mark.parametrize("value", [NAN, INF])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(1, 4, 4, 2, 64, 64), (9, 4, 4, 2, 64, 64), (50, 4, 4, 2, 104, 64), (200, 4, 4, 2, 128, 128), (700, 4, 4, 2, 64, 128), (50, 4, 4, 2, 7, 33)],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_states_that_come_in(shape, dtype, value):
+    """A bad state that comes in reaches the steps up to the first flag, the gradient of the one that is left those behind the last."""
+    T, Be = shape[:2]
+    c = Case(*shape, dtype)
+    done = _steps(T, Be, (T // 2,), (0, T - 1), (T // 3, T // 2 + 1))  # none for the last env
+    c.done = done.to(torch.uint8).to(DEV)
+    (ow, sw), (oa, sa) = plain.attention(*c.args()), plain.attention_abs(*c.args())
+    want, size = (f(*c.args(), c.do, c.ds) for f in (plain.attention, plain.attention_abs))
+    fwd = (done.cumsum(0) - done.long() == 0).to(DEV)
+    back = (done.flip(0).cumsum(0).flip(0) == 0).to(DEV)
+    free = ~done.any(0).to(DEV)
+    c.s0.fill_(value), c.ds.fill_(value)
+    o, s = c.fwd()
+    g = c.bwd()
+    d = max(c.dk, c.dv) * 2
+    for got, ref, span, reached, type_ in ((o, ow, oa, fwd, dtype), (g[0], want[0], size[0], fwd, dtype), (g[1], want[1], size[1], back, dtype),
+                                           (g[2], want[2], size[2], back, dtype), (s, sw, sa, free, F32), (g[3], want[3], size[3], free, F32)):
+        if bool((~reached).any()):
+            _near(got[~reached], ref[~reached], span[~reached], T, d, type_)
+        assert not bool(torch.isfinite(got[reached][:, -1].float()).any())  # of the last head, whose decay is 1
+    assert ppo.ppo_poll_status() == 0
