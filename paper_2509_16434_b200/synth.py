@@ -8,7 +8,7 @@ zeroed (missing returns), proprioception is 32 standard normals, rewards and old
 values are standard normals, dones are Bernoulli.
 
 Two back ends produce the same distributions: numpy (Philox, for parity-sized
-cases that also feed the CPU checker) and torch on the device (for buffers of
+cases that also feed the CPU oracle) and torch on the device (for buffers of
 many GB that never visit the host).
 """
 from __future__ import annotations
