@@ -500,6 +500,100 @@ int ppo_token_loss_fwd_bwd(const ppo_token_desc *desc, const ppo_token_loss_coef
                            const float *dev_weight, void *dev_dlogits, int64_t ld_grad, float *dev_logp_out, float *dev_loss_out,
                            int accumulate, void *dev_workspace, size_t ws_bytes, void *stream);
 
+/* The layers of a memory that chooses what it keeps, over the same sequence minibatches (row = t * Be + e), flags and decisions as the decay
+ * attention above: a short convolution along the steps of each env, and the selective scan it feeds.
+ *
+ * Causal convolution of each channel:  s_t = bias + sum_{i < width} weight[i] x_{t - width + 1 + i},  y_t = act(s_t), where the input of
+ * step t' < t counts as 0 if done is set at any of t' .. t - 1, and inputs from in front of the sequence come from the state.
+ *   x, y [T*Be][C] of type dtype, ldx and ldy elements from row to row (>= C); weight fp32 [C][width], 2 <= width <= 8; bias fp32 [C]
+ *   (NULL: 0); done uint8 [T][Be] (NULL: no flag is set); states of type dtype [Be][width - 1][C], the oldest step first: the inputs that the
+ *   step after the sequence sees (in NULL: zeros; out NULL: not wanted).  States need the alignment of their elements.
+ * Sums in fp32.  T * Be up to 0x7f000000 (else UNSUPPORTED).  Needs ppo_causal_conv_workspace_bytes for the gradients only. */
+typedef struct {
+    int32_t T, Be, C, width, act, dtype;
+    int64_t ldx, ldy;
+} ppo_causal_conv_desc;
+
+size_t ppo_causal_conv_workspace_bytes(const ppo_causal_conv_desc *desc);
+
+/* dev_state_out may be dev_state_in. */
+int ppo_causal_conv_fwd(const ppo_causal_conv_desc *desc, const void *dev_x, const float *dev_weight, const float *dev_bias, const uint8_t *dev_done,
+                        const void *dev_state_in, void *dev_y, void *dev_state_out, void *stream);
+
+/* Gradients from dL/dy (dev_dy, strided as y) and of the state that is left (dev_dstate_out, NULL: zeros): dev_dx (strided as x) and dev_dstate_in
+ * (may be NULL) are written, dL/dweight fp32 [C][width] and dL/dbias fp32 [C] (each may be NULL) added to (accumulate != 0) or written.
+ * Sums in a fixed order: same bits run to run. */
+int ppo_causal_conv_bwd(const ppo_causal_conv_desc *desc, const void *dev_x, const float *dev_weight, const float *dev_bias, const uint8_t *dev_done,
+                        const void *dev_state_in, const void *dev_dy, const void *dev_dstate_out, void *dev_dx, void *dev_dstate_in,
+                        float *dev_dweight, float *dev_dbias, int accumulate, void *dev_workspace, size_t ws_bytes, void *stream);
+
+/* One decision (desc->T == 1, else SHAPE) with the state updated in place; dev_start uint8 [Be] (NULL: none): envs whose flag is set start from a
+ * zero state, whatever dev_state holds for them. */
+int ppo_causal_conv_step(const ppo_causal_conv_desc *desc, const void *dev_x, const float *dev_weight, const float *dev_bias,
+                         const uint8_t *dev_start, void *dev_state, void *dev_y, void *stream);
+
+/* Selective scan: every channel c keeps a state h [N], whose decay and input the data choose, and B and C are shared by the
+ * channels / groups neighbouring channels of a group:
+ *   d_t = dt_t + dt_bias, or log(1 + exp(dt_t + dt_bias)) with softplus != 0
+ *   h_t = exp(d_t A) h'_{t-1} + d_t x_t B_t,   y_t = (sum_n C_t h_t + D x_t) silu(z_t),   h'_t = h_t, or zeros where done[t] is set
+ *   x, dt, z, y [T*Be][C], B, C [T*Be][groups][N] of type dtype with ldx, lddt, ldz, ldy, ldb, ldc elements from row to row (at least the row's
+ *   own length); A fp32 [C][N]; D, dt_bias fp32 [C] (NULL: 0), z NULL: no factor; done uint8 [T][Be] (NULL: no flag is set); states fp32
+ *   [Be][C][N] (in NULL: zeros, h'_{-1}; out NULL: not wanted, h'_{T-1}).
+ * States, sums and arithmetic in fp32.  1 <= N <= 64; channels a multiple of groups (else SHAPE); T * Be up to 0x7f000000 and Be * channels up to
+ * 0x1fffffff (else UNSUPPORTED). */
+typedef struct {
+    int32_t T, Be, channels, N, groups, dtype, softplus;
+    int64_t ldx, lddt, ldb, ldc, ldz, ldy;
+} ppo_selective_scan_desc;
+
+size_t ppo_selective_scan_workspace_bytes(const ppo_selective_scan_desc *desc, int backward);
+
+/* y and the state that is left.  dev_state_out may be dev_state_in. */
+int ppo_selective_scan_fwd(const ppo_selective_scan_desc *desc, const void *dev_x, const void *dev_dt, const float *dev_A, const void *dev_B,
+                           const void *dev_C, const float *dev_D, const void *dev_z, const float *dev_dt_bias, const uint8_t *dev_done,
+                           const float *dev_state_in, void *dev_y, float *dev_state_out, void *dev_workspace, size_t ws_bytes, void *stream);
+
+/* Gradients from dL/dy (dev_dy, strided as y) and of the state that is left (dev_dstate_out, NULL: zeros).  Written: those of x, dt, B, C and, where it
+ * is given, z, each strided as what it is the gradient of, and of the state that came in (dev_dstate_in, may be NULL and may be dev_dstate_out).
+ * Written or, with accumulate != 0, added to: dL/dA fp32 [C][N], dL/dD and dL/ddt_bias fp32 [C] (each may be NULL).  Sums in a fixed
+ * order: same bits run to run. */
+int ppo_selective_scan_bwd(const ppo_selective_scan_desc *desc, const void *dev_x, const void *dev_dt, const float *dev_A, const void *dev_B,
+                           const void *dev_C, const float *dev_D, const void *dev_z, const float *dev_dt_bias, const uint8_t *dev_done,
+                           const float *dev_state_in, const void *dev_dy, const float *dev_dstate_out, void *dev_dx, void *dev_ddt, float *dev_dA,
+                           void *dev_dB, void *dev_dC, float *dev_dD, void *dev_dz, float *dev_ddt_bias, float *dev_dstate_in, int accumulate,
+                           void *dev_workspace, size_t ws_bytes, void *stream);
+
+/* One decision (desc->T == 1, else SHAPE) with the state updated in place; dev_start as in ppo_causal_conv_step. */
+int ppo_selective_scan_step(const ppo_selective_scan_desc *desc, const void *dev_x, const void *dev_dt, const float *dev_A, const void *dev_B,
+                            const void *dev_C, const float *dev_D, const void *dev_z, const float *dev_dt_bias, const uint8_t *dev_start,
+                            float *dev_state, void *dev_y, void *stream);
+
+/* Norms of queries and keys with the rotation by their positions, as they stand in front of an attention: each head's d elements x become
+ *   n_i = gamma_i x_i / sqrt(mean_j x_j^2 + eps)
+ * and of the first 2 pairs elements of n, pair j turned by the angle pos * freq[j]: (n_a, n_b) -> (n_a cos - n_b sin, n_a sin + n_b cos), with
+ * (a, b) = (2 j, 2 j + 1) where interleaved, else (j, j + pairs); the others stay.
+ *   q [rows][heads][d], k [rows][kv_heads][d] of type dtype, ldq and ldk elements from row to row (at least the row's own length), their outputs
+ *   in rows of ldqo and ldko; gamma fp32 [d], one of queries and one of keys (NULL: 1); pos int32 [rows]; freq fp64 [pairs], radians a position.
+ * Angles in fp64, the rest in fp32: the sum of a head's squares has to be finite there.  d <= 256, 2 pairs <= d.  With pairs == 0 pos and freq
+ * may be NULL.  q_out may be q where ldqo == ldq, and k_out k where ldko == ldk. */
+typedef struct {
+    int32_t rows, heads, kv_heads, d, pairs, interleaved, dtype;
+    int64_t ldq, ldk, ldqo, ldko;
+} ppo_qk_norm_desc;
+
+size_t ppo_qk_norm_rotate_workspace_bytes(const ppo_qk_norm_desc *desc);
+
+int ppo_qk_norm_rotate_fwd(const ppo_qk_norm_desc *desc, float eps, const void *dev_q, const void *dev_k, const float *dev_gamma_q,
+                           const float *dev_gamma_k, const int32_t *dev_pos, const double *dev_freq, void *dev_q_out, void *dev_k_out, void *stream);
+
+/* Gradients of q and k (strided as these) from those of q_out and k_out (strided as those; dev_dq may be dev_dq_out where ldqo == ldq, likewise
+ * dev_dk), and from q and k as they came in.  dL/dgamma of queries and of keys fp32 [d] (each may be NULL) are added to (accumulate != 0) or
+ * written.  Sums in a fixed order: same bits run to run.  The workspace is needed where one of them is wanted. */
+int ppo_qk_norm_rotate_bwd(const ppo_qk_norm_desc *desc, float eps, const void *dev_q, const void *dev_k, const float *dev_gamma_q,
+                           const float *dev_gamma_k, const int32_t *dev_pos, const double *dev_freq, const void *dev_dq_out, const void *dev_dk_out,
+                           void *dev_dq, void *dev_dk, float *dev_dgamma_q, float *dev_dgamma_k, int accumulate, void *dev_workspace,
+                           size_t ws_bytes, void *stream);
+
 /* Number of kernels and memsets the library has enqueued in this process so far (all handles, all
  * devices).  Instrumentation for benchmarks that report launches per step; no counterpart in the paper. */
 uint64_t ppo_launch_count(void);

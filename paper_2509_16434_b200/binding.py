@@ -34,6 +34,9 @@ EXPORTS = [
     "ppo_decay_attention_workspace_bytes", "ppo_decay_attention_fwd", "ppo_decay_attention_bwd", "ppo_decay_attention_step",
     "ppo_group_norm_workspace_bytes", "ppo_group_norm_fwd", "ppo_group_norm_bwd", "ppo_token_logp",
     "ppo_token_loss_workspace_bytes", "ppo_token_loss_fwd_bwd",
+    "ppo_causal_conv_workspace_bytes", "ppo_causal_conv_fwd", "ppo_causal_conv_bwd", "ppo_causal_conv_step",
+    "ppo_selective_scan_workspace_bytes", "ppo_selective_scan_fwd", "ppo_selective_scan_bwd", "ppo_selective_scan_step",
+    "ppo_qk_norm_rotate_workspace_bytes", "ppo_qk_norm_rotate_fwd", "ppo_qk_norm_rotate_bwd",
 ]
 
 
@@ -75,6 +78,20 @@ class TokenDesc(C.Structure):
 
 class TokenLossCoef(C.Structure):
     _fields_ = [(n, C.c_float) for n in ("clip_low", "clip_high", "kl_coef", "ent_coef", "grad_scale")] + [("B_total", C.c_int32)]
+
+
+class CausalConvDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "Be", "C", "width", "act", "dtype")] + [("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
+class SelectiveScanDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "Be", "channels", "N", "groups", "dtype", "softplus")] + \
+               [(n, C.c_int64) for n in ("ldx", "lddt", "ldb", "ldc", "ldz", "ldy")]
+
+
+class QkNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "heads", "kv_heads", "d", "pairs", "interleaved", "dtype")] + \
+               [(n, C.c_int64) for n in ("ldq", "ldk", "ldqo", "ldko")]
 
 
 _lib = None
@@ -156,6 +173,20 @@ def lib():
         L.ppo_token_loss_workspace_bytes.argtypes = [C.POINTER(TokenDesc)]
         L.ppo_token_loss_fwd_bwd.argtypes = [C.POINTER(TokenDesc), C.POINTER(TokenLossCoef)] + [C.c_void_p] * 7 + \
                                             [C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ppo_causal_conv_workspace_bytes.restype = C.c_size_t
+        L.ppo_causal_conv_workspace_bytes.argtypes = [C.POINTER(CausalConvDesc)]
+        L.ppo_causal_conv_fwd.argtypes = [C.POINTER(CausalConvDesc)] + [C.c_void_p] * 8
+        L.ppo_causal_conv_bwd.argtypes = [C.POINTER(CausalConvDesc)] + [C.c_void_p] * 11 + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ppo_causal_conv_step.argtypes = [C.POINTER(CausalConvDesc)] + [C.c_void_p] * 7
+        L.ppo_selective_scan_workspace_bytes.restype = C.c_size_t
+        L.ppo_selective_scan_workspace_bytes.argtypes = [C.POINTER(SelectiveScanDesc), C.c_int]
+        L.ppo_selective_scan_fwd.argtypes = [C.POINTER(SelectiveScanDesc)] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p]
+        L.ppo_selective_scan_bwd.argtypes = [C.POINTER(SelectiveScanDesc)] + [C.c_void_p] * 21 + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ppo_selective_scan_step.argtypes = [C.POINTER(SelectiveScanDesc)] + [C.c_void_p] * 12
+        L.ppo_qk_norm_rotate_workspace_bytes.restype = C.c_size_t
+        L.ppo_qk_norm_rotate_workspace_bytes.argtypes = [C.POINTER(QkNormDesc)]
+        L.ppo_qk_norm_rotate_fwd.argtypes = [C.POINTER(QkNormDesc), C.c_float] + [C.c_void_p] * 9
+        L.ppo_qk_norm_rotate_bwd.argtypes = [C.POINTER(QkNormDesc), C.c_float] + [C.c_void_p] * 12 + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -702,3 +733,176 @@ def ppo_token_loss_fwd_bwd(logits, tokens, logp_old, adv, B_total: int, dlogits,
                                         _dense(f, dev, logp_ref, _F32, row), _dense(f, dev, adv, _F32, row), _dense(f, dev, weight, _F32, row), pg, ldg,
                                         _dense(f, dev, logp_out, _F32, row), _dense(f, dev, loss_out, _F32, (5,)), int(accumulate), ws, size,
                                         _stream_on(f, dev, stream)), f)
+
+
+def ppo_causal_conv_workspace_bytes(x, width: int) -> int:
+    """Bytes the gradients of this x [T,Be,C] need (0: none)."""
+    T, Be, n = x.shape
+    d = CausalConvDesc(T, Be, n, width, 0, _DTYPES[x.dtype], n, n)
+    return lib().ppo_causal_conv_workspace_bytes(C.byref(d))
+
+
+def _conv(where: str, x, weight, y, act: str, lead: int):
+    """Descriptor, device, and the addresses of x, weight, y."""
+    dev, shape = _device_of(where, x, _DTYPES), tuple(x.shape)
+    if act not in _ACTS:
+        raise PpoError(1, where)
+    if len(shape) != lead + 1 or weight.dim() != 2:
+        raise PpoError(2, where)
+    px, ldx = _operand(where, dev, x, x.dtype, shape, lead)
+    py, ldy = _operand(where, dev, y, x.dtype, shape, lead)
+    T, Be = shape[:2] if lead == 2 else (1, shape[0])
+    n, width = shape[lead], weight.shape[1]
+    return CausalConvDesc(T, Be, n, width, _ACTS[act], _DTYPES[x.dtype], ldx, ldy), dev, px, _dense(where, dev, weight, _F32, (n, width)), py
+
+
+def ppo_causal_conv_fwd(x, weight, bias, y, done=None, state_in=None, state_out=None, act: str = "none", stream=None):
+    """x, y [T,Be,C] (fp32, bf16 or fp16; rows may be parts of wider ones), weight fp32 [C,width], bias fp32 [C] or None; done uint8 [T,Be];
+    states [Be,width-1,C] of the type of x; act: none, relu or silu."""
+    f = "ppo_causal_conv_fwd"
+    d, dev, px, pw, py = _conv(f, x, weight, y, act, 2)
+    state = (d.Be, d.width - 1, d.C)
+    _check(lib().ppo_causal_conv_fwd(C.byref(d), px, pw, _dense(f, dev, bias, _F32, (d.C,)), _dense(f, dev, done, _U8, (d.T, d.Be)),
+                                     _dense(f, dev, state_in, x.dtype, state), py, _dense(f, dev, state_out, x.dtype, state), _stream_on(f, dev, stream)), f)
+
+
+def ppo_causal_conv_bwd(x, weight, bias, dy, dx, dweight=None, dbias=None, done=None, state_in=None, dstate_out=None, dstate_in=None, act: str = "none",
+                        accumulate: bool = False, workspace=None, stream=None):
+    """dx (strided as x) and dstate_in from dy and dstate_out; dweight fp32 [C,width], dbias fp32 [C] (added to where accumulate)."""
+    f = "ppo_causal_conv_bwd"
+    d, dev, px, pw, py = _conv(f, x, weight, dy, act, 2)
+    pd, ldd = _operand(f, dev, dx, x.dtype, tuple(x.shape), 2)
+    if ldd != d.ldx:
+        raise PpoError(2, f)
+    state = (d.Be, d.width - 1, d.C)
+    ws, size = _space(f, dev, workspace)
+    _check(lib().ppo_causal_conv_bwd(C.byref(d), px, pw, _dense(f, dev, bias, _F32, (d.C,)), _dense(f, dev, done, _U8, (d.T, d.Be)),
+                                     _dense(f, dev, state_in, x.dtype, state), py, _dense(f, dev, dstate_out, x.dtype, state), pd,
+                                     _dense(f, dev, dstate_in, x.dtype, state), _dense(f, dev, dweight, _F32, (d.C, d.width)),
+                                     _dense(f, dev, dbias, _F32, (d.C,)), int(accumulate), ws, size, _stream_on(f, dev, stream)), f)
+
+
+def ppo_causal_conv_step(x, weight, bias, state, y, start=None, act: str = "none", stream=None):
+    """One decision: x, y [Be,C], state [Be,width-1,C] in place; start uint8 [Be]: envs that start from a zero state."""
+    f = "ppo_causal_conv_step"
+    d, dev, px, pw, py = _conv(f, x, weight, y, act, 1)
+    _check(lib().ppo_causal_conv_step(C.byref(d), px, pw, _dense(f, dev, bias, _F32, (d.C,)), _dense(f, dev, start, _U8, (d.Be,)),
+                                      _dense(f, dev, state, x.dtype, (d.Be, d.width - 1, d.C)), py, _stream_on(f, dev, stream)), f)
+
+
+def ppo_selective_scan_workspace_bytes(x, B, backward: bool) -> int:
+    """Bytes the calls with these x [T,Be,C], B [T,Be,groups,N] need (0: none)."""
+    (T, Be, n), (groups, N) = x.shape, B.shape[2:]
+    d = SelectiveScanDesc(T, Be, n, N, groups, _DTYPES[x.dtype], 0, n, n, groups * N, groups * N, n, n)
+    return lib().ppo_selective_scan_workspace_bytes(C.byref(d), int(backward))
+
+
+def _scan(where: str, x, dt, A, B, Cm, D, z, dt_bias, y, softplus: bool, lead: int):
+    """Descriptor, device, and the addresses of x, dt, A, B, C, D, z, dt_bias; and that of y."""
+    dev, dtype, shape = _device_of(where, x, _DTYPES), x.dtype, tuple(x.shape)
+    if len(shape) != lead + 1 or B.dim() != lead + 2:
+        raise PpoError(2, where)
+    n, few = shape[lead], shape[:lead] + tuple(B.shape[lead:])
+    px, ldx = _operand(where, dev, x, dtype, shape, lead)
+    pt, ldt = _operand(where, dev, dt, dtype, shape, lead)
+    pb, ldb = _operand(where, dev, B, dtype, few, lead)
+    pc, ldc = _operand(where, dev, Cm, dtype, few, lead)
+    pz, ldz = (None, n) if z is None else _operand(where, dev, z, dtype, shape, lead)
+    py, ldy = _operand(where, dev, y, dtype, shape, lead)
+    T, Be = shape[:2] if lead == 2 else (1, shape[0])
+    groups, N = few[lead:]
+    d = SelectiveScanDesc(T, Be, n, N, groups, _DTYPES[dtype], int(softplus), ldx, ldt, ldb, ldc, ldz, ldy)
+    return d, dev, (px, pt, _dense(where, dev, A, _F32, (n, N)), pb, pc, _dense(where, dev, D, _F32, (n,)), pz, _dense(where, dev, dt_bias, _F32, (n,))), py
+
+
+def ppo_selective_scan_fwd(x, dt, A, B, C_, y, D=None, z=None, dt_bias=None, softplus: bool = True, done=None, state_in=None, state_out=None,
+                           workspace=None, stream=None):
+    """x, dt, z, y [T,Be,channels], B, C_ [T,Be,groups,N] (fp32, bf16 or fp16; rows may be parts of wider ones); A fp32 [channels,N]; D, dt_bias
+    fp32 [channels]; done uint8 [T,Be]; states fp32 [Be,channels,N]."""
+    f = "ppo_selective_scan_fwd"
+    d, dev, ins, py = _scan(f, x, dt, A, B, C_, D, z, dt_bias, y, softplus, 2)
+    state = (d.Be, d.channels, d.N)
+    ws, size = _space(f, dev, workspace)
+    _check(lib().ppo_selective_scan_fwd(C.byref(d), *ins, _dense(f, dev, done, _U8, (d.T, d.Be)), _dense(f, dev, state_in, _F32, state), py,
+                                        _dense(f, dev, state_out, _F32, state), ws, size, _stream_on(f, dev, stream)), f)
+
+
+def ppo_selective_scan_bwd(x, dt, A, B, C_, dy, dx, ddt, dA, dB, dC, D=None, z=None, dt_bias=None, softplus: bool = True, done=None, state_in=None,
+                           dstate_out=None, dD=None, dz=None, ddt_bias=None, dstate_in=None, accumulate: bool = False, workspace=None, stream=None):
+    """dx, ddt, dB, dC, dz (strided as x, dt, B, C_, z) and dstate_in from dy and dstate_out; dA, dD, ddt_bias fp32 (None: not wanted; added
+    to where accumulate)."""
+    f = "ppo_selective_scan_bwd"
+    d, dev, ins, py = _scan(f, x, dt, A, B, C_, D, z, dt_bias, dy, softplus, 2)
+    if (z is None) != (dz is None):
+        raise PpoError(1, f)
+    out = []
+    for t, like, ld in ((dx, x, d.ldx), (ddt, dt, d.lddt), (dB, B, d.ldb), (dC, C_, d.ldc), (dz, z, d.ldz)):
+        if t is None and like is None:
+            out.append(None)
+            continue
+        p, ldt = _operand(f, dev, t, x.dtype, tuple(like.shape), 2)
+        if ldt != ld:
+            raise PpoError(2, f)
+        out.append(p)
+    state, n = (d.Be, d.channels, d.N), (d.channels,)
+    ws, size = _space(f, dev, workspace)
+    _check(lib().ppo_selective_scan_bwd(C.byref(d), *ins, _dense(f, dev, done, _U8, (d.T, d.Be)), _dense(f, dev, state_in, _F32, state), py,
+                                        _dense(f, dev, dstate_out, _F32, state), out[0], out[1], _dense(f, dev, dA, _F32, n + (d.N,)), out[2], out[3],
+                                        _dense(f, dev, dD, _F32, n), out[4], _dense(f, dev, ddt_bias, _F32, n), _dense(f, dev, dstate_in, _F32, state),
+                                        int(accumulate), ws, size, _stream_on(f, dev, stream)), f)
+
+
+def ppo_selective_scan_step(x, dt, A, B, C_, state, y, D=None, z=None, dt_bias=None, softplus: bool = True, start=None, stream=None):
+    """One decision: x, dt, z, y [Be,channels], B, C_ [Be,groups,N], state fp32 [Be,channels,N] in place; start uint8 [Be]: envs that start
+    from a zero state."""
+    f = "ppo_selective_scan_step"
+    d, dev, ins, py = _scan(f, x, dt, A, B, C_, D, z, dt_bias, y, softplus, 1)
+    _check(lib().ppo_selective_scan_step(C.byref(d), *ins, _dense(f, dev, start, _U8, (d.Be,)), _dense(f, dev, state, _F32, (d.Be, d.channels, d.N)), py,
+                                         _stream_on(f, dev, stream)), f)
+
+
+def ppo_qk_norm_rotate_workspace_bytes(q, k) -> int:
+    """Bytes the gradients of gamma need with these q [rows,heads,d], k [rows,kv_heads,d]."""
+    (rows, heads, n), kv = q.shape, k.shape[1]
+    d = QkNormDesc(rows, heads, kv, n, 0, 0, _DTYPES[q.dtype], heads * n, kv * n, heads * n, kv * n)
+    return lib().ppo_qk_norm_rotate_workspace_bytes(C.byref(d))
+
+
+def _qk(where: str, q, k, gamma_q, gamma_k, pos, freq, q_out, k_out, interleaved: bool):
+    """Descriptor, device, the addresses of q, k, gamma_q, gamma_k, pos, freq, and those of q_out, k_out."""
+    dev, shape = _device_of(where, q, _DTYPES), tuple(q.shape)
+    if len(shape) != 3 or k.dim() != 3:
+        raise PpoError(2, where)
+    (rows, heads, n), kv = shape, k.shape[1]
+    few = (rows, kv, n)
+    pq, ldq = _operand(where, dev, q, q.dtype, shape, 1)
+    pk, ldk = _operand(where, dev, k, q.dtype, few, 1)
+    po, ldqo = _operand(where, dev, q_out, q.dtype, shape, 1)
+    pp, ldko = _operand(where, dev, k_out, q.dtype, few, 1)
+    pairs = 0 if freq is None else freq.numel()
+    d = QkNormDesc(rows, heads, kv, n, pairs, int(interleaved), _DTYPES[q.dtype], ldq, ldk, ldqo, ldko)
+    ins = (pq, pk, _dense(where, dev, gamma_q, _F32, (n,)), _dense(where, dev, gamma_k, _F32, (n,)), _dense(where, dev, pos, _I32, (rows,)),
+           _dense(where, dev, freq, torch.float64, (pairs,)))
+    return d, dev, ins, (po, pp)
+
+
+def ppo_qk_norm_rotate_fwd(q, k, gamma_q, gamma_k, pos, freq, q_out, k_out, eps: float = 1e-6, interleaved: bool = False, stream=None):
+    """q, q_out [rows,heads,d], k, k_out [rows,kv_heads,d] (fp32, bf16 or fp16; rows may be parts of wider ones; an output may be its input); gamma
+    fp32 [d] or None; pos int32 [rows]; freq fp64 [pairs], radians a position (None: no rotation)."""
+    f = "ppo_qk_norm_rotate_fwd"
+    d, dev, ins, outs = _qk(f, q, k, gamma_q, gamma_k, pos, freq, q_out, k_out, interleaved)
+    _check(lib().ppo_qk_norm_rotate_fwd(C.byref(d), eps, *ins, *outs, _stream_on(f, dev, stream)), f)
+
+
+def ppo_qk_norm_rotate_bwd(q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, dq, dk, dgamma_q=None, dgamma_k=None, eps: float = 1e-6,
+                           interleaved: bool = False, accumulate: bool = False, workspace=None, stream=None):
+    """dq, dk (strided as q, k) from dq_out, dk_out; dgamma_q, dgamma_k fp32 [d] (None: not wanted; added to where accumulate)."""
+    f = "ppo_qk_norm_rotate_bwd"
+    d, dev, ins, outs = _qk(f, q, k, gamma_q, gamma_k, pos, freq, dq_out, dk_out, interleaved)
+    pq, ldq = _operand(f, dev, dq, q.dtype, tuple(q.shape), 1)
+    pk, ldk = _operand(f, dev, dk, q.dtype, tuple(k.shape), 1)
+    if ldq != d.ldq or ldk != d.ldk:
+        raise PpoError(2, f)
+    ws, size = _space(f, dev, workspace)
+    _check(lib().ppo_qk_norm_rotate_bwd(C.byref(d), eps, *ins, *outs, pq, pk, _dense(f, dev, dgamma_q, _F32, (d.d,)), _dense(f, dev, dgamma_k, _F32, (d.d,)),
+                                        int(accumulate), ws, size, _stream_on(f, dev, stream)), f)
