@@ -9,6 +9,7 @@
 // in front of it: the gradient of the state that is left enters the last step undecayed, that of the state that came in
 // leaves the first one decayed.
 #include "elem.cuh"
+#include "pair32.cuh"
 #include "tcgen05.cuh"
 #include "tma_host.cuh"
 
@@ -37,29 +38,6 @@ struct Sweep {
 
 // decay ** n
 __device__ __forceinline__ float power(float log2_decay, int n) { return n == 0 ? 1.f : exp2f((float)n * log2_decay); }
-
-// Two 32-bit numbers in a register pair, one instruction for both.
-typedef unsigned long long pair32;
-__device__ __forceinline__ pair32 pair_of(float a, float b) {
-    pair32 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 parts(pair32 p) {
-    float2 f;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
-    return f;
-}
-__device__ __forceinline__ pair32 fma2(pair32 a, pair32 b, pair32 c) {
-    pair32 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ pair32 mul2(pair32 a, pair32 b) {
-    pair32 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 
 // ---- step by step (32 bits, and rows that no vector fits) ----
 //

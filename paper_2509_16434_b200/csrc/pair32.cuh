@@ -1,0 +1,24 @@
+// Two 32-bit numbers in a register pair: arithmetic on both in one instruction.
+#pragma once
+
+typedef unsigned long long pair32;
+__device__ __forceinline__ pair32 pair_of(float a, float b) {
+    pair32 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 parts(pair32 p) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+    return f;
+}
+__device__ __forceinline__ pair32 fma2(pair32 a, pair32 b, pair32 c) {
+    pair32 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ pair32 mul2(pair32 a, pair32 b) {
+    pair32 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
