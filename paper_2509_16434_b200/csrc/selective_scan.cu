@@ -171,30 +171,59 @@ __device__ __forceinline__ void get_floats(const float *p, float (&v)[V]) {
     }
 }
 
-// The rows of B or C, padded with zeros to NP elements; zeros behind the last step.
+// The rows of B or C, padded with zeros to NP elements, each of them twice, as packed arithmetic on two channels takes it; zeros behind the
+// last step.
 template <typename T, int NP>
-__device__ __forceinline__ void stage_few(float (&to)[kSteps][NP], const T *from, long long step, int rows, int N) {
+__device__ __forceinline__ void stage_few(float2 (&to)[kSteps][NP], const T *from, long long step, int rows, int N) {
     for (int i = threadIdx.x; i < kSteps * NP; i += kThreads) {
         const int t = i / NP, n = i % NP;
-        to[t][n] = t < rows && n < N ? to_f32(from[t * step + n]) : 0.f;
+        const float v = t < rows && n < N ? to_f32(from[t * step + n]) : 0.f;
+        to[t][n] = make_float2(v, v);
     }
+}
+// Of the tile's channels; zeros where there are none.
+template <int CT>
+__device__ __forceinline__ void stage_channels(float (&to)[CT], const float *from, const Work &w) {
+    for (int i = threadIdx.x; i < CT; i += kThreads) to[i] = from && w.c0 + i < w.c1 ? from[w.c0 + i] : 0.f;
+}
+// Bit r: the flag of step t + r, 0 behind the last one.
+__device__ __forceinline__ uint32_t flags_of(const ScanArgs &a, int e, int t, int rows) {
+    const int r = threadIdx.x % 32;
+    return a.done ? __ballot_sync(0xffffffffu, r < min(rows, kSteps) && t + r >= 0 && a.done[(long long)(t + r) * a.Be + e]) : 0u;
 }
 
 // NPT elements of four channels' states, [e][channel][N] in memory; zeros where there are none.
 template <int NPT>
 __device__ __forceinline__ void load_state(const float *from, const ScanArgs &a, int e, int c, int c1, int n0, float (&h)[4][NPT]) {
+    const bool whole = NPT == 4 && a.N % 4 == 0 && (reinterpret_cast<uintptr_t>(from) & 15) == 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
 #pragma unroll
-        for (int n = 0; n < NPT; ++n) h[j][n] = from && c + j < c1 && n0 + n < a.N ? from[((long long)e * a.channels + c + j) * a.N + n0 + n] : 0.f;
+        for (int n = 0; n < NPT; ++n) h[j][n] = 0.f;
+        if (!from || c + j >= c1) continue;
+        const float *p = from + ((long long)e * a.channels + c + j) * a.N + n0;
+        if (whole) {
+            if constexpr (NPT == 4) {
+                if (n0 < a.N) {
+                    const float4 f = *reinterpret_cast<const float4 *>(p);
+                    h[j][0] = f.x, h[j][1] = f.y, h[j][2] = f.z, h[j][3] = f.w;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NPT; ++n)
+                if (n0 + n < a.N) h[j][n] = p[n];
+        }
+    }
 }
 template <int NPT>
-__device__ __forceinline__ void store_state(float *to, const ScanArgs &a, int e, int c, int c1, int n0, const float (&h)[4][NPT], bool aligned = true) {
+__device__ __forceinline__ void store_state(float *to, const ScanArgs &a, int e, int c, int c1, int n0, const float (&h)[4][NPT]) {
+    const bool whole = NPT == 4 && a.N % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & 15) == 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         if (c + j >= c1) break;
         float *p = to + ((long long)e * a.channels + c + j) * a.N + n0;
-        if (NPT == 4 && aligned && a.N % 4 == 0) {
+        if (whole) {
             if (n0 < a.N) *reinterpret_cast<float4 *>(p) = make_float4(h[j][0], h[j][1], h[j][2], h[j][3]);
         } else {
 #pragma unroll
@@ -237,13 +266,16 @@ __device__ __forceinline__ void load_pairs(const float *p, pair32 (&v)[2]) {
     v[0] = u.x, v[1] = u.y;
 }
 template <int NPT>
-__device__ __forceinline__ void load_few(const float *p, float (&v)[NPT]) {
-    if constexpr (NPT == 4) {
-        const float4 f = *reinterpret_cast<const float4 *>(p);
-        v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+__device__ __forceinline__ void load_few(const float2 *p, pair32 (&v)[NPT]) {
+    if constexpr (NPT % 2 == 0) {
+#pragma unroll
+        for (int n = 0; n < NPT; n += 2) {
+            const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(p + n);
+            v[n] = u.x, v[n + 1] = u.y;
+        }
     } else {
 #pragma unroll
-        for (int n = 0; n < NPT; ++n) v[n] = p[n];
+        for (int n = 0; n < NPT; ++n) v[n] = *reinterpret_cast<const pair32 *>(p + n);
     }
 }
 
@@ -283,14 +315,14 @@ enum Mode {
 };
 
 template <typename T, int NPT, int NL, int MODE, bool VEC>
-__global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
+__global__ void __launch_bounds__(kThreads, MODE == BOTH ? 3 : 5) scan_kernel(ScanArgs a) {
     grid_wait();
     using S = Shape<NPT, NL>;
     constexpr int CT = S::CT, NP = S::NP;
     constexpr bool WITH_C = MODE == OUTPUT || MODE == BOTH, WITH_DY = MODE == BOTH;
     using R = Rows<T, CT, VEC>;
-    __shared__ alignas(16) float sd[kSteps][CT], su[kSteps][CT], sg[WITH_DY ? kSteps : 1][CT], sB[kSteps][NP], sC[WITH_C ? kSteps : 1][NP];
-    __shared__ uint8_t flag[kSteps];
+    __shared__ alignas(16) float sd[kSteps][CT], su[kSteps][CT], sg[WITH_DY ? kSteps : 1][CT], sD[CT], sbias[CT];
+    __shared__ alignas(16) float2 sB[kSteps][NP], sC[kSteps][WITH_C ? NP : 1];
     const Work w = work_of<CT>(a, blockIdx.x % a.tiles, blockIdx.x / a.tiles);
     const int lane = threadIdx.x % 32, ln = lane % NL, c = w.c0 + (threadIdx.x / 32 * S::GROUPS + lane / NL) * 4, n0 = ln * NPT, local = c - w.c0;
     const int cols = w.c1 - w.c0;
@@ -327,6 +359,9 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
     R rx, rt;
     rx.fetch(x + w.t0 * sx, sx, w.t1 - w.t0, cols);
     rt.fetch(dt + w.t0 * st, st, w.t1 - w.t0, cols);
+    stage_channels(sbias, a.bias, w);
+    if constexpr (MODE == OUTPUT) stage_channels(sD, a.D, w);
+    __syncthreads();
     float total[4] = {};
     bool cut = false;
     for (int t = w.t0; t < w.t1; t += kSteps) {
@@ -342,11 +377,13 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
             if (r >= kSteps) break;
             float d[R::V] = {}, u[R::V] = {}, g[R::V] = {};
             if (r < rows && l < cols) {
+                float b[R::V];
                 rt.get(i, d);
                 rx.get(i, u);
+                get_floats(&sbias[l], b);
 #pragma unroll
                 for (int v = 0; v < R::V; ++v) {
-                    d[v] += a.bias ? a.bias[w.c0 + l + v] : 0.f;
+                    d[v] += b[v];
                     if (a.softplus) d[v] = softplus(d[v]);
                     u[v] *= d[v];
                 }
@@ -366,7 +403,7 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
         }
         stage_few<T, NP>(sB, B + t * sb, sb, rows, a.N);
         if constexpr (WITH_C) stage_few<T, NP>(sC, C + t * sc, sc, rows, a.N);
-        if (threadIdx.x < kSteps) flag[threadIdx.x] = a.done && (int)threadIdx.x < rows && a.done[(long long)(t + threadIdx.x) * a.Be + w.e];
+        const uint32_t flag = flags_of(a, w.e, t, rows);
         __syncthreads();
         if (t + kSteps < w.t1) {
             rx.fetch(x + (t + kSteps) * sx, sx, rows - kSteps, cols);
@@ -382,7 +419,7 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 pair32 d[2], u[2], g[2], acc[2] = {0, 0};
-                float b[NPT], cc[NPT];
+                pair32 b[NPT], cc[NPT];
                 load_pairs(&sd[s + k][local], d);
                 load_pairs(&su[s + k][local], u);
                 load_few<NPT>(&sB[s + k][n0], b);
@@ -393,11 +430,11 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         const pair32 f = exp2_pair(mul2(d[p], A[n][p]));
-                        h[n][p] = fma2(f, h[n][p], mul2(u[p], twice(b[n])));
-                        if constexpr (MODE == OUTPUT) acc[p] = fma2(twice(cc[n]), h[n][p], acc[p]);
+                        h[n][p] = fma2(f, h[n][p], mul2(u[p], b[n]));
+                        if constexpr (MODE == OUTPUT) acc[p] = fma2(cc[n], h[n][p], acc[p]);
                         if constexpr (WITH_DY) {
                             P[n][p] = mul2(P[n][p], f);
-                            if (!cut) G[n][p] = fma2(mul2(P[n][p], g[p]), twice(cc[n]), G[n][p]);
+                            if (!cut) G[n][p] = fma2(mul2(P[n][p], g[p]), cc[n], G[n][p]);
                         }
                     }
                 if constexpr (MODE == OUTPUT) {
@@ -408,7 +445,7 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
                     const float2 p = parts(d[0]), q = parts(d[1]);
                     total[0] += p.x, total[1] += p.y, total[2] += q.x, total[3] += q.y;
                 }
-                if (flag[s + k]) {
+                if (flag >> (s + k) & 1) {
                     cut = true;
 #pragma unroll
                     for (int n = 0; n < NPT; ++n) h[n][0] = h[n][1] = 0;
@@ -438,9 +475,11 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
                 float o[R::V], v[R::V];
                 get_floats(&sd[r][l], o);
                 if (a.D) {
+                    float D[R::V];
                     again.get(i, v);
+                    get_floats(&sD[l], D);
 #pragma unroll
-                    for (int k = 0; k < R::V; ++k) o[k] = fmaf(a.D[w.c0 + l + k], v[k], o[k]);
+                    for (int k = 0; k < R::V; ++k) o[k] = fmaf(D[k], v[k], o[k]);
                 }
                 if (z) {
                     gate.get(i, v);
@@ -480,14 +519,21 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
 // Four steps at a time, backwards: from the states in front of them forwards once more, which leaves the factors and exp(d A) h' of the
 // four steps in registers (and y and the sums of dC on the way), then backwards over these.  A block goes through as many envs, or
 // segments, as fall to it and keeps its shares of the parameters' gradients.
+// A long sum as two numbers: what hi rounds away stays in lo (Knuth's error of a sum).
+__device__ __forceinline__ void add_to(float &hi, float &lo, float v) {
+    const float sum = __fadd_rn(hi, v), w = __fsub_rn(sum, hi);
+    lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(sum, w)), __fsub_rn(v, w));
+    hi = sum;
+}
+
 template <typename T, int NL, bool VEC>
 struct GradShared {
     static constexpr int CT = Shape<4, NL>::CT, NP = Shape<4, NL>::NP;
-    float sd[kSteps][CT], su[kSteps][CT], sg[kSteps][CT], sy[kSteps][CT], sB[kSteps][NP], sC[kSteps][NP];
+    float sd[kSteps][CT], su[kSteps][CT], sg[kSteps][CT], sy[kSteps][CT], sD[CT], sbias[CT];
+    float2 sB[kSteps][NP], sC[kSteps][NP];
     float few[kThreads / 32][kSteps][2 * NP];
     float mark[4][4][kThreads * 4];
-    float kept[2][kThreads * Rows<T, CT, VEC>::V];
-    uint8_t flag[kSteps + 1];  // flag[r]: of the step in front of row r
+    float dA[2][16][kThreads], kept[2][2][Rows<T, CT, VEC>::V][kThreads];  // [..][2]: hi and lo of the sums
 };
 
 __device__ __forceinline__ void copy_async(float *to, const float *from) {
@@ -520,8 +566,14 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
 #pragma unroll
         for (int n = 0; n < NPT; ++n) dA[n][0] = dA[n][1] = 0;
     }
+    stage_channels(s.sD, a.D, w);
+    stage_channels(s.sbias, a.bias, w);
 #pragma unroll
-    for (int v = 0; v < R::V; ++v) s.kept[0][threadIdx.x * R::V + v] = s.kept[1][threadIdx.x * R::V + v] = 0.f;
+    for (int v = 0; v < R::V; ++v)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s.kept[k / 2][k % 2][v][threadIdx.x] = 0.f;
+#pragma unroll
+    for (int n = 0; n < 16; ++n) s.dA[0][n][threadIdx.x] = s.dA[1][n][threadIdx.x] = 0.f;
 
     const long long items = (long long)a.Be * a.nseg;
     for (long long item = slice; item < items; item += a.parts) {
@@ -541,6 +593,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
         }
         for (int t = w.t0 + (w.t1 - 1 - w.t0) / kSteps * kSteps; t >= w.t0; t -= kSteps) {
             const int rows = w.t1 - t;
+            const uint32_t flag = flags_of(a, w.e, t, rows);
             __syncthreads();  // the tile behind is done with
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
@@ -557,10 +610,6 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                 if (z) rz.fetch(z + t * sz, sz, rows, cols);
                 stage_few<T, NP>(s.sB, B + t * sb, sb, rows, a.N);
                 stage_few<T, NP>(s.sC, C + t * sc, sc, rows, a.N);
-                if (threadIdx.x <= kSteps) {
-                    const int r = t + (int)threadIdx.x - 1;
-                    s.flag[threadIdx.x] = a.done && r >= 0 && r < w.t1 && a.done[(long long)r * a.Be + w.e];
-                }
 #pragma unroll
                 for (int i = 0; i < R::PASSES; ++i) {
                     const int r = R::row(i), l = R::col(i);
@@ -570,9 +619,11 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                         rt.get(i, d);
                         rx.get(i, u);
                         rg.get(i, v);
+                        float b[R::V];
+                        get_floats(&s.sbias[l], b);
 #pragma unroll
                         for (int k = 0; k < R::V; ++k) {
-                            d[k] += a.bias ? a.bias[w.c0 + l + k] : 0.f;
+                            d[k] += b[k];
                             if (a.softplus) d[k] = softplus(d[k]);
                             u[k] *= d[k];
                         }
@@ -605,13 +656,13 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                         for (int i = 0; i < 2; ++i) {
                             const int r = r0 + k + i;
                             pair32 d[2], u[2], v[2], acc[2] = {0, 0};
-                            float b[NPT], cc[NPT];
+                            pair32 b[NPT], cc[NPT];
                             load_pairs(&s.sd[r][local], d);
                             load_pairs(&s.su[r][local], u);
                             load_pairs(&s.sg[r][local], v);
                             load_few<NPT>(&s.sB[r][n0], b);
                             load_few<NPT>(&s.sC[r][n0], cc);
-                            if (k + i > 0 && s.flag[r]) {
+                            if (k + i > 0 && flag >> (r - 1) & 1) {
 #pragma unroll
                                 for (int n = 0; n < NPT; ++n) h[n][0] = h[n][1] = 0;
                             }
@@ -623,8 +674,8 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                                     const pair32 e = exp2_pair(mul2(d[p], A[n][p])), qq = mul2(e, h[n][p]);
                                     f[k + i][n][p] = e;
                                     q[k + i][n][p] = qq;
-                                    h[n][p] = fma2(u[p], twice(b[n]), qq);
-                                    acc[p] = fma2(twice(cc[n]), h[n][p], acc[p]);
+                                    h[n][p] = fma2(u[p], b[n], qq);
+                                    acc[p] = fma2(cc[n], h[n][p], acc[p]);
                                     sum = fma2(v[p], h[n][p], sum);
                                 }
                                 const float2 e = parts(sum);
@@ -650,13 +701,13 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                     for (int i = 1; i >= 0; --i) {
                         const int r = r0 + k + i;
                         pair32 d[2], u[2], v[2], s1[2] = {0, 0}, s2[2] = {0, 0};
-                        float b[NPT], cc[NPT];
+                        pair32 b[NPT], cc[NPT];
                         load_pairs(&s.sd[r][local], d);
                         load_pairs(&s.su[r][local], u);
                         load_pairs(&s.sg[r][local], v);
                         load_few<NPT>(&s.sB[r][n0], b);
                         load_few<NPT>(&s.sC[r][n0], cc);
-                        if (s.flag[r + 1]) {
+                        if (flag >> r & 1) {
 #pragma unroll
                             for (int n = 0; n < NPT; ++n) g[n][0] = g[n][1] = 0;
                         }
@@ -665,9 +716,9 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                             pair32 sum = 0;
 #pragma unroll
                             for (int p = 0; p < 2; ++p) {
-                                g[n][p] = fma2(twice(cc[n]), v[p], g[n][p]);
+                                g[n][p] = fma2(cc[n], v[p], g[n][p]);
                                 sum = fma2(g[n][p], u[p], sum);
-                                s1[p] = fma2(g[n][p], twice(b[n]), s1[p]);
+                                s1[p] = fma2(g[n][p], b[n], s1[p]);
                                 const pair32 qq = mul2(g[n][p], q[k + i][n][p]);
                                 s2[p] = fma2(qq, A[n][p], s2[p]);
                                 dA[n][p] = fma2(qq, d[p], dA[n][p]);
@@ -711,12 +762,14 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                 if (z) rz.fetch(z + t * sz, sz, rows, cols);
                 T *dx = static_cast<T *>(a.dx) + w.e * a.ldx + w.c0, *ddt = static_cast<T *>(a.ddt) + w.e * a.lddt + w.c0;
                 T *dz = z ? static_cast<T *>(a.dz) + w.e * a.ldz + w.c0 : nullptr;
-                float *kept = &s.kept[0][threadIdx.x * R::V], *kept2 = &s.kept[1][threadIdx.x * R::V];
+                float sumD[R::V] = {}, sumb[R::V] = {};
 #pragma unroll
                 for (int i = 0; i < R::PASSES; ++i) {
                     const int r = R::row(i), l = R::col(i);
                     if (r >= kSteps || r >= rows || l >= cols) continue;
-                    float d[R::V], s1[R::V], s2[R::V], xv[R::V], tv[R::V], gv[R::V], o[R::V];
+                    float d[R::V], s1[R::V], s2[R::V], xv[R::V], tv[R::V], gv[R::V], D[R::V], bias[R::V], o[R::V];
+                    get_floats(&s.sD[l], D);
+                    get_floats(&s.sbias[l], bias);
                     get_floats(&s.sd[r][l], d);
                     get_floats(&s.su[r][l], s1);
                     get_floats(&s.sg[r][l], s2);
@@ -729,7 +782,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                         get_floats(&s.sy[r][l], yv);
 #pragma unroll
                         for (int k = 0; k < R::V; ++k) {
-                            const float p = sigmoid(zv[k]), all = a.D ? fmaf(a.D[w.c0 + l + k], xv[k], yv[k]) : yv[k];
+                            const float p = sigmoid(zv[k]), all = a.D ? fmaf(D[k], xv[k], yv[k]) : yv[k];
                             o[k] = gv[k] * all * (p * fmaf(zv[k], 1.f - p, 1.f));
                             gv[k] *= zv[k] * p;
                         }
@@ -737,19 +790,30 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                     }
 #pragma unroll
                     for (int k = 0; k < R::V; ++k) {
-                        o[k] = a.D ? fmaf(d[k], s1[k], a.D[w.c0 + l + k] * gv[k]) : d[k] * s1[k];
-                        kept[k] = fmaf(gv[k], xv[k], kept[k]);
+                        o[k] = a.D ? fmaf(d[k], s1[k], D[k] * gv[k]) : d[k] * s1[k];
+                        sumD[k] = fmaf(gv[k], xv[k], sumD[k]);
                     }
                     R::put(dx + (t + r) * sx + l, o);
 #pragma unroll
                     for (int k = 0; k < R::V; ++k) {
                         o[k] = fmaf(xv[k], s1[k], kLn2 * s2[k]);
-                        if (a.softplus) o[k] *= sigmoid(tv[k] + (a.bias ? a.bias[w.c0 + l + k] : 0.f));
-                        kept2[k] += o[k];
+                        if (a.softplus) o[k] *= sigmoid(tv[k] + bias[k]);
+                        sumb[k] += o[k];
                     }
                     R::put(ddt + (t + r) * st + l, o);
                 }
+#pragma unroll
+                for (int k = 0; k < R::V; ++k) {
+                    add_to(s.kept[0][0][k][threadIdx.x], s.kept[0][1][k][threadIdx.x], sumD[k]);
+                    add_to(s.kept[1][0][k][threadIdx.x], s.kept[1][1][k][threadIdx.x], sumb[k]);
+                }
             }
+            float f[4][NPT];
+            unpack<NPT>(dA, f);
+#pragma unroll
+            for (int n = 0; n < 16; ++n) add_to(s.dA[0][n][threadIdx.x], s.dA[1][n][threadIdx.x], f[n / 4][n % 4]);
+#pragma unroll
+            for (int n = 0; n < NPT; ++n) dA[n][0] = dA[n][1] = 0;
         }
         if (a.dstate_in && w.t0 == 0) {
             float f[4][NPT];
@@ -761,15 +825,19 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
     float *part = a.part + (size_t)slice * a.channels * (a.N + 2);
     {
         float f[4][NPT];
-        unpack<NPT>(dA, f);
-        store_state<NPT>(part, a, 0, c, w.c1, n0, f, false);  // a share starts at any element
+#pragma unroll
+        for (int n = 0; n < 16; ++n) f[n / 4][n % 4] = s.dA[0][n][threadIdx.x] + s.dA[1][n][threadIdx.x];
+        store_state<NPT>(part, a, 0, c, w.c1, n0, f);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * CT; i += kThreads) {
         const int k = i / CT, l = i % CT;
         if (l >= cols) continue;
         float sum = 0.f;
-        for (int r = 0; r < kThreads / R::COLS; ++r) sum += s.kept[k][(r * R::COLS + l / R::V) * R::V + l % R::V];
+        for (int r = 0; r < kThreads / R::COLS; ++r) {
+            const int i = r * R::COLS + l / R::V;
+            sum += s.kept[k][0][l % R::V][i] + s.kept[k][1][l % R::V][i];
+        }
         part[(size_t)a.channels * (a.N + k) + w.c0 + l] = sum;
     }
 }
@@ -894,7 +962,7 @@ Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     if (bwd) {
         p.mark = ppo_cdiv(d->T, 4) * held;
         p.few = (size_t)d->T * d->Be * p.tiles * 2 * p.NP;
-        const long long items = (long long)d->Be * p.nseg, per = ppo_cdiv(2 * 148, p.tiles);
+        const long long items = (long long)d->Be * p.nseg, per = p.tiles < 2 * 148 ? 2 * 148 / p.tiles : 1;  // one round of two blocks an SM
         p.parts = (int)(items < per ? items : per);
         p.part = up((size_t)p.parts * d->channels * (d->N + 2));
     }
