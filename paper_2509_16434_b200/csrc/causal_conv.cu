@@ -1,11 +1,16 @@
 // Causal convolution of each channel along the steps of an env, with an activation, and its gradients.
 //
-// A thread takes V neighbouring channels over a run of steps of one env and keeps the last width - 1 inputs in registers: every input is
-// read once (but for the width - 1 in front of a run) and every output written once.  Sums in 32 bits.
+// A thread takes V neighbouring channels over a run of steps of one env: every input is read once (but for the width - 1 in front of a run) and
+// every output written once; the last width - 1 inputs stay in registers.  Bound by memory as long as enough is on its way: a thread copies
+// its own rows ahead into a ring in shared memory, a batch of rows at a time, and waits for nobody else.  Arithmetic on two channels in one
+// instruction, sums in 32 bits.
 #include "elem.cuh"
+#include "pair32.cuh"
 #include "param_sum.cuh"
 
 namespace {
+
+constexpr int kThreads = 128;
 
 struct ConvArgs {
     const void *x, *state_in, *dy, *dstate_out;
@@ -29,47 +34,79 @@ __device__ __forceinline__ float grad_act(float z, int act) {
     return act == PPO_ACT_RELU && !(z > 0.f) ? 0.f : 1.f;
 }
 
-// V elements, aligned to all of them.
+// V elements, aligned to all of them, as they lie in memory; V / 2 pairs of them in 32 bits (one, with a second channel of zeros, where V is 1).
 template <typename T, int V>
-__device__ __forceinline__ void load(const T *p, float (&v)[V]) {
-    if constexpr (V == 1) {
-        v[0] = to_f32(*p);
-    } else if constexpr (V * sizeof(T) == 16) {
-        Vec<T> r;
-        r.raw = *reinterpret_cast<const uint4 *>(p);
-        r.get(v);
-    } else {
-        static_assert(V * sizeof(T) == 8);
-        const uint2 h = *reinterpret_cast<const uint2 *>(p);
-        Vec<T> r;
-        float all[8];
-        r.raw = make_uint4(h.x, h.y, 0, 0);
-        r.get(all);
+struct Raw {
+    static constexpr int BYTES = V * sizeof(T), PAIRS = (V + 1) / 2;
+    static_assert(V == 1 || BYTES == 8 || BYTES == 16);
+    using Word = std::conditional_t<V == 1, T, std::conditional_t<BYTES == 8, uint2, uint4>>;
+    Word w;
+    __device__ __forceinline__ void load(const T *p) { w = *reinterpret_cast<const Word *>(p); }
+    __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<Word *>(p) = w; }
+    __device__ __forceinline__ void get(pair32 (&v)[PAIRS]) const {
+        if constexpr (V == 1) {
+            v[0] = pair_of(to_f32(w), 0.f);
+        } else {
+            Vec<T> all;
+            float f[Vec<T>::N];
+            if constexpr (BYTES == 8) all.raw = make_uint4(w.x, w.y, 0, 0);
+            else all.raw = w;
+            all.get(f);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = all[i];
+            for (int i = 0; i < PAIRS; ++i) v[i] = pair_of(f[2 * i], f[2 * i + 1]);
+        }
     }
+    __device__ __forceinline__ void set(const pair32 (&v)[PAIRS]) {
+        if constexpr (V == 1) {
+            w = from_f32<T>(parts(v[0]).x);
+        } else {
+            Vec<T> all;
+            float f[Vec<T>::N] = {};
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                const float2 p = parts(v[i]);
+                f[2 * i] = p.x, f[2 * i + 1] = p.y;
+            }
+            all.set(f);
+            if constexpr (BYTES == 8) w = make_uint2(all.raw.x, all.raw.y);
+            else w = all.raw;
+        }
+    }
+};
+
+// A thread's places in a ring of shared memory: S rows of V elements.
+template <typename T, int V, int S>
+struct Ring {
+    using Word = typename Raw<T, V>::Word;
+    Word (*at)[kThreads];
+    __device__ __forceinline__ void copy(int slot, const T *from) const {
+        if constexpr (V == 1) {
+            at[slot][threadIdx.x] = *from;
+        } else {
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(&at[slot][threadIdx.x]);
+            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(Raw<T, V>::BYTES) : "memory");
+        }
+    }
+    __device__ __forceinline__ void get(int slot, Raw<T, V> &r) const { r.w = at[slot][threadIdx.x]; }
+};
+__device__ __forceinline__ void batch_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All batches but the N youngest have arrived.
+template <int N>
+__device__ __forceinline__ void batch_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-template <typename T, int V>
-__device__ __forceinline__ void store(T *p, const float (&v)[V]) {
-    if constexpr (V == 1) {
-        *p = from_f32<T>(v[0]);
-    } else if constexpr (V * sizeof(T) == 16) {
-        Vec<T> r;
-        r.set(v);
-        *reinterpret_cast<uint4 *>(p) = r.raw;
-    } else {
-        float all[8] = {};
-#pragma unroll
-        for (int i = 0; i < V; ++i) all[i] = v[i];
-        Vec<T> r;
-        r.set(all);
-        *reinterpret_cast<uint2 *>(p) = make_uint2(r.raw.x, r.raw.y);
-    }
+__device__ __forceinline__ pair32 map2(pair32 p, int act) {
+    const float2 f = parts(p);
+    return pair_of(activate(f.x, act), activate(f.y, act));
+}
+__device__ __forceinline__ pair32 grad2(pair32 p, int act) {
+    const float2 f = parts(p);
+    return pair_of(grad_act(f.x, act), grad_act(f.y, act));
 }
 
 // The inputs in front of step t0 that it sees: rows t0 - W + 1 + i as h[i]; returns which ones lie behind the last flag (bit i).
-template <typename T, int W, int V>
-__device__ __forceinline__ int history(const ConvArgs &a, const T *x, const T *state, int e, int t0, float (&h)[W - 1][V]) {
+template <typename T, int W, int V, int P>
+__device__ __forceinline__ int history(const ConvArgs &a, const T *x, const T *state, int e, int t0, pair32 (&h)[W - 1][P]) {
     int seen = 0;
     bool cut = false;
 #pragma unroll
@@ -77,30 +114,52 @@ __device__ __forceinline__ int history(const ConvArgs &a, const T *x, const T *s
         const int t = t0 - W + 1 + i;
         if (t >= 0 && a.done && a.done[(long long)t * a.Be + e]) cut = true;
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[i][v] = 0.f;
+        for (int p = 0; p < P; ++p) h[i][p] = 0;
         if (cut) continue;
         seen |= 1 << i;
-        if (t >= 0) load(x + (long long)t * a.Be * a.ldx, h[i]);
-        else if (state) load(state + (long long)(t + W - 1) * a.C, h[i]);
+        Raw<T, V> r;
+        if (t >= 0) r.load(x + (long long)t * a.Be * a.ldx);
+        else if (state) r.load(state + (long long)(t + W - 1) * a.C);
+        else continue;
+        r.get(h[i]);
     }
     return seen;
 }
 
-template <int W, int V>
-__device__ __forceinline__ void params(const ConvArgs &a, int c, float (&w)[W][V], float (&b)[V]) {
+template <int W, int V, int P>
+__device__ __forceinline__ void params(const ConvArgs &a, int c, pair32 (&w)[W][P], pair32 (&b)[P]) {
+    float f[2 * P * W] = {}, g[2 * P] = {};
+    const float *from = a.weight + (long long)c * W;
+    if (V % 4 == 0 && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        b[v] = a.bias ? a.bias[c + v] : 0.f;
+        for (int i = 0; i < V * W / 4; ++i) {
+            const float4 v = reinterpret_cast<const float4 *>(from)[i];
+            f[4 * i] = v.x, f[4 * i + 1] = v.y, f[4 * i + 2] = v.z, f[4 * i + 3] = v.w;
+        }
+    } else {
 #pragma unroll
-        for (int i = 0; i < W; ++i) w[i][v] = a.weight[(long long)(c + v) * W + i];
+        for (int i = 0; i < V * W; ++i) f[i] = from[i];
+    }
+    if (a.bias) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) g[v] = a.bias[c + v];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        b[p] = pair_of(g[2 * p], g[2 * p + 1]);
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i][p] = pair_of(f[2 * p * W + i], f[(2 * p + 1) * W + i]);
     }
 }
 
 template <typename T, int W, int V>
-__global__ void __launch_bounds__(256) conv_fwd_kernel(ConvArgs a) {
+__global__ void __launch_bounds__(kThreads) conv_fwd_kernel(ConvArgs a) {
     grid_wait();
+    constexpr int P = Raw<T, V>::PAIRS, AHEAD = 3;  // batches of 4 rows on their way
+    __shared__ typename Raw<T, V>::Word rows[4 * (AHEAD + 1)][kThreads];
+    const Ring<T, V, 4 * (AHEAD + 1)> ring = {rows};
     const int cols = a.C / V;
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, item = id / cols;
+    const long long id = (long long)blockIdx.x * kThreads + threadIdx.x, item = id / cols;
     const int c = (int)(id - item * cols) * V, tile = (int)(item / a.Be), e = (int)(item - (long long)tile * a.Be);
     if (tile >= a.tiles) return;
     const T *x = static_cast<const T *>(a.x) + e * a.ldx + c, *state = nullptr;
@@ -108,36 +167,49 @@ __global__ void __launch_bounds__(256) conv_fwd_kernel(ConvArgs a) {
     const uint8_t *done = a.done ? a.done + e : nullptr;
     const long long sx = (long long)a.Be * a.ldx, sy = (long long)a.Be * a.ldy;
     if (a.state_in) state = static_cast<const T *>(a.state_in) + (long long)e * (W - 1) * a.C + c;
-    float w[W][V], b[V], h[W - 1][V];
-    params(a, c, w, b);
     const int t0 = tile * a.run, t1 = min(a.T, t0 + a.run);
+    const auto fetch = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (t + j < t1) ring.copy((t - t0 + j) % (4 * (AHEAD + 1)), x + (t + j) * sx);
+        batch_end();
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fetch(t0 + 4 * i);
+    pair32 w[W][P], b[P], h[W - 1][P];
+    params<W, V>(a, c, w, b);
     history<T, W, V>(a, x, state, e, t0, h);
     for (int t = t0; t < t1; t += 4) {
-        float in[4][V];
+        fetch(t + 4 * AHEAD);
         bool flag[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            flag[j] = false;
-            if (t + j < t1) {
-                load(x + (t + j) * sx, in[j]);
-                flag[j] = done && done[(long long)(t + j) * a.Be];
-            }
-        }
+        for (int j = 0; j < 4; ++j) flag[j] = done && t + j < t1 && done[(long long)(t + j) * a.Be];
+        batch_wait<AHEAD>();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (t + j >= t1) break;
-            float o[V];
+            Raw<T, V> r;
+            pair32 in[P], o[P];
+            ring.get((t - t0 + j) % (4 * (AHEAD + 1)), r);
+            r.get(in);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float s = b[v];
+            for (int p = 0; p < P; ++p) {
+                pair32 s = b[p];
 #pragma unroll
-                for (int i = 0; i < W - 1; ++i) s = fmaf(w[i][v], h[i][v], s);
-                o[v] = activate(fmaf(w[W - 1][v], in[j][v], s), a.act);
+                for (int i = 0; i < W - 1; ++i) s = fma2(w[i][p], h[i][p], s);
+                o[p] = map2(fma2(w[W - 1][p], in[p], s), a.act);
 #pragma unroll
-                for (int i = 0; i < W - 2; ++i) h[i][v] = flag[j] ? 0.f : h[i + 1][v];
-                h[W - 2][v] = flag[j] ? 0.f : in[j][v];
+                for (int i = 0; i < W - 2; ++i) h[i][p] = h[i + 1][p];
+                h[W - 2][p] = in[p];
             }
-            store(y + (t + j) * sy, o);
+            if (flag[j]) {
+#pragma unroll
+                for (int i = 0; i < W - 1; ++i)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) h[i][p] = 0;
+            }
+            r.set(o);
+            r.store(y + (t + j) * sy);
         }
     }
     // the first run writes the state that is left: it alone reads the one that came in, which may be the same
@@ -145,54 +217,71 @@ __global__ void __launch_bounds__(256) conv_fwd_kernel(ConvArgs a) {
         history<T, W, V>(a, x, state, e, a.T, h);
         T *out = static_cast<T *>(a.state_out) + (long long)e * (W - 1) * a.C + c;
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i) store(out + (long long)i * a.C, h[i]);
+        for (int i = 0; i < W - 1; ++i) {
+            Raw<T, V> r;
+            r.set(h[i]);
+            r.store(out + (long long)i * a.C);
+        }
     }
 }
 
-// One step, the state in place.
+// One step of `envs` envs, the state in place.
 template <typename T, int W, int V>
-__global__ void __launch_bounds__(256) conv_step_kernel(ConvArgs a) {
+__global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs a, int envs) {
     grid_wait();
+    constexpr int P = Raw<T, V>::PAIRS;
     const int cols = a.C / V;
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, e = id / cols;
-    const int c = (int)(id - e * cols) * V;
-    if (e >= a.Be) return;
-    float w[W][V], b[V], h[W][V], o[V];
-    T *state = static_cast<T *>(a.state_out) + e * (W - 1) * a.C + c;
-    const bool start = a.done && a.done[e];
-    load(static_cast<const T *>(a.x) + e * a.ldx + c, h[W - 1]);
+    const long long id = (long long)blockIdx.x * kThreads + threadIdx.x, item = id / cols;
+    const int c = (int)(id - item * cols) * V;
+    if (item * envs >= a.Be) return;
+    const int e0 = (int)item * envs, e1 = min(a.Be, e0 + envs);
+    pair32 w[W][P], b[P];
+    params<W, V>(a, c, w, b);
+#pragma unroll 2
+    for (int e = e0; e < e1; ++e) {
+        Raw<T, V> r[W];
+        T *state = static_cast<T *>(a.state_out) + (long long)e * (W - 1) * a.C + c;
+        const bool start = a.done && a.done[e];
+        r[W - 1].load(static_cast<const T *>(a.x) + e * a.ldx + c);
 #pragma unroll
-    for (int i = 0; i < W - 1; ++i) load(state + (long long)i * a.C, h[i]);
-    params(a, c, w, b);
+        for (int i = 0; i < W - 1; ++i) {
+            r[i].w = typename Raw<T, V>::Word{};
+            if (!start) r[i].load(state + (long long)i * a.C);
+        }
+        pair32 s[P], v[P];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        float s = b[v];
+        for (int p = 0; p < P; ++p) s[p] = b[p];
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            if (i < W - 1 && start) h[i][v] = 0.f;
-            s = fmaf(w[i][v], h[i][v], s);
-        }
-        o[v] = activate(s, a.act);
-    }
-    store(static_cast<T *>(a.y) + e * a.ldy + c, o);
+            r[i].get(v);
 #pragma unroll
-    for (int i = 0; i < W - 1; ++i) store(state + (long long)i * a.C, h[i + 1]);
+            for (int p = 0; p < P; ++p) s[p] = fma2(w[i][p], v[p], s[p]);
+            if (i > 0) r[i].store(state + (long long)(i - 1) * a.C);
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) s[p] = map2(s[p], a.act);
+        r[0].set(s);
+        r[0].store(static_cast<T *>(a.y) + e * a.ldy + c);
+    }
 }
 
 // Gradients of a run: its own rows' sums are made again, those of the width - 1 steps behind it as well, whose gradients reach back.  Threads
 // (p, l): l columns of V channels side by side, p runs; a thread takes every so many of them and keeps its shares of the gradients of weight
 // and bias.
 template <typename T, int W, int V>
-__global__ void __launch_bounds__(256) conv_bwd_kernel(ConvArgs a, int lanes) {
+__global__ void __launch_bounds__(kThreads) conv_bwd_kernel(ConvArgs a, int lanes) {
     grid_wait();
-    __shared__ float sum[256];
-    const int l = threadIdx.x % lanes, p = threadIdx.x / lanes, rows = 256 / lanes, c = (blockIdx.x * lanes + l) * V;
+    constexpr int P = Raw<T, V>::PAIRS, AHEAD = 3, S = 2 * (AHEAD + 1);  // batches of 2 rows on their way
+    __shared__ typename Raw<T, V>::Word rx[S][kThreads], rg[S][kThreads];
+    __shared__ float sum[kThreads];
+    const Ring<T, V, S> xs = {rx}, gs = {rg};
+    const int l = threadIdx.x % lanes, p0 = threadIdx.x / lanes, rows = kThreads / lanes, c = (blockIdx.x * lanes + l) * V;
     const bool on = c < a.C;
     const long long sx = (long long)a.Be * a.ldx, sy = (long long)a.Be * a.ldy;
-    float w[W][V] = {}, b[V] = {}, dw[W][V] = {}, db[V] = {};
-    if (on) params(a, c, w, b);
+    pair32 w[W][P] = {}, b[P] = {}, dw[W][P] = {}, db[P] = {};
+    if (on) params<W, V>(a, c, w, b);
     const long long items = (long long)a.Be * a.tiles;
-    for (long long item = (long long)blockIdx.y * rows + p; on && item < items; item += (long long)gridDim.y * rows) {
+    for (long long item = (long long)blockIdx.y * rows + p0; on && item < items; item += (long long)gridDim.y * rows) {
         const int tile = (int)(item / a.Be), e = (int)(item - (long long)tile * a.Be);
         const T *x = static_cast<const T *>(a.x) + e * a.ldx + c, *dy = static_cast<const T *>(a.dy) + e * a.ldy + c;
         T *dx = static_cast<T *>(a.dx) + e * a.ldx + c;
@@ -201,52 +290,101 @@ __global__ void __launch_bounds__(256) conv_bwd_kernel(ConvArgs a, int lanes) {
         const T *state = a.state_in ? static_cast<const T *>(a.state_in) + states : nullptr;
         T *dstate = a.dstate_in ? static_cast<T *>(a.dstate_in) + states : nullptr;
         const int t0 = tile * a.run, t1 = min(a.T, t0 + a.run), end = min(a.T, t1 + W - 1);
-        float h[W - 1][V], acc[W][V] = {};
-        int seen = history<T, W, V>(a, x, state, e, t0, h) | 1 << (W - 1);
-        const auto put = [&](int t, const float (&g)[V]) {  // the gradient of the input of step t is complete
-            if (t >= t0 && t < t1) store(dx + t * sx, g);
-            else if (t < 0 && t >= 1 - W && dstate) store(dstate + (long long)(t + W - 1) * a.C, g);
-        };
-        for (int t = t0; t < end; ++t) {
-            float in[V], g[V];
-            load(x + t * sx, in);
-            load(dy + t * sy, g);
-            const bool flag = done && done[(long long)t * a.Be];
+        const auto fetch = [&](int t) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float s = b[v];
-#pragma unroll
-                for (int i = 0; i < W - 1; ++i) s = fmaf(w[i][v], h[i][v], s);
-                g[v] *= grad_act(fmaf(w[W - 1][v], in[v], s), a.act);
-#pragma unroll
-                for (int i = 0; i < W; ++i) acc[i][v] = fmaf(w[i][v], seen >> i & 1 ? g[v] : 0.f, acc[i][v]);
-                if (t < t1) {
-#pragma unroll
-                    for (int i = 0; i < W - 1; ++i) dw[i][v] = fmaf(g[v], h[i][v], dw[i][v]);
-                    dw[W - 1][v] = fmaf(g[v], in[v], dw[W - 1][v]);
-                    db[v] += g[v];
+            for (int j = 0; j < 2; ++j)
+                if (t + j < end) {
+                    xs.copy((t - t0 + j) % S, x + (t + j) * sx);
+                    gs.copy((t - t0 + j) % S, dy + (t + j) * sy);
                 }
+            batch_end();
+        };
 #pragma unroll
-                for (int i = 0; i < W - 2; ++i) h[i][v] = flag ? 0.f : h[i + 1][v];
-                h[W - 2][v] = flag ? 0.f : in[v];
+        for (int i = 0; i < AHEAD; ++i) fetch(t0 + 2 * i);
+        pair32 h[W - 1][P], acc[W][P] = {};
+        int seen = history<T, W, V>(a, x, state, e, t0, h) | 1 << (W - 1);
+        const auto put = [&](int t, const pair32 (&g)[P]) {  // the gradient of the input of step t is complete
+            Raw<T, V> r;
+            r.set(g);
+            if (t >= t0 && t < t1) r.store(dx + t * sx);
+            else if (t < 0 && t >= 1 - W && dstate) r.store(dstate + (long long)(t + W - 1) * a.C);
+        };
+        for (int t = t0; t < end; t += 2) {
+            fetch(t + 2 * AHEAD);
+            bool flag[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) flag[j] = done && t + j < end && done[(long long)(t + j) * a.Be];
+            batch_wait<AHEAD>();
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (t + j >= end) break;
+                pair32 in[P], g[P];
+                Raw<T, V> r;
+                xs.get((t - t0 + j) % S, r);
+                r.get(in);
+                gs.get((t - t0 + j) % S, r);
+                r.get(g);
+                const bool own = t + j < t1;
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    pair32 s = b[p];
+#pragma unroll
+                    for (int i = 0; i < W - 1; ++i) s = fma2(w[i][p], h[i][p], s);
+                    g[p] = mul2(g[p], grad2(fma2(w[W - 1][p], in[p], s), a.act));
+                }
+                if (seen == (1 << W) - 1) {
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+#pragma unroll
+                        for (int p = 0; p < P; ++p) acc[i][p] = fma2(w[i][p], g[p], acc[i][p]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+                        if (seen >> i & 1) {
+#pragma unroll
+                            for (int p = 0; p < P; ++p) acc[i][p] = fma2(w[i][p], g[p], acc[i][p]);
+                        }
+                }
+                if (own) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+#pragma unroll
+                        for (int i = 0; i < W - 1; ++i) dw[i][p] = fma2(g[p], h[i][p], dw[i][p]);
+                        dw[W - 1][p] = fma2(g[p], in[p], dw[W - 1][p]);
+                        db[p] = add2(db[p], g[p]);
+                    }
+                }
+                put(t + j - W + 1, acc[0]);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+#pragma unroll
+                    for (int i = 0; i < W - 1; ++i) acc[i][p] = acc[i + 1][p];
+                    acc[W - 1][p] = 0;
+#pragma unroll
+                    for (int i = 0; i < W - 2; ++i) h[i][p] = h[i + 1][p];
+                    h[W - 2][p] = in[p];
+                }
+                seen = seen >> 1 | 1 << (W - 1);
+                if (flag[j]) {
+                    seen = 1 << (W - 1);
+#pragma unroll
+                    for (int i = 0; i < W - 1; ++i)
+#pragma unroll
+                        for (int p = 0; p < P; ++p) h[i][p] = 0;
+                }
             }
-            put(t - W + 1, acc[0]);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-#pragma unroll
-                for (int i = 0; i < W - 1; ++i) acc[i][v] = acc[i + 1][v];
-                acc[W - 1][v] = 0.f;
-            }
-            seen = (flag ? 0 : seen >> 1) | 1 << (W - 1);
         }
+        batch_wait<0>();
         if (end == a.T) {  // what is left of the sequence, and reaches on into the state
 #pragma unroll
             for (int i = 0; i < W - 1; ++i) {
                 if (a.dstate_out && seen >> i & 1) {
-                    float s[V];
-                    load(static_cast<const T *>(a.dstate_out) + states + (long long)i * a.C, s);
+                    Raw<T, V> r;
+                    pair32 s[P];
+                    r.load(static_cast<const T *>(a.dstate_out) + states + (long long)i * a.C);
+                    r.get(s);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) acc[i][v] += s[v];
+                    for (int p = 0; p < P; ++p) acc[i][p] = add2(acc[i][p], s[p]);
                 }
                 put(a.T - W + 1 + i, acc[i]);
             }
@@ -258,10 +396,11 @@ __global__ void __launch_bounds__(256) conv_bwd_kernel(ConvArgs a, int lanes) {
     for (int i = 0; i <= W; ++i) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
+            const float2 f = parts(i < W ? dw[i < W ? i : 0][v / 2] : db[v / 2]);
             __syncthreads();
-            sum[threadIdx.x] = i < W ? dw[i < W ? i : 0][v] : db[v];
+            sum[threadIdx.x] = v % 2 ? f.y : f.x;
             __syncthreads();
-            if (p == 0 && on) {
+            if (p0 == 0 && on) {
                 float s = 0.f;
                 for (int k = 0; k < rows; ++k) s += sum[k * lanes + l];
                 part[i < W ? (size_t)(c + v) * W + i : (size_t)a.C * W + c + v] = s;
@@ -283,6 +422,8 @@ bool misaligned(std::initializer_list<const void *> ps, size_t a) {
     return false;
 }
 
+constexpr int kRun = 32;  // steps of a run
+
 ConvArgs args(const ppo_causal_conv_desc *d, const void *x, const float *weight, const float *bias, const uint8_t *done) {
     ConvArgs a = {};
     a.x = x;
@@ -295,7 +436,7 @@ ConvArgs args(const ppo_causal_conv_desc *d, const void *x, const float *weight,
     a.Be = d->Be;
     a.C = d->C;
     a.act = d->act;
-    a.run = 32;
+    a.run = kRun;
     a.tiles = ppo_cdiv(d->T, a.run);
     return a;
 }
@@ -308,8 +449,8 @@ BwdPlan plan_bwd(const ppo_causal_conv_desc *d, int V) {
     BwdPlan p = {1, 0, 0};
     while (p.lanes < 32 && p.lanes * V < d->C) p.lanes *= 2;
     p.cols = ppo_cdiv(d->C, p.lanes * V);
-    const long long items = (long long)d->Be * ppo_cdiv(d->T, 32);
-    const long long all = (items + 256 / p.lanes - 1) / (256 / p.lanes), want = ppo_cdiv(4 * 148, p.cols);
+    const long long items = (long long)d->Be * ppo_cdiv(d->T, kRun);
+    const long long all = (items + kThreads / p.lanes - 1) / (kThreads / p.lanes), want = ppo_cdiv(4 * 148, p.cols);
     p.blocks = (int)(all < want ? all : want);
     return p;
 }
@@ -333,13 +474,22 @@ int with_width(const ppo_causal_conv_desc *d, F &&fn) {
 bool vectors(const ppo_causal_conv_desc *d, int V, std::initializer_list<const void *> ps) {
     return d->C % V == 0 && d->ldx % V == 0 && d->ldy % V == 0 && !misaligned(ps, V * elem_bytes(d->dtype));
 }
-constexpr int kV = 4;
+// Channels of a thread: 16 bytes of them, but 8 bytes of 16-bit gradients, whose shares need the registers.
+constexpr int kBwdV = 4;
+// fn(T{}, width, V)
+template <typename F>
+int with_columns(const ppo_causal_conv_desc *d, bool vec, F &&fn) {
+    return with_width(d, [&](auto t, auto w) -> int {
+        constexpr int V = 16 / (int)sizeof(t);
+        return vec ? fn(t, w, std::integral_constant<int, V>{}) : fn(t, w, std::integral_constant<int, 1>{});
+    });
+}
 
 }  // namespace
 
 extern "C" size_t ppo_causal_conv_workspace_bytes(const ppo_causal_conv_desc *d) {
     if (check(d) != PPO_OK) return 0;
-    const int one = plan_bwd(d, 1).blocks, many = plan_bwd(d, kV).blocks;
+    const int one = plan_bwd(d, 1).blocks, many = plan_bwd(d, kBwdV).blocks;
     return (size_t)(one > many ? one : many) * d->C * (d->width + 1) * sizeof(float);
 }
 
@@ -352,13 +502,12 @@ extern "C" int ppo_causal_conv_fwd(const ppo_causal_conv_desc *d, const void *x,
     a.state_in = state_in;
     a.y = y;
     a.state_out = state_out;
-    const bool vec = vectors(d, kV, {x, y, state_in, state_out});
-    const long long threads = (long long)(vec ? d->C / kV : d->C) * d->Be * a.tiles;
-    if (threads > 0x7fffffffll * 256) return PPO_ERR_UNSUPPORTED;
-    return with_width(d, [&](auto t, auto w) -> int {
-        using T = decltype(t);
-        constexpr int W = decltype(w)::value;
-        return ppo_launch(vec ? conv_fwd_kernel<T, W, kV> : conv_fwd_kernel<T, W, 1>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0,
+    const int V = 16 / (int)elem_bytes(d->dtype);
+    const bool vec = vectors(d, V, {x, y, state_in, state_out});
+    const long long blocks = ((long long)(vec ? d->C / V : d->C) * d->Be * a.tiles + kThreads - 1) / kThreads;
+    if (blocks > 0x7fffffffll) return PPO_ERR_UNSUPPORTED;
+    return with_columns(d, vec, [&](auto t, auto w, auto v) -> int {
+        return ppo_launch(conv_fwd_kernel<decltype(t), decltype(w)::value, decltype(v)::value>, dim3((unsigned)blocks), dim3(kThreads), 0,
                           static_cast<cudaStream_t>(stream), a);
     });
 }
@@ -378,14 +527,14 @@ extern "C" int ppo_causal_conv_bwd(const ppo_causal_conv_desc *d, const void *x,
     a.dstate_out = dstate_out;
     a.dx = dx;
     a.dstate_in = dstate_in;
-    const bool params = dweight || dbias, vec = vectors(d, kV, {x, dy, dx, state_in, dstate_out, dstate_in});
+    const bool params = dweight || dbias, vec = vectors(d, kBwdV, {x, dy, dx, state_in, dstate_out, dstate_in});
     a.part = params ? static_cast<float *>(workspace) : nullptr;
-    const BwdPlan p = plan_bwd(d, vec ? kV : 1);
+    const BwdPlan p = plan_bwd(d, vec ? kBwdV : 1);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     PPO_TRY(with_width(d, [&](auto t, auto w) -> int {
         using T = decltype(t);
         constexpr int W = decltype(w)::value;
-        return ppo_launch(vec ? conv_bwd_kernel<T, W, kV> : conv_bwd_kernel<T, W, 1>, dim3(p.cols, p.blocks), dim3(256), 0, st, a, p.lanes);
+        return ppo_launch(vec ? conv_bwd_kernel<T, W, kBwdV> : conv_bwd_kernel<T, W, 1>, dim3(p.cols, p.blocks), dim3(kThreads), 0, st, a, p.lanes);
     }));
     return params ? ppo_param_sum(a.part, p.blocks, {{dweight, dbias, nullptr}, {d->C * d->width, d->C, 0}}, accumulate, st) : PPO_OK;
 }
@@ -399,13 +548,14 @@ extern "C" int ppo_causal_conv_step(const ppo_causal_conv_desc *d, const void *x
     ConvArgs a = args(d, x, weight, bias, start);
     a.y = y;
     a.state_out = state;
-    const bool vec = vectors(d, kV, {x, y, state});
-    const long long threads = (long long)(vec ? d->C / kV : d->C) * d->Be;
-    if (threads > 0x7fffffffll * 256) return PPO_ERR_UNSUPPORTED;
-    return with_width(d, [&](auto t, auto w) -> int {
-        using T = decltype(t);
-        constexpr int W = decltype(w)::value;
-        return ppo_launch(vec ? conv_step_kernel<T, W, kV> : conv_step_kernel<T, W, 1>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0,
-                          static_cast<cudaStream_t>(stream), a);
+    const int V = 16 / (int)elem_bytes(d->dtype);
+    const bool vec = vectors(d, V, {x, y, state});
+    const long long cols = vec ? d->C / V : d->C, most = cols * d->Be / (148 * 1024);  // envs of a thread: as many as leave every SM 1024 threads
+    const int envs = most < 1 ? 1 : most > 8 ? 8 : (int)most;
+    const long long blocks = (cols * ppo_cdiv(d->Be, envs) + kThreads - 1) / kThreads;
+    if (blocks > 0x7fffffffll) return PPO_ERR_UNSUPPORTED;
+    return with_columns(d, vec, [&](auto t, auto w, auto v) -> int {
+        return ppo_launch(conv_step_kernel<decltype(t), decltype(w)::value, decltype(v)::value>, dim3((unsigned)blocks), dim3(kThreads), 0,
+                          static_cast<cudaStream_t>(stream), a, envs);
     });
 }

@@ -22,3 +22,8 @@ __device__ __forceinline__ pair32 mul2(pair32 a, pair32 b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+__device__ __forceinline__ pair32 add2(pair32 a, pair32 b) {
+    pair32 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
