@@ -4,6 +4,7 @@
 // every output written once; the last width - 1 inputs stay in registers.  Bound by memory as long as enough is on its way: a thread copies
 // its own rows ahead into a ring in shared memory, a batch of rows at a time, and waits for nobody else.  Arithmetic on two channels in one
 // instruction, sums in 32 bits.
+#include "approx.cuh"
 #include "elem.cuh"
 #include "pair32.cuh"
 #include "param_sum.cuh"
@@ -21,18 +22,6 @@ struct ConvArgs {
     long long ldx, ldy;
     int T, Be, C, act, run, tiles;
 };
-
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
-__device__ __forceinline__ float activate(float z, int act) {
-    return act == PPO_ACT_SILU ? z * sigmoid(z) : act == PPO_ACT_RELU ? (z < 0.f ? 0.f : z) : z;
-}
-__device__ __forceinline__ float grad_act(float z, int act) {
-    if (act == PPO_ACT_SILU) {
-        const float p = sigmoid(z);
-        return p * fmaf(z, 1.f - p, 1.f);
-    }
-    return act == PPO_ACT_RELU && !(z > 0.f) ? 0.f : 1.f;
-}
 
 // V elements, aligned to all of them, as they lie in memory; V / 2 pairs of them in 32 bits (one, with a second channel of zeros, where V is 1).
 template <typename T, int V>
@@ -95,13 +84,42 @@ template <int N>
 __device__ __forceinline__ void batch_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ pair32 map2(pair32 p, int act) {
-    const float2 f = parts(p);
-    return pair_of(activate(f.x, act), activate(f.y, act));
+// sigmoid of both
+__device__ __forceinline__ pair32 sigmoid2(pair32 z) {
+    const float2 f = parts(mul2(z, pair_of(-kLog2e, -kLog2e)));
+    const float2 d = parts(add2(pair_of(exp2_fast(f.x), exp2_fast(f.y)), pair_of(1.f, 1.f)));
+    return pair_of(rcp_fast(d.x), rcp_fast(d.y));
 }
-__device__ __forceinline__ pair32 grad2(pair32 p, int act) {
-    const float2 f = parts(p);
-    return pair_of(grad_act(f.x, act), grad_act(f.y, act));
+// act(z), in place
+template <int P>
+__device__ __forceinline__ void activate(pair32 (&z)[P], int act) {
+    if (act == PPO_ACT_SILU) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) z[p] = mul2(z[p], sigmoid2(z[p]));
+    } else if (act == PPO_ACT_RELU) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const float2 f = parts(z[p]);
+            z[p] = pair_of(f.x < 0.f ? 0.f : f.x, f.y < 0.f ? 0.f : f.y);  // a NaN stays
+        }
+    }
+}
+// g act'(z), in place; s (1 + z (1 - s)) with s = sigmoid(z) for SiLU
+template <int P>
+__device__ __forceinline__ void through_act(pair32 (&g)[P], const pair32 (&z)[P], int act) {
+    if (act == PPO_ACT_SILU) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const pair32 one = pair_of(1.f, 1.f), s = sigmoid2(z[p]), rest = fma2(s, pair_of(-1.f, -1.f), one);
+            g[p] = mul2(g[p], mul2(s, fma2(z[p], rest, one)));
+        }
+    } else if (act == PPO_ACT_RELU) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const float2 f = parts(z[p]), v = parts(g[p]);
+            g[p] = pair_of(f.x > 0.f ? v.x : 0.f, f.y > 0.f ? v.y : 0.f);
+        }
+    }
 }
 
 // The inputs in front of step t0 that it sees: rows t0 - W + 1 + i as h[i]; returns which ones lie behind the last flag (bit i).
@@ -168,19 +186,24 @@ __global__ void __launch_bounds__(kThreads) conv_fwd_kernel(ConvArgs a) {
     const long long sx = (long long)a.Be * a.ldx, sy = (long long)a.Be * a.ldy;
     if (a.state_in) state = static_cast<const T *>(a.state_in) + (long long)e * (W - 1) * a.C + c;
     const int t0 = tile * a.run, t1 = min(a.T, t0 + a.run);
-    const auto fetch = [&](int t) {
+    const T *ahead = x + t0 * sx;
+    T *out = y + t0 * sy;
+    int fetched = t0;
+    const auto fetch = [&] {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (t + j < t1) ring.copy((t - t0 + j) % (4 * (AHEAD + 1)), x + (t + j) * sx);
+            if (fetched + j < t1) ring.copy((fetched - t0) % (4 * (AHEAD + 1)) + j, ahead + j * sx);
         batch_end();
+        fetched += 4;
+        ahead += 4 * sx;
     };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) fetch(t0 + 4 * i);
+    for (int i = 0; i < AHEAD; ++i) fetch();
     pair32 w[W][P], b[P], h[W - 1][P];
     params<W, V>(a, c, w, b);
     history<T, W, V>(a, x, state, e, t0, h);
     for (int t = t0; t < t1; t += 4) {
-        fetch(t + 4 * AHEAD);
+        fetch();
         bool flag[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) flag[j] = done && t + j < t1 && done[(long long)(t + j) * a.Be];
@@ -190,14 +213,14 @@ __global__ void __launch_bounds__(kThreads) conv_fwd_kernel(ConvArgs a) {
             if (t + j >= t1) break;
             Raw<T, V> r;
             pair32 in[P], o[P];
-            ring.get((t - t0 + j) % (4 * (AHEAD + 1)), r);
+            ring.get((t - t0) % (4 * (AHEAD + 1)) + j, r);
             r.get(in);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 pair32 s = b[p];
 #pragma unroll
                 for (int i = 0; i < W - 1; ++i) s = fma2(w[i][p], h[i][p], s);
-                o[p] = map2(fma2(w[W - 1][p], in[p], s), a.act);
+                o[p] = fma2(w[W - 1][p], in[p], s);
 #pragma unroll
                 for (int i = 0; i < W - 2; ++i) h[i][p] = h[i + 1][p];
                 h[W - 2][p] = in[p];
@@ -208,19 +231,21 @@ __global__ void __launch_bounds__(kThreads) conv_fwd_kernel(ConvArgs a) {
 #pragma unroll
                     for (int p = 0; p < P; ++p) h[i][p] = 0;
             }
+            activate(o, a.act);
             r.set(o);
-            r.store(y + (t + j) * sy);
+            r.store(out);
+            out += sy;
         }
     }
     // the first run writes the state that is left: it alone reads the one that came in, which may be the same
     if (tile == 0 && a.state_out) {
         history<T, W, V>(a, x, state, e, a.T, h);
-        T *out = static_cast<T *>(a.state_out) + (long long)e * (W - 1) * a.C + c;
+        T *left = static_cast<T *>(a.state_out) + (long long)e * (W - 1) * a.C + c;
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) {
             Raw<T, V> r;
             r.set(h[i]);
-            r.store(out + (long long)i * a.C);
+            r.store(left + (long long)i * a.C);
         }
     }
 }
@@ -237,31 +262,37 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs a, int env
     const int e0 = (int)item * envs, e1 = min(a.Be, e0 + envs);
     pair32 w[W][P], b[P];
     params<W, V>(a, c, w, b);
-#pragma unroll 2
-    for (int e = e0; e < e1; ++e) {
-        Raw<T, V> r[W];
-        T *state = static_cast<T *>(a.state_out) + (long long)e * (W - 1) * a.C + c;
-        const bool start = a.done && a.done[e];
-        r[W - 1].load(static_cast<const T *>(a.x) + e * a.ldx + c);
+    for (int e = e0; e < e1; e += 2) {
+        Raw<T, V> r[2][W];
+        bool start[2];
+        T *state[2];
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i) {
-            r[i].w = typename Raw<T, V>::Word{};
-            if (!start) r[i].load(state + (long long)i * a.C);
-        }
-        pair32 s[P], v[P];
+        for (int k = 0; k < 2; ++k) {
+            if (e + k >= e1) break;
+            state[k] = static_cast<T *>(a.state_out) + (long long)(e + k) * (W - 1) * a.C + c;
+            start[k] = a.done && a.done[e + k];
+            r[k][W - 1].load(static_cast<const T *>(a.x) + (e + k) * a.ldx + c);
 #pragma unroll
-        for (int p = 0; p < P; ++p) s[p] = b[p];
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            r[i].get(v);
-#pragma unroll
-            for (int p = 0; p < P; ++p) s[p] = fma2(w[i][p], v[p], s[p]);
-            if (i > 0) r[i].store(state + (long long)(i - 1) * a.C);
+            for (int i = 0; i < W - 1; ++i) r[k][i].load(state[k] + (long long)i * a.C);
         }
 #pragma unroll
-        for (int p = 0; p < P; ++p) s[p] = map2(s[p], a.act);
-        r[0].set(s);
-        r[0].store(static_cast<T *>(a.y) + e * a.ldy + c);
+        for (int k = 0; k < 2; ++k) {
+            if (e + k >= e1) break;
+            pair32 s[P], v[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) s[p] = b[p];
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                if (i < W - 1 && start[k]) r[k][i].w = typename Raw<T, V>::Word{};
+                r[k][i].get(v);
+#pragma unroll
+                for (int p = 0; p < P; ++p) s[p] = fma2(w[i][p], v[p], s[p]);
+                if (i > 0) r[k][i].store(state[k] + (long long)(i - 1) * a.C);
+            }
+            activate(s, a.act);
+            r[k][0].set(s);
+            r[k][0].store(static_cast<T *>(a.y) + (e + k) * a.ldy + c);
+        }
     }
 }
 
@@ -290,17 +321,22 @@ __global__ void __launch_bounds__(kThreads) conv_bwd_kernel(ConvArgs a, int lane
         const T *state = a.state_in ? static_cast<const T *>(a.state_in) + states : nullptr;
         T *dstate = a.dstate_in ? static_cast<T *>(a.dstate_in) + states : nullptr;
         const int t0 = tile * a.run, t1 = min(a.T, t0 + a.run), end = min(a.T, t1 + W - 1);
-        const auto fetch = [&](int t) {
+        const T *ahead = x + t0 * sx, *gahead = dy + t0 * sy;
+        int fetched = t0;
+        const auto fetch = [&] {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                if (t + j < end) {
-                    xs.copy((t - t0 + j) % S, x + (t + j) * sx);
-                    gs.copy((t - t0 + j) % S, dy + (t + j) * sy);
+                if (fetched + j < end) {
+                    xs.copy((fetched - t0) % S + j, ahead + j * sx);
+                    gs.copy((fetched - t0) % S + j, gahead + j * sy);
                 }
             batch_end();
+            fetched += 2;
+            ahead += 2 * sx;
+            gahead += 2 * sy;
         };
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) fetch(t0 + 2 * i);
+        for (int i = 0; i < AHEAD; ++i) fetch();
         pair32 h[W - 1][P], acc[W][P] = {};
         int seen = history<T, W, V>(a, x, state, e, t0, h) | 1 << (W - 1);
         const auto put = [&](int t, const pair32 (&g)[P]) {  // the gradient of the input of step t is complete
@@ -310,7 +346,7 @@ __global__ void __launch_bounds__(kThreads) conv_bwd_kernel(ConvArgs a, int lane
             else if (t < 0 && t >= 1 - W && dstate) r.store(dstate + (long long)(t + W - 1) * a.C);
         };
         for (int t = t0; t < end; t += 2) {
-            fetch(t + 2 * AHEAD);
+            fetch();
             bool flag[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) flag[j] = done && t + j < end && done[(long long)(t + j) * a.Be];
@@ -318,11 +354,11 @@ __global__ void __launch_bounds__(kThreads) conv_bwd_kernel(ConvArgs a, int lane
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 if (t + j >= end) break;
-                pair32 in[P], g[P];
+                pair32 in[P], g[P], z[P];
                 Raw<T, V> r;
-                xs.get((t - t0 + j) % S, r);
+                xs.get((t - t0) % S + j, r);
                 r.get(in);
-                gs.get((t - t0 + j) % S, r);
+                gs.get((t - t0) % S + j, r);
                 r.get(g);
                 const bool own = t + j < t1;
 #pragma unroll
@@ -330,8 +366,9 @@ __global__ void __launch_bounds__(kThreads) conv_bwd_kernel(ConvArgs a, int lane
                     pair32 s = b[p];
 #pragma unroll
                     for (int i = 0; i < W - 1; ++i) s = fma2(w[i][p], h[i][p], s);
-                    g[p] = mul2(g[p], grad2(fma2(w[W - 1][p], in[p], s), a.act));
+                    z[p] = fma2(w[W - 1][p], in[p], s);
                 }
+                through_act(g, z, a.act);
                 if (seen == (1 << W) - 1) {
 #pragma unroll
                     for (int i = 0; i < W; ++i)
@@ -550,8 +587,8 @@ extern "C" int ppo_causal_conv_step(const ppo_causal_conv_desc *d, const void *x
     a.state_out = state;
     const int V = 16 / (int)elem_bytes(d->dtype);
     const bool vec = vectors(d, V, {x, y, state});
-    const long long cols = vec ? d->C / V : d->C, most = cols * d->Be / (148 * 1024);  // envs of a thread: as many as leave every SM 1024 threads
-    const int envs = most < 1 ? 1 : most > 8 ? 8 : (int)most;
+    const long long cols = vec ? d->C / V : d->C, most = cols * d->Be / (148 * 512);  // envs of a thread: as many as leave every SM 512 threads
+    const int envs = most < 2 ? 1 : most > 8 ? 8 : (int)most / 2 * 2;
     const long long blocks = (cols * ppo_cdiv(d->Be, envs) + kThreads - 1) / kThreads;
     if (blocks > 0x7fffffffll) return PPO_ERR_UNSUPPORTED;
     return with_columns(d, vec, [&](auto t, auto w, auto v) -> int {

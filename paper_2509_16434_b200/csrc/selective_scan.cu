@@ -7,6 +7,7 @@
 // channel and step and left in shared memory, with the rows of B and C; then every thread goes through the steps with NPT elements of the states
 // of four neighbouring channels in registers, packed arithmetic on two channels at a time; sums over the elements of a state go over the NL
 // lanes that share its channel, halving what each holds (three shuffles a step for four channels).  States, sums and arithmetic in 32 bits.
+#include "approx.cuh"
 #include "elem.cuh"
 #include "pair32.cuh"
 #include "param_sum.cuh"
@@ -14,7 +15,6 @@
 namespace {
 
 constexpr int kMaxN = 64, kThreads = 128, kSteps = 16;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct ScanArgs {
     const void *x, *dt, *B, *C, *z, *dy;
@@ -36,25 +36,6 @@ struct ScanArgs {
     float *part;  // shares of the gradients of A, D and dt_bias, [parts][channels * (N + 2)]
     int parts;
 };
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + exp2_fast(-z * kLog2e)); }
-// log(1 + e) = 2 artanh(e / (2 + e)) with e = exp(-|v|): the argument is at most 1/3, where the series to its 15th power is off by 2^-26.
-__device__ __forceinline__ float softplus(float v) {
-    const float e = exp2_fast(-fabsf(v) * kLog2e), s = __fdividef(e, 2.f + e), q = s * s;
-    float p = fmaf(q, 1.f / 15, 1.f / 13);
-    p = fmaf(q, p, 1.f / 11);
-    p = fmaf(q, p, 1.f / 9);
-    p = fmaf(q, p, 1.f / 7);
-    p = fmaf(q, p, 1.f / 5);
-    p = fmaf(q, p, 1.f / 3);
-    p = fmaf(q, p, 1.f);
-    return fmaf(2.f * s, p, v > 0.f ? v : v == v ? 0.f : v);
-}
 
 __device__ __forceinline__ pair32 twice(float a) { return pair_of(a, a); }
 __device__ __forceinline__ pair32 exp2_pair(pair32 p) {
@@ -384,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, MODE == BOTH ? 3 : 5) scan_kernel(Sc
 #pragma unroll
                 for (int v = 0; v < R::V; ++v) {
                     d[v] += b[v];
-                    if (a.softplus) d[v] = softplus(d[v]);
+                    if (a.softplus) d[v] = softplus_fast(d[v]);
                     u[v] *= d[v];
                 }
                 if constexpr (WITH_DY) {
@@ -393,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, MODE == BOTH ? 3 : 5) scan_kernel(Sc
                         float f[R::V];
                         rz.get(i, f);
 #pragma unroll
-                        for (int v = 0; v < R::V; ++v) g[v] *= f[v] * sigmoid(f[v]);
+                        for (int v = 0; v < R::V; ++v) g[v] *= f[v] * sigmoid_fast(f[v]);
                     }
                 }
             }
@@ -484,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, MODE == BOTH ? 3 : 5) scan_kernel(Sc
                 if (z) {
                     gate.get(i, v);
 #pragma unroll
-                    for (int k = 0; k < R::V; ++k) o[k] *= v[k] * sigmoid(v[k]);
+                    for (int k = 0; k < R::V; ++k) o[k] *= v[k] * sigmoid_fast(v[k]);
                 }
                 R::put(y + (t + r) * sy + l, o);
             }
@@ -624,14 +605,14 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
 #pragma unroll
                         for (int k = 0; k < R::V; ++k) {
                             d[k] += b[k];
-                            if (a.softplus) d[k] = softplus(d[k]);
+                            if (a.softplus) d[k] = softplus_fast(d[k]);
                             u[k] *= d[k];
                         }
                         if (z) {
                             float f[R::V];
                             rz.get(i, f);
 #pragma unroll
-                            for (int k = 0; k < R::V; ++k) v[k] *= f[k] * sigmoid(f[k]);
+                            for (int k = 0; k < R::V; ++k) v[k] *= f[k] * sigmoid_fast(f[k]);
                         }
                     }
                     put_floats(&s.sd[r][l], d);
@@ -782,7 +763,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                         get_floats(&s.sy[r][l], yv);
 #pragma unroll
                         for (int k = 0; k < R::V; ++k) {
-                            const float p = sigmoid(zv[k]), all = a.D ? fmaf(D[k], xv[k], yv[k]) : yv[k];
+                            const float p = sigmoid_fast(zv[k]), all = a.D ? fmaf(D[k], xv[k], yv[k]) : yv[k];
                             o[k] = gv[k] * all * (p * fmaf(zv[k], 1.f - p, 1.f));
                             gv[k] *= zv[k] * p;
                         }
@@ -797,7 +778,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
 #pragma unroll
                     for (int k = 0; k < R::V; ++k) {
                         o[k] = fmaf(xv[k], s1[k], kLn2 * s2[k]);
-                        if (a.softplus) o[k] *= sigmoid(tv[k] + bias[k]);
+                        if (a.softplus) o[k] *= sigmoid_fast(tv[k] + bias[k]);
                         sumb[k] += o[k];
                     }
                     R::put(ddt + (t + r) * st + l, o);
@@ -891,7 +872,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a, int envs) {
             }
             x = to_f32(static_cast<const T *>(a.x)[e * a.ldx + c]);
             float d = to_f32(static_cast<const T *>(a.dt)[e * a.lddt + c]) + bias;
-            if (a.softplus) d = softplus(d);
+            if (a.softplus) d = softplus_fast(d);
             const T *B = static_cast<const T *>(a.B) + e * a.ldb + (long long)group * a.N + n0, *C = static_cast<const T *>(a.C) + e * a.ldc + (long long)group * a.N + n0;
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
@@ -913,7 +894,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a, int envs) {
             y = fmaf(D, x, y);
             if (a.z) {
                 const float z = to_f32(static_cast<const T *>(a.z)[e * a.ldz + c]);
-                y *= z * sigmoid(z);
+                y *= z * sigmoid_fast(z);
             }
             static_cast<T *>(a.y)[e * a.ldy + c] = from_f32<T>(y);
         }
