@@ -2,22 +2,23 @@
 
 namespace {
 
-// 32 columns a block, every eighth share a warp.
-__global__ void __launch_bounds__(256) param_sum_kernel(const float *part, int parts, ParamSums s, int accumulate) {
+// 32 columns a block, every so many shares a warp.
+template <int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) param_sum_kernel(const float *part, int parts, ParamSums s, int accumulate) {
     grid_wait();
-    __shared__ double sum[8][32];
+    __shared__ double sum[WARPS][32];
     const long long n = (long long)s.n[0] + s.n[1] + s.n[2];
     const int l = threadIdx.x % 32, w = threadIdx.x / 32;
     long long i = (long long)blockIdx.x * 32 + l;
     double v = 0;
     if (i < n) {
 #pragma unroll 8
-        for (int p = w; p < parts; p += 8) v += part[p * n + i];
+        for (int p = w; p < parts; p += WARPS) v += part[p * n + i];
     }
     sum[w][l] = v;
     __syncthreads();
     if (w > 0 || i >= n) return;
-    for (int k = 1; k < 8; ++k) v += sum[k][l];
+    for (int k = 1; k < WARPS; ++k) v += sum[k][l];
     int k = 0;
     for (; k < 2 && i >= s.n[k]; ++k) i -= s.n[k];
     float *out = k == 0 ? s.out[0] : k == 1 ? s.out[1] : s.out[2];
@@ -28,5 +29,8 @@ __global__ void __launch_bounds__(256) param_sum_kernel(const float *part, int p
 
 int ppo_param_sum(const float *part, int parts, const ParamSums &s, int accumulate, cudaStream_t st) {
     const long long n = (long long)s.n[0] + s.n[1] + s.n[2];
-    return ppo_launch(param_sum_kernel, dim3((unsigned)((n + 31) / 32)), dim3(256), 0, st, part, parts, s, accumulate);
+    const dim3 grid((unsigned)((n + 31) / 32));
+    // 592 shares of 128 columns: 14.5 us by eight warps, 6.5 by 32
+    if (parts > 64) return ppo_launch(param_sum_kernel<32>, grid, dim3(1024), 0, st, part, parts, s, accumulate);
+    return ppo_launch(param_sum_kernel<8>, grid, dim3(256), 0, st, part, parts, s, accumulate);
 }

@@ -1,7 +1,10 @@
 // Norms of queries and keys for each head with the rotation by their positions, and the gradients.
 //
-// Angles in 64 bits down to the fraction of a turn, which fits 32; the rest in 32 bits; what is stored is rounded once.
+// Angles in 64 bits down to the fraction of a turn, which fits 32; the rest in 32 bits; what is stored is rounded once.  Everything is read and
+// written once: bound by memory.  A warp takes the heads of a row side by side, a few lanes each, two vectors of 16 bytes a lane such that a
+// lane has both elements of every pair it turns; the row's cosines and sines are made once for all its heads, d / 64 of them a lane.
 #include "elem.cuh"
+#include "pair32.cuh"
 #include "param_sum.cuh"
 
 namespace {
@@ -140,6 +143,294 @@ __global__ void __launch_bounds__(256) qk_bwd_any_kernel(QkArgs a) {
     }
 }
 
+// ---- rows of aligned vectors ----
+
+// How the warps go about it: lanes of a head (a power of two, of which `slots` hold something), the parts that a row's heads are dealt to, heads
+// of a part.
+struct Lanes {
+    int lanes, slots, parts, heads;
+};
+
+// The row's turns, and where a lane's two vectors stand in a head.
+template <typename T, bool INTERLEAVED>
+struct Turns {
+    static constexpr int V = Vec<T>::N, P = V / 2;
+    int first, second;
+    bool on;
+    pair32 c[INTERLEAVED ? V : P], s[INTERLEAVED ? V : P];  // interleaved: of each pair twice, the sine's first one negative
+
+    __device__ __forceinline__ Turns(const QkArgs &a, const Lanes &k) {
+        const int slot = threadIdx.x % k.lanes, turned = a.pairs / V;  // slots whose vectors are turned with one another
+        on = slot < k.slots;
+        if (INTERLEAVED) {
+            first = 2 * V * slot;
+            second = first + V;
+        } else if (slot < turned) {
+            first = V * slot;
+            second = a.pairs + first;
+        } else {
+            first = 2 * a.pairs + 2 * V * (slot - turned);
+            second = first + V;
+        }
+    }
+    // table: of the warp; made by all its lanes
+    __device__ __forceinline__ void row(const QkArgs &a, long long row, float2 *table) {
+        __syncwarp();
+        if (a.pairs > 0) {
+            const int pos = a.pos[row];
+            for (int i = threadIdx.x % 32; i < a.pairs; i += 32) table[i] = turn(pos, a.freq[i]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < (INTERLEAVED ? V : P); ++i) {
+            if constexpr (INTERLEAVED) {
+                const int p = (i < P ? first : second - V) / 2 + i;
+                const float2 t = on && p < a.pairs ? table[p] : make_float2(1.f, 0.f);
+                c[i] = pair_of(t.x, t.x), s[i] = pair_of(-t.y, t.y);
+            } else {
+                float2 t = make_float2(1.f, 0.f), u = t;
+                if (on && first < a.pairs) t = table[first + 2 * i], u = table[first + 2 * i + 1];
+                c[i] = pair_of(t.x, u.x), s[i] = pair_of(t.y, u.y);
+            }
+        }
+    }
+    static __device__ __forceinline__ pair32 minus(pair32 p) { return mul2(p, pair_of(-1.f, -1.f)); }
+    static __device__ __forceinline__ pair32 swap(pair32 p) {
+        const float2 f = parts(p);
+        return pair_of(f.y, f.x);
+    }
+    // x: the pairs of neighbours of both vectors; BACK: by the opposite angle
+    template <bool BACK>
+    __device__ __forceinline__ void apply(pair32 (&x)[V]) const {
+        if constexpr (INTERLEAVED) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const pair32 o = swap(x[i]);
+                x[i] = fma2(x[i], c[i], mul2(o, BACK ? minus(s[i]) : s[i]));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const pair32 a = x[i], b = x[P + i], n = minus(BACK ? a : b);
+                x[i] = fma2(a, c[i], mul2(BACK ? b : n, s[i]));
+                x[P + i] = fma2(b, c[i], mul2(BACK ? n : a, s[i]));
+            }
+        }
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void pairs_of(const uint4 &raw, pair32 *p) {
+    Vec<T> v;
+    float f[Vec<T>::N];
+    v.raw = raw;
+    v.get(f);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::N / 2; ++i) p[i] = pair_of(f[2 * i], f[2 * i + 1]);
+}
+template <typename T>
+__device__ __forceinline__ uint4 raw_of(const pair32 *p) {
+    Vec<T> v;
+    float f[Vec<T>::N];
+#pragma unroll
+    for (int i = 0; i < Vec<T>::N / 2; ++i) {
+        const float2 u = parts(p[i]);
+        f[2 * i] = u.x, f[2 * i + 1] = u.y;
+    }
+    v.set(f);
+    return v.raw;
+}
+template <int P>
+__device__ __forceinline__ void floats_of(const float *f, pair32 *p) {
+#pragma unroll
+    for (int i = 0; i < P; i += 2) {
+        const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(f + 2 * i);
+        p[i] = u.x, p[i + 1] = u.y;
+    }
+}
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < lanes) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// gamma of queries and of keys
+__device__ __forceinline__ void stage_gamma(const QkArgs &a, float (&to)[2][kMaxD]) {
+    for (int i = threadIdx.x; i < 2 * a.d; i += 256) {
+        const float *from = i < a.d ? a.gamma_q : a.gamma_k;
+        const int n = i < a.d ? i : i - a.d;
+        to[i >= a.d][n] = from ? from[n] : 1.f;
+    }
+    __syncthreads();
+}
+
+constexpr int kHeads = 4;  // of a lane's, on their way at a time
+
+template <typename T, bool INTERLEAVED>
+__global__ void __launch_bounds__(256) qk_fwd_kernel(QkArgs a, Lanes k) {
+    grid_wait();
+    constexpr int V = Vec<T>::N, P = V / 2;
+    __shared__ alignas(16) float gamma[2][kMaxD];
+    __shared__ float2 tables[8][kMaxD / 2];
+    stage_gamma(a, gamma);
+    Turns<T, INTERLEAVED> turns(a, k);
+    const int group = threadIdx.x % 32 / k.lanes, groups = 32 / k.lanes, all = a.heads + a.kv;
+    const long long items = (long long)a.rows * k.parts, step = (long long)gridDim.x * 8;
+    for (long long item = (long long)blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
+        const long long row = item / k.parts;
+        const int h0 = (int)(item - row * k.parts) * k.heads, h1 = min(all, h0 + k.heads);
+        const T *q = static_cast<const T *>(a.q) + row * a.ldq, *key = static_cast<const T *>(a.k) + row * a.ldk - (long long)a.heads * a.d;
+        T *qo = static_cast<T *>(a.qo) + row * a.ldqo, *ko = static_cast<T *>(a.ko) + row * a.ldko - (long long)a.heads * a.d;
+        bool made = false;
+        for (int h = h0 + group; h - group < h1; h += kHeads * groups) {
+            uint4 raw[kHeads][2];
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i) {
+                const int n = h + i * groups;
+                raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
+                if (n < h1 && turns.on) {
+                    const T *x = (n < a.heads ? q : key) + (long long)n * a.d;
+                    raw[i][0] = *reinterpret_cast<const uint4 *>(x + turns.first);
+                    raw[i][1] = *reinterpret_cast<const uint4 *>(x + turns.second);
+                }
+            }
+            if (!made) turns.row(a, row, tables[threadIdx.x / 32]);
+            made = true;
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i) {
+                const int n = h + i * groups;
+                if (n - group >= h1) break;
+                pair32 x[V], g[V], s = 0;
+                pairs_of<T>(raw[i][0], x);
+                pairs_of<T>(raw[i][1], x + P);
+#pragma unroll
+                for (int j = 0; j < V; ++j) s = fma2(x[j], x[j], s);
+                const float2 f = parts(s);
+                const float r = 1.f / sqrtf(lanes_sum(f.x + f.y, k.lanes) / (float)a.d + a.eps);
+                if (n >= h1 || !turns.on) continue;
+                floats_of<P>(&gamma[n >= a.heads][turns.first], g);
+                floats_of<P>(&gamma[n >= a.heads][turns.second], g + P);
+                const pair32 rr = pair_of(r, r);
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] = mul2(mul2(x[j], rr), g[j]);
+                turns.template apply<false>(x);
+                T *y = (n < a.heads ? qo : ko) + (long long)n * a.d;
+                *reinterpret_cast<uint4 *>(y + turns.first) = raw_of<T>(x);
+                *reinterpret_cast<uint4 *>(y + turns.second) = raw_of<T>(x + P);
+            }
+        }
+    }
+}
+
+// With n = R^T dy (turned back), g = gamma n and r = 1 / sqrt(mean x^2 + eps): dx = r g - x r^3 mean(g x), dgamma += n x r.  Both sums of a head are
+// made at once.
+template <typename T, bool INTERLEAVED>
+__global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, Lanes k) {
+    grid_wait();
+    constexpr int V = Vec<T>::N, P = V / 2, U = 2;
+    __shared__ alignas(16) float gamma[2][kMaxD];
+    __shared__ float2 tables[8][kMaxD / 2];
+    __shared__ float shares[8][kMaxD];
+    stage_gamma(a, gamma);
+    Turns<T, INTERLEAVED> turns(a, k);
+    const int group = threadIdx.x % 32 / k.lanes, groups = 32 / k.lanes, w = threadIdx.x / 32;
+    pair32 sum[2][V] = {};
+    const long long items = (long long)a.rows * k.parts, step = (long long)gridDim.x * 8;
+    for (long long item = (long long)blockIdx.x * 8 + w; item < items; item += step) {
+        const long long row = item / k.parts;
+        const int h0 = (int)(item - row * k.parts) * k.heads, h1 = min(a.heads + a.kv, h0 + k.heads);
+        bool made = false;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            // queries, then keys
+            const int from = which == 0 ? h0 : max(h0, a.heads), to = which == 0 ? min(h1, a.heads) : h1;
+            const long long ld = which == 0 ? a.ldq : a.ldk, ldo = which == 0 ? a.ldqo : a.ldko, before = which == 0 ? 0 : (long long)a.heads * a.d;
+            const T *x0 = static_cast<const T *>(which == 0 ? a.q : a.k) + row * ld - before;
+            const T *dy0 = static_cast<const T *>(which == 0 ? a.dqo : a.dko) + row * ldo - before;
+            T *dx0 = static_cast<T *>(which == 0 ? a.dq : a.dk) + row * ld - before;
+            for (int h = from + group; h - group < to; h += U * groups) {
+                uint4 xr[U][2], gr[U][2];
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int n = h + i * groups;
+                    xr[i][0] = xr[i][1] = gr[i][0] = gr[i][1] = make_uint4(0, 0, 0, 0);
+                    if (n < to && turns.on) {
+                        const T *x = x0 + (long long)n * a.d, *dy = dy0 + (long long)n * a.d;
+                        xr[i][0] = *reinterpret_cast<const uint4 *>(x + turns.first);
+                        xr[i][1] = *reinterpret_cast<const uint4 *>(x + turns.second);
+                        gr[i][0] = *reinterpret_cast<const uint4 *>(dy + turns.first);
+                        gr[i][1] = *reinterpret_cast<const uint4 *>(dy + turns.second);
+                    }
+                }
+                if (!made) turns.row(a, row, tables[w]);
+                made = true;
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int n = h + i * groups;
+                    if (n - group >= to) break;
+                    pair32 x[V], g[V], s = 0, t = 0;
+                    pairs_of<T>(xr[i][0], x);
+                    pairs_of<T>(xr[i][1], x + P);
+                    pairs_of<T>(gr[i][0], g);
+                    pairs_of<T>(gr[i][1], g + P);
+                    turns.template apply<true>(g);
+                    pair32 nx[V], gam[V];
+                    if (turns.on) {
+                        floats_of<P>(&gamma[which][turns.first], gam);
+                        floats_of<P>(&gamma[which][turns.second], gam + P);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) gam[j] = 0;
+                    }
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        s = fma2(x[j], x[j], s);
+                        nx[j] = mul2(g[j], x[j]);
+                        t = fma2(nx[j], gam[j], t);
+                        g[j] = mul2(g[j], gam[j]);
+                    }
+                    const float2 f = parts(s), u = parts(t);
+                    const float r = 1.f / sqrtf(lanes_sum(f.x + f.y, k.lanes) / (float)a.d + a.eps);
+                    const float m = -(lanes_sum(u.x + u.y, k.lanes) / (float)a.d) * r * r;
+                    if (n >= to || !turns.on) continue;
+                    const pair32 rr = pair_of(r, r), mm = pair_of(m, m);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        sum[which][j] = fma2(nx[j], rr, sum[which][j]);
+                        g[j] = mul2(rr, fma2(x[j], mm, g[j]));
+                    }
+                    T *dx = dx0 + (long long)n * a.d;
+                    *reinterpret_cast<uint4 *>(dx + turns.first) = raw_of<T>(g);
+                    *reinterpret_cast<uint4 *>(dx + turns.second) = raw_of<T>(g + P);
+                }
+            }
+        }
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float2 f = parts(sum[which][j]);
+            for (int o = k.lanes; o < 32; o *= 2) {
+                f.x += __shfl_xor_sync(0xffffffffu, f.x, o);
+                f.y += __shfl_xor_sync(0xffffffffu, f.y, o);
+            }
+            if (group == 0 && turns.on) {
+                float *to = &shares[w][j < P ? turns.first + 2 * j : turns.second + 2 * (j - P)];
+                to[0] = f.x, to[1] = f.y;
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.d; i += 256) {
+            float s = 0.f;
+            for (int n = 0; n < 8; ++n) s += shares[n][i];
+            a.part[((size_t)blockIdx.x * 2 + which) * a.d + i] = s;
+        }
+    }
+}
+
 int check(const ppo_qk_norm_desc *d) {
     if (!d || d->rows <= 0 || d->heads <= 0 || d->kv_heads <= 0 || d->d <= 0 || d->pairs < 0) return PPO_ERR_INVALID_ARG;
     if (d->dtype < PPO_F32 || d->dtype > PPO_F16) return PPO_ERR_INVALID_ARG;
@@ -177,16 +468,40 @@ QkArgs args(const ppo_qk_norm_desc *d, float eps, const void *q, const void *k, 
     return a;
 }
 
-// Blocks of a call with gradients of gamma: by sizes alone, so that the order of the sums goes by them.
-int blocks_of(const ppo_qk_norm_desc *d) {
-    const long long all = ((long long)d->rows * (d->heads + d->kv_heads) + 7) / 8;
-    return (int)(all < 4 * 148 ? all : 4 * 148);
+// Blocks of eight warps, each with a head, or with the lanes' heads of a row: by sizes alone, so that the order of the sums goes by them.
+int blocks_of(long long items, int per_sm) {
+    const long long all = (items + 7) / 8;
+    return (int)(all < per_sm * 148 ? all : per_sm * 148);
+}
+int any_blocks(const ppo_qk_norm_desc *d) { return blocks_of((long long)d->rows * (d->heads + d->kv_heads), 4); }
+
+// Whether every row is made of whole, aligned vectors, and pairs lie in two of a lane's.
+bool vectors(const ppo_qk_norm_desc *d, std::initializer_list<const void *> ps) {
+    const int V = 16 / (int)elem_bytes(d->dtype);
+    return d->d % (2 * V) == 0 && (d->interleaved || d->pairs % V == 0) && d->ldq % V == 0 && d->ldk % V == 0 && d->ldqo % V == 0 && d->ldko % V == 0 &&
+           !misaligned(ps, 16);
+}
+// Rows are taken whole, as long as they give every SM `warps` warps; fewer rows are dealt out by as many heads as the lanes of a warp take at once.
+Lanes lanes_of(const ppo_qk_norm_desc *d, int warps) {
+    const int V = 16 / (int)elem_bytes(d->dtype), all = d->heads + d->kv_heads;
+    Lanes k = {1, d->d / (2 * V), 1, all};
+    while (k.lanes < k.slots) k.lanes *= 2;
+    const int side = 32 / k.lanes, most = ppo_cdiv(all, side);
+    long long want = ((long long)warps * 148 + d->rows - 1) / d->rows;
+    k.parts = (int)(want < most ? want : most);
+    k.heads = ppo_cdiv(ppo_cdiv(all, k.parts), side) * side;
+    k.parts = ppo_cdiv(all, k.heads);
+    return k;
+}
+template <typename F>
+int with_order(const ppo_qk_norm_desc *d, F &&fn) {
+    return with_elem(d->dtype, [&](auto t) -> int { return d->interleaved ? fn(t, std::true_type{}) : fn(t, std::false_type{}); });
 }
 
 }  // namespace
 
 extern "C" size_t ppo_qk_norm_rotate_workspace_bytes(const ppo_qk_norm_desc *d) {
-    return check(d) == PPO_OK ? (size_t)blocks_of(d) * 2 * d->d * sizeof(float) : 0;
+    return check(d) == PPO_OK ? (size_t)4 * 148 * 2 * d->d * sizeof(float) : 0;
 }
 
 extern "C" int ppo_qk_norm_rotate_fwd(const ppo_qk_norm_desc *d, float eps, const void *q, const void *k, const float *gamma_q, const float *gamma_k,
@@ -198,8 +513,12 @@ extern "C" int ppo_qk_norm_rotate_fwd(const ppo_qk_norm_desc *d, float eps, cons
     QkArgs a = args(d, eps, q, k, gamma_q, gamma_k, pos, freq);
     a.qo = q_out;
     a.ko = k_out;
-    return with_elem(d->dtype, [&](auto t) {
-        return ppo_launch(qk_fwd_any_kernel<decltype(t)>, dim3(blocks_of(d)), dim3(256), 0, static_cast<cudaStream_t>(stream), a);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!vectors(d, {q, k, q_out, k_out}))
+        return with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_fwd_any_kernel<decltype(t)>, dim3(any_blocks(d)), dim3(256), 0, st, a); });
+    const Lanes l = lanes_of(d, 16);
+    return with_order(d, [&](auto t, auto order) {
+        return ppo_launch(qk_fwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks_of((long long)d->rows * l.parts, 8)), dim3(256), 0, st, a, l);
     });
 }
 
@@ -221,7 +540,15 @@ extern "C" int ppo_qk_norm_rotate_bwd(const ppo_qk_norm_desc *d, float eps, cons
     a.dk = dk;
     a.part = params ? static_cast<float *>(workspace) : nullptr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int blocks = blocks_of(d);
-    PPO_TRY(with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_bwd_any_kernel<decltype(t)>, dim3(blocks), dim3(256), 0, st, a); }));
+    int blocks = any_blocks(d);
+    if (vectors(d, {q, k, dq_out, dk_out, dq, dk})) {
+        const Lanes l = lanes_of(d, 16);
+        blocks = blocks_of((long long)d->rows * l.parts, 2);
+        PPO_TRY(with_order(d, [&](auto t, auto order) {
+            return ppo_launch(qk_bwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks), dim3(256), 0, st, a, l);
+        }));
+    } else {
+        PPO_TRY(with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_bwd_any_kernel<decltype(t)>, dim3(blocks), dim3(256), 0, st, a); }));
+    }
     return params ? ppo_param_sum(a.part, blocks, {{dgamma_q, dgamma_k, nullptr}, {d->d, d->d, 0}}, accumulate, st) : PPO_OK;
 }

@@ -104,17 +104,21 @@ def test_one_row_of_queries_keys_and_values_side_by_side(d, at, gap, dtype):
         return row, parts
     row, (q, k) = wide(p["q"], p["k"])
     _fwd({**p, "q": q, "k": k}, False, q, k)
-    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+    aligned = at % 8 == 0 and width % 8 == 0
+    if aligned and d % 16 == 0:
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+    else:  # element by element: the sum of squares in another order, which the bound counts whatever the order
+        for a, n in ((q, "q"), (k, "k")):
+            plain.within(a.contiguous(), plain.qk(p[n], p["g" + n], EPS, p["pos"], p["freq"], False))
     assert bool(torch.isnan(row[:, :at]).all()) and bool(torch.isnan(row[:, at + (heads + kv) * d:]).all())
     drow, (dq, dk) = wide(p["dqo"], p["dko"])
     _, (q, k) = wide(p["q"], p["k"])
     got = _bwd({**p, "q": q, "k": k, "dqo": dq, "dko": dk}, False, dq, dk)
-    aligned = at % 8 == 0 and width % 8 == 0
     for n, i in (("q", 0), ("k", 1)):
         dx, dgamma = plain.qk(p[n], p["g" + n], EPS, p["pos"], p["freq"], False, p["d" + n + "o"])
         plain.within(got[i].contiguous(), dx)
         plain.within(got[2 + i], dgamma)
-        assert not aligned or torch.equal(got[i], grads[i])
+        assert not (aligned and d % 16 == 0) or torch.equal(got[i], grads[i])
     assert bool(torch.isnan(drow[:, :at]).all()) and bool(torch.isnan(drow[:, at + (heads + kv) * d:]).all())
 
 
