@@ -84,18 +84,12 @@ template <int N>
 __device__ __forceinline__ void batch_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// sigmoid of both
-__device__ __forceinline__ pair32 sigmoid2(pair32 z) {
-    const float2 f = parts(mul2(z, pair_of(-kLog2e, -kLog2e)));
-    const float2 d = parts(add2(pair_of(exp2_fast(f.x), exp2_fast(f.y)), pair_of(1.f, 1.f)));
-    return pair_of(rcp_fast(d.x), rcp_fast(d.y));
-}
 // act(z), in place
 template <int P>
 __device__ __forceinline__ void activate(pair32 (&z)[P], int act) {
     if (act == PPO_ACT_SILU) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) z[p] = mul2(z[p], sigmoid2(z[p]));
+        for (int p = 0; p < P; ++p) z[p] = mul2(z[p], sigmoid_pair(z[p]));
     } else if (act == PPO_ACT_RELU) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -110,7 +104,7 @@ __device__ __forceinline__ void through_act(pair32 (&g)[P], const pair32 (&z)[P]
     if (act == PPO_ACT_SILU) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const pair32 one = pair_of(1.f, 1.f), s = sigmoid2(z[p]), rest = fma2(s, pair_of(-1.f, -1.f), one);
+            const pair32 one = pair_of(1.f, 1.f), s = sigmoid_pair(z[p]), rest = fma2(s, pair_of(-1.f, -1.f), one);
             g[p] = mul2(g[p], mul2(s, fma2(z[p], rest, one)));
         }
     } else if (act == PPO_ACT_RELU) {

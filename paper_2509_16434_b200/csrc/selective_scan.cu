@@ -3,10 +3,12 @@
 // h_t = exp(d_t A) h_{t-1} + d_t x_t B_t: one exponential and four multiply-adds for each element of a state and step, against 8 bytes
 // for each channel and step in 16 bits: with 16 elements a channel the exponentials (16 a clock and SM) bound it, not memory.
 //
-// A block of four warps takes a tile of channels of one env through the steps, 16 at a time: step sizes and inputs are made once for each
-// channel and step and left in shared memory, with the rows of B and C; then every thread goes through the steps with NPT elements of the states
-// of four neighbouring channels in registers, packed arithmetic on two channels at a time; sums over the elements of a state go over the NL
-// lanes that share its channel, halving what each holds (three shuffles a step for four channels).  States, sums and arithmetic in 32 bits.
+// Forwards a thread takes a channel, or two neighbouring ones, of one env through the steps, with 16 elements of the states in registers (channels
+// with more of them belong to two or four lanes): nothing is shared but the rows of B and C, and a step's sum over the elements is the
+// thread's own.  Backwards four channels by four elements are a thread's, since there sums go over the channels as well as over the elements.
+// States, sums and arithmetic in 32 bits, packed arithmetic on two numbers at a time.
+//
+// Long sequences of few channels are cut into segments: a pass makes what each segment ends with, and each starts from the ends in front of it.
 #include "approx.cuh"
 #include "elem.cuh"
 #include "pair32.cuh"
@@ -26,22 +28,16 @@ struct ScanArgs {
     int T, Be, channels, N, groups, per, softplus;  // per: channels of a group
     int tiles, group_tiles;                         // tiles of channels, in all and of a group
     int len, nseg;                                  // steps of a segment
-    // Of every segment, env and tile, as the threads of a tile hold them: the states it ends with (starting from zeros, but for the first one;
-    // in the last one's place the state that comes in) and the gradients it hands to the steps in front (getting zeros; in the first
-    // one's place the gradient of the state that is left); what its step sizes add up to for each channel, and whether a flag is set in it.
+    // Of every segment and env, [channels][NP] (N padded): the states it ends with (starting from zeros, but for the first one; in the last one's place
+    // the state that comes in) and the gradients it hands to the steps in front (getting zeros; in the first one's place the gradient
+    // of the state that is left); what its step sizes add up to for each channel, and whether a flag is set in it.
     float *seg, *back, *sum;
     int *cut;
-    float *mark;  // the states in front of every fourth step, [ceil(T / 4)][Be][tiles] as the threads hold them
+    float *mark;  // the states in front of every fourth step, [ceil(T / 4)][Be][channels][NP]
     float *few;   // shares of the gradients of B and C, [group_tiles][T * Be][groups][2][NP]
     float *part;  // shares of the gradients of A, D and dt_bias, [parts][channels * (N + 2)]
     int parts;
 };
-
-__device__ __forceinline__ pair32 twice(float a) { return pair_of(a, a); }
-__device__ __forceinline__ pair32 exp2_pair(pair32 p) {
-    const float2 f = parts(p);
-    return pair_of(exp2_fast(f.x), exp2_fast(f.y));
-}
 
 // Sums of V values over LANES lanes, STRIDE apart: halves go to the lanes' halves as long as there are values, lane bit by lane bit from the
 // highest; a lane is left with max(1, V / LANES) of them in v[0 ..].  index() says which.
@@ -73,10 +69,10 @@ __device__ __forceinline__ int spread_first(int l) {
     else return 0;
 }
 
-// NL lanes share four channels and hold NPT elements each of their states.
-template <int NPT, int NL>
+// Backwards NL lanes share four channels and hold four elements each of their states.
+template <int NL>
 struct Shape {
-    static constexpr int NP = NPT * NL, GROUPS = 32 / NL, CT = 4 * GROUPS * (kThreads / 32);
+    static constexpr int NP = 4 * NL, GROUPS = 32 / NL, CT = 4 * GROUPS * (kThreads / 32);
 };
 
 // What a block works on: a tile of channels of one env over steps t0 .. t1 - 1.
@@ -173,119 +169,71 @@ __device__ __forceinline__ uint32_t flags_of(const ScanArgs &a, int e, int t, in
     return a.done ? __ballot_sync(0xffffffffu, r < min(rows, kSteps) && t + r >= 0 && a.done[(long long)(t + r) * a.Be + e]) : 0u;
 }
 
-// NPT elements of four channels' states, [e][channel][N] in memory; zeros where there are none.
-template <int NPT>
-__device__ __forceinline__ void load_state(const float *from, const ScanArgs &a, int e, int c, int c1, int n0, float (&h)[4][NPT]) {
-    const bool whole = NPT == 4 && a.N % 4 == 0 && (reinterpret_cast<uintptr_t>(from) & 15) == 0;
+// Elements n0 .. n0 + W - 1 of a state of N in memory; zeros behind the last one.
+template <int W>
+__device__ __forceinline__ void load_row(const float *p, int N, int n0, float (&h)[W]) {
+    const bool whole = N % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int n = 0; n < NPT; ++n) h[j][n] = 0.f;
-        if (!from || c + j >= c1) continue;
-        const float *p = from + ((long long)e * a.channels + c + j) * a.N + n0;
+    for (int n = 0; n < W; n += 4) {
         if (whole) {
-            if constexpr (NPT == 4) {
-                if (n0 < a.N) {
-                    const float4 f = *reinterpret_cast<const float4 *>(p);
-                    h[j][0] = f.x, h[j][1] = f.y, h[j][2] = f.z, h[j][3] = f.w;
-                }
-            }
+            const float4 f = n0 + n < N ? *reinterpret_cast<const float4 *>(p + n0 + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+            h[n] = f.x, h[n + 1] = f.y, h[n + 2] = f.z, h[n + 3] = f.w;
         } else {
 #pragma unroll
-            for (int n = 0; n < NPT; ++n)
-                if (n0 + n < a.N) h[j][n] = p[n];
+            for (int i = 0; i < 4; ++i) h[n + i] = n0 + n + i < N ? p[n0 + n + i] : 0.f;
         }
     }
 }
-template <int NPT>
-__device__ __forceinline__ void store_state(float *to, const ScanArgs &a, int e, int c, int c1, int n0, const float (&h)[4][NPT]) {
-    const bool whole = NPT == 4 && a.N % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & 15) == 0;
+template <int W>
+__device__ __forceinline__ void store_row(float *p, int N, int n0, const float (&h)[W]) {
+    const bool whole = N % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (c + j >= c1) break;
-        float *p = to + ((long long)e * a.channels + c + j) * a.N + n0;
+    for (int n = 0; n < W; n += 4) {
         if (whole) {
-            if (n0 < a.N) *reinterpret_cast<float4 *>(p) = make_float4(h[j][0], h[j][1], h[j][2], h[j][3]);
+            if (n0 + n < N) *reinterpret_cast<float4 *>(p + n0 + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
         } else {
 #pragma unroll
-            for (int n = 0; n < NPT; ++n)
-                if (n0 + n < a.N) p[n] = h[j][n];
+            for (int i = 0; i < 4; ++i)
+                if (n0 + n + i < N) p[n0 + n + i] = h[n + i];
         }
-    }
-}
-// The same as the threads hold them.
-template <int NPT>
-__device__ __forceinline__ void load_held(const float *from, long long tile, float (&h)[4][NPT]) {
-    const float *p = from + tile * (kThreads * 4 * NPT) + threadIdx.x * 4;
-#pragma unroll
-    for (int n = 0; n < NPT; ++n) {
-        const float4 f = *reinterpret_cast<const float4 *>(p + n * kThreads * 4);
-        h[0][n] = f.x, h[1][n] = f.y, h[2][n] = f.z, h[3][n] = f.w;
-    }
-}
-template <int NPT>
-__device__ __forceinline__ void store_held(float *to, long long tile, const float (&h)[4][NPT]) {
-    float *p = to + tile * (kThreads * 4 * NPT) + threadIdx.x * 4;
-#pragma unroll
-    for (int n = 0; n < NPT; ++n) *reinterpret_cast<float4 *>(p + n * kThreads * 4) = make_float4(h[0][n], h[1][n], h[2][n], h[3][n]);
-}
-template <int NPT>
-__device__ __forceinline__ void pack(const float (&h)[4][NPT], pair32 (&p)[NPT][2]) {
-#pragma unroll
-    for (int n = 0; n < NPT; ++n) p[n][0] = pair_of(h[0][n], h[1][n]), p[n][1] = pair_of(h[2][n], h[3][n]);
-}
-template <int NPT>
-__device__ __forceinline__ void unpack(const pair32 (&p)[NPT][2], float (&h)[4][NPT]) {
-#pragma unroll
-    for (int n = 0; n < NPT; ++n) {
-        const float2 u = parts(p[n][0]), v = parts(p[n][1]);
-        h[0][n] = u.x, h[1][n] = u.y, h[2][n] = v.x, h[3][n] = v.y;
     }
 }
 __device__ __forceinline__ void load_pairs(const float *p, pair32 (&v)[2]) {
     const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(p);
     v[0] = u.x, v[1] = u.y;
 }
-template <int NPT>
-__device__ __forceinline__ void load_few(const float2 *p, pair32 (&v)[NPT]) {
-    if constexpr (NPT % 2 == 0) {
+__device__ __forceinline__ void load_few(const float2 *p, pair32 (&v)[4]) {
 #pragma unroll
-        for (int n = 0; n < NPT; n += 2) {
-            const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(p + n);
-            v[n] = u.x, v[n + 1] = u.y;
-        }
-    } else {
-#pragma unroll
-        for (int n = 0; n < NPT; ++n) v[n] = *reinterpret_cast<const pair32 *>(p + n);
+    for (int n = 0; n < 4; n += 2) {
+        const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(p + n);
+        v[n] = u.x, v[n + 1] = u.y;
     }
 }
 
-// exp2(A sum of a segment's step sizes) h + add, or add alone behind a flag.
-template <int NPT>
-__device__ __forceinline__ void through(const ScanArgs &a, const Work &w, int s, int c, const float (&A)[4][NPT], const float *from, float (&h)[4][NPT]) {
-    const long long at = (long long)s * a.Be + w.e;
-    float add[4][NPT];
-    load_held<NPT>(from, at * a.tiles + w.tile, add);
+// Takes elements n0 .. of a channel's state, or gradient, through segment s: exp2(A sum of its step sizes) h + add, or add alone behind a flag.  from: what
+// each segment adds; A: times log2(e).
+template <int W>
+__device__ __forceinline__ void through(const ScanArgs &a, int NP, int s, int e, int c, int n0, const float (&A)[W], const float *from, float (&h)[W]) {
+    const long long at = (long long)s * a.Be + e;
+    float add[W];
+    load_row<W>(from + (at * a.channels + c) * NP, NP, n0, add);
     const bool cut = a.cut[at];
+    const float d = a.sum[at * a.channels + c];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float d = c + j < w.c1 ? a.sum[at * a.channels + c + j] : 0.f;
-#pragma unroll
-        for (int n = 0; n < NPT; ++n) h[j][n] = cut ? add[j][n] : fmaf(exp2_fast(d * A[j][n]), h[j][n], add[j][n]);
-    }
+    for (int n = 0; n < W; ++n) h[n] = cut ? add[n] : fmaf(exp2_fast(d * A[n]), h[n], add[n]);
 }
 // What a segment starts from: the state that comes in, or what the first segment ends with, taken through the segments in between.
-template <int NPT>
-__device__ __forceinline__ void start_of(const ScanArgs &a, const Work &w, int c, const float (&A)[4][NPT], float (&h)[4][NPT]) {
+template <int W>
+__device__ __forceinline__ void start_of(const ScanArgs &a, int NP, const Work &w, int c, int n0, const float (&A)[W], float (&h)[W]) {
     const long long at = (long long)(w.seg == 0 ? a.nseg - 1 : 0) * a.Be + w.e;
-    load_held<NPT>(a.seg, at * a.tiles + w.tile, h);
-    for (int s = 1; s < w.seg; ++s) through<NPT>(a, w, s, c, A, a.seg, h);
+    load_row<W>(a.seg + (at * a.channels + c) * NP, NP, n0, h);
+    for (int s = 1; s < w.seg; ++s) through<W>(a, NP, s, w.e, c, n0, A, a.seg, h);
 }
 // The gradient that a segment gets of the state it leaves.
-template <int NPT>
-__device__ __forceinline__ void end_of(const ScanArgs &a, const Work &w, int c, const float (&A)[4][NPT], float (&g)[4][NPT]) {
-    load_held<NPT>(a.back, (long long)w.e * a.tiles + w.tile, g);
-    for (int s = a.nseg - 1; s > w.seg; --s) through<NPT>(a, w, s, c, A, a.back, g);
+template <int W>
+__device__ __forceinline__ void end_of(const ScanArgs &a, int NP, const Work &w, int c, int n0, const float (&A)[W], float (&g)[W]) {
+    load_row<W>(a.back + ((long long)w.e * a.channels + c) * NP, NP, n0, g);
+    for (int s = a.nseg - 1; s > w.seg; --s) through<W>(a, NP, s, w.e, c, n0, A, a.back, g);
 }
 
 enum Mode {
@@ -295,202 +243,257 @@ enum Mode {
     MARKS    // the states in front of every fourth step
 };
 
-template <typename T, int NPT, int NL, int MODE, bool VEC>
-__global__ void __launch_bounds__(kThreads, MODE == BOTH ? 3 : 5) scan_kernel(ScanArgs a) {
-    grid_wait();
-    using S = Shape<NPT, NL>;
-    constexpr int CT = S::CT, NP = S::NP;
-    constexpr bool WITH_C = MODE == OUTPUT || MODE == BOTH, WITH_DY = MODE == BOTH;
-    using R = Rows<T, CT, VEC>;
-    __shared__ alignas(16) float sd[kSteps][CT], su[kSteps][CT], sg[WITH_DY ? kSteps : 1][CT], sD[CT], sbias[CT];
-    __shared__ alignas(16) float2 sB[kSteps][NP], sC[kSteps][WITH_C ? NP : 1];
-    const Work w = work_of<CT>(a, blockIdx.x % a.tiles, blockIdx.x / a.tiles);
-    const int lane = threadIdx.x % 32, ln = lane % NL, c = w.c0 + (threadIdx.x / 32 * S::GROUPS + lane / NL) * 4, n0 = ln * NPT, local = c - w.c0;
-    const int cols = w.c1 - w.c0;
-    const long long sx = a.Be * a.ldx, st = a.Be * a.lddt, sb = a.Be * a.ldb, sc = a.Be * a.ldc, sz = a.Be * a.ldz, sy = a.Be * a.ldy;
-    const T *x = static_cast<const T *>(a.x) + w.e * a.ldx + w.c0, *dt = static_cast<const T *>(a.dt) + w.e * a.lddt + w.c0;
-    const T *B = static_cast<const T *>(a.B) + w.e * a.ldb + (long long)w.group * a.N, *C = static_cast<const T *>(a.C) + w.e * a.ldc + (long long)w.group * a.N;
-    const T *z = a.z ? static_cast<const T *>(a.z) + w.e * a.ldz + w.c0 : nullptr;
-    const T *dy = WITH_DY ? static_cast<const T *>(a.dy) + w.e * a.ldy + w.c0 : nullptr;
-
-    pair32 A[NPT][2], h[NPT][2], P[WITH_DY ? NPT : 1][2], G[WITH_DY ? NPT : 1][2];
-    const long long held = ((long long)w.seg * a.Be + w.e) * a.tiles + w.tile;
-    {
-        float Af[4][NPT], f[4][NPT] = {};
-        load_state<NPT>(a.A, a, 0, c, w.c1, n0, Af);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int n = 0; n < NPT; ++n) Af[j][n] *= kLog2e;
-        pack<NPT>(Af, A);
-        if (MODE == ENDS || MODE == BOTH || a.nseg == 1) {
-            if (w.seg == 0) {
-                load_state<NPT>(a.state_in, a, w.e, c, w.c1, n0, f);
-                if (a.nseg > 1) store_held<NPT>(a.seg, held + (long long)(a.nseg - 1) * a.Be * a.tiles, f);
-            }
+// CPT neighbouring channels of a row, as they lie in memory.
+template <typename T, int CPT>
+struct Cell {
+    using Word = std::conditional_t<CPT == 1, T, std::conditional_t<sizeof(T) == 2, uint32_t, uint2>>;
+    Word w;
+    __device__ __forceinline__ void load(const T *p) { w = *reinterpret_cast<const Word *>(p); }
+    // the second one of a single channel is 0
+    __device__ __forceinline__ pair32 get() const {
+        if constexpr (CPT == 1) {
+            return pair_of(to_f32(w), 0.f);
         } else {
-            start_of<NPT>(a, w, c, Af, f);
-        }
-        pack<NPT>(f, h);
-        if constexpr (WITH_DY) {
-#pragma unroll
-            for (int n = 0; n < NPT; ++n) P[n][0] = P[n][1] = twice(1.f), G[n][0] = G[n][1] = 0;
+            Vec<T> v;
+            float f[Vec<T>::N];
+            if constexpr (sizeof(T) == 2) v.raw = make_uint4(w, 0, 0, 0);
+            else v.raw = make_uint4(w.x, w.y, 0, 0);
+            v.get(f);
+            return pair_of(f[0], f[1]);
         }
     }
-    R rx, rt;
-    rx.fetch(x + w.t0 * sx, sx, w.t1 - w.t0, cols);
-    rt.fetch(dt + w.t0 * st, st, w.t1 - w.t0, cols);
-    stage_channels(sbias, a.bias, w);
-    if constexpr (MODE == OUTPUT) stage_channels(sD, a.D, w);
-    __syncthreads();
-    float total[4] = {};
-    bool cut = false;
-    for (int t = w.t0; t < w.t1; t += kSteps) {
-        const int rows = w.t1 - t;
-        R rg, rz;
-        if constexpr (WITH_DY) {
-            rg.fetch(dy + t * sy, sy, rows, cols);
-            if (z) rz.fetch(z + t * sz, sz, rows, cols);
+    static __device__ __forceinline__ pair32 softplus(pair32 v) {
+        if constexpr (CPT == 1) return pair_of(softplus_fast(parts(v).x), 0.f);
+        else return softplus_pair(v);
+    }
+    static __device__ __forceinline__ pair32 silu(pair32 v) {
+        if constexpr (CPT == 1) return pair_of(parts(v).x * sigmoid_fast(parts(v).x), 0.f);
+        else return mul2(v, sigmoid_pair(v));
+    }
+    static __device__ __forceinline__ void put(T *p, pair32 v) {
+        const float2 f = parts(v);
+        if constexpr (CPT == 1) {
+            *p = from_f32<T>(f.x);
+        } else {
+            float all[Vec<T>::N] = {f.x, f.y};
+            Vec<T> r;
+            r.set(all);
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(p) = r.raw.x;
+            else *reinterpret_cast<uint2 *>(p) = make_uint2(r.raw.x, r.raw.y);
         }
+    }
+};
+
+// The rows of B and C of kSteps steps on their way from memory to shared memory, padded with zeros.
+template <typename T, int NP, bool WITH_C>
+struct FewRows {
+    static constexpr int EACH = kSteps * NP / kThreads;
+    static_assert(kThreads % NP == 0);
+    T b[EACH], c[WITH_C ? EACH : 1];
+    // B, C: of the first step
+    __device__ __forceinline__ void fetch(const T *B, const T *C, long long sb, long long sc, int rows, int N) {
+        const int n = threadIdx.x % NP, t0 = threadIdx.x / NP;
 #pragma unroll
-        for (int i = 0; i < R::PASSES; ++i) {
-            const int r = R::row(i), l = R::col(i);
-            if (r >= kSteps) break;
-            float d[R::V] = {}, u[R::V] = {}, g[R::V] = {};
-            if (r < rows && l < cols) {
-                float b[R::V];
-                rt.get(i, d);
-                rx.get(i, u);
-                get_floats(&sbias[l], b);
+        for (int i = 0; i < EACH; ++i) {
+            const int t = t0 + i * (kThreads / NP);
+            const bool ok = t < rows && n < N;
+            b[i] = ok ? B[t * sb + n] : from_f32<T>(0.f);
+            if (WITH_C) c[i] = ok ? C[t * sc + n] : from_f32<T>(0.f);
+        }
+    }
+    __device__ __forceinline__ void put(float (&B)[kSteps][NP], float (&C)[WITH_C ? kSteps : 1][NP]) const {
+        const int n = threadIdx.x % NP, t0 = threadIdx.x / NP;
 #pragma unroll
-                for (int v = 0; v < R::V; ++v) {
-                    d[v] += b[v];
-                    if (a.softplus) d[v] = softplus_fast(d[v]);
-                    u[v] *= d[v];
+        for (int i = 0; i < EACH; ++i) {
+            B[t0 + i * (kThreads / NP)][n] = to_f32(b[i]);
+            if (WITH_C) C[t0 + i * (kThreads / NP)][n] = to_f32(c[i]);
+        }
+    }
+};
+
+template <typename T, int NL, int CPT, int MODE>
+__global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) scan_kernel(ScanArgs a) {
+    grid_wait();
+    constexpr int W = 16, P = W / 2, NP = W * NL, CT = kThreads / NL * CPT;
+    constexpr bool WITH_C = MODE == OUTPUT || MODE == BOTH, WITH_DY = MODE == BOTH, WITH_Z = MODE == OUTPUT || MODE == BOTH;
+    using Word = Cell<T, CPT>;
+    __shared__ alignas(16) float sB[2][kSteps][NP], sC[2][WITH_C ? kSteps : 1][NP];
+    const Work w = work_of<CT>(a, blockIdx.x % a.tiles, blockIdx.x / a.tiles);
+    const int ln = threadIdx.x % NL, c = w.c0 + threadIdx.x / NL * CPT, n0 = ln * W;
+    const bool on = c < w.c1;
+    const long long sx = a.Be * a.ldx, st = a.Be * a.lddt, sb = a.Be * a.ldb, sc = a.Be * a.ldc, sz = a.Be * a.ldz, sy = a.Be * a.ldy;
+    const T *x = static_cast<const T *>(a.x) + w.e * a.ldx + c + w.t0 * sx, *dt = static_cast<const T *>(a.dt) + w.e * a.lddt + c + w.t0 * st;
+    const T *B = static_cast<const T *>(a.B) + w.e * a.ldb + (long long)w.group * a.N + w.t0 * sb;
+    const T *C = static_cast<const T *>(a.C) + w.e * a.ldc + (long long)w.group * a.N + w.t0 * sc;
+    const T *z = WITH_Z && a.z ? static_cast<const T *>(a.z) + w.e * a.ldz + c + w.t0 * sz : nullptr;
+    const T *dy = WITH_DY ? static_cast<const T *>(a.dy) + w.e * a.ldy + c + w.t0 * sy : nullptr;
+    T *y = MODE == OUTPUT ? static_cast<T *>(a.y) + w.e * a.ldy + c + w.t0 * sy : nullptr;
+
+    Word rx[4], rt[4], rz[WITH_Z ? 4 : 1], rg[WITH_DY ? 4 : 1];
+    const auto fetch = [&](int rows) {  // of the four steps at x, dt, z and dy
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (!on || k >= rows) break;
+            rx[k].load(x + k * sx);
+            rt[k].load(dt + k * st);
+            if (WITH_Z && z) rz[k].load(z + k * sz);
+            if (WITH_DY) rg[k].load(dy + k * sy);
+        }
+    };
+    fetch(w.t1 - w.t0);
+    FewRows<T, NP, WITH_C> few;
+    few.fetch(B, C, sb, sc, w.t1 - w.t0, a.N);
+
+    pair32 A[CPT][P], h[CPT][P], Pr[WITH_DY ? P : 1], G[WITH_DY ? P : 1], D = 0, bias = 0;
+    const long long held = ((long long)w.seg * a.Be + w.e) * a.channels;
+#pragma unroll
+    for (int j = 0; j < CPT; ++j) {
+        float Af[W] = {}, f[W] = {};
+        if (on) {
+            load_row<W>(a.A + (long long)(c + j) * a.N, a.N, n0, Af);
+#pragma unroll
+            for (int n = 0; n < W; ++n) Af[n] *= kLog2e;
+            if (MODE == ENDS || MODE == BOTH || a.nseg == 1) {
+                if (w.seg == 0) {
+                    if (a.state_in) load_row<W>(a.state_in + ((long long)w.e * a.channels + c + j) * a.N, a.N, n0, f);
+                    if (a.nseg > 1) store_row<W>(a.seg + (held + (long long)(a.nseg - 1) * a.Be * a.channels + c + j) * NP, NP, n0, f);
                 }
-                if constexpr (WITH_DY) {
-                    rg.get(i, g);
-                    if (z) {
-                        float f[R::V];
-                        rz.get(i, f);
-#pragma unroll
-                        for (int v = 0; v < R::V; ++v) g[v] *= f[v] * sigmoid_fast(f[v]);
-                    }
-                }
+            } else {
+                start_of<W>(a, NP, w, c + j, n0, Af, f);
             }
-            put_floats(&sd[r][l], d);
-            put_floats(&su[r][l], u);
-            if constexpr (WITH_DY) put_floats(&sg[r][l], g);
         }
-        stage_few<T, NP>(sB, B + t * sb, sb, rows, a.N);
-        if constexpr (WITH_C) stage_few<T, NP>(sC, C + t * sc, sc, rows, a.N);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            A[j][i] = pair_of(Af[2 * i], Af[2 * i + 1]);
+            h[j][i] = pair_of(f[2 * i], f[2 * i + 1]);
+        }
+    }
+    if (on) {
+        if (a.D && MODE == OUTPUT) D = pair_of(a.D[c], CPT == 2 ? a.D[c + CPT - 1] : 0.f);
+        if (a.bias) bias = pair_of(a.bias[c], CPT == 2 ? a.bias[c + CPT - 1] : 0.f);
+    }
+    if constexpr (WITH_DY) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) Pr[i] = twice(1.f), G[i] = 0;
+    }
+    few.put(sB[0], sC[0]);
+    __syncthreads();
+    pair32 total = 0;
+    bool cut = false;
+    int buffer = 0;
+    for (int t = w.t0; t < w.t1; t += kSteps, buffer ^= 1) {
+        const int rows = w.t1 - t;
         const uint32_t flag = flags_of(a, w.e, t, rows);
-        __syncthreads();
-        if (t + kSteps < w.t1) {
-            rx.fetch(x + (t + kSteps) * sx, sx, rows - kSteps, cols);
-            rt.fetch(dt + (t + kSteps) * st, st, rows - kSteps, cols);
-        }
+        B += kSteps * sb;
+        C += kSteps * sc;
+        if (rows > kSteps) few.fetch(B, C, sb, sc, rows - kSteps, a.N);
+#pragma unroll 1
         for (int s = 0; s < kSteps && s < rows; s += 4) {
             if constexpr (MODE == MARKS) {
-                float f[4][NPT];
-                unpack<NPT>(h, f);
-                store_held<NPT>(a.mark, ((long long)((t + s) / 4) * a.Be + w.e) * a.tiles + w.tile, f);
+                float *to = a.mark + (((long long)((t + s) / 4) * a.Be + w.e) * a.channels + c) * NP + n0;
+#pragma unroll
+                for (int j = 0; j < CPT; ++j)
+#pragma unroll
+                    for (int i = 0; i < P; i += 2)
+                        if (on) *reinterpret_cast<ulonglong2 *>(to + j * NP + 2 * i) = make_ulonglong2(h[j][i], h[j][i + 1]);
             }
-            float out[16];
+            pair32 xs[4], ds[4], zs[4], gs[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                pair32 d[2], u[2], g[2], acc[2] = {0, 0};
-                pair32 b[NPT], cc[NPT];
-                load_pairs(&sd[s + k][local], d);
-                load_pairs(&su[s + k][local], u);
-                load_few<NPT>(&sB[s + k][n0], b);
-                if constexpr (WITH_C) load_few<NPT>(&sC[s + k][n0], cc);
-                if constexpr (WITH_DY) load_pairs(&sg[s + k][local], g);
+                xs[k] = ds[k] = zs[k] = gs[k] = 0;
+                if (!on || s + k >= rows) continue;
+                xs[k] = rx[k].get();
+                ds[k] = add2(rt[k].get(), bias);
+                if (a.softplus) ds[k] = Word::softplus(ds[k]);
+                if (WITH_Z && z) zs[k] = Word::silu(rz[k].get());
+                if (WITH_DY) gs[k] = rg[k].get();
+                if (WITH_DY && z) gs[k] = mul2(gs[k], zs[k]);
+            }
+            x += 4 * sx;
+            dt += 4 * st;
+            if (WITH_Z && z) z += 4 * sz;
+            if (WITH_DY) dy += 4 * sy;
+            fetch(rows - s - 4);
 #pragma unroll
-                for (int n = 0; n < NPT; ++n)
+            for (int k = 0; k < 4; ++k) {
+                pair32 out[CPT];
+                const float2 d = parts(ds[k]), u = parts(mul2(ds[k], xs[k])), g = parts(gs[k]);
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        const pair32 f = exp2_pair(mul2(d[p], A[n][p]));
-                        h[n][p] = fma2(f, h[n][p], mul2(u[p], b[n]));
-                        if constexpr (MODE == OUTPUT) acc[p] = fma2(cc[n], h[n][p], acc[p]);
-                        if constexpr (WITH_DY) {
-                            P[n][p] = mul2(P[n][p], f);
-                            if (!cut) G[n][p] = fma2(mul2(P[n][p], g[p]), cc[n], G[n][p]);
+                for (int j = 0; j < CPT; ++j) out[j] = 0;
+#pragma unroll
+                for (int i = 0; i < P; i += 2) {
+                    pair32 b[2], cc[2] = {};
+                    load_pairs(&sB[buffer][s + k][n0 + 2 * i], b);
+                    if constexpr (WITH_C) load_pairs(&sC[buffer][s + k][n0 + 2 * i], cc);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int j = 0; j < CPT; ++j) {
+                            const pair32 f = exp2_pair(mul2(twice(j == 0 ? d.x : d.y), A[j][i + m]));
+                            h[j][i + m] = fma2(f, h[j][i + m], mul2(twice(j == 0 ? u.x : u.y), b[m]));
+                            if constexpr (MODE == OUTPUT) out[j] = fma2(cc[m], h[j][i + m], out[j]);
+                            if constexpr (WITH_DY) {
+                                Pr[i + m] = mul2(Pr[i + m], f);
+                                if (!cut) G[i + m] = fma2(mul2(Pr[i + m], twice(g.x)), cc[m], G[i + m]);
+                            }
                         }
-                    }
-                if constexpr (MODE == OUTPUT) {
-                    const float2 p = parts(acc[0]), q = parts(acc[1]);
-                    out[4 * k] = p.x, out[4 * k + 1] = p.y, out[4 * k + 2] = q.x, out[4 * k + 3] = q.y;
                 }
-                if constexpr (MODE == ENDS || MODE == BOTH) {
-                    const float2 p = parts(d[0]), q = parts(d[1]);
-                    total[0] += p.x, total[1] += p.y, total[2] += q.x, total[3] += q.y;
+                if constexpr (MODE == ENDS || MODE == BOTH) total = add2(total, ds[k]);
+                if constexpr (MODE == OUTPUT) {
+                    const float2 o = parts(out[0]), q = parts(out[CPT - 1]);
+                    float lo = o.x + o.y, hi = CPT == 2 ? q.x + q.y : 0.f;
+#pragma unroll
+                    for (int m = NL / 2; m > 0; m /= 2) {
+                        lo += __shfl_xor_sync(0xffffffffu, lo, m);
+                        if (CPT == 2) hi += __shfl_xor_sync(0xffffffffu, hi, m);
+                    }
+                    pair32 v = a.D ? fma2(D, xs[k], pair_of(lo, hi)) : pair_of(lo, hi);
+                    if (z) v = mul2(v, zs[k]);
+                    if (on && ln == 0 && s + k < rows) Word::put(y + k * sy, v);
                 }
                 if (flag >> (s + k) & 1) {
                     cut = true;
 #pragma unroll
-                    for (int n = 0; n < NPT; ++n) h[n][0] = h[n][1] = 0;
+                    for (int j = 0; j < CPT; ++j)
+#pragma unroll
+                        for (int i = 0; i < P; ++i) h[j][i] = 0;
                 }
             }
-            if constexpr (MODE == OUTPUT) {
-                // every lane of the channels has read the step sizes of these steps: the sums take their place
-                spread_sum<16, NL, 1>(out, lane);
-                constexpr int LEFT = 16 / NL;
-                const int first = spread_first<16, NL>(ln);
-                float *to = &sd[s + first / 4][local + first % 4];
-                if constexpr (LEFT == 4) *reinterpret_cast<float4 *>(to) = make_float4(out[0], out[1], out[2], out[3]);
-                else if constexpr (LEFT == 2) *reinterpret_cast<float2 *>(to) = make_float2(out[0], out[1]);
-                else *to = out[0];
-            }
+            if (MODE == OUTPUT) y += 4 * sy;
         }
+        if (rows > kSteps) few.put(sB[buffer ^ 1], sC[buffer ^ 1]);
         __syncthreads();
-        if constexpr (MODE == OUTPUT) {
-            T *y = static_cast<T *>(a.y) + w.e * a.ldy + w.c0;
-            R again, gate;
-            again.fetch(x + t * sx, sx, rows, cols);
-            if (z) gate.fetch(z + t * sz, sz, rows, cols);
-#pragma unroll
-            for (int i = 0; i < R::PASSES; ++i) {
-                const int r = R::row(i), l = R::col(i);
-                if (r >= kSteps || r >= rows || l >= cols) continue;
-                float o[R::V], v[R::V];
-                get_floats(&sd[r][l], o);
-                if (a.D) {
-                    float D[R::V];
-                    again.get(i, v);
-                    get_floats(&sD[l], D);
-#pragma unroll
-                    for (int k = 0; k < R::V; ++k) o[k] = fmaf(D[k], v[k], o[k]);
-                }
-                if (z) {
-                    gate.get(i, v);
-#pragma unroll
-                    for (int k = 0; k < R::V; ++k) o[k] *= v[k] * sigmoid_fast(v[k]);
-                }
-                R::put(y + (t + r) * sy + l, o);
-            }
-            __syncthreads();
-        }
     }
-    float f[4][NPT];
-    unpack<NPT>(h, f);
-    if constexpr (MODE == OUTPUT) {
-        if (a.state_out && w.t1 == a.T) store_state<NPT>(a.state_out, a, w.e, c, w.c1, n0, f);
+    if (!on) return;
+    const long long at = (long long)w.seg * a.Be + w.e;
+#pragma unroll
+    for (int j = 0; j < CPT; ++j) {
+        float f[W];
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const float2 v = parts(h[j][i]);
+            f[2 * i] = v.x, f[2 * i + 1] = v.y;
+        }
+        if constexpr (MODE == OUTPUT) {
+            if (a.state_out && w.t1 == a.T) store_row<W>(a.state_out + ((long long)w.e * a.channels + c + j) * a.N, a.N, n0, f);
+        }
+        if constexpr (MODE == ENDS || MODE == BOTH) {
+            if (w.seg < a.nseg - 1) store_row<W>(a.seg + (held + c + j) * NP, NP, n0, f);
+            const float2 sums = parts(total);
+            if (ln == 0) a.sum[at * a.channels + c + j] = j == 0 ? sums.x : sums.y;
+        }
+        if constexpr (MODE == BOTH) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const float2 v = parts(G[i]);
+                f[2 * i] = w.seg > 0 ? v.x : 0.f, f[2 * i + 1] = w.seg > 0 ? v.y : 0.f;
+            }
+            if (w.seg == 0 && a.dstate_out) load_row<W>(a.dstate_out + ((long long)w.e * a.channels + c + j) * a.N, a.N, n0, f);
+            store_row<W>(a.back + (held + c + j) * NP, NP, n0, f);
+        }
     }
     if constexpr (MODE == ENDS || MODE == BOTH) {
-        const long long at = (long long)w.seg * a.Be + w.e;
-        if (w.seg < a.nseg - 1) store_held<NPT>(a.seg, held, f);
-        if (ln == 0) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c + j < w.c1) a.sum[at * a.channels + c + j] = total[j];
-        }
         if (threadIdx.x == 0 && w.tile == 0) a.cut[at] = cut;
-    }
-    if constexpr (MODE == BOTH) {
-        if (w.seg > 0) unpack<NPT>(G, f);
-        else load_state<NPT>(a.dstate_out, a, w.e, c, w.c1, n0, f);
-        store_held<NPT>(a.back, held, f);
     }
 }
 
@@ -500,6 +503,33 @@ __global__ void __launch_bounds__(kThreads, MODE == BOTH ? 3 : 5) scan_kernel(Sc
 // Four steps at a time, backwards: from the states in front of them forwards once more, which leaves the factors and exp(d A) h' of the
 // four steps in registers (and y and the sums of dC on the way), then backwards over these.  A block goes through as many envs, or
 // segments, as fall to it and keeps its shares of the parameters' gradients.
+// Four elements of the states of four channels, [e][channel][N] in memory; zeros where there are none.
+__device__ __forceinline__ void load_block(const float *from, const ScanArgs &a, int e, int c, int c1, int n0, float (&h)[4][4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) h[j][n] = 0.f;
+        if (from && c + j < c1) load_row<4>(from + ((long long)e * a.channels + c + j) * a.N, a.N, n0, h[j]);
+    }
+}
+__device__ __forceinline__ void store_block(float *to, const ScanArgs &a, int e, int c, int c1, int n0, const float (&h)[4][4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (c + j < c1) store_row<4>(to + ((long long)e * a.channels + c + j) * a.N, a.N, n0, h[j]);
+}
+// As pairs of neighbouring channels.
+__device__ __forceinline__ void pack(const float (&h)[4][4], pair32 (&p)[4][2]) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) p[n][0] = pair_of(h[0][n], h[1][n]), p[n][1] = pair_of(h[2][n], h[3][n]);
+}
+__device__ __forceinline__ void unpack(const pair32 (&p)[4][2], float (&h)[4][4]) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const float2 u = parts(p[n][0]), v = parts(p[n][1]);
+        h[0][n] = u.x, h[1][n] = u.y, h[2][n] = v.x, h[3][n] = v.y;
+    }
+}
+
 // A long sum as two numbers: what hi rounds away stays in lo (Knuth's error of a sum).
 __device__ __forceinline__ void add_to(float &hi, float &lo, float v) {
     const float sum = __fadd_rn(hi, v), w = __fsub_rn(sum, hi);
@@ -509,7 +539,7 @@ __device__ __forceinline__ void add_to(float &hi, float &lo, float v) {
 
 template <typename T, int NL, bool VEC>
 struct GradShared {
-    static constexpr int CT = Shape<4, NL>::CT, NP = Shape<4, NL>::NP;
+    static constexpr int CT = Shape<NL>::CT, NP = Shape<NL>::NP;
     float sd[kSteps][CT], su[kSteps][CT], sg[kSteps][CT], sy[kSteps][CT], sD[CT], sbias[CT];
     float2 sB[kSteps][NP], sC[kSteps][NP];
     float few[kThreads / 32][kSteps][2 * NP];
@@ -517,15 +547,16 @@ struct GradShared {
     float dA[2][16][kThreads], kept[2][2][Rows<T, CT, VEC>::V][kThreads];  // [..][2]: hi and lo of the sums
 };
 
-__device__ __forceinline__ void copy_async(float *to, const float *from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+// Four numbers, or zeros.
+__device__ __forceinline__ void copy_async(float *to, const float *from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 
 template <typename T, int NL, bool VEC>
 __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
     grid_wait();
     constexpr int NPT = 4;
-    using S = Shape<NPT, NL>;
+    using S = Shape<NL>;
     constexpr int CT = S::CT, NP = S::NP, GROUPS = S::GROUPS;
     using R = Rows<T, CT, VEC>;
     extern __shared__ __align__(16) char smem[];
@@ -538,12 +569,12 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
     pair32 A[NPT][2], g[NPT][2], dA[NPT][2];
     {
         float f[4][NPT];
-        load_state<NPT>(a.A, a, 0, c, w.c1, n0, f);
+        load_block(a.A, a, 0, c, w.c1, n0, f);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int n = 0; n < NPT; ++n) f[j][n] *= kLog2e;
-        pack<NPT>(f, A);
+        pack(f, A);
 #pragma unroll
         for (int n = 0; n < NPT; ++n) dA[n][0] = dA[n][1] = 0;
     }
@@ -565,12 +596,17 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
         {
             float f[4][NPT], Af[4][NPT];
             if (a.nseg == 1) {
-                load_state<NPT>(a.dstate_out, a, w.e, c, w.c1, n0, f);
+                load_block(a.dstate_out, a, w.e, c, w.c1, n0, f);
             } else {
-                unpack<NPT>(A, Af);
-                end_of<NPT>(a, w, c, Af, f);
+                unpack(A, Af);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) f[j][n] = 0.f;
+                    if (c + j < w.c1) end_of<4>(a, NP, w, c + j, n0, Af[j], f[j]);
+                }
             }
-            pack<NPT>(f, g);
+            pack(f, g);
         }
         for (int t = w.t0 + (w.t1 - 1 - w.t0) / kSteps * kSteps; t >= w.t0; t -= kSteps) {
             const int rows = w.t1 - t;
@@ -579,9 +615,9 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
                 if (4 * m >= rows) break;
-                const float *from = a.mark + (((long long)(t / 4 + m) * a.Be + w.e) * a.tiles + tile) * (kThreads * 16) + threadIdx.x * 4;
+                const float *from = a.mark + (((long long)(t / 4 + m) * a.Be + w.e) * a.channels + c) * NP + n0;
 #pragma unroll
-                for (int n = 0; n < NPT; ++n) copy_async(&s.mark[m][n][threadIdx.x * 4], from + n * kThreads * 4);
+                for (int j = 0; j < 4; ++j) copy_async(&s.mark[m][j][threadIdx.x * 4], c + j < w.c1 ? from + j * NP : a.mark, c + j < w.c1);
             }
             {
                 R rx, rt, rg, rz;
@@ -595,25 +631,30 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                 for (int i = 0; i < R::PASSES; ++i) {
                     const int r = R::row(i), l = R::col(i);
                     if (r >= kSteps) break;
-                    float d[R::V] = {}, u[R::V] = {}, v[R::V] = {};
+                    float d[R::V], u[R::V], v[R::V];
                     if (r < rows && l < cols) {
                         rt.get(i, d);
                         rx.get(i, u);
                         rg.get(i, v);
-                        float b[R::V];
+                        float b[R::V], f[R::V];
                         get_floats(&s.sbias[l], b);
+                        if (z) rz.get(i, f);
 #pragma unroll
-                        for (int k = 0; k < R::V; ++k) {
-                            d[k] += b[k];
-                            if (a.softplus) d[k] = softplus_fast(d[k]);
-                            u[k] *= d[k];
+                        for (int k = 0; k < R::V; k += 2) {
+                            constexpr int TWO = R::V > 1;
+                            pair32 step = add2(pair_of(d[k], d[k + TWO]), pair_of(b[k], b[k + TWO]));
+                            if (a.softplus) step = softplus_pair(step);
+                            const float2 p = parts(step), q = parts(mul2(pair_of(u[k], u[k + TWO]), step));
+                            d[k] = p.x, d[k + TWO] = p.y, u[k] = q.x, u[k + TWO] = q.y;
+                            if (z) {
+                                const pair32 zz = pair_of(f[k], f[k + TWO]);
+                                const float2 g = parts(mul2(pair_of(v[k], v[k + TWO]), mul2(zz, sigmoid_pair(zz))));
+                                v[k] = g.x, v[k + TWO] = g.y;
+                            }
                         }
-                        if (z) {
-                            float f[R::V];
-                            rz.get(i, f);
+                    } else {
 #pragma unroll
-                            for (int k = 0; k < R::V; ++k) v[k] *= f[k] * sigmoid_fast(f[k]);
-                        }
+                        for (int k = 0; k < R::V; ++k) d[k] = u[k] = v[k] = 0.f;
                     }
                     put_floats(&s.sd[r][l], d);
                     put_floats(&s.su[r][l], u);
@@ -628,8 +669,10 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                 pair32 f[4][NPT][2], q[4][NPT][2];  // of each step the factors, and these times the state in front
                 {
                     pair32 h[NPT][2];
+                    float start[4][NPT];
 #pragma unroll
-                    for (int n = 0; n < NPT; ++n) load_pairs(&s.mark[m][n][threadIdx.x * 4], h[n]);
+                    for (int j = 0; j < 4; ++j) get_floats(&s.mark[m][j][threadIdx.x * 4], start[j]);
+                    pack(start, h);
 #pragma unroll
                     for (int k = 0; k < 4; k += 2) {
                         float ys[8], cs[8];
@@ -641,8 +684,8 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                             load_pairs(&s.sd[r][local], d);
                             load_pairs(&s.su[r][local], u);
                             load_pairs(&s.sg[r][local], v);
-                            load_few<NPT>(&s.sB[r][n0], b);
-                            load_few<NPT>(&s.sC[r][n0], cc);
+                            load_few(&s.sB[r][n0], b);
+                            load_few(&s.sC[r][n0], cc);
                             if (k + i > 0 && flag >> (r - 1) & 1) {
 #pragma unroll
                                 for (int n = 0; n < NPT; ++n) h[n][0] = h[n][1] = 0;
@@ -686,8 +729,8 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                         load_pairs(&s.sd[r][local], d);
                         load_pairs(&s.su[r][local], u);
                         load_pairs(&s.sg[r][local], v);
-                        load_few<NPT>(&s.sB[r][n0], b);
-                        load_few<NPT>(&s.sC[r][n0], cc);
+                        load_few(&s.sB[r][n0], b);
+                        load_few(&s.sC[r][n0], cc);
                         if (flag >> r & 1) {
 #pragma unroll
                             for (int n = 0; n < NPT; ++n) g[n][0] = g[n][1] = 0;
@@ -790,7 +833,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                 }
             }
             float f[4][NPT];
-            unpack<NPT>(dA, f);
+            unpack(dA, f);
 #pragma unroll
             for (int n = 0; n < 16; ++n) add_to(s.dA[0][n][threadIdx.x], s.dA[1][n][threadIdx.x], f[n / 4][n % 4]);
 #pragma unroll
@@ -798,8 +841,8 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
         }
         if (a.dstate_in && w.t0 == 0) {
             float f[4][NPT];
-            unpack<NPT>(g, f);
-            store_state<NPT>(a.dstate_in, a, w.e, c, w.c1, n0, f);
+            unpack(g, f);
+            store_block(a.dstate_in, a, w.e, c, w.c1, n0, f);
         }
     }
     if (!a.part) return;
@@ -808,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
         float f[4][NPT];
 #pragma unroll
         for (int n = 0; n < 16; ++n) f[n / 4][n % 4] = s.dA[0][n][threadIdx.x] + s.dA[1][n][threadIdx.x];
-        store_state<NPT>(part, a, 0, c, w.c1, n0, f);
+        store_block(part, a, 0, c, w.c1, n0, f);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * CT; i += kThreads) {
@@ -918,24 +961,26 @@ bool misaligned(std::initializer_list<const void *> ps, size_t a) {
 
 // By sizes alone, so that the workspace and the order of sums go by them.
 struct Plan {
-    int NL, CT, NP, tiles, group_tiles, len, nseg, parts;
+    int NL, NP, len, nseg, parts;  // NL: lanes of a channel forwards
+    int tiles, group_tiles;        // backwards
     size_t seg, sums, mark, few, part;  // floats of each area of the workspace
 };
 Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     Plan p = {};
-    p.NL = d->N <= 16 ? 4 : d->N <= 32 ? 8 : 16;
-    p.NP = 4 * p.NL;
-    p.CT = 512 / p.NL;
+    p.NL = d->N <= 16 ? 1 : d->N <= 32 ? 2 : 4;
+    p.NP = 16 * p.NL;
     const auto up = [](size_t n) { return (n + 7) & ~(size_t)7; };  // whole 32 bytes
-    p.group_tiles = ppo_cdiv(d->channels / d->groups, p.CT);
+    const int per = d->channels / d->groups;
+    p.group_tiles = ppo_cdiv(per, 128 / p.NL);
     p.tiles = p.group_tiles * d->groups;
-    const long long blocks = (long long)d->Be * p.tiles, want = (bwd ? 2 : 4) * 148;
-    long long n = blocks < want ? want / blocks : 1;
+    // segments: as many as give the GPU the warps that it can hold at a time, none shorter than 64 steps
+    const long long warps = bwd ? 4ll * d->Be * p.tiles : (long long)d->Be * d->groups * ppo_cdiv(per, 64 / p.NL), want = (bwd ? 8 : 16) * 148;
+    long long n = warps < want ? want / warps : 1;
     const int most = ppo_cdiv(d->T, 64);
     if (n > most) n = most;
     p.len = ppo_cdiv(ppo_cdiv(d->T, n), kSteps) * kSteps;
     p.nseg = ppo_cdiv(d->T, p.len);
-    const size_t held = (size_t)d->Be * p.tiles * kThreads * 16;
+    const size_t held = (size_t)d->Be * d->channels * p.NP;
     if (p.nseg > 1) {
         p.seg = p.nseg * held;
         p.sums = up((size_t)p.nseg * d->Be * (d->channels + 1));
@@ -943,8 +988,8 @@ Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     if (bwd) {
         p.mark = ppo_cdiv(d->T, 4) * held;
         p.few = (size_t)d->T * d->Be * p.tiles * 2 * p.NP;
-        const long long items = (long long)d->Be * p.nseg, per = p.tiles < 2 * 148 ? 2 * 148 / p.tiles : 1;  // one round of two blocks an SM
-        p.parts = (int)(items < per ? items : per);
+        const long long items = (long long)d->Be * p.nseg, slices = p.tiles < 2 * 148 ? 2 * 148 / p.tiles : 1;  // one round of two blocks an SM
+        p.parts = (int)(items < slices ? items : slices);
         p.part = up((size_t)p.parts * d->channels * (d->N + 2));
     }
     return p;
@@ -982,23 +1027,38 @@ ScanArgs args(const ppo_selective_scan_desc *d, const Plan &p, const void *x, co
     return a;
 }
 
-// Rows of whole, aligned vectors of 16 bytes, also where a group ends.
-bool vectors(const ppo_selective_scan_desc *d, std::initializer_list<const void *> ps) {
-    const int V = 16 / (int)elem_bytes(d->dtype);
-    return d->channels / d->groups % V == 0 && d->ldx % V == 0 && d->lddt % V == 0 && d->ldz % V == 0 && d->ldy % V == 0 && !misaligned(ps, 16);
+// Rows of whole vectors of V elements, aligned to these, also where a group ends.
+bool vectors(const ppo_selective_scan_desc *d, int V, std::initializer_list<const void *> ps) {
+    return d->channels / d->groups % V == 0 && d->ldx % V == 0 && d->lddt % V == 0 && d->ldz % V == 0 && d->ldy % V == 0 &&
+           !misaligned(ps, V * elem_bytes(d->dtype));
 }
 
-// fn(T{}, lanes of a channel, whether rows are vectors)
+// fn(T{}, NL)
 template <typename F>
-int with_shape(const ppo_selective_scan_desc *d, const Plan &p, bool vec, F &&fn) {
+int with_lanes(const ppo_selective_scan_desc *d, const Plan &p, F &&fn) {
     return with_elem(d->dtype, [&](auto t) -> int {
-        const auto lanes = [&](auto v) -> int {
-            if (p.NL == 4) return fn(t, std::integral_constant<int, 4>{}, v);
-            if (p.NL == 8) return fn(t, std::integral_constant<int, 8>{}, v);
-            return fn(t, std::integral_constant<int, 16>{}, v);
-        };
-        return vec ? lanes(std::true_type{}) : lanes(std::false_type{});
+        if (p.NL == 1) return fn(t, std::integral_constant<int, 1>{});
+        if (p.NL == 2) return fn(t, std::integral_constant<int, 2>{});
+        return fn(t, std::integral_constant<int, 4>{});
     });
+}
+// A pass over the first `segs` segments, `two` channels a thread.
+template <typename T, int NL, int CPT, int MODE>
+int pass_of(ScanArgs a, int segs, cudaStream_t st) {
+    a.group_tiles = ppo_cdiv(a.per, kThreads / NL * CPT);
+    a.tiles = a.group_tiles * a.groups;
+    return ppo_launch(scan_kernel<T, NL, CPT, MODE>, dim3((unsigned)(a.Be * a.tiles) * segs), dim3(kThreads), 0, st, a);
+}
+template <typename T, int NL, bool VEC>
+int back_launch(const ScanArgs &a, cudaStream_t st) {
+    constexpr size_t smem = sizeof(GradShared<T, NL, VEC>);
+    static PerDevice<bool> allowed;
+    PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(scan_bwd_kernel<T, NL, VEC>, smem); }));
+    return ppo_launch(scan_bwd_kernel<T, NL, VEC>, dim3((unsigned)(a.tiles * a.parts)), dim3(kThreads), smem, st, a);
+}
+template <typename T, int NL, int MODE>
+int pass(const ScanArgs &a, bool two, int segs, cudaStream_t st) {
+    return two ? pass_of<T, NL, 2, MODE>(a, segs, st) : pass_of<T, NL, 1, MODE>(a, segs, st);
 }
 
 }  // namespace
@@ -1029,14 +1089,12 @@ extern "C" int ppo_selective_scan_fwd(const ppo_selective_scan_desc *d, const vo
     a.sum = a.seg + p.seg;
     a.cut = reinterpret_cast<int *>(a.sum + (size_t)p.nseg * d->Be * d->channels);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const unsigned blocks = (unsigned)(d->Be * p.tiles);
-    return with_shape(d, p, vectors(d, {x, dt, z, y}), [&](auto t, auto nl, auto v) -> int {
+    const bool two = vectors(d, 2, {x, dt, z, y});
+    return with_lanes(d, p, [&](auto t, auto nl) -> int {
         using T = decltype(t);
         constexpr int NL = decltype(nl)::value;
-        constexpr bool VEC = decltype(v)::value;
-        // the last segment hands nothing on
-        if (p.nseg > 1) PPO_TRY(ppo_launch(scan_kernel<T, 4, NL, ENDS, VEC>, dim3(blocks * (p.nseg - 1)), dim3(kThreads), 0, st, a));
-        return ppo_launch(scan_kernel<T, 4, NL, OUTPUT, VEC>, dim3(blocks * p.nseg), dim3(kThreads), 0, st, a);
+        if (p.nseg > 1) PPO_TRY((pass<T, NL, ENDS>(a, two, p.nseg - 1, st)));  // the last segment hands nothing on
+        return pass<T, NL, OUTPUT>(a, two, p.nseg, st);
     });
 }
 
@@ -1072,19 +1130,15 @@ extern "C" int ppo_selective_scan_bwd(const ppo_selective_scan_desc *d, const vo
     a.sum = a.few + p.few + p.part;
     a.cut = reinterpret_cast<int *>(a.sum + (size_t)p.nseg * d->Be * d->channels);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const unsigned blocks = (unsigned)(d->Be * p.tiles) * p.nseg;
-    PPO_TRY(with_shape(d, p, vectors(d, {x, dt, z, dy, dx, ddt, dz}), [&](auto t, auto nl, auto v) -> int {
+    const bool two = vectors(d, 2, {x, dt}), vec = vectors(d, 16 / (int)elem_bytes(d->dtype), {x, dt, z, dy, dx, ddt, dz});
+    PPO_TRY(with_lanes(d, p, [&](auto t, auto nl) -> int {
         using T = decltype(t);
         constexpr int NL = decltype(nl)::value;
-        constexpr bool VEC = decltype(v)::value;
-        constexpr size_t smem = sizeof(GradShared<T, NL, VEC>);
-        static PerDevice<bool> allowed;
-        PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(scan_bwd_kernel<T, NL, VEC>, smem); }));
-        if (p.nseg > 1) PPO_TRY(ppo_launch(scan_kernel<T, 4, NL, BOTH, VEC>, dim3(blocks), dim3(kThreads), 0, st, a));
-        PPO_TRY(ppo_launch(scan_kernel<T, 4, NL, MARKS, VEC>, dim3(blocks), dim3(kThreads), 0, st, a));
-        PPO_TRY(ppo_launch(scan_bwd_kernel<T, NL, VEC>, dim3((unsigned)(p.tiles * p.parts)), dim3(kThreads), smem, st, a));
+        if (p.nseg > 1) PPO_TRY((pass_of<T, NL, 1, BOTH>(a, p.nseg, st)));
+        PPO_TRY((pass<T, NL, MARKS>(a, two, p.nseg, st)));
+        PPO_TRY((vec ? back_launch<T, 4 * NL, true>(a, st) : back_launch<T, 4 * NL, false>(a, st)));
         const long long few = (long long)d->T * d->Be * d->groups * 2 * p.NP;
-        return ppo_launch(scan_few_kernel<T, 4 * NL>, dim3((unsigned)((few + 255) / 256)), dim3(256), 0, st, a);
+        return ppo_launch(scan_few_kernel<T, 16 * NL>, dim3((unsigned)((few + 255) / 256)), dim3(256), 0, st, a);
     }));
     return params ? ppo_param_sum(a.part, p.parts, {{dA, dD, ddt_bias}, {d->channels * d->N, d->channels, d->channels}}, accumulate, st) : PPO_OK;
 }
