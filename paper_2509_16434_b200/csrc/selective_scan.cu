@@ -33,11 +33,16 @@ struct ScanArgs {
     // of the state that is left); what its step sizes add up to for each channel, and whether a flag is set in it.
     float *seg, *back, *sum;
     int *cut;
-    float *mark;  // the states in front of every fourth step, [ceil(T / 4)][Be][channels][NP]
+    float *mark;  // the states in front of every 16th step, [ceil(T / 16)][Be][channels][NP] (up to 16 steps: none)
     float *few;   // shares of the gradients of B and C, [group_tiles][T * Be][groups][2][NP]
     float *part;  // shares of the gradients of A, D and dt_bias, [parts][channels * (N + 2)]
     int parts;
 };
+
+// exp(d A), A times log2(e).  The hardware's exponential lies 0.4 units of 2^-24 too low on average for arguments between -0.5 and -0.01, which adds up over
+// the hundreds of steps that a state remembers; with its argument moved by 2e-8 the mean is within 0.2 from -0.5 to 0 (one million arguments
+// each), as near as expf's, at no cost.
+__device__ __forceinline__ pair32 factors(pair32 d, pair32 A) { return exp2_pair(fma2(d, A, twice(2e-8f))); }
 
 // Sums of V values over LANES lanes, STRIDE apart: halves go to the lanes' halves as long as there are values, lane bit by lane bit from the
 // highest; a lane is left with max(1, V / LANES) of them in v[0 ..].  index() says which.
@@ -69,10 +74,10 @@ __device__ __forceinline__ int spread_first(int l) {
     else return 0;
 }
 
-// Backwards NL lanes share four channels and hold four elements each of their states.
+// Backwards NL lanes share four channels and hold two elements each of their states.
 template <int NL>
 struct Shape {
-    static constexpr int NP = 4 * NL, GROUPS = 32 / NL, CT = 4 * GROUPS * (kThreads / 32);
+    static constexpr int NP = 2 * NL, GROUPS = 32 / NL, CT = 4 * GROUPS * (kThreads / 32);
 };
 
 // What a block works on: a tile of channels of one env over steps t0 .. t1 - 1.
@@ -93,11 +98,11 @@ __device__ __forceinline__ Work work_of(const ScanArgs &a, int tile, long long i
     return w;
 }
 
-// kSteps rows of a tile's channels on their way from memory: vectors of V elements, dealt out to the threads.
+// kSteps rows of a tile's channels on their way from memory: vectors of four elements, or single ones, dealt out to the threads.
 template <typename T, int CT, bool VEC>
 struct Rows {
-    static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1, COLS = CT / V, PASSES = (kSteps * COLS + kThreads - 1) / kThreads;
-    using Raw = std::conditional_t<VEC, uint4, T>;
+    static constexpr int V = VEC ? 4 : 1, COLS = CT / V, PASSES = (kSteps * COLS + kThreads - 1) / kThreads;
+    using Raw = std::conditional_t<VEC, std::conditional_t<sizeof(T) == 4, uint4, uint2>, T>;
     Raw raw[PASSES];
     static __device__ __forceinline__ int row(int i) { return (threadIdx.x + i * kThreads) / COLS; }
     static __device__ __forceinline__ int col(int i) { return (threadIdx.x + i * kThreads) % COLS * V; }
@@ -107,57 +112,48 @@ struct Rows {
         for (int i = 0; i < PASSES; ++i)
             if (row(i) < min(rows, kSteps) && col(i) < cols) raw[i] = *reinterpret_cast<const Raw *>(p + row(i) * step + col(i));
     }
-    __device__ __forceinline__ void get(int i, float (&v)[V]) const {
+    // as pairs; of a single element the second is 0
+    static constexpr int PAIRS = (V + 1) / 2;
+    static __device__ __forceinline__ void get(const Raw &w, pair32 (&v)[PAIRS]) {
         if constexpr (VEC) {
             Vec<T> x;
-            x.raw = raw[i];
-            x.get(v);
+            float f[Vec<T>::N];
+            if constexpr (sizeof(T) == 4) x.raw = w;
+            else x.raw = make_uint4(w.x, w.y, 0, 0);
+            x.get(f);
+            v[0] = pair_of(f[0], f[1]), v[1] = pair_of(f[2], f[3]);
         } else {
-            v[0] = to_f32(raw[i]);
+            v[0] = pair_of(to_f32(w), 0.f);
         }
     }
-    static __device__ __forceinline__ void put(T *p, const float (&v)[V]) {
+    static __device__ __forceinline__ void put(T *p, const pair32 (&v)[PAIRS]) {
         if constexpr (VEC) {
+            const float2 a = parts(v[0]), b = parts(v[1]);
+            float f[Vec<T>::N] = {a.x, a.y, b.x, b.y};
             Vec<T> x;
-            x.set(v);
-            *reinterpret_cast<uint4 *>(p) = x.raw;
+            x.set(f);
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(p) = x.raw;
+            else *reinterpret_cast<uint2 *>(p) = make_uint2(x.raw.x, x.raw.y);
         } else {
-            *p = from_f32<T>(v[0]);
+            *p = from_f32<T>(parts(v[0]).x);
         }
     }
+    // of 32-bit numbers in shared memory
+    static __device__ __forceinline__ void put_shared(float *p, const pair32 (&v)[PAIRS]) {
+        if constexpr (VEC) *reinterpret_cast<ulonglong2 *>(p) = make_ulonglong2(v[0], v[1]);
+        else *p = parts(v[0]).x;
+    }
+    static __device__ __forceinline__ void get_shared(const float *p, pair32 (&v)[PAIRS]) {
+        if constexpr (VEC) {
+            const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(p);
+            v[0] = u.x, v[1] = u.y;
+        } else {
+            v[0] = pair_of(*p, 0.f);
+        }
+    }
+    static __device__ __forceinline__ pair32 softplus(pair32 v) { return VEC ? softplus_pair(v) : pair_of(softplus_fast(parts(v).x), 0.f); }
+    static __device__ __forceinline__ pair32 sigmoid(pair32 v) { return VEC ? sigmoid_pair(v) : pair_of(sigmoid_fast(parts(v).x), 0.f); }
 };
-template <int V>
-__device__ __forceinline__ void put_floats(float *p, const float (&v)[V]) {
-    if constexpr (V == 1) {
-        *p = v[0];
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    }
-}
-template <int V>
-__device__ __forceinline__ void get_floats(const float *p, float (&v)[V]) {
-    if constexpr (V == 1) {
-        v[0] = *p;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; i += 4) {
-            const float4 f = *reinterpret_cast<const float4 *>(p + i);
-            v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
-        }
-    }
-}
-
-// The rows of B or C, padded with zeros to NP elements, each of them twice, as packed arithmetic on two channels takes it; zeros behind the
-// last step.
-template <typename T, int NP>
-__device__ __forceinline__ void stage_few(float2 (&to)[kSteps][NP], const T *from, long long step, int rows, int N) {
-    for (int i = threadIdx.x; i < kSteps * NP; i += kThreads) {
-        const int t = i / NP, n = i % NP;
-        const float v = t < rows && n < N ? to_f32(from[t * step + n]) : 0.f;
-        to[t][n] = make_float2(v, v);
-    }
-}
 // Of the tile's channels; zeros where there are none.
 template <int CT>
 __device__ __forceinline__ void stage_channels(float (&to)[CT], const float *from, const Work &w) {
@@ -169,45 +165,44 @@ __device__ __forceinline__ uint32_t flags_of(const ScanArgs &a, int e, int t, in
     return a.done ? __ballot_sync(0xffffffffu, r < min(rows, kSteps) && t + r >= 0 && a.done[(long long)(t + r) * a.Be + e]) : 0u;
 }
 
-// Elements n0 .. n0 + W - 1 of a state of N in memory; zeros behind the last one.
+// Elements n0 .. n0 + W - 1 of a state of N in memory, by vectors of four or two where these fit; zeros behind the last one.
 template <int W>
 __device__ __forceinline__ void load_row(const float *p, int N, int n0, float (&h)[W]) {
-    const bool whole = N % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+    constexpr int V = W % 4 == 0 ? 4 : 2;
+    const bool whole = N % V == 0 && (reinterpret_cast<uintptr_t>(p) & (4 * V - 1)) == 0;
 #pragma unroll
-    for (int n = 0; n < W; n += 4) {
-        if (whole) {
+    for (int n = 0; n < W; n += V) {
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[n + i] = n0 + n + i < N ? p[n0 + n + i] : 0.f;
+        } else if constexpr (V == 4) {
             const float4 f = n0 + n < N ? *reinterpret_cast<const float4 *>(p + n0 + n) : make_float4(0.f, 0.f, 0.f, 0.f);
             h[n] = f.x, h[n + 1] = f.y, h[n + 2] = f.z, h[n + 3] = f.w;
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) h[n + i] = n0 + n + i < N ? p[n0 + n + i] : 0.f;
+            const float2 f = n0 + n < N ? *reinterpret_cast<const float2 *>(p + n0 + n) : make_float2(0.f, 0.f);
+            h[n] = f.x, h[n + 1] = f.y;
         }
     }
 }
 template <int W>
 __device__ __forceinline__ void store_row(float *p, int N, int n0, const float (&h)[W]) {
-    const bool whole = N % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+    constexpr int V = W % 4 == 0 ? 4 : 2;
+    const bool whole = N % V == 0 && (reinterpret_cast<uintptr_t>(p) & (4 * V - 1)) == 0;
 #pragma unroll
-    for (int n = 0; n < W; n += 4) {
-        if (whole) {
-            if (n0 + n < N) *reinterpret_cast<float4 *>(p + n0 + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
-        } else {
+    for (int n = 0; n < W; n += V) {
+        if (!whole) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < V; ++i)
                 if (n0 + n + i < N) p[n0 + n + i] = h[n + i];
+        } else if (n0 + n < N) {
+            if constexpr (V == 4) *reinterpret_cast<float4 *>(p + n0 + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
+            else *reinterpret_cast<float2 *>(p + n0 + n) = make_float2(h[n], h[n + 1]);
         }
     }
 }
 __device__ __forceinline__ void load_pairs(const float *p, pair32 (&v)[2]) {
     const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(p);
     v[0] = u.x, v[1] = u.y;
-}
-__device__ __forceinline__ void load_few(const float2 *p, pair32 (&v)[4]) {
-#pragma unroll
-    for (int n = 0; n < 4; n += 2) {
-        const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(p + n);
-        v[n] = u.x, v[n + 1] = u.y;
-    }
 }
 
 // Takes elements n0 .. of a channel's state, or gradient, through segment s: exp2(A sum of its step sizes) h + add, or add alone behind a flag.  from: what
@@ -240,7 +235,7 @@ enum Mode {
     OUTPUT,  // y and the state that is left
     ENDS,    // what each segment ends with
     BOTH,    // that, and the gradients it hands to the steps in front
-    MARKS    // the states in front of every fourth step
+    MARKS    // the states in front of every kSteps-th step
 };
 
 // CPT neighbouring channels of a row, as they lie in memory.
@@ -387,16 +382,16 @@ __global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) 
         B += kSteps * sb;
         C += kSteps * sc;
         if (rows > kSteps) few.fetch(B, C, sb, sc, rows - kSteps, a.N);
+        if constexpr (MODE == MARKS) {
+            float *to = a.mark + (((long long)(t / kSteps) * a.Be + w.e) * a.channels + c) * NP + n0;
+#pragma unroll
+            for (int j = 0; j < CPT; ++j)
+#pragma unroll
+                for (int i = 0; i < P; i += 2)
+                    if (on) *reinterpret_cast<ulonglong2 *>(to + j * NP + 2 * i) = make_ulonglong2(h[j][i], h[j][i + 1]);
+        }
 #pragma unroll 1
         for (int s = 0; s < kSteps && s < rows; s += 4) {
-            if constexpr (MODE == MARKS) {
-                float *to = a.mark + (((long long)((t + s) / 4) * a.Be + w.e) * a.channels + c) * NP + n0;
-#pragma unroll
-                for (int j = 0; j < CPT; ++j)
-#pragma unroll
-                    for (int i = 0; i < P; i += 2)
-                        if (on) *reinterpret_cast<ulonglong2 *>(to + j * NP + 2 * i) = make_ulonglong2(h[j][i], h[j][i + 1]);
-            }
             pair32 xs[4], ds[4], zs[4], gs[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -429,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) 
                     for (int m = 0; m < 2; ++m)
 #pragma unroll
                         for (int j = 0; j < CPT; ++j) {
-                            const pair32 f = exp2_pair(mul2(twice(j == 0 ? d.x : d.y), A[j][i + m]));
+                            const pair32 f = factors(twice(j == 0 ? d.x : d.y), A[j][i + m]);
                             h[j][i + m] = fma2(f, h[j][i + m], mul2(twice(j == 0 ? u.x : u.y), b[m]));
                             if constexpr (MODE == OUTPUT) out[j] = fma2(cc[m], h[j][i + m], out[j]);
                             if constexpr (WITH_DY) {
@@ -503,67 +498,71 @@ __global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) 
 // Four steps at a time, backwards: from the states in front of them forwards once more, which leaves the factors and exp(d A) h' of the
 // four steps in registers (and y and the sums of dC on the way), then backwards over these.  A block goes through as many envs, or
 // segments, as fall to it and keeps its shares of the parameters' gradients.
-// Four elements of the states of four channels, [e][channel][N] in memory; zeros where there are none.
-__device__ __forceinline__ void load_block(const float *from, const ScanArgs &a, int e, int c, int c1, int n0, float (&h)[4][4]) {
+// Two elements of the states of four channels, [e][channel][N] in memory; zeros where there are none.
+__device__ __forceinline__ void load_block(const float *from, const ScanArgs &a, int e, int c, int c1, int n0, float (&h)[4][2]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int n = 0; n < 4; ++n) h[j][n] = 0.f;
-        if (from && c + j < c1) load_row<4>(from + ((long long)e * a.channels + c + j) * a.N, a.N, n0, h[j]);
+        h[j][0] = h[j][1] = 0.f;
+        if (from && c + j < c1) load_row<2>(from + ((long long)e * a.channels + c + j) * a.N, a.N, n0, h[j]);
     }
 }
-__device__ __forceinline__ void store_block(float *to, const ScanArgs &a, int e, int c, int c1, int n0, const float (&h)[4][4]) {
+__device__ __forceinline__ void store_block(float *to, const ScanArgs &a, int e, int c, int c1, int n0, const float (&h)[4][2]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (c + j < c1) store_row<4>(to + ((long long)e * a.channels + c + j) * a.N, a.N, n0, h[j]);
+        if (c + j < c1) store_row<2>(to + ((long long)e * a.channels + c + j) * a.N, a.N, n0, h[j]);
 }
 // As pairs of neighbouring channels.
-__device__ __forceinline__ void pack(const float (&h)[4][4], pair32 (&p)[4][2]) {
+__device__ __forceinline__ void pack(const float (&h)[4][2], pair32 (&p)[2][2]) {
 #pragma unroll
-    for (int n = 0; n < 4; ++n) p[n][0] = pair_of(h[0][n], h[1][n]), p[n][1] = pair_of(h[2][n], h[3][n]);
+    for (int n = 0; n < 2; ++n) p[n][0] = pair_of(h[0][n], h[1][n]), p[n][1] = pair_of(h[2][n], h[3][n]);
 }
-__device__ __forceinline__ void unpack(const pair32 (&p)[4][2], float (&h)[4][4]) {
+__device__ __forceinline__ void unpack(const pair32 (&p)[2][2], float (&h)[4][2]) {
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    for (int n = 0; n < 2; ++n) {
         const float2 u = parts(p[n][0]), v = parts(p[n][1]);
         h[0][n] = u.x, h[1][n] = u.y, h[2][n] = v.x, h[3][n] = v.y;
     }
 }
 
-// A long sum as two numbers: what hi rounds away stays in lo (Knuth's error of a sum).
-__device__ __forceinline__ void add_to(float &hi, float &lo, float v) {
-    const float sum = __fadd_rn(hi, v), w = __fsub_rn(sum, hi);
-    lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(sum, w)), __fsub_rn(v, w));
-    hi = sum;
-}
-
 template <typename T, int NL, bool VEC>
 struct GradShared {
     static constexpr int CT = Shape<NL>::CT, NP = Shape<NL>::NP;
+    using R = Rows<T, CT, VEC>;
     float sd[kSteps][CT], su[kSteps][CT], sg[kSteps][CT], sy[kSteps][CT], sD[CT], sbias[CT];
-    float2 sB[kSteps][NP], sC[kSteps][NP];
+    float2 sB[kSteps][NP], sC[kSteps][NP];  // every element twice, as packed arithmetic on two channels takes it
     float few[kThreads / 32][kSteps][2 * NP];
-    float mark[4][4][kThreads * 4];
-    float dA[2][16][kThreads], kept[2][2][Rows<T, CT, VEC>::V][kThreads];  // [..][2]: hi and lo of the sums
+    // a thread's own: the states in front of the next tile; those in front of every fourth step of this one; its sums of the gradients of D and
+    // dt_bias; its elements of the next tile's rows of x, dt, dy, z
+    float2 mark[4][kThreads];
+    float4 inner[4][2][kThreads];
+    float kept[2][kThreads * R::V];
+    typename R::Raw next[4][R::PASSES][kThreads];
 };
 
-// Four numbers, or zeros.
-__device__ __forceinline__ void copy_async(float *to, const float *from, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+// BYTES of them, or zeros.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void *to, const void *from, bool there) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (BYTES == 2) {
+        if (there) *static_cast<uint16_t *>(to) = *static_cast<const uint16_t *>(from);
+    } else {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(at), "l"(from), "n"(BYTES), "r"(there ? BYTES : 0) : "memory");
+    }
 }
 
 template <typename T, int NL, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_kernel(ScanArgs a) {
     grid_wait();
-    constexpr int NPT = 4;
+    constexpr int NPT = 2;
     using S = Shape<NL>;
-    constexpr int CT = S::CT, NP = S::NP, GROUPS = S::GROUPS;
+    constexpr int CT = S::CT, NP = S::NP, GROUPS = S::GROUPS, FEW = kSteps * NP / kThreads;
     using R = Rows<T, CT, VEC>;
+    constexpr int BYTES = sizeof(typename R::Raw);
     extern __shared__ __align__(16) char smem[];
     GradShared<T, NL, VEC> &s = *reinterpret_cast<GradShared<T, NL, VEC> *>(smem);
     const int tile = blockIdx.x % a.tiles, slice = blockIdx.x / a.tiles;
     const int lane = threadIdx.x % 32, ln = lane % NL, warp = threadIdx.x / 32, n0 = ln * NPT, local = (warp * GROUPS + lane / NL) * 4;
-    Work w = work_of<CT>(a, tile, 0);
+    Work w = work_of<CT>(a, tile, slice);
     const int c = w.c0 + local, cols = w.c1 - w.c0;
     const long long sx = a.Be * a.ldx, st = a.Be * a.lddt, sb = a.Be * a.ldb, sc = a.Be * a.ldc, sz = a.Be * a.ldz, sy = a.Be * a.ldy;
     pair32 A[NPT][2], g[NPT][2], dA[NPT][2];
@@ -581,18 +580,50 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
     stage_channels(s.sD, a.D, w);
     stage_channels(s.sbias, a.bias, w);
 #pragma unroll
-    for (int v = 0; v < R::V; ++v)
+    for (int v = 0; v < R::V; ++v) s.kept[0][threadIdx.x * R::V + v] = s.kept[1][threadIdx.x * R::V + v] = 0.f;
+
+    // of the tile that comes next
+    T fb[FEW], fc[FEW];
+    const auto fetch = [&](const Work &w, int t) {
+        const int rows = min(w.t1 - t, kSteps);
+        const T *x = static_cast<const T *>(a.x) + w.e * a.ldx + w.c0 + t * sx, *dt = static_cast<const T *>(a.dt) + w.e * a.lddt + w.c0 + t * st;
+        const T *dy = static_cast<const T *>(a.dy) + w.e * a.ldy + w.c0 + t * sy, *z = a.z ? static_cast<const T *>(a.z) + w.e * a.ldz + w.c0 + t * sz : nullptr;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s.kept[k / 2][k % 2][v][threadIdx.x] = 0.f;
+        for (int i = 0; i < R::PASSES; ++i) {
+            const int r = R::row(i), l = R::col(i);
+            if (r >= rows || l >= cols) continue;
+            copy_async<BYTES>(&s.next[0][i][threadIdx.x], x + r * sx + l, true);
+            copy_async<BYTES>(&s.next[1][i][threadIdx.x], dt + r * st + l, true);
+            copy_async<BYTES>(&s.next[2][i][threadIdx.x], dy + r * sy + l, true);
+            if (z) copy_async<BYTES>(&s.next[3][i][threadIdx.x], z + r * sz + l, true);
+        }
+        const T *B = static_cast<const T *>(a.B) + w.e * a.ldb + (long long)w.group * a.N + t * sb;
+        const T *C = static_cast<const T *>(a.C) + w.e * a.ldc + (long long)w.group * a.N + t * sc;
 #pragma unroll
-    for (int n = 0; n < 16; ++n) s.dA[0][n][threadIdx.x] = s.dA[1][n][threadIdx.x] = 0.f;
+        for (int i = 0; i < FEW; ++i) {
+            const int r = threadIdx.x / NP + i * (kThreads / NP), n = threadIdx.x % NP;
+            const bool ok = r < rows && n < a.N;
+            fb[i] = ok ? B[r * sb + n] : from_f32<T>(0.f);
+            fc[i] = ok ? C[r * sc + n] : from_f32<T>(0.f);
+        }
+        // up to kSteps steps start from the state that comes in, whose rows need not be aligned
+        const float *mark = a.mark + (((long long)(t / kSteps) * a.Be + w.e) * a.channels + c) * NP + n0;
+        if (a.T > kSteps) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) copy_async<8>(&s.mark[j][threadIdx.x], c + j < w.c1 ? mark + j * NP : a.mark, c + j < w.c1);
+        } else {
+            float f[4][NPT];
+            load_block(a.state_in, a, w.e, c, w.c1, n0, f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s.mark[j][threadIdx.x] = make_float2(f[j][0], f[j][1]);
+        }
+    };
+    const auto last_tile = [&](const Work &w) { return w.t0 + (w.t1 - 1 - w.t0) / kSteps * kSteps; };
+    fetch(w, last_tile(w));
 
     const long long items = (long long)a.Be * a.nseg;
     for (long long item = slice; item < items; item += a.parts) {
         w = work_of<CT>(a, tile, item);
-        const T *x = static_cast<const T *>(a.x) + w.e * a.ldx + w.c0, *dt = static_cast<const T *>(a.dt) + w.e * a.lddt + w.c0;
-        const T *B = static_cast<const T *>(a.B) + w.e * a.ldb + (long long)w.group * a.N, *C = static_cast<const T *>(a.C) + w.e * a.ldc + (long long)w.group * a.N;
-        const T *z = a.z ? static_cast<const T *>(a.z) + w.e * a.ldz + w.c0 : nullptr, *dy = static_cast<const T *>(a.dy) + w.e * a.ldy + w.c0;
         {
             float f[4][NPT], Af[4][NPT];
             if (a.nseg == 1) {
@@ -601,136 +632,158 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                 unpack(A, Af);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) f[j][n] = 0.f;
-                    if (c + j < w.c1) end_of<4>(a, NP, w, c + j, n0, Af[j], f[j]);
+                    f[j][0] = f[j][1] = 0.f;
+                    if (c + j < w.c1) end_of<2>(a, NP, w, c + j, n0, Af[j], f[j]);
                 }
             }
             pack(f, g);
         }
-        for (int t = w.t0 + (w.t1 - 1 - w.t0) / kSteps * kSteps; t >= w.t0; t -= kSteps) {
-            const int rows = w.t1 - t;
+        for (int t = last_tile(w); t >= w.t0; t -= kSteps) {
+            const int rows = min(w.t1 - t, kSteps);
             const uint32_t flag = flags_of(a, w.e, t, rows);
             __syncthreads();  // the tile behind is done with
+            asm volatile("cp.async.wait_all;" ::: "memory");  // a thread reads what it copied itself
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                if (4 * m >= rows) break;
-                const float *from = a.mark + (((long long)(t / 4 + m) * a.Be + w.e) * a.channels + c) * NP + n0;
+            for (int i = 0; i < FEW; ++i) {
+                const int r = threadIdx.x / NP + i * (kThreads / NP), n = threadIdx.x % NP;
+                const float b = to_f32(fb[i]), f = to_f32(fc[i]);
+                s.sB[r][n] = make_float2(b, b);
+                s.sC[r][n] = make_float2(f, f);
+            }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) copy_async(&s.mark[m][j][threadIdx.x * 4], c + j < w.c1 ? from + j * NP : a.mark, c + j < w.c1);
+            for (int i = 0; i < R::PASSES; ++i) {
+                const int r = R::row(i), l = R::col(i);
+                pair32 d[R::PAIRS] = {}, u[R::PAIRS] = {}, v[R::PAIRS] = {};
+                if (r < rows && l < cols) {
+                    pair32 b[R::PAIRS];
+                    R::get(s.next[0][i][threadIdx.x], u);
+                    R::get(s.next[1][i][threadIdx.x], d);
+                    R::get(s.next[2][i][threadIdx.x], v);
+                    R::get_shared(&s.sbias[l], b);
+#pragma unroll
+                    for (int k = 0; k < R::PAIRS; ++k) {
+                        d[k] = add2(d[k], b[k]);
+                        if (a.softplus) d[k] = R::softplus(d[k]);
+                        u[k] = mul2(u[k], d[k]);
+                    }
+                    if (a.z) {
+                        pair32 f[R::PAIRS];
+                        R::get(s.next[3][i][threadIdx.x], f);
+#pragma unroll
+                        for (int k = 0; k < R::PAIRS; ++k) v[k] = mul2(v[k], mul2(f[k], R::sigmoid(f[k])));
+                    }
+                }
+                if (r >= kSteps) break;
+                R::put_shared(&s.sd[r][l], d);
+                R::put_shared(&s.su[r][l], u);
+                R::put_shared(&s.sg[r][l], v);
+            }
+            float start[4][NPT];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = s.mark[j][threadIdx.x];
+                start[j][0] = f.x, start[j][1] = f.y;
             }
             {
-                R rx, rt, rg, rz;
-                rx.fetch(x + t * sx, sx, rows, cols);
-                rt.fetch(dt + t * st, st, rows, cols);
-                rg.fetch(dy + t * sy, sy, rows, cols);
-                if (z) rz.fetch(z + t * sz, sz, rows, cols);
-                stage_few<T, NP>(s.sB, B + t * sb, sb, rows, a.N);
-                stage_few<T, NP>(s.sC, C + t * sc, sc, rows, a.N);
-#pragma unroll
-                for (int i = 0; i < R::PASSES; ++i) {
-                    const int r = R::row(i), l = R::col(i);
-                    if (r >= kSteps) break;
-                    float d[R::V], u[R::V], v[R::V];
-                    if (r < rows && l < cols) {
-                        rt.get(i, d);
-                        rx.get(i, u);
-                        rg.get(i, v);
-                        float b[R::V], f[R::V];
-                        get_floats(&s.sbias[l], b);
-                        if (z) rz.get(i, f);
-#pragma unroll
-                        for (int k = 0; k < R::V; k += 2) {
-                            constexpr int TWO = R::V > 1;
-                            pair32 step = add2(pair_of(d[k], d[k + TWO]), pair_of(b[k], b[k + TWO]));
-                            if (a.softplus) step = softplus_pair(step);
-                            const float2 p = parts(step), q = parts(mul2(pair_of(u[k], u[k + TWO]), step));
-                            d[k] = p.x, d[k + TWO] = p.y, u[k] = q.x, u[k + TWO] = q.y;
-                            if (z) {
-                                const pair32 zz = pair_of(f[k], f[k + TWO]);
-                                const float2 g = parts(mul2(pair_of(v[k], v[k + TWO]), mul2(zz, sigmoid_pair(zz))));
-                                v[k] = g.x, v[k + TWO] = g.y;
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < R::V; ++k) d[k] = u[k] = v[k] = 0.f;
-                    }
-                    put_floats(&s.sd[r][l], d);
-                    put_floats(&s.su[r][l], u);
-                    put_floats(&s.sg[r][l], v);
+                // on its way while this tile is worked on
+                const bool more = t > w.t0;
+                if (more || item + a.parts < items) {
+                    const Work v = more ? w : work_of<CT>(a, tile, item + a.parts);
+                    fetch(v, more ? t - kSteps : last_tile(v));
                 }
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");  // a thread reads what it copied itself
             __syncthreads();
+            const int top = (rows - 1) / 4;
+            pair32 h[NPT][2];
+            pack(start, h);
+            // forwards to the states in front of every fourth step
 #pragma unroll 1
-            for (int m = (min(rows, kSteps) - 1) / 4; m >= 0; --m) {
-                const int r0 = 4 * m;
-                pair32 f[4][NPT][2], q[4][NPT][2];  // of each step the factors, and these times the state in front
-                {
-                    pair32 h[NPT][2];
-                    float start[4][NPT];
+            for (int m = 0; m < top; ++m) {
+                s.inner[m][0][threadIdx.x] = make_float4(parts(h[0][0]).x, parts(h[0][0]).y, parts(h[0][1]).x, parts(h[0][1]).y);
+                s.inner[m][1][threadIdx.x] = make_float4(parts(h[1][0]).x, parts(h[1][0]).y, parts(h[1][1]).x, parts(h[1][1]).y);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) get_floats(&s.mark[m][j][threadIdx.x * 4], start[j]);
-                    pack(start, h);
+                for (int k = 0; k < 4; ++k) {
+                    const int r = 4 * m + k;
+                    pair32 d[2], u[2], b[2];
+                    load_pairs(&s.sd[r][local], d);
+                    load_pairs(&s.su[r][local], u);
+                    load_pairs(&s.sB[r][n0].x, b);
 #pragma unroll
-                    for (int k = 0; k < 4; k += 2) {
-                        float ys[8], cs[8];
+                    for (int n = 0; n < NPT; ++n)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int r = r0 + k + i;
-                            pair32 d[2], u[2], v[2], acc[2] = {0, 0};
-                            pair32 b[NPT], cc[NPT];
-                            load_pairs(&s.sd[r][local], d);
-                            load_pairs(&s.su[r][local], u);
-                            load_pairs(&s.sg[r][local], v);
-                            load_few(&s.sB[r][n0], b);
-                            load_few(&s.sC[r][n0], cc);
-                            if (k + i > 0 && flag >> (r - 1) & 1) {
+                        for (int p = 0; p < 2; ++p) h[n][p] = fma2(factors(d[p], A[n][p]), h[n][p], mul2(u[p], b[n]));
+                    if (flag >> r & 1) {
 #pragma unroll
-                                for (int n = 0; n < NPT; ++n) h[n][0] = h[n][1] = 0;
-                            }
-#pragma unroll
-                            for (int n = 0; n < NPT; ++n) {
-                                pair32 sum = 0;
-#pragma unroll
-                                for (int p = 0; p < 2; ++p) {
-                                    const pair32 e = exp2_pair(mul2(d[p], A[n][p])), qq = mul2(e, h[n][p]);
-                                    f[k + i][n][p] = e;
-                                    q[k + i][n][p] = qq;
-                                    h[n][p] = fma2(u[p], b[n], qq);
-                                    acc[p] = fma2(cc[n], h[n][p], acc[p]);
-                                    sum = fma2(v[p], h[n][p], sum);
-                                }
-                                const float2 e = parts(sum);
-                                cs[4 * i + n] = e.x + e.y;
-                            }
-                            const float2 e = parts(acc[0]), o = parts(acc[1]);
-                            ys[4 * i] = e.x, ys[4 * i + 1] = e.y, ys[4 * i + 2] = o.x, ys[4 * i + 3] = o.y;
-                        }
-                        spread_sum<8, NL, 1>(ys, lane);
-                        spread_sum<8, GROUPS, NL>(cs, lane);
-                        int at = spread_first<8, NL>(ln);
-#pragma unroll
-                        for (int i = 0; i < (NL >= 8 ? 1 : 8 / NL); ++i) s.sy[r0 + k + at / 4][local + at % 4 + i] = ys[i];
-                        at = spread_first<8, GROUPS>(lane / NL);
-#pragma unroll
-                        for (int i = 0; i < 8 / GROUPS; ++i) s.few[warp][r0 + k + at / 4][NP + n0 + at % 4 + i] = cs[i];
+                        for (int n = 0; n < NPT; ++n) h[n][0] = h[n][1] = 0;
                     }
                 }
+            }
+#pragma unroll 1
+            for (int m = top; m >= 0; --m) {
+                const int r0 = 4 * m;
+                if (m < top) {
 #pragma unroll
-                for (int k = 2; k >= 0; k -= 2) {
-                    float bs[8];
+                    for (int n = 0; n < NPT; ++n) {
+                        const float4 f = s.inner[m][n][threadIdx.x];
+                        h[n][0] = pair_of(f.x, f.y), h[n][1] = pair_of(f.z, f.w);
+                    }
+                }
+                pair32 q[4][NPT][2];  // of each step exp(d A) times the state in front
 #pragma unroll
-                    for (int i = 1; i >= 0; --i) {
+                for (int k = 0; k < 4; k += 2) {
+                    float ys[8], cs[4];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
                         const int r = r0 + k + i;
-                        pair32 d[2], u[2], v[2], s1[2] = {0, 0}, s2[2] = {0, 0};
-                        pair32 b[NPT], cc[NPT];
+                        pair32 d[2], u[2], v[2], acc[2] = {0, 0}, b[2], cc[2];
                         load_pairs(&s.sd[r][local], d);
                         load_pairs(&s.su[r][local], u);
                         load_pairs(&s.sg[r][local], v);
-                        load_few(&s.sB[r][n0], b);
-                        load_few(&s.sC[r][n0], cc);
+                        load_pairs(&s.sB[r][n0].x, b);
+                        load_pairs(&s.sC[r][n0].x, cc);
+                        if (k + i > 0 && flag >> (r - 1) & 1) {
+#pragma unroll
+                            for (int n = 0; n < NPT; ++n) h[n][0] = h[n][1] = 0;
+                        }
+#pragma unroll
+                        for (int n = 0; n < NPT; ++n) {
+                            pair32 sum = 0;
+#pragma unroll
+                            for (int p = 0; p < 2; ++p) {
+                                const pair32 qq = mul2(factors(d[p], A[n][p]), h[n][p]);
+                                q[k + i][n][p] = qq;
+                                h[n][p] = fma2(u[p], b[n], qq);
+                                acc[p] = fma2(cc[n], h[n][p], acc[p]);
+                                sum = fma2(v[p], h[n][p], sum);
+                            }
+                            const float2 e = parts(sum);
+                            cs[2 * i + n] = e.x + e.y;
+                        }
+                        const float2 e = parts(acc[0]), o = parts(acc[1]);
+                        ys[4 * i] = e.x, ys[4 * i + 1] = e.y, ys[4 * i + 2] = o.x, ys[4 * i + 3] = o.y;
+                    }
+                    if (a.z) {
+                        spread_sum<8, NL, 1>(ys, lane);
+                        const int at = spread_first<8, NL>(ln);
+                        s.sy[r0 + k + at / 4][local + at % 4] = ys[0];
+                    }
+                    spread_sum<4, GROUPS, NL>(cs, lane);
+                    const int at = spread_first<4, GROUPS>(lane / NL);
+#pragma unroll
+                    for (int i = 0; i < 4 / GROUPS; ++i) s.few[warp][r0 + k + (at + i) / 2][NP + n0 + (at + i) % 2] = cs[i];
+                }
+#pragma unroll
+                for (int k = 2; k >= 0; k -= 2) {
+                    float bs[4];
+#pragma unroll
+                    for (int i = 1; i >= 0; --i) {
+                        const int r = r0 + k + i;
+                        pair32 d[2], u[2], v[2], s1[2] = {0, 0}, s2[2] = {0, 0}, b[2], cc[2];
+                        load_pairs(&s.sd[r][local], d);
+                        load_pairs(&s.su[r][local], u);
+                        load_pairs(&s.sg[r][local], v);
+                        load_pairs(&s.sB[r][n0].x, b);
+                        load_pairs(&s.sC[r][n0].x, cc);
                         if (flag >> r & 1) {
 #pragma unroll
                             for (int n = 0; n < NPT; ++n) g[n][0] = g[n][1] = 0;
@@ -746,10 +799,10 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                                 const pair32 qq = mul2(g[n][p], q[k + i][n][p]);
                                 s2[p] = fma2(qq, A[n][p], s2[p]);
                                 dA[n][p] = fma2(qq, d[p], dA[n][p]);
-                                g[n][p] = mul2(g[n][p], f[k + i][n][p]);
+                                g[n][p] = mul2(g[n][p], factors(d[p], A[n][p]));
                             }
                             const float2 e = parts(sum);
-                            bs[4 * i + n] = e.x + e.y;
+                            bs[2 * i + n] = e.x + e.y;
                         }
                         float both[8];
                         const float2 e = parts(s1[0]), o = parts(s1[1]), e2 = parts(s2[0]), o2 = parts(s2[1]);
@@ -758,14 +811,12 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                         // every lane of the channels has read this step's row: the sums take its place
                         spread_sum<8, NL, 1>(both, lane);
                         const int at = spread_first<8, NL>(ln);
-                        float *to = (at < 4 ? &s.su[r][local] : &s.sg[r][local - 4]) + at;
-#pragma unroll
-                        for (int j = 0; j < (NL >= 8 ? 1 : 8 / NL); ++j) to[j] = both[j];
+                        *((at < 4 ? &s.su[r][local] : &s.sg[r][local - 4]) + at) = both[0];
                     }
-                    spread_sum<8, GROUPS, NL>(bs, lane);
-                    const int at = spread_first<8, GROUPS>(lane / NL);
+                    spread_sum<4, GROUPS, NL>(bs, lane);
+                    const int at = spread_first<4, GROUPS>(lane / NL);
 #pragma unroll
-                    for (int i = 0; i < 8 / GROUPS; ++i) s.few[warp][r0 + k + at / 4][n0 + at % 4 + i] = bs[i];
+                    for (int i = 0; i < 4 / GROUPS; ++i) s.few[warp][r0 + k + (at + i) / 2][n0 + (at + i) % 2] = bs[i];
                 }
             }
             __syncthreads();
@@ -779,65 +830,60 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
                 a.few[(((long long)(tile - w.group * a.group_tiles) * a.T * a.Be + row) * a.groups + w.group) * (2 * NP) + n] = sum;
             }
             {
+                const long long ax = w.e * a.ldx + w.c0 + t * sx, at = w.e * a.lddt + w.c0 + t * st, az = w.e * a.ldz + w.c0 + t * sz, ay = w.e * a.ldy + w.c0 + t * sy;
                 R rx, rt, rg, rz;
-                rx.fetch(x + t * sx, sx, rows, cols);
-                rt.fetch(dt + t * st, st, rows, cols);
-                rg.fetch(dy + t * sy, sy, rows, cols);
-                if (z) rz.fetch(z + t * sz, sz, rows, cols);
-                T *dx = static_cast<T *>(a.dx) + w.e * a.ldx + w.c0, *ddt = static_cast<T *>(a.ddt) + w.e * a.lddt + w.c0;
-                T *dz = z ? static_cast<T *>(a.dz) + w.e * a.ldz + w.c0 : nullptr;
-                float sumD[R::V] = {}, sumb[R::V] = {};
+                rx.fetch(static_cast<const T *>(a.x) + ax, sx, rows, cols);
+                rt.fetch(static_cast<const T *>(a.dt) + at, st, rows, cols);
+                rg.fetch(static_cast<const T *>(a.dy) + ay, sy, rows, cols);
+                if (a.z) rz.fetch(static_cast<const T *>(a.z) + az, sz, rows, cols);
+                T *dx = static_cast<T *>(a.dx) + ax, *ddt = static_cast<T *>(a.ddt) + at, *dz = a.z ? static_cast<T *>(a.dz) + az : nullptr;
+                pair32 D[R::PAIRS], bias[R::PAIRS], sumD[R::PAIRS], sumb[R::PAIRS];
+                float *keptD = &s.kept[0][threadIdx.x * R::V], *keptb = &s.kept[1][threadIdx.x * R::V];
+                R::get_shared(&s.sD[R::col(0)], D);  // every pass has the same columns
+                R::get_shared(&s.sbias[R::col(0)], bias);
+                R::get_shared(keptD, sumD);
+                R::get_shared(keptb, sumb);
 #pragma unroll
                 for (int i = 0; i < R::PASSES; ++i) {
                     const int r = R::row(i), l = R::col(i);
-                    if (r >= kSteps || r >= rows || l >= cols) continue;
-                    float d[R::V], s1[R::V], s2[R::V], xv[R::V], tv[R::V], gv[R::V], D[R::V], bias[R::V], o[R::V];
-                    get_floats(&s.sD[l], D);
-                    get_floats(&s.sbias[l], bias);
-                    get_floats(&s.sd[r][l], d);
-                    get_floats(&s.su[r][l], s1);
-                    get_floats(&s.sg[r][l], s2);
-                    rx.get(i, xv);
-                    rt.get(i, tv);
-                    rg.get(i, gv);
-                    if (z) {
-                        float zv[R::V], yv[R::V];
-                        rz.get(i, zv);
-                        get_floats(&s.sy[r][l], yv);
+                    if (r >= rows || l >= cols) continue;
+                    pair32 d[R::PAIRS], s1[R::PAIRS], s2[R::PAIRS], xv[R::PAIRS], tv[R::PAIRS], gv[R::PAIRS], o[R::PAIRS];
+                    R::get_shared(&s.sd[r][l], d);
+                    R::get_shared(&s.su[r][l], s1);
+                    R::get_shared(&s.sg[r][l], s2);
+                    R::get(rx.raw[i], xv);
+                    R::get(rt.raw[i], tv);
+                    R::get(rg.raw[i], gv);
+                    if (a.z) {
+                        pair32 zv[R::PAIRS], yv[R::PAIRS];
+                        R::get(rz.raw[i], zv);
+                        R::get_shared(&s.sy[r][l], yv);
 #pragma unroll
-                        for (int k = 0; k < R::V; ++k) {
-                            const float p = sigmoid_fast(zv[k]), all = a.D ? fmaf(D[k], xv[k], yv[k]) : yv[k];
-                            o[k] = gv[k] * all * (p * fmaf(zv[k], 1.f - p, 1.f));
-                            gv[k] *= zv[k] * p;
+                        for (int k = 0; k < R::PAIRS; ++k) {
+                            const pair32 p = R::sigmoid(zv[k]), all = a.D ? fma2(D[k], xv[k], yv[k]) : yv[k], one = twice(1.f);
+                            o[k] = mul2(mul2(gv[k], all), mul2(p, fma2(zv[k], fma2(p, twice(-1.f), one), one)));
+                            gv[k] = mul2(gv[k], mul2(zv[k], p));
                         }
-                        R::put(dz + (t + r) * sz + l, o);
+                        R::put(dz + r * sz + l, o);
                     }
 #pragma unroll
-                    for (int k = 0; k < R::V; ++k) {
-                        o[k] = a.D ? fmaf(d[k], s1[k], D[k] * gv[k]) : d[k] * s1[k];
-                        sumD[k] = fmaf(gv[k], xv[k], sumD[k]);
+                    for (int k = 0; k < R::PAIRS; ++k) {
+                        o[k] = mul2(d[k], s1[k]);
+                        if (a.D) o[k] = fma2(D[k], gv[k], o[k]);
+                        sumD[k] = fma2(gv[k], xv[k], sumD[k]);
                     }
-                    R::put(dx + (t + r) * sx + l, o);
+                    R::put(dx + r * sx + l, o);
 #pragma unroll
-                    for (int k = 0; k < R::V; ++k) {
-                        o[k] = fmaf(xv[k], s1[k], kLn2 * s2[k]);
-                        if (a.softplus) o[k] *= sigmoid_fast(tv[k] + bias[k]);
-                        sumb[k] += o[k];
+                    for (int k = 0; k < R::PAIRS; ++k) {
+                        o[k] = fma2(xv[k], s1[k], mul2(twice(kLn2), s2[k]));
+                        if (a.softplus) o[k] = mul2(o[k], R::sigmoid(add2(tv[k], bias[k])));
+                        sumb[k] = add2(sumb[k], o[k]);
                     }
-                    R::put(ddt + (t + r) * st + l, o);
+                    R::put(ddt + r * st + l, o);
                 }
-#pragma unroll
-                for (int k = 0; k < R::V; ++k) {
-                    add_to(s.kept[0][0][k][threadIdx.x], s.kept[0][1][k][threadIdx.x], sumD[k]);
-                    add_to(s.kept[1][0][k][threadIdx.x], s.kept[1][1][k][threadIdx.x], sumb[k]);
-                }
+                R::put_shared(keptD, sumD);
+                R::put_shared(keptb, sumb);
             }
-            float f[4][NPT];
-            unpack(dA, f);
-#pragma unroll
-            for (int n = 0; n < 16; ++n) add_to(s.dA[0][n][threadIdx.x], s.dA[1][n][threadIdx.x], f[n / 4][n % 4]);
-#pragma unroll
-            for (int n = 0; n < NPT; ++n) dA[n][0] = dA[n][1] = 0;
         }
         if (a.dstate_in && w.t0 == 0) {
             float f[4][NPT];
@@ -849,8 +895,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
     float *part = a.part + (size_t)slice * a.channels * (a.N + 2);
     {
         float f[4][NPT];
-#pragma unroll
-        for (int n = 0; n < 16; ++n) f[n / 4][n % 4] = s.dA[0][n][threadIdx.x] + s.dA[1][n][threadIdx.x];
+        unpack(dA, f);
         store_block(part, a, 0, c, w.c1, n0, f);
     }
     __syncthreads();
@@ -858,10 +903,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_bwd_kernel(ScanArgs a) {
         const int k = i / CT, l = i % CT;
         if (l >= cols) continue;
         float sum = 0.f;
-        for (int r = 0; r < kThreads / R::COLS; ++r) {
-            const int i = r * R::COLS + l / R::V;
-            sum += s.kept[k][0][l % R::V][i] + s.kept[k][1][l % R::V][i];
-        }
+        for (int r = 0; r < kThreads / R::COLS; ++r) sum += s.kept[k][(r * R::COLS + l / R::V) * R::V + l % R::V];
         part[(size_t)a.channels * (a.N + k) + w.c0 + l] = sum;
     }
 }
@@ -971,11 +1013,13 @@ Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     p.NP = 16 * p.NL;
     const auto up = [](size_t n) { return (n + 7) & ~(size_t)7; };  // whole 32 bytes
     const int per = d->channels / d->groups;
-    p.group_tiles = ppo_cdiv(per, 128 / p.NL);
+    p.group_tiles = ppo_cdiv(per, 64 / p.NL);
     p.tiles = p.group_tiles * d->groups;
-    // segments: as many as give the GPU the warps that it can hold at a time, none shorter than 64 steps
-    const long long warps = bwd ? 4ll * d->Be * p.tiles : (long long)d->Be * d->groups * ppo_cdiv(per, 64 / p.NL), want = (bwd ? 8 : 16) * 148;
-    long long n = warps < want ? want / warps : 1;
+    // segments, none shorter than 64 steps: forwards as many as fill three blocks an SM; backwards, where three passes go over them, as many as
+    // deal three to each slice of blocks
+    const int slices = p.tiles < 4 * 148 ? 4 * 148 / p.tiles : 1;  // four blocks an SM
+    const long long blocks = (long long)d->Be * d->groups * ppo_cdiv(per, 256 / p.NL);
+    long long n = bwd ? (d->Be < slices ? 3ll * slices / d->Be : 1) : (blocks < 3 * 148 ? 3 * 148 / blocks : 1);
     const int most = ppo_cdiv(d->T, 64);
     if (n > most) n = most;
     p.len = ppo_cdiv(ppo_cdiv(d->T, n), kSteps) * kSteps;
@@ -986,9 +1030,9 @@ Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
         p.sums = up((size_t)p.nseg * d->Be * (d->channels + 1));
     }
     if (bwd) {
-        p.mark = ppo_cdiv(d->T, 4) * held;
+        p.mark = d->T > kSteps ? ppo_cdiv(d->T, kSteps) * held : 0;
         p.few = (size_t)d->T * d->Be * p.tiles * 2 * p.NP;
-        const long long items = (long long)d->Be * p.nseg, slices = p.tiles < 2 * 148 ? 2 * 148 / p.tiles : 1;  // one round of two blocks an SM
+        const long long items = (long long)d->Be * p.nseg;
         p.parts = (int)(items < slices ? items : slices);
         p.part = up((size_t)p.parts * d->channels * (d->N + 2));
     }
@@ -1130,13 +1174,13 @@ extern "C" int ppo_selective_scan_bwd(const ppo_selective_scan_desc *d, const vo
     a.sum = a.few + p.few + p.part;
     a.cut = reinterpret_cast<int *>(a.sum + (size_t)p.nseg * d->Be * d->channels);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool two = vectors(d, 2, {x, dt}), vec = vectors(d, 16 / (int)elem_bytes(d->dtype), {x, dt, z, dy, dx, ddt, dz});
+    const bool two = vectors(d, 2, {x, dt}), vec = vectors(d, 4, {x, dt, z, dy, dx, ddt, dz});
     PPO_TRY(with_lanes(d, p, [&](auto t, auto nl) -> int {
         using T = decltype(t);
         constexpr int NL = decltype(nl)::value;
         if (p.nseg > 1) PPO_TRY((pass_of<T, NL, 1, BOTH>(a, p.nseg, st)));
-        PPO_TRY((pass<T, NL, MARKS>(a, two, p.nseg, st)));
-        PPO_TRY((vec ? back_launch<T, 4 * NL, true>(a, st) : back_launch<T, 4 * NL, false>(a, st)));
+        if (d->T > kSteps) PPO_TRY((pass<T, NL, MARKS>(a, two, p.nseg, st)));
+        PPO_TRY((vec ? back_launch<T, 8 * NL, true>(a, st) : back_launch<T, 8 * NL, false>(a, st)));
         const long long few = (long long)d->T * d->Be * d->groups * 2 * p.NP;
         return ppo_launch(scan_few_kernel<T, 16 * NL>, dim3((unsigned)((few + 255) / 256)), dim3(256), 0, st, a);
     }));
