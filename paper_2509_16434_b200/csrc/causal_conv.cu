@@ -19,7 +19,7 @@ struct ConvArgs {
     const float *weight, *bias;
     const uint8_t *done;
     float *part;  // shares of the gradients of weight and bias, [parts][C * width + C]
-    long long ldx, ldy;
+    long long ldx, ldy, sx, sy;  // from row to row, and from step to step
     int T, Be, C, act, run, tiles;
 };
 
@@ -167,61 +167,66 @@ __device__ __forceinline__ void params(const ConvArgs &a, int c, pair32 (&w)[W][
 template <typename T, int W, int V>
 __global__ void __launch_bounds__(kThreads) conv_fwd_kernel(ConvArgs a) {
     grid_wait();
-    constexpr int P = Raw<T, V>::PAIRS, AHEAD = 3;  // batches of 4 rows on their way
-    __shared__ typename Raw<T, V>::Word rows[4 * (AHEAD + 1)][kThreads];
-    const Ring<T, V, 4 * (AHEAD + 1)> ring = {rows};
+    // batches of BATCH rows, AHEAD of them on their way; a multiple of W, so that which input lies how far back is known when this is compiled
+    constexpr int P = Raw<T, V>::PAIRS, BATCH = W == 2 ? 4 : W, AHEAD = W <= 6 ? 3 : 2, S = BATCH * (AHEAD + 1);
+    __shared__ typename Raw<T, V>::Word rows[S][kThreads];
+    const Ring<T, V, S> ring = {rows};
     const int cols = a.C / V;
     const long long id = (long long)blockIdx.x * kThreads + threadIdx.x, item = id / cols;
     const int c = (int)(id - item * cols) * V, tile = (int)(item / a.Be), e = (int)(item - (long long)tile * a.Be);
     if (tile >= a.tiles) return;
     const T *x = static_cast<const T *>(a.x) + e * a.ldx + c, *state = nullptr;
-    T *y = static_cast<T *>(a.y) + e * a.ldy + c;
     const uint8_t *done = a.done ? a.done + e : nullptr;
-    const long long sx = (long long)a.Be * a.ldx, sy = (long long)a.Be * a.ldy;
+    const long long &sx = a.sx, &sy = a.sy;
     if (a.state_in) state = static_cast<const T *>(a.state_in) + (long long)e * (W - 1) * a.C + c;
     const int t0 = tile * a.run, t1 = min(a.T, t0 + a.run);
     const T *ahead = x + t0 * sx;
-    T *out = y + t0 * sy;
-    int fetched = t0;
+    T *out = static_cast<T *>(a.y) + e * a.ldy + c + t0 * sy;
+    int left = t1 - t0, to = 0;  // rows that are not fetched yet, and where in the ring the next batch goes
     const auto fetch = [&] {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (fetched + j < t1) ring.copy((fetched - t0) % (4 * (AHEAD + 1)) + j, ahead + j * sx);
+        for (int j = 0; j < BATCH; ++j)
+            if (j < left) ring.copy(to + j, ahead + j * sx);
         batch_end();
-        fetched += 4;
-        ahead += 4 * sx;
+        left -= BATCH;
+        ahead += BATCH * sx;
+        to = to + BATCH == S ? 0 : to + BATCH;
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) fetch();
-    pair32 w[W][P], b[P], h[W - 1][P];
+    pair32 w[W][P], b[P], h[W][P];  // h[t % W]: the input of step t0 + t
     params<W, V>(a, c, w, b);
-    history<T, W, V>(a, x, state, e, t0, h);
-    for (int t = t0; t < t1; t += 4) {
-        fetch();
-        bool flag[4];
+    {
+        pair32 f[W - 1][P];
+        history<T, W, V>(a, x, state, e, t0, f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) flag[j] = done && t + j < t1 && done[(long long)(t + j) * a.Be];
+        for (int i = 0; i < W - 1; ++i)
+#pragma unroll
+            for (int p = 0; p < P; ++p) h[i + 1][p] = f[i][p];
+    }
+    int from = 0;
+    for (int t = t0; t < t1; t += BATCH) {
+        fetch();
+        bool flag[BATCH];
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) flag[j] = done && t + j < t1 && done[(long long)(t + j) * a.Be];
         batch_wait<AHEAD>();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < BATCH; ++j) {
             if (t + j >= t1) break;
             Raw<T, V> r;
-            pair32 in[P], o[P];
-            ring.get((t - t0) % (4 * (AHEAD + 1)) + j, r);
-            r.get(in);
+            pair32 o[P];
+            ring.get(from + j, r);
+            r.get(h[j % W]);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                pair32 s = b[p];
+                o[p] = b[p];
 #pragma unroll
-                for (int i = 0; i < W - 1; ++i) s = fma2(w[i][p], h[i][p], s);
-                o[p] = fma2(w[W - 1][p], in[p], s);
-#pragma unroll
-                for (int i = 0; i < W - 2; ++i) h[i][p] = h[i + 1][p];
-                h[W - 2][p] = in[p];
+                for (int i = 0; i < W; ++i) o[p] = fma2(w[i][p], h[(j + 1 + i) % W][p], o[p]);
             }
             if (flag[j]) {
 #pragma unroll
-                for (int i = 0; i < W - 1; ++i)
+                for (int i = 0; i < W; ++i)
 #pragma unroll
                     for (int p = 0; p < P; ++p) h[i][p] = 0;
             }
@@ -230,16 +235,18 @@ __global__ void __launch_bounds__(kThreads) conv_fwd_kernel(ConvArgs a) {
             r.store(out);
             out += sy;
         }
+        from = from + BATCH == S ? 0 : from + BATCH;
     }
     // the first run writes the state that is left: it alone reads the one that came in, which may be the same
     if (tile == 0 && a.state_out) {
-        history<T, W, V>(a, x, state, e, a.T, h);
-        T *left = static_cast<T *>(a.state_out) + (long long)e * (W - 1) * a.C + c;
+        pair32 f[W - 1][P];
+        history<T, W, V>(a, x, state, e, a.T, f);
+        T *to = static_cast<T *>(a.state_out) + (long long)e * (W - 1) * a.C + c;
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) {
             Raw<T, V> r;
-            r.set(h[i]);
-            r.store(left + (long long)i * a.C);
+            r.set(f[i]);
+            r.store(to + (long long)i * a.C);
         }
     }
 }
@@ -294,130 +301,143 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs a, int env
 // (p, l): l columns of V channels side by side, p runs; a thread takes every so many of them and keeps its shares of the gradients of weight
 // and bias.
 template <typename T, int W, int V>
-__global__ void __launch_bounds__(kThreads) conv_bwd_kernel(ConvArgs a, int lanes) {
+__global__ void __launch_bounds__(kThreads, W <= 4 ? 4 : 2) conv_bwd_kernel(ConvArgs a, int lanes) {
     grid_wait();
-    constexpr int P = Raw<T, V>::PAIRS, AHEAD = 3, S = 2 * (AHEAD + 1);  // batches of 2 rows on their way
+    constexpr int P = Raw<T, V>::PAIRS, BATCH = W == 2 ? 4 : W, AHEAD = W <= 4 ? 2 : 1, S = BATCH * (AHEAD + 1), ALL = (1 << W) - 1;
     __shared__ typename Raw<T, V>::Word rx[S][kThreads], rg[S][kThreads];
     __shared__ float sum[kThreads];
     const Ring<T, V, S> xs = {rx}, gs = {rg};
     const int l = threadIdx.x % lanes, p0 = threadIdx.x / lanes, rows = kThreads / lanes, c = (blockIdx.x * lanes + l) * V;
     const bool on = c < a.C;
-    const long long sx = (long long)a.Be * a.ldx, sy = (long long)a.Be * a.ldy;
+    const long long &sx = a.sx, &sy = a.sy;
     pair32 w[W][P] = {}, b[P] = {}, dw[W][P] = {}, db[P] = {};
     if (on) params<W, V>(a, c, w, b);
     const long long items = (long long)a.Be * a.tiles;
     for (long long item = (long long)blockIdx.y * rows + p0; on && item < items; item += (long long)gridDim.y * rows) {
         const int tile = (int)(item / a.Be), e = (int)(item - (long long)tile * a.Be);
-        const T *x = static_cast<const T *>(a.x) + e * a.ldx + c, *dy = static_cast<const T *>(a.dy) + e * a.ldy + c;
-        T *dx = static_cast<T *>(a.dx) + e * a.ldx + c;
+        const T *x = static_cast<const T *>(a.x) + e * a.ldx + c;
         const uint8_t *done = a.done ? a.done + e : nullptr;
         const long long states = (long long)e * (W - 1) * a.C + c;
         const T *state = a.state_in ? static_cast<const T *>(a.state_in) + states : nullptr;
         T *dstate = a.dstate_in ? static_cast<T *>(a.dstate_in) + states : nullptr;
         const int t0 = tile * a.run, t1 = min(a.T, t0 + a.run), end = min(a.T, t1 + W - 1);
-        const T *ahead = x + t0 * sx, *gahead = dy + t0 * sy;
-        int fetched = t0;
+        const T *ahead = x + t0 * sx, *gahead = static_cast<const T *>(a.dy) + e * a.ldy + c + t0 * sy;
+        int left = end - t0, to = 0;
         const auto fetch = [&] {
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (fetched + j < end) {
-                    xs.copy((fetched - t0) % S + j, ahead + j * sx);
-                    gs.copy((fetched - t0) % S + j, gahead + j * sy);
+            for (int j = 0; j < BATCH; ++j)
+                if (j < left) {
+                    xs.copy(to + j, ahead + j * sx);
+                    gs.copy(to + j, gahead + j * sy);
                 }
             batch_end();
-            fetched += 2;
-            ahead += 2 * sx;
-            gahead += 2 * sy;
+            left -= BATCH;
+            ahead += BATCH * sx;
+            gahead += BATCH * sy;
+            to = to + BATCH == S ? 0 : to + BATCH;
         };
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) fetch();
-        pair32 h[W - 1][P], acc[W][P] = {};
-        int seen = history<T, W, V>(a, x, state, e, t0, h) | 1 << (W - 1);
-        const auto put = [&](int t, const pair32 (&g)[P]) {  // the gradient of the input of step t is complete
+        // h[t % W]: the input of step t0 + t, acc[t % W]: its gradient; bit i of seen: whether step t still sees the input of step t - W + 1 + i
+        pair32 h[W][P], acc[W][P] = {};
+        int seen;
+        {
+            pair32 f[W - 1][P];
+            seen = history<T, W, V>(a, x, state, e, t0, f) | 1 << (W - 1);
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i)
+#pragma unroll
+                for (int p = 0; p < P; ++p) h[i + 1][p] = f[i][p];
+        }
+        T *dx = static_cast<T *>(a.dx) + e * a.ldx + c + (t0 - W + 1) * sx;  // of the step whose gradient is complete next
+        const auto put = [&](int t, const pair32 (&g)[P]) {
             Raw<T, V> r;
             r.set(g);
-            if (t >= t0 && t < t1) r.store(dx + t * sx);
-            else if (t < 0 && t >= 1 - W && dstate) r.store(dstate + (long long)(t + W - 1) * a.C);
+            if (t >= t0) {
+                if (t < t1) r.store(dx);
+            } else if (t < 0 && t >= 1 - W && dstate) {
+                r.store(dstate + (long long)(t + W - 1) * a.C);
+            }
+            dx += sx;
         };
-        for (int t = t0; t < end; t += 2) {
+        int from = 0;
+        for (int t = t0; t < end; t += BATCH) {
             fetch();
-            bool flag[2];
+            bool flag[BATCH];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) flag[j] = done && t + j < end && done[(long long)(t + j) * a.Be];
+            for (int j = 0; j < BATCH; ++j) flag[j] = done && t + j < end && done[(long long)(t + j) * a.Be];
             batch_wait<AHEAD>();
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < BATCH; ++j) {
                 if (t + j >= end) break;
-                pair32 in[P], g[P], z[P];
+                pair32 g[P], z[P];
                 Raw<T, V> r;
-                xs.get((t - t0) % S + j, r);
-                r.get(in);
-                gs.get((t - t0) % S + j, r);
+                xs.get(from + j, r);
+                r.get(h[j % W]);
+                gs.get(from + j, r);
                 r.get(g);
-                const bool own = t + j < t1;
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    pair32 s = b[p];
+                    z[p] = b[p];
 #pragma unroll
-                    for (int i = 0; i < W - 1; ++i) s = fma2(w[i][p], h[i][p], s);
-                    z[p] = fma2(w[W - 1][p], in[p], s);
+                    for (int i = 0; i < W; ++i) z[p] = fma2(w[i][p], h[(j + 1 + i) % W][p], z[p]);
                 }
                 through_act(g, z, a.act);
-                if (seen == (1 << W) - 1) {
+                if (seen == ALL) {
 #pragma unroll
                     for (int i = 0; i < W; ++i)
 #pragma unroll
-                        for (int p = 0; p < P; ++p) acc[i][p] = fma2(w[i][p], g[p], acc[i][p]);
+                        for (int p = 0; p < P; ++p) acc[(j + 1 + i) % W][p] = fma2(w[i][p], g[p], acc[(j + 1 + i) % W][p]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < W; ++i)
                         if (seen >> i & 1) {
 #pragma unroll
-                            for (int p = 0; p < P; ++p) acc[i][p] = fma2(w[i][p], g[p], acc[i][p]);
+                            for (int p = 0; p < P; ++p) acc[(j + 1 + i) % W][p] = fma2(w[i][p], g[p], acc[(j + 1 + i) % W][p]);
                         }
                 }
-                if (own) {
+                if (t + j < t1) {
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
 #pragma unroll
-                        for (int i = 0; i < W - 1; ++i) dw[i][p] = fma2(g[p], h[i][p], dw[i][p]);
-                        dw[W - 1][p] = fma2(g[p], in[p], dw[W - 1][p]);
+                        for (int i = 0; i < W; ++i) dw[i][p] = fma2(g[p], h[(j + 1 + i) % W][p], dw[i][p]);
                         db[p] = add2(db[p], g[p]);
                     }
                 }
-                put(t + j - W + 1, acc[0]);
+                put(t + j - W + 1, acc[(j + 1) % W]);
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-#pragma unroll
-                    for (int i = 0; i < W - 1; ++i) acc[i][p] = acc[i + 1][p];
-                    acc[W - 1][p] = 0;
-#pragma unroll
-                    for (int i = 0; i < W - 2; ++i) h[i][p] = h[i + 1][p];
-                    h[W - 2][p] = in[p];
-                }
+                for (int p = 0; p < P; ++p) acc[(j + 1) % W][p] = 0;
                 seen = seen >> 1 | 1 << (W - 1);
                 if (flag[j]) {
                     seen = 1 << (W - 1);
 #pragma unroll
-                    for (int i = 0; i < W - 1; ++i)
+                    for (int i = 0; i < W; ++i)
 #pragma unroll
                         for (int p = 0; p < P; ++p) h[i][p] = 0;
                 }
             }
+            from = from + BATCH == S ? 0 : from + BATCH;
         }
         batch_wait<0>();
-        if (end == a.T) {  // what is left of the sequence, and reaches on into the state
+        // What is left at the end of the sequence reaches on into the state.  Behind the last step, of which there were end - t0, the gradient of the
+        // input i steps from the oldest one is acc[(end - t0 + i + 1) % W].
+        if (end == a.T) {
+            const int turn = (end - t0) % W;
 #pragma unroll
             for (int i = 0; i < W - 1; ++i) {
+                pair32 s[P] = {};
                 if (a.dstate_out && seen >> i & 1) {
                     Raw<T, V> r;
-                    pair32 s[P];
                     r.load(static_cast<const T *>(a.dstate_out) + states + (long long)i * a.C);
                     r.get(s);
-#pragma unroll
-                    for (int p = 0; p < P; ++p) acc[i][p] = add2(acc[i][p], s[p]);
                 }
-                put(a.T - W + 1 + i, acc[i]);
+#pragma unroll
+                for (int k = 0; k < W; ++k)
+                    if ((turn + i + 1) % W == k) {
+#pragma unroll
+                        for (int p = 0; p < P; ++p) s[p] = add2(acc[k][p], s[p]);
+                    }
+                put(a.T - W + 1 + i, s);
             }
         }
     }
@@ -463,6 +483,8 @@ ConvArgs args(const ppo_causal_conv_desc *d, const void *x, const float *weight,
     a.done = done;
     a.ldx = d->ldx;
     a.ldy = d->ldy;
+    a.sx = d->Be * d->ldx;
+    a.sy = d->Be * d->ldy;
     a.T = d->T;
     a.Be = d->Be;
     a.C = d->C;
@@ -481,7 +503,7 @@ BwdPlan plan_bwd(const ppo_causal_conv_desc *d, int V) {
     while (p.lanes < 32 && p.lanes * V < d->C) p.lanes *= 2;
     p.cols = ppo_cdiv(d->C, p.lanes * V);
     const long long items = (long long)d->Be * ppo_cdiv(d->T, kRun);
-    const long long all = (items + kThreads / p.lanes - 1) / (kThreads / p.lanes), want = ppo_cdiv(4 * 148, p.cols);
+    const long long all = (items + kThreads / p.lanes - 1) / (kThreads / p.lanes), want = p.cols < 4 * 148 ? 4 * 148 / p.cols : 1;  // one round of four blocks an SM
     p.blocks = (int)(all < want ? all : want);
     return p;
 }
@@ -505,8 +527,8 @@ int with_width(const ppo_causal_conv_desc *d, F &&fn) {
 bool vectors(const ppo_causal_conv_desc *d, int V, std::initializer_list<const void *> ps) {
     return d->C % V == 0 && d->ldx % V == 0 && d->ldy % V == 0 && !misaligned(ps, V * elem_bytes(d->dtype));
 }
-// Channels of a thread: 16 bytes of them, but 8 bytes of 16-bit gradients, whose shares need the registers.
-constexpr int kBwdV = 4;
+// Channels of a thread: 16 bytes of them, but 8 bytes in the gradients, whose shares need the registers.
+int bwd_v(const ppo_causal_conv_desc *d) { return 8 / (int)elem_bytes(d->dtype); }
 // fn(T{}, width, V)
 template <typename F>
 int with_columns(const ppo_causal_conv_desc *d, bool vec, F &&fn) {
@@ -520,7 +542,7 @@ int with_columns(const ppo_causal_conv_desc *d, bool vec, F &&fn) {
 
 extern "C" size_t ppo_causal_conv_workspace_bytes(const ppo_causal_conv_desc *d) {
     if (check(d) != PPO_OK) return 0;
-    const int one = plan_bwd(d, 1).blocks, many = plan_bwd(d, kBwdV).blocks;
+    const int one = plan_bwd(d, 1).blocks, many = plan_bwd(d, bwd_v(d)).blocks;
     return (size_t)(one > many ? one : many) * d->C * (d->width + 1) * sizeof(float);
 }
 
@@ -558,14 +580,14 @@ extern "C" int ppo_causal_conv_bwd(const ppo_causal_conv_desc *d, const void *x,
     a.dstate_out = dstate_out;
     a.dx = dx;
     a.dstate_in = dstate_in;
-    const bool params = dweight || dbias, vec = vectors(d, kBwdV, {x, dy, dx, state_in, dstate_out, dstate_in});
+    const bool params = dweight || dbias, vec = vectors(d, bwd_v(d), {x, dy, dx, state_in, dstate_out, dstate_in});
     a.part = params ? static_cast<float *>(workspace) : nullptr;
-    const BwdPlan p = plan_bwd(d, vec ? kBwdV : 1);
+    const BwdPlan p = plan_bwd(d, vec ? bwd_v(d) : 1);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     PPO_TRY(with_width(d, [&](auto t, auto w) -> int {
         using T = decltype(t);
         constexpr int W = decltype(w)::value;
-        return ppo_launch(vec ? conv_bwd_kernel<T, W, kBwdV> : conv_bwd_kernel<T, W, 1>, dim3(p.cols, p.blocks), dim3(kThreads), 0, st, a, p.lanes);
+        return ppo_launch(vec ? conv_bwd_kernel<T, W, 8 / (int)sizeof(T)> : conv_bwd_kernel<T, W, 1>, dim3(p.cols, p.blocks), dim3(kThreads), 0, st, a, p.lanes);
     }));
     return params ? ppo_param_sum(a.part, p.blocks, {{dweight, dbias, nullptr}, {d->C * d->width, d->C, 0}}, accumulate, st) : PPO_OK;
 }

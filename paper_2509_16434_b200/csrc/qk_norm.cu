@@ -267,7 +267,7 @@ __device__ __forceinline__ void stage_gamma(const QkArgs &a, float (&to)[2][kMax
 constexpr int kHeads = 4;  // of a lane's, on their way at a time
 
 template <typename T, bool INTERLEAVED>
-__global__ void __launch_bounds__(256) qk_fwd_kernel(QkArgs a, Lanes k) {
+__global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
     constexpr int V = Vec<T>::N, P = V / 2;
     __shared__ alignas(16) float gamma[2][kMaxD];
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(256) qk_fwd_kernel(QkArgs a, Lanes k) {
 // With n = R^T dy (turned back), g = gamma n and r = 1 / sqrt(mean x^2 + eps): dx = r g - x r^3 mean(g x), dgamma += n x r.  Both sums of a head are
 // made at once.
 template <typename T, bool INTERLEAVED>
-__global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, Lanes k) {
+__global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
     constexpr int V = Vec<T>::N, P = V / 2, U = 2;
     __shared__ alignas(16) float gamma[2][kMaxD];

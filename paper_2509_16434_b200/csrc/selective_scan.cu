@@ -24,7 +24,8 @@ struct ScanArgs {
     const uint8_t *done;
     void *y, *dx, *ddt, *dB, *dC, *dz;
     float *state_out, *dstate_in;
-    long long ldx, lddt, ldb, ldc, ldz, ldy;
+    long long ldx, lddt, ldb, ldc, ldz, ldy;  // from row to row, and from step to step:
+    long long sx, st, sb, sc, sz, sy;
     int T, Be, channels, N, groups, per, softplus;  // per: channels of a group
     int tiles, group_tiles;                         // tiles of channels, in all and of a group
     int len, nseg;                                  // steps of a segment
@@ -42,7 +43,8 @@ struct ScanArgs {
 // exp(d A), A times log2(e).  The hardware's exponential lies 0.4 units of 2^-24 too low on average for arguments between -0.5 and -0.01, which adds up over
 // the hundreds of steps that a state remembers; with its argument moved by 2e-8 the mean is within 0.2 from -0.5 to 0 (one million arguments
 // each), as near as expf's, at no cost.
-__device__ __forceinline__ pair32 factors(pair32 d, pair32 A) { return exp2_pair(fma2(d, A, twice(2e-8f))); }
+constexpr float kShift = 2e-8f;
+__device__ __forceinline__ pair32 factors(pair32 d, pair32 A) { return exp2_pair(fma2(d, A, twice(kShift))); }
 
 // Sums of V values over LANES lanes, STRIDE apart: halves go to the lanes' halves as long as there are values, lane bit by lane bit from the
 // highest; a lane is left with max(1, V / LANES) of them in v[0 ..].  index() says which.
@@ -307,7 +309,7 @@ struct FewRows {
 };
 
 template <typename T, int NL, int CPT, int MODE>
-__global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) scan_kernel(ScanArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) scan_kernel(ScanArgs a) {
     grid_wait();
     constexpr int W = 16, P = W / 2, NP = W * NL, CT = kThreads / NL * CPT;
     constexpr bool WITH_C = MODE == OUTPUT || MODE == BOTH, WITH_DY = MODE == BOTH, WITH_Z = MODE == OUTPUT || MODE == BOTH;
@@ -316,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) 
     const Work w = work_of<CT>(a, blockIdx.x % a.tiles, blockIdx.x / a.tiles);
     const int ln = threadIdx.x % NL, c = w.c0 + threadIdx.x / NL * CPT, n0 = ln * W;
     const bool on = c < w.c1;
-    const long long sx = a.Be * a.ldx, st = a.Be * a.lddt, sb = a.Be * a.ldb, sc = a.Be * a.ldc, sz = a.Be * a.ldz, sy = a.Be * a.ldy;
+    const long long &sx = a.sx, &st = a.st, &sb = a.sb, &sc = a.sc, &sz = a.sz, &sy = a.sy;
     const T *x = static_cast<const T *>(a.x) + w.e * a.ldx + c + w.t0 * sx, *dt = static_cast<const T *>(a.dt) + w.e * a.lddt + c + w.t0 * st;
     const T *B = static_cast<const T *>(a.B) + w.e * a.ldb + (long long)w.group * a.N + w.t0 * sb;
     const T *C = static_cast<const T *>(a.C) + w.e * a.ldc + (long long)w.group * a.N + w.t0 * sc;
@@ -325,17 +327,15 @@ __global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) 
     T *y = MODE == OUTPUT ? static_cast<T *>(a.y) + w.e * a.ldy + c + w.t0 * sy : nullptr;
 
     Word rx[4], rt[4], rz[WITH_Z ? 4 : 1], rg[WITH_DY ? 4 : 1];
-    const auto fetch = [&](int rows) {  // of the four steps at x, dt, z and dy
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (!on || k >= rows) break;
-            rx[k].load(x + k * sx);
-            rt[k].load(dt + k * st);
-            if (WITH_Z && z) rz[k].load(z + k * sz);
-            if (WITH_DY) rg[k].load(dy + k * sy);
-        }
+    const auto fetch = [&](int k, bool there) {  // step k of the four at x, dt, z and dy
+        if (!there) return;
+        rx[k].load(x + k * sx);
+        rt[k].load(dt + k * st);
+        if (WITH_Z && z) rz[k].load(z + k * sz);
+        if (WITH_DY) rg[k].load(dy + k * sy);
     };
-    fetch(w.t1 - w.t0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) fetch(k, on && w.t0 + k < w.t1);
     FewRows<T, NP, WITH_C> few;
     few.fetch(B, C, sb, sc, w.t1 - w.t0, a.N);
 
@@ -392,27 +392,25 @@ __global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) 
         }
 #pragma unroll 1
         for (int s = 0; s < kSteps && s < rows; s += 4) {
-            pair32 xs[4], ds[4], zs[4], gs[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                xs[k] = ds[k] = zs[k] = gs[k] = 0;
-                if (!on || s + k >= rows) continue;
-                xs[k] = rx[k].get();
-                ds[k] = add2(rt[k].get(), bias);
-                if (a.softplus) ds[k] = Word::softplus(ds[k]);
-                if (WITH_Z && z) zs[k] = Word::silu(rz[k].get());
-                if (WITH_DY) gs[k] = rg[k].get();
-                if (WITH_DY && z) gs[k] = mul2(gs[k], zs[k]);
-            }
             x += 4 * sx;
             dt += 4 * st;
             if (WITH_Z && z) z += 4 * sz;
             if (WITH_DY) dy += 4 * sy;
-            fetch(rows - s - 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
+                pair32 xk = 0, dk = 0, zk = 0, gk = 0;
+                if (on && s + k < rows) {
+                    xk = rx[k].get();
+                    dk = add2(rt[k].get(), bias);
+                    if (WITH_Z && z) zk = rz[k].get();
+                    if (WITH_DY) gk = rg[k].get();
+                }
+                fetch(k, on && s + k + 4 < rows);  // the step that comes four steps later is on its way meanwhile
+                if (a.softplus && on && s + k < rows) dk = Word::softplus(dk);
+                if (WITH_Z && z) zk = Word::silu(zk);
+                if (WITH_DY && z) gk = mul2(gk, zk);
                 pair32 out[CPT];
-                const float2 d = parts(ds[k]), u = parts(mul2(ds[k], xs[k])), g = parts(gs[k]);
+                const float2 d = parts(dk), u = parts(mul2(dk, xk)), g = parts(gk);
 #pragma unroll
                 for (int j = 0; j < CPT; ++j) out[j] = 0;
 #pragma unroll
@@ -433,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) 
                             }
                         }
                 }
-                if constexpr (MODE == ENDS || MODE == BOTH) total = add2(total, ds[k]);
+                if constexpr (MODE == ENDS || MODE == BOTH) total = add2(total, dk);
                 if constexpr (MODE == OUTPUT) {
                     const float2 o = parts(out[0]), q = parts(out[CPT - 1]);
                     float lo = o.x + o.y, hi = CPT == 2 ? q.x + q.y : 0.f;
@@ -442,8 +440,8 @@ __global__ void __launch_bounds__(kThreads, CPT == 2 && MODE == OUTPUT ? 3 : 4) 
                         lo += __shfl_xor_sync(0xffffffffu, lo, m);
                         if (CPT == 2) hi += __shfl_xor_sync(0xffffffffu, hi, m);
                     }
-                    pair32 v = a.D ? fma2(D, xs[k], pair_of(lo, hi)) : pair_of(lo, hi);
-                    if (z) v = mul2(v, zs[k]);
+                    pair32 v = a.D ? fma2(D, xk, pair_of(lo, hi)) : pair_of(lo, hi);
+                    if (z) v = mul2(v, zk);
                     if (on && ln == 0 && s + k < rows) Word::put(y + k * sy, v);
                 }
                 if (flag >> (s + k) & 1) {
@@ -531,10 +529,10 @@ struct GradShared {
     float sd[kSteps][CT], su[kSteps][CT], sg[kSteps][CT], sy[kSteps][CT], sD[CT], sbias[CT];
     float2 sB[kSteps][NP], sC[kSteps][NP];  // every element twice, as packed arithmetic on two channels takes it
     float few[kThreads / 32][kSteps][2 * NP];
-    // a thread's own: the states in front of the next tile; those in front of every fourth step of this one; its sums of the gradients of D and
+    // a thread's own: the states in front of the tile; those in front of its 8th and 12th step (the last four start where the way forwards ends); its sums of the gradients of D and
     // dt_bias; its elements of the next tile's rows of x, dt, dy, z
     float2 mark[4][kThreads];
-    float4 inner[4][2][kThreads];
+    float4 inner[2][2][kThreads];
     float kept[2][kThreads * R::V];
     typename R::Raw next[4][R::PASSES][kThreads];
 };
@@ -564,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
     const int lane = threadIdx.x % 32, ln = lane % NL, warp = threadIdx.x / 32, n0 = ln * NPT, local = (warp * GROUPS + lane / NL) * 4;
     Work w = work_of<CT>(a, tile, slice);
     const int c = w.c0 + local, cols = w.c1 - w.c0;
-    const long long sx = a.Be * a.ldx, st = a.Be * a.lddt, sb = a.Be * a.ldb, sc = a.Be * a.ldc, sz = a.Be * a.ldz, sy = a.Be * a.ldy;
+    const long long &sx = a.sx, &st = a.st, &sb = a.sb, &sc = a.sc, &sz = a.sz, &sy = a.sy;
     pair32 A[NPT][2], g[NPT][2], dA[NPT][2];
     {
         float f[4][NPT];
@@ -606,6 +604,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
             fb[i] = ok ? B[r * sb + n] : from_f32<T>(0.f);
             fc[i] = ok ? C[r * sc + n] : from_f32<T>(0.f);
         }
+    };
+    const auto fetch_mark = [&](const Work &w, int t) {
         // up to kSteps steps start from the state that comes in, whose rows need not be aligned
         const float *mark = a.mark + (((long long)(t / kSteps) * a.Be + w.e) * a.channels + c) * NP + n0;
         if (a.T > kSteps) {
@@ -620,6 +620,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
     };
     const auto last_tile = [&](const Work &w) { return w.t0 + (w.t1 - 1 - w.t0) / kSteps * kSteps; };
     fetch(w, last_tile(w));
+    fetch_mark(w, last_tile(w));
 
     const long long items = (long long)a.Be * a.nseg;
     for (long long item = slice; item < items; item += a.parts) {
@@ -678,12 +679,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
                 R::put_shared(&s.su[r][l], u);
                 R::put_shared(&s.sg[r][l], v);
             }
-            float start[4][NPT];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 f = s.mark[j][threadIdx.x];
-                start[j][0] = f.x, start[j][1] = f.y;
-            }
             {
                 // on its way while this tile is worked on
                 const bool more = t > w.t0;
@@ -695,12 +690,29 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
             __syncthreads();
             const int top = (rows - 1) / 4;
             pair32 h[NPT][2];
-            pack(start, h);
+            const auto load_start = [&](int m) {  // the states in front of steps 4 m ..
+                if (m == 0) {
+                    float f[4][NPT];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 v = s.mark[j][threadIdx.x];
+                        f[j][0] = v.x, f[j][1] = v.y;
+                    }
+                    pack(f, h);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < NPT; ++n) {
+                        const float4 f = s.inner[m - 1][n][threadIdx.x];
+                        h[n][0] = pair_of(f.x, f.y), h[n][1] = pair_of(f.z, f.w);
+                    }
+                }
+            };
+            load_start(0);
             // forwards to the states in front of every fourth step
 #pragma unroll 1
             for (int m = 0; m < top; ++m) {
-                s.inner[m][0][threadIdx.x] = make_float4(parts(h[0][0]).x, parts(h[0][0]).y, parts(h[0][1]).x, parts(h[0][1]).y);
-                s.inner[m][1][threadIdx.x] = make_float4(parts(h[1][0]).x, parts(h[1][0]).y, parts(h[1][1]).x, parts(h[1][1]).y);
+                if (m > 0) s.inner[m - 1][0][threadIdx.x] = make_float4(parts(h[0][0]).x, parts(h[0][0]).y, parts(h[0][1]).x, parts(h[0][1]).y);
+                if (m > 0) s.inner[m - 1][1][threadIdx.x] = make_float4(parts(h[1][0]).x, parts(h[1][0]).y, parts(h[1][1]).x, parts(h[1][1]).y);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int r = 4 * m + k;
@@ -721,13 +733,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
 #pragma unroll 1
             for (int m = top; m >= 0; --m) {
                 const int r0 = 4 * m;
-                if (m < top) {
-#pragma unroll
-                    for (int n = 0; n < NPT; ++n) {
-                        const float4 f = s.inner[m][n][threadIdx.x];
-                        h[n][0] = pair_of(f.x, f.y), h[n][1] = pair_of(f.z, f.w);
-                    }
-                }
+                if (m < top) load_start(m);
                 pair32 q[4][NPT][2];  // of each step exp(d A) times the state in front
 #pragma unroll
                 for (int k = 0; k < 4; k += 2) {
@@ -829,6 +835,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
                 const long long row = (long long)(t + r) * a.Be + w.e;
                 a.few[(((long long)(tile - w.group * a.group_tiles) * a.T * a.Be + row) * a.groups + w.group) * (2 * NP) + n] = sum;
             }
+            if (const bool more = t > w.t0; more || item + a.parts < items) {
+                const Work v = more ? w : work_of<CT>(a, tile, item + a.parts);
+                fetch_mark(v, more ? t - kSteps : last_tile(v));
+            }
             {
                 const long long ax = w.e * a.ldx + w.c0 + t * sx, at = w.e * a.lddt + w.c0 + t * st, az = w.e * a.ldz + w.c0 + t * sz, ay = w.e * a.ldy + w.c0 + t * sy;
                 R rx, rt, rg, rz;
@@ -924,64 +934,105 @@ __global__ void __launch_bounds__(256) scan_few_kernel(ScanArgs a) {
     else static_cast<T *>(a.dC)[row * a.ldc + group * a.N + n] = from_f32<T>(sum);
 }
 
-// One step, the state in place: NL lanes share a channel, four elements each.
+// One step, the state in place: NL lanes share a channel, four elements each, and take two envs at a time, whose step sizes and outputs they
+// share out among them.  Bound by memory, since the states go through once: a thread copies its own of the next envs ahead into shared memory.
+constexpr int kPairs = 4;  // pairs of envs in the ring
+
 template <typename T, int NL>
-__global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a, int envs) {
+__global__ void __launch_bounds__(256, 4) scan_step_kernel(ScanArgs a, int envs) {
     grid_wait();
-    constexpr int CHANNELS = 256 / NL;
-    const int cols = (a.channels + CHANNELS - 1) / CHANNELS, c = blockIdx.x % cols * CHANNELS + threadIdx.x / NL, n0 = threadIdx.x % NL * 4;
-    const int e0 = blockIdx.x / cols * envs;
-    const bool on = c < a.channels, whole = a.N % 4 == 0;
-    float A[4] = {}, D = 0.f, bias = 0.f;
-    const int group = on ? c / a.per : 0;
-    if (on) {
+    constexpr int CHANNELS = 256 / NL, LEFT = NL >= 2 ? 1 : 2, EACH = NL >= 2 ? NL / 2 : 1;  // envs of a lane; lanes that have the same one
+    __shared__ float4 ring[kPairs][2][256];
+    const int cols = (a.channels + CHANNELS - 1) / CHANNELS, c = blockIdx.x % cols * CHANNELS + threadIdx.x / NL, ln = threadIdx.x % NL, n0 = ln * 4;
+    const int e0 = blockIdx.x / cols * envs, e1 = min(a.Be, e0 + envs), first = ln / EACH * LEFT;
+    const bool on = c < a.channels, whole = a.N % 4 == 0, ahead = whole && on && n0 < a.N;
+    const bool few = whole && ((a.ldb | a.ldc) & 3) == 0 && ((reinterpret_cast<uintptr_t>(a.B) | reinterpret_cast<uintptr_t>(a.C)) & (4 * sizeof(T) - 1)) == 0;
+    const long long next = (long long)a.channels * a.N;
+    float *state = a.state_out + ((long long)e0 * a.channels + c) * a.N;
+    const auto fetch = [&](int e, int slot) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n) A[n] = n0 + n < a.N ? a.A[(long long)c * a.N + n0 + n] * kLog2e : 0.f;
+        for (int k = 0; k < 2; ++k)
+            if (ahead && e + k < e1) {
+                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&ring[slot][k][threadIdx.x]);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(a.state_out + ((long long)(e + k) * a.channels + c) * a.N + n0) : "memory");
+            }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kPairs - 1; ++i) fetch(e0 + 2 * i, i);
+    float A[4] = {}, D = 0.f, bias = 0.f;
+    const int at = on ? c / a.per * a.N + n0 : 0;
+    if (on) {
+        load_row<4>(a.A + (long long)c * a.N, a.N, n0, A);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) A[n] *= kLog2e;
         if (a.D) D = a.D[c];
         if (a.bias) bias = a.bias[c];
     }
-    for (int e = e0; e < min(a.Be, e0 + envs); ++e) {
-        float h[4] = {}, y = 0.f, x = 0.f;
-        float *state = a.state_out + ((long long)e * a.channels + c) * a.N + n0;
-        if (on) {
-            const bool empty = a.done && a.done[e];
-            if (whole) {
-                if (n0 < a.N && !empty) {
-                    const float4 f = *reinterpret_cast<const float4 *>(state);
-                    h[0] = f.x, h[1] = f.y, h[2] = f.z, h[3] = f.w;
-                }
+    const auto load_four = [&](const T *p, float (&v)[4]) {
+        if (few && n0 < a.N) {
+            Vec<T> r;
+            float f[Vec<T>::N];
+            if constexpr (sizeof(T) == 4) {
+                r.raw = *reinterpret_cast<const uint4 *>(p);
             } else {
-#pragma unroll
-                for (int n = 0; n < 4; ++n)
-                    if (n0 + n < a.N && !empty) h[n] = state[n];
+                const uint2 u = *reinterpret_cast<const uint2 *>(p);
+                r.raw = make_uint4(u.x, u.y, 0, 0);
             }
-            x = to_f32(static_cast<const T *>(a.x)[e * a.ldx + c]);
-            float d = to_f32(static_cast<const T *>(a.dt)[e * a.lddt + c]) + bias;
-            if (a.softplus) d = softplus_fast(d);
-            const T *B = static_cast<const T *>(a.B) + e * a.ldb + (long long)group * a.N + n0, *C = static_cast<const T *>(a.C) + e * a.ldc + (long long)group * a.N + n0;
+            r.get(f);
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                if (n0 + n >= a.N) break;
-                h[n] = fmaf(exp2_fast(d * A[n]), h[n], d * x * to_f32(B[n]));
-                y = fmaf(to_f32(C[n]), h[n], y);
-            }
-            if (whole) {
-                if (n0 < a.N) *reinterpret_cast<float4 *>(state) = make_float4(h[0], h[1], h[2], h[3]);
-            } else {
+            for (int n = 0; n < 4; ++n) v[n] = f[n];
+        } else {
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
-                    if (n0 + n < a.N) state[n] = h[n];
-            }
+            for (int n = 0; n < 4; ++n) v[n] = n0 + n < a.N ? to_f32(p[n]) : 0.f;
+        }
+    };
+    int slot = 0;
+    for (int e = e0; e < e1; e += 2, slot = (slot + 1) % kPairs, state += 2 * next) {
+        fetch(e + 2 * (kPairs - 1), (slot + kPairs - 1) % kPairs);
+        float h[2][4] = {}, b[2][4] = {}, cc[2][4] = {}, x[LEFT] = {}, z[LEFT] = {}, d[LEFT] = {}, y[2] = {};
+        bool empty[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (!on || e + k >= e1) break;
+            empty[k] = a.done && a.done[e + k];
+            load_four(static_cast<const T *>(a.B) + (e + k) * a.ldb + at, b[k]);
+            load_four(static_cast<const T *>(a.C) + (e + k) * a.ldc + at, cc[k]);
+            if (!whole && !empty[k]) load_row<4>(state + k * next, a.N, n0, h[k]);
         }
 #pragma unroll
-        for (int o = NL / 2; o > 0; o /= 2) y += __shfl_xor_sync(0xffffffffu, y, o);
-        if (on && n0 == 0) {
-            y = fmaf(D, x, y);
-            if (a.z) {
-                const float z = to_f32(static_cast<const T *>(a.z)[e * a.ldz + c]);
-                y *= z * sigmoid_fast(z);
+        for (int i = 0; i < LEFT; ++i) {
+            const int k = e + first + i;
+            if (!on || k >= e1) break;
+            x[i] = to_f32(static_cast<const T *>(a.x)[k * a.ldx + c]);
+            d[i] = to_f32(static_cast<const T *>(a.dt)[k * a.lddt + c]) + bias;
+            if (a.softplus) d[i] = softplus_fast(d[i]);
+            if (a.z) z[i] = to_f32(static_cast<const T *>(a.z)[k * a.ldz + c]);
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kPairs - 1) : "memory");
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float dk = __shfl_sync(0xffffffffu, d[k % LEFT], k / LEFT * EACH, NL), uk = __shfl_sync(0xffffffffu, d[k % LEFT] * x[k % LEFT], k / LEFT * EACH, NL);
+            if (!on || e + k >= e1) continue;
+            if (ahead && !empty[k]) {
+                const float4 f = ring[slot][k][threadIdx.x];
+                h[k][0] = f.x, h[k][1] = f.y, h[k][2] = f.z, h[k][3] = f.w;
             }
-            static_cast<T *>(a.y)[e * a.ldy + c] = from_f32<T>(y);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                h[k][n] = fmaf(exp2_fast(fmaf(dk, A[n], kShift)), h[k][n], uk * b[k][n]);
+                y[k] = fmaf(cc[k][n], h[k][n], y[k]);
+            }
+            store_row<4>(state + k * next, a.N, n0, h[k]);
+        }
+        spread_sum<2, NL, 1>(y, ln);
+#pragma unroll
+        for (int i = 0; i < LEFT; ++i) {
+            const int k = e + first + i;
+            if (!on || k >= e1 || ln % EACH != 0) break;
+            float v = a.D ? fmaf(D, x[i], y[i]) : y[i];
+            if (a.z) v *= z[i] * sigmoid_fast(z[i]);
+            static_cast<T *>(a.y)[k * a.ldy + c] = from_f32<T>(v);
         }
     }
 }
@@ -1015,11 +1066,11 @@ Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     const int per = d->channels / d->groups;
     p.group_tiles = ppo_cdiv(per, 64 / p.NL);
     p.tiles = p.group_tiles * d->groups;
-    // segments, none shorter than 64 steps: forwards as many as fill three blocks an SM; backwards, where three passes go over them, as many as
-    // deal three to each slice of blocks
+    // segments, none shorter than 64 steps: forwards as many as fill four blocks an SM; backwards, where three passes go over them, as many as
+    // deal two to each slice of blocks
     const int slices = p.tiles < 4 * 148 ? 4 * 148 / p.tiles : 1;  // four blocks an SM
     const long long blocks = (long long)d->Be * d->groups * ppo_cdiv(per, 256 / p.NL);
-    long long n = bwd ? (d->Be < slices ? 3ll * slices / d->Be : 1) : (blocks < 3 * 148 ? 3 * 148 / blocks : 1);
+    long long n = bwd ? (d->Be < slices ? 2ll * slices / d->Be : 1) : (blocks < 4 * 148 ? 4 * 148 / blocks : 1);
     const int most = ppo_cdiv(d->T, 64);
     if (n > most) n = most;
     p.len = ppo_cdiv(ppo_cdiv(d->T, n), kSteps) * kSteps;
@@ -1056,6 +1107,12 @@ ScanArgs args(const ppo_selective_scan_desc *d, const Plan &p, const void *x, co
     a.ldc = d->ldc;
     a.ldz = d->ldz;
     a.ldy = d->ldy;
+    a.sx = d->Be * d->ldx;
+    a.st = d->Be * d->lddt;
+    a.sb = d->Be * d->ldb;
+    a.sc = d->Be * d->ldc;
+    a.sz = d->Be * d->ldz;
+    a.sy = d->Be * d->ldy;
     a.T = d->T;
     a.Be = d->Be;
     a.channels = d->channels;
@@ -1102,6 +1159,8 @@ int back_launch(const ScanArgs &a, cudaStream_t st) {
 }
 template <typename T, int NL, int MODE>
 int pass(const ScanArgs &a, bool two, int segs, cudaStream_t st) {
+    // one channel a thread where two would leave SMs with less than two blocks
+    two = two && (long long)a.Be * a.groups * ppo_cdiv(a.per, kThreads / NL * 2) * segs >= 2 * 148;
     return two ? pass_of<T, NL, 2, MODE>(a, segs, st) : pass_of<T, NL, 1, MODE>(a, segs, st);
 }
 
@@ -1202,8 +1261,8 @@ extern "C" int ppo_selective_scan_step(const ppo_selective_scan_desc *d, const v
         const auto run = [&](auto nl) -> int {
             constexpr int NL = decltype(nl)::value;
             const long long cols = ppo_cdiv(d->channels, 256 / NL);
-            int envs = (int)(cols * d->Be / (8 * 148));  // as many envs a block as leave every SM eight
-            if (envs < 1) envs = 1;
+            // by pairs, as many envs a block as make one round of four blocks an SM
+            const int slices = cols < 4 * 148 ? (int)(4 * 148 / cols) : 1, envs = ppo_cdiv(ppo_cdiv(d->Be, slices), 2) * 2;
             return ppo_launch(scan_step_kernel<T, NL>, dim3((unsigned)(cols * ppo_cdiv(d->Be, envs))), dim3(256), 0, static_cast<cudaStream_t>(stream), a, envs);
         };
         if (d->N <= 4) return run(std::integral_constant<int, 1>{});
