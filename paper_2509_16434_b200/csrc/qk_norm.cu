@@ -149,6 +149,7 @@ __global__ void __launch_bounds__(256) qk_bwd_any_kernel(QkArgs a) {
 // of a part.
 struct Lanes {
     int lanes, slots, parts, heads;
+    int warps;  // of a block, for the queries (gradients, where a warp has either queries or keys)
 };
 
 // The row's turns, and where a lane's two vectors stand in a head.
@@ -157,7 +158,7 @@ struct Turns {
     static constexpr int V = Vec<T>::N, P = V / 2;
     int first, second;
     bool on;
-    pair32 c[INTERLEAVED ? V : P], s[INTERLEAVED ? V : P];  // interleaved: of each pair twice, the sine's first one negative
+    pair32 c[P], s[P];  // of two pairs each
 
     __device__ __forceinline__ Turns(const QkArgs &a, const Lanes &k) {
         const int slot = threadIdx.x % k.lanes, turned = a.pairs / V;  // slots whose vectors are turned with one another
@@ -182,16 +183,12 @@ struct Turns {
         }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < (INTERLEAVED ? V : P); ++i) {
-            if constexpr (INTERLEAVED) {
-                const int p = (i < P ? first : second - V) / 2 + i;
-                const float2 t = on && p < a.pairs ? table[p] : make_float2(1.f, 0.f);
-                c[i] = pair_of(t.x, t.x), s[i] = pair_of(-t.y, t.y);
-            } else {
-                float2 t = make_float2(1.f, 0.f), u = t;
-                if (on && first < a.pairs) t = table[first + 2 * i], u = table[first + 2 * i + 1];
-                c[i] = pair_of(t.x, u.x), s[i] = pair_of(t.y, u.y);
-            }
+        for (int i = 0; i < P; ++i) {
+            float2 t = make_float2(1.f, 0.f), u = t;
+            const int p = (INTERLEAVED ? first / 2 : first) + 2 * i;
+            if (on && p < a.pairs) t = table[p];
+            if (on && p + 1 < a.pairs) u = table[p + 1];
+            c[i] = pair_of(t.x, u.x), s[i] = pair_of(t.y, u.y);
         }
     }
     static __device__ __forceinline__ pair32 minus(pair32 p) { return mul2(p, pair_of(-1.f, -1.f)); }
@@ -205,8 +202,9 @@ struct Turns {
         if constexpr (INTERLEAVED) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const pair32 o = swap(x[i]);
-                x[i] = fma2(x[i], c[i], mul2(o, BACK ? minus(s[i]) : s[i]));
+                const float2 ct = parts(c[i / 2]), st = parts(s[i / 2]);
+                const float cos = i % 2 ? ct.y : ct.x, sin = BACK ? -(i % 2 ? st.y : st.x) : i % 2 ? st.y : st.x;
+                x[i] = fma2(x[i], pair_of(cos, cos), mul2(swap(x[i]), pair_of(-sin, sin)));
             }
         } else {
 #pragma unroll
@@ -323,7 +321,7 @@ __global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
 }
 
 // With n = R^T dy (turned back), g = gamma n and r = 1 / sqrt(mean x^2 + eps): dx = r g - x r^3 mean(g x), dgamma += n x r.  Both sums of a head are
-// made at once.
+// made at once.  A warp has either queries or keys, and keeps its share of the gradient of their gamma.
 template <typename T, bool INTERLEAVED>
 __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
@@ -334,100 +332,92 @@ __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
     stage_gamma(a, gamma);
     Turns<T, INTERLEAVED> turns(a, k);
     const int group = threadIdx.x % 32 / k.lanes, groups = 32 / k.lanes, w = threadIdx.x / 32;
-    pair32 sum[2][V] = {};
-    const long long items = (long long)a.rows * k.parts, step = (long long)gridDim.x * 8;
-    for (long long item = (long long)blockIdx.x * 8 + w; item < items; item += step) {
-        const long long row = item / k.parts;
-        const int h0 = (int)(item - row * k.parts) * k.heads, h1 = min(a.heads + a.kv, h0 + k.heads);
+    const bool keys = w >= k.warps;
+    const int heads = keys ? a.kv : a.heads, mine = keys ? w - k.warps : w, warps = keys ? 8 - k.warps : k.warps;
+    const long long ld = keys ? a.ldk : a.ldq, ldo = keys ? a.ldko : a.ldqo;
+    const T *x0 = static_cast<const T *>(keys ? a.k : a.q), *dy0 = static_cast<const T *>(keys ? a.dko : a.dqo);
+    T *dx0 = static_cast<T *>(keys ? a.dk : a.dq);
+    pair32 sum[V] = {};
+    const int parts_ = (heads + k.heads - 1) / k.heads;  // of a row
+    const long long items = (long long)a.rows * parts_, step = (long long)gridDim.x * warps;
+    for (long long item = (long long)blockIdx.x * warps + mine; item < items; item += step) {
+        const long long row = item / parts_;
+        const int h0 = (int)(item - row * parts_) * k.heads, h1 = min(heads, h0 + k.heads);
         bool made = false;
+        for (int h = h0 + group; h - group < h1; h += U * groups) {
+            uint4 xr[U][2], gr[U][2];
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            // queries, then keys
-            const int from = which == 0 ? h0 : max(h0, a.heads), to = which == 0 ? min(h1, a.heads) : h1;
-            const long long ld = which == 0 ? a.ldq : a.ldk, ldo = which == 0 ? a.ldqo : a.ldko, before = which == 0 ? 0 : (long long)a.heads * a.d;
-            const T *x0 = static_cast<const T *>(which == 0 ? a.q : a.k) + row * ld - before;
-            const T *dy0 = static_cast<const T *>(which == 0 ? a.dqo : a.dko) + row * ldo - before;
-            T *dx0 = static_cast<T *>(which == 0 ? a.dq : a.dk) + row * ld - before;
-            for (int h = from + group; h - group < to; h += U * groups) {
-                uint4 xr[U][2], gr[U][2];
-#pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const int n = h + i * groups;
-                    xr[i][0] = xr[i][1] = gr[i][0] = gr[i][1] = make_uint4(0, 0, 0, 0);
-                    if (n < to && turns.on) {
-                        const T *x = x0 + (long long)n * a.d, *dy = dy0 + (long long)n * a.d;
-                        xr[i][0] = *reinterpret_cast<const uint4 *>(x + turns.first);
-                        xr[i][1] = *reinterpret_cast<const uint4 *>(x + turns.second);
-                        gr[i][0] = *reinterpret_cast<const uint4 *>(dy + turns.first);
-                        gr[i][1] = *reinterpret_cast<const uint4 *>(dy + turns.second);
-                    }
+            for (int i = 0; i < U; ++i) {
+                const int n = h + i * groups;
+                xr[i][0] = xr[i][1] = gr[i][0] = gr[i][1] = make_uint4(0, 0, 0, 0);
+                if (n < h1 && turns.on) {
+                    const T *x = x0 + row * ld + (long long)n * a.d, *dy = dy0 + row * ldo + (long long)n * a.d;
+                    xr[i][0] = *reinterpret_cast<const uint4 *>(x + turns.first);
+                    xr[i][1] = *reinterpret_cast<const uint4 *>(x + turns.second);
+                    gr[i][0] = *reinterpret_cast<const uint4 *>(dy + turns.first);
+                    gr[i][1] = *reinterpret_cast<const uint4 *>(dy + turns.second);
                 }
-                if (!made) turns.row(a, row, tables[w]);
-                made = true;
+            }
+            if (!made) turns.row(a, row, tables[w]);
+            made = true;
 #pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const int n = h + i * groups;
-                    if (n - group >= to) break;
-                    pair32 x[V], g[V], s = 0, t = 0;
-                    pairs_of<T>(xr[i][0], x);
-                    pairs_of<T>(xr[i][1], x + P);
-                    pairs_of<T>(gr[i][0], g);
-                    pairs_of<T>(gr[i][1], g + P);
-                    turns.template apply<true>(g);
-                    pair32 nx[V], gam[V];
-                    if (turns.on) {
-                        floats_of<P>(&gamma[which][turns.first], gam);
-                        floats_of<P>(&gamma[which][turns.second], gam + P);
-                    } else {
+            for (int i = 0; i < U; ++i) {
+                const int n = h + i * groups;
+                if (n - group >= h1) break;
+                pair32 x[V], g[V], s = 0, t = 0;
+                pairs_of<T>(xr[i][0], x);
+                pairs_of<T>(xr[i][1], x + P);
+                pairs_of<T>(gr[i][0], g);
+                pairs_of<T>(gr[i][1], g + P);
+                turns.template apply<true>(g);
+                pair32 gam[V];
+                if (turns.on) {
+                    floats_of<P>(&gamma[keys][turns.first], gam);
+                    floats_of<P>(&gamma[keys][turns.second], gam + P);
+                } else {
 #pragma unroll
-                        for (int j = 0; j < V; ++j) gam[j] = 0;
-                    }
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        s = fma2(x[j], x[j], s);
-                        nx[j] = mul2(g[j], x[j]);
-                        t = fma2(nx[j], gam[j], t);
-                        g[j] = mul2(g[j], gam[j]);
-                    }
-                    const float2 f = parts(s), u = parts(t);
-                    const float r = 1.f / sqrtf(lanes_sum(f.x + f.y, k.lanes) / (float)a.d + a.eps);
-                    const float m = -(lanes_sum(u.x + u.y, k.lanes) / (float)a.d) * r * r;
-                    if (n >= to || !turns.on) continue;
-                    const pair32 rr = pair_of(r, r), mm = pair_of(m, m);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        sum[which][j] = fma2(nx[j], rr, sum[which][j]);
-                        g[j] = mul2(rr, fma2(x[j], mm, g[j]));
-                    }
-                    T *dx = dx0 + (long long)n * a.d;
-                    *reinterpret_cast<uint4 *>(dx + turns.first) = raw_of<T>(g);
-                    *reinterpret_cast<uint4 *>(dx + turns.second) = raw_of<T>(g + P);
+                    for (int j = 0; j < V; ++j) gam[j] = 0;
                 }
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    s = fma2(x[j], x[j], s);
+                    t = fma2(mul2(g[j], x[j]), gam[j], t);
+                }
+                const float2 f = parts(s), u = parts(t);
+                const float r = 1.f / sqrtf(lanes_sum(f.x + f.y, k.lanes) / (float)a.d + a.eps);
+                const float m = -(lanes_sum(u.x + u.y, k.lanes) / (float)a.d) * r * r;
+                if (n >= h1 || !turns.on) continue;
+                const pair32 rr = pair_of(r, r), mm = pair_of(m, m);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    sum[j] = fma2(mul2(g[j], x[j]), rr, sum[j]);
+                    g[j] = mul2(rr, fma2(x[j], mm, mul2(g[j], gam[j])));
+                }
+                T *dx = dx0 + row * ld + (long long)n * a.d;
+                *reinterpret_cast<uint4 *>(dx + turns.first) = raw_of<T>(g);
+                *reinterpret_cast<uint4 *>(dx + turns.second) = raw_of<T>(g + P);
             }
         }
     }
     if (!a.part) return;
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float2 f = parts(sum[which][j]);
-            for (int o = k.lanes; o < 32; o *= 2) {
-                f.x += __shfl_xor_sync(0xffffffffu, f.x, o);
-                f.y += __shfl_xor_sync(0xffffffffu, f.y, o);
-            }
-            if (group == 0 && turns.on) {
-                float *to = &shares[w][j < P ? turns.first + 2 * j : turns.second + 2 * (j - P)];
-                to[0] = f.x, to[1] = f.y;
-            }
+    for (int j = 0; j < V; ++j) {
+        float2 f = parts(sum[j]);
+        for (int o = k.lanes; o < 32; o *= 2) {
+            f.x += __shfl_xor_sync(0xffffffffu, f.x, o);
+            f.y += __shfl_xor_sync(0xffffffffu, f.y, o);
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < a.d; i += 256) {
-            float s = 0.f;
-            for (int n = 0; n < 8; ++n) s += shares[n][i];
-            a.part[((size_t)blockIdx.x * 2 + which) * a.d + i] = s;
+        if (group == 0 && turns.on) {
+            float *to = &shares[w][j < P ? turns.first + 2 * j : turns.second + 2 * (j - P)];
+            to[0] = f.x, to[1] = f.y;
         }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.d; i += 256) {
+        const int which = i >= a.d, n = which ? i - a.d : i;
+        float s = 0.f;
+        for (int v = which ? k.warps : 0; v < (which ? 8 : k.warps); ++v) s += shares[v][n];
+        a.part[((size_t)blockIdx.x * 2 + which) * a.d + n] = s;
     }
 }
 
@@ -491,6 +481,8 @@ Lanes lanes_of(const ppo_qk_norm_desc *d, int warps) {
     k.parts = (int)(want < most ? want : most);
     k.heads = ppo_cdiv(ppo_cdiv(all, k.parts), side) * side;
     k.parts = ppo_cdiv(all, k.heads);
+    k.warps = (8 * d->heads + all / 2) / all;
+    k.warps = k.warps < 1 ? 1 : k.warps > 7 ? 7 : k.warps;
     return k;
 }
 template <typename F>

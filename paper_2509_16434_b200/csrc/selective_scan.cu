@@ -939,7 +939,7 @@ __global__ void __launch_bounds__(256) scan_few_kernel(ScanArgs a) {
 constexpr int kPairs = 4;  // pairs of envs in the ring
 
 template <typename T, int NL>
-__global__ void __launch_bounds__(256, 4) scan_step_kernel(ScanArgs a, int envs) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 3) scan_step_kernel(ScanArgs a, int envs) {
     grid_wait();
     constexpr int CHANNELS = 256 / NL, LEFT = NL >= 2 ? 1 : 2, EACH = NL >= 2 ? NL / 2 : 1;  // envs of a lane; lanes that have the same one
     __shared__ float4 ring[kPairs][2][256];
@@ -969,52 +969,80 @@ __global__ void __launch_bounds__(256, 4) scan_step_kernel(ScanArgs a, int envs)
         if (a.D) D = a.D[c];
         if (a.bias) bias = a.bias[c];
     }
-    const auto load_four = [&](const T *p, float (&v)[4]) {
+    using Four = std::conditional_t<sizeof(T) == 4, uint4, uint2>;
+    const auto load_four = [&](const T *p) {
+        Four w;
         if (few && n0 < a.N) {
-            Vec<T> r;
-            float f[Vec<T>::N];
-            if constexpr (sizeof(T) == 4) {
-                r.raw = *reinterpret_cast<const uint4 *>(p);
-            } else {
-                const uint2 u = *reinterpret_cast<const uint2 *>(p);
-                r.raw = make_uint4(u.x, u.y, 0, 0);
-            }
-            r.get(f);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) v[n] = f[n];
+            w = *reinterpret_cast<const Four *>(p);
         } else {
+            T *v = reinterpret_cast<T *>(&w);
 #pragma unroll
-            for (int n = 0; n < 4; ++n) v[n] = n0 + n < a.N ? to_f32(p[n]) : 0.f;
+            for (int n = 0; n < 4; ++n) v[n] = n0 + n < a.N ? p[n] : from_f32<T>(0.f);
         }
+        return w;
     };
-    int slot = 0;
-    for (int e = e0; e < e1; e += 2, slot = (slot + 1) % kPairs, state += 2 * next) {
-        fetch(e + 2 * (kPairs - 1), (slot + kPairs - 1) % kPairs);
-        float h[2][4] = {}, b[2][4] = {}, cc[2][4] = {}, x[LEFT] = {}, z[LEFT] = {}, d[LEFT] = {}, y[2] = {};
-        bool empty[2];
+    const auto floats = [](const Four &w, float (&v)[4]) {
+        Vec<T> r;
+        float f[Vec<T>::N];
+        if constexpr (sizeof(T) == 4) r.raw = w;
+        else r.raw = make_uint4(w.x, w.y, 0, 0);
+        r.get(f);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) v[n] = f[n];
+    };
+    // of the two envs that come next
+    Four rb[2], rc[2];
+    T rx[LEFT], rt[LEFT], rz[LEFT];
+    bool empty[2];
+    const auto read = [&](int e) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             if (!on || e + k >= e1) break;
             empty[k] = a.done && a.done[e + k];
-            load_four(static_cast<const T *>(a.B) + (e + k) * a.ldb + at, b[k]);
-            load_four(static_cast<const T *>(a.C) + (e + k) * a.ldc + at, cc[k]);
-            if (!whole && !empty[k]) load_row<4>(state + k * next, a.N, n0, h[k]);
+            rb[k] = load_four(static_cast<const T *>(a.B) + (e + k) * a.ldb + at);
+            rc[k] = load_four(static_cast<const T *>(a.C) + (e + k) * a.ldc + at);
         }
 #pragma unroll
         for (int i = 0; i < LEFT; ++i) {
             const int k = e + first + i;
             if (!on || k >= e1) break;
-            x[i] = to_f32(static_cast<const T *>(a.x)[k * a.ldx + c]);
-            d[i] = to_f32(static_cast<const T *>(a.dt)[k * a.lddt + c]) + bias;
-            if (a.softplus) d[i] = softplus_fast(d[i]);
-            if (a.z) z[i] = to_f32(static_cast<const T *>(a.z)[k * a.ldz + c]);
+            rx[i] = static_cast<const T *>(a.x)[k * a.ldx + c];
+            rt[i] = static_cast<const T *>(a.dt)[k * a.lddt + c];
+            if (a.z) rz[i] = static_cast<const T *>(a.z)[k * a.ldz + c];
+        }
+    };
+    read(e0);
+    int slot = 0;
+    for (int e = e0; e < e1; e += 2, slot = (slot + 1) % kPairs, state += 2 * next) {
+        fetch(e + 2 * (kPairs - 1), (slot + kPairs - 1) % kPairs);
+        float h[2][4] = {}, b[2][4] = {}, cc[2][4] = {}, x[LEFT] = {}, z[LEFT] = {}, d[LEFT] = {}, y[2] = {};
+        bool start[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (!on || e + k >= e1) break;
+            start[k] = empty[k];
+            floats(rb[k], b[k]);
+            floats(rc[k], cc[k]);
+            if (!whole && !start[k]) load_row<4>(state + k * next, a.N, n0, h[k]);
+        }
+#pragma unroll
+        for (int i = 0; i < LEFT; ++i) {
+            if (!on || e + first + i >= e1) break;
+            x[i] = to_f32(rx[i]);
+            d[i] = to_f32(rt[i]) + bias;
+            if (a.z) z[i] = to_f32(rz[i]);
+        }
+        read(e + 2);
+        if (a.softplus) {
+#pragma unroll
+            for (int i = 0; i < LEFT; ++i) d[i] = softplus_fast(d[i]);
         }
         asm volatile("cp.async.wait_group %0;" ::"n"(kPairs - 1) : "memory");
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const float dk = __shfl_sync(0xffffffffu, d[k % LEFT], k / LEFT * EACH, NL), uk = __shfl_sync(0xffffffffu, d[k % LEFT] * x[k % LEFT], k / LEFT * EACH, NL);
             if (!on || e + k >= e1) continue;
-            if (ahead && !empty[k]) {
+            if (ahead && !start[k]) {
                 const float4 f = ring[slot][k][threadIdx.x];
                 h[k][0] = f.x, h[k][1] = f.y, h[k][2] = f.z, h[k][3] = f.w;
             }
