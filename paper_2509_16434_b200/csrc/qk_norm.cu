@@ -1,8 +1,8 @@
 // Norms of queries and keys for each head with the rotation by their positions, and the gradients.
 //
 // Angles in 64 bits down to the fraction of a turn, which fits 32; the rest in 32 bits; what is stored is rounded once.  Everything is read and
-// written once: bound by memory.  A warp takes the heads of a row side by side, a few lanes each, two vectors of 16 bytes a lane such that a
-// lane has both elements of every pair it turns; the row's cosines and sines are made once for all its heads, d / 64 of them a lane.
+// written once: bound by memory.  A warp takes the heads of a row side by side, a few lanes each, two vectors of four elements a lane such that a
+// lane has both elements of every pair it turns (vectors of 16 bytes in 16 bits: half as many warps an SM, 44 us for the larger case below); the row's cosines and sines are made once for all its heads, d / 64 of them a lane.
 #include "elem.cuh"
 #include "pair32.cuh"
 #include "param_sum.cuh"
@@ -20,15 +20,24 @@ struct QkArgs {
     float *part;  // shares of the gradients of gamma, [blocks][2][d]
     long long ldq, ldk, ldqo, ldko;
     int rows, heads, kv, d, pairs, interleaved;
-    float eps;
+    float eps, inv_d;
 };
 
-// cos and sin of pos * freq.
-__device__ __forceinline__ float2 turn(int pos, double freq) {
-    const double t = (double)pos * freq * 0.15915494309189535;  // turns
+constexpr double kTurn = 0.15915494309189535;  // of a radian
+// cos and sin of the angle pos * f, f in turns.
+__device__ __forceinline__ float2 turn(int pos, double f) {
+    const double t = (double)pos * f;
     float2 r;
     sincospif((float)(2. * (t - rint(t))), &r.y, &r.x);
     return r;
+}
+// 1 / sqrt(sum / d + eps): the hardware's approximation and a step of Newton's method, which leaves a unit of the last place.
+__device__ __forceinline__ float root(const QkArgs &a, float sum) {
+    const float m = fmaf(sum, a.inv_d, a.eps);
+    float r;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(m));
+    const float h = 0.5f * m * r;
+    return m > 3e38f ? r : fmaf(r, fmaf(-h, r, 0.5f), r);  // an infinite sum makes zeros
 }
 
 // Where element i of a head stands in the rotation: its pair, and which of the two it is; pair -1: it stays.
@@ -63,14 +72,14 @@ __global__ void __launch_bounds__(256) qk_fwd_any_kernel(QkArgs a) {
             n[i] = to_f32(x[i]);
             s = fmaf(n[i], n[i], s);
         }
-        const float r = 1.f / sqrtf(warp_sum(s) / (float)a.d + a.eps);
+        const float r = root(a, warp_sum(s));
         for (int i = lane; i < a.d; i += 32) n[i] *= r * (gamma ? gamma[i] : 1.f);
         __syncwarp();
         for (int i = lane; i < a.d; i += 32) {
             const Place p = place(a, i);
             float v = n[i];
             if (p.pair >= 0) {
-                const float2 t = turn(a.pos[row], a.freq[p.pair]);
+                const float2 t = turn(a.pos[row], a.freq[p.pair] * kTurn);
                 v = p.second ? fmaf(n[p.other], t.y, v * t.x) : fmaf(-n[p.other], t.y, v * t.x);
             }
             y[i] = from_f32<T>(v);
@@ -102,7 +111,7 @@ __global__ void __launch_bounds__(256) qk_bwd_any_kernel(QkArgs a) {
             if (i < a.d) n[i] = to_f32(dy[i]);
             s = fmaf(v[j], v[j], s);
         }
-        const float r = 1.f / sqrtf(warp_sum(s) / (float)a.d + a.eps);
+        const float r = root(a, warp_sum(s));
         __syncwarp();
         float g[kMaxD / 32], dot = 0.f;
 #pragma unroll
@@ -113,7 +122,7 @@ __global__ void __launch_bounds__(256) qk_bwd_any_kernel(QkArgs a) {
             const Place p = place(a, i);
             g[j] = n[i];
             if (p.pair >= 0) {
-                const float2 t = turn(a.pos[row], a.freq[p.pair]);
+                const float2 t = turn(a.pos[row], a.freq[p.pair] * kTurn);
                 g[j] = p.second ? fmaf(-n[p.other], t.y, g[j] * t.x) : fmaf(n[p.other], t.y, g[j] * t.x);
             }
             v[j] *= r;
@@ -121,7 +130,7 @@ __global__ void __launch_bounds__(256) qk_bwd_any_kernel(QkArgs a) {
             g[j] *= gamma ? gamma[i] : 1.f;
             dot = fmaf(g[j], v[j], dot);
         }
-        dot = warp_sum(dot) / (float)a.d;
+        dot = warp_sum(dot) * a.inv_d;
 #pragma unroll
         for (int j = 0; j < kMaxD / 32; ++j) {
             const int i = lane + 32 * j;
@@ -145,6 +154,12 @@ __global__ void __launch_bounds__(256) qk_bwd_any_kernel(QkArgs a) {
 
 // ---- rows of aligned vectors ----
 
+// Four elements: what a lane has of a head is two times four.
+template <typename T>
+struct Four {
+    using Word = std::conditional_t<sizeof(T) == 4, uint4, uint2>;
+};
+
 // How the warps go about it: lanes of a head (a power of two, of which `slots` hold something), the parts that a row's heads are dealt to, heads
 // of a part.
 struct Lanes {
@@ -155,14 +170,20 @@ struct Lanes {
 // The row's turns, and where a lane's two vectors stand in a head.
 template <typename T, bool INTERLEAVED>
 struct Turns {
-    static constexpr int V = Vec<T>::N, P = V / 2;
+    static constexpr int V = 4, P = V / 2;
     int first, second;
     bool on;
-    pair32 c[P], s[P];  // of two pairs each
+    pair32 c[P], s[P], n[P];  // of two pairs each: cosines, sines, and these negative
+    double f[kMaxD / 64];     // turns a position of the pairs that a lane makes
 
     __device__ __forceinline__ Turns(const QkArgs &a, const Lanes &k) {
         const int slot = threadIdx.x % k.lanes, turned = a.pairs / V;  // slots whose vectors are turned with one another
         on = slot < k.slots;
+#pragma unroll
+        for (int i = 0; i < kMaxD / 64; ++i) {
+            const int p = threadIdx.x % 32 + 32 * i;
+            f[i] = p < a.pairs ? a.freq[p] * kTurn : 0.;
+        }
         if (INTERLEAVED) {
             first = 2 * V * slot;
             second = first + V;
@@ -179,7 +200,9 @@ struct Turns {
         __syncwarp();
         if (a.pairs > 0) {
             const int pos = a.pos[row];
-            for (int i = threadIdx.x % 32; i < a.pairs; i += 32) table[i] = turn(pos, a.freq[i]);
+#pragma unroll
+            for (int i = 0; i < kMaxD / 64; ++i)
+                if ((int)threadIdx.x % 32 + 32 * i < a.pairs) table[threadIdx.x % 32 + 32 * i] = turn(pos, f[i]);
         }
         __syncwarp();
 #pragma unroll
@@ -188,10 +211,9 @@ struct Turns {
             const int p = (INTERLEAVED ? first / 2 : first) + 2 * i;
             if (on && p < a.pairs) t = table[p];
             if (on && p + 1 < a.pairs) u = table[p + 1];
-            c[i] = pair_of(t.x, u.x), s[i] = pair_of(t.y, u.y);
+            c[i] = pair_of(t.x, u.x), s[i] = pair_of(t.y, u.y), n[i] = pair_of(-t.y, -u.y);
         }
     }
-    static __device__ __forceinline__ pair32 minus(pair32 p) { return mul2(p, pair_of(-1.f, -1.f)); }
     static __device__ __forceinline__ pair32 swap(pair32 p) {
         const float2 f = parts(p);
         return pair_of(f.y, f.x);
@@ -202,41 +224,37 @@ struct Turns {
         if constexpr (INTERLEAVED) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float2 ct = parts(c[i / 2]), st = parts(s[i / 2]);
-                const float cos = i % 2 ? ct.y : ct.x, sin = BACK ? -(i % 2 ? st.y : st.x) : i % 2 ? st.y : st.x;
-                x[i] = fma2(x[i], pair_of(cos, cos), mul2(swap(x[i]), pair_of(-sin, sin)));
+                const float2 ct = parts(c[i / 2]), st = parts(BACK ? n[i / 2] : s[i / 2]), nt = parts(BACK ? s[i / 2] : n[i / 2]);
+                x[i] = fma2(x[i], i % 2 ? pair_of(ct.y, ct.y) : pair_of(ct.x, ct.x), mul2(swap(x[i]), i % 2 ? pair_of(nt.y, st.y) : pair_of(nt.x, st.x)));
             }
         } else {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                const pair32 a = x[i], b = x[P + i], n = minus(BACK ? a : b);
-                x[i] = fma2(a, c[i], mul2(BACK ? b : n, s[i]));
-                x[P + i] = fma2(b, c[i], mul2(BACK ? n : a, s[i]));
+                const pair32 a = x[i], b = x[P + i];
+                x[i] = fma2(a, c[i], mul2(b, BACK ? s[i] : n[i]));
+                x[P + i] = fma2(b, c[i], mul2(a, BACK ? n[i] : s[i]));
             }
         }
     }
 };
 
 template <typename T>
-__device__ __forceinline__ void pairs_of(const uint4 &raw, pair32 *p) {
+__device__ __forceinline__ void pairs_of(const typename Four<T>::Word &raw, pair32 *p) {
     Vec<T> v;
     float f[Vec<T>::N];
-    v.raw = raw;
+    if constexpr (sizeof(T) == 4) v.raw = raw;
+    else v.raw = make_uint4(raw.x, raw.y, 0, 0);
     v.get(f);
-#pragma unroll
-    for (int i = 0; i < Vec<T>::N / 2; ++i) p[i] = pair_of(f[2 * i], f[2 * i + 1]);
+    p[0] = pair_of(f[0], f[1]), p[1] = pair_of(f[2], f[3]);
 }
 template <typename T>
-__device__ __forceinline__ uint4 raw_of(const pair32 *p) {
+__device__ __forceinline__ typename Four<T>::Word raw_of(const pair32 *p) {
+    const float2 a = parts(p[0]), b = parts(p[1]);
+    const float f[8] = {a.x, a.y, b.x, b.y};
     Vec<T> v;
-    float f[Vec<T>::N];
-#pragma unroll
-    for (int i = 0; i < Vec<T>::N / 2; ++i) {
-        const float2 u = parts(p[i]);
-        f[2 * i] = u.x, f[2 * i + 1] = u.y;
-    }
     v.set(f);
-    return v.raw;
+    if constexpr (sizeof(T) == 4) return v.raw;
+    else return make_uint2(v.raw.x, v.raw.y);
 }
 template <int P>
 __device__ __forceinline__ void floats_of(const float *f, pair32 *p) {
@@ -267,7 +285,8 @@ constexpr int kHeads = 4;  // of a lane's, on their way at a time
 template <typename T, bool INTERLEAVED>
 __global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
-    constexpr int V = Vec<T>::N, P = V / 2;
+    constexpr int V = 4, P = V / 2;
+    using Word = typename Four<T>::Word;
     __shared__ alignas(16) float gamma[2][kMaxD];
     __shared__ float2 tables[8][kMaxD / 2];
     stage_gamma(a, gamma);
@@ -281,15 +300,15 @@ __global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
         T *qo = static_cast<T *>(a.qo) + row * a.ldqo, *ko = static_cast<T *>(a.ko) + row * a.ldko - (long long)a.heads * a.d;
         bool made = false;
         for (int h = h0 + group; h - group < h1; h += kHeads * groups) {
-            uint4 raw[kHeads][2];
+            Word raw[kHeads][2];
 #pragma unroll
             for (int i = 0; i < kHeads; ++i) {
                 const int n = h + i * groups;
-                raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
+                raw[i][0] = raw[i][1] = Word{};
                 if (n < h1 && turns.on) {
                     const T *x = (n < a.heads ? q : key) + (long long)n * a.d;
-                    raw[i][0] = *reinterpret_cast<const uint4 *>(x + turns.first);
-                    raw[i][1] = *reinterpret_cast<const uint4 *>(x + turns.second);
+                    raw[i][0] = *reinterpret_cast<const Word *>(x + turns.first);
+                    raw[i][1] = *reinterpret_cast<const Word *>(x + turns.second);
                 }
             }
             if (!made) turns.row(a, row, tables[threadIdx.x / 32]);
@@ -304,7 +323,7 @@ __global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) s = fma2(x[j], x[j], s);
                 const float2 f = parts(s);
-                const float r = 1.f / sqrtf(lanes_sum(f.x + f.y, k.lanes) / (float)a.d + a.eps);
+                const float r = root(a, lanes_sum(f.x + f.y, k.lanes));
                 if (n >= h1 || !turns.on) continue;
                 floats_of<P>(&gamma[n >= a.heads][turns.first], g);
                 floats_of<P>(&gamma[n >= a.heads][turns.second], g + P);
@@ -313,8 +332,8 @@ __global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
                 for (int j = 0; j < V; ++j) x[j] = mul2(mul2(x[j], rr), g[j]);
                 turns.template apply<false>(x);
                 T *y = (n < a.heads ? qo : ko) + (long long)n * a.d;
-                *reinterpret_cast<uint4 *>(y + turns.first) = raw_of<T>(x);
-                *reinterpret_cast<uint4 *>(y + turns.second) = raw_of<T>(x + P);
+                *reinterpret_cast<Word *>(y + turns.first) = raw_of<T>(x);
+                *reinterpret_cast<Word *>(y + turns.second) = raw_of<T>(x + P);
             }
         }
     }
@@ -323,9 +342,10 @@ __global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
 // With n = R^T dy (turned back), g = gamma n and r = 1 / sqrt(mean x^2 + eps): dx = r g - x r^3 mean(g x), dgamma += n x r.  Both sums of a head are
 // made at once.  A warp has either queries or keys, and keeps its share of the gradient of their gamma.
 template <typename T, bool INTERLEAVED>
-__global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
+__global__ void __launch_bounds__(256, 3) qk_bwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
-    constexpr int V = Vec<T>::N, P = V / 2, U = 2;
+    constexpr int V = 4, P = V / 2, U = 2;
+    using Word = typename Four<T>::Word;
     __shared__ alignas(16) float gamma[2][kMaxD];
     __shared__ float2 tables[8][kMaxD / 2];
     __shared__ float shares[8][kMaxD];
@@ -345,17 +365,17 @@ __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
         const int h0 = (int)(item - row * parts_) * k.heads, h1 = min(heads, h0 + k.heads);
         bool made = false;
         for (int h = h0 + group; h - group < h1; h += U * groups) {
-            uint4 xr[U][2], gr[U][2];
+            Word xr[U][2], gr[U][2];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
                 const int n = h + i * groups;
-                xr[i][0] = xr[i][1] = gr[i][0] = gr[i][1] = make_uint4(0, 0, 0, 0);
+                xr[i][0] = xr[i][1] = gr[i][0] = gr[i][1] = Word{};
                 if (n < h1 && turns.on) {
                     const T *x = x0 + row * ld + (long long)n * a.d, *dy = dy0 + row * ldo + (long long)n * a.d;
-                    xr[i][0] = *reinterpret_cast<const uint4 *>(x + turns.first);
-                    xr[i][1] = *reinterpret_cast<const uint4 *>(x + turns.second);
-                    gr[i][0] = *reinterpret_cast<const uint4 *>(dy + turns.first);
-                    gr[i][1] = *reinterpret_cast<const uint4 *>(dy + turns.second);
+                    xr[i][0] = *reinterpret_cast<const Word *>(x + turns.first);
+                    xr[i][1] = *reinterpret_cast<const Word *>(x + turns.second);
+                    gr[i][0] = *reinterpret_cast<const Word *>(dy + turns.first);
+                    gr[i][1] = *reinterpret_cast<const Word *>(dy + turns.second);
                 }
             }
             if (!made) turns.row(a, row, tables[w]);
@@ -384,8 +404,8 @@ __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
                     t = fma2(mul2(g[j], x[j]), gam[j], t);
                 }
                 const float2 f = parts(s), u = parts(t);
-                const float r = 1.f / sqrtf(lanes_sum(f.x + f.y, k.lanes) / (float)a.d + a.eps);
-                const float m = -(lanes_sum(u.x + u.y, k.lanes) / (float)a.d) * r * r;
+                const float r = root(a, lanes_sum(f.x + f.y, k.lanes));
+                const float m = -lanes_sum(u.x + u.y, k.lanes) * a.inv_d * r * r;
                 if (n >= h1 || !turns.on) continue;
                 const pair32 rr = pair_of(r, r), mm = pair_of(m, m);
 #pragma unroll
@@ -394,8 +414,8 @@ __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
                     g[j] = mul2(rr, fma2(x[j], mm, mul2(g[j], gam[j])));
                 }
                 T *dx = dx0 + row * ld + (long long)n * a.d;
-                *reinterpret_cast<uint4 *>(dx + turns.first) = raw_of<T>(g);
-                *reinterpret_cast<uint4 *>(dx + turns.second) = raw_of<T>(g + P);
+                *reinterpret_cast<Word *>(dx + turns.first) = raw_of<T>(g);
+                *reinterpret_cast<Word *>(dx + turns.second) = raw_of<T>(g + P);
             }
         }
     }
@@ -455,6 +475,7 @@ QkArgs args(const ppo_qk_norm_desc *d, float eps, const void *q, const void *k, 
     a.pairs = d->pairs;
     a.interleaved = d->interleaved;
     a.eps = eps;
+    a.inv_d = 1.f / (float)d->d;
     return a;
 }
 
@@ -467,14 +488,14 @@ int any_blocks(const ppo_qk_norm_desc *d) { return blocks_of((long long)d->rows 
 
 // Whether every row is made of whole, aligned vectors, and pairs lie in two of a lane's.
 bool vectors(const ppo_qk_norm_desc *d, std::initializer_list<const void *> ps) {
-    const int V = 16 / (int)elem_bytes(d->dtype);
+    constexpr int V = 4;
     return d->d % (2 * V) == 0 && (d->interleaved || d->pairs % V == 0) && d->ldq % V == 0 && d->ldk % V == 0 && d->ldqo % V == 0 && d->ldko % V == 0 &&
-           !misaligned(ps, 16);
+           !misaligned(ps, V * elem_bytes(d->dtype));
 }
 // Rows are taken whole, as long as they give every SM `warps` warps; fewer rows are dealt out by as many heads as the lanes of a warp take at once.
 Lanes lanes_of(const ppo_qk_norm_desc *d, int warps) {
-    const int V = 16 / (int)elem_bytes(d->dtype), all = d->heads + d->kv_heads;
-    Lanes k = {1, d->d / (2 * V), 1, all};
+    const int all = d->heads + d->kv_heads;
+    Lanes k = {1, d->d / 8, 1, all};
     while (k.lanes < k.slots) k.lanes *= 2;
     const int side = 32 / k.lanes, most = ppo_cdiv(all, side);
     long long want = ((long long)warps * 148 + d->rows - 1) / d->rows;
@@ -508,7 +529,7 @@ extern "C" int ppo_qk_norm_rotate_fwd(const ppo_qk_norm_desc *d, float eps, cons
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (!vectors(d, {q, k, q_out, k_out}))
         return with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_fwd_any_kernel<decltype(t)>, dim3(any_blocks(d)), dim3(256), 0, st, a); });
-    const Lanes l = lanes_of(d, 16);
+    const Lanes l = lanes_of(d, 32);
     return with_order(d, [&](auto t, auto order) {
         return ppo_launch(qk_fwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks_of((long long)d->rows * l.parts, 8)), dim3(256), 0, st, a, l);
     });
@@ -534,8 +555,8 @@ extern "C" int ppo_qk_norm_rotate_bwd(const ppo_qk_norm_desc *d, float eps, cons
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int blocks = any_blocks(d);
     if (vectors(d, {q, k, dq_out, dk_out, dq, dk})) {
-        const Lanes l = lanes_of(d, 16);
-        blocks = blocks_of((long long)d->rows * l.parts, 2);
+        const Lanes l = lanes_of(d, 32);
+        blocks = blocks_of((long long)d->rows * l.parts, 3);
         PPO_TRY(with_order(d, [&](auto t, auto order) {
             return ppo_launch(qk_bwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks), dim3(256), 0, st, a, l);
         }));

@@ -34,6 +34,8 @@ struct ScanArgs {
     // of the state that is left); what its step sizes add up to for each channel, and whether a flag is set in it.
     float *seg, *back, *sum;
     int *cut;
+    float *cum;     // BOTH: what the step sizes from the start of a segment add up to in front of every 16th step, [ceil(T / 16)][Be][channels]
+    int *cum_cut;  // and whether a flag is set among them, [ceil(T / 16)][Be]
     float *mark;  // the states in front of every 16th step, [ceil(T / 16)][Be][channels][NP] (up to 16 steps: none)
     float *few;   // shares of the gradients of B and C, [group_tiles][T * Be][groups][2][NP]
     float *part;  // shares of the gradients of A, D and dt_bias, [parts][channels * (N + 2)]
@@ -236,7 +238,7 @@ __device__ __forceinline__ void end_of(const ScanArgs &a, int NP, const Work &w,
 enum Mode {
     OUTPUT,  // y and the state that is left
     ENDS,    // what each segment ends with
-    BOTH,    // that, and the gradients it hands to the steps in front
+    BOTH,    // that, the gradients it hands to the steps in front, and the states in front of every kSteps-th step (starting from zeros)
     MARKS    // the states in front of every kSteps-th step
 };
 
@@ -382,13 +384,18 @@ __global__ void __launch_bounds__(kThreads, 4) scan_kernel(ScanArgs a) {
         B += kSteps * sb;
         C += kSteps * sc;
         if (rows > kSteps) few.fetch(B, C, sb, sc, rows - kSteps, a.N);
-        if constexpr (MODE == MARKS) {
-            float *to = a.mark + (((long long)(t / kSteps) * a.Be + w.e) * a.channels + c) * NP + n0;
+        if constexpr (MODE == MARKS || MODE == BOTH) {
+            const long long at = (long long)(t / kSteps) * a.Be + w.e;
+            float *to = a.mark + (at * a.channels + c) * NP + n0;
 #pragma unroll
             for (int j = 0; j < CPT; ++j)
 #pragma unroll
                 for (int i = 0; i < P; i += 2)
                     if (on) *reinterpret_cast<ulonglong2 *>(to + j * NP + 2 * i) = make_ulonglong2(h[j][i], h[j][i + 1]);
+            if constexpr (MODE == BOTH) {
+                if (on && ln == 0) a.cum[at * a.channels + c] = parts(total).x;
+                if (threadIdx.x == 0 && w.tile == 0) a.cum_cut[at] = cut;
+            }
         }
 #pragma unroll 1
         for (int s = 0; s < kSteps && s < rows; s += 4) {
@@ -487,6 +494,37 @@ __global__ void __launch_bounds__(kThreads, 4) scan_kernel(ScanArgs a) {
     }
     if constexpr (MODE == ENDS || MODE == BOTH) {
         if (threadIdx.x == 0 && w.tile == 0) a.cut[at] = cut;
+    }
+}
+
+// The states in front of every kSteps-th step of the segments but the first, from those that started from zeros: what the segment starts from, taken
+// through the steps in front of them, is added.  A thread has four elements of a channel in one segment.
+__global__ void __launch_bounds__(256) scan_marks_kernel(ScanArgs a, int NP) {
+    grid_wait();
+    const int quads = NP / 4;
+    const long long all = (long long)(a.nseg - 1) * a.Be * a.channels * quads, id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= all) return;
+    const long long chan = id / quads, item = chan / a.channels;
+    const int n0 = (int)(id - chan * quads) * 4, c = (int)(chan - item * a.channels);
+    Work w = {};
+    w.seg = (int)(item / a.Be) + 1;
+    w.e = (int)(item % a.Be);
+    w.t0 = w.seg * a.len;
+    w.t1 = min(a.T, w.t0 + a.len);
+    float A[4], h[4], f[4];
+    load_row<4>(a.A + (long long)c * a.N, a.N, n0, A);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) A[n] *= kLog2e;
+    start_of<4>(a, NP, w, c, n0, A, h);
+    for (int t = w.t0; t < w.t1; t += kSteps) {
+        const long long at = (long long)(t / kSteps) * a.Be + w.e;
+        if (a.cum_cut[at]) break;
+        const float d = a.cum[at * a.channels + c];
+        float *mark = a.mark + (at * a.channels + c) * NP;
+        load_row<4>(mark, NP, n0, f);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) f[n] = fmaf(exp2_fast(d * A[n]), h[n], f[n]);
+        store_row<4>(mark, NP, n0, f);
     }
 }
 
@@ -1084,7 +1122,7 @@ bool misaligned(std::initializer_list<const void *> ps, size_t a) {
 struct Plan {
     int NL, NP, len, nseg, parts;  // NL: lanes of a channel forwards
     int tiles, group_tiles;        // backwards
-    size_t seg, sums, mark, few, part;  // floats of each area of the workspace
+    size_t seg, sums, mark, cum, few, part;  // floats of each area of the workspace
 };
 Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     Plan p = {};
@@ -1110,6 +1148,7 @@ Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     }
     if (bwd) {
         p.mark = d->T > kSteps ? ppo_cdiv(d->T, kSteps) * held : 0;
+        p.cum = p.nseg > 1 ? up((size_t)ppo_cdiv(d->T, kSteps) * d->Be * (d->channels + 1)) : 0;
         p.few = (size_t)d->T * d->Be * p.tiles * 2 * p.NP;
         const long long items = (long long)d->Be * p.nseg;
         p.parts = (int)(items < slices ? items : slices);
@@ -1197,7 +1236,7 @@ int pass(const ScanArgs &a, bool two, int segs, cudaStream_t st) {
 extern "C" size_t ppo_selective_scan_workspace_bytes(const ppo_selective_scan_desc *d, int backward) {
     if (check(d) != PPO_OK) return 0;
     const Plan p = plan_of(d, backward != 0);
-    return ((backward ? 2 : 1) * p.seg + p.sums + p.mark + p.few + p.part) * sizeof(float);
+    return ((backward ? 2 : 1) * p.seg + p.sums + p.mark + p.cum + p.few + p.part) * sizeof(float);
 }
 
 extern "C" int ppo_selective_scan_fwd(const ppo_selective_scan_desc *d, const void *x, const void *dt, const float *A, const void *B, const void *C,
@@ -1255,7 +1294,9 @@ extern "C" int ppo_selective_scan_bwd(const ppo_selective_scan_desc *d, const vo
     a.seg = static_cast<float *>(workspace);
     a.back = a.seg + p.seg;
     a.mark = a.back + p.seg;
-    a.few = a.mark + p.mark;
+    a.cum = a.mark + p.mark;
+    a.cum_cut = reinterpret_cast<int *>(a.cum + (size_t)ppo_cdiv(d->T, kSteps) * d->Be * d->channels);
+    a.few = a.cum + p.cum;
     const bool params = dA || dD || ddt_bias;
     a.part = params ? a.few + p.few : nullptr;
     a.sum = a.few + p.few + p.part;
@@ -1265,8 +1306,13 @@ extern "C" int ppo_selective_scan_bwd(const ppo_selective_scan_desc *d, const vo
     PPO_TRY(with_lanes(d, p, [&](auto t, auto nl) -> int {
         using T = decltype(t);
         constexpr int NL = decltype(nl)::value;
-        if (p.nseg > 1) PPO_TRY((pass_of<T, NL, 1, BOTH>(a, p.nseg, st)));
-        if (d->T > kSteps) PPO_TRY((pass<T, NL, MARKS>(a, two, p.nseg, st)));
+        if (p.nseg > 1) {
+            PPO_TRY((pass_of<T, NL, 1, BOTH>(a, p.nseg, st)));
+            const long long quads = (long long)(p.nseg - 1) * d->Be * d->channels * (p.NP / 4);
+            PPO_TRY(ppo_launch(scan_marks_kernel, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a, p.NP));
+        } else if (d->T > kSteps) {
+            PPO_TRY((pass<T, NL, MARKS>(a, two, 1, st)));
+        }
         PPO_TRY((vec ? back_launch<T, 8 * NL, true>(a, st) : back_launch<T, 8 * NL, false>(a, st)));
         const long long few = (long long)d->T * d->Be * d->groups * 2 * p.NP;
         return ppo_launch(scan_few_kernel<T, 16 * NL>, dim3((unsigned)((few + 255) / 256)), dim3(256), 0, st, a);
