@@ -152,7 +152,13 @@ __device__ __forceinline__ void params(const ConvArgs &a, int c, pair32 (&w)[W][
 #pragma unroll
         for (int i = 0; i < V * W; ++i) f[i] = from[i];
     }
-    if (a.bias) {
+    if (V % 4 == 0 && a.bias && (reinterpret_cast<uintptr_t>(a.bias) & 15) == 0) {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+            const float4 v = reinterpret_cast<const float4 *>(a.bias + c)[i];
+            g[4 * i] = v.x, g[4 * i + 1] = v.y, g[4 * i + 2] = v.z, g[4 * i + 3] = v.w;
+        }
+    } else if (a.bias) {
 #pragma unroll
         for (int v = 0; v < V; ++v) g[v] = a.bias[c + v];
     }
@@ -261,21 +267,25 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs a, int env
     const int c = (int)(id - item * cols) * V;
     if (item * envs >= a.Be) return;
     const int e0 = (int)item * envs, e1 = min(a.Be, e0 + envs);
-    pair32 w[W][P], b[P];
-    params<W, V>(a, c, w, b);
-    for (int e = e0; e < e1; e += 2) {
-        Raw<T, V> r[2][W];
-        bool start[2];
-        T *state[2];
+    Raw<T, V> r[2][W];
+    bool start[2];
+    T *const states = static_cast<T *>(a.state_out) + c;
+    const long long each = (long long)(W - 1) * a.C;
+    const auto read = [&](int e) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             if (e + k >= e1) break;
-            state[k] = static_cast<T *>(a.state_out) + (long long)(e + k) * (W - 1) * a.C + c;
             start[k] = a.done && a.done[e + k];
             r[k][W - 1].load(static_cast<const T *>(a.x) + (e + k) * a.ldx + c);
 #pragma unroll
-            for (int i = 0; i < W - 1; ++i) r[k][i].load(state[k] + (long long)i * a.C);
+            for (int i = 0; i < W - 1; ++i) r[k][i].load(states + (e + k) * each + (long long)i * a.C);
         }
+    };
+    read(e0);
+    pair32 w[W][P], b[P];
+    params<W, V>(a, c, w, b);
+    for (int e = e0; e < e1; e += 2) {
+        if (e > e0) read(e);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             if (e + k >= e1) break;
@@ -288,7 +298,7 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs a, int env
                 r[k][i].get(v);
 #pragma unroll
                 for (int p = 0; p < P; ++p) s[p] = fma2(w[i][p], v[p], s[p]);
-                if (i > 0) r[k][i].store(state[k] + (long long)(i - 1) * a.C);
+                if (i > 0) r[k][i].store(states + (e + k) * each + (long long)(i - 1) * a.C);
             }
             activate(s, a.act);
             r[k][0].set(s);
@@ -603,7 +613,7 @@ extern "C" int ppo_causal_conv_step(const ppo_causal_conv_desc *d, const void *x
     a.state_out = state;
     const int V = 16 / (int)elem_bytes(d->dtype);
     const bool vec = vectors(d, V, {x, y, state});
-    const long long cols = vec ? d->C / V : d->C, most = cols * d->Be / (148 * 512);  // envs of a thread: as many as leave every SM 512 threads
+    const long long cols = vec ? d->C / V : d->C, most = cols * d->Be / (148 * 256);  // envs of a thread: as many as leave every SM 256 threads
     const int envs = most < 2 ? 1 : most > 8 ? 8 : (int)most / 2 * 2;
     const long long blocks = (cols * ppo_cdiv(d->Be, envs) + kThreads - 1) / kThreads;
     if (blocks > 0x7fffffffll) return PPO_ERR_UNSUPPORTED;

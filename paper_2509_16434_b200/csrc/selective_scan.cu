@@ -972,46 +972,52 @@ __global__ void __launch_bounds__(256) scan_few_kernel(ScanArgs a) {
     else static_cast<T *>(a.dC)[row * a.ldc + group * a.N + n] = from_f32<T>(sum);
 }
 
-// One step, the state in place: NL lanes share a channel, four elements each, and take two envs at a time, whose step sizes and outputs they
-// share out among them.  Bound by memory, since the states go through once: a thread copies its own of the next envs ahead into shared memory.
-constexpr int kPairs = 4;  // pairs of envs in the ring
+// One step, the state in place: NL lanes share four channels of a group, four elements of each, whose step sizes and outputs they share out among
+// them.  Bound by memory, since the states go through once: a thread copies its own of the next envs ahead into shared memory, and reads
+// the next env's rows while it works on this one's.
+constexpr int kAhead = 3;  // envs in the ring
 
 template <typename T, int NL>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 3) scan_step_kernel(ScanArgs a, int envs) {
+__global__ void __launch_bounds__(256, 3) scan_step_kernel(ScanArgs a, int envs) {
     grid_wait();
-    constexpr int CHANNELS = 256 / NL, LEFT = NL >= 2 ? 1 : 2, EACH = NL >= 2 ? NL / 2 : 1;  // envs of a lane; lanes that have the same one
-    __shared__ float4 ring[kPairs][2][256];
-    const int cols = (a.channels + CHANNELS - 1) / CHANNELS, c = blockIdx.x % cols * CHANNELS + threadIdx.x / NL, ln = threadIdx.x % NL, n0 = ln * 4;
-    const int e0 = blockIdx.x / cols * envs, e1 = min(a.Be, e0 + envs), first = ln / EACH * LEFT;
-    const bool on = c < a.channels, whole = a.N % 4 == 0, ahead = whole && on && n0 < a.N;
+    constexpr int CH = 256 / NL, LEFT = NL >= 4 ? 1 : 4 / NL, EACH = NL >= 4 ? NL / 4 : 1;  // channels side by side; of a lane's own; lanes of one
+    extern __shared__ float4 ring[][4][256];
+    const int cols = (a.per + 4 * CH - 1) / (4 * CH), col = blockIdx.x % (cols * a.groups), group = col / cols;
+    const int c = group * a.per + col % cols * 4 * CH + threadIdx.x / NL, end = (group + 1) * a.per, ln = threadIdx.x % NL, n0 = ln * 4;
+    const int e0 = blockIdx.x / (cols * a.groups) * envs, e1 = min(a.Be, e0 + envs), first = ln / EACH * LEFT;
+    const bool whole = a.N % 4 == 0, ahead = whole && n0 < a.N;
     const bool few = whole && ((a.ldb | a.ldc) & 3) == 0 && ((reinterpret_cast<uintptr_t>(a.B) | reinterpret_cast<uintptr_t>(a.C)) & (4 * sizeof(T) - 1)) == 0;
     const long long next = (long long)a.channels * a.N;
-    float *state = a.state_out + ((long long)e0 * a.channels + c) * a.N;
-    const auto fetch = [&](int e, int slot) {
+    const int apart = CH * a.N;  // from one of the four channels to the next
+    // of the envs that are copied ahead, read, and written next
+    float *state = a.state_out + ((long long)e0 * a.channels + c) * a.N + n0;
+    const float *to_copy = state;
+    const T *B = static_cast<const T *>(a.B) + e0 * a.ldb + group * a.N + n0, *C = static_cast<const T *>(a.C) + e0 * a.ldc + group * a.N + n0;
+    const int own = c + first * CH;  // the first of the channels that are this lane's
+    const T *xp = static_cast<const T *>(a.x) + e0 * a.ldx + own, *tp = static_cast<const T *>(a.dt) + e0 * a.lddt + own;
+    const T *zp = static_cast<const T *>(a.z) + e0 * a.ldz + own;
+    T *yp = static_cast<T *>(a.y) + e0 * a.ldy + own;
+    const uint8_t *done = a.done + e0;
+    int copied = e0, slot_to = 0;
+    const auto fetch = [&] {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (ahead && e + k < e1) {
-                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&ring[slot][k][threadIdx.x]);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(a.state_out + ((long long)(e + k) * a.channels + c) * a.N + n0) : "memory");
+        for (int j = 0; j < 4; ++j)
+            if (ahead && copied < e1 && c + j * CH < end) {
+                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&ring[slot_to][j][threadIdx.x]);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(to_copy + j * apart) : "memory");
             }
         asm volatile("cp.async.commit_group;" ::: "memory");
+        ++copied;
+        to_copy += next;
+        slot_to = slot_to == kAhead - 1 ? 0 : slot_to + 1;
     };
 #pragma unroll
-    for (int i = 0; i < kPairs - 1; ++i) fetch(e0 + 2 * i, i);
-    float A[4] = {}, D = 0.f, bias = 0.f;
-    const int at = on ? c / a.per * a.N + n0 : 0;
-    if (on) {
-        load_row<4>(a.A + (long long)c * a.N, a.N, n0, A);
-#pragma unroll
-        for (int n = 0; n < 4; ++n) A[n] *= kLog2e;
-        if (a.D) D = a.D[c];
-        if (a.bias) bias = a.bias[c];
-    }
+    for (int i = 0; i < kAhead - 1; ++i) fetch();
     using Four = std::conditional_t<sizeof(T) == 4, uint4, uint2>;
     const auto load_four = [&](const T *p) {
-        Four w;
-        if (few && n0 < a.N) {
-            w = *reinterpret_cast<const Four *>(p);
+        Four w = {};
+        if (few) {
+            if (n0 < a.N) w = *reinterpret_cast<const Four *>(p);
         } else {
             T *v = reinterpret_cast<T *>(&w);
 #pragma unroll
@@ -1028,77 +1034,87 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 3) scan_step_kernel(
 #pragma unroll
         for (int n = 0; n < 4; ++n) v[n] = f[n];
     };
-    // of the two envs that come next
-    Four rb[2], rc[2];
+    Four rb, rc;
     T rx[LEFT], rt[LEFT], rz[LEFT];
-    bool empty[2];
+    bool empty = false;
     const auto read = [&](int e) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (!on || e + k >= e1) break;
-            empty[k] = a.done && a.done[e + k];
-            rb[k] = load_four(static_cast<const T *>(a.B) + (e + k) * a.ldb + at);
-            rc[k] = load_four(static_cast<const T *>(a.C) + (e + k) * a.ldc + at);
-        }
+        if (e >= e1) return;
+        empty = a.done && *done;
+        rb = load_four(B);
+        rc = load_four(C);
 #pragma unroll
         for (int i = 0; i < LEFT; ++i) {
-            const int k = e + first + i;
-            if (!on || k >= e1) break;
-            rx[i] = static_cast<const T *>(a.x)[k * a.ldx + c];
-            rt[i] = static_cast<const T *>(a.dt)[k * a.lddt + c];
-            if (a.z) rz[i] = static_cast<const T *>(a.z)[k * a.ldz + c];
+            if (own + i * CH >= end) break;
+            rx[i] = xp[i * CH];
+            rt[i] = tp[i * CH];
+            if (a.z) rz[i] = zp[i * CH];
         }
+        B += a.ldb, C += a.ldc, xp += a.ldx, tp += a.lddt, zp += a.ldz, ++done;
     };
     read(e0);
-    int slot = 0;
-    for (int e = e0; e < e1; e += 2, slot = (slot + 1) % kPairs, state += 2 * next) {
-        fetch(e + 2 * (kPairs - 1), (slot + kPairs - 1) % kPairs);
-        float h[2][4] = {}, b[2][4] = {}, cc[2][4] = {}, x[LEFT] = {}, z[LEFT] = {}, d[LEFT] = {}, y[2] = {};
-        bool start[2];
+    float A[4][4], D[LEFT], bias[LEFT];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (!on || e + k >= e1) break;
-            start[k] = empty[k];
-            floats(rb[k], b[k]);
-            floats(rc[k], cc[k]);
-            if (!whole && !start[k]) load_row<4>(state + k * next, a.N, n0, h[k]);
-        }
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) A[j][n] = 0.f;
+        if (c + j * CH < end) load_row<4>(a.A + (long long)(c + j * CH) * a.N, a.N, n0, A[j]);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) A[j][n] *= kLog2e;
+    }
+#pragma unroll
+    for (int i = 0; i < LEFT; ++i) {
+        D[i] = a.D && own + i * CH < end ? a.D[own + i * CH] : 0.f;
+        bias[i] = a.bias && own + i * CH < end ? a.bias[own + i * CH] : 0.f;
+    }
+    int slot = 0;
+    for (int e = e0; e < e1; ++e, slot = slot == kAhead - 1 ? 0 : slot + 1, state += next, yp += a.ldy) {
+        fetch();
+        float b[4], cc[4], x[LEFT] = {}, z[LEFT] = {}, d[LEFT] = {}, y[4];
+        const bool start = empty;
+        floats(rb, b);
+        floats(rc, cc);
 #pragma unroll
         for (int i = 0; i < LEFT; ++i) {
-            if (!on || e + first + i >= e1) break;
+            if (own + i * CH >= end) break;
             x[i] = to_f32(rx[i]);
-            d[i] = to_f32(rt[i]) + bias;
+            d[i] = to_f32(rt[i]) + bias[i];
             if (a.z) z[i] = to_f32(rz[i]);
         }
-        read(e + 2);
+        read(e + 1);
         if (a.softplus) {
 #pragma unroll
             for (int i = 0; i < LEFT; ++i) d[i] = softplus_fast(d[i]);
         }
-        asm volatile("cp.async.wait_group %0;" ::"n"(kPairs - 1) : "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float dk = __shfl_sync(0xffffffffu, d[k % LEFT], k / LEFT * EACH, NL), uk = __shfl_sync(0xffffffffu, d[k % LEFT] * x[k % LEFT], k / LEFT * EACH, NL);
-            if (!on || e + k >= e1) continue;
-            if (ahead && !start[k]) {
-                const float4 f = ring[slot][k][threadIdx.x];
-                h[k][0] = f.x, h[k][1] = f.y, h[k][2] = f.z, h[k][3] = f.w;
+        for (int j = 0; j < 4; ++j) {
+            const float dj = __shfl_sync(0xffffffffu, d[j % LEFT], j / LEFT * EACH, NL), uj = __shfl_sync(0xffffffffu, d[j % LEFT] * x[j % LEFT], j / LEFT * EACH, NL);
+            float h[4] = {};
+            y[j] = 0.f;
+            if (c + j * CH >= end) continue;
+            if (!start) {
+                if (ahead) {
+                    const float4 f = ring[slot][j][threadIdx.x];
+                    h[0] = f.x, h[1] = f.y, h[2] = f.z, h[3] = f.w;
+                } else if (!whole) {
+                    load_row<4>(state - n0 + j * apart, a.N, n0, h);
+                }
             }
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                h[k][n] = fmaf(exp2_fast(fmaf(dk, A[n], kShift)), h[k][n], uk * b[k][n]);
-                y[k] = fmaf(cc[k][n], h[k][n], y[k]);
+                h[n] = fmaf(exp2_fast(fmaf(dj, A[j][n], kShift)), h[n], uj * b[n]);
+                y[j] = fmaf(cc[n], h[n], y[j]);
             }
-            store_row<4>(state + k * next, a.N, n0, h[k]);
+            if (ahead) *reinterpret_cast<float4 *>(state + j * apart) = make_float4(h[0], h[1], h[2], h[3]);
+            else if (!whole) store_row<4>(state - n0 + j * apart, a.N, n0, h);
         }
-        spread_sum<2, NL, 1>(y, ln);
+        spread_sum<4, NL, 1>(y, ln);
 #pragma unroll
         for (int i = 0; i < LEFT; ++i) {
-            const int k = e + first + i;
-            if (!on || k >= e1 || ln % EACH != 0) break;
-            float v = a.D ? fmaf(D, x[i], y[i]) : y[i];
+            if (own + i * CH >= end || ln % EACH != 0) break;
+            float v = a.D ? fmaf(D[i], x[i], y[i]) : y[i];
             if (a.z) v *= z[i] * sigmoid_fast(z[i]);
-            static_cast<T *>(a.y)[k * a.ldy + c] = from_f32<T>(v);
+            yp[i * CH] = from_f32<T>(v);
         }
     }
 }
@@ -1334,10 +1350,14 @@ extern "C" int ppo_selective_scan_step(const ppo_selective_scan_desc *d, const v
         using T = decltype(t);
         const auto run = [&](auto nl) -> int {
             constexpr int NL = decltype(nl)::value;
-            const long long cols = ppo_cdiv(d->channels, 256 / NL);
-            // by pairs, as many envs a block as make one round of four blocks an SM
-            const int slices = cols < 4 * 148 ? (int)(4 * 148 / cols) : 1, envs = ppo_cdiv(ppo_cdiv(d->Be, slices), 2) * 2;
-            return ppo_launch(scan_step_kernel<T, NL>, dim3((unsigned)(cols * ppo_cdiv(d->Be, envs))), dim3(256), 0, static_cast<cudaStream_t>(stream), a, envs);
+            constexpr size_t smem = kAhead * 4 * 256 * sizeof(float4);
+            static PerDevice<bool> allowed;
+            PPO_TRY(ppo_once_per_device(allowed, [] { return ppo_allow_smem(scan_step_kernel<T, NL>, smem); }));
+            // as many envs a block as make one round of three blocks an SM
+            const int cols = d->groups * ppo_cdiv(d->channels / d->groups, 4 * (256 / NL)), slices = cols < 3 * 148 ? 3 * 148 / cols : 1, envs = ppo_cdiv(d->Be, slices);
+            const long long blocks = (long long)cols * ppo_cdiv(d->Be, envs);
+            if (blocks > 0x7fffffffll) return PPO_ERR_UNSUPPORTED;
+            return ppo_launch(scan_step_kernel<T, NL>, dim3((unsigned)blocks), dim3(256), smem, static_cast<cudaStream_t>(stream), a, envs);
         };
         if (d->N <= 4) return run(std::integral_constant<int, 1>{});
         if (d->N <= 8) return run(std::integral_constant<int, 2>{});
