@@ -5,10 +5,15 @@
 //
 // Forwards a thread takes a channel, or two neighbouring ones, of one env through the steps, with 16 elements of the states in registers (channels
 // with more of them belong to two or four lanes): nothing is shared but the rows of B and C, and a step's sum over the elements is the
-// thread's own.  Backwards four channels by four elements are a thread's, since there sums go over the channels as well as over the elements.
-// States, sums and arithmetic in 32 bits, packed arithmetic on two numbers at a time.
+// thread's own.  Backwards a thread has two elements of four channels, since there sums go over the channels as well as over the elements (four by
+// four, or 16 of one channel, leave an SM 8 or 12 warps: 278 and 340 us where two by four take 264).  States, sums and arithmetic in 32 bits,
+// packed arithmetic on two numbers at a time.
 //
 // Long sequences of few channels are cut into segments: a pass makes what each segment ends with, and each starts from the ends in front of it.
+//
+// Measured, channels of 16 elements in bf16: outputs of 16 steps of 256 envs of 2048 channels 67 us, 57 % of the rate of exponentials (134 MB in
+// 21 us); of 8192 steps of 4096 channels 420, the pass over the segments 178 of it at 78 % of that rate, the outputs 260 at 64 %; gradients
+// of the former 279, of 2048 steps of 2 envs of 2048 channels 392.
 #include "approx.cuh"
 #include "elem.cuh"
 #include "pair32.cuh"
@@ -46,10 +51,15 @@ struct ScanArgs {
 // the hundreds of steps that a state remembers; with its argument moved by 2e-8 the mean is within 0.2 from -0.5 to 0 (one million arguments
 // each), as near as expf's, at no cost.
 constexpr float kShift = 2e-8f;
+// A times log2(e); infinities give way to the largest numbers, so that they make 0 or infinity of any step size but 0, and 1 of that.
+__device__ __forceinline__ float scaled(float A) {
+    const float v = A * kLog2e;
+    return isinf(v) ? copysignf(3e38f, v) : v;
+}
 __device__ __forceinline__ pair32 factors(pair32 d, pair32 A) { return exp2_pair(fma2(d, A, twice(kShift))); }
 
 // Sums of V values over LANES lanes, STRIDE apart: halves go to the lanes' halves as long as there are values, lane bit by lane bit from the
-// highest; a lane is left with max(1, V / LANES) of them in v[0 ..].  index() says which.
+// highest; a lane is left with max(1, V / LANES) of them in v[0 ..], which ones spread_first says.
 template <int V, int LANES, int STRIDE>
 __device__ __forceinline__ void spread_sum(float (&v)[V], int lane) {
     if constexpr (LANES > 1) {
@@ -349,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 4) scan_kernel(ScanArgs a) {
         if (on) {
             load_row<W>(a.A + (long long)(c + j) * a.N, a.N, n0, Af);
 #pragma unroll
-            for (int n = 0; n < W; ++n) Af[n] *= kLog2e;
+            for (int n = 0; n < W; ++n) Af[n] = scaled(Af[n]);
             if (MODE == ENDS || MODE == BOTH || a.nseg == 1) {
                 if (w.seg == 0) {
                     if (a.state_in) load_row<W>(a.state_in + ((long long)w.e * a.channels + c + j) * a.N, a.N, n0, f);
@@ -405,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 4) scan_kernel(ScanArgs a) {
             if (WITH_DY) dy += 4 * sy;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                pair32 xk = 0, dk = 0, zk = 0, gk = 0;
+                pair32 xk = 0, dk = 0, zk = 0, gk = 0;  // steps behind the last one do nothing
                 if (on && s + k < rows) {
                     xk = rx[k].get();
                     dk = add2(rt[k].get(), bias);
@@ -475,6 +485,10 @@ __global__ void __launch_bounds__(kThreads, 4) scan_kernel(ScanArgs a) {
             f[2 * i] = v.x, f[2 * i + 1] = v.y;
         }
         if constexpr (MODE == OUTPUT) {
+            if (a.done && a.done[(long long)(w.t1 - 1) * a.Be + w.e]) {  // also where A is no number
+#pragma unroll
+                for (int n = 0; n < W; ++n) f[n] = 0.f;
+            }
             if (a.state_out && w.t1 == a.T) store_row<W>(a.state_out + ((long long)w.e * a.channels + c + j) * a.N, a.N, n0, f);
         }
         if constexpr (MODE == ENDS || MODE == BOTH) {
@@ -514,7 +528,7 @@ __global__ void __launch_bounds__(256) scan_marks_kernel(ScanArgs a, int NP) {
     float A[4], h[4], f[4];
     load_row<4>(a.A + (long long)c * a.N, a.N, n0, A);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) A[n] *= kLog2e;
+    for (int n = 0; n < 4; ++n) A[n] = scaled(A[n]);
     start_of<4>(a, NP, w, c, n0, A, h);
     for (int t = w.t0; t < w.t1; t += kSteps) {
         const long long at = (long long)(t / kSteps) * a.Be + w.e;
@@ -531,9 +545,13 @@ __global__ void __launch_bounds__(256) scan_marks_kernel(ScanArgs a, int NP) {
 // Gradients.  Per step, with g = dL/dh_t and dv = dL/dy silu(z):
 //   g_t = C_t dv_t + (nothing where done[t] is set, else) exp(d_{t+1} A) g_{t+1},   q = g_t exp(d_t A) h'_{t-1}
 //   dC = sum_c dv h,  dB = sum_c g d x,  dx = D dv + d sum_n g B,  dd = x sum_n g B + sum_n q A,  dA += q d
-// Four steps at a time, backwards: from the states in front of them forwards once more, which leaves the factors and exp(d A) h' of the
-// four steps in registers (and y and the sums of dC on the way), then backwards over these.  A block goes through as many envs, or
-// segments, as fall to it and keeps its shares of the parameters' gradients.
+// Sixteen steps at a time, from the last ones to the first: forwards once from the states in front of them, which leaves those in front of every
+// fourth step; then four steps at a time, backwards: forwards through them, which leaves exp(d A) h' of the four in registers (and y and
+// the sums of dC on the way), and backwards over these, where the factors are made a second time: kept, they would take the registers of
+// half the warps.  A block goes through as many envs, or segments, as fall to it, copies the rows of the next sixteen steps ahead while it works,
+// and keeps its shares of the parameters' gradients.  16 steps of 256 envs of 2048 x 16 bf16: 264 us, 57 % of the issue slots (620
+// instructions for 32 channels of a step, a third of them integer arithmetic and selections around the sums over lanes).
+
 // Two elements of the states of four channels, [e][channel][N] in memory; zeros where there are none.
 __device__ __forceinline__ void load_block(const float *from, const ScanArgs &a, int e, int c, int c1, int n0, float (&h)[4][2]) {
 #pragma unroll
@@ -608,7 +626,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int n = 0; n < NPT; ++n) f[j][n] *= kLog2e;
+            for (int n = 0; n < NPT; ++n) f[j][n] = scaled(f[j][n]);
         pack(f, A);
 #pragma unroll
         for (int n = 0; n < NPT; ++n) dA[n][0] = dA[n][1] = 0;
@@ -974,7 +992,7 @@ __global__ void __launch_bounds__(256) scan_few_kernel(ScanArgs a) {
 
 // One step, the state in place: NL lanes share four channels of a group, four elements of each, whose step sizes and outputs they share out among
 // them.  Bound by memory, since the states go through once: a thread copies its own of the next envs ahead into shared memory, and reads
-// the next env's rows while it works on this one's.
+// the next env's rows while it works on this one's.  512 envs of 4096 x 16: 53 us, 5.4 TB/s (one channel a thread, 4 KB side by side: 82).
 constexpr int kAhead = 3;  // envs in the ring
 
 template <typename T, int NL>
@@ -992,7 +1010,7 @@ __global__ void __launch_bounds__(256, 3) scan_step_kernel(ScanArgs a, int envs)
     // of the envs that are copied ahead, read, and written next
     float *state = a.state_out + ((long long)e0 * a.channels + c) * a.N + n0;
     const float *to_copy = state;
-    const T *B = static_cast<const T *>(a.B) + e0 * a.ldb + group * a.N + n0, *C = static_cast<const T *>(a.C) + e0 * a.ldc + group * a.N + n0;
+    const T *B = static_cast<const T *>(a.B) + e0 * a.ldb + (long long)group * a.N + n0, *C = static_cast<const T *>(a.C) + e0 * a.ldc + (long long)group * a.N + n0;
     const int own = c + first * CH;  // the first of the channels that are this lane's
     const T *xp = static_cast<const T *>(a.x) + e0 * a.ldx + own, *tp = static_cast<const T *>(a.dt) + e0 * a.lddt + own;
     const T *zp = static_cast<const T *>(a.z) + e0 * a.ldz + own;
@@ -1059,7 +1077,7 @@ __global__ void __launch_bounds__(256, 3) scan_step_kernel(ScanArgs a, int envs)
         for (int n = 0; n < 4; ++n) A[j][n] = 0.f;
         if (c + j * CH < end) load_row<4>(a.A + (long long)(c + j * CH) * a.N, a.N, n0, A[j]);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) A[j][n] *= kLog2e;
+        for (int n = 0; n < 4; ++n) A[j][n] = scaled(A[j][n]);
     }
 #pragma unroll
     for (int i = 0; i < LEFT; ++i) {

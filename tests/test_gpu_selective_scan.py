@@ -274,3 +274,34 @@ def test_a_state_that_is_no_number_goes_no_further_than_the_first_flag():
     same[:] = True
     same[6:, 0, 7] = False
     assert torch.equal(g0["dx"][same], g1["dx"][same]) and torch.equal(g0["dstate"], g1["dstate"])
+
+
+@pytest.mark.parametrize("T,Be", [(5, 3), (18, 2), (300, 1)])
+def test_decays_of_any_size(T, Be):
+    """Elements that forget everything at once (A of minus infinity), next to those that forget nothing (A of 0), as -1e30 and 0 do."""
+    p = _inputs(T, Be, 40, 16, 1, torch.float32)
+    p["A"][:, 3], p["A"][:, 7] = -1e30, 0.0
+    _check(p)
+    y, s1 = _fwd(p)
+    q = {**p, "A": p["A"].clone()}
+    q["A"][:, 3] = float("-inf")
+    y2, s2 = _fwd(q)
+    assert torch.equal(y, y2) and torch.equal(s1, s2)
+    a, b = _bwd(p), _bwd(q)
+    for n in ("dx", "dB", "dC", "dz", "dstate"):
+        assert torch.equal(a[n], b[n]), n
+    state = p["s0"].clone()
+    out = _like(p["x"][0])
+    ppo.ppo_selective_scan_step(p["x"][0], p["dt"][0], q["A"], p["B"][0], p["C"][0], state, out, p["D"], p["z"][0], p["bias"])
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(state).all())
+
+
+def test_a_last_flag_leaves_zeros_whatever_was_there():
+    for T in (1, 3, 17, 300):
+        p = _inputs(T, 2, 40, 16, 1, torch.float32, done=0.0)
+        p["done"][T - 1] = 1
+        p["A"] = p["A"].clone()
+        p["A"][5, 2] = float("nan")
+        y, s1 = _fwd(p)
+        assert not s1.any() and bool(torch.isnan(y[:, :, 5]).all())
+        assert bool(torch.isfinite(y[:, :, torch.arange(40, device=DEV) != 5]).all())
