@@ -539,7 +539,8 @@ int ppo_causal_conv_step(const ppo_causal_conv_desc *desc, const void *dev_x, co
  *   x, dt, z, y [T*Be][C], B, C [T*Be][groups][N] of type dtype with ldx, lddt, ldz, ldy, ldb, ldc elements from row to row (at least the row's
  *   own length); A fp32 [C][N]; D, dt_bias fp32 [C] (NULL: 0), z NULL: no factor; done uint8 [T][Be] (NULL: no flag is set); states fp32
  *   [Be][C][N] (in NULL: zeros, h'_{-1}; out NULL: not wanted, h'_{T-1}).
- * States, sums and arithmetic in fp32.  1 <= N <= 64; channels a multiple of groups (else SHAPE); T * Be up to 0x7f000000 and Be * channels up to
+ * States, sums and arithmetic in fp32; an infinity in A makes 0, or infinity, of every step size but 0, and 1 of that.  1 <= N <= 64; channels a multiple
+ * of groups (else SHAPE); T * Be up to 0x7f000000 and Be * channels up to
  * 0x1fffffff (else UNSUPPORTED). */
 typedef struct {
     int32_t T, Be, channels, N, groups, dtype, softplus;
