@@ -316,9 +316,12 @@ template <typename T, int W, int V>
 __global__ void __launch_bounds__(kThreads, W <= 4 ? 4 : 2) conv_bwd_kernel(ConvArgs a, int lanes) {
     grid_wait();
     constexpr int P = Raw<T, V>::PAIRS, BATCH = W == 2 ? 4 : W, AHEAD = W <= 4 ? 2 : 1, S = BATCH * (AHEAD + 1), ALL = (1 << W) - 1;
-    __shared__ typename Raw<T, V>::Word rx[S][kThreads], rg[S][kThreads];
-    __shared__ float sum[kThreads];
-    const Ring<T, V, S> xs = {rx}, gs = {rg};
+    using Word = typename Raw<T, V>::Word;
+    constexpr int SUMS = (W + 1) * V;
+    // the rings of x and dy; behind the last run, the sums of all threads
+    __shared__ alignas(16) char shared[2 * S * sizeof(Word) > SUMS * sizeof(float) ? 2 * S * sizeof(Word) * kThreads : SUMS * sizeof(float) * kThreads];
+    const Ring<T, V, S> xs = {reinterpret_cast<Word(*)[kThreads]>(shared)}, gs = {xs.at + S};
+    float(*const sums)[kThreads] = reinterpret_cast<float(*)[kThreads]>(shared);
     const int l = threadIdx.x % lanes, p0 = threadIdx.x / lanes, rows = kThreads / lanes, c = (blockIdx.x * lanes + l) * V;
     const bool on = c < a.C;
     const long long &sx = a.sx, &sy = a.sy;
@@ -454,21 +457,20 @@ __global__ void __launch_bounds__(kThreads, W <= 4 ? 4 : 2) conv_bwd_kernel(Conv
         }
     }
     if (!a.part) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i) {
+        const float2 f = parts(i < W * V ? dw[i < W * V ? i / V : 0][i % V / 2] : db[i % V / 2]);
+        sums[i][threadIdx.x] = i % V % 2 ? f.y : f.x;
+    }
+    __syncthreads();
     float *part = a.part + (size_t)blockIdx.y * a.C * (W + 1);
-#pragma unroll
-    for (int i = 0; i <= W; ++i) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float2 f = parts(i < W ? dw[i < W ? i : 0][v / 2] : db[v / 2]);
-            __syncthreads();
-            sum[threadIdx.x] = v % 2 ? f.y : f.x;
-            __syncthreads();
-            if (p0 == 0 && on) {
-                float s = 0.f;
-                for (int k = 0; k < rows; ++k) s += sum[k * lanes + l];
-                part[i < W ? (size_t)(c + v) * W + i : (size_t)a.C * W + c + v] = s;
-            }
-        }
+    for (int o = threadIdx.x; o < SUMS * lanes; o += kThreads) {
+        const int i = o / lanes, at = o % lanes, to = (blockIdx.x * lanes + at) * V + i % V;
+        if (to >= a.C) continue;
+        float s = 0.f;
+        for (int k = 0; k < rows; ++k) s += sums[i][k * lanes + at];
+        part[i < W * V ? (size_t)to * W + i / V : (size_t)a.C * W + to] = s;
     }
 }
 

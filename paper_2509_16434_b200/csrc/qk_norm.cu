@@ -282,10 +282,10 @@ __device__ __forceinline__ void stage_gamma(const QkArgs &a, float (&to)[2][kMax
     __syncthreads();
 }
 
-constexpr int kHeads = 4;  // of a lane's, on their way at a time
+constexpr int kHeads = 2;  // of a lane's, on their way at a time
 
 template <typename T, bool INTERLEAVED>
-__global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
+__global__ void __launch_bounds__(256, 4) qk_fwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
     constexpr int V = 4, P = V / 2;
     using Word = typename Four<T>::Word;
@@ -344,9 +344,9 @@ __global__ void __launch_bounds__(256, 3) qk_fwd_kernel(QkArgs a, Lanes k) {
 // With n = R^T dy (turned back), g = gamma n and r = 1 / sqrt(mean x^2 + eps): dx = r g - x r^3 mean(g x), dgamma += n x r.  Both sums of a head are
 // made at once.  A warp has either queries or keys, and keeps its share of the gradient of their gamma.
 template <typename T, bool INTERLEAVED>
-__global__ void __launch_bounds__(256, 3) qk_bwd_kernel(QkArgs a, Lanes k) {
+__global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
-    constexpr int V = 4, P = V / 2, U = 2;
+    constexpr int V = 4, P = V / 2, U = 4;
     using Word = typename Four<T>::Word;
     __shared__ alignas(16) float gamma[2][kMaxD];
     __shared__ float2 tables[8][kMaxD / 2];
@@ -533,7 +533,7 @@ extern "C" int ppo_qk_norm_rotate_fwd(const ppo_qk_norm_desc *d, float eps, cons
         return with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_fwd_any_kernel<decltype(t)>, dim3(any_blocks(d)), dim3(256), 0, st, a); });
     const Lanes l = lanes_of(d, 32);
     return with_order(d, [&](auto t, auto order) {
-        return ppo_launch(qk_fwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks_of((long long)d->rows * l.parts, 8)), dim3(256), 0, st, a, l);
+        return ppo_launch(qk_fwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks_of((long long)d->rows * l.parts, 4)), dim3(256), 0, st, a, l);
     });
 }
 
@@ -558,7 +558,7 @@ extern "C" int ppo_qk_norm_rotate_bwd(const ppo_qk_norm_desc *d, float eps, cons
     int blocks = any_blocks(d);
     if (vectors(d, {q, k, dq_out, dk_out, dq, dk})) {
         const Lanes l = lanes_of(d, 32);
-        blocks = blocks_of((long long)d->rows * l.parts, 3);
+        blocks = blocks_of((long long)d->rows * l.parts, 2);
         PPO_TRY(with_order(d, [&](auto t, auto order) {
             return ppo_launch(qk_bwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks), dim3(256), 0, st, a, l);
         }));
