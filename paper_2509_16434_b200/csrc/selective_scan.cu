@@ -1169,7 +1169,7 @@ Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     // segments: forwards as many as fill four blocks an SM; backwards, where three passes go over them, as many as deal two to each slice of blocks;
     // none shorter than 32 steps (gradients of 119 steps of 37 envs of 202 channels: 127 us with 64, 113 with 32, 115 with 16), no more than 64, since
     // each starts by going through those in front of it (8192 steps of 512 channels: 174 us with 32 of them, 124 with 64, 120 with 96, 490 with 256)
-    const int slices = p.tiles < 4 * 148 ? 4 * 148 / p.tiles : 1;  // four blocks an SM
+    const int room = (d->dtype == PPO_F32 ? 3 : 4) * 148, slices = p.tiles < room ? room / p.tiles : 1;  // one round of scan_bwd_kernel's blocks
     const long long blocks = (long long)d->Be * d->groups * ppo_cdiv(per, 256 / p.NL);
     long long n = bwd ? (d->Be < slices ? 2ll * slices / d->Be : 1) : (blocks < 4 * 148 ? 4 * 148 / blocks : 1);
     const int most = ppo_cdiv(d->T, 32);
