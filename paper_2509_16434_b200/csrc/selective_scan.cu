@@ -585,8 +585,8 @@ struct GradShared {
     float sd[kSteps][CT], su[kSteps][CT], sg[kSteps][CT], sy[kSteps][CT], sD[CT], sbias[CT];
     float2 sB[kSteps][NP], sC[kSteps][NP];  // every element twice, as packed arithmetic on two channels takes it
     float few[kThreads / 32][kSteps][2 * NP];
-    // a thread's own: the states in front of the tile; those in front of its 8th and 12th step (the last four start where the way forwards ends); its sums of the gradients of D and
-    // dt_bias; its elements of the next tile's rows of x, dt, dy, z
+    // a thread's own: the states in front of the tile, and of its steps 4 and 8 (from 12 on they start where the way forwards ends); its sums of
+    // the gradients of D and dt_bias; its elements of the next tile's rows of x, dt, dy, z
     float2 mark[4][kThreads];
     float4 inner[2][2][kThreads];
     float kept[2][kThreads * R::V];
