@@ -870,9 +870,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
                         const float2 e = parts(s1[0]), o = parts(s1[1]), e2 = parts(s2[0]), o2 = parts(s2[1]);
                         both[0] = e.x, both[1] = e.y, both[2] = o.x, both[3] = o.y;
                         both[4] = e2.x, both[5] = e2.y, both[6] = o2.x, both[7] = o2.y;
-                        // every lane of the channels has read this step's row: the sums take its place
                         spread_sum<8, NL, 1>(both, lane);
                         const int at = spread_first<8, NL>(ln);
+                        __syncwarp();  // every lane of the channels has read this step's row: the sums take its place
                         *((at < 4 ? &s.su[r][local] : &s.sg[r][local - 4]) + at) = both[0];
                     }
                     spread_sum<4, GROUPS, NL>(bs, lane);
