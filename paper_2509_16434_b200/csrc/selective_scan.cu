@@ -696,16 +696,19 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
             pack(f, g);
         }
         for (int t = last_tile(w); t >= w.t0; t -= kSteps) {
-            const int rows = min(w.t1 - t, kSteps);
-            const uint32_t flag = flags_of(a, w.e, t, rows);
+            // A last tile's rows are moved behind up to three rows of zeros, so that they end with a whole group of four: steps of size 0 in front of the
+            // first one hand its state and its gradient through, and no gradient passes any behind the last one, which may drop it.
+            const int rows = min(w.t1 - t, kSteps), pad = -rows & 3;
+            const auto place = [pad](int r) { return (r + pad) & (kSteps - 1); };
+            const uint32_t flag = flags_of(a, w.e, t, rows) << pad;
             __syncthreads();  // the tile behind is done with
             asm volatile("cp.async.wait_all;" ::: "memory");  // a thread reads what it copied itself
 #pragma unroll
             for (int i = 0; i < FEW; ++i) {
                 const int r = threadIdx.x / NP + i * (kThreads / NP), n = threadIdx.x % NP;
                 const float b = to_f32(fb[i]), f = to_f32(fc[i]);
-                s.sB[r][n] = make_float2(b, b);
-                s.sC[r][n] = make_float2(f, f);
+                s.sB[place(r)][n] = make_float2(b, b);
+                s.sC[place(r)][n] = make_float2(f, f);
             }
 #pragma unroll
             for (int i = 0; i < R::PASSES; ++i) {
@@ -731,9 +734,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
                     }
                 }
                 if (r >= kSteps) break;
-                R::put_shared(&s.sd[r][l], d);
-                R::put_shared(&s.su[r][l], u);
-                R::put_shared(&s.sg[r][l], v);
+                R::put_shared(&s.sd[place(r)][l], d);
+                R::put_shared(&s.su[place(r)][l], u);
+                R::put_shared(&s.sg[place(r)][l], v);
             }
             {
                 // on its way while this tile is worked on
@@ -887,7 +890,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
                 if (r >= rows) break;
                 float sum = 0.f;
 #pragma unroll
-                for (int k = 0; k < kThreads / 32; ++k) sum += s.few[k][r][n];
+                for (int k = 0; k < kThreads / 32; ++k) sum += s.few[k][place(r)][n];
                 const long long row = (long long)(t + r) * a.Be + w.e;
                 a.few[(((long long)(tile - w.group * a.group_tiles) * a.T * a.Be + row) * a.groups + w.group) * (2 * NP) + n] = sum;
             }
@@ -914,16 +917,16 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
                     const int r = R::row(i), l = R::col(i);
                     if (r >= rows || l >= cols) continue;
                     pair32 d[R::PAIRS], s1[R::PAIRS], s2[R::PAIRS], xv[R::PAIRS], tv[R::PAIRS], gv[R::PAIRS], o[R::PAIRS];
-                    R::get_shared(&s.sd[r][l], d);
-                    R::get_shared(&s.su[r][l], s1);
-                    R::get_shared(&s.sg[r][l], s2);
+                    R::get_shared(&s.sd[place(r)][l], d);
+                    R::get_shared(&s.su[place(r)][l], s1);
+                    R::get_shared(&s.sg[place(r)][l], s2);
                     R::get(rx.raw[i], xv);
                     R::get(rt.raw[i], tv);
                     R::get(rg.raw[i], gv);
                     if (a.z) {
                         pair32 zv[R::PAIRS], yv[R::PAIRS];
                         R::get(rz.raw[i], zv);
-                        R::get_shared(&s.sy[r][l], yv);
+                        R::get_shared(&s.sy[place(r)][l], yv);
 #pragma unroll
                         for (int k = 0; k < R::PAIRS; ++k) {
                             const pair32 p = R::sigmoid(zv[k]), all = a.D ? fma2(D[k], xv[k], yv[k]) : yv[k], one = twice(1.f);
