@@ -57,6 +57,14 @@ __device__ __forceinline__ float scaled(float A) {
     return isinf(v) ? copysignf(3e38f, v) : v;
 }
 __device__ __forceinline__ pair32 factors(pair32 d, pair32 A) { return exp2_pair(fma2(d, A, twice(kShift))); }
+// h 2^(3 x) + add, the steps of a segment taken at once, a third of the way at a time: 2^(3 x) may leave the range where its product with h does not, and
+// what is 0 stays 0 however much it would grow.  Beyond 2^360 the product leaves the range whatever h is.
+__device__ __forceinline__ float carried(float x, float h, float add) {
+    float y;
+    asm("min.NaN.f32 %0, %1, 0f42F00000;" : "=f"(y) : "f"(x));  // 120
+    const float f = exp2_fast(y);
+    return fmaf(h * f * f, f, add);
+}
 
 // Sums of V values over LANES lanes, STRIDE apart: halves go to the lanes' halves as long as there are values, lane bit by lane bit from the
 // highest; a lane is left with max(1, V / LANES) of them in v[0 ..], which ones spread_first says.
@@ -219,17 +227,17 @@ __device__ __forceinline__ void load_pairs(const float *p, pair32 (&v)[2]) {
     v[0] = u.x, v[1] = u.y;
 }
 
-// Takes elements n0 .. of a channel's state, or gradient, through segment s: exp2(A sum of its step sizes) h + add, or add alone behind a flag.  from: what
-// each segment adds; A: times log2(e).
+// Takes elements n0 .. of a channel's state, or gradient, through segment s: exp2(A sum of its step sizes) h + add, or add alone behind a flag (selected
+// in front: the loops over segments then have their loads together).  from: what each segment adds; A: times log2(e).
 template <int W>
 __device__ __forceinline__ void through(const ScanArgs &a, int NP, int s, int e, int c, int n0, const float (&A)[W], const float *from, float (&h)[W]) {
     const long long at = (long long)s * a.Be + e;
     float add[W];
     load_row<W>(from + (at * a.channels + c) * NP, NP, n0, add);
     const bool cut = a.cut[at];
-    const float d = a.sum[at * a.channels + c];
+    const float sum = a.sum[at * a.channels + c], d = cut ? 0.f : sum * (1.f / 3);
 #pragma unroll
-    for (int n = 0; n < W; ++n) h[n] = cut ? add[n] : fmaf(exp2_fast(d * A[n]), h[n], add[n]);
+    for (int n = 0; n < W; ++n) h[n] = carried(d * A[n], cut ? 0.f : h[n], add[n]);
 }
 // What a segment starts from: the state that comes in, or what the first segment ends with, taken through the segments in between.
 template <int W>
@@ -242,6 +250,7 @@ __device__ __forceinline__ void start_of(const ScanArgs &a, int NP, const Work &
 template <int W>
 __device__ __forceinline__ void end_of(const ScanArgs &a, int NP, const Work &w, int c, int n0, const float (&A)[W], float (&g)[W]) {
     load_row<W>(a.back + ((long long)w.e * a.channels + c) * NP, NP, n0, g);
+#pragma unroll 4
     for (int s = a.nseg - 1; s > w.seg; --s) through<W>(a, NP, s, w.e, c, n0, A, a.back, g);
 }
 
@@ -511,8 +520,36 @@ __global__ void __launch_bounds__(kThreads, 4) scan_kernel(ScanArgs a) {
     }
 }
 
+// The gradient that a segment hands to the steps in front, getting zeros, step by step from its last one: four elements of channel c.
+template <typename T>
+__device__ void handed(const ScanArgs &a, const Work &w, int c, int n0, const float (&A)[4], float (&g)[4]) {
+    const int group = c / a.per;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) g[n] = 0.f;
+    for (int t = w.t1 - 1; t >= w.t0; --t) {
+        if (a.done && a.done[(long long)t * a.Be + w.e]) {
+#pragma unroll
+            for (int n = 0; n < 4; ++n) g[n] = 0.f;
+        }
+        const T *C = static_cast<const T *>(a.C) + w.e * a.ldc + t * a.sc + (long long)group * a.N;
+        float d = to_f32(static_cast<const T *>(a.dt)[w.e * a.lddt + t * a.st + c]) + (a.bias ? a.bias[c] : 0.f);
+        float v = to_f32(static_cast<const T *>(a.dy)[w.e * a.ldy + t * a.sy + c]);
+        if (a.softplus) d = softplus_fast(d);
+        if (a.z) {
+            const float z = to_f32(static_cast<const T *>(a.z)[w.e * a.ldz + t * a.sz + c]);
+            v *= z * sigmoid_fast(z);
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+            if (n0 + n < a.N) g[n] = fmaf(to_f32(C[n0 + n]), v, g[n]) * exp2_fast(fmaf(d, A[n], kShift));
+    }
+}
+
 // The states in front of every kSteps-th step of the segments but the first, from those that started from zeros: what the segment starts from, taken
-// through the steps in front of them, is added.  A thread has four elements of a channel in one segment.
+// through the steps in front of them, is added.  A thread has four elements of a channel in one segment.  It also looks at the gradient that the
+// segment hands to the steps in front, a sum of products of factors forwards: where these have left the range, which leaves no finite sum, though the
+// gradients of the steps need not have, it is made again.  (Where they fall below 2^-149 they count as 0.)
+template <typename T>
 __global__ void __launch_bounds__(256) scan_marks_kernel(ScanArgs a, int NP) {
     grid_wait();
     const int quads = NP / 4;
@@ -525,21 +562,26 @@ __global__ void __launch_bounds__(256) scan_marks_kernel(ScanArgs a, int NP) {
     w.e = (int)(item % a.Be);
     w.t0 = w.seg * a.len;
     w.t1 = min(a.T, w.t0 + a.len);
-    float A[4], h[4], f[4];
+    float A[4], h[4], f[4], g[4];
     load_row<4>(a.A + (long long)c * a.N, a.N, n0, A);
 #pragma unroll
     for (int n = 0; n < 4; ++n) A[n] = scaled(A[n]);
+    float *back = a.back + (((long long)w.seg * a.Be + w.e) * a.channels + c) * NP;
+    load_row<4>(back, NP, n0, g);
     start_of<4>(a, NP, w, c, n0, A, h);
     for (int t = w.t0; t < w.t1; t += kSteps) {
         const long long at = (long long)(t / kSteps) * a.Be + w.e;
         if (a.cum_cut[at]) break;
-        const float d = a.cum[at * a.channels + c];
+        const float d = a.cum[at * a.channels + c] * (1.f / 3);
         float *mark = a.mark + (at * a.channels + c) * NP;
         load_row<4>(mark, NP, n0, f);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) f[n] = fmaf(exp2_fast(d * A[n]), h[n], f[n]);
+        for (int n = 0; n < 4; ++n) f[n] = carried(d * A[n], h[n], f[n]);
         store_row<4>(mark, NP, n0, f);
     }
+    if (isfinite(g[0]) && isfinite(g[1]) && isfinite(g[2]) && isfinite(g[3])) return;
+    handed<T>(a, w, c, n0, A, g);
+    store_row<4>(back, NP, n0, g);
 }
 
 // Gradients.  Per step, with g = dL/dh_t and dv = dL/dy silu(z):
@@ -1348,7 +1390,7 @@ extern "C" int ppo_selective_scan_bwd(const ppo_selective_scan_desc *d, const vo
         if (p.nseg > 1) {
             PPO_TRY((pass_of<T, NL, 1, BOTH>(a, p.nseg, st)));
             const long long quads = (long long)(p.nseg - 1) * d->Be * d->channels * (p.NP / 4);
-            PPO_TRY(ppo_launch(scan_marks_kernel, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a, p.NP));
+            PPO_TRY(ppo_launch(scan_marks_kernel<T>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a, p.NP));
         } else if (d->T > kSteps) {
             PPO_TRY((pass<T, NL, MARKS>(a, two, 1, st)));
         }
