@@ -603,7 +603,7 @@ extern "C" int ppo_causal_conv_bwd(const ppo_causal_conv_desc *d, const void *x,
         constexpr int W = decltype(w)::value;
         return ppo_launch(vec ? conv_bwd_kernel<T, W, 8 / (int)sizeof(T)> : conv_bwd_kernel<T, W, 1>, dim3(p.cols, p.blocks), dim3(kThreads), 0, st, a, p.lanes);
     }));
-    return params ? ppo_param_sum(a.part, p.blocks, {{dweight, dbias, nullptr}, {d->C * d->width, d->C, 0}}, accumulate, st) : PPO_OK;
+    return params ? ppo_param_sum(a.part, p.blocks, {{dweight, dbias, nullptr}, {(long long)d->C * d->width, d->C, 0}}, accumulate, st) : PPO_OK;
 }
 
 extern "C" int ppo_causal_conv_step(const ppo_causal_conv_desc *d, const void *x, const float *weight, const float *bias, const uint8_t *start,

@@ -7,7 +7,7 @@ template <int WARPS>
 __global__ void __launch_bounds__(32 * WARPS) param_sum_kernel(const float *part, int parts, ParamSums s, int accumulate) {
     grid_wait();
     __shared__ double sum[WARPS][32];
-    const long long n = (long long)s.n[0] + s.n[1] + s.n[2];
+    const long long n = s.n[0] + s.n[1] + s.n[2];
     const int l = threadIdx.x % 32, w = threadIdx.x / 32;
     long long i = (long long)blockIdx.x * 32 + l;
     double v = 0;
@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(32 * WARPS) param_sum_kernel(const float *part
 }  // namespace
 
 int ppo_param_sum(const float *part, int parts, const ParamSums &s, int accumulate, cudaStream_t st) {
-    const long long n = (long long)s.n[0] + s.n[1] + s.n[2];
+    const long long n = s.n[0] + s.n[1] + s.n[2];
     const dim3 grid((unsigned)((n + 31) / 32));
     // 592 shares of 128 columns: 14.5 us by eight warps; 444 of them by 32: 6.8
     if (parts > 64) return ppo_launch(param_sum_kernel<32>, grid, dim3(1024), 0, st, part, parts, s, accumulate);

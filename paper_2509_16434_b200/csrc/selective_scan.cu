@@ -1398,7 +1398,7 @@ extern "C" int ppo_selective_scan_bwd(const ppo_selective_scan_desc *d, const vo
         const long long few = (long long)d->T * d->Be * d->groups * 2 * p.NP;
         return ppo_launch(scan_few_kernel<T, 16 * NL>, dim3((unsigned)((few + 255) / 256)), dim3(256), 0, st, a);
     }));
-    return params ? ppo_param_sum(a.part, p.parts, {{dA, dD, ddt_bias}, {d->channels * d->N, d->channels, d->channels}}, accumulate, st) : PPO_OK;
+    return params ? ppo_param_sum(a.part, p.parts, {{dA, dD, ddt_bias}, {(long long)d->channels * d->N, d->channels, d->channels}}, accumulate, st) : PPO_OK;
 }
 
 extern "C" int ppo_selective_scan_step(const ppo_selective_scan_desc *d, const void *x, const void *dt, const float *A, const void *B, const void *C,
