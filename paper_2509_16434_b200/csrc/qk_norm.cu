@@ -5,6 +5,8 @@
 // elements of every pair it turns; the row's cosines and sines are made once for all its heads, d / 64 of them a lane.  16384 rows of 20 heads of
 // 128 bf16: 40 us, 4.2 TB/s, 69 % of the issue slots; gradients of 4096 rows of 32 heads of 64: 21 us with the launch that sums the shares, bound
 // by the chain from a row's position to its turns and sums.  Vectors of eight elements (half as many warps an SM): 44 and 27.
+#include <cfloat>
+
 #include "elem.cuh"
 #include "pair32.cuh"
 #include "param_sum.cuh"
@@ -33,11 +35,14 @@ __device__ __forceinline__ float2 turn(int pos, double f) {
     sincospif((float)(2. * (t - rint(t))), &r.y, &r.x);
     return r;
 }
-// 1 / sqrt(sum / d + eps): the hardware's approximation and a step of Newton's method, which leaves a unit of the last place.
+// 1 / sqrt(sum / d + eps): the hardware's approximation and a step of Newton's method, which leaves a unit of the last place.  SMALL: of a mean below the
+// normal numbers as well, which an eps below them allows (41.0 us where the larger case above takes 40.4, so not for every eps).
+template <bool SMALL>
 __device__ __forceinline__ float root(const QkArgs &a, float sum) {
     const float m = fmaf(sum, a.inv_d, a.eps);
     float r;
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(m));
+    if (SMALL) asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(m));
+    else asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(m));
     const float h = 0.5f * m * r;
     return m > 3e38f ? r : fmaf(r, fmaf(-h, r, 0.5f), r);  // an infinite sum makes zeros
 }
@@ -74,7 +79,7 @@ __global__ void __launch_bounds__(256) qk_fwd_any_kernel(QkArgs a) {
             n[i] = to_f32(x[i]);
             s = fmaf(n[i], n[i], s);
         }
-        const float r = root(a, warp_sum(s));
+        const float r = root<true>(a, warp_sum(s));
         for (int i = lane; i < a.d; i += 32) n[i] *= r * (gamma ? gamma[i] : 1.f);
         __syncwarp();
         for (int i = lane; i < a.d; i += 32) {
@@ -113,7 +118,7 @@ __global__ void __launch_bounds__(256) qk_bwd_any_kernel(QkArgs a) {
             if (i < a.d) n[i] = to_f32(dy[i]);
             s = fmaf(v[j], v[j], s);
         }
-        const float r = root(a, warp_sum(s));
+        const float r = root<true>(a, warp_sum(s));
         __syncwarp();
         float g[kMaxD / 32], dot = 0.f;
 #pragma unroll
@@ -284,7 +289,7 @@ __device__ __forceinline__ void stage_gamma(const QkArgs &a, float (&to)[2][kMax
 
 constexpr int kHeads = 2;  // of a lane's, on their way at a time: the larger case above 40 us; one 56, three 40, four 43
 
-template <typename T, bool INTERLEAVED>
+template <typename T, bool INTERLEAVED, bool SMALL>
 __global__ void __launch_bounds__(256, 4) qk_fwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
     constexpr int V = 4, P = V / 2;
@@ -325,7 +330,7 @@ __global__ void __launch_bounds__(256, 4) qk_fwd_kernel(QkArgs a, Lanes k) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) s = fma2(x[j], x[j], s);
                 const float2 f = parts(s);
-                const float r = root(a, lanes_sum(f.x + f.y, k.lanes));
+                const float r = root<SMALL>(a, lanes_sum(f.x + f.y, k.lanes));
                 if (n >= h1 || !turns.on) continue;
                 floats_of<P>(&gamma[n >= a.heads][turns.first], g);
                 floats_of<P>(&gamma[n >= a.heads][turns.second], g + P);
@@ -343,7 +348,7 @@ __global__ void __launch_bounds__(256, 4) qk_fwd_kernel(QkArgs a, Lanes k) {
 
 // With n = R^T dy (turned back), g = gamma n and r = 1 / sqrt(mean x^2 + eps): dx = r g - x r^3 mean(g x), dgamma += n x r.  Both sums of a head are
 // made at once.  A warp has either queries or keys, and keeps its share of the gradient of their gamma.
-template <typename T, bool INTERLEAVED>
+template <typename T, bool INTERLEAVED, bool SMALL>
 __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
     constexpr int V = 4, P = V / 2, U = 4;
@@ -406,7 +411,7 @@ __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
                     t = fma2(mul2(g[j], x[j]), gam[j], t);
                 }
                 const float2 f = parts(s), u = parts(t);
-                const float r = root(a, lanes_sum(f.x + f.y, k.lanes));
+                const float r = root<SMALL>(a, lanes_sum(f.x + f.y, k.lanes));
                 const float m = -lanes_sum(u.x + u.y, k.lanes) * a.inv_d * r * r;
                 if (n >= h1 || !turns.on) continue;
                 const pair32 rr = pair_of(r, r), mm = pair_of(m, m);
@@ -508,9 +513,13 @@ Lanes lanes_of(const ppo_qk_norm_desc *d, int warps) {
     k.warps = k.warps < 1 ? 1 : k.warps > 7 ? 7 : k.warps;
     return k;
 }
+// fn(T{}, interleaved, eps below the normal numbers)
 template <typename F>
-int with_order(const ppo_qk_norm_desc *d, F &&fn) {
-    return with_elem(d->dtype, [&](auto t) -> int { return d->interleaved ? fn(t, std::true_type{}) : fn(t, std::false_type{}); });
+int with_order(const ppo_qk_norm_desc *d, float eps, F &&fn) {
+    return with_elem(d->dtype, [&](auto t) -> int {
+        const auto ordered = [&](auto small) -> int { return d->interleaved ? fn(t, std::true_type{}, small) : fn(t, std::false_type{}, small); };
+        return eps < FLT_MIN ? ordered(std::true_type{}) : ordered(std::false_type{});
+    });
 }
 
 }  // namespace
@@ -532,8 +541,8 @@ extern "C" int ppo_qk_norm_rotate_fwd(const ppo_qk_norm_desc *d, float eps, cons
     if (!vectors(d, {q, k, q_out, k_out}))
         return with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_fwd_any_kernel<decltype(t)>, dim3(any_blocks(d)), dim3(256), 0, st, a); });
     const Lanes l = lanes_of(d, 32);
-    return with_order(d, [&](auto t, auto order) {
-        return ppo_launch(qk_fwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks_of((long long)d->rows * l.parts, 4)), dim3(256), 0, st, a, l);
+    return with_order(d, eps, [&](auto t, auto order, auto small) {
+        return ppo_launch(qk_fwd_kernel<decltype(t), decltype(order)::value, decltype(small)::value>, dim3(blocks_of((long long)d->rows * l.parts, 4)), dim3(256), 0, st, a, l);
     });
 }
 
@@ -559,8 +568,8 @@ extern "C" int ppo_qk_norm_rotate_bwd(const ppo_qk_norm_desc *d, float eps, cons
     if (vectors(d, {q, k, dq_out, dk_out, dq, dk})) {
         const Lanes l = lanes_of(d, 32);
         blocks = blocks_of((long long)d->rows * l.parts, 2);
-        PPO_TRY(with_order(d, [&](auto t, auto order) {
-            return ppo_launch(qk_bwd_kernel<decltype(t), decltype(order)::value>, dim3(blocks), dim3(256), 0, st, a, l);
+        PPO_TRY(with_order(d, eps, [&](auto t, auto order, auto small) {
+            return ppo_launch(qk_bwd_kernel<decltype(t), decltype(order)::value, decltype(small)::value>, dim3(blocks), dim3(256), 0, st, a, l);
         }));
     } else {
         PPO_TRY(with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_bwd_any_kernel<decltype(t)>, dim3(blocks), dim3(256), 0, st, a); }));
