@@ -972,7 +972,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) scan_bwd_ker
 #pragma unroll
                         for (int k = 0; k < R::PAIRS; ++k) {
                             const pair32 p = R::sigmoid(zv[k]), all = a.D ? fma2(D[k], xv[k], yv[k]) : yv[k], one = twice(1.f);
-                            o[k] = mul2(mul2(gv[k], all), mul2(p, fma2(zv[k], fma2(p, twice(-1.f), one), one)));
+                            o[k] = mul2(gv[k], mul2(all, mul2(p, fma2(zv[k], fma2(p, twice(-1.f), one), one))));
                             gv[k] = mul2(gv[k], mul2(zv[k], p));
                         }
                         R::put(dz + r * sz + l, o);

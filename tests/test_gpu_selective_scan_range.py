@@ -73,3 +73,17 @@ def test_a_gradient_from_the_end_of_a_segment_that_grows(dtype, at):
     p["dy"][at] = (torch.randn(2, 40, device=DEV) * 2.0 ** -112).to(dtype)
     p["z"] = None
     _check(p)
+
+
+@pytest.mark.parametrize("channels", [40, 39])
+@pytest.mark.parametrize("z", [-80.0, -30.0])
+def test_a_gate_that_is_nearly_shut_on_large_values(channels, z):
+    """The gradient of the gate: outputs of 2^60 and gradients of 2^70, whose product leaves the range, times a slope of 1e-33 or 1e-12."""
+    p = _inputs(20, 2, channels, 16, 1, torch.float32, done=0.0)
+    p["x"] = p["x"] * 2.0 ** 60
+    p["dy"] = p["dy"] * 2.0 ** 70
+    p["z"][:] = z
+    p.update(s0=None, ds=None)
+    got, want = _bwd(p), _want(p, True)
+    for name in ("dz", "ddt", "dx", "dB", "dC"):
+        plain.within(got[name], want[name], name)
