@@ -580,7 +580,9 @@ __global__ void __launch_bounds__(256) scan_marks_kernel(ScanArgs a, int NP) {
         store_row<4>(mark, NP, n0, f);
     }
     if (isfinite(g[0]) && isfinite(g[1]) && isfinite(g[2]) && isfinite(g[3])) return;
-    handed<T>(a, w, c, n0, A, g);
+    handed<T>(a, w, c, n0, A, h);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) g[n] = isfinite(g[n]) ? g[n] : h[n];
     store_row<4>(back, NP, n0, g);
 }
 

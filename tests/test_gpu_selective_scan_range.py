@@ -87,3 +87,16 @@ def test_a_gate_that_is_nearly_shut_on_large_values(channels, z):
     got, want = _bwd(p), _want(p, True)
     for name in ("dz", "ddt", "dx", "dB", "dC"):
         plain.within(got[name], want[name], name)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("T,N", [(88, 16), (300, 16), (177, 17)])
+def test_an_element_that_is_no_number_leaves_its_neighbours_as_they_were(T, N, bad):
+    p = _inputs(T, 2, 40, N, 1, torch.float32, done=0.0)
+    want = _bwd(p)
+    q = {**p, "C": p["C"].clone()}
+    q["C"][T - 8, 1, 0, 2] = bad
+    got = _bwd(q)
+    rest = torch.arange(N, device=DEV) != 2
+    assert torch.equal(got["dA"][:, rest], want["dA"][:, rest]) and not torch.isfinite(got["dstate"][1, :, 2]).any()
+    assert torch.equal(got["dB"][..., rest], want["dB"][..., rest]) and torch.equal(got["dstate"][..., rest], want["dstate"][..., rest])
