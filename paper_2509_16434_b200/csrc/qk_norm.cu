@@ -174,11 +174,11 @@ struct Lanes {
     int warps;  // of a block, for the queries (gradients, where a warp has either queries or keys)
 };
 
-// The row's turns, and where a lane's two vectors stand in a head.
-template <typename T, bool INTERLEAVED>
+// The row's turns, and where a lane's two vectors stand in a head.  ALL: every pair of every head is turned.
+template <typename T, bool INTERLEAVED, bool ALL>
 struct Turns {
     static constexpr int V = 4, P = V / 2;
-    int first, second;
+    int first, second, own;  // own: how many of the lane's four pairs of neighbours are turned; the others have nothing to do with one another
     bool on;
     pair32 c[P], s[P], n[P];  // of two pairs each: cosines, sines, and these negative
     double f[kMaxD / 64];     // turns a position of the pairs that a lane makes
@@ -201,6 +201,7 @@ struct Turns {
             first = 2 * a.pairs + 2 * V * (slot - turned);
             second = first + V;
         }
+        own = INTERLEAVED && on ? max(0, min(V, a.pairs - first / 2)) : 0;
     }
     // table: of the warp; made by all its lanes
     __device__ __forceinline__ void row(const QkArgs &a, long long row, float2 *table) {
@@ -225,21 +226,28 @@ struct Turns {
         const float2 f = parts(p);
         return pair_of(f.y, f.x);
     }
-    // x: the pairs of neighbours of both vectors; BACK: by the opposite angle
+    // a c + b where it is turned, else a
+    static __device__ __forceinline__ void add_if(bool turned, pair32 &a, pair32 c, pair32 b) {
+        if (ALL) a = fma2(a, c, b);
+        else asm("{\n.reg .pred p;\nsetp.ne.s32 p, %3, 0;\n@p fma.rn.f32x2 %0, %0, %1, %2;\n}" : "+l"(a) : "l"(c), "l"(b), "r"((int)turned));
+    }
+    // x: the pairs of neighbours of both vectors; BACK: by the opposite angle.  Pairs that stay are left out by a predicate or by a branch, whichever
+    // takes less (half of each head turned: 40.4 us where neighbours are turned with one another, by a branch 41.4; 41.6 by halves, 43.1 by a
+    // predicate; 38.9 and 40.9 without either).
     template <bool BACK>
-    __device__ __forceinline__ void apply(pair32 (&x)[V]) const {
+    __device__ __forceinline__ void apply(const QkArgs &k, pair32 (&x)[V]) const {
         if constexpr (INTERLEAVED) {
+            if (BACK && !ALL && own == 0) return;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float2 ct = parts(c[i / 2]), st = parts(BACK ? n[i / 2] : s[i / 2]), nt = parts(BACK ? s[i / 2] : n[i / 2]);
-                x[i] = fma2(x[i], i % 2 ? pair_of(ct.y, ct.y) : pair_of(ct.x, ct.x), mul2(swap(x[i]), i % 2 ? pair_of(nt.y, st.y) : pair_of(nt.x, st.x)));
+                add_if(i < own, x[i], i % 2 ? pair_of(ct.y, ct.y) : pair_of(ct.x, ct.x), mul2(swap(x[i]), i % 2 ? pair_of(nt.y, st.y) : pair_of(nt.x, st.x)));
             }
         } else {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                const pair32 a = x[i], b = x[P + i];
-                x[i] = fma2(a, c[i], mul2(b, BACK ? s[i] : n[i]));
-                x[P + i] = fma2(b, c[i], mul2(a, BACK ? n[i] : s[i]));
+                const pair32 b = mul2(x[P + i], BACK ? s[i] : n[i]), a = mul2(x[i], BACK ? n[i] : s[i]);
+                if (ALL || first < k.pairs) x[i] = fma2(x[i], c[i], b), x[P + i] = fma2(x[P + i], c[i], a);
             }
         }
     }
@@ -289,7 +297,7 @@ __device__ __forceinline__ void stage_gamma(const QkArgs &a, float (&to)[2][kMax
 
 constexpr int kHeads = 2;  // of a lane's, on their way at a time: the larger case above 40 us; one 56, three 40, four 43
 
-template <typename T, bool INTERLEAVED, bool SMALL>
+template <typename T, bool INTERLEAVED, bool ALL, bool SMALL>
 __global__ void __launch_bounds__(256, 4) qk_fwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
     constexpr int V = 4, P = V / 2;
@@ -297,7 +305,7 @@ __global__ void __launch_bounds__(256, 4) qk_fwd_kernel(QkArgs a, Lanes k) {
     __shared__ alignas(16) float gamma[2][kMaxD];
     __shared__ float2 tables[8][kMaxD / 2];
     stage_gamma(a, gamma);
-    Turns<T, INTERLEAVED> turns(a, k);
+    Turns<T, INTERLEAVED, ALL> turns(a, k);
     const int group = threadIdx.x % 32 / k.lanes, groups = 32 / k.lanes, all = a.heads + a.kv;
     const long long items = (long long)a.rows * k.parts, step = (long long)gridDim.x * 8;
     for (long long item = (long long)blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
@@ -337,7 +345,7 @@ __global__ void __launch_bounds__(256, 4) qk_fwd_kernel(QkArgs a, Lanes k) {
                 const pair32 rr = pair_of(r, r);
 #pragma unroll
                 for (int j = 0; j < V; ++j) x[j] = mul2(mul2(x[j], rr), g[j]);
-                turns.template apply<false>(x);
+                turns.template apply<false>(a, x);
                 T *y = (n < a.heads ? qo : ko) + (long long)n * a.d;
                 *reinterpret_cast<Word *>(y + turns.first) = raw_of<T>(x);
                 *reinterpret_cast<Word *>(y + turns.second) = raw_of<T>(x + P);
@@ -348,7 +356,7 @@ __global__ void __launch_bounds__(256, 4) qk_fwd_kernel(QkArgs a, Lanes k) {
 
 // With n = R^T dy (turned back), g = gamma n and r = 1 / sqrt(mean x^2 + eps): dx = r g - x r^3 mean(g x), dgamma += n x r.  Both sums of a head are
 // made at once.  A warp has either queries or keys, and keeps its share of the gradient of their gamma.
-template <typename T, bool INTERLEAVED, bool SMALL>
+template <typename T, bool INTERLEAVED, bool ALL, bool SMALL>
 __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
     grid_wait();
     constexpr int V = 4, P = V / 2, U = 4;
@@ -357,7 +365,7 @@ __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
     __shared__ float2 tables[8][kMaxD / 2];
     __shared__ float shares[8][kMaxD];
     stage_gamma(a, gamma);
-    Turns<T, INTERLEAVED> turns(a, k);
+    Turns<T, INTERLEAVED, ALL> turns(a, k);
     const int group = threadIdx.x % 32 / k.lanes, groups = 32 / k.lanes, w = threadIdx.x / 32;
     const bool keys = w >= k.warps;
     const int heads = keys ? a.kv : a.heads, mine = keys ? w - k.warps : w, warps = keys ? 8 - k.warps : k.warps;
@@ -396,7 +404,7 @@ __global__ void __launch_bounds__(256, 2) qk_bwd_kernel(QkArgs a, Lanes k) {
                 pairs_of<T>(xr[i][1], x + P);
                 pairs_of<T>(gr[i][0], g);
                 pairs_of<T>(gr[i][1], g + P);
-                turns.template apply<true>(g);
+                turns.template apply<true>(a, g);
                 pair32 gam[V];
                 if (turns.on) {
                     floats_of<P>(&gamma[keys][turns.first], gam);
@@ -513,12 +521,15 @@ Lanes lanes_of(const ppo_qk_norm_desc *d, int warps) {
     k.warps = k.warps < 1 ? 1 : k.warps > 7 ? 7 : k.warps;
     return k;
 }
-// fn(T{}, interleaved, eps below the normal numbers)
+// fn(T{}, interleaved, whole heads turned, eps below the normal numbers)
 template <typename F>
 int with_order(const ppo_qk_norm_desc *d, float eps, F &&fn) {
+    const std::true_type yes;
+    const std::false_type no;
     return with_elem(d->dtype, [&](auto t) -> int {
-        const auto ordered = [&](auto small) -> int { return d->interleaved ? fn(t, std::true_type{}, small) : fn(t, std::false_type{}, small); };
-        return eps < FLT_MIN ? ordered(std::true_type{}) : ordered(std::false_type{});
+        const auto ordered = [&](auto all, auto small) -> int { return d->interleaved ? fn(t, yes, all, small) : fn(t, no, all, small); };
+        if (eps < FLT_MIN) return ordered(no, yes);
+        return 2 * d->pairs == d->d ? ordered(yes, no) : ordered(no, no);
     });
 }
 
@@ -541,8 +552,9 @@ extern "C" int ppo_qk_norm_rotate_fwd(const ppo_qk_norm_desc *d, float eps, cons
     if (!vectors(d, {q, k, q_out, k_out}))
         return with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_fwd_any_kernel<decltype(t)>, dim3(any_blocks(d)), dim3(256), 0, st, a); });
     const Lanes l = lanes_of(d, 32);
-    return with_order(d, eps, [&](auto t, auto order, auto small) {
-        return ppo_launch(qk_fwd_kernel<decltype(t), decltype(order)::value, decltype(small)::value>, dim3(blocks_of((long long)d->rows * l.parts, 4)), dim3(256), 0, st, a, l);
+    return with_order(d, eps, [&](auto t, auto order, auto all, auto small) {
+        return ppo_launch(qk_fwd_kernel<decltype(t), decltype(order)::value, decltype(all)::value, decltype(small)::value>,
+                          dim3(blocks_of((long long)d->rows * l.parts, 4)), dim3(256), 0, st, a, l);
     });
 }
 
@@ -568,8 +580,9 @@ extern "C" int ppo_qk_norm_rotate_bwd(const ppo_qk_norm_desc *d, float eps, cons
     if (vectors(d, {q, k, dq_out, dk_out, dq, dk})) {
         const Lanes l = lanes_of(d, 32);
         blocks = blocks_of((long long)d->rows * l.parts, 2);
-        PPO_TRY(with_order(d, eps, [&](auto t, auto order, auto small) {
-            return ppo_launch(qk_bwd_kernel<decltype(t), decltype(order)::value, decltype(small)::value>, dim3(blocks), dim3(256), 0, st, a, l);
+        PPO_TRY(with_order(d, eps, [&](auto t, auto order, auto all, auto small) {
+            return ppo_launch(qk_bwd_kernel<decltype(t), decltype(order)::value, decltype(all)::value, decltype(small)::value>, dim3(blocks), dim3(256), 0, st, a,
+                              l);
         }));
     } else {
         PPO_TRY(with_elem(d->dtype, [&](auto t) { return ppo_launch(qk_bwd_any_kernel<decltype(t)>, dim3(blocks), dim3(256), 0, st, a); }));
