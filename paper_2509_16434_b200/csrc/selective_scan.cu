@@ -227,17 +227,17 @@ __device__ __forceinline__ void load_pairs(const float *p, pair32 (&v)[2]) {
     v[0] = u.x, v[1] = u.y;
 }
 
-// Takes elements n0 .. of a channel's state, or gradient, through segment s: exp2(A sum of its step sizes) h + add, or add alone behind a flag (selected
-// in front: the loops over segments then have their loads together).  from: what each segment adds; A: times log2(e).
+// Takes elements n0 .. of a channel's state, or gradient, through segment s: exp2(A sum of its step sizes) h + add, or add alone behind a flag.  from: what
+// each segment adds; A: times log2(e).
 template <int W>
 __device__ __forceinline__ void through(const ScanArgs &a, int NP, int s, int e, int c, int n0, const float (&A)[W], const float *from, float (&h)[W]) {
     const long long at = (long long)s * a.Be + e;
     float add[W];
     load_row<W>(from + (at * a.channels + c) * NP, NP, n0, add);
     const bool cut = a.cut[at];
-    const float sum = a.sum[at * a.channels + c], d = cut ? 0.f : sum * (1.f / 3);
+    const float d = a.sum[at * a.channels + c] * (1.f / 3);
 #pragma unroll
-    for (int n = 0; n < W; ++n) h[n] = carried(d * A[n], cut ? 0.f : h[n], add[n]);
+    for (int n = 0; n < W; ++n) h[n] = cut ? add[n] : carried(d * A[n], h[n], add[n]);
 }
 // What a segment starts from: the state that comes in, or what the first segment ends with, taken through the segments in between.
 template <int W>
