@@ -1,5 +1,5 @@
-// Exponentials, sigmoids and their relatives from the hardware's approximations, each within a few units of the last of 24 bits; results below
-// 2^-126 are 0.
+// Exponentials, sigmoids and their relatives from the hardware's approximations, within a few units of the last of 24 bits, and |z| more of them where
+// an argument z is multiplied by log2(e) in front, which rounds it (sigmoids of z far below 0, and softplus there); results below 2^-126 are 0.
 #pragma once
 #include "pair32.cuh"
 

@@ -11,9 +11,10 @@
 //
 // Long sequences of few channels are cut into segments: a pass makes what each segment ends with, and each starts from the ends in front of it.
 //
-// Measured, channels of 16 elements in bf16: outputs of 16 steps of 256 envs of 2048 channels 67 us, 57 % of the rate of exponentials (134 MB in
-// 21 us); of 8192 steps of 4096 channels 420, the pass over the segments 178 of it at 78 % of that rate, the outputs 260 at 64 %; gradients
-// of the former 279, of 2048 steps of 2 envs of 2048 channels 392.
+// Measured, channels of 16 elements in bf16: outputs of 16 steps of 256 envs of 2048 channels 68 us, 57 % of the rate of exponentials (134 MB in
+// 21 us); of 8192 steps of 4096 channels 422 (in a profiler, one launch at a time: the pass over the segments 179 at 78 % of that rate, the
+// outputs 262 at 64 %); gradients
+// of the former 281, of 2048 steps of 2 envs of 2048 channels 396.
 #include "approx.cuh"
 #include "elem.cuh"
 #include "pair32.cuh"
@@ -593,8 +594,9 @@ __global__ void __launch_bounds__(256) scan_marks_kernel(ScanArgs a, int NP) {
 // fourth step; then four steps at a time, backwards: forwards through them, which leaves exp(d A) h' of the four in registers (and y and
 // the sums of dC on the way), and backwards over these, where the factors are made a second time: kept, they would take the registers of
 // half the warps.  A block goes through as many envs, or segments, as fall to it, copies the rows of the next sixteen steps ahead while it works,
-// and keeps its shares of the parameters' gradients.  16 steps of 256 envs of 2048 x 16 bf16: 264 us, 57 % of the issue slots (620
-// instructions for 32 channels of a step, a third of them integer arithmetic and selections around the sums over lanes).
+// and keeps its shares of the parameters' gradients.  16 steps of 256 envs of 2048 x 16 bf16: 277 us in a profiler, 57 % of the issue
+// slots (620 instructions for 32 channels of a step, a third of them integer arithmetic and selections around the sums over lanes; 128 registers,
+// as many as four blocks an SM leave, and 52 bytes a thread beside them in local memory).
 
 // Two elements of the states of four channels, [e][channel][N] in memory; zeros where there are none.
 __device__ __forceinline__ void load_block(const float *from, const ScanArgs &a, int e, int c, int c1, int n0, float (&h)[4][2]) {
@@ -1039,7 +1041,7 @@ __global__ void __launch_bounds__(256) scan_few_kernel(ScanArgs a) {
 
 // One step, the state in place: NL lanes share four channels of a group, four elements of each, whose step sizes and outputs they share out among
 // them.  Bound by memory, since the states go through once: a thread copies its own of the next envs ahead into shared memory, and reads
-// the next env's rows while it works on this one's.  512 envs of 4096 x 16: 53 us, 5.4 TB/s (one channel a thread, 4 KB side by side: 82).
+// the next env's rows while it works on this one's.  512 envs of 4096 x 16: 55 us, 5.2 TB/s (one channel a thread, 4 KB side by side: 82).
 constexpr int kAhead = 3;  // envs in the ring
 
 template <typename T, int NL>
@@ -1214,8 +1216,8 @@ Plan plan_of(const ppo_selective_scan_desc *d, bool bwd) {
     p.group_tiles = ppo_cdiv(per, 64 / p.NL);
     p.tiles = p.group_tiles * d->groups;
     // segments: forwards as many as fill four blocks an SM; backwards, where three passes go over them, as many as deal two to each slice of blocks;
-    // none shorter than 32 steps (gradients of 119 steps of 37 envs of 202 channels: 127 us with 64, 113 with 32, 115 with 16), no more than 64, since
-    // each starts by going through those in front of it (8192 steps of 512 channels: 174 us with 32 of them, 124 with 64, 120 with 96, 490 with 256)
+    // none shorter than 32 steps (gradients of 119 steps of 37 envs of 202 channels: 110 us with 64, 94 with 32, 95 with 16), no more than 64, since
+    // each starts by going through those in front of it (8192 steps of 512 channels: 165 us with 32 of them, 115 with 64, 113 with 96, 483 with 256)
     const int room = (d->dtype == PPO_F32 ? 3 : 4) * 148, slices = p.tiles < room ? room / p.tiles : 1;  // one round of scan_bwd_kernel's blocks
     const long long blocks = (long long)d->Be * d->groups * ppo_cdiv(per, 256 / p.NL);
     long long n = bwd ? (d->Be < slices ? 2ll * slices / d->Be : 1) : (blocks < 4 * 148 ? 4 * 148 / blocks : 1);
@@ -1293,7 +1295,7 @@ int with_lanes(const ppo_selective_scan_desc *d, const Plan &p, F &&fn) {
         return fn(t, std::integral_constant<int, 4>{});
     });
 }
-// A pass over the first `segs` segments, `two` channels a thread.
+// A pass over the first `segs` segments, CPT channels a thread.
 template <typename T, int NL, int CPT, int MODE>
 int pass_of(ScanArgs a, int segs, cudaStream_t st) {
     a.group_tiles = ppo_cdiv(a.per, kThreads / NL * CPT);
