@@ -576,7 +576,8 @@ int ppo_selective_scan_step(const ppo_selective_scan_desc *desc, const void *dev
  *   q [rows][heads][d], k [rows][kv_heads][d] of type dtype, ldq and ldk elements from row to row (at least the row's own length), their outputs
  *   in rows of ldqo and ldko; gamma fp32 [d], one of queries and one of keys (NULL: 1); pos int32 [rows]; freq fp64 [pairs], radians a position.
  * Angles in fp64, the rest in fp32: the sum of a head's squares has to be finite there, backwards that of its products with the gradients too, and
- * squares or products below 2^-126 keep fewer bits, below 2^-150 none.  d <= 256, 2 pairs <= d.  With pairs == 0 pos and freq may be NULL.  q_out may be q where ldqo == ldq, and k_out k where ldko == ldk. */
+ * squares or products below 2^-126 keep fewer bits, below 2^-150 none.  d <= 256, 2 pairs <= d.  With pairs == 0 pos and freq may be NULL.  q_out may be q where
+ * ldqo == ldq, and k_out k where ldko == ldk. */
 typedef struct {
     int32_t rows, heads, kv_heads, d, pairs, interleaved, dtype;
     int64_t ldq, ldk, ldqo, ldko;
